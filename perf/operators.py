@@ -299,13 +299,15 @@ def rotate_plain(x, cs, rot, inter):
 
 
 def norm_plain(x, w, eps=1e-6):
-    """x / sqrt(mean(x^2) + eps) * w; the squares are summed by halving, which fixes the order."""
+    """x / sqrt(mean(x^2) + eps) * w.  The order of the sum is fixed: the halves of the row are added,
+    then neighbours until one value is left."""
     x = x.float()
     if w is None:
         return x
     s, d = x * x, x.shape[-1]
-    for _ in range(d.bit_length() - 1):
-        s = s[..., :s.shape[-1] // 2] + s[..., s.shape[-1] // 2:]
+    s = s[..., :d // 2] + s[..., d // 2:]
+    for _ in range((d // 2).bit_length() - 1):
+        s = s[..., 0::2] + s[..., 1::2]
     r = 1.0 / torch.sqrt(s / d + eps)
     return x * r * w.float()
 
