@@ -111,7 +111,7 @@ def quantise(x):
     """fp32 rows [..., D] -> codes (uint8), scale, minimum (bf16)."""
     lo, hi = x.amin(-1), x.amax(-1)
     m = lo.to(torch.bfloat16)
-    s = ((hi - m.float()) / 15.0).to(torch.bfloat16).clamp(min=TINY)
+    s = ((hi - m.float()) * (1.0 / 15.0)).to(torch.bfloat16).clamp(min=TINY)
     inv = 1.0 / s.float()
     c = torch.round((x - m.float()[..., None]) * inv[..., None]).clamp(0, 15).to(torch.uint8)
     return c, s, m
@@ -337,7 +337,7 @@ def run_plan_plain(s):
     take = (j >= held[:, None]) & (j < need[:, None]) & served[:, None]
     src = count - 1 - ((total - want)[:, None] + (j - held[:, None]))
     table = torch.where(take, room[torch.where(take, src, torch.zeros_like(src))], table)
-    count = count - torch.where(served, total, torch.zeros_like(total)).amax()
+    count = count - torch.where(served & (want > 0), total, torch.zeros_like(total)).amax()
     free = torch.where(torch.arange(pool, device="cuda") < count, room[:pool], torch.full_like(free, -1))
     held = torch.where(served, torch.maximum(held, need), held)
     kv = cached + torch.where(served, new, torch.zeros_like(new))
