@@ -95,6 +95,7 @@ typedef enum aasd_verify_mode {
 #define AASD_STATUS_INTERNAL 32u      /* checked builds only (compiled with AASD_BOUNDS_CHECK): an
                                          index computed inside a kernel fell outside its array;
                                          the access was skipped */
+#define AASD_STATUS_KV_FULL 64u       /* aasd_kv_plan: a sequence got no pages for its new tokens */
 
 /* Bits of a draft token's flag byte (Sec. 3.3, last paragraph). */
 #define AASD_FLAG_CONDITIONAL 1u /* from the input context or alignment sampling */
@@ -406,6 +407,173 @@ int aasd_verify_tree(aasd_ctx* ctx, const void* target_logits, const int32_t* no
                      const int32_t* tree_offsets, int32_t n_trees, int64_t n_rows,
                      const aasd_verify_params* params, int32_t emit_stride, void* workspace,
                      size_t workspace_bytes, const aasd_tree_out* out);
+
+/* ---- the cache of a real target model: pages of 64 tokens held in 4 bits ------------------ */
+
+/* (No counterpart in the paper, which runs a library model.)  Between aasd_tree_build and
+ * aasd_verify_tree the target model runs on the draft tokens.  These calls are the part of each
+ * of its layers that deals with draft tokens and the cache:
+ *   aasd_kv_plan    once per step: pages for the new tokens, slot and position of each;
+ *   aasd_kv_write   per layer: head norms and rotation of queries and keys, store of the entries;
+ *   aasd_kv_attend  per layer: attention of the new tokens over the cache, draft trees included;
+ *   aasd_kv_commit  once per step: the accepted path's entries move to consecutive slots;
+ *   aasd_kv_read    entries as values (hand-over to other code, checks).
+ *
+ * Layout.  A layer's cache is a pool of n_pages pages; a page holds AASD_KV_PAGE tokens of all
+ * n_kv_heads key/value heads, one block of aasd_kv_head_bytes(head_dim) bytes per head:
+ *   keys    [64][D/2]  byte i of a token: channel i in the low half, channel i + D/2 in the high one
+ *   values  [D/2][64]  byte t of row i: channels i and i + D/2 of token t
+ *   [64] u32           per token: the keys' scale (bf16, low half) and minimum (bf16, high half)
+ *   [64] u32           the values'
+ * A code c (0..15) stands for scale * c + minimum.  The pool starts on a 16-byte boundary.  A slot
+ * is page * 64 + place in the page.  Token c of sequence b lives in page block_table[b][c / 64].
+ * What lies in a page past a sequence's end is never looked at, whatever it holds.
+ *
+ * Storing a row x of D values (fp32): m = bf16(min x), s = max(bf16((max x - m) * (1/15)), 2^-60),
+ * code = rint((x - m) * (1 / s)) held to 0..15, every operation rounded to nearest in fp32.  A row
+ * with a NaN or infinity (or whose range overflows) is stored as zeros and raises
+ * AASD_STATUS_BAD_ROW.  The cache's bytes are thus a function of the inputs alone.
+ *
+ * New tokens.  The n_new[b] tokens that a sequence runs through the model in this step (one, a
+ * chunk of a prompt, or the nodes of its draft tree) follow its cached_len[b] cached ones: token i
+ * takes cache place cached_len[b] + i.  Their rows in the token arrays are tok_offsets[b] + i
+ * (packed), or b * rows_per_seq + i when rows_per_seq > 0 (padded, as aasd_tree_build lays its
+ * nodes out; rows past n_new[b] are padding). */
+#define AASD_KV_PAGE 64
+
+typedef struct aasd_kv_plan_params {
+    int32_t n_seqs;
+    int32_t n_pages;        /* pages of the pool */
+    int32_t max_pages;      /* width of a block-table row */
+    int32_t rows_per_seq;   /* > 0: padded token rows; 0: packed */
+    int64_t n_tokens;       /* length of slot_map / positions (n_seqs * rows_per_seq when padded) */
+} aasd_kv_plan_params;
+
+typedef struct aasd_kv_plan_state {   /* all read and written */
+    int32_t* block_table;   /* [n_seqs x max_pages] pages of each sequence, NONE past the held ones */
+    int32_t* seq_pages;     /* [n_seqs] pages held */
+    int32_t* free_pages;    /* [n_pages] stack of free pages, NONE above the top */
+    int32_t* n_free;        /* [1] pages on the stack */
+} aasd_kv_plan_state;
+
+typedef struct aasd_kv_plan_out {     /* all required (tok_offsets: NULL allowed when padded) */
+    int32_t* kv_len;        /* [n_seqs] tokens in the cache once the placed ones are stored */
+    int32_t* tok_offsets;   /* [n_seqs+1] first token row of each sequence */
+    int32_t* slot_map;      /* [n_tokens] slot of each token, NONE for padding and unplaced tokens */
+    int32_t* positions;     /* [n_tokens] position of each token, NONE likewise */
+} aasd_kv_plan_out;
+
+/* Brings the page tables in line with cached_len[b] + n_new[b] tokens per sequence (need =
+ * ceil(that / 64) pages).  First every page past its sequence's need goes back on the stack (in
+ * order of sequence, then of place).  Then, sequence by sequence, missing pages come off the top;
+ * a sequence whose pages the stack cannot give any more, or whose need exceeds max_pages, gets
+ * none: its n_new tokens are not placed (slots NONE, kv_len = cached_len) and
+ * AASD_STATUS_KV_FULL is raised; sequences after it that need no page are placed all the same.
+ * Packed tokens past n_tokens are not placed either: the whole sequence is left out the same way.
+ * positions = cached_len + i, or cached_len + node_depth[row] when node_depth (as aasd_tree_build
+ * writes it, one entry per token row) is given.  A sequence that has ended passes 0 and 0 and gives
+ * all its pages back.  Inconsistent books (a held count outside the table, fewer held pages than
+ * cached tokens, page ids outside the pool, a stack that would overflow) raise
+ * AASD_STATUS_BAD_OFFSETS; nothing outside the arrays is touched. */
+int aasd_kv_plan(aasd_ctx* ctx, const int32_t* cached_len, const int32_t* n_new,
+                 const int32_t* node_depth, const aasd_kv_plan_params* params,
+                 const aasd_kv_plan_state* state, const aasd_kv_plan_out* out);
+
+/* Bytes of one head's block of a page: 64 * head_dim + 512.  head_dim is 64, 128 or 256
+ * everywhere (AASD_ERR_UNSUPPORTED otherwise). */
+int aasd_kv_head_bytes(int32_t head_dim, size_t* bytes);
+
+/* aasd_kv_write_params.flags */
+#define AASD_KV_ROPE_INTERLEAVED 1u   /* rotated pairs are (2i, 2i+1) instead of (i, i + rotary_dim/2) */
+
+typedef struct aasd_kv_write_params {
+    int32_t n_q_heads, n_kv_heads, head_dim;
+    int32_t n_pages;
+    int32_t dtype;          /* aasd_dtype of q, k, v, the weights and the outputs */
+    int64_t q_stride, k_stride, v_stride;  /* elements between consecutive tokens (heads are contiguous) */
+    int32_t rotary_dim;     /* channels that are rotated, even, 0..head_dim */
+    int32_t max_positions;  /* rows of cos_sin */
+    float eps;              /* of the norm, >= 0 */
+    uint32_t flags;
+} aasd_kv_write_params;
+
+/* For every token row: q and k heads x (fp32) are normed, x * (1 / sqrt(mean(x^2) + eps)) * weight
+ * (skipped where the weight is NULL; the squares are summed in a fixed order: the row's halves,
+ * then neighbours), and their first rotary_dim channels rotated by row positions[t] of cos_sin
+ * (fp32 [max_positions x rotary_dim]: cosines, then sines): (a, b) -> (a cos - b sin,
+ * b cos + a sin).  q goes to q_out [n_tokens x n_q_heads x D], rounded once; k to k_out likewise
+ * (NULL: not written) and, with v, into the cache at slot_map[t].  A slot of NONE stores nothing.
+ * A position of NONE marks a padding row (zeros to the outputs, nothing stored); one outside the
+ * table, or a slot outside the pool, raises AASD_STATUS_ID_RANGE and counts as NONE.  q and q_out
+ * may be NULL together with n_q_heads = 0, k and v with n_kv_heads = 0.  Two tokens must not share
+ * a slot. */
+int aasd_kv_write(aasd_ctx* ctx, const void* q, const void* k, const void* v,
+                  const void* q_weight, const void* k_weight, const float* cos_sin,
+                  const int32_t* positions, const int32_t* slot_map, int64_t n_tokens,
+                  const aasd_kv_write_params* params, void* pages, void* q_out, void* k_out);
+
+/* Scratch of aasd_kv_attend: partial results of sequences that several CTAs share. */
+int aasd_kv_workspace_bytes(int32_t head_dim, size_t* bytes);
+/* Registers a 256-byte aligned device buffer of at least that size and clears what must start at
+ * zero (asynchronous).  Like the other workspace, it must not be shared by overlapping calls;
+ * aasd_workspace_release forgets it. */
+int aasd_kv_workspace_init(aasd_ctx* ctx, void* workspace, size_t bytes, int32_t head_dim);
+
+typedef struct aasd_kv_attend_params {
+    int32_t n_seqs;
+    int32_t n_q_heads, n_kv_heads, head_dim;   /* n_q_heads a multiple of n_kv_heads */
+    int32_t n_pages, max_pages;
+    int32_t dtype;          /* of q and out */
+    int32_t rows_per_seq;   /* > 0: padded token rows; 0: packed (tok_offsets) */
+    int64_t n_tokens;
+    int64_t q_stride;       /* elements between consecutive tokens of q */
+    float scale;            /* of the products before the softmax; 0 = 1 / sqrt(head_dim) */
+} aasd_kv_attend_params;
+
+typedef struct aasd_kv_attend_out {
+    void* out;              /* [n_tokens x n_q_heads x D] */
+    float* lse;             /* [n_tokens x n_q_heads] ln sum exp of the scaled products, or NULL */
+} aasd_kv_attend_out;
+
+/* Query head h reads key/value head h / (n_q_heads / n_kv_heads).  New token i of a sequence sees
+ * its cached_len[b] cached tokens and, among the new ones (which must have been stored: kv_len[b] -
+ * cached_len[b] of them), tokens 0..i, or with node_parent (one entry per token row, index inside
+ * the sequence, NONE = no parent; parents precede their children) itself and its ancestors.
+ * Sums and the softmax's statistics are fp32; bf16 queries are used as they are, probabilities are
+ * rounded to 11 bits (fp32 queries: both to 22) for the products on the tensor cores; the result is
+ * rounded once.  Rows that see nothing (padding, tokens that were not placed) give zeros and an lse of
+ * -inf.  A page id outside the pool, or a parent that does not precede its child, raises
+ * AASD_STATUS_BAD_OFFSETS; what lies behind it counts as not visible. */
+int aasd_kv_attend(aasd_ctx* ctx, const void* q, const void* pages, const int32_t* block_table,
+                   const int32_t* cached_len, const int32_t* kv_len, const int32_t* tok_offsets,
+                   const int32_t* node_parent, const aasd_kv_attend_params* params, void* workspace,
+                   size_t workspace_bytes, const aasd_kv_attend_out* out);
+
+typedef struct aasd_kv_commit_params {
+    int32_t n_seqs;
+    int32_t n_kv_heads, head_dim;
+    int32_t n_pages, max_pages;
+    int32_t rows_per_seq;   /* > 0: padded node rows; 0: tok_offsets */
+    int32_t n_layers;
+    int64_t layer_stride;   /* bytes between the layers' pools, a multiple of 16 */
+} aasd_kv_commit_params;
+
+/* After aasd_verify_tree: the entries of best_node[b] and its ancestors move, in every layer, to
+ * places cached_len[b] + depth, and new_len[b] = cached_len[b] + the path's length (root included):
+ * the cached_len of the next step.  A best_node of NONE, or one whose token was not placed, leaves
+ * new_len[b] = cached_len[b]; so does a path whose parents do not precede their children or whose
+ * pages are not in the pool (AASD_STATUS_BAD_OFFSETS).  At most AASD_KV_MAX_NODES new tokens per
+ * sequence (more raise that status too).  new_len must not be cached_len. */
+#define AASD_KV_MAX_NODES 4096
+int aasd_kv_commit(aasd_ctx* ctx, void* pages, const int32_t* block_table, const int32_t* cached_len,
+                   const int32_t* kv_len, const int32_t* tok_offsets, const int32_t* best_node,
+                   const int32_t* node_parent, const aasd_kv_commit_params* params, int32_t* new_len);
+
+/* Values scale * code + minimum of the entries at slots[0..n), rounded to dtype: k_out and v_out
+ * [n x n_kv_heads x D] (NULL: not written).  Slots of NONE read as zeros; so do slots outside the
+ * pool, which raise AASD_STATUS_ID_RANGE. */
+int aasd_kv_read(aasd_ctx* ctx, const void* pages, const int32_t* slots, int64_t n, int32_t n_pages,
+                 int32_t n_kv_heads, int32_t head_dim, int32_t dtype, void* k_out, void* v_out);
 
 /* ---- measurement aid ------------------------------------------------------------------ */
 

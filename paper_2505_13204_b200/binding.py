@@ -18,12 +18,15 @@ F32, BF16 = 0, 1
 ALIGN_TOPK, ALIGN_GUMBEL = 0, 1
 VERIFY_CONDITIONAL, VERIFY_STRICT_GREEDY, VERIFY_STRICT_SAMPLED, VERIFY_TOP_K = 0, 1, 2, 3
 STATUS_BAD_ROW, STATUS_ID_RANGE, STATUS_HIST_OVERFLOW, STATUS_BAD_OFFSETS, STATUS_TIMEOUT = 1, 2, 4, 8, 16
-STATUS_INTERNAL = 32
+STATUS_INTERNAL, STATUS_KV_FULL = 32, 64
 FLAG_CONDITIONAL, FLAG_EXTRA = 1, 2
 DRAFT_MATCH_ALIGN = 1
 HINT_FINITE = 1
 STEP_REUSE_DRAFT = 1
 STEP_EXTEND_TABLE = 2
+KV_PAGE = 64
+KV_MAX_NODES = 4096
+KV_ROPE_INTERLEAVED = 1
 ERR_UNSUPPORTED = 7
 
 EXPORTS = [
@@ -32,6 +35,8 @@ EXPORTS = [
     "aasd_workspace_init", "aasd_workspace_release", "aasd_align_sample", "aasd_draft",
     "aasd_verify", "aasd_select", "aasd_append", "aasd_step", "aasd_verify_static",
     "aasd_tree_build", "aasd_verify_tree", "aasd_probe_read", "aasd_debug_withhold_tile",
+    "aasd_kv_plan", "aasd_kv_head_bytes", "aasd_kv_write", "aasd_kv_read", "aasd_kv_commit",
+    "aasd_kv_workspace_bytes", "aasd_kv_workspace_init", "aasd_kv_attend",
 ]
 STATIC_MAX_ROWS = STATIC_MAX_CANDS = 8192
 
@@ -90,6 +95,43 @@ class StepArgs(C.Structure):
                 ("emit_ids", _vp), ("flags", C.c_uint32), ("table_ids", _vp), ("table_n", _vp)]
 
 
+class KvPlanParams(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32),
+                ("rows_per_seq", C.c_int32), ("n_tokens", C.c_int64)]
+
+
+class KvPlanState(C.Structure):
+    _fields_ = [(n, _vp) for n in ("block_table", "seq_pages", "free_pages", "n_free")]
+
+
+class KvPlanOut(C.Structure):
+    _fields_ = [(n, _vp) for n in ("kv_len", "tok_offsets", "slot_map", "positions")]
+
+
+class KvWriteParams(C.Structure):
+    _fields_ = [("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("n_pages", C.c_int32), ("dtype", C.c_int32), ("q_stride", C.c_int64),
+                ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("rotary_dim", C.c_int32),
+                ("max_positions", C.c_int32), ("eps", C.c_float), ("flags", C.c_uint32)]
+
+
+class KvAttendParams(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32),
+                ("dtype", C.c_int32), ("rows_per_seq", C.c_int32), ("n_tokens", C.c_int64),
+                ("q_stride", C.c_int64), ("scale", C.c_float)]
+
+
+class KvAttendOut(C.Structure):
+    _fields_ = [("out", _vp), ("lse", _vp)]
+
+
+class KvCommitParams(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("n_pages", C.c_int32), ("max_pages", C.c_int32), ("rows_per_seq", C.c_int32),
+                ("n_layers", C.c_int32), ("layer_stride", C.c_int64)]
+
+
 class Counters(C.Structure):
     _fields_ = [(n, C.c_uint64) for n in ("rows", "bad_rows", "redo_rows", "near_threshold",
                                           "accepted", "sampler_recheck", "sampler_exact",
@@ -141,6 +183,15 @@ def load_library(path: str | None = None):
     lib.aasd_debug_withhold_tile.argtypes = [_vp, C.c_int64, C.c_int32, C.c_uint32]
     lib.aasd_verify_static.argtypes = [C.c_int, _vp, _vp, _vp, _vp, _vp, C.c_int32, C.c_int64,
                                        C.POINTER(VerifyParams), C.POINTER(VerifyOut), _vp]
+    lib.aasd_kv_plan.argtypes = [_vp, _vp, _vp, _vp, C.POINTER(KvPlanParams), C.POINTER(KvPlanState),
+                                 C.POINTER(KvPlanOut)]
+    lib.aasd_kv_head_bytes.argtypes = [C.c_int32, C.POINTER(C.c_size_t)]
+    lib.aasd_kv_write.argtypes = [_vp] * 9 + [C.c_int64, C.POINTER(KvWriteParams), _vp, _vp, _vp]
+    lib.aasd_kv_read.argtypes = [_vp, _vp, _vp, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _vp, _vp]
+    lib.aasd_kv_commit.argtypes = [_vp] * 8 + [C.POINTER(KvCommitParams), _vp]
+    lib.aasd_kv_workspace_bytes.argtypes = [C.c_int32, C.POINTER(C.c_size_t)]
+    lib.aasd_kv_workspace_init.argtypes = [_vp, _vp, C.c_size_t, C.c_int32]
+    lib.aasd_kv_attend.argtypes = [_vp] * 8 + [C.POINTER(KvAttendParams), _vp, C.c_size_t, C.POINTER(KvAttendOut)]
     if path == _build.LIB:
         _lib = lib
     return lib
@@ -177,6 +228,30 @@ def _dev_i32(x, device):
         assert x.dtype == torch.int32 and x.is_cuda and x.is_contiguous()
         return x
     return torch.as_tensor(x, dtype=torch.int32).to(device)
+
+
+def kv_head_bytes(head_dim: int) -> int:
+    """Bytes of one key/value head's block of a cache page (aasd_kv_head_bytes)."""
+    n = C.c_size_t()
+    _check(load_library().aasd_kv_head_bytes(int(head_dim), C.byref(n)), "aasd_kv_head_bytes")
+    return n.value
+
+
+def kv_pages(n_pages: int, n_kv_heads: int, head_dim: int, layers: int | None = None, device="cuda") -> torch.Tensor:
+    """An empty page pool, uint8 [n_pages, n_kv_heads, head bytes], or one per layer with a
+    leading dimension.  What it holds before it is written does not matter."""
+    shape = (n_pages, n_kv_heads, kv_head_bytes(head_dim))
+    return torch.empty(shape if layers is None else (layers,) + shape, dtype=torch.uint8, device=device)
+
+
+def _kv_dim(pages: torch.Tensor) -> int:
+    """Head dimension of a page pool."""
+    return (pages.shape[-1] - 512) // KV_PAGE
+
+
+def _kv_i32(*tensors):
+    for t in tensors:
+        assert t is None or (t.dtype == torch.int32 and t.is_cuda and t.is_contiguous()), "int32, on the device, contiguous"
 
 
 def verify_static(target_logits, draft_ids, cand_offsets=None, draft_flags=None, alpha=0.1,
@@ -240,6 +315,7 @@ class Context:
         self._h = h
         self._ws = None
         self._ws_rows = self._ws_cands = -1
+        self._kv_ws, self._kv_ws_dim = None, 0
 
     def close(self):
         if self._h:
@@ -454,6 +530,118 @@ class Context:
         """aasd_probe_read: one read-only pass over ``buffer`` (a measurement aid)."""
         n = buffer.numel() * buffer.element_size()
         _check(self.lib.aasd_probe_read(self._h, _p(buffer), n - n % 16, _p(sink)), "aasd_probe_read")
+
+    # ---- the paged 4-bit cache ------------------------------------------------------------
+    def kv_plan(self, cached_len, n_new, block_table, seq_pages, free_pages, n_free, n_tokens,
+                rows_per_seq=0, node_depth=None, outputs=None):
+        """aasd_kv_plan: brings ``block_table`` [B, max_pages], ``seq_pages``, ``free_pages`` and
+        ``n_free`` (all int32, changed in place) in line with ``cached_len + n_new`` tokens per
+        sequence; returns kv_len, tok_offsets, slot_map and positions of the new tokens."""
+        _kv_i32(cached_len, n_new, block_table, seq_pages, free_pages, n_free, node_depth)
+        B, P = block_table.shape
+        dev = block_table.device
+        o = outputs or dict(kv_len=torch.empty(B, dtype=torch.int32, device=dev),
+                            tok_offsets=torch.empty(B + 1, dtype=torch.int32, device=dev),
+                            slot_map=torch.empty(n_tokens, dtype=torch.int32, device=dev),
+                            positions=torch.empty(n_tokens, dtype=torch.int32, device=dev))
+        prm = KvPlanParams(B, free_pages.numel(), P, int(rows_per_seq), int(n_tokens))
+        st = KvPlanState(_p(block_table), _p(seq_pages), _p(free_pages), _p(n_free))
+        out = KvPlanOut(_p(o["kv_len"]), _p(o["tok_offsets"]), _p(o["slot_map"]), _p(o["positions"]))
+        _check(self.lib.aasd_kv_plan(self._h, _p(cached_len), _p(n_new), _p(node_depth), C.byref(prm),
+                                     C.byref(st), C.byref(out)), "aasd_kv_plan")
+        return o
+
+    def kv_write(self, pages, q, k, v, slot_map, positions, cos_sin=None, q_weight=None, k_weight=None,
+                 eps=1e-6, interleaved=False, keep_k=False, outputs=None):
+        """aasd_kv_write: norms and rotates ``q`` [T, Hq, D] and ``k`` [T, Hkv, D] (views into a
+        fused projection are fine: only the heads of a token have to be contiguous), stores k and
+        ``v`` at ``slot_map``.  ``cos_sin``: fp32 [positions, rotary_dim] or None.  Returns a dict
+        with q and, with ``keep_k``, the rotated k."""
+        _kv_i32(slot_map, positions)
+        T, Hq, D = q.shape
+        Hkv = k.shape[1]
+        assert q.stride(2) == 1 and (T == 0 or (q.stride(1) == D and k.stride(1) == D and v.stride(1) == D))
+        assert k.dtype == q.dtype and v.dtype == q.dtype and k.shape == v.shape and k.shape[2] == D and _kv_dim(pages) == D
+        assert pages.dtype == torch.uint8 and pages.is_contiguous() and pages.shape[1] == Hkv
+        assert slot_map.numel() == T and positions.numel() == T
+        for w in (q_weight, k_weight):
+            assert w is None or (w.dtype == q.dtype and w.numel() == D and w.is_contiguous())
+        assert cos_sin is None or (cos_sin.dtype == torch.float32 and cos_sin.is_contiguous())
+        o = outputs or dict(q=torch.empty((T, Hq, D), dtype=q.dtype, device=q.device),
+                            k=torch.empty((T, Hkv, D), dtype=q.dtype, device=q.device) if keep_k else None)
+        prm = KvWriteParams(Hq, Hkv, D, pages.shape[0], _dtype_code(q), q.stride(0), k.stride(0), v.stride(0),
+                            0 if cos_sin is None else cos_sin.shape[1], 0 if cos_sin is None else cos_sin.shape[0],
+                            eps, KV_ROPE_INTERLEAVED if interleaved else 0)
+        _check(self.lib.aasd_kv_write(self._h, _p(q), _p(k), _p(v), _p(q_weight), _p(k_weight), _p(cos_sin),
+                                      _p(positions), _p(slot_map), T, C.byref(prm), _p(pages), _p(o["q"]),
+                                      _p(o.get("k"))), "aasd_kv_write")
+        return o
+
+    def kv_workspace(self, head_dim: int) -> torch.Tensor:
+        """The context's own scratch for ``kv_attend``."""
+        if self._kv_ws is None or head_dim > self._kv_ws_dim:
+            n = C.c_size_t()
+            _check(self.lib.aasd_kv_workspace_bytes(int(head_dim), C.byref(n)), "aasd_kv_workspace_bytes")
+            if self._kv_ws is not None:
+                self.stream.synchronize()
+                self.lib.aasd_workspace_release(self._h, _vp(self._kv_ws.data_ptr()))
+            with torch.cuda.stream(self.stream):
+                ws = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+            _check(self.lib.aasd_kv_workspace_init(self._h, _vp(ws.data_ptr()), n.value, int(head_dim)),
+                   "aasd_kv_workspace_init")
+            self._kv_ws, self._kv_ws_dim = ws, head_dim
+        return self._kv_ws
+
+    def kv_attend(self, q, pages, block_table, cached_len, kv_len, tok_offsets=None, rows_per_seq=0,
+                  node_parent=None, scale=0.0, want_lse=False, outputs=None):
+        """aasd_kv_attend: attention of the new tokens ``q`` [T, Hq, D] over the cache.  Token rows
+        are packed (``tok_offsets``) or padded (``rows_per_seq``); ``node_parent`` makes them draft
+        trees.  Returns a dict with out [T, Hq, D] and, with ``want_lse``, lse [T, Hq]."""
+        _kv_i32(block_table, cached_len, kv_len, tok_offsets, node_parent)
+        T, Hq, D = q.shape
+        B, P = block_table.shape
+        assert q.stride(2) == 1 and (T == 0 or q.stride(1) == D) and _kv_dim(pages) == D
+        assert pages.dtype == torch.uint8 and pages.is_contiguous()
+        o = outputs or dict(out=torch.empty((T, Hq, D), dtype=q.dtype, device=q.device))
+        if want_lse and "lse" not in o:
+            o["lse"] = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
+        prm = KvAttendParams(B, Hq, pages.shape[1], D, pages.shape[0], P, _dtype_code(q), int(rows_per_seq), T,
+                             q.stride(0), scale)
+        out = KvAttendOut(_p(o["out"]), _p(o.get("lse")))
+        ws = self.kv_workspace(D)
+        _check(self.lib.aasd_kv_attend(self._h, _p(q), _p(pages), _p(block_table), _p(cached_len), _p(kv_len),
+                                       _p(tok_offsets), _p(node_parent), C.byref(prm), _p(ws), ws.numel(),
+                                       C.byref(out)), "aasd_kv_attend")
+        return o
+
+    def kv_commit(self, pages, block_table, cached_len, kv_len, best_node, node_parent, tok_offsets=None,
+                  outputs=None):
+        """aasd_kv_commit: moves the accepted paths' entries in the pools of all layers (``pages``
+        [layers, n_pages, Hkv, bytes]) and returns the new cached lengths.  ``node_parent`` is
+        [B, rows_per_seq], or flat with ``tok_offsets``."""
+        _kv_i32(block_table, cached_len, kv_len, best_node, node_parent, tok_offsets)
+        assert pages.dim() == 4 and pages.dtype == torch.uint8 and pages.is_contiguous()
+        B, P = block_table.shape
+        L, N, H, _ = pages.shape
+        new_len = outputs if outputs is not None else torch.empty_like(cached_len)
+        prm = KvCommitParams(B, H, _kv_dim(pages), N, P, 0 if tok_offsets is not None else node_parent.shape[1], L,
+                             pages.stride(0))
+        _check(self.lib.aasd_kv_commit(self._h, _p(pages), _p(block_table), _p(cached_len), _p(kv_len),
+                                       _p(tok_offsets), _p(best_node), _p(node_parent), C.byref(prm), _p(new_len)),
+               "aasd_kv_commit")
+        return new_len
+
+    def kv_read(self, pages, slots, head_dim, dtype=torch.bfloat16, outputs=None):
+        """aasd_kv_read: the entries at ``slots`` as values, k and v [n, Hkv, D].  Several layers at
+        once: pass ``pages.flatten(0, 1)`` and slots raised by layer * n_pages * KV_PAGE."""
+        _kv_i32(slots)
+        assert pages.dim() == 3 and pages.dtype == torch.uint8 and pages.is_contiguous() and _kv_dim(pages) == head_dim
+        n, H = slots.numel(), pages.shape[1]
+        o = outputs or dict(k=torch.empty((n, H, head_dim), dtype=dtype, device=pages.device),
+                            v=torch.empty((n, H, head_dim), dtype=dtype, device=pages.device))
+        _check(self.lib.aasd_kv_read(self._h, _p(pages), _p(slots), n, pages.shape[0], H, int(head_dim),
+                                     _dtype_code(o["k"]), _p(o["k"]), _p(o["v"])), "aasd_kv_read")
+        return o
 
     def select(self, accept_len, next_token, draft_ids, emit_stride, cand_offsets=None,
                rows_per_cand=0, seq_cand_offsets=None, cands_per_seq=0, n_seqs=None):

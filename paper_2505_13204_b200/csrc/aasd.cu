@@ -2,7 +2,6 @@
 // launch geometry.  Every step of the path runs in the kernels of aasd_rows.cuh and
 // aasd_tokens.cuh; nothing here computes on the host.
 #include <cuda_runtime.h>
-#include <nvtx3/nvToolsExt.h>
 
 #include <cstdio>
 #include <cstdlib>
@@ -19,19 +18,6 @@
 using namespace aasd;
 
 namespace {
-// Named range around an entry point, visible to tools that collect NVTX (no cost without one).
-struct TraceRange {
-    explicit TraceRange(const char* name) { nvtxRangePushA(name); }
-    ~TraceRange() { nvtxRangePop(); }
-};
-
-// Two environment switches for measurements and tests, read once per context:
-// AASD_NO_CLUSTER=1 sends the pieces of cut rows through global memory instead of a cluster's
-// shared memory, AASD_STREAM_CHUNKS=n sets the piece count of scarce rows.
-struct Tuning {
-    bool no_cluster;
-    long stream_chunks;   // 0: the library's own choice
-};
 Tuning read_tuning() {
     Tuning t{};
     t.no_cluster = getenv("AASD_NO_CLUSTER") != nullptr;
@@ -43,26 +29,7 @@ Tuning read_tuning() {
 }
 }  // namespace
 
-struct aasd_ctx {
-    int device;
-    cudaStream_t stream;
-    int sm_count;
-    DeviceState* state;
-    uint64_t launches;
-    Tuning tuning;
-    std::map<void*, WorkspaceLayout> workspaces;
-    // testing aid, armed by aasd_debug_withhold_tile and used up by the next streaming launch
-    long long withhold_item = -1;
-    int withhold_tile = 0;
-    unsigned int test_wait_limit = 0;
-};
-
 namespace {
-
-int after_launch(aasd_ctx* ctx, int n) {
-    ctx->launches += (uint64_t)n;
-    return cudaGetLastError() == cudaSuccess ? AASD_OK : AASD_ERR_CUDA;
-}
 
 const WorkspaceLayout* find_workspace(aasd_ctx* ctx, void* ws, size_t bytes, int64_t rows, int64_t cands,
                                       int* err) {
@@ -312,6 +279,7 @@ int aasd_workspace_init(aasd_ctx* ctx, void* workspace, size_t bytes, int64_t ma
 int aasd_workspace_release(aasd_ctx* ctx, void* workspace) {
     if (ctx == nullptr) return AASD_ERR_INVALID_ARG;
     ctx->workspaces.erase(workspace);
+    ctx->kv_workspaces.erase(workspace);
     return AASD_OK;
 }
 

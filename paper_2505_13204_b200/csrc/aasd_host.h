@@ -5,6 +5,7 @@
 #pragma once
 
 #include <cuda_runtime.h>
+#include <nvtx3/nvToolsExt.h>
 
 #include <atomic>
 #include <map>
@@ -154,5 +155,43 @@ int launch_align_gumbel_f32(const LaunchEnv& env, const StreamJob& sj, const Ali
 int launch_align_gumbel_bf16(const LaunchEnv& env, const StreamJob& sj, const AlignArgs& a, unsigned int grid);
 int launch_tree_f32(const LaunchEnv& env, const StreamJob* sj, const TreeArgs& a, unsigned int grid);
 int launch_tree_bf16(const LaunchEnv& env, const StreamJob* sj, const TreeArgs& a, unsigned int grid);
+
+// Named range around an entry point, visible to tools that collect NVTX (no cost without one).
+struct TraceRange {
+    explicit TraceRange(const char* name) { nvtxRangePushA(name); }
+    ~TraceRange() { nvtxRangePop(); }
+};
+
+// Two environment switches for measurements and tests, read once per context:
+// AASD_NO_CLUSTER=1 sends the pieces of cut rows through global memory instead of a cluster's
+// shared memory, AASD_STREAM_CHUNKS=n sets the piece count of scarce rows.
+struct Tuning {
+    bool no_cluster;
+    long stream_chunks;   // 0: the library's own choice
+};
+
+}  // namespace aasd
+
+struct aasd_ctx {
+    int device;
+    cudaStream_t stream;
+    int sm_count;
+    aasd::DeviceState* state;
+    uint64_t launches;
+    aasd::Tuning tuning;
+    std::map<void*, aasd::WorkspaceLayout> workspaces;
+    std::map<void*, int> kv_workspaces;   // head_dim that the scratch of aasd_kv_attend was registered for
+    // testing aid, armed by aasd_debug_withhold_tile and used up by the next streaming launch
+    long long withhold_item = -1;
+    int withhold_tile = 0;
+    unsigned int test_wait_limit = 0;
+};
+
+namespace aasd {
+
+inline int after_launch(aasd_ctx* ctx, int n) {
+    ctx->launches += (uint64_t)n;
+    return cudaGetLastError() == cudaSuccess ? AASD_OK : AASD_ERR_CUDA;
+}
 
 }  // namespace aasd

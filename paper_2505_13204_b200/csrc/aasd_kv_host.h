@@ -1,0 +1,43 @@
+// Host-side internals of the paged 4-bit cache, shared by aasd_kv.cu and aasd_kv_attend.cu.
+#pragma once
+
+#include <initializer_list>
+#include <type_traits>
+
+#include "aasd_host.h"
+#include "aasd_kv.cuh"
+#include "aasd_kv_attend.cuh"
+
+namespace aasd {
+
+// Scratch of the attention kernels.
+struct KvScratch {
+    size_t bytes, zero_bytes;
+};
+constexpr KvScratch kv_attend_scratch(int head_dim) {
+    KvScratch L{};
+    L.zero_bytes = 256;
+    L.bytes = 256;
+    (void)head_dim;
+    return L;
+}
+
+// A launch with a second grid dimension (see launch()).
+template <class... Params, class... Args>
+void launch_grid2(void (*kernel)(Params...), unsigned int gx, unsigned int gy, unsigned int block, cudaStream_t stream, Args&&... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(gx, gy, 1);
+    cfg.blockDim = dim3(block, 1, 1);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.numAttrs = 1;
+    cfg.attrs = attr;
+    cudaLaunchKernelEx(&cfg, kernel, Params(args)...);   // errors surface in cudaGetLastError
+}
+
+int launch_kv_attend_f32(const LaunchEnv& env, int sm_count, const KvAttendArgs& a, void* scratch, int* launches);
+int launch_kv_attend_bf16(const LaunchEnv& env, int sm_count, const KvAttendArgs& a, void* scratch, int* launches);
+
+}  // namespace aasd
