@@ -107,17 +107,21 @@ struct LaunchEnv {
 
 constexpr int kMaxDevices = 64;
 
-// The streaming kernel needs more dynamic shared memory than a kernel gets by default; the
-// attribute is set once per kernel and device, not on every call.
-template <auto Kernel>
-int enable_stream_smem(int device) {
+// A kernel that needs more dynamic shared memory than a kernel gets by default; the attribute
+// is set once per kernel and device, not on every call.
+template <auto Kernel, size_t Bytes>
+int enable_smem(int device) {
     static std::atomic<unsigned long long> done{0ull};
     const unsigned long long bit = 1ull << (device & (kMaxDevices - 1));
     if (done.load(std::memory_order_acquire) & bit) return AASD_OK;
-    if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kStreamSmemBytes) != cudaSuccess)
+    if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Bytes) != cudaSuccess)
         return AASD_ERR_CUDA;
     done.fetch_or(bit, std::memory_order_release);
     return AASD_OK;
+}
+template <auto Kernel>
+int enable_stream_smem(int device) {
+    return enable_smem<Kernel, kStreamSmemBytes>(device);
 }
 
 // One launch of the streaming kernel.  Rows that stream faster than a finisher gets through

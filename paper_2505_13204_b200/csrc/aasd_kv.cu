@@ -208,6 +208,8 @@ int aasd_kv_attend(aasd_ctx* ctx, const void* q, const void* pages, const int32_
     a.node_parent = node_parent;
     a.p = *p;
     a.o = *o;
+    a.q_vec = aligned16(q) && (p->q_stride * es) % 16 == 0;
+    a.out_vec = aligned16(o->out);
     a.scale_log2 = (p->scale > 0.f ? p->scale : 1.0f / sqrtf((float)p->head_dim)) * kLog2e;
     a.state = ctx->state;
     AASD_CUDA(cudaSetDevice(ctx->device));

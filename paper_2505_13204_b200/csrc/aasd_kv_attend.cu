@@ -8,20 +8,41 @@
 
 namespace aasd {
 
+namespace {
+
+template <int DT, int D, int NT>
+int launch_split(const LaunchEnv& env, int sm_count, const KvAttendArgs& a) {
+    constexpr auto kernel = kv_attend_split_kernel<DT, D, NT>;
+    constexpr size_t smem = sizeof(KvSplitShared<D, NT>);
+    static_assert(smem <= 227 * 1024, "fits an SM");
+    if (enable_smem<kernel, smem>(env.device) != AASD_OK) return AASD_ERR_CUDA;
+    launch(kernel, (unsigned int)(sm_count < kKvMaxCtas ? sm_count : kKvMaxCtas), (unsigned int)KvSplitShape<D>::kThreads, smem, env.stream, a);
+    return AASD_OK;
+}
+
+}  // namespace
+
 #if AASD_DT == 0
-int launch_kv_attend_f32(const LaunchEnv& env, int sm_count, const KvAttendArgs& a, void* scratch, int* launches) {
+int launch_kv_attend_f32(const LaunchEnv& env, int sm_count, const KvAttendArgs& args, void* scratch, int* launches) {
 #else
-int launch_kv_attend_bf16(const LaunchEnv& env, int sm_count, const KvAttendArgs& a, void* scratch, int* launches) {
+int launch_kv_attend_bf16(const LaunchEnv& env, int sm_count, const KvAttendArgs& args, void* scratch, int* launches) {
 #endif
     constexpr int DT = AASD_DT;
-    (void)sm_count;
-    (void)scratch;
-    const unsigned int grid = (unsigned int)((a.p.n_tokens * a.p.n_q_heads + 7) / 8);
-    if (a.p.head_dim == 64) launch(kv_attend_kernel<DT, 64>, grid, 256u, 0, env.stream, a);
-    else if (a.p.head_dim == 128) launch(kv_attend_kernel<DT, 128>, grid, 256u, 0, env.stream, a);
-    else launch(kv_attend_kernel<DT, 256>, grid, 256u, 0, env.stream, a);
+    KvAttendArgs a = args;
+    const KvScratch L = kv_attend_scratch(a.p.head_dim);
+    char* ws = static_cast<char*>(scratch);
+    a.tickets = reinterpret_cast<unsigned int*>(ws);
+    a.cta_parts = reinterpret_cast<float*>(ws + L.off_cta);
+    a.warp_parts = reinterpret_cast<float*>(ws + L.off_warp);
+    // rows per key/value head that a sequence brings (packed rows: on average)
+    const int64_t per_seq = a.p.rows_per_seq > 0 ? a.p.rows_per_seq : (a.p.n_tokens + a.p.n_seqs - 1) / (a.p.n_seqs > 0 ? a.p.n_seqs : 1);
+    const int64_t rows = per_seq * (a.p.n_q_heads / a.p.n_kv_heads);
     *launches = 1;
-    return AASD_OK;
+    if (a.p.head_dim == 64)
+        return rows > 8 ? launch_split<DT, 64, 2>(env, sm_count, a) : launch_split<DT, 64, 1>(env, sm_count, a);
+    if (a.p.head_dim == 128)
+        return rows > 8 ? launch_split<DT, 128, 2>(env, sm_count, a) : launch_split<DT, 128, 1>(env, sm_count, a);
+    return launch_split<DT, 256, 1>(env, sm_count, a);
 }
 
 }  // namespace aasd

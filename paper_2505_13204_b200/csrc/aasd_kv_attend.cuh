@@ -1,7 +1,19 @@
 // Attention of a step's new tokens over the paged 4-bit cache.
+//
+// The rows of a key/value head are the queries of its group of query heads for every new token:
+// row = i * G + g for token i and query head h * G + g.  A code c stands for s c + m with the
+// token's own scale and minimum, so
+//     q . k_t     = s_t (q . c_t) + m_t sum(q)
+//     sum p_t v_t = sum (p_t s_t) c_t + sum p_t m_t
+// and the matrix products run on the bare codes.  A code needs no conversion to get there: the
+// 16 bits 0x000c are the fp16 number c 2^-24 and 0x00c0 are c 2^-20 (both exact), so one AND per
+// two codes makes a tensor-core operand, and the powers of two join the factors above.
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include "aasd_kv.cuh"
+#include "aasd_stream.cuh"
 
 namespace aasd {
 
@@ -16,119 +28,786 @@ struct KvAttendArgs {
     aasd_kv_attend_params p;
     aasd_kv_attend_out o;
     float scale_log2;             // scale * log2 e
+    int q_vec, out_vec;           // rows of q / out start on 16-byte boundaries
     DeviceState* state;
+    unsigned int* tickets;        // scratch, zero between calls
+    float* cta_parts;             // scratch: partial results of segments that several CTAs share
+    float* warp_parts;            // scratch: a warp's first piece, when it goes on to another segment
 };
 
-// Where a token row belongs: its sequence and place among the new tokens.
-__device__ __forceinline__ void kv_row_owner(const KvAttendArgs& a, int64_t t, int& b, int64_t& i) {
+constexpr int kKvMaxCtas = 160;        // CTAs of a launch (one per SM)
+constexpr float kKvNothing = -1.0e30f; // running maximum of a row that has seen nothing
+constexpr float kKvHidden = -2.0e30f;  // exponent of a key that the row does not see
+
+// ---- what there is to do ---------------------------------------------------------------------------
+
+struct KvSeq {
+    int cached, fresh;        // cached tokens; new tokens in the cache
+    int first;                // token row of the first new one
+    int rows;                 // token rows, padding included
+    int pages;                // pages that hold them
+    int tiles;                // row tiles of a key/value head
+};
+
+// tile_rows: rows of a tile
+__device__ __forceinline__ KvSeq kv_load_seq(const KvAttendArgs& a, int b, int tile_rows) {
+    KvSeq s;
+    s.cached = a.cached_len[b];
+    const long long fresh = (long long)a.kv_len[b] - s.cached;
+    long long first, rows;
     if (a.p.rows_per_seq > 0) {
-        b = (int)(t / a.p.rows_per_seq);
-        i = t - (int64_t)b * a.p.rows_per_seq;
-        return;
+        first = (long long)b * a.p.rows_per_seq;
+        rows = a.p.rows_per_seq;
+    } else {
+        first = a.tok_offsets[b];
+        rows = (long long)a.tok_offsets[b + 1] - first;
     }
-    int lo = 0, hi = a.p.n_seqs;
-    if (t < a.tok_offsets[0] || t >= a.tok_offsets[hi]) {
-        b = -1;
-        i = 0;
-        return;
-    }
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.tok_offsets[mid] <= t) lo = mid;
-        else hi = mid;
-    }
-    b = lo;
-    i = t - a.tok_offsets[lo];
+    const bool inside = first >= 0 && rows >= 0 && first + rows <= a.p.n_tokens;
+    s.first = inside ? (int)first : 0;
+    s.rows = inside ? (int)rows : 0;
+    s.fresh = s.cached < 0 || fresh < 0 ? 0 : (int)(fresh < s.rows ? fresh : s.rows);
+    const long long pages = ((long long)s.cached + s.fresh + kPage - 1) / kPage;
+    s.pages = s.fresh == 0 ? 0 : (int)(pages < a.p.max_pages ? pages : a.p.max_pages);
+    const long long n = (long long)s.fresh * (a.p.n_q_heads / a.p.n_kv_heads);
+    s.tiles = (int)((n + tile_rows - 1) / tile_rows);
+    return s;
+}
+// Units of work (one page of one head for one row tile) of a sequence.
+__device__ __forceinline__ long long kv_units(const KvAttendArgs& a, const KvSeq& s) {
+    return (long long)s.pages * s.tiles * a.p.n_kv_heads;
 }
 
-// One warp per (token row, query head), one key after the other.
-template <int DT, int D>
-__global__ void __launch_bounds__(256) kv_attend_kernel(const KvAttendArgs a) {
-    constexpr int H = D / 2, C = H / 32;   // a lane's pairs: channels lane + 32 c and H + lane + 32 c
-    pdl_launch_dependents();
-    pdl_wait();
-    const int lane = threadIdx.x & 31;
-    const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 5;
-    if (row >= a.p.n_tokens * a.p.n_q_heads) return;
-    const int64_t t = row / a.p.n_q_heads;
-    const int h = (int)(row - t * a.p.n_q_heads);
-    const int head = h / (a.p.n_q_heads / a.p.n_kv_heads);
-    int b;
-    int64_t i;
-    kv_row_owner(a, t, b, i);
-    float qx[C], qy[C], ox[C], oy[C];
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        qx[c] = Elt<DT>::load(a.q, t * a.p.q_stride + (int64_t)h * D + lane + 32 * c);
-        qy[c] = Elt<DT>::load(a.q, t * a.p.q_stride + (int64_t)h * D + H + lane + 32 * c);
-        ox[c] = oy[c] = 0.f;
+// A place in the list of all units: sequence by sequence, head by head, tile by tile, page by page.
+struct KvCursor {
+    int b, h, tile, pg;
+    KvSeq s;
+    __device__ __forceinline__ void seek(const KvAttendArgs& a, int b_, const KvSeq& s_, long long rem) {
+        b = b_;
+        s = s_;
+        const long long seg = rem / s.pages;
+        pg = (int)(rem - seg * s.pages);
+        h = (int)(seg / s.tiles);
+        tile = (int)(seg - (long long)h * s.tiles);
     }
-    float m = -CUDART_INF_F, l = 0.f;
-    auto visit = [&](int64_t at) {
-        const int64_t pg = at / kPage;
-        const int page = pg < a.p.max_pages ? a.block_table[(int64_t)b * a.p.max_pages + pg] : -1;
-        if (page < 0 || page >= a.p.n_pages) {
+    __device__ __forceinline__ void next(const KvAttendArgs& a, int tile_rows) {
+        if (++pg < s.pages) return;
+        pg = 0;
+        if (++tile < s.tiles) return;
+        tile = 0;
+        if (++h < a.p.n_kv_heads) return;
+        h = 0;
+        do {
+            if (++b >= a.p.n_seqs) return;   // (past the last unit: never looked at)
+            s = kv_load_seq(a, b, tile_rows);
+        } while (s.pages == 0 || s.tiles == 0);
+    }
+    // Block of the current unit, or NULL (the table's entry is not a page).
+    __device__ __forceinline__ const uint8_t* block(const KvAttendArgs& a, int head_bytes) const {
+        const int page = a.block_table[(long long)b * a.p.max_pages + pg];
+        if (page < 0 || page >= a.p.n_pages) return nullptr;
+        return a.pages + ((long long)page * a.p.n_kv_heads + h) * head_bytes;
+    }
+};
+
+// Bit j of the result: new token (64 pg + j - cached) of the sequence's tokens, or a cached one at
+// that place, is seen by new token i.
+__device__ __forceinline__ u64 kv_seen(const KvAttendArgs& a, const KvSeq& s, int pg, int i) {
+    const long long at = (long long)pg * kPage;
+    if (i >= s.fresh) return 0ull;
+    const long long before = s.cached - at;                       // cached tokens of this page
+    u64 seen = before >= kPage ? ~0ull : before <= 0 ? 0ull : (1ull << before) - 1ull;
+    if (a.node_parent == nullptr) {
+        const long long upto = (long long)s.cached + i + 1 - at;  // causal
+        return upto >= kPage ? ~0ull : upto <= 0 ? 0ull : (1ull << upto) - 1ull;
+    }
+    int x = i;
+    while (x >= 0) {
+        const long long j = (long long)s.cached + x - at;
+        if (j < 0) break;                                         // ancestors only get smaller
+        if (j < kPage) seen |= 1ull << j;
+        const int p = a.node_parent[s.first + x];
+        if (p >= x || p < AASD_NONE) {
             raise(a.state, AASD_STATUS_BAD_OFFSETS);
-            return;
+            break;
         }
-        const uint8_t* block = a.pages + ((int64_t)page * a.p.n_kv_heads + head) * kv_head_bytes(D);
-        const int off = (int)(at % kPage);
-        const unsigned int km = reinterpret_cast<const unsigned int*>(block + kv_key_meta_offset(D))[off];
-        const unsigned int vm = reinterpret_cast<const unsigned int*>(block + kv_value_meta_offset(D))[off];
-        float s = 0.f;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const unsigned int w = block[off * H + lane + 32 * c];
-            s += qx[c] * (meta_scale(km) * (float)(w & 15u) + meta_min(km)) + qy[c] * (meta_scale(km) * (float)(w >> 4) + meta_min(km));
+        x = p;
+    }
+    return seen;
+}
+
+// ---- tensor-core and packing primitives --------------------------------------------------------------
+
+__device__ __forceinline__ void mma_16816(float (&c)[4], unsigned int a0, unsigned int a1, unsigned int a2, unsigned int a3,
+                                          unsigned int b0, unsigned int b1) {
+    asm(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ unsigned int transpose_8x8(unsigned int x) {
+    unsigned int y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ unsigned int pack_half(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const unsigned int*>(&h);
+}
+// What rounding to fp16 left out of a and b.
+__device__ __forceinline__ unsigned int pack_rest(float a, float b, unsigned int h) {
+    const float2 r = __half22float2(*reinterpret_cast<const __half2*>(&h));
+    return pack_half(a - r.x, b - r.y);
+}
+// Two codes of a word as fp16 numbers: those in bits 0-3 and 16-19 (HIGH = false) or 4-7 and 20-23.
+// CENTRED = false: c 2^-24, or c 2^-20 for the high ones.  CENTRED: c - 8, one operation more, for
+// fp32 queries: sums of c itself are several times the result that is left when the minimum's part
+// is added, and fp32 results would show it.
+template <bool CENTRED, bool HIGH>
+__device__ __forceinline__ unsigned int codes(unsigned int w) {
+    constexpr unsigned int mask = HIGH ? 0x00F000F0u : 0x000F000Fu;
+    if constexpr (!CENTRED) {
+        return w & mask;
+    } else {
+        const unsigned int b = (w & mask) | 0x64006400u;            // 1024 + c, or 1024 + 16 c
+        __half2 h = *reinterpret_cast<const __half2*>(&b);
+        h = HIGH ? __hfma2(h, __float2half2_rn(0.0625f), __float2half2_rn(-72.f)) : __hsub2(h, __float2half2_rn(1032.f));
+        return *reinterpret_cast<const unsigned int*>(&h);
+    }
+}
+__device__ __forceinline__ float pow2f(int e) { return __uint_as_float((unsigned int)(e + 127) << 23); }   // -126 <= e <= 127
+
+template <int DT>
+__device__ __forceinline__ void store4(void* base, long long i, float4 x, bool vec) {
+    if constexpr (DT == AASD_F32) {
+        float* p = static_cast<float*>(base) + i;
+        if (vec) *reinterpret_cast<float4*>(p) = x;
+        else { p[0] = x.x; p[1] = x.y; p[2] = x.z; p[3] = x.w; }
+    } else {
+        __nv_bfloat16* p = static_cast<__nv_bfloat16*>(base) + i;
+        if (vec) *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+        else {
+            p[0] = __float2bfloat16_rn(x.x);
+            p[1] = __float2bfloat16_rn(x.y);
+            p[2] = __float2bfloat16_rn(x.z);
+            p[3] = __float2bfloat16_rn(x.w);
         }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-        s *= a.scale_log2;
-        const float nm = fmaxf(m, s);
-        const float keep = exp2f(m - nm), p = exp2f(s - nm);
-        m = nm;
-        l = l * keep + p;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const unsigned int w = block[kv_value_offset(D) + (lane + 32 * c) * kPage + off];
-            ox[c] = ox[c] * keep + p * (meta_scale(vm) * (float)(w & 15u) + meta_min(vm));
-            oy[c] = oy[c] * keep + p * (meta_scale(vm) * (float)(w >> 4) + meta_min(vm));
+    }
+}
+
+// ---- rows that see nothing ---------------------------------------------------------------------------
+
+// Zeros (and an lse of -inf) for the token rows that hold no placed token; the warps of the whole
+// grid share the sequences.  Rows outside every sequence's range count as rows past the last one.
+template <int DT>
+__device__ __forceinline__ void kv_clear_rows(const KvAttendArgs& a, int D, int warp, int warps) {
+    const int lane = threadIdx.x & 31;
+    const int Hq = a.p.n_q_heads;
+    for (int b = warp; b <= a.p.n_seqs; b += warps) {
+        long long lo, hi;
+        if (b < a.p.n_seqs) {
+            const KvSeq s = kv_load_seq(a, b, 8);
+            lo = (long long)s.first + s.fresh;
+            hi = (long long)s.first + s.rows;
+        } else {
+            lo = a.p.rows_per_seq > 0 ? a.p.n_tokens : a.p.n_seqs > 0 ? a.tok_offsets[a.p.n_seqs] : 0;
+            lo = lo < 0 ? 0 : lo;
+            hi = a.p.n_tokens;
         }
-    };
-    if (b >= 0) {
-        const int cached = a.cached_len[b];
-        const int64_t fresh = (int64_t)a.kv_len[b] - cached;
-        if (i < fresh) {
-            for (int64_t at = 0; at < cached; ++at) visit(at);
-            if (a.node_parent == nullptr) {
-                for (int64_t j = 0; j <= i; ++j) visit(cached + j);
-            } else {
-                int64_t x = i;
-                while (x >= 0) {
-                    visit(cached + x);
-                    const int p = a.node_parent[t - i + x];
-                    if (p >= x || p < AASD_NONE) {
-                        raise(a.state, AASD_STATUS_BAD_OFFSETS);
-                        break;
-                    }
-                    x = p;
+        const long long e0 = lo * Hq * D, e1 = hi * Hq * D;
+        for (long long e = e0 + lane * 4; e < e1; e += 128) store4<DT>(a.o.out, e, make_float4(0.f, 0.f, 0.f, 0.f), a.out_vec);
+        if (a.o.lse)
+            for (long long e = lo * Hq + lane; e < hi * Hq; e += 32) a.o.lse[e] = -CUDART_INF_F;
+    }
+}
+
+// ---- few rows per head: the keys split over all warps -----------------------------------------------
+
+// W warps per CTA, each with a ring of S blocks of its own that lane 0 fills with one bulk copy per
+// block; S blocks per warp keep 70 to 200 KB per SM in flight (memory wants about 40).
+template <int D>
+struct KvSplitShape {
+    static constexpr int W = D == 256 ? 4 : 8;
+    static constexpr int S = D == 64 ? 5 : 3;
+    static constexpr int kBlock = kv_head_bytes(D);
+    static constexpr int kThreads = W * 32;
+};
+
+// A partial result: the part of a segment (one row tile of one head of one sequence) whose pages
+// one warp, or one CTA, has been through.  Rows are padded by four floats in shared memory so that
+// a warp's stores meet every bank once.
+struct KvPiece {
+    long long seg;      // first unit of the segment, -1: no piece
+    int pages;          // units of the segment
+    int h, row0, n;     // head, first row of the tile, rows in use
+    int first;          // token row of the sequence's first new token
+};
+
+template <int D, int NT>
+struct KvSplitShared {
+    using Sh = KvSplitShape<D>;
+    static constexpr int R = 8 * NT;
+    alignas(128) unsigned char ring[Sh::W][Sh::S][Sh::kBlock];
+    long long base[Sh::kThreads + 1];
+    long long scan[Sh::W];
+    KvPiece piece[2 * Sh::W];
+    float m[2 * Sh::W][R], l[2 * Sh::W][R];
+    u64 full[Sh::W][Sh::S];
+    int abort_flag, last;
+};
+
+// DT: type of the queries.  bf16 values fit an fp16 number scaled by the row's own power of two;
+// fp32 queries and their probabilities travel as two fp16 numbers each (22 bits).
+// NT: row tiles of eight that share the codes of a page.
+template <int DT, int D, int NT>
+__global__ void __launch_bounds__(KvSplitShape<D>::kThreads, 1) kv_attend_split_kernel(const KvAttendArgs a) {
+    using Sh = KvSplitShape<D>;
+    using Shared = KvSplitShared<D, NT>;
+    constexpr int W = Sh::W, S = Sh::S, R = 8 * NT, H = D / 2, TS = D + 4;
+    constexpr int NP = DT == AASD_F32 ? 2 : 1;      // fp16 numbers per query element and probability
+    constexpr bool CEN = NP == 2;                   // codes are centred (see codes())
+    constexpr int kC = CEN ? 0 : 24;                // the operands hold the codes times 2^-kC
+    constexpr float kHigh = CEN ? 1.f : 0.0625f;    // undoes the high codes' factor
+    constexpr int KW = H / 16;                      // words of a token's keys per lane
+    constexpr int MQ = H / 16;                      // channel tiles of each half
+    // Probabilities are scaled to at most 2^kP before they are rounded to fp16, so that small ones
+    // keep their bits; the running maximum may lag by 2^kLazy before everything is rescaled.
+    constexpr float kLazy = DT == AASD_F32 ? 0.f : 4.f;
+    constexpr int kP = DT == AASD_F32 ? 14 : 10;
+    static_assert(R * TS * 4 + R * kKvMaxCtas * 4 <= S * Sh::kBlock, "a piece and the weights of a join fit a warp's ring");
+    extern __shared__ __align__(128) unsigned char smem_raw[];
+    Shared& sh = *reinterpret_cast<Shared*>(smem_raw);
+    pdl_launch_dependents();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int g = lane >> 2, j = lane & 3;
+    if (tid == 0) {
+        for (int i = 0; i < W * S; ++i) mbar_init(&sh.full[0][0] + i, 1);
+        sh.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (tid < 2 * W) sh.piece[tid].seg = -1;
+    pdl_wait();
+    const int B = a.p.n_seqs, G = a.p.n_q_heads / a.p.n_kv_heads;
+    // every thread adds up the units of its strip of sequences
+    const int strip = (B + Sh::kThreads - 1) / Sh::kThreads;
+    long long mine = 0;
+    for (int b = tid * strip; b < min(B, (tid + 1) * strip); ++b) {
+        const KvSeq s = kv_load_seq(a, b, R);
+        mine += kv_units(a, s);
+        if (s.fresh > 0 && (long long)s.cached + s.fresh > (long long)a.p.max_pages * kPage) raise(a.state, AASD_STATUS_BAD_OFFSETS);
+    }
+    long long total;
+    const long long before = block_scan<Sh::kThreads>(mine, sh.scan, total);
+    sh.base[tid] = before;
+    __syncthreads();
+    // CTAs at work: as many as leave every warp a page
+    long long active = (total + W - 1) / W;
+    active = active > gridDim.x ? gridDim.x : active;
+    const long long c = blockIdx.x;
+    const bool works = c < active;
+    const long long u0 = works ? total * (c * W + warp) / (active * W) : 0;
+    const long long u1 = works ? total * (c * W + warp + 1) / (active * W) : 0;
+    volatile int* abort_flag = &sh.abort_flag;
+    u64* full = sh.full[warp];
+
+    if (u0 < u1) {
+        KvCursor at, ahead;
+        {
+            int lo = 0, hi = Sh::kThreads;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (sh.base[mid] <= u0) lo = mid;
+                else hi = mid;
+            }
+            long long rem = u0 - sh.base[lo];
+            int b = lo * strip;
+            KvSeq s = kv_load_seq(a, b, R);
+            while (rem >= kv_units(a, s)) {
+                rem -= kv_units(a, s);
+                s = kv_load_seq(a, ++b, R);
+            }
+            at.seek(a, b, s, rem);
+        }
+        ahead = at;
+        unsigned int missing = 0;   // bit s: stage s holds no block (the table names no page)
+        auto issue = [&](int stage) {
+            const uint8_t* src = ahead.block(a, Sh::kBlock);
+            missing = (missing & ~(1u << stage)) | (src == nullptr ? 1u << stage : 0u);
+            if (lane == 0) {
+                if (src == nullptr) {
+                    raise(a.state, AASD_STATUS_BAD_OFFSETS);
+                    mbar_arrive(&full[stage]);
+                } else {
+                    mbar_arrive_expect_tx(&full[stage], Sh::kBlock);
+                    bulk_copy_g2s(sh.ring[warp][stage], src, Sh::kBlock, &full[stage]);
                 }
             }
-        }
-    }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+            ahead.next(a, R);
+        };
+        long long issued = u0;
+        for (int s = 0; s < S && issued < u1; ++s, ++issued) issue(s);
+
+        unsigned int qf[NP][NT][D / 16][2];   // query operands
+        float rfac[NT][2], qsum[NT][2];       // per column: what scales the codes' products, and the sum of q, in base 2
+        float mref[NT][2], l[NT][2], mv[NT][2];
+        float oacc[NT][2][MQ][4];             // [tile][half][channel tile][fragment]
+        int ev = 0;                           // exponent field that the probabilities are scaled by
+        bool fresh_segment = true;
+        int stage = 0;
+        unsigned int phase = 0;
+
+        for (long long u = u0; u < u1; ++u) {
+            if (fresh_segment) {
+                fresh_segment = false;
+                ev = 64;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int64_t at = row * D + lane + 32 * c;
-        if (DT == AASD_F32) {
-            static_cast<float*>(a.o.out)[at] = ox[c] * inv;
-            static_cast<float*>(a.o.out)[at + H] = oy[c] * inv;
-        } else {
-            static_cast<__nv_bfloat16*>(a.o.out)[at] = __float2bfloat16_rn(ox[c] * inv);
-            static_cast<__nv_bfloat16*>(a.o.out)[at + H] = __float2bfloat16_rn(oy[c] * inv);
+                for (int nt = 0; nt < NT; ++nt) {
+                    // lane (g, j): row 8 nt + g, channels (H / 4) j .. of each half
+                    const long long row = (long long)at.tile * R + 8 * nt + g;
+                    const bool valid = row < (long long)at.s.fresh * G;
+                    const long long tok = at.s.first + (valid ? row / G : 0);
+                    const long long q0 = tok * a.p.q_stride + (long long)(at.h * G + (valid ? row % G : 0)) * D + (H / 4) * j;
+                    float top = 0.f, sum = 0.f;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+#pragma unroll
+                        for (int k = 0; k < H / 4; k += 8) {
+                            float x[8];
+                            if (a.q_vec) load8<DT, true>(a.q, q0 + half * H + k, x);
+                            else load8<DT, false>(a.q, q0 + half * H + k, x);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                top = fmaxf(top, fabsf(x[e]));
+                                sum += x[e];
+                            }
+                        }
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+                    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
+                    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
+                    // the row's largest element becomes 2^14 .. 2^15
+                    int e = (int)(__float_as_uint(top) >> 23) - 127;
+                    e = e < -100 ? -100 : e > 100 ? 100 : e;
+                    const float up = pow2f(14 - e);
+#pragma unroll
+                    for (int k = 0; k < H / 4; k += 8) {
+                        float x[2][8];
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            if (a.q_vec) load8<DT, true>(a.q, q0 + half * H + k, x[half]);
+                            else load8<DT, false>(a.q, q0 + half * H + k, x[half]);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) x[half][i] = valid ? x[half][i] * (half ? up * kHigh : up) : 0.f;
+                        }
+#pragma unroll
+                        for (int w = 0; w < 2; ++w)
+#pragma unroll
+                            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                                for (int r = 0; r < 2; ++r) {
+                                    const float p = x[half][4 * w + r], q = x[half][4 * w + r + 2];
+                                    const unsigned int hi = pack_half(p, q);
+                                    const int ks = 2 * (k / 4 + w) + half;
+                                    qf[0][nt][ks][r] = hi;
+                                    if (NP == 2) qf[NP - 1][nt][ks][r] = pack_rest(p, q, hi);
+                                }
+                    }
+                    const float rf = a.scale_log2 * pow2f(e + kC - 14);   // of the codes and of the row
+                    sum *= a.scale_log2;
+#pragma unroll
+                    for (int col = 0; col < 2; ++col) {
+                        rfac[nt][col] = __shfl_sync(0xFFFFFFFFu, rf, (2 * j + col) * 4);
+                        qsum[nt][col] = __shfl_sync(0xFFFFFFFFu, sum, (2 * j + col) * 4);
+                        mref[nt][col] = kKvNothing;
+                        l[nt][col] = mv[nt][col] = 0.f;
+                    }
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+#pragma unroll
+                        for (int q = 0; q < MQ; ++q)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) oacc[nt][half][q][i] = 0.f;
+                }
+            }
+            if (!mbar_wait(&full[stage], phase, abort_flag, kWaitLimit)) {
+                give_up(abort_flag, a.state);
+                break;
+            }
+            if (!(missing & (1u << stage))) {
+                const unsigned char* st = sh.ring[warp][stage];
+                // S^T: tokens are the rows of the product, queries its columns.  Row g (and g + 8) of token
+                // tile mt is token 16 (g / 2) + 4 mt + 2 (g % 2) (and the next): the order in which a lane
+                // finds the values of its tokens in 16 consecutive bytes below.
+                const int t0 = 16 * (g >> 1) + 2 * (g & 1);
+                float x[NT][4][4];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[nt][mt][i] = 0.f;
+                // (the token tiles take turns, so that products into the same registers stand apart)
+                constexpr int KB = KW < 4 ? KW : 4;   // words fetched at a time
+#pragma unroll
+                for (int wb = 0; wb < KW; wb += KB) {
+                    unsigned int k0[4][KB], k1[4][KB];
+#pragma unroll
+                    for (int mt = 0; mt < 4; ++mt) {
+                        const unsigned char* kp = st + (t0 + 4 * mt) * H + (H / 4) * j + 4 * wb;
+                        if constexpr (KB == 2) {
+                            const uint2 p = *reinterpret_cast<const uint2*>(kp), q = *reinterpret_cast<const uint2*>(kp + H);
+                            k0[mt][0] = p.x; k0[mt][1] = p.y; k1[mt][0] = q.x; k1[mt][1] = q.y;
+                        } else {
+                            const uint4 p = lds16(kp), q = lds16(kp + H);
+                            k0[mt][0] = p.x; k0[mt][1] = p.y; k0[mt][2] = p.z; k0[mt][3] = p.w;
+                            k1[mt][0] = q.x; k1[mt][1] = q.y; k1[mt][2] = q.z; k1[mt][3] = q.w;
+                        }
+                    }
+#pragma unroll
+                    for (int w = 0; w < KB; ++w)
+#pragma unroll
+                        for (int half = 0; half < 2; ++half)
+#pragma unroll
+                            for (int mt = 0; mt < 4; ++mt) {
+                                const unsigned int a0 = half ? codes<CEN, true>(k0[mt][w]) : codes<CEN, false>(k0[mt][w]);
+                                const unsigned int a1 = half ? codes<CEN, true>(k1[mt][w]) : codes<CEN, false>(k1[mt][w]);
+                                const unsigned int a2 = half ? codes<CEN, true>(k0[mt][w] >> 8) : codes<CEN, false>(k0[mt][w] >> 8);
+                                const unsigned int a3 = half ? codes<CEN, true>(k1[mt][w] >> 8) : codes<CEN, false>(k1[mt][w] >> 8);
+                                const int ks = 2 * (wb + w) + half;
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                    for (int np = 0; np < NP; ++np) mma_16816(x[nt][mt], a0, a1, a2, a3, qf[np][nt][ks][0], qf[np][nt][ks][1]);
+                            }
+                }
+                // scales, masks, running maximum
+                uint2 vm[4];
+                const bool masked = (long long)(at.pg + 1) * kPage > at.s.cached;
+                const int live = (int)min((long long)kPage, (long long)at.s.cached + at.s.fresh - (long long)at.pg * kPage);
+                float mx[NT][2];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mx[nt][0] = mx[nt][1] = kKvHidden;
+                unsigned int vmax = 0;
+#pragma unroll
+                for (int mt = 0; mt < 4; ++mt) {
+                    const int t = t0 + 4 * mt;
+                    uint2 km = *reinterpret_cast<const uint2*>(st + kv_key_meta_offset(D) + 4 * t);
+                    vm[mt] = *reinterpret_cast<const uint2*>(st + kv_value_meta_offset(D) + 4 * t);
+                    if (masked) {   // places past the end hold anything
+                        if (t >= live) km.x = vm[mt].x = 0;
+                        if (t + 1 >= live) km.y = vm[mt].y = 0;
+                    }
+                    vmax = max(vmax, max(vm[mt].x & 0xFFFFu, vm[mt].y & 0xFFFFu));
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const unsigned int m = i < 2 ? km.x : km.y;
+                            const float mn = CEN ? fmaf(8.f, meta_scale(m), meta_min(m)) : meta_min(m);
+                            x[nt][mt][i] = fmaf(meta_scale(m), x[nt][mt][i] * rfac[nt][i & 1], mn * qsum[nt][i & 1]);
+                        }
+                }
+                if (masked) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int col = 0; col < 2; ++col) {
+                            const long long row = (long long)at.tile * R + 8 * nt + 2 * j + col;
+                            const u64 seen = kv_seen(a, at.s, at.pg, (int)(row / G));
+#pragma unroll
+                            for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+                                for (int f = 0; f < 2; ++f)
+                                    if (!((seen >> (t0 + 4 * mt + f)) & 1ull)) x[nt][mt][2 * f + col] = kKvHidden;
+                        }
+                }
+                bool grow = false;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int col = 0; col < 2; ++col) {
+                        float m = kKvHidden;
+#pragma unroll
+                        for (int mt = 0; mt < 4; ++mt) m = fmaxf(m, fmaxf(x[nt][mt][col], x[nt][mt][2 + col]));
+                        m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 4));
+                        m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
+                        m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
+                        mx[nt][col] = m;
+                        grow = grow || m > mref[nt][col] + kLazy;
+                    }
+                const int ep = (int)(__reduce_max_sync(0xFFFFFFFFu, vmax) >> 7);   // exponent field of the largest value scale
+                if (__any_sync(0xFFFFFFFFu, grow || ep > ev)) {
+                    const int en = max(ev, min(ep, 250));
+                    const float shift = en - ev > 126 ? 0.f : pow2f(ev - en);
+                    ev = en;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int col = 0; col < 2; ++col) {
+                            const float mn = fmaxf(mref[nt][col], mx[nt][col]);
+                            const float f = ex2_approx(mref[nt][col] - mn);
+                            mref[nt][col] = mn;
+                            l[nt][col] *= f;
+                            mv[nt][col] *= f;
+#pragma unroll
+                            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                                for (int q = 0; q < MQ; ++q) {
+                                    oacc[nt][half][q][col] *= f * shift;
+                                    oacc[nt][half][q][2 + col] *= f * shift;
+                                }
+                        }
+                }
+                const float vup = pow2f(kP - (ev - 127));
+                // probabilities, as the second operand of the next product
+                unsigned int pb[NP][NT][4][2];
+#pragma unroll
+                for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+                    for (int f = 0; f < 2; ++f) {
+                        const unsigned int m = f ? vm[mt].y : vm[mt].x;
+                        const float sv = meta_scale(m) * vup, mn = CEN ? fmaf(8.f, meta_scale(m), meta_min(m)) : meta_min(m);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            float p[2];
+#pragma unroll
+                            for (int col = 0; col < 2; ++col) {
+                                p[col] = ex2_approx(x[nt][mt][2 * f + col] - mref[nt][col]);
+                                l[nt][col] += p[col];
+                                mv[nt][col] = fmaf(p[col], mn, mv[nt][col]);
+                                p[col] *= sv;
+                            }
+                            const unsigned int hi = pack_half(p[0], p[1]);
+                            pb[0][nt][mt][f] = transpose_8x8(hi);
+                            if (NP == 2) pb[NP - 1][nt][mt][f] = transpose_8x8(pack_rest(p[0], p[1], hi));
+                        }
+                    }
+                // O^T: channels are the rows; a lane's 16 bytes of a channel are its tokens in order
+#pragma unroll
+                for (int qb = 0; qb < MQ; qb += 2) {
+                    unsigned int w0[2][4], w1[2][4];
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const unsigned char* vp = st + kv_value_offset(D) + (16 * (qb + q) + g) * kPage + 16 * j;
+                        const uint4 v0 = lds16(vp), v1 = lds16(vp + 8 * kPage);
+                        w0[q][0] = v0.x; w0[q][1] = v0.y; w0[q][2] = v0.z; w0[q][3] = v0.w;
+                        w1[q][0] = v1.x; w1[q][1] = v1.y; w1[q][2] = v1.z; w1[q][3] = v1.w;
+                    }
+                    float part[NP == 2 ? NT : 1][2][2][4];
+                    if (NP == 2) {   // fp32: a page's sum is added in full precision
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) part[nt][0][0][i] = part[nt][0][1][i] = part[nt][1][0][i] = part[nt][1][1][i] = 0.f;
+                    }
+#pragma unroll
+                    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                        for (int q = 0; q < 2; ++q)
+#pragma unroll
+                            for (int half = 0; half < 2; ++half) {
+                                const unsigned int a0 = half ? codes<CEN, true>(w0[q][kt]) : codes<CEN, false>(w0[q][kt]);
+                                const unsigned int a1 = half ? codes<CEN, true>(w1[q][kt]) : codes<CEN, false>(w1[q][kt]);
+                                const unsigned int a2 = half ? codes<CEN, true>(w0[q][kt] >> 8) : codes<CEN, false>(w0[q][kt] >> 8);
+                                const unsigned int a3 = half ? codes<CEN, true>(w1[q][kt] >> 8) : codes<CEN, false>(w1[q][kt] >> 8);
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) {
+                                    if (NP == 2) {
+                                        mma_16816(part[nt][half][q], a0, a1, a2, a3, pb[0][nt][kt][0], pb[0][nt][kt][1]);
+                                        mma_16816(part[nt][half][q], a0, a1, a2, a3, pb[NP - 1][nt][kt][0], pb[NP - 1][nt][kt][1]);
+                                    } else {
+                                        mma_16816(oacc[nt][half][qb + q], a0, a1, a2, a3, pb[0][nt][kt][0], pb[0][nt][kt][1]);
+                                    }
+                                }
+                            }
+                    if (NP == 2) {
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) oacc[nt][half][qb + q][i] += part[nt][half][q][i];
+                    }
+                }
+            }
+            __syncwarp();   // the stage has been read by every lane
+            if (issued < u1) {
+                issue(stage);
+                ++issued;
+            }
+            if (++stage == S) {
+                stage = 0;
+                phase ^= 1u;
+            }
+            const bool seg_end = at.pg == at.s.pages - 1;
+            if (seg_end || u == u1 - 1) {
+                // the piece is done
+                fresh_segment = true;
+                const long long seg = u - at.pg;
+                const bool complete = seg >= u0 && seg_end;
+                const bool tail = u == u1 - 1;
+                const float unscale = pow2f((ev - 127) - kP), back = pow2f(kC);
+                const int n = (int)min((long long)R, (long long)at.s.fresh * G - (long long)at.tile * R);
+                const int slot = 2 * warp + (tail ? 1 : 0);
+                float* to = tail ? reinterpret_cast<float*>(sh.ring[warp][0]) : a.warp_parts + (long long)(c * W + warp) * (R * TS);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int col = 0; col < 2; ++col) {
+                        float ls = l[nt][col], ms = mv[nt][col];
+#pragma unroll
+                        for (int o = 4; o < 32; o <<= 1) {
+                            ls += __shfl_xor_sync(0xFFFFFFFFu, ls, o);
+                            ms += __shfl_xor_sync(0xFFFFFFFFu, ms, o);
+                        }
+                        const int r = 8 * nt + 2 * j + col;
+                        const long long row = (long long)at.tile * R + r;
+                        const float inv = complete ? (ls > 0.f ? 1.f / ls : 0.f) : 1.f;
+                        const long long head = ((long long)at.s.first + row / G) * a.p.n_q_heads + at.h * G + row % G;
+                        if (g == 0) {
+                            if (!complete) {
+                                sh.m[slot][r] = mref[nt][col];
+                                sh.l[slot][r] = ls;
+                            } else if (a.o.lse != nullptr && r < n) {
+                                a.o.lse[head] = ls > 0.f ? (mref[nt][col] + log2f(ls)) * (float)kLn2 : -CUDART_INF_F;
+                            }
+                        }
+                        if (r < n) {
+#pragma unroll
+                            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                                for (int q = 0; q < MQ; ++q)
+#pragma unroll
+                                    for (int i = 0; i < 2; ++i) {
+                                        const int ch = half * H + 16 * q + 8 * i + g;
+                                        const float o = fmaf(oacc[nt][half][q][2 * i + col] * (half ? back * kHigh : back), unscale, ms) * inv;
+                                        if (!complete) to[r * TS + ch] = o;
+                                        else if (DT == AASD_F32) static_cast<float*>(a.o.out)[head * D + ch] = o;
+                                        else static_cast<__nv_bfloat16*>(a.o.out)[head * D + ch] = __float2bfloat16_rn(o);
+                                    }
+                        }
+                    }
+                if (!complete && lane == 0) sh.piece[slot] = KvPiece{seg, at.s.pages, at.h, at.tile * R, n, at.s.first};
+            }
+            at.next(a, R);
+        }
+        if (*abort_flag) {   // nothing may be on its way into this CTA's shared memory when it leaves
+            for (int s = 0; s < S; ++s)
+                for (unsigned int it = 0; it < kWaitLimit && u0 + s < issued && !mbar_try_wait(&full[s], ((unsigned int)((issued - 1 - u0 - s) / S)) & 1u); ++it) {}
         }
     }
-    if (a.o.lse != nullptr && lane == 0) a.o.lse[row] = l > 0.f ? (m + log2f(l)) * (float)kLn2 : -CUDART_INF_F;
+    __syncthreads();
+    if (works && !*abort_flag) {
+        const long long U0 = total * c / active, U1 = total * (c + 1) / active;
+        constexpr int Q4 = D / 4;
+        for (int p = 0; p < 2 * W;) {
+            const KvPiece pc = sh.piece[p];
+            if (pc.seg < 0) {
+                ++p;
+                continue;
+            }
+            int e = p + 1;
+            while (e < 2 * W && (sh.piece[e].seg < 0 || sh.piece[e].seg == pc.seg)) ++e;
+            const bool complete = pc.seg >= U0 && pc.seg + pc.pages <= U1;
+            // scratch slot of this CTA: 0 for a segment that began before it, 1 for one that begins in it
+            const int which = pc.seg < U0 ? 0 : 1;
+            constexpr int kPart = R * D + 2 * R;
+            float* part = a.cta_parts + (c * 2 + which) * kPart;
+            for (int i = tid; i < pc.n * Q4; i += Sh::kThreads) {
+                const int r = i / Q4, ch = (i - r * Q4) * 4;
+                float M = kKvNothing;
+                for (int k = p; k < e; ++k)
+                    if (sh.piece[k].seg >= 0) M = fmaxf(M, sh.m[k][r]);
+                float L = 0.f;
+                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int k = p; k < e; ++k) {
+                    if (sh.piece[k].seg < 0) continue;
+                    const float f = ex2_approx(sh.m[k][r] - M);
+                    L = fmaf(sh.l[k][r], f, L);
+                    const float* from = (k & 1) ? reinterpret_cast<const float*>(sh.ring[k >> 1][0])
+                                                : a.warp_parts + (c * W + (k >> 1)) * (R * TS);
+                    const float4 x = *reinterpret_cast<const float4*>(from + r * TS + ch);
+                    o.x = fmaf(x.x, f, o.x);
+                    o.y = fmaf(x.y, f, o.y);
+                    o.z = fmaf(x.z, f, o.z);
+                    o.w = fmaf(x.w, f, o.w);
+                }
+                if (complete) {
+                    const float inv = L > 0.f ? 1.f / L : 0.f;
+                    const long long row = pc.row0 + r;
+                    const long long head = ((long long)pc.first + row / G) * a.p.n_q_heads + pc.h * G + row % G;
+                    store4<DT>(a.o.out, head * D + ch, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), a.out_vec);
+                    if (a.o.lse != nullptr && ch == 0) a.o.lse[head] = L > 0.f ? (M + log2f(L)) * (float)kLn2 : -CUDART_INF_F;
+                } else {
+                    *reinterpret_cast<float4*>(part + r * D + ch) = o;
+                    if (ch == 0) {
+                        part[R * D + r] = M;
+                        part[R * D + R + r] = L;
+                    }
+                }
+            }
+            if (!complete) {
+                // the last of the segment's CTAs joins the parts
+                const long long c0 = ((pc.seg + 1) * active - 1) / total, c1 = ((pc.seg + pc.pages) * active - 1) / total;
+                __syncthreads();
+                if (tid == 0) {
+                    __threadfence();
+                    sh.last = take_ticket(a.tickets + c0) == (unsigned int)(c1 - c0);
+                    if (sh.last) a.tickets[c0] = 0;
+                }
+                __syncthreads();
+                if (sh.last) {
+                    // weights of the parts first, one row per warp, so that the sums below are a stream of
+                    // independent loads
+                    const int parts = (int)(c1 - c0) + 1;
+                    float* wgt = reinterpret_cast<float*>(sh.ring[0][0]) + R * TS;   // (behind the first warp's piece)
+                    for (int r = warp; r < pc.n; r += W) {
+                        float M = kKvNothing;
+                        for (int k = lane; k < parts; k += 32) M = fmaxf(M, __ldcg(a.cta_parts + ((c0 + k) * 2 + (k == 0)) * kPart + R * D + r));
+#pragma unroll
+                        for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
+                        float L = 0.f;
+                        for (int k = lane; k < parts; k += 32) {
+                            const float* from = a.cta_parts + ((c0 + k) * 2 + (k == 0)) * kPart + R * D + r;
+                            const float f = ex2_approx(__ldcg(from) - M);
+                            wgt[r * kKvMaxCtas + k] = f;
+                            L = fmaf(__ldcg(from + R), f, L);
+                        }
+#pragma unroll
+                        for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xFFFFFFFFu, L, o);
+                        if (lane == 0) {
+                            sh.m[0][r] = M;
+                            sh.l[0][r] = L;
+                        }
+                    }
+                    __syncthreads();
+                    for (int i = tid; i < pc.n * Q4; i += Sh::kThreads) {
+                        const int r = i / Q4, ch = (i - r * Q4) * 4;
+                        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+                        const float* from = a.cta_parts + c0 * 2 * kPart + r * D + ch;
+#pragma unroll 8
+                        for (int k = 0; k < parts; ++k) {
+                            const float f = wgt[r * kKvMaxCtas + k];
+                            const float4 x = __ldcg(reinterpret_cast<const float4*>(from + (k * 2 + (k == 0)) * kPart));
+                            o.x = fmaf(x.x, f, o.x);
+                            o.y = fmaf(x.y, f, o.y);
+                            o.z = fmaf(x.z, f, o.z);
+                            o.w = fmaf(x.w, f, o.w);
+                        }
+                        const float L = sh.l[0][r], inv = L > 0.f ? 1.f / L : 0.f;
+                        const long long row = pc.row0 + r;
+                        const long long head = ((long long)pc.first + row / G) * a.p.n_q_heads + pc.h * G + row % G;
+                        store4<DT>(a.o.out, head * D + ch, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), a.out_vec);
+                        if (a.o.lse != nullptr && ch == 0) a.o.lse[head] = L > 0.f ? (sh.m[0][r] + log2f(L)) * (float)kLn2 : -CUDART_INF_F;
+                    }
+                    __syncthreads();
+                }
+            }
+            p = e;
+        }
+    }
+    kv_clear_rows<DT>(a, D, (int)(blockIdx.x * W + warp), (int)(gridDim.x * W));
 }
 
 }  // namespace aasd

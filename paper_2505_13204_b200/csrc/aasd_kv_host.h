@@ -10,15 +10,18 @@
 
 namespace aasd {
 
-// Scratch of the attention kernels.
+// Scratch of the attention kernels: tickets (zero between calls), then per CTA two partial
+// results, then per warp one.
 struct KvScratch {
-    size_t bytes, zero_bytes;
+    size_t zero_bytes, off_cta, off_warp, bytes;
 };
 constexpr KvScratch kv_attend_scratch(int head_dim) {
     KvScratch L{};
-    L.zero_bytes = 256;
-    L.bytes = 256;
-    (void)head_dim;
+    const size_t D = (size_t)head_dim, R = 16, W = 8;
+    L.zero_bytes = align_up(4 * kKvMaxCtas, 256);
+    L.off_cta = L.zero_bytes;
+    L.off_warp = align_up(L.off_cta + kKvMaxCtas * 2 * (R * D + 2 * R) * 4, 256);
+    L.bytes = align_up(L.off_warp + kKvMaxCtas * W * R * (D + 4) * 4, 256);
     return L;
 }
 
