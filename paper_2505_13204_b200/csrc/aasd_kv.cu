@@ -182,7 +182,7 @@ int aasd_kv_attend(aasd_ctx* ctx, const void* q, const void* pages, const int32_
     if (ctx == nullptr || p == nullptr || o == nullptr) return AASD_ERR_INVALID_ARG;
     if (!dtype_ok(p->dtype)) return AASD_ERR_BAD_DTYPE;
     if (!head_dim_ok(p->head_dim)) return AASD_ERR_UNSUPPORTED;
-    if (p->n_seqs < 0 || p->n_tokens < 0 || p->n_kv_heads < 1 || p->n_q_heads < 1 || p->n_q_heads % p->n_kv_heads != 0 ||
+    if (p->n_seqs < 0 || p->n_tokens < 0 || p->n_kv_heads < 1 || p->n_q_heads < 1 || p->n_q_heads > 65536 || p->n_q_heads % p->n_kv_heads != 0 ||
         p->n_pages < 0 || p->n_pages > 0x7FFFFFFF / kPage || p->max_pages < 1 || p->max_pages > 0x7FFFFFFF / kPage || p->rows_per_seq < 0 ||
         p->q_stride < (int64_t)p->n_q_heads * p->head_dim)
         return AASD_ERR_BAD_SHAPE;

@@ -13,10 +13,10 @@ namespace {
 template <int DT, int D, int NT>
 int launch_split(const LaunchEnv& env, int sm_count, const KvAttendArgs& a) {
     constexpr auto kernel = kv_attend_split_kernel<DT, D, NT>;
-    constexpr size_t smem = sizeof(KvSplitShared<D, NT>);
+    constexpr size_t smem = sizeof(KvSplitShared<DT, D, NT>);
     static_assert(smem <= 227 * 1024, "fits an SM");
     if (enable_smem<kernel, smem>(env.device) != AASD_OK) return AASD_ERR_CUDA;
-    launch(kernel, (unsigned int)(sm_count < kKvMaxCtas ? sm_count : kKvMaxCtas), (unsigned int)KvSplitShape<D>::kThreads, smem, env.stream, a);
+    launch(kernel, (unsigned int)(sm_count < kKvMaxCtas ? sm_count : kKvMaxCtas), (unsigned int)KvSplitShape<DT, D, NT>::kThreads, smem, env.stream, a);
     return AASD_OK;
 }
 

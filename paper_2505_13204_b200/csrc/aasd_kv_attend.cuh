@@ -12,6 +12,8 @@
 
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "aasd_kv.cuh"
 #include "aasd_stream.cuh"
 
@@ -72,26 +74,37 @@ __device__ __forceinline__ KvSeq kv_load_seq(const KvAttendArgs& a, int b, int t
     s.tiles = (int)((n + tile_rows - 1) / tile_rows);
     return s;
 }
-// Units of work (one page of one head for one row tile) of a sequence.
+// Work is counted in pages: a segment (one row tile of one head of one sequence) is kSegCost + its
+// pages, the first for loading the queries and handing the result on, which take a warp about as
+// long as a page.  Page p of the segment is unit kSegCost + p of it.
+constexpr int kSegCost = 1;
 __device__ __forceinline__ long long kv_units(const KvAttendArgs& a, const KvSeq& s) {
-    return (long long)s.pages * s.tiles * a.p.n_kv_heads;
+    return s.pages == 0 ? 0 : (long long)(s.pages + kSegCost) * s.tiles * a.p.n_kv_heads;
 }
 
 // A place in the list of all units: sequence by sequence, head by head, tile by tile, page by page.
 struct KvCursor {
     int b, h, tile, pg;
+    long long unit;           // of page pg
     KvSeq s;
-    __device__ __forceinline__ void seek(const KvAttendArgs& a, int b_, const KvSeq& s_, long long rem) {
+    const int32_t* table;     // the sequence's row of the block table
+    // To the first page at or behind unit u, which is unit rem of sequence b_.
+    __device__ __forceinline__ void seek(const KvAttendArgs& a, int b_, const KvSeq& s_, long long rem, long long u) {
         b = b_;
         s = s_;
-        const long long seg = rem / s.pages;
-        pg = (int)(rem - seg * s.pages);
-        h = (int)(seg / s.tiles);
-        tile = (int)(seg - (long long)h * s.tiles);
+        unit = u;
+        const int seg = (int)(rem / (s.pages + kSegCost));
+        unit -= rem;                                           // (of the sequence's first unit)
+        rem -= (long long)seg * (s.pages + kSegCost);
+        pg = rem < kSegCost ? 0 : (int)rem - kSegCost;
+        unit += (long long)seg * (s.pages + kSegCost) + kSegCost + pg;
+        h = seg / s.tiles;
+        tile = seg - h * s.tiles;
+        table = a.block_table + (long long)b * a.p.max_pages;
     }
-    __device__ __forceinline__ void next(const KvAttendArgs& a, int tile_rows) {
-        if (++pg < s.pages) return;
+    __device__ __forceinline__ void next_segment(const KvAttendArgs& a, int tile_rows) {
         pg = 0;
+        unit += kSegCost;
         if (++tile < s.tiles) return;
         tile = 0;
         if (++h < a.p.n_kv_heads) return;
@@ -100,18 +113,37 @@ struct KvCursor {
             if (++b >= a.p.n_seqs) return;   // (past the last unit: never looked at)
             s = kv_load_seq(a, b, tile_rows);
         } while (s.pages == 0 || s.tiles == 0);
+        table = a.block_table + (long long)b * a.p.max_pages;
     }
-    // Block of the current unit, or NULL (the table's entry is not a page).
-    __device__ __forceinline__ const uint8_t* block(const KvAttendArgs& a, int head_bytes) const {
-        const int page = a.block_table[(long long)b * a.p.max_pages + pg];
-        if (page < 0 || page >= a.p.n_pages) return nullptr;
-        return a.pages + ((long long)page * a.p.n_kv_heads + h) * head_bytes;
+};
+
+// `total` units in `n` shares that differ by one unit at most, the larger ones first.
+struct KvShares {
+    long long each, more;     // units of a small share; shares with one more
+    __device__ __forceinline__ KvShares(long long total, long long n) {
+        if (total < 0x7FFFFFFFLL) each = (long long)((unsigned int)total / (unsigned int)n);
+        else each = total / n;
+        more = total - each * n;
     }
+    __device__ __forceinline__ long long first(long long share) const { return each * share + (share < more ? share : more); }
+    __device__ __forceinline__ long long owner(long long unit) const {
+        const long long big = (each + 1) * more;
+        return unit < big ? unit / (each + 1) : more + (unit - big) / each;
+    }
+};
+
+// One row tile of one head of one sequence, as a warp works on it.
+struct KvSegment {
+    int cached, fresh, first; // see KvSeq
+    int pages;
+    int h, row0;              // head, first row of the tile
+    int pg;                   // the warp's first page of it
+    long long unit;           // of page 0
 };
 
 // Bit j of the result: new token (64 pg + j - cached) of the sequence's tokens, or a cached one at
 // that place, is seen by new token i.
-__device__ __forceinline__ u64 kv_seen(const KvAttendArgs& a, const KvSeq& s, int pg, int i) {
+__device__ __forceinline__ u64 kv_seen(const KvAttendArgs& a, const KvSegment& s, int pg, int i) {
     const long long at = (long long)pg * kPage;
     if (i >= s.fresh) return 0ull;
     const long long before = s.cached - at;                       // cached tokens of this page
@@ -223,11 +255,13 @@ __device__ __forceinline__ void kv_clear_rows(const KvAttendArgs& a, int D, int 
 // ---- few rows per head: the keys split over all warps -----------------------------------------------
 
 // W warps per CTA, each with a ring of S blocks of its own that lane 0 fills with one bulk copy per
-// block; S blocks per warp keep 70 to 200 KB per SM in flight (memory wants about 40).
-template <int D>
+// block: 100 to 200 KB per SM are on their way at any time (memory wants about 40).  Twelve warps
+// where their registers allow it (168 each): the chains of a page's products and exponentials leave
+// issue slots that only other warps fill.
+template <int DT, int D, int NT>
 struct KvSplitShape {
-    static constexpr int W = D == 256 ? 4 : 8;
-    static constexpr int S = D == 64 ? 5 : 3;
+    static constexpr int W = D == 256 ? 4 : DT == AASD_BF16 && NT == 1 ? 12 : 8;
+    static constexpr int S = D == 64 ? (W == 12 ? 4 : 5) : W == 12 ? 2 : 3;
     static constexpr int kBlock = kv_head_bytes(D);
     static constexpr int kThreads = W * 32;
 };
@@ -236,32 +270,33 @@ struct KvSplitShape {
 // one warp, or one CTA, has been through.  Rows are padded by four floats in shared memory so that
 // a warp's stores meet every bank once.
 struct KvPiece {
-    long long seg;      // first unit of the segment, -1: no piece
-    int pages;          // units of the segment
+    long long seg;      // unit of the segment's first page, -1: no piece
+    int pages;          // of the segment
     int h, row0, n;     // head, first row of the tile, rows in use
     int first;          // token row of the sequence's first new token
 };
 
-template <int D, int NT>
+template <int DT, int D, int NT>
 struct KvSplitShared {
-    using Sh = KvSplitShape<D>;
+    using Sh = KvSplitShape<DT, D, NT>;
     static constexpr int R = 8 * NT;
     alignas(128) unsigned char ring[Sh::W][Sh::S][Sh::kBlock];
     long long base[Sh::kThreads + 1];
     long long scan[Sh::W];
+    KvSegment seg[Sh::W][Sh::S + 1];   // of the blocks on their way, and the one being worked on
     KvPiece piece[2 * Sh::W];
     float m[2 * Sh::W][R], l[2 * Sh::W][R];
     u64 full[Sh::W][Sh::S];
-    int abort_flag, last;
+    int abort_flag, last[2];
 };
 
 // DT: type of the queries.  bf16 values fit an fp16 number scaled by the row's own power of two;
 // fp32 queries and their probabilities travel as two fp16 numbers each (22 bits).
 // NT: row tiles of eight that share the codes of a page.
 template <int DT, int D, int NT>
-__global__ void __launch_bounds__(KvSplitShape<D>::kThreads, 1) kv_attend_split_kernel(const KvAttendArgs a) {
-    using Sh = KvSplitShape<D>;
-    using Shared = KvSplitShared<D, NT>;
+__global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_attend_split_kernel(const KvAttendArgs a) {
+    using Sh = KvSplitShape<DT, D, NT>;
+    using Shared = KvSplitShared<DT, D, NT>;
     constexpr int W = Sh::W, S = Sh::S, R = 8 * NT, H = D / 2, TS = D + 4;
     constexpr int NP = DT == AASD_F32 ? 2 : 1;      // fp16 numbers per query element and probability
     constexpr bool CEN = NP == 2;                   // codes are centred (see codes())
@@ -273,7 +308,7 @@ __global__ void __launch_bounds__(KvSplitShape<D>::kThreads, 1) kv_attend_split_
     // keep their bits; the running maximum may lag by 2^kLazy before everything is rescaled.
     constexpr float kLazy = DT == AASD_F32 ? 0.f : 4.f;
     constexpr int kP = DT == AASD_F32 ? 14 : 10;
-    static_assert(R * TS * 4 + R * kKvMaxCtas * 4 <= S * Sh::kBlock, "a piece and the weights of a join fit a warp's ring");
+    static_assert(R * TS * 4 <= S * Sh::kBlock, "a piece fits its warp's ring");
     extern __shared__ __align__(128) unsigned char smem_raw[];
     Shared& sh = *reinterpret_cast<Shared*>(smem_raw);
     pdl_launch_dependents();
@@ -284,7 +319,7 @@ __global__ void __launch_bounds__(KvSplitShape<D>::kThreads, 1) kv_attend_split_
         sh.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (tid < 2 * W) sh.piece[tid].seg = -1;
+    for (int i = tid; i < 2 * W; i += Sh::kThreads) sh.piece[i].seg = -1;
     pdl_wait();
     const int B = a.p.n_seqs, G = a.p.n_q_heads / a.p.n_kv_heads;
     // every thread adds up the units of its strip of sequences
@@ -304,15 +339,15 @@ __global__ void __launch_bounds__(KvSplitShape<D>::kThreads, 1) kv_attend_split_
     active = active > gridDim.x ? gridDim.x : active;
     const long long c = blockIdx.x;
     const bool works = c < active;
-    const long long u0 = works ? total * (c * W + warp) / (active * W) : 0;
-    const long long u1 = works ? total * (c * W + warp + 1) / (active * W) : 0;
+    const KvShares shares(total, works ? active * W : 1);
+    const long long u0 = works ? shares.first(c * W + warp) : 0, u1 = works ? shares.first(c * W + warp + 1) : 0;
     volatile int* abort_flag = &sh.abort_flag;
     u64* full = sh.full[warp];
 
     if (u0 < u1) {
-        KvCursor at, ahead;
+        KvCursor ahead;
         {
-            int lo = 0, hi = Sh::kThreads;
+            int lo = 0, hi = (B + strip - 1) / strip;
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
                 if (sh.base[mid] <= u0) lo = mid;
@@ -325,26 +360,62 @@ __global__ void __launch_bounds__(KvSplitShape<D>::kThreads, 1) kv_attend_split_
                 rem -= kv_units(a, s);
                 s = kv_load_seq(a, ++b, R);
             }
-            at.seek(a, b, s, rem);
+            ahead.seek(a, b, s, rem, u0);
         }
-        ahead = at;
+        const unsigned int page_stride = (unsigned int)a.p.n_kv_heads * Sh::kBlock;
         unsigned int missing = 0;   // bit s: stage s holds no block (the table names no page)
-        auto issue = [&](int stage) {
-            const uint8_t* src = ahead.block(a, Sh::kBlock);
-            missing = (missing & ~(1u << stage)) | (src == nullptr ? 1u << stage : 0u);
-            if (lane == 0) {
-                if (src == nullptr) {
-                    raise(a.state, AASD_STATUS_BAD_OFFSETS);
-                    mbar_arrive(&full[stage]);
-                } else {
-                    mbar_arrive_expect_tx(&full[stage], Sh::kBlock);
-                    bulk_copy_g2s(sh.ring[warp][stage], src, Sh::kBlock, &full[stage]);
+        int seg_in = 0;             // where the next segment's description goes
+        bool begins = true;         // the next block is the first of a segment
+        int issued = 0;             // blocks asked for so far
+        // a segment's queries are wanted when the blocks in front of its own are done
+        auto prefetch_queries = [&]() {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const int row = ahead.tile * R + 8 * nt + g;
+                if (row < ahead.s.fresh * G) {
+                    constexpr int es = DT == AASD_F32 ? 4 : 2;
+                    const char* q0 = static_cast<const char*>(a.q) + ((long long)(ahead.s.first + row / G) * a.p.q_stride +
+                                                                      (long long)(ahead.h * G + row % G) * D + (H / 4) * j) * es;
+                    asm volatile("prefetch.global.L1 [%0];" ::"l"(q0));
+                    asm volatile("prefetch.global.L1 [%0];" ::"l"(q0 + H * es));
                 }
             }
-            ahead.next(a, R);
         };
-        long long issued = u0;
-        for (int s = 0; s < S && issued < u1; ++s, ++issued) issue(s);
+        int ids = 0, ids_b = -1, ids_at = 0;   // lane k: the table's entry ids_at + k of sequence ids_b
+        auto issue = [&](int stage) {
+            if (ids_b != ahead.b || (unsigned int)(ahead.pg - ids_at) >= 32u) {
+                ids_b = ahead.b;
+                ids_at = ahead.pg;
+                ids = ids_at + lane < ahead.s.pages ? ahead.table[ids_at + lane] : -1;
+            }
+            const int page = __shfl_sync(0xFFFFFFFFu, ids, ahead.pg - ids_at);
+            const bool ok = page >= 0 && page < a.p.n_pages;
+            missing = (missing & ~(1u << stage)) | (ok ? 0u : 1u << stage);
+            if (lane == 0) {
+                if (ok) {
+                    mbar_arrive_expect_tx(&full[stage], Sh::kBlock);
+                    bulk_copy_g2s(sh.ring[warp][stage], a.pages + (u64)(unsigned int)page * page_stride + (u64)(ahead.h * Sh::kBlock),
+                                  Sh::kBlock, &full[stage]);
+                } else {
+                    raise(a.state, AASD_STATUS_BAD_OFFSETS);
+                    mbar_arrive(&full[stage]);
+                }
+            }
+            if (begins) {
+                begins = false;
+                if (lane == 0) sh.seg[warp][seg_in] = KvSegment{ahead.s.cached, ahead.s.fresh, ahead.s.first, ahead.s.pages, ahead.h, ahead.tile * R, ahead.pg, ahead.unit - ahead.pg};
+                if (++seg_in > S) seg_in = 0;
+                if (issued > 0) prefetch_queries();
+            }
+            ++ahead.unit;
+            if (++ahead.pg == ahead.s.pages) {
+                ahead.next_segment(a, R);
+                begins = true;
+            }
+        };
+        if (ahead.unit < u1) prefetch_queries();   // (in front of the copies, which would hold them up)
+        for (int s = 0; s < S && ahead.unit < u1; ++s, ++issued) issue(s);
+        __syncwarp();
 
         unsigned int qf[NP][NT][D / 16][2];   // query operands
         float rfac[NT][2], qsum[NT][2];       // per column: what scales the codes' products, and the sum of q, in base 2
@@ -352,32 +423,40 @@ __global__ void __launch_bounds__(KvSplitShape<D>::kThreads, 1) kv_attend_split_
         float oacc[NT][2][MQ][4];             // [tile][half][channel tile][fragment]
         int ev = 0;                           // exponent field that the probabilities are scaled by
         bool fresh_segment = true;
-        int stage = 0;
+        int stage = 0, seg_out = -1, pg = 0, last_pg = 0, cached = 0, end = 0;
         unsigned int phase = 0;
 
-        for (long long u = u0; u < u1; ++u) {
+        for (int u = 0; u < issued; ++u) {
             if (fresh_segment) {
                 fresh_segment = false;
+                seg_out = seg_out == S ? 0 : seg_out + 1;
+                const KvSegment at = sh.seg[warp][seg_out];
+                pg = at.pg;
+                last_pg = at.pages - 1;
+                cached = at.cached;
+                end = at.cached + at.fresh;
                 ev = 64;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     // lane (g, j): row 8 nt + g, channels (H / 4) j .. of each half
-                    const long long row = (long long)at.tile * R + 8 * nt + g;
-                    const bool valid = row < (long long)at.s.fresh * G;
-                    const long long tok = at.s.first + (valid ? row / G : 0);
+                    const int row = at.row0 + 8 * nt + g;
+                    const bool valid = row < at.fresh * G;
+                    const long long tok = at.first + (valid ? row / G : 0);
                     const long long q0 = tok * a.p.q_stride + (long long)(at.h * G + (valid ? row % G : 0)) * D + (H / 4) * j;
                     float top = 0.f, sum = 0.f;
+                    float x[2][H / 4];
 #pragma unroll
                     for (int half = 0; half < 2; ++half)
 #pragma unroll
                         for (int k = 0; k < H / 4; k += 8) {
-                            float x[8];
-                            if (a.q_vec) load8<DT, true>(a.q, q0 + half * H + k, x);
-                            else load8<DT, false>(a.q, q0 + half * H + k, x);
+                            float y[8];
+                            if (a.q_vec) load8<DT, true>(a.q, q0 + half * H + k, y);
+                            else load8<DT, false>(a.q, q0 + half * H + k, y);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                top = fmaxf(top, fabsf(x[e]));
-                                sum += x[e];
+                            for (int i = 0; i < 8; ++i) {
+                                x[half][k + i] = valid ? y[i] : 0.f;
+                                top = fmaxf(top, fabsf(x[half][k + i]));
+                                sum += x[half][k + i];
                             }
                         }
                     top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
@@ -389,28 +468,17 @@ __global__ void __launch_bounds__(KvSplitShape<D>::kThreads, 1) kv_attend_split_
                     e = e < -100 ? -100 : e > 100 ? 100 : e;
                     const float up = pow2f(14 - e);
 #pragma unroll
-                    for (int k = 0; k < H / 4; k += 8) {
-                        float x[2][8];
+                    for (int w = 0; w < KW; ++w)
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            if (a.q_vec) load8<DT, true>(a.q, q0 + half * H + k, x[half]);
-                            else load8<DT, false>(a.q, q0 + half * H + k, x[half]);
+                        for (int half = 0; half < 2; ++half)
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) x[half][i] = valid ? x[half][i] * (half ? up * kHigh : up) : 0.f;
-                        }
-#pragma unroll
-                        for (int w = 0; w < 2; ++w)
-#pragma unroll
-                            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                                for (int r = 0; r < 2; ++r) {
-                                    const float p = x[half][4 * w + r], q = x[half][4 * w + r + 2];
-                                    const unsigned int hi = pack_half(p, q);
-                                    const int ks = 2 * (k / 4 + w) + half;
-                                    qf[0][nt][ks][r] = hi;
-                                    if (NP == 2) qf[NP - 1][nt][ks][r] = pack_rest(p, q, hi);
-                                }
-                    }
+                            for (int r = 0; r < 2; ++r) {
+                                const float f = half ? up * kHigh : up;
+                                const float p = x[half][4 * w + r] * f, q = x[half][4 * w + r + 2] * f;
+                                const unsigned int hi = pack_half(p, q);
+                                qf[0][nt][2 * w + half][r] = hi;
+                                if (NP == 2) qf[NP - 1][nt][2 * w + half][r] = pack_rest(p, q, hi);
+                            }
                     const float rf = a.scale_log2 * pow2f(e + kC - 14);   // of the codes and of the row
                     sum *= a.scale_log2;
 #pragma unroll
@@ -481,8 +549,8 @@ __global__ void __launch_bounds__(KvSplitShape<D>::kThreads, 1) kv_attend_split_
                 }
                 // scales, masks, running maximum
                 uint2 vm[4];
-                const bool masked = (long long)(at.pg + 1) * kPage > at.s.cached;
-                const int live = (int)min((long long)kPage, (long long)at.s.cached + at.s.fresh - (long long)at.pg * kPage);
+                const bool masked = (pg + 1) * kPage > cached;
+                const int live = end - pg * kPage;
                 float mx[NT][2];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) mx[nt][0] = mx[nt][1] = kKvHidden;
@@ -507,12 +575,12 @@ __global__ void __launch_bounds__(KvSplitShape<D>::kThreads, 1) kv_attend_split_
                         }
                 }
                 if (masked) {
+                    const KvSegment at = sh.seg[warp][seg_out];
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int col = 0; col < 2; ++col) {
-                            const long long row = (long long)at.tile * R + 8 * nt + 2 * j + col;
-                            const u64 seen = kv_seen(a, at.s, at.pg, (int)(row / G));
+                            const u64 seen = kv_seen(a, at, pg, (at.row0 + 8 * nt + 2 * j + col) / G);
 #pragma unroll
                             for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
@@ -632,25 +700,27 @@ __global__ void __launch_bounds__(KvSplitShape<D>::kThreads, 1) kv_attend_split_
                 }
             }
             __syncwarp();   // the stage has been read by every lane
-            if (issued < u1) {
+            if (ahead.unit < u1) {
                 issue(stage);
                 ++issued;
+                __syncwarp();   // (a segment's description may have been written)
             }
             if (++stage == S) {
                 stage = 0;
                 phase ^= 1u;
             }
-            const bool seg_end = at.pg == at.s.pages - 1;
-            if (seg_end || u == u1 - 1) {
+            const bool seg_end = pg == last_pg;
+            ++pg;
+            const bool tail = u == issued - 1;   // (blocks are asked for at least one ahead)
+            if (seg_end || tail) {
                 // the piece is done
                 fresh_segment = true;
-                const long long seg = u - at.pg;
-                const bool complete = seg >= u0 && seg_end;
-                const bool tail = u == u1 - 1;
+                const KvSegment at = sh.seg[warp][seg_out];
+                const bool complete = at.pg == 0 && seg_end;
                 const float unscale = pow2f((ev - 127) - kP), back = pow2f(kC);
-                const int n = (int)min((long long)R, (long long)at.s.fresh * G - (long long)at.tile * R);
+                const int n = min(R, at.fresh * G - at.row0);
                 const int slot = 2 * warp + (tail ? 1 : 0);
-                float* to = tail ? reinterpret_cast<float*>(sh.ring[warp][0]) : a.warp_parts + (long long)(c * W + warp) * (R * TS);
+                float* to = tail ? reinterpret_cast<float*>(sh.ring[warp][0]) : a.warp_parts + (c * W + warp) * (R * TS);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -662,9 +732,9 @@ __global__ void __launch_bounds__(KvSplitShape<D>::kThreads, 1) kv_attend_split_
                             ms += __shfl_xor_sync(0xFFFFFFFFu, ms, o);
                         }
                         const int r = 8 * nt + 2 * j + col;
-                        const long long row = (long long)at.tile * R + r;
+                        const int row = at.row0 + r;
                         const float inv = complete ? (ls > 0.f ? 1.f / ls : 0.f) : 1.f;
-                        const long long head = ((long long)at.s.first + row / G) * a.p.n_q_heads + at.h * G + row % G;
+                        const long long head = ((long long)at.first + row / G) * a.p.n_q_heads + at.h * G + row % G;
                         if (g == 0) {
                             if (!complete) {
                                 sh.m[slot][r] = mref[nt][col];
@@ -688,123 +758,190 @@ __global__ void __launch_bounds__(KvSplitShape<D>::kThreads, 1) kv_attend_split_
                                     }
                         }
                     }
-                if (!complete && lane == 0) sh.piece[slot] = KvPiece{seg, at.s.pages, at.h, at.tile * R, n, at.s.first};
+                if (!complete && lane == 0) sh.piece[slot] = KvPiece{at.unit, at.pages, at.h, at.row0, n, at.first};
             }
-            at.next(a, R);
         }
         if (*abort_flag) {   // nothing may be on its way into this CTA's shared memory when it leaves
             for (int s = 0; s < S; ++s)
-                for (unsigned int it = 0; it < kWaitLimit && u0 + s < issued && !mbar_try_wait(&full[s], ((unsigned int)((issued - 1 - u0 - s) / S)) & 1u); ++it) {}
+                for (unsigned int it = 0; it < kWaitLimit && s < issued && !mbar_try_wait(&full[s], ((unsigned int)((issued - 1 - s) / S)) & 1u); ++it) {}
         }
     }
     __syncthreads();
     if (works && !*abort_flag) {
-        const long long U0 = total * c / active, U1 = total * (c + 1) / active;
-        constexpr int Q4 = D / 4;
-        for (int p = 0; p < 2 * W;) {
-            const KvPiece pc = sh.piece[p];
-            if (pc.seg < 0) {
-                ++p;
-                continue;
+        // Joining the pieces.  Every warp finds the groups of pieces that belong together (lane k looks
+        // at piece k) and the warps share the groups' rows; a row's weights are found lane by lane, its
+        // channels summed as independent loads.
+        static_assert(2 * W <= 32, "a lane per piece");
+        constexpr int kPart = R * D + 2 * R;
+        const long long U0 = shares.first(c * W), U1 = shares.first(c * W + W);
+        const long long seg = lane < 2 * W ? sh.piece[lane].seg : -1;
+        const unsigned int valid = __ballot_sync(0xFFFFFFFFu, seg >= 0);
+        const unsigned int below = valid & ((1u << lane) - 1u);
+        const long long previous = __shfl_sync(0xFFFFFFFFu, seg, below ? 31 - __clz(below) : 0);
+        unsigned int starts = __ballot_sync(0xFFFFFFFFu, seg >= 0 && (below == 0 || previous != seg));
+        auto finish_row = [&](const KvPiece& pc, int r, float M, float L, float4 o, int ch) {
+            const float inv = L > 0.f ? 1.f / L : 0.f;
+            const int row = pc.row0 + r;
+            const long long head = ((long long)pc.first + row / G) * a.p.n_q_heads + pc.h * G + row % G;
+            store4<DT>(a.o.out, head * D + ch, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), a.out_vec);
+            if (a.o.lse != nullptr && ch == 0) a.o.lse[head] = L > 0.f ? (M + log2f(L)) * (float)kLn2 : -CUDART_INF_F;
+        };
+        int open[2] = {-1, -1};        // first pieces of the groups that other CTAs hold parts of: begun before this CTA, in it
+        // rows r0 .. r0 + RB of the group of pieces `group`
+        auto join_rows = [&](auto rb, const KvPiece& pc, unsigned int group, bool complete, float* part, int r0) {
+            constexpr int RB = decltype(rb)::value;
+            const bool in = (group >> lane) & 1u;
+            const int own = lane < 2 * W ? lane : 0;
+            float M[RB], L[RB], f[RB];
+#pragma unroll
+            for (int i = 0; i < RB; ++i) {
+                const int r = min(r0 + i, pc.n - 1);
+                const float m = in ? sh.m[own][r] : kKvNothing;
+                M[i] = m;
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) M[i] = fmaxf(M[i], __shfl_xor_sync(0xFFFFFFFFu, M[i], o));
+                f[i] = in ? ex2_approx(m - M[i]) : 0.f;
+                L[i] = in ? sh.l[own][r] * f[i] : 0.f;
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) L[i] += __shfl_xor_sync(0xFFFFFFFFu, L[i], o);
             }
-            int e = p + 1;
-            while (e < 2 * W && (sh.piece[e].seg < 0 || sh.piece[e].seg == pc.seg)) ++e;
-            const bool complete = pc.seg >= U0 && pc.seg + pc.pages <= U1;
-            // scratch slot of this CTA: 0 for a segment that began before it, 1 for one that begins in it
-            const int which = pc.seg < U0 ? 0 : 1;
-            constexpr int kPart = R * D + 2 * R;
-            float* part = a.cta_parts + (c * 2 + which) * kPart;
-            for (int i = tid; i < pc.n * Q4; i += Sh::kThreads) {
-                const int r = i / Q4, ch = (i - r * Q4) * 4;
-                float M = kKvNothing;
-                for (int k = p; k < e; ++k)
-                    if (sh.piece[k].seg >= 0) M = fmaxf(M, sh.m[k][r]);
-                float L = 0.f;
-                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-                for (int k = p; k < e; ++k) {
-                    if (sh.piece[k].seg < 0) continue;
-                    const float f = ex2_approx(sh.m[k][r] - M);
-                    L = fmaf(sh.l[k][r], f, L);
+            for (int cb = 0; cb < D; cb += 128) {
+                const int ch = cb + lane * 4;
+                const bool on = ch < D;
+                float4 o[RB];
+#pragma unroll
+                for (int i = 0; i < RB; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                unsigned int left = group;
+                while (left) {
+                    const int k = __ffs(left) - 1;
+                    left &= left - 1;
                     const float* from = (k & 1) ? reinterpret_cast<const float*>(sh.ring[k >> 1][0])
                                                 : a.warp_parts + (c * W + (k >> 1)) * (R * TS);
-                    const float4 x = *reinterpret_cast<const float4*>(from + r * TS + ch);
-                    o.x = fmaf(x.x, f, o.x);
-                    o.y = fmaf(x.y, f, o.y);
-                    o.z = fmaf(x.z, f, o.z);
-                    o.w = fmaf(x.w, f, o.w);
+                    float4 x[RB];
+#pragma unroll
+                    for (int i = 0; i < RB; ++i) {
+                        x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        if (on) x[i] = *reinterpret_cast<const float4*>(from + min(r0 + i, pc.n - 1) * TS + ch);
+                    }
+#pragma unroll
+                    for (int i = 0; i < RB; ++i) {
+                        const float fk = __shfl_sync(0xFFFFFFFFu, f[i], k);
+                        o[i].x = fmaf(x[i].x, fk, o[i].x);
+                        o[i].y = fmaf(x[i].y, fk, o[i].y);
+                        o[i].z = fmaf(x[i].z, fk, o[i].z);
+                        o[i].w = fmaf(x[i].w, fk, o[i].w);
+                    }
                 }
-                if (complete) {
-                    const float inv = L > 0.f ? 1.f / L : 0.f;
-                    const long long row = pc.row0 + r;
-                    const long long head = ((long long)pc.first + row / G) * a.p.n_q_heads + pc.h * G + row % G;
-                    store4<DT>(a.o.out, head * D + ch, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), a.out_vec);
-                    if (a.o.lse != nullptr && ch == 0) a.o.lse[head] = L > 0.f ? (M + log2f(L)) * (float)kLn2 : -CUDART_INF_F;
-                } else {
-                    *reinterpret_cast<float4*>(part + r * D + ch) = o;
-                    if (ch == 0) {
-                        part[R * D + r] = M;
-                        part[R * D + R + r] = L;
+#pragma unroll
+                for (int i = 0; i < RB; ++i) {
+                    const int r = r0 + i;
+                    if (!on || r >= pc.n) continue;
+                    if (complete) {
+                        finish_row(pc, r, M[i], L[i], o[i], ch);
+                    } else {
+                        *reinterpret_cast<float4*>(part + r * D + ch) = o[i];
+                        if (ch == 0) {
+                            part[R * D + r] = M[i];
+                            part[R * D + R + r] = L[i];
+                        }
                     }
                 }
             }
-            if (!complete) {
-                // the last of the segment's CTAs joins the parts
-                const long long c0 = ((pc.seg + 1) * active - 1) / total, c1 = ((pc.seg + pc.pages) * active - 1) / total;
-                __syncthreads();
-                if (tid == 0) {
-                    __threadfence();
-                    sh.last = take_ticket(a.tickets + c0) == (unsigned int)(c1 - c0);
-                    if (sh.last) a.tickets[c0] = 0;
+        };
+        const bool few = __popc(starts) * 2 < W;   // few groups: a row per warp, else four rows at a time
+        int done = 0;                              // row batches dealt with so far, modulo W
+        while (starts) {
+            const int p = __ffs(starts) - 1;
+            starts &= starts - 1;
+            const unsigned int group = valid & ~((1u << p) - 1u) & (starts ? (1u << (__ffs(starts) - 1)) - 1u : 0xFFFFFFFFu);
+            const KvPiece pc = sh.piece[p];
+            const bool complete = pc.seg >= U0 && pc.seg + pc.pages <= U1;
+            const int which = pc.seg < U0 ? 0 : 1;   // scratch slot of this CTA
+            if (!complete) open[which] = p;
+            float* part = a.cta_parts + (c * 2 + which) * kPart;
+            const int batches = few ? pc.n : (pc.n + 3) / 4;
+            int k = warp - done;
+            k += k < 0 ? W : 0;
+            done = (done + batches) % W;
+            for (; k < batches; k += W) {
+                if (few) join_rows(std::integral_constant<int, 1>(), pc, group, complete, part, k);
+                else join_rows(std::integral_constant<int, 4>(), pc, group, complete, part, 4 * k);
+            }
+        }
+        // the last CTA that delivers a part of a segment joins them all
+        if (open[0] >= 0 || open[1] >= 0) {
+            __syncthreads();
+            if (tid < 2) {
+                int last = 0;
+                if (open[tid] >= 0) {
+                    const KvPiece pc = sh.piece[open[tid]];
+                    const long long c0 = shares.owner(pc.seg) / W, c1 = shares.owner(pc.seg + pc.pages - 1) / W;
+                    last = take_ticket(a.tickets + c0) == (unsigned int)(c1 - c0);
+                    if (last) a.tickets[c0] = 0;
                 }
-                __syncthreads();
-                if (sh.last) {
-                    // weights of the parts first, one row per warp, so that the sums below are a stream of
-                    // independent loads
-                    const int parts = (int)(c1 - c0) + 1;
-                    float* wgt = reinterpret_cast<float*>(sh.ring[0][0]) + R * TS;   // (behind the first warp's piece)
-                    for (int r = warp; r < pc.n; r += W) {
-                        float M = kKvNothing;
-                        for (int k = lane; k < parts; k += 32) M = fmaxf(M, __ldcg(a.cta_parts + ((c0 + k) * 2 + (k == 0)) * kPart + R * D + r));
+                sh.last[tid] = last;
+            }
+            __syncthreads();
 #pragma unroll
-                        for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
-                        float L = 0.f;
-                        for (int k = lane; k < parts; k += 32) {
-                            const float* from = a.cta_parts + ((c0 + k) * 2 + (k == 0)) * kPart + R * D + r;
-                            const float f = ex2_approx(__ldcg(from) - M);
-                            wgt[r * kKvMaxCtas + k] = f;
-                            L = fmaf(__ldcg(from + R), f, L);
-                        }
+            for (int which = 0; which < 2; ++which) {
+                if (!sh.last[which]) continue;
+                const KvPiece pc = sh.piece[open[which]];
+                const long long c0 = shares.owner(pc.seg) / W;
+                const int parts = (int)(shares.owner(pc.seg + pc.pages - 1) / W - c0) + 1;
+                const float* base = a.cta_parts + c0 * 2 * kPart;   // part k: 2 k, the first one's 1
+                for (int r = warp; r < pc.n; r += W) {
+                    constexpr int NK = (kKvMaxCtas + 31) / 32;
+                    float M = kKvNothing, L = 0.f;
+                    float m[NK], l[NK];
 #pragma unroll
-                        for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xFFFFFFFFu, L, o);
-                        if (lane == 0) {
-                            sh.m[0][r] = M;
-                            sh.l[0][r] = L;
+                    for (int i = 0; i < NK; ++i) {
+                        const int k = 32 * i + lane;
+                        const float* from = base + (2 * k + (k == 0)) * kPart + R * D + r;
+                        m[i] = kKvNothing;
+                        l[i] = 0.f;
+                        if (k < parts) {
+                            m[i] = __ldcg(from);
+                            l[i] = __ldcg(from + R);
                         }
+                        M = fmaxf(M, m[i]);
                     }
-                    __syncthreads();
-                    for (int i = tid; i < pc.n * Q4; i += Sh::kThreads) {
-                        const int r = i / Q4, ch = (i - r * Q4) * 4;
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
+#pragma unroll
+                    for (int i = 0; i < NK; ++i) {
+                        m[i] = ex2_approx(m[i] - M);
+                        L = fmaf(l[i], m[i], L);
+                    }
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xFFFFFFFFu, L, o);
+                    for (int cb = 0; cb < D; cb += 128) {
+                        const int ch = cb + lane * 4;
+                        const bool on = ch < D;
                         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-                        const float* from = a.cta_parts + c0 * 2 * kPart + r * D + ch;
-#pragma unroll 8
-                        for (int k = 0; k < parts; ++k) {
-                            const float f = wgt[r * kKvMaxCtas + k];
-                            const float4 x = __ldcg(reinterpret_cast<const float4*>(from + (k * 2 + (k == 0)) * kPart));
-                            o.x = fmaf(x.x, f, o.x);
-                            o.y = fmaf(x.y, f, o.y);
-                            o.z = fmaf(x.z, f, o.z);
-                            o.w = fmaf(x.w, f, o.w);
+#pragma unroll
+                        for (int i = 0; i < NK; ++i) {
+                            for (int q0 = 0; q0 < min(32, parts - 32 * i); q0 += 8) {
+                                float4 x[8];
+#pragma unroll
+                                for (int q = 0; q < 8; ++q) {
+                                    const int k = 32 * i + q0 + q;
+                                    x[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+                                    if (on && k < parts) x[q] = __ldcg(reinterpret_cast<const float4*>(base + (2 * k + (k == 0)) * kPart + r * D + ch));
+                                }
+#pragma unroll
+                                for (int q = 0; q < 8; ++q) {
+                                    const float fk = __shfl_sync(0xFFFFFFFFu, m[i], q0 + q);
+                                    o.x = fmaf(x[q].x, fk, o.x);
+                                    o.y = fmaf(x[q].y, fk, o.y);
+                                    o.z = fmaf(x[q].z, fk, o.z);
+                                    o.w = fmaf(x[q].w, fk, o.w);
+                                }
+                            }
                         }
-                        const float L = sh.l[0][r], inv = L > 0.f ? 1.f / L : 0.f;
-                        const long long row = pc.row0 + r;
-                        const long long head = ((long long)pc.first + row / G) * a.p.n_q_heads + pc.h * G + row % G;
-                        store4<DT>(a.o.out, head * D + ch, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), a.out_vec);
-                        if (a.o.lse != nullptr && ch == 0) a.o.lse[head] = L > 0.f ? (sh.m[0][r] + log2f(L)) * (float)kLn2 : -CUDART_INF_F;
+                        if (on) finish_row(pc, r, M, L, o, ch);
                     }
-                    __syncthreads();
                 }
             }
-            p = e;
         }
     }
     kv_clear_rows<DT>(a, D, (int)(blockIdx.x * W + warp), (int)(gridDim.x * W));

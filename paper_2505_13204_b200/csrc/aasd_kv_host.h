@@ -17,7 +17,7 @@ struct KvScratch {
 };
 constexpr KvScratch kv_attend_scratch(int head_dim) {
     KvScratch L{};
-    const size_t D = (size_t)head_dim, R = 16, W = 8;
+    const size_t D = (size_t)head_dim, R = 16, W = 12;
     L.zero_bytes = align_up(4 * kKvMaxCtas, 256);
     L.off_cta = L.zero_bytes;
     L.off_warp = align_up(L.off_cta + kKvMaxCtas * 2 * (R * D + 2 * R) * 4, 256);
