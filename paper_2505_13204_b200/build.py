@@ -24,7 +24,7 @@ UNITS = [("aasd.cu", "host", [])] + [
     for src in ("aasd_verify.cu", "aasd_align.cu", "aasd_align_gumbel.cu", "aasd_tree.cu", "aasd_kv_attend.cu")
     for dt in (1, 0)] + [("aasd_kv.cu", "kv", [])]
 DEPENDS = ["aasd.cu", "aasd_verify.cu", "aasd_align.cu", "aasd_align_gumbel.cu", "aasd_tree.cu", "aasd_host.h",
-           "aasd_kv.cu", "aasd_kv_attend.cu", "aasd_kv_host.h", "aasd_kv.cuh", "aasd_kv_attend.cuh",
+           "aasd_kv.cu", "aasd_kv_attend.cu", "aasd_kv_host.h", "aasd_kv.cuh", "aasd_kv_attend.cuh", "aasd_kv_tile.cuh",
            "aasd_device.cuh", "aasd_rows.cuh", "aasd_sampler.cuh", "aasd_stream.cuh", "aasd_tokens.cuh",
            "aasd_tree.cuh", os.path.join("..", "..", "include", "aasd.h")]
 # -fno-gnu-unique / -Bsymbolic: two builds of the library (the normal and the checked one) can

@@ -10,6 +10,9 @@ namespace aasd {
 
 namespace {
 
+// Rows per key/value head up to which the split kernel takes bf16 queries.
+constexpr int64_t kSplitRows = 16;
+
 template <int DT, int D, int NT>
 int launch_split(const LaunchEnv& env, int sm_count, const KvAttendArgs& a) {
     constexpr auto kernel = kv_attend_split_kernel<DT, D, NT>;
@@ -19,6 +22,24 @@ int launch_split(const LaunchEnv& env, int sm_count, const KvAttendArgs& a) {
     launch(kernel, (unsigned int)(sm_count < kKvMaxCtas ? sm_count : kKvMaxCtas), (unsigned int)KvSplitShape<DT, D, NT>::kThreads, smem, env.stream, a);
     return AASD_OK;
 }
+
+#if AASD_DT == 1
+template <int D, bool PAIR>
+int launch_tile(const LaunchEnv& env, int sm_count, const KvAttendArgs& a) {
+    constexpr auto kernel = kv_attend_tile_kernel<D, PAIR>;
+    constexpr size_t smem = sizeof(KvTileShared<D, PAIR>) + 1024;   // (its first member wants a 1024-byte boundary)
+    static_assert(smem <= 227 * 1024, "fits an SM");
+    if (enable_smem<kernel, smem>(env.device) != AASD_OK) return AASD_ERR_CUDA;
+    // the softmax warps wait for registers that the launch must have brought along
+    static const bool enough = [] {
+        cudaFuncAttributes f;
+        return cudaFuncGetAttributes(&f, kernel) == cudaSuccess && f.numRegs >= kTileLaunchRegs;
+    }();
+    if (!enough) return AASD_ERR_UNSUPPORTED;
+    launch(kernel, (unsigned int)(sm_count < kKvMaxCtas ? sm_count : kKvMaxCtas), (unsigned int)kTileThreads, smem, env.stream, a);
+    return AASD_OK;
+}
+#endif
 
 }  // namespace
 
@@ -38,6 +59,12 @@ int launch_kv_attend_bf16(const LaunchEnv& env, int sm_count, const KvAttendArgs
     const int64_t per_seq = a.p.rows_per_seq > 0 ? a.p.rows_per_seq : (a.p.n_tokens + a.p.n_seqs - 1) / (a.p.n_seqs > 0 ? a.p.n_seqs : 1);
     const int64_t rows = per_seq * (a.p.n_q_heads / a.p.n_kv_heads);
     *launches = 1;
+#if AASD_DT == 1
+    if (rows > kSplitRows && a.p.head_dim <= 128) {
+        if (a.p.head_dim == 64) return rows > kTileRows ? launch_tile<64, true>(env, sm_count, a) : launch_tile<64, false>(env, sm_count, a);
+        return rows > kTileRows ? launch_tile<128, true>(env, sm_count, a) : launch_tile<128, false>(env, sm_count, a);
+    }
+#endif
     if (a.p.head_dim == 64)
         return rows > 8 ? launch_split<DT, 64, 2>(env, sm_count, a) : launch_split<DT, 64, 1>(env, sm_count, a);
     if (a.p.head_dim == 128)

@@ -120,6 +120,7 @@ struct KvCursor {
 // `total` units in `n` shares that differ by one unit at most, the larger ones first.
 struct KvShares {
     long long each, more;     // units of a small share; shares with one more
+    KvShares() = default;
     __device__ __forceinline__ KvShares(long long total, long long n) {
         if (total < 0x7FFFFFFFLL) each = (long long)((unsigned int)total / (unsigned int)n);
         else each = total / n;
@@ -141,23 +142,22 @@ struct KvSegment {
     long long unit;           // of page 0
 };
 
-// Bit j of the result: new token (64 pg + j - cached) of the sequence's tokens, or a cached one at
-// that place, is seen by new token i.
-__device__ __forceinline__ u64 kv_seen(const KvAttendArgs& a, const KvSegment& s, int pg, int i) {
-    const long long at = (long long)pg * kPage;
-    if (i >= s.fresh) return 0ull;
-    const long long before = s.cached - at;                       // cached tokens of this page
+// Bit j of the result: place 64 pg + j of a sequence (a cached token or a new one) is seen by its new
+// token i.  cached, fresh, first: see KvSeq.
+__device__ __forceinline__ u64 kv_seen(const KvAttendArgs& a, int cached, int fresh, int first, int pg, int i) {
+    if (i >= fresh) return 0ull;
+    const int before = cached - pg * kPage;                       // cached tokens of this page
     u64 seen = before >= kPage ? ~0ull : before <= 0 ? 0ull : (1ull << before) - 1ull;
     if (a.node_parent == nullptr) {
-        const long long upto = (long long)s.cached + i + 1 - at;  // causal
+        const int upto = before + i + 1;                          // causal
         return upto >= kPage ? ~0ull : upto <= 0 ? 0ull : (1ull << upto) - 1ull;
     }
     int x = i;
     while (x >= 0) {
-        const long long j = (long long)s.cached + x - at;
+        const int j = before + x;
         if (j < 0) break;                                         // ancestors only get smaller
         if (j < kPage) seen |= 1ull << j;
-        const int p = a.node_parent[s.first + x];
+        const int p = a.node_parent[first + x];
         if (p >= x || p < AASD_NONE) {
             raise(a.state, AASD_STATUS_BAD_OFFSETS);
             break;
@@ -496,7 +496,8 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
                             for (int i = 0; i < 4; ++i) oacc[nt][half][q][i] = 0.f;
                 }
             }
-            if (!mbar_wait(&full[stage], phase, abort_flag, kWaitLimit)) {
+            // (the lanes of a warp go on, or give up, together)
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait(&full[stage], phase, abort_flag, kWaitLimit))) {
                 give_up(abort_flag, a.state);
                 break;
             }
@@ -580,7 +581,7 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int col = 0; col < 2; ++col) {
-                            const u64 seen = kv_seen(a, at, pg, (at.row0 + 8 * nt + 2 * j + col) / G);
+                            const u64 seen = kv_seen(a, at.cached, at.fresh, at.first, pg, (at.row0 + 8 * nt + 2 * j + col) / G);
 #pragma unroll
                             for (int mt = 0; mt < 4; ++mt)
 #pragma unroll

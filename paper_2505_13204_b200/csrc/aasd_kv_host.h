@@ -7,6 +7,7 @@
 #include "aasd_host.h"
 #include "aasd_kv.cuh"
 #include "aasd_kv_attend.cuh"
+#include "aasd_kv_tile.cuh"
 
 namespace aasd {
 
@@ -17,11 +18,13 @@ struct KvScratch {
 };
 constexpr KvScratch kv_attend_scratch(int head_dim) {
     KvScratch L{};
-    const size_t D = (size_t)head_dim, R = 16, W = 12;
+    // a scratch for one head dimension serves the smaller ones too
+    const size_t D = (size_t)head_dim, W = 12;
+    const size_t part = 2 * kTileRows * ((D < 128 ? D : 128) + 2);   // the largest: two tiles of 128 rows (head_dim 256 has parts of 8 rows)
     L.zero_bytes = align_up(4 * kKvMaxCtas, 256);
     L.off_cta = L.zero_bytes;
-    L.off_warp = align_up(L.off_cta + kKvMaxCtas * 2 * (R * D + 2 * R) * 4, 256);
-    L.bytes = align_up(L.off_warp + kKvMaxCtas * W * R * (D + 4) * 4, 256);
+    L.off_warp = align_up(L.off_cta + kKvMaxCtas * 2 * part * 4, 256);
+    L.bytes = align_up(L.off_warp + kKvMaxCtas * W * 16 * (D + 4) * 4, 256);
     return L;
 }
 
