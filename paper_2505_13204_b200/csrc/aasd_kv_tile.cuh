@@ -3,17 +3,22 @@
 //
 // One persistent CTA per SM; its warps have roles:
 //   loader      brings pages (packed blocks) in by bulk copies;
-//   unpackers   (4 warps) turn a page's codes into fp16 operands in shared memory, K-major rows of
-//               128 bytes in the 128-byte swizzle, one AND per two codes (see aasd_kv_attend.cuh), and
-//               its scales into fp32;
-//   issuer      one thread issues tcgen05.mma: S = Q K^T, O += P V, with Q and P read from tensor memory
-//               (so that the shared-memory port serves the keys and values alone);
+//   unpackers   (4 warps) turn a page's codes into fp16 operands in shared memory, K-major rows of 128
+//               bytes in the 128-byte swizzle;
+//   two issuers, one thread each: tcgen05.mma of S = Q K^T (both operands in shared memory) and
+//               O += P V (P in tensor memory) for one softmax group, a page (64 tokens) at a time;
 //   two softmax groups of 4 warps, a thread per row: S to registers, probabilities back as P.
 // The two groups work on two row tiles of the same pages (PAIR), or, where a segment has no more
-// than 128 rows, on alternate pages of one tile, joined at the end: while one group computes
-// exponentials the tensor cores work for the other.
+// than 128 rows, on alternate pages of one tile, joined at the end.  A group has two S buffers, so
+// that the next page's products are there when it is done with one.
 //
-// Tensor memory (512 columns): S of each group, whose first half P takes over, Q and O of each.
+// Keys stay bare codes, whose scale and minimum are applied to S (exactly: see aasd_kv_attend.cuh).
+// Values are expanded here, relative to the largest exponent of the segment's pages so far (so that
+// values of any size fit fp16), and rounded to 11 bits like the probabilities: a value is used for 128
+// rows, and scaling the probabilities instead, with a sum of the minima beside them, costs the
+// softmax groups, which pace the kernel, a third more instructions.
+//
+// Tensor memory (512 columns): two S buffers of each group, whose first halves P takes over, and O.
 #pragma once
 
 #include "aasd_kv_attend.cuh"
@@ -26,10 +31,9 @@ constexpr int kTileThreads = 512;      // 8 softmax warps, 4 unpackers; issuer, 
 constexpr int kTileLaunchRegs = 128, kTileSoftmaxRegs = 184, kTileOtherRegs = 72;
 static_assert(2 * kTileSoftmaxRegs + 2 * kTileOtherRegs <= 4 * kTileLaunchRegs, "the shares add up to the launch's registers");
 constexpr int kTileRows = 128;
-constexpr int kTileRaw = 4, kTileKeys = 3, kTileValues = 3, kTileMeta = 4;   // ring depths
+constexpr int kTileRaw = 4, kTileKeys = 3, kTileValues = 4, kTileMeta = 6;   // ring depths, in pages
 // the probabilities' power of two and the running maximum's lag (see the split kernel)
-constexpr int kTileP = 6;
-constexpr float kTileLazy = 8.f;
+constexpr float kTileP = 7.f, kTileLazy = 8.f;
 
 // ---- the list of work ---------------------------------------------------------------------------------
 
@@ -93,14 +97,15 @@ struct KvTileWalk {
 template <int D, bool PAIR>
 struct KvTileShared {
     static constexpr int R = PAIR ? 2 * kTileRows : kTileRows;
-    alignas(1024) unsigned char keys[kTileKeys][kPage * D * 2];
-    alignas(1024) unsigned char values[kTileValues][kPage * D * 2];
+    alignas(1024) unsigned char queries[PAIR ? 2 : 1][kTileRows * D * 2];
+    unsigned char keys[kTileKeys][kPage * D * 2];
+    unsigned char values[kTileValues][kPage * D * 2];
     alignas(128) unsigned char raw[kTileRaw][kv_head_bytes(D)];
-    alignas(16) float4 kmeta[kTileMeta][kPage / 2], vmeta[kTileMeta][kPage / 2];   // token pairs: scales, minima
-    int ev[kTileMeta];                 // exponent field that the values' scales are relative to; -1: page hidden
+    float4 kmeta[kTileMeta][kPage / 2];   // token pairs: the keys' scales, and minima
+    uint4 vmeta[4][kPage / 4];         // per unpacking warp, four tokens each: scales of 0 and 2, 1 and 3, minima likewise
+    int ev[kTileMeta];                 // exponent field that a page's values are relative to; -1: page hidden
     int raw_missing[kTileRaw];
-    float exchange[PAIR ? 4 : kTileRows * (D + 4)];
-    float exchange_m[kTileRows], exchange_l[kTileRows];
+    float exchange_m[kTileRows], exchange_l[kTileRows], exchange_up[kTileRows];   // between the groups, where they share a tile
     long long base[kTileThreads];
     long long scan[kTileThreads / 32];
     KvTileWalk start;                  // the CTA's share of the work: where it begins, and the unit behind its last one
@@ -110,7 +115,7 @@ struct KvTileShared {
     u64 raw_full[kTileRaw], raw_empty[kTileRaw];
     u64 k_full[kTileKeys], k_empty[kTileKeys], v_full[kTileValues], v_empty[kTileValues];
     u64 m_full[kTileMeta], m_empty[kTileMeta];
-    u64 q_full[2], s_full[2], p_full[2], o_done[2], x_full, x_empty, drain;
+    u64 q_full[2], s_full[2][2], p_full[2][2], o_done[2], x_full, x_empty, r_full, drain[2];
     unsigned int tmem;
     int abort_flag, last[2];
 };
@@ -135,6 +140,14 @@ __device__ __forceinline__ void tc_mma(unsigned int d, unsigned int a, u64 b, un
         "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
         "r"(a), "l"(b), "r"(idesc), "r"(add ? 1u : 0u)
+        : "memory");
+}
+// ... with A in shared memory
+__device__ __forceinline__ void tc_mma_ss(unsigned int d, u64 a, u64 b, unsigned int idesc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(add ? 1u : 0u)
         : "memory");
 }
 // fp32 result, fp16 operands, both K-major, M = 128
@@ -165,6 +178,15 @@ __device__ __forceinline__ void tc_store8(unsigned int addr, unsigned int x0, un
                  : "memory");
 }
 __device__ __forceinline__ void tc_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ __half2 as_half2(unsigned int x) { return *reinterpret_cast<const __half2*>(&x); }
+// Values of two codes of a word (those in bits 0-3 and 16-19, or 4-7 and 20-23).
+template <bool HIGH>
+__device__ __forceinline__ unsigned int expand(unsigned int w, __half2 scale, __half2 minimum) {
+    const unsigned int b = (w & (HIGH ? 0x00F000F0u : 0x000F000Fu)) | 0x64006400u;     // 1024 + c, or 1024 + 16 c
+    const __half2 c = HIGH ? __hfma2(as_half2(b), __float2half2_rn(0.0625f), __float2half2_rn(-64.f)) : __hsub2(as_half2(b), __float2half2_rn(1024.f));
+    const __half2 v = __hfma2(c, scale, minimum);
+    return *reinterpret_cast<const unsigned int*>(&v);
+}
 template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
@@ -178,8 +200,7 @@ template <int D, bool PAIR>
 __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const KvAttendArgs a) {
     using Shared = KvTileShared<D, PAIR>;
     constexpr int R = Shared::R, H = D / 2;
-    constexpr unsigned int kColS = 0, kColQ = 128, kColO = 256;    // first columns of group 0's S, Q, O
-    constexpr unsigned int kStepS = 64, kStepQ = D / 2, kStepO = D;   // and how far group 1's are behind
+    constexpr unsigned int kColS = 0, kColO = 256, kStep = 128;    // first columns of group 0's S and O; group 1's are kStep behind
     constexpr unsigned int kIdescS = tc_idesc(kPage), kIdescO = tc_idesc(D);
     extern __shared__ unsigned char smem_raw[];
     Shared& sh = *reinterpret_cast<Shared*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
@@ -192,11 +213,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
         }
         for (int i = 0; i < kTileKeys; ++i) {
             mbar_init(&sh.k_full[i], 4);
-            mbar_init(&sh.k_empty[i], 1);
+            mbar_init(&sh.k_empty[i], PAIR ? 2 : 1);
         }
         for (int i = 0; i < kTileValues; ++i) {
             mbar_init(&sh.v_full[i], 4);
-            mbar_init(&sh.v_empty[i], 1);
+            mbar_init(&sh.v_empty[i], PAIR ? 2 : 1);
         }
         for (int i = 0; i < kTileMeta; ++i) {
             mbar_init(&sh.m_full[i], 4);
@@ -204,14 +225,17 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.q_full[i], 4);
-            mbar_init(&sh.s_full[i], 1);
-            mbar_init(&sh.p_full[i], 4);
+            for (int b = 0; b < 2; ++b) {
+                mbar_init(&sh.s_full[i][b], 1);
+                mbar_init(&sh.p_full[i][b], 4);
+            }
             mbar_init(&sh.o_done[i], 1);
+            mbar_init(&sh.drain[i], 1);
             sh.open[i].seg = -1;
         }
         mbar_init(&sh.x_full, 4);
         mbar_init(&sh.x_empty, 4);
-        mbar_init(&sh.drain, 1);
+        mbar_init(&sh.r_full, 4);
         sh.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -322,121 +346,115 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
             if (*abort_flag)   // nothing may be on its way into this CTA's shared memory when it leaves
                 for (int k = max(0, n - kTileRaw); k < n; ++k)
                     for (unsigned int it = 0; it < kWaitLimit && !mbar_try_wait(&sh.raw_full[k % kTileRaw], (k / kTileRaw) & 1); ++it) {}
-        } else if (warp == 12) {
-            // ---- issuer: job k multiplies for group k & 1
+        } else if (warp == 12 || warp == 14) {
+            // ---- issuers: warp 12 for group 0, warp 14 for group 1
             if (lane == 0) {
-                struct Jobs {
+                const int x = (warp - 12) >> 1;
+                // The group's pages: all of a piece, or every other page of the share.
+                struct Pages {
                     KvTileWalk w;
-                    int np, i, n, x, piece;   // pages of the piece, page in it, page of the share, group, piece of the share
+                    int np, i, n, j, piece;   // pages of the piece, page in it, page of the share, of the group, piece of the share
+                    bool first;               // of the group in this piece
+                };
+                auto skip = [&](Pages& p) {   // one page on, into the next piece if need be
+                    ++p.n;
+                    if (++p.i == p.np) {
+                        p.i = 0;
+                        ++p.piece;
+                        p.first = true;
+                        p.w.next(a, R, G);
+                        if (p.w.live()) p.np = p.w.piece_pages();
+                    }
                 };
                 auto begin = [&]() {
-                    Jobs j{sh.start, sh.start.piece_pages(), 0, 0, 0, 0};
-                    return j;
+                    Pages p{sh.start, sh.start.piece_pages(), 0, 0, 0, 0, true};
+                    if (!PAIR && x == 1 && p.w.live()) skip(p);
+                    return p;
                 };
-                auto step = [&](Jobs& j) {
-                    if (PAIR) {
-                        j.x ^= 1;
-                        if (j.x) return;
-                    }
-                    ++j.n;
-                    if (!PAIR) j.x = j.n & 1;
-                    if (++j.i == j.np) {
-                        j.i = 0;
-                        ++j.piece;
-                        j.w.next(a, R, G);
-                        if (j.w.live()) j.np = j.w.piece_pages();
-                    }
+                auto step = [&](Pages& p) {
+                    p.first = false;
+                    ++p.j;
+                    skip(p);
+                    if (!PAIR && p.w.live()) skip(p);
                 };
                 bool ok = true;
-                int asked[2] = {0, 0};   // pieces whose queries have been waited for
-                auto multiply_keys = [&](Jobs& j) {
-                    const int slot = j.n % kTileKeys;
-                    while (ok && asked[j.x] <= j.piece) {
-                        ok = wait_one(&sh.q_full[j.x], asked[j.x] & 1);
-                        ++asked[j.x];
+                int asked = 0;           // pieces whose queries have been waited for
+                auto multiply_keys = [&](Pages& p) {
+                    const int slot = p.n % kTileKeys, buf = p.j & 1;
+                    while (ok && asked <= p.piece) {
+                        ok = wait_one(&sh.q_full[x], asked & 1);
+                        ++asked;
                     }
-                    ok = ok && wait_one(&sh.k_full[slot], (j.n / kTileKeys) & 1);
+                    ok = ok && wait_one(&sh.k_full[slot], (p.n / kTileKeys) & 1);
                     if (!ok) return;
                     tc_fence_after();
-                    const unsigned int keys = smem_u32(sh.keys[slot]);
+                    const u64 q = tc_desc(smem_u32(sh.queries[PAIR ? x : 0])), k = tc_desc(smem_u32(sh.keys[slot]));
 #pragma unroll
-                    for (int ks = 0; ks < D / 16; ++ks)
-                        tc_mma(tm + kColS + j.x * kStepS, tm + kColQ + j.x * kStepQ + ks * 8, tc_desc(keys + (ks / 4) * (kPage * 128) + (ks % 4) * 32),
-                               kIdescS, ks > 0);
-                    tc_commit(&sh.s_full[j.x]);
-                    if (!PAIR || j.x) tc_commit(&sh.k_empty[slot]);
-                    step(j);
+                    for (int ks = 0; ks < D / 16; ++ks)   // (descriptors count 16 bytes; a panel is 64 channels of all rows)
+                        tc_mma_ss(tm + kColS + x * kStep + buf * 64, q + (ks / 4) * (kTileRows * 8) + (ks % 4) * 2,
+                                  k + (ks / 4) * (kPage * 8) + (ks % 4) * 2, kIdescS, ks > 0);
+                    tc_commit(&sh.s_full[x][buf]);
+                    tc_commit(&sh.k_empty[slot]);
+                    step(p);
                 };
-                int given[2] = {0, 0};   // probabilities taken, per group
-                Jobs keys = begin(), vals = begin();
-                for (int k = 0; k < 2 && ok && keys.w.live(); ++k) multiply_keys(keys);
+                Pages keys = begin(), vals = begin();
                 while (ok && vals.w.live()) {
-                    const int slot = vals.n % kTileValues, x = vals.x;
-                    ok = wait_one(&sh.v_full[slot], (vals.n / kTileValues) & 1) && wait_one(&sh.p_full[x], given[x] & 1);
+                    // (not into the next piece: its queries come when this one's last page is in O)
+                    while (ok && keys.w.live() && keys.piece == vals.piece && keys.j < vals.j + 2) multiply_keys(keys);
+                    const int slot = vals.n % kTileValues, buf = vals.j & 1;
+                    ok = ok && wait_one(&sh.v_full[slot], (vals.n / kTileValues) & 1) && wait_one(&sh.p_full[x][buf], (vals.j >> 1) & 1);
                     if (!ok) break;
-                    ++given[x];
                     tc_fence_after();
-                    const bool first = PAIR ? vals.i == 0 : vals.i < 2;
-                    const unsigned int values = smem_u32(sh.values[slot]);
+                    const u64 v = tc_desc(smem_u32(sh.values[slot]));
 #pragma unroll
                     for (int ks = 0; ks < kPage / 16; ++ks)
-                        tc_mma(tm + kColO + x * kStepO, tm + kColS + x * kStepS + ks * 8, tc_desc(values + ks * 32), kIdescO, !first || ks > 0);
-                    if (!PAIR || x) tc_commit(&sh.v_empty[slot]);
-                    if (PAIR ? vals.i == vals.np - 1 : vals.i >= vals.np - 2) tc_commit(&sh.o_done[x]);
+                        tc_mma(tm + kColO + x * kStep, tm + kColS + x * kStep + buf * 64 + ks * 8, v + ks * 2, kIdescO, !vals.first || ks > 0);
+                    tc_commit(&sh.v_empty[slot]);
+                    tc_commit(&sh.o_done[x]);
                     step(vals);
-                    if (keys.w.live()) multiply_keys(keys);
                 }
                 // products in flight read this CTA's shared memory
-                tc_commit(&sh.drain);
-                for (unsigned int it = 0; it < kWaitLimit && !mbar_try_wait(&sh.drain, 0); ++it) {}
+                tc_commit(&sh.drain[x]);
+                for (unsigned int it = 0; it < kWaitLimit && !mbar_try_wait(&sh.drain[x], 0); ++it) {}
             }
             __syncwarp();
         }
     } else if (warp >= 8) {
         // ---- unpackers
         fewer_registers<kTileOtherRegs>();
-        const int u = tid - 256;
+        const int u = tid - 256, uw = warp - 8;
         int n = 0;
         bool ok = true;
         for (KvTileWalk w = sh.start; ok && w.live(); w.next(a, R, G)) {
             const int np = w.piece_pages();
             int ev = 64;
-            for (int i = 0; i < np && ok; ++i, ++n) {
-                const int slot = n % kTileRaw, mslot = n % kTileMeta;
-                ok = wait(&sh.raw_full[slot], (n / kTileRaw) & 1) && wait(&sh.m_empty[mslot], ((n / kTileMeta) & 1) ^ 1);
+            for (int i = 0; i < np; ++i, ++n) {
+                const int slot = n % kTileRaw, mslot = n % kTileMeta, kslot = n % kTileKeys, vslot = n % kTileValues;
+                ok = wait(&sh.raw_full[slot], (n / kTileRaw) & 1) && wait(&sh.m_empty[mslot], ((n / kTileMeta) & 1) ^ 1) &&
+                     wait(&sh.k_empty[kslot], ((n / kTileKeys) & 1) ^ 1);
                 if (!ok) break;
                 const unsigned char* raw = sh.raw[slot];
                 const bool missing = sh.raw_missing[slot] != 0;
                 const int left = missing ? 0 : w.cached + w.fresh - (w.pg + i) * kPage;   // places in use
-                // scales: thread u < 64 has token u
-                unsigned int km = 0, vm = 0;
-                if (u < kPage && u < left) {
-                    km = *reinterpret_cast<const unsigned int*>(raw + kv_key_meta_offset(D) + 4 * u);
-                    vm = *reinterpret_cast<const unsigned int*>(raw + kv_value_meta_offset(D) + 4 * u);
-                }
-                // (every warp finds the page's largest value scale for itself)
-                const uint2 both = *reinterpret_cast<const uint2*>(raw + kv_value_meta_offset(D) + 8 * lane);
-                const unsigned int mine_top = max(2 * lane < left ? both.x & 0xFFFFu : 0u, 2 * lane + 1 < left ? both.y & 0xFFFFu : 0u);
-                ev = max(ev, min(250, (int)(__reduce_max_sync(0xFFFFFFFFu, mine_top) >> 7)));
+                // largest value of the page (every warp for itself): codes run from the minimum to 15 scales above it
+                const uint2 vm = *reinterpret_cast<const uint2*>(raw + kv_value_meta_offset(D) + 8 * lane);
+                auto reach = [](unsigned int m) { return fmaxf(fabsf(meta_min(m)), fabsf(fmaf(15.f, meta_scale(m), meta_min(m)))); };
+                float vt = 2 * lane < left ? reach(vm.x) : 0.f;
+                if (2 * lane + 1 < left) vt = fmaxf(vt, reach(vm.y));
+                // (an exponent field, held to a range in which the factors below are normal numbers)
+                ev = max(ev, min(250, (int)(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(vt)) >> 23)));
                 if (u < kPage) {
+                    const unsigned int km = u < left ? *reinterpret_cast<const unsigned int*>(raw + kv_key_meta_offset(D) + 4 * u) : 0u;
                     float* kq = reinterpret_cast<float*>(&sh.kmeta[mslot][u >> 1]);
-                    float* vq = reinterpret_cast<float*>(&sh.vmeta[mslot][u >> 1]);
                     kq[u & 1] = meta_scale(km);
                     kq[2 + (u & 1)] = meta_min(km);
-                    vq[u & 1] = meta_scale(vm) * pow2f(kTileP - (ev - 127));
-                    vq[2 + (u & 1)] = meta_min(vm);
-                    if (u == 0) sh.ev[mslot] = missing ? -1 - ev : ev;
+                    if (u == 0) sh.ev[mslot] = missing ? -1 : ev;
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.m_full[mslot]);
-                // keys: half a token's row per thread.  Word k of a token (channels 4k .. of each half) becomes
-                // 16-byte piece k of its row; the two threads of a token take their pieces in orders that keep
-                // eight neighbouring threads on eight different pieces.
-                constexpr int NW = H / 8;                       // words per thread: a token's H / 4, halved
-                const int kslot = n % kTileKeys;
-                ok = wait(&sh.k_empty[kslot], ((n / kTileKeys) & 1) ^ 1);
-                if (!ok) break;
                 {
+                    // keys: half a token's row per thread.  Word k of a token (channels 4k .. of each half) becomes
+                    // 16-byte piece k of its row; the two threads of a token take their pieces in orders that keep
+                    // eight neighbouring threads on eight different pieces.
+                    constexpr int NW = H / 8;                       // words per thread: a token's H / 4, halved
                     const int t = u >> 1, part = u & 1;
                     const unsigned char* from = raw + t * H + part * (H / 2);
                     unsigned int wd[NW];
@@ -451,37 +469,51 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                         const int kk = NW == 8 ? k ^ (part * 4) : k;
                         const unsigned int x = NW == 8 ? (part ? wd[k ^ 4] : wd[k]) : wd[k], y = x >> 8;
                         const int piece = part * NW + kk;        // of the token's H / 4
-                        const uint4 o = make_uint4(x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u);
-                        *reinterpret_cast<uint4*>(to + (piece >> 3) * (kPage * 128) + (((piece & 7) ^ (t & 7)) << 4)) = o;
+                        *reinterpret_cast<uint4*>(to + (piece >> 3) * (kPage * 128) + (((piece & 7) ^ (t & 7)) << 4)) =
+                            make_uint4(x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u);
                     }
+                }
+                // the values' table: lane q < 16 has tokens 4q .. 4q + 3, in the order in which their codes leave a word
+                const float norm = pow2f(127 - ev);
+                if (lane < kPage / 4) {
+                    const uint4 m = lds16(raw + kv_value_meta_offset(D) + 16 * lane);
+                    const unsigned int m0 = 4 * lane < left ? m.x : 0u, m1 = 4 * lane + 1 < left ? m.y : 0u, m2 = 4 * lane + 2 < left ? m.z : 0u,
+                                       m3 = 4 * lane + 3 < left ? m.w : 0u;
+                    sh.vmeta[uw][lane] = make_uint4(pack_half(meta_scale(m0) * norm, meta_scale(m2) * norm), pack_half(meta_scale(m1) * norm, meta_scale(m3) * norm),
+                                                    pack_half(meta_min(m0) * norm, meta_min(m2) * norm), pack_half(meta_min(m1) * norm, meta_min(m3) * norm));
                 }
                 fence_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.k_full[kslot]);
+                if (lane == 0) {
+                    mbar_arrive(&sh.k_full[kslot]);
+                    mbar_arrive(&sh.m_full[mslot]);
+                }
                 // values: rows of channels; 8 tokens of a channel are a 16-byte piece
-                const int vslot = n % kTileValues;
                 ok = wait(&sh.v_empty[vslot], ((n / kTileValues) & 1) ^ 1);
                 if (!ok) break;
-                {
-                    constexpr int TPR = 128 / H;                 // threads per channel-pair row
-                    constexpr int NP = 8 / TPR;                  // pieces per thread and half
-                    const int r = u / TPR, part = u % TPR;
-                    const unsigned char* from = raw + kv_value_offset(D) + r * kPage + part * (kPage / TPR);
-                    unsigned int wd[2 * NP];
+                constexpr int TPR = 128 / H;                 // threads per channel-pair row
+                constexpr int NP = 8 / TPR;                  // pieces per thread and half
+                const int r = u / TPR, part = u % TPR;
+                const unsigned char* from = raw + kv_value_offset(D) + r * kPage + part * (kPage / TPR);
+                unsigned int wd[2 * NP];
 #pragma unroll
-                    for (int k = 0; k < 2 * NP; k += 4) {
-                        const uint4 q = lds16(from + 4 * k);
-                        wd[k] = q.x; wd[k + 1] = q.y; wd[k + 2] = q.z; wd[k + 3] = q.w;
-                    }
-                    unsigned char* lo = sh.values[vslot] + r * 128;
-                    unsigned char* hi = lo + H * 128;            // (H is a multiple of 8: the same swizzle)
+                for (int k = 0; k < 2 * NP; k += 4) {
+                    const uint4 q = lds16(from + 4 * k);
+                    wd[k] = q.x; wd[k + 1] = q.y; wd[k + 2] = q.z; wd[k + 3] = q.w;
+                }
+                unsigned char* lo = sh.values[vslot] + r * 128;
+                unsigned char* hi = lo + H * 128;            // (H is a multiple of 8: the same swizzle)
 #pragma unroll
-                    for (int k = 0; k < NP; ++k) {
-                        const unsigned int x0 = wd[2 * k], x1 = wd[2 * k + 1], y0 = x0 >> 8, y1 = x1 >> 8;
-                        const int at = ((part * NP + k) ^ (r & 7)) << 4;
-                        *reinterpret_cast<uint4*>(lo + at) = make_uint4(x0 & 0x000F000Fu, y0 & 0x000F000Fu, x1 & 0x000F000Fu, y1 & 0x000F000Fu);
-                        *reinterpret_cast<uint4*>(hi + at) = make_uint4(x0 & 0x00F000F0u, y0 & 0x00F000F0u, x1 & 0x00F000F0u, y1 & 0x00F000F0u);
-                    }
+                for (int k = 0; k < NP; ++k) {
+                    const unsigned int x0 = wd[2 * k], x1 = wd[2 * k + 1], y0 = x0 >> 8, y1 = x1 >> 8;
+                    const uint4 q0 = sh.vmeta[uw][2 * (part * NP + k)], q1 = sh.vmeta[uw][2 * (part * NP + k) + 1];
+                    const __half2 s0 = as_half2(q0.x), s1 = as_half2(q0.y), m0 = as_half2(q0.z), m1 = as_half2(q0.w);
+                    const __half2 s2 = as_half2(q1.x), s3 = as_half2(q1.y), m2 = as_half2(q1.z), m3 = as_half2(q1.w);
+                    const int at = ((part * NP + k) ^ (r & 7)) << 4;
+                    *reinterpret_cast<uint4*>(lo + at) =
+                        make_uint4(expand<false>(x0, s0, m0), expand<false>(y0, s1, m1), expand<false>(x1, s2, m2), expand<false>(y1, s3, m3));
+                    *reinterpret_cast<uint4*>(hi + at) =
+                        make_uint4(expand<true>(x0, s0, m0), expand<true>(y0, s1, m1), expand<true>(x1, s2, m2), expand<true>(y1, s3, m3));
                 }
                 fence_async_smem();
                 __syncwarp();
@@ -496,17 +528,19 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
         more_registers<kTileSoftmaxRegs>();
         const int x = warp >> 2, row_in = tid & 127;
         const unsigned int lanes = (unsigned int)(warp & 3) << 21;         // the warp's lanes in an address: 32 (warp % 4) << 16
-        const unsigned int col_s = tm + kColS + x * kStepS + lanes, col_q = tm + kColQ + x * kStepQ + lanes, col_o = tm + kColO + x * kStepO + lanes;
-        int n0 = 0, jobs = 0, ends = 0, pieces = 0;    // pages before the piece; S tiles taken; results taken; pieces done
+        const unsigned int col_s = tm + kColS + x * kStep + lanes, col_o = tm + kColO + x * kStep + lanes;
+        int n0 = 0, taken = 0, added = 0, pieces = 0;    // pages before the piece; pages taken; pages known to be in O; pieces done
         bool ok = true;
         for (KvTileWalk w = sh.start; ok && w.live(); w.next(a, R, G)) {
             const int np = w.piece_pages();
             const int row = w.tile * R + (PAIR ? x * kTileRows : 0) + row_in;
             const bool valid = row < w.fresh * G;
-            const long long head = ((long long)w.first + (valid ? row / G : 0)) * a.p.n_q_heads + w.h * G + (valid ? row % G : 0);
-            float rfac, qfac;              // exponent (base 2) = rfac * (s q.c + m qfac)
-            {
-                const long long q0 = ((long long)w.first + (valid ? row / G : 0)) * a.p.q_stride + (long long)(w.h * G + (valid ? row % G : 0)) * D;
+            const int tok = valid ? row / G : 0;
+            const long long head = ((long long)w.first + tok) * a.p.n_q_heads + w.h * G + (valid ? row - tok * G : 0);
+            float rfac = 1.f, qfac = 0.f;  // exponent (base 2) of a product = rfac * (scale * S + minimum * qfac)
+            if (PAIR || x == 0) {
+                // the row's queries as fp16 numbers, its largest element 2^14 .. 2^15, channels in the order of the keys' words
+                const long long q0 = ((long long)w.first + tok) * a.p.q_stride + (head - ((long long)w.first + tok) * a.p.n_q_heads) * D;
                 float top = 0.f, sum = 0.f;
 #pragma unroll 4
                 for (int k = 0; k < D; k += 8) {
@@ -524,8 +558,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                 const float up = valid ? pow2f(14 - e) : 0.f;
                 rfac = fmaxf(a.scale_log2 * pow2f(e + 10), 1e-37f);   // (never 0: what is hidden is -inf times it)
                 qfac = valid ? sum * pow2f(-10 - e) : 0.f;
+                unsigned char* to = sh.queries[PAIR ? x : 0] + row_in * 128;
 #pragma unroll 4
-                for (int cb = 0; cb < H; cb += 8) {       // eight channels of each half are eight columns
+                for (int cb = 0; cb < H; cb += 8) {       // eight channels of each half are two 16-byte pieces
                     float lo[8], hi[8];
                     if (a.q_vec) {
                         load8<AASD_BF16, true>(a.q, q0 + cb, lo);
@@ -539,25 +574,45 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                         lo[q] = valid ? lo[q] * up : 0.f;
                         hi[q] = valid ? hi[q] * (up * 0.0625f) : 0.f;
                     }
-                    tc_store8(col_q + cb, pack_half(lo[0], lo[2]), pack_half(lo[1], lo[3]), pack_half(hi[0], hi[2]), pack_half(hi[1], hi[3]),
-                              pack_half(lo[4], lo[6]), pack_half(lo[5], lo[7]), pack_half(hi[4], hi[6]), pack_half(hi[5], hi[7]));
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const int piece = cb / 4 + q;
+                        *reinterpret_cast<uint4*>(to + (piece >> 3) * (kTileRows * 128) + (((piece & 7) ^ (row_in & 7)) << 4)) =
+                            make_uint4(pack_half(lo[4 * q], lo[4 * q + 2]), pack_half(lo[4 * q + 1], lo[4 * q + 3]), pack_half(hi[4 * q], hi[4 * q + 2]),
+                                       pack_half(hi[4 * q + 1], hi[4 * q + 3]));
+                    }
                 }
-                tc_wait_store();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sh.q_full[x]);
+                fence_async_smem();
+                if (!PAIR) {
+                    sh.exchange_up[row_in] = rfac;
+                    sh.exchange_m[row_in] = qfac;
+                }
             }
-            float mref = kKvNothing, l = 0.f, mv = 0.f;
+            if (!PAIR) {
+                // one set of queries for both groups
+                if (x == 0) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.r_full);
+                } else {
+                    ok = wait(&sh.r_full, pieces & 1);
+                    if (!ok) break;
+                    rfac = sh.exchange_up[row_in];
+                    qfac = sh.exchange_m[row_in];
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.q_full[x]);
+            float mref = kKvNothing, l = 0.f;
             int ev = 64;
             bool first = true;
+            float s[64];
             for (int i = PAIR ? 0 : (n0 ^ x) & 1; i < np; i += PAIR ? 1 : 2) {
-                const int n = n0 + i, mslot = n % kTileMeta, pg = w.pg + i;
-                ok = wait(&sh.m_full[mslot], (n / kTileMeta) & 1) && wait(&sh.s_full[x], jobs & 1);
-                ++jobs;
+                const int n = n0 + i, mslot = n % kTileMeta, pg = w.pg + i, buf = taken & 1;
+                const unsigned int col = col_s + buf * 64;
+                ok = wait(&sh.m_full[mslot], (n / kTileMeta) & 1) && wait(&sh.s_full[x][buf], (taken >> 1) & 1);
                 if (!ok) break;
                 tc_fence_after();
-                float s[64];
-                tc_load64(col_s, s);
+                tc_load64(col, s);
                 const int evn = sh.ev[mslot];
 #pragma unroll
                 for (int k = 0; k < 32; ++k) {
@@ -567,8 +622,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                     s[2 * k] = y.x;
                     s[2 * k + 1] = y.y;
                 }
-                if (evn < 0 || (pg + 1) * kPage > w.cached) {
-                    const u64 seen = evn < 0 || !valid ? 0ull : kv_seen(a, w.cached, w.fresh, w.first, pg, row / G);
+                if (evn < 0 || (pg + 1) * kPage > w.cached) {   // what the row does not see becomes -inf
+                    const u64 seen = evn < 0 || !valid ? 0ull : kv_seen(a, w.cached, w.fresh, w.first, pg, tok);
 #pragma unroll
                     for (int k = 0; k < 64; ++k)
                         if (!((seen >> k) & 1ull)) s[k] = -CUDART_INF_F;
@@ -582,16 +637,21 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                     m3 = fmaxf(m3, s[k + 3]);
                 }
                 const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * rfac;
-                const int en = evn < 0 ? ev : evn;
+                // (the page before is in O: the issuer's products of it ran during the steps above)
+                if (added < taken) {
+                    ok = wait(&sh.o_done[x], added & 1);
+                    ++added;
+                    if (!ok) break;
+                }
+                const int en = max(ev, evn);
                 if (__any_sync(0xFFFFFFFFu, top > mref + kTileLazy || en > ev)) {
                     const float mn = fmaxf(mref, top);
                     const float f = ex2_approx(mref - mn);
-                    const float fo = en - ev > 126 ? 0.f : f * pow2f(ev - en);
                     mref = mn;
-                    ev = en;
                     l *= f;
-                    mv *= f;
                     if (!first) {
+                        tc_fence_after();
+                        const float fo = en - ev > 126 ? 0.f : f * pow2f(ev - en);
 #pragma unroll
                         for (int cb = 0; cb < D; cb += 32) {
                             float o[32];
@@ -603,37 +663,35 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                                           __float_as_uint(o[k + 6] * fo), __float_as_uint(o[k + 7] * fo));
                         }
                     }
+                    ev = en;
                 }
                 first = false;
-                float2 ls = make_float2(l, 0.f), ms = make_float2(mv, 0.f);
+                // probabilities, to 32 columns in the order of the values' words
+                const float2 ff = make_float2(rfac, rfac), mm = make_float2(kTileP - mref, kTileP - mref);
+                float2 l0 = make_float2(0.f, 0.f), l1 = make_float2(0.f, 0.f);
 #pragma unroll
-                for (int kb = 0; kb < 4; ++kb) {             // sixteen tokens are eight columns of P
+                for (int kb = 0; kb < 4; ++kb) {             // sixteen tokens are eight columns
                     unsigned int pk[8];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        float2 p[2];
-#pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            const int t = 16 * kb + 4 * k + 2 * q;
-                            const float4 m = sh.vmeta[mslot][t / 2];
-                            const float2 y = __ffma2_rn(make_float2(s[t], s[t + 1]), make_float2(rfac, rfac), make_float2(-mref, -mref));
-                            p[q] = make_float2(ex2_approx(y.x), ex2_approx(y.y));
-                            ls = __fadd2_rn(ls, p[q]);
-                            ms = __ffma2_rn(p[q], make_float2(m.z, m.w), ms);
-                            p[q] = __fmul2_rn(p[q], make_float2(m.x, m.y));
-                        }
-                        pk[2 * k] = pack_half(p[0].x, p[1].x);
-                        pk[2 * k + 1] = pack_half(p[0].y, p[1].y);
+                        const int t = 16 * kb + 4 * k;
+                        float2 p = __ffma2_rn(make_float2(s[t], s[t + 1]), ff, mm), q = __ffma2_rn(make_float2(s[t + 2], s[t + 3]), ff, mm);
+                        p = make_float2(ex2_approx(p.x), ex2_approx(p.y));
+                        q = make_float2(ex2_approx(q.x), ex2_approx(q.y));
+                        l0 = __fadd2_rn(l0, p);
+                        l1 = __fadd2_rn(l1, q);
+                        pk[2 * k] = pack_half(p.x, q.x);
+                        pk[2 * k + 1] = pack_half(p.y, q.y);
                     }
-                    tc_store8(col_s + 8 * kb, pk[0], pk[1], pk[2], pk[3], pk[4], pk[5], pk[6], pk[7]);
+                    tc_store8(col + 8 * kb, pk[0], pk[1], pk[2], pk[3], pk[4], pk[5], pk[6], pk[7]);
                 }
-                l = ls.x + ls.y;
-                mv = ms.x + ms.y;
+                l += (l0.x + l0.y) + (l1.x + l1.y);
+                ++taken;
                 tc_wait_store();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) {
-                    mbar_arrive(&sh.p_full[x]);
+                    mbar_arrive(&sh.p_full[x][buf]);
                     mbar_arrive(&sh.m_empty[mslot]);
                 }
             }
@@ -641,56 +699,45 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
             // the result of the piece
             const bool any = !first;
             if (any) {
-                ok = wait(&sh.o_done[x], ends & 1);
-                ++ends;
+                ok = wait(&sh.o_done[x], added & 1);
+                ++added;
                 if (!ok) break;
                 tc_fence_after();
             }
-            const float unscale = pow2f((ev - 127) - kTileP);
+            float unscale = pow2f(ev - 127);
+            mref -= kTileP;                // (l and O carry the probabilities' power of two)
             const bool complete = w.pg == 0 && np == w.pages;
             const int which = w.pg > 0 ? 0 : 1;
             const int rows = min(R, w.fresh * G - w.tile * R);
             constexpr int kPart = R * D + 2 * R;
             const int r = (PAIR ? x * kTileRows : 0) + row_in;
             float* part = a.cta_parts + (c * 2 + which) * kPart;
-            float other_f = 0.f, own_f = 1.f;
+            float other = 0.f;             // factor of the other group's O
             if (!PAIR) {
-                // group 1 hands its pages' part to group 0
+                // group 0 reads both groups' O (the same lanes of tensor memory)
                 if (x == 1) {
-                    ok = wait(&sh.x_empty, (pieces & 1) ^ 1);
-                    if (!ok) break;
                     sh.exchange_m[row_in] = mref;
                     sh.exchange_l[row_in] = l;
-                    if (any) {
-#pragma unroll
-                        for (int cb = 0; cb < D; cb += 32) {
-                            float o[32];
-                            tc_load32(col_o + cb, o);
-                            const float up = pow2f(24) * (cb >= H ? 0.0625f : 1.f);
-#pragma unroll
-                            for (int k = 0; k < 32; k += 4)
-                                *reinterpret_cast<float4*>(&sh.exchange[row_in * (D + 4) + cb + k]) =
-                                    make_float4(fmaf(o[k] * up, unscale, mv), fmaf(o[k + 1] * up, unscale, mv), fmaf(o[k + 2] * up, unscale, mv),
-                                                fmaf(o[k + 3] * up, unscale, mv));
-                        }
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < D; k += 4) *reinterpret_cast<float4*>(&sh.exchange[row_in * (D + 4) + k]) = make_float4(0.f, 0.f, 0.f, 0.f);
-                    }
+                    sh.exchange_up[row_in] = any ? unscale : 0.f;
                     __syncwarp();
+                    tc_fence_before();
                     if (lane == 0) mbar_arrive(&sh.x_full);
+                    ok = wait(&sh.x_empty, pieces & 1);
+                    if (!ok) break;
                 } else {
                     ok = wait(&sh.x_full, pieces & 1);
                     if (!ok) break;
-                    const float om = sh.exchange_m[row_in], mn = fmaxf(mref, om);
-                    own_f = ex2_approx(mref - mn);
-                    other_f = ex2_approx(om - mn);
-                    l = l * own_f + sh.exchange_l[row_in] * other_f;
+                    tc_fence_after();
+                    const float om = sh.exchange_m[row_in], mn = fmaxf(mref, om), of = ex2_approx(om - mn), own = ex2_approx(mref - mn);
+                    l = l * own + sh.exchange_l[row_in] * of;
+                    unscale *= own;
+                    other = sh.exchange_up[row_in] * of;
                     mref = mn;
                 }
             }
             if (PAIR || x == 0) {
-                const float inv = l > 0.f ? 1.f / l : 0.f;
+                const bool any1 = !PAIR && __any_sync(0xFFFFFFFFu, sh.exchange_up[row_in] != 0.f);   // (the same for every row)
+                const float inv = complete ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
 #pragma unroll
                 for (int cb = 0; cb < D; cb += 32) {
                     float o[32];
@@ -700,18 +747,13 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
 #pragma unroll
                         for (int k = 0; k < 32; ++k) o[k] = 0.f;
                     }
-                    const float up = pow2f(24) * (cb >= H ? 0.0625f : 1.f);
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) o[k] = any ? fmaf(o[k] * up, unscale, mv) : 0.f;
-                    if (!PAIR) {
+                    for (int k = 0; k < 32; ++k) o[k] *= unscale;
+                    if (!PAIR && any1) {
+                        float y[32];
+                        tc_load32(col_o + kStep + cb, y);
 #pragma unroll
-                        for (int k = 0; k < 32; k += 4) {
-                            const float4 e = *reinterpret_cast<const float4*>(&sh.exchange[row_in * (D + 4) + cb + k]);
-                            o[k] = fmaf(e.x, other_f, o[k] * own_f);
-                            o[k + 1] = fmaf(e.y, other_f, o[k + 1] * own_f);
-                            o[k + 2] = fmaf(e.z, other_f, o[k + 2] * own_f);
-                            o[k + 3] = fmaf(e.w, other_f, o[k + 3] * own_f);
-                        }
+                        for (int k = 0; k < 32; ++k) o[k] = fmaf(y[k], other, o[k]);
                     }
                     if (r < rows) {
                         if (complete) {
@@ -739,7 +781,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                 }
                 if (!complete && tid == 0) sh.open[which] = KvPiece{sh.end - w.left - w.pg, w.pages, w.h, w.tile * R, rows, w.first};
             }
-            if (!PAIR && x == 0) {   // the exchange has been read
+            if (!PAIR && x == 0) {   // group 1 may go on
+                tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.x_empty);
             }

@@ -342,6 +342,71 @@ def test_attend(ctx, B, new, longest, Hq, Hkv, D, dtype, tree):
     _check_attend(ctx, pool, q, cached, offs, rows, parent)
 
 
+LONG = [  # sequences, new tokens, contexts from .. to, query heads, key heads, D, dtype, trees: every CTA passes many pages and segments
+    (64, 1, 100, 3000, 28, 4, 128, "bf16", False), (33, 1, 1, 4000, 16, 8, 64, "bf16", False), (40, 1, 500, 1500, 8, 8, 256, "bf16", False),
+    (64, 2, 0, 2000, 32, 4, 128, "bf16", True), (48, 33, 700, 2200, 16, 8, 128, "bf16", True), (60, 33, 0, 1800, 32, 8, 128, "bf16", True),
+    (70, 17, 1, 2500, 10, 5, 64, "bf16", True), (3, 1500, 0, 700, 16, 4, 128, "bf16", False), (2, 1100, 300, 900, 16, 8, 64, "bf16", False),
+    (9, 65, 1000, 1400, 8, 8, 128, "bf16", False), (40, 5, 600, 1900, 8, 2, 128, "f32", True), (20, 1, 10, 2000, 32, 8, 64, "f32", False)]
+
+
+@pytest.mark.parametrize("B,new,lo,hi,Hq,Hkv,D,dtype,tree", LONG)
+def test_attend_long(ctx, B, new, lo, hi, Hq, Hkv, D, dtype, tree):
+    """Larger batches against 64-bit sums on the same device; the entries come through kv_read (fp32, one rounding)."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(B * 7 + new)
+    cached = torch.randint(lo, hi + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    kv = cached + new
+    need = (kv + PAGE - 1) // PAGE
+    P, n = int(need.max()) + 1, int(need.sum()) + 3
+    start = torch.cumsum(need, 0) - need
+    j = torch.arange(P, device="cuda")
+    order = torch.randperm(n, generator=g, device="cuda").to(torch.int32)
+    table = torch.where(j < need[:, None], order[(start[:, None] + j).clamp(max=n - 1)], -1).to(torch.int32).contiguous()
+    pages = binding.kv_pages(n, Hkv, D)
+    pages.fill_(255)
+    b = torch.repeat_interleave(torch.arange(B, device="cuda"), kv.long())
+    t = torch.arange(b.numel(), device="cuda") - (torch.cumsum(kv, 0) - kv)[b]
+    slots = (table[b, t // PAGE] * PAGE + t % PAGE).to(torch.int32)
+    for i in range(0, b.numel(), 50000):
+        m = min(50000, b.numel() - i)
+        k = torch.randn((m, Hkv, D), generator=g, device="cuda")
+        v = torch.randn((m, Hkv, D), generator=g, device="cuda")
+        ctx.kv_write(pages, k[:, :0], k, v, slots[i:i + m].contiguous(), torch.zeros(m, dtype=torch.int32, device="cuda"),
+                     outputs=dict(q=k[:, :0]))
+    q = (torch.randn((B * new, Hq, D), generator=g, device="cuda") * 1.3).to(DT[dtype])
+    rng = np.random.default_rng(B)
+    parent = None
+    if tree:
+        parent = np.stack([_tree(rng, new) for _ in range(B)])
+    o = ctx.kv_attend(q, pages, table, cached, kv, rows_per_seq=new, node_parent=None if parent is None else i32(parent), want_lse=True)
+    assert ctx.poll_status() == 0
+    off = torch.cumsum(kv, 0) - kv
+    for s in range(B):
+        lo_t, n_t, c = int(off[s]), int(kv[s]), int(cached[s])
+        e = ctx.kv_read(pages, slots[lo_t:lo_t + n_t].contiguous(), D, torch.float32)
+        k, v = e["k"].double(), e["v"].double()
+        see = torch.zeros((new, n_t), dtype=torch.bool)
+        see[:, :c] = True
+        for i in range(new):
+            see[i, [c + x for x in (range(i + 1) if parent is None else ref.path_of(i, parent[s]))]] = True
+        see = see.cuda()
+        qs = q[s * new:(s + 1) * new].double().view(new, Hkv, Hq // Hkv, D)
+        w = torch.einsum("nhgd,thd->hgnt", qs, k) / np.sqrt(D)
+        size = torch.einsum("nhgd,thd->hgnt", qs.abs(), k.abs()).amax(-1) / np.sqrt(D)
+        w = w.masked_fill(~see, float("-inf"))
+        lse = torch.logsumexp(w, -1)
+        want = torch.einsum("hgnt,thd->nhgd", torch.exp(w - lse[..., None]), v).reshape(new, Hq, D)
+        wrong = size * 2.0 ** -20 + 2.0 ** -20 + lse.abs() * 2.0 ** -22               # as in _check_attend
+        spread = v.amax((0, 2)) - v.amin((0, 2))
+        lim = spread[:, None, None] * (2 * wrong + (2.0 ** -21 if dtype == "f32" else 2.0 ** -11) + 2.0 ** -20) + 2.0 ** -21 * v.abs().max()
+        lim = lim.permute(2, 0, 1).reshape(new, Hq)[..., None] + want.abs() * (2.0 ** -24 if dtype == "f32" else 2.0 ** -8)
+        got = o["out"][s * new:(s + 1) * new].double()
+        assert bool(((got - want).abs() <= lim).all()), (s, float(((got - want).abs() / lim).max()))
+        gl = o["lse"][s * new:(s + 1) * new].double()
+        le, lw = lse.permute(2, 0, 1).reshape(new, Hq), wrong.permute(2, 0, 1).reshape(new, Hq)
+        assert bool(((gl - le).abs() <= lw + 2.0 ** -21 * le.abs()).all())
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attend_with_large_products_and_values_of_any_size(ctx, dtype):
     """Sharp softmaxes, scales of the values far from 1 and different by token, rows without a range."""
