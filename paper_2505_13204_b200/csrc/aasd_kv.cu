@@ -29,6 +29,11 @@ void with_type(int dtype, F&& f) {
 // Token rows up to which the planning CTA writes the token arrays itself (a second launch costs
 // about 2 us; one CTA places 256 tokens per 0.6 us).
 constexpr int64_t kInlineTokens = 1024;
+// Threads from which the lanes of a query or key row go through four rows of a token: with fewer, one
+// row each (and four times the CTAs) fills the machine better.
+constexpr int64_t kManyRowThreads = 1 << 18;
+// Sequences up to which the planning CTA has 256 threads: its scans cost a barrier per warp.
+constexpr int kPlanManySeqs = 64;
 
 }  // namespace
 
@@ -54,9 +59,11 @@ int aasd_kv_plan(aasd_ctx* ctx, const int32_t* cached_len, const int32_t* n_new,
     if (p->n_tokens > 0 && (!o->slot_map || !o->positions)) return AASD_ERR_INVALID_ARG;
     if (p->rows_per_seq == 0 && !o->tok_offsets) return AASD_ERR_INVALID_ARG;
     KvPlanArgs a{cached_len, n_new, node_depth, *p, *s, *o, ctx->state, 0};
-    a.tokens_inline = p->n_tokens <= kInlineTokens && p->n_seqs <= kPlanThreads;
+    const bool many = p->n_seqs > kPlanManySeqs;
+    a.tokens_inline = p->n_tokens <= kInlineTokens && p->n_seqs <= (many ? kPlanThreadsMany : kPlanThreads);
     AASD_CUDA(cudaSetDevice(ctx->device));
-    launch(kv_plan_kernel, 1u, (unsigned int)kPlanThreads, 0, ctx->stream, a);
+    if (many) launch(kv_plan_kernel<kPlanThreadsMany>, 1u, (unsigned int)kPlanThreadsMany, 0, ctx->stream, a);
+    else launch(kv_plan_kernel<kPlanThreads>, 1u, (unsigned int)kPlanThreads, 0, ctx->stream, a);
     if (a.tokens_inline || p->n_tokens == 0) return after_launch(ctx, 1);
     launch(kv_tokens_kernel, (unsigned int)((p->n_tokens + 1023) / 1024), 256u, 0, ctx->stream, a);
     return after_launch(ctx, 2);
@@ -83,20 +90,27 @@ int aasd_kv_write(aasd_ctx* ctx, const void* q, const void* k, const void* v, co
     for (const void* x : {q, k, v, q_weight, k_weight, (const void*)q_out, (const void*)k_out})
         if (((uintptr_t)x % es) != 0) return AASD_ERR_INVALID_ARG;
     KvWriteArgs a{q, k, v, q_weight, k_weight, cos_sin, positions, slot_map, n_tokens, *p, static_cast<uint8_t*>(pages), q_out, k_out,
-                  ctx->state};
-    const int64_t threads = n_tokens * (hq + 2 * hkv) * (D / 16);
-    if (threads / 256 >= 0x7FFFFFFFLL) return AASD_ERR_BAD_SHAPE;
+                  ctx->state, 0u};
     // 16-byte accesses where every row of every operand starts on a 16-byte boundary
-    bool vec = true;
+    bool vec = p->rotary_dim == 0 || aligned16(cos_sin);
     for (const void* x : {q, k, v, q_weight, k_weight, (const void*)q_out, (const void*)k_out}) vec = vec && aligned16(x);
     if (hq > 0) vec = vec && (p->q_stride * es) % 16 == 0;
     if (hkv > 0) vec = vec && (p->k_stride * es) % 16 == 0 && (p->v_stride * es) % 16 == 0;
+    const int lanes = D / 16;
+    const int64_t rows = n_tokens * (hq + hkv);
+    const bool sets = vec && rows * lanes >= kManyRowThreads;
+    const int64_t groups = sets ? n_tokens * ((hq + hkv + 3) / 4) : rows;
+    const int64_t value_blocks = (n_tokens + kValueTokens - 1) / kValueTokens * hkv;
+    const int64_t blocks = value_blocks + (groups * lanes + kWriteThreads - 1) / kWriteThreads;
+    if (blocks > 0x7FFFFFFFLL) return AASD_ERR_BAD_SHAPE;
+    a.value_blocks = (unsigned int)value_blocks;
     AASD_CUDA(cudaSetDevice(ctx->device));
-    const unsigned int grid = (unsigned int)((threads + 255) / 256);
     with_type(p->dtype, [&](auto dt) {
         with_dim(D, [&](auto d) {
-            if (vec) launch(kv_write_kernel<dt(), d(), true>, grid, 256u, 0, ctx->stream, a);
-            else launch(kv_write_kernel<dt(), d(), false>, grid, 256u, 0, ctx->stream, a);
+            auto go = [&](auto kernel) { launch(kernel, (unsigned int)blocks, (unsigned int)kWriteThreads, 0, ctx->stream, a); };
+            if (vec && sets) go(kv_write_kernel<dt(), d(), true, 4>);
+            else if (vec) go(kv_write_kernel<dt(), d(), true, 1>);
+            else go(kv_write_kernel<dt(), d(), false, 1>);
         });
     });
     return after_launch(ctx, 1);
@@ -114,15 +128,15 @@ int aasd_kv_read(aasd_ctx* ctx, const void* pages, const int32_t* slots, int64_t
     const size_t es = elt_size(dtype);
     if (((uintptr_t)k_out % es) != 0 || ((uintptr_t)v_out % es) != 0) return AASD_ERR_INVALID_ARG;
     KvReadArgs a{static_cast<const uint8_t*>(pages), slots, n, n_pages, n_kv_heads, k_out, v_out, ctx->state};
-    const int64_t threads = n * 2 * n_kv_heads * (head_dim / 16);
-    if (threads / 256 >= 0x7FFFFFFFLL) return AASD_ERR_BAD_SHAPE;
+    const int64_t blocks = (n + kValueTokens - 1) / kValueTokens * n_kv_heads;
+    if (blocks > 0x7FFFFFFFLL) return AASD_ERR_BAD_SHAPE;
     const bool vec = aligned16(k_out) && aligned16(v_out);
     AASD_CUDA(cudaSetDevice(ctx->device));
-    const unsigned int grid = (unsigned int)((threads + 255) / 256);
+    const unsigned int grid = (unsigned int)blocks;
     with_type(dtype, [&](auto dt) {
         with_dim(head_dim, [&](auto d) {
-            if (vec) launch(kv_read_kernel<dt(), d(), true>, grid, 256u, 0, ctx->stream, a);
-            else launch(kv_read_kernel<dt(), d(), false>, grid, 256u, 0, ctx->stream, a);
+            if (vec) launch(kv_read_kernel<dt(), d(), true>, grid, (unsigned int)kWriteThreads, 0, ctx->stream, a);
+            else launch(kv_read_kernel<dt(), d(), false>, grid, (unsigned int)kWriteThreads, 0, ctx->stream, a);
         });
     });
     return after_launch(ctx, 1);

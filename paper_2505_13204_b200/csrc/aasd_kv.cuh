@@ -158,14 +158,14 @@ __device__ __forceinline__ void kv_place_token(const KvPlanArgs& a, int64_t t, i
 }
 
 #ifdef AASD_KV_TU
-constexpr int kPlanThreads = 256;
+constexpr int kPlanThreads = 256, kPlanThreadsMany = 1024;   // of batches up to 64 sequences, and larger ones
 
-// One CTA: the books of all sequences (kPlanThreads at a time) by prefix sums, the pages moved
+// One CTA: the books of all sequences (NT at a time) by prefix sums, the pages moved
 // by all threads together (a thread finds its page's sequence by bisection of the sums), so one
 // long sequence that ends or arrives costs no more than many short ones.  Latency-bound: four
 // scans and three trips to memory.
-__global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const KvPlanArgs a) {
-    constexpr int NT = kPlanThreads;
+template <int NT>
+__global__ void __launch_bounds__(NT) kv_plan_kernel(const KvPlanArgs a) {
     __shared__ long long s_warp[NT / 32];
     __shared__ int s_first[NT + 1], s_at[NT];
     __shared__ int s_off[NT + 1];
@@ -249,13 +249,22 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const KvPlanArgs 
         // the sequences that get what they ask for are the first ones of those that ask
         long long got;
         block_scan<NT>(served ? want : 0, s_warp, got);   // (also the barrier for the arrays above)
-        for (int r = tid; r < (int)got; r += NT) {
-            const int k = last_not_above(s_first, NT, r);
-            const long long from = n_free - 1 - (asked + r);
-            const int page = a.s.free_pages[from];
-            a.s.free_pages[from] = AASD_NONE;
-            if (page < 0 || page >= a.p.n_pages) bits |= AASD_STATUS_BAD_OFFSETS;
-            a.s.block_table[(int64_t)(base + k) * P + s_at[k] + (r - s_first[k])] = page;
+        for (int r0 = tid; r0 < (int)got; r0 += 4 * NT) {
+            int page[4];   // (four loads under way before the first store)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int r = r0 + e * NT;
+                page[e] = r < (int)got ? a.s.free_pages[n_free - 1 - (asked + r)] : 0;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int r = r0 + e * NT;
+                if (r >= (int)got) break;
+                const int k = last_not_above(s_first, NT, r);
+                a.s.free_pages[n_free - 1 - (asked + r)] = AASD_NONE;
+                if (page[e] < 0 || page[e] >= a.p.n_pages) bits |= AASD_STATUS_BAD_OFFSETS;
+                a.s.block_table[(int64_t)(base + k) * P + s_at[k] + (r - s_first[k])] = page[e];
+            }
         }
         asked += want_total;
         taken += got;
@@ -290,16 +299,34 @@ __global__ void __launch_bounds__(kPlanThreads) kv_plan_kernel(const KvPlanArgs 
     if (bits) raise(a.state, bits);
 }
 
-// Token arrays of large steps: four tokens per thread.
+// Token arrays of large steps: four tokens per thread.  A CTA's 1024 tokens belong to few
+// sequences, which its first warp finds by bisection of the offsets, a 32nd of the range at a time.
 __global__ void __launch_bounds__(256) kv_tokens_kernel(const KvPlanArgs a) {
+    __shared__ int s_b;
     pdl_launch_dependents();
     pdl_wait();
-    const int64_t t0 = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (t0 >= a.p.n_tokens) return;
+    const int64_t c0 = (int64_t)blockIdx.x * 1024, t0 = c0 + threadIdx.x * 4;
     const int B = a.p.n_seqs;
     int b;
-    if (a.p.rows_per_seq > 0) b = (int)(t0 / a.p.rows_per_seq);
-    else b = t0 < a.o.tok_offsets[B] ? last_not_above(a.o.tok_offsets, B, (int)t0) : B;
+    if (a.p.rows_per_seq > 0) {
+        b = (int)(t0 / a.p.rows_per_seq);
+    } else {
+        if (threadIdx.x < 32) {
+            int lo = 0, n = B + 1;                            // the last offset <= c0 is among [lo, lo + n)
+            while (n > 1) {
+                const int step = (n + 31) / 32, at = lo + (int)threadIdx.x * step;
+                const unsigned int below = __ballot_sync(0xFFFFFFFFu, at < lo + n && a.o.tok_offsets[at] <= c0);
+                const int k = below ? 31 - __clz(below) : 0;
+                n = min(step, lo + n - (lo + k * step));
+                lo += k * step;
+            }
+            if (threadIdx.x == 0) s_b = lo;
+        }
+        __syncthreads();
+        b = s_b;
+        while (b < B && t0 >= a.o.tok_offsets[b + 1]) ++b;
+    }
+    if (t0 >= a.p.n_tokens) return;
     int slot[4], pos[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -340,138 +367,45 @@ struct KvWriteArgs {
     uint8_t* pages;
     void *q_out, *k_out;
     DeviceState* state;
+    unsigned int value_blocks;   // CTAs that store values; the others take queries and keys
 };
 
 #ifdef AASD_KV_TU
-// D / 16 lanes share a head row: a lane holds eight channels of each half of the row, so that
-// both members of a rotated pair, and both halves of a stored byte, are its own.
+// A CTA either takes query and key rows or stores values; both kinds share the launch.
 //
-// The norm's sum follows the order of the definition: halves, then neighbours (three steps
-// inside the lane, the others across lanes by butterfly; a sum does not ask which operand is
-// first), each operation rounded by itself.
-template <int DT, int D, bool VEC>
-__global__ void __launch_bounds__(256) kv_write_kernel(const KvWriteArgs a) {
-    constexpr int L = D / 16;              // lanes of a row
-    constexpr int H = D / 2;
-    __shared__ float s_rows[256 / L * D];
-    pdl_launch_dependents();
-    pdl_wait();
-    const int hq = a.p.n_q_heads, hkv = a.p.n_kv_heads;
-    const int heads = hq + 2 * hkv;
-    const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
-    const int l = threadIdx.x % L;
-    const bool live = row < a.n_tokens * heads;
-    const int64_t t = live ? row / heads : 0;
-    const int h = live ? (int)(row - t * heads) : 0;
-    const int kind = h < hq ? 0 : h < hq + hkv ? 1 : 2;   // query, key, value
-    const int head = kind == 0 ? h : kind == 1 ? h - hq : h - hq - hkv;
-    float x[8], y[8];   // channels 8l + e and D/2 + 8l + e
-    int pos = AASD_NONE, slot = AASD_NONE;
+// Query and key rows: D / 16 lanes share a row, a lane holds eight channels of each half, so that both
+// members of a rotated pair, and both halves of a stored byte, are its own.  The lanes stay with
+// one token for up to HP of its heads, whose loads are under way together and which share the
+// cosines and weights.  The norm's sum follows the order of the definition: halves, then
+// neighbours (three steps inside the lane, the others across lanes by butterfly; a sum does not
+// ask which operand is first), each operation rounded by itself.
+//
+// Values: a CTA takes kValueTokens tokens of one head.  Their codes meet in shared memory, and lane t
+// of a warp stores the bytes of token t: neighbouring tokens, which lie in neighbouring bytes, in one
+// go (byte by byte from the rows' own lanes, 4096 tokens took 62 us in all instead of 25).
+constexpr int kValueTokens = 32;
+constexpr int kWriteThreads = 256;
+
+// What a row's lanes know about its token.
+__device__ __forceinline__ unsigned int kv_write_token(const KvWriteArgs& a, int64_t t, bool store, int& pos, int& slot) {
     unsigned int bits = 0;
-    if (live) {
-        pos = a.positions[t];
-        slot = kind > 0 ? a.slot_map[t] : AASD_NONE;
-        if (pos < AASD_NONE || (a.p.rotary_dim > 0 && pos >= a.p.max_positions)) {
-            bits |= AASD_STATUS_ID_RANGE;
-            pos = AASD_NONE;
-        }
-        if (slot < AASD_NONE || slot / kPage >= a.p.n_pages) {
-            bits |= AASD_STATUS_ID_RANGE;
-            slot = AASD_NONE;
-        }
-        if (pos == AASD_NONE) slot = AASD_NONE;
+    pos = a.positions[t];
+    slot = store ? a.slot_map[t] : AASD_NONE;
+    if (pos < AASD_NONE || (a.p.rotary_dim > 0 && pos >= a.p.max_positions)) {
+        bits |= AASD_STATUS_ID_RANGE;
+        pos = AASD_NONE;
     }
-    const bool used = live && pos != AASD_NONE;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = y[e] = 0.f;
-    if (used && AASD_IN_RANGE(t < a.n_tokens && head >= 0 && head < (kind == 0 ? hq : hkv), a.state)) {
-        const void* src = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
-        const int64_t at = t * (kind == 0 ? a.p.q_stride : kind == 1 ? a.p.k_stride : a.p.v_stride) + (int64_t)head * D + 8 * l;
-        load8<DT, VEC>(src, at, x);
-        load8<DT, VEC>(src, at + H, y);
+    if (slot < AASD_NONE || slot / kPage >= a.p.n_pages) {
+        bits |= AASD_STATUS_ID_RANGE;
+        slot = AASD_NONE;
     }
-    const void* w = kind == 0 ? a.q_weight : kind == 1 ? a.k_weight : nullptr;
-    // (the lanes of a row take the same way; shuffles stay among all lanes of the warp)
-    float s[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s[e] = __fadd_rn(__fmul_rn(x[e], x[e]), __fmul_rn(y[e], y[e]));
-    float sum = __fadd_rn(__fadd_rn(__fadd_rn(s[0], s[1]), __fadd_rn(s[2], s[3])), __fadd_rn(__fadd_rn(s[4], s[5]), __fadd_rn(s[6], s[7])));
-#pragma unroll
-    for (int o = 1; o < L; o <<= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xFFFFFFFFu, sum, o));
-    if (used && w != nullptr) {
-        const float r = __frcp_rn(__fsqrt_rn(__fadd_rn(__fmul_rn(sum, 1.0f / D), a.p.eps)));
-        float wx[8], wy[8];
-        load8<DT, VEC>(w, 8 * l, wx);
-        load8<DT, VEC>(w, H + 8 * l, wy);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            x[e] = __fmul_rn(__fmul_rn(x[e], r), wx[e]);
-            y[e] = __fmul_rn(__fmul_rn(y[e], r), wy[e]);
-        }
-    }
-    // (the branches on the form of the rotation are the same for every lane of the launch)
-    const int rot = a.p.rotary_dim, half = rot / 2;
-    const bool turn = used && kind < 2 && AASD_IN_RANGE(rot == 0 || (pos >= 0 && pos < a.p.max_positions), a.state);
-    const float* cs = a.cos_sin + (int64_t)(turn ? pos : 0) * rot;
-    if (rot > 0 && (a.p.flags & AASD_KV_ROPE_INTERLEAVED)) {
-#pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            float(&z)[8] = part ? y : x;
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                const int c = part * H + 8 * l + e;
-                if (turn && c < rot) {
-                    const float co = cs[c / 2], si = cs[half + c / 2];
-                    const float p = z[e], q = z[e + 1];
-                    z[e] = __fsub_rn(__fmul_rn(p, co), __fmul_rn(q, si));
-                    z[e + 1] = __fadd_rn(__fmul_rn(q, co), __fmul_rn(p, si));
-                }
-            }
-        }
-    } else if (rot == D) {
-        if (turn) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float co = cs[8 * l + e], si = cs[half + 8 * l + e];
-                const float p = x[e], q = y[e];
-                x[e] = __fsub_rn(__fmul_rn(p, co), __fmul_rn(q, si));
-                y[e] = __fadd_rn(__fmul_rn(q, co), __fmul_rn(p, si));
-            }
-        }
-    } else if (rot > 0) {
-        // a pair (c, c + half) inside the first rot channels: its members may be different lanes',
-        // so the warp's rows pass through shared memory (partial rotation is the rare case)
-        float* mine = s_rows + (threadIdx.x / L) * D;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            mine[8 * l + e] = x[e];
-            mine[H + 8 * l + e] = y[e];
-        }
-        __syncwarp();
-        if (turn) {
-#pragma unroll
-            for (int part = 0; part < 2; ++part) {
-                float(&z)[8] = part ? y : x;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int c = part * H + 8 * l + e;
-                    if (c < half) z[e] = __fsub_rn(__fmul_rn(z[e], cs[c]), __fmul_rn(mine[c + half], cs[half + c]));
-                    else if (c < rot) z[e] = __fadd_rn(__fmul_rn(z[e], cs[c - half]), __fmul_rn(mine[c - half], cs[c]));
-                }
-            }
-        }
-    }
-    if (live && kind == 0 && AASD_IN_RANGE(a.q_out != nullptr && head < hq, a.state)) {
-        const int64_t at = (t * hq + head) * D + 8 * l;
-        store8<DT, VEC>(a.q_out, at, x);
-        store8<DT, VEC>(a.q_out, at + H, y);
-    }
-    if (live && kind == 1 && a.k_out != nullptr) {
-        const int64_t at = (t * hkv + head) * D + 8 * l;
-        store8<DT, VEC>(a.k_out, at, x);
-        store8<DT, VEC>(a.k_out, at + H, y);
-    }
-    float lo = x[0], hi = x[0], sick = 0.f;   // sick: NaN or infinite as soon as one value is
+    if (pos == AASD_NONE) slot = AASD_NONE;
+    return bits;
+}
+// Quantiser of a row spread over L lanes; every lane of the warp takes part.
+template <int L>
+__device__ __forceinline__ KvQuant kv_row_quantiser(const float (&x)[8], const float (&y)[8], bool& bad) {
+    float lo = x[0], hi = x[0], sick = 0.f;   // sick: NaN as soon as one value is NaN or infinite
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         lo = fminf(lo, fminf(x[e], y[e]));
@@ -484,27 +418,217 @@ __global__ void __launch_bounds__(256) kv_write_kernel(const KvWriteArgs a) {
         hi = fmaxf(hi, __shfl_xor_sync(0xFFFFFFFFu, hi, o));
         sick += __shfl_xor_sync(0xFFFFFFFFu, sick, o);
     }
-    if (live && kind > 0 && slot != AASD_NONE) {
-        const bool bad = sick != 0.f || !(hi - bf16_round(lo) <= 3.3e38f) || !(fabsf(bf16_round(lo)) <= 3.4e38f);
-        if (bad) bits |= AASD_STATUS_BAD_ROW;
-        const KvQuant z = kv_quantiser(lo, hi, bad);
-        unsigned long long bytes = 0;
+    const float m = bf16_round(lo);
+    bad = sick != 0.f || !(hi - m <= 3.3e38f) || !(fabsf(m) <= 3.4e38f);
+    return kv_quantiser(lo, hi, bad);
+}
+__device__ __forceinline__ unsigned long long kv_row_codes(const float (&x)[8], const float (&y)[8], const KvQuant& z, bool bad) {
+    unsigned long long bytes = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const unsigned int b = bad ? 0u : kv_code(x[e], z) | (kv_code(y[e], z) << 4);
-            bytes |= (unsigned long long)b << (8 * e);
+    for (int e = 0; e < 8; ++e) {
+        const unsigned int b = bad ? 0u : kv_code(x[e], z) | (kv_code(y[e], z) << 4);
+        bytes |= (unsigned long long)b << (8 * e);
+    }
+    return bytes;
+}
+
+template <int DT, int D, bool VEC, int HP>
+__global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteArgs a) {
+    constexpr int L = D / 16;              // lanes of a row
+    constexpr int H = D / 2;
+    // rows in passage: partial rotation (a float per channel), or the values' codes (rows padded to 8 bytes more)
+    constexpr int kRows = kWriteThreads / L, kPitch = H + 8;
+    __shared__ alignas(16) unsigned char s_mem[kRows * D * 4 > kValueTokens * kPitch ? kRows * D * 4 : kValueTokens * kPitch];
+    __shared__ int s_slot[kValueTokens];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int hq = a.p.n_q_heads, hkv = a.p.n_kv_heads;
+    const int l = threadIdx.x % L, group = threadIdx.x / L;
+    unsigned int bits = 0;
+    if (blockIdx.x < a.value_blocks) {
+        // ---- values
+        const int64_t t0 = (int64_t)(blockIdx.x / hkv) * kValueTokens;
+        const int head = (int)(blockIdx.x % hkv);
+        for (int k = group; k < kValueTokens; k += kRows) {
+            const int64_t t = t0 + k;
+            const bool live = t < a.n_tokens;
+            int pos, slot = AASD_NONE;
+            if (live) bits |= kv_write_token(a, t, true, pos, slot);
+            float x[8], y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = y[e] = 0.f;
+            if (slot != AASD_NONE) {
+                const int64_t at = t * a.p.v_stride + (int64_t)head * D + 8 * l;
+                load8<DT, VEC>(a.v, at, x);
+                load8<DT, VEC>(a.v, at + H, y);
+            }
+            bool bad;
+            const KvQuant z = kv_row_quantiser<L>(x, y, bad);
+            if (slot != AASD_NONE && bad) bits |= AASD_STATUS_BAD_ROW;
+            *reinterpret_cast<unsigned long long*>(s_mem + k * kPitch + 8 * l) = kv_row_codes(x, y, z, bad);
+            if (l == 0) {
+                s_slot[k] = slot;
+                if (slot != AASD_NONE) {
+                    uint8_t* block = a.pages + ((int64_t)(slot / kPage) * hkv + head) * kv_head_bytes(D);
+                    reinterpret_cast<unsigned int*>(block + kv_value_meta_offset(D))[slot % kPage] = z.meta;
+                }
+            }
         }
-        uint8_t* block = a.pages + ((int64_t)(slot / kPage) * hkv + head) * kv_head_bytes(D);
-        const int at = slot % kPage;
-        if (!AASD_IN_RANGE(slot >= 0 && slot / kPage < a.p.n_pages && head >= 0 && head < hkv, a.state)) {
-        } else if (kind == 1) {
-            *reinterpret_cast<unsigned long long*>(block + at * H + 8 * l) = bytes;
-            if (l == 0) reinterpret_cast<unsigned int*>(block + kv_key_meta_offset(D))[at] = z.meta;
-        } else {
-            uint8_t* col = block + kv_value_offset(D) + at;
+        __syncthreads();
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        static_assert(kValueTokens == 32, "a lane per token");
+        const int slot = s_slot[lane];
+        if (slot != AASD_NONE && AASD_IN_RANGE(slot / kPage < a.p.n_pages && head < hkv, a.state)) {
+            uint8_t* col = a.pages + ((int64_t)(slot / kPage) * hkv + head) * kv_head_bytes(D) + kv_value_offset(D) + slot % kPage;
+            constexpr int kWordsPerWarp = H / 4 / (kWriteThreads / 32);   // 1, 2 or 4 words of four channel pairs
 #pragma unroll
-            for (int e = 0; e < 8; ++e) col[(8 * l + e) * kPage] = (uint8_t)(bytes >> (8 * e));
-            if (l == 0) reinterpret_cast<unsigned int*>(block + kv_value_meta_offset(D))[at] = z.meta;
+            for (int w = 0; w < kWordsPerWarp; ++w) {
+                const int i = (warp * kWordsPerWarp + w) * 4;
+                const unsigned int b = *reinterpret_cast<const unsigned int*>(s_mem + lane * kPitch + i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) col[(i + e) * kPage] = (uint8_t)(b >> (8 * e));
+            }
+        }
+        if (bits) raise(a.state, bits);
+        return;
+    }
+    // ---- queries and keys
+    float* s_rows = reinterpret_cast<float*>(s_mem);
+    const int heads = hq + hkv;
+    const int sets = (heads + HP - 1) / HP;                 // sets of HP rows of a token
+    const int64_t g = ((int64_t)(blockIdx.x - a.value_blocks) * kWriteThreads + threadIdx.x) / L;
+    const bool live = g < a.n_tokens * sets;
+    const int64_t t = live ? g / sets : 0;
+    const int h0 = live ? (int)(g - t * sets) * HP : 0;
+    int pos = AASD_NONE, slot = AASD_NONE;
+    if (live) bits |= kv_write_token(a, t, hkv > 0, pos, slot);
+    const bool used = live && pos != AASD_NONE;
+    float x[HP][8], y[HP][8];   // channels 8l + e and D/2 + 8l + e
+#pragma unroll
+    for (int i = 0; i < HP; ++i) {
+        const int h = h0 + i;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[i][e] = y[i][e] = 0.f;
+        if (used && h < heads) {
+            const void* src = h < hq ? a.q : a.k;
+            const int64_t at = h < hq ? t * a.p.q_stride + (int64_t)h * D + 8 * l : t * a.p.k_stride + (int64_t)(h - hq) * D + 8 * l;
+            load8<DT, VEC>(src, at, x[i]);
+            load8<DT, VEC>(src, at + H, y[i]);
+        }
+    }
+    // cosines and sines of the lane's pairs (the branches on the form of the rotation are the same for every lane)
+    const int rot = a.p.rotary_dim, half = rot / 2;
+    const bool neighbours = (a.p.flags & AASD_KV_ROPE_INTERLEAVED) != 0;
+    const float* cs = a.cos_sin + (int64_t)(used ? pos : 0) * rot;
+    float co[8], si[8];   // neighbours: pairs of the low half, then of the high half; else of channels 8l + e
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        co[e] = 1.f;
+        si[e] = 0.f;
+    }
+    if (rot > 0 && used) {
+        if (neighbours) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int c = (e < 4 ? 8 * l : H + 8 * l) + 2 * (e & 3);
+                if (c < rot) {
+                    co[e] = __ldg(cs + c / 2);
+                    si[e] = __ldg(cs + half + c / 2);
+                }
+            }
+        } else if (rot == D) {
+            load8<AASD_F32, VEC>(cs, 8 * l, co);
+            load8<AASD_F32, VEC>(cs, half + 8 * l, si);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < HP; ++i) {
+        const int h = h0 + i;
+        const bool row = used && h < heads, key = h >= hq;
+        const void* w = key ? a.k_weight : a.q_weight;
+        float(&u)[8] = x[i];
+        float(&v)[8] = y[i];
+        // (the lanes of a row take the same way; shuffles stay among all lanes of the warp)
+        float s[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] = __fadd_rn(__fmul_rn(u[e], u[e]), __fmul_rn(v[e], v[e]));
+        float sum = __fadd_rn(__fadd_rn(__fadd_rn(s[0], s[1]), __fadd_rn(s[2], s[3])), __fadd_rn(__fadd_rn(s[4], s[5]), __fadd_rn(s[6], s[7])));
+#pragma unroll
+        for (int o = 1; o < L; o <<= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xFFFFFFFFu, sum, o));
+        if (row && w != nullptr) {
+            const float r = __frcp_rn(__fsqrt_rn(__fadd_rn(__fmul_rn(sum, 1.0f / D), a.p.eps)));
+            float wx[8], wy[8];
+            load8<DT, VEC>(w, 8 * l, wx);
+            load8<DT, VEC>(w, H + 8 * l, wy);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                u[e] = __fmul_rn(__fmul_rn(u[e], r), wx[e]);
+                v[e] = __fmul_rn(__fmul_rn(v[e], r), wy[e]);
+            }
+        }
+        if (rot > 0 && neighbours) {
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                float(&z)[8] = part ? v : u;
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    if (part * H + 8 * l + e < rot) {
+                        const float p = z[e], q = z[e + 1], c = co[4 * part + e / 2], n = si[4 * part + e / 2];
+                        z[e] = __fsub_rn(__fmul_rn(p, c), __fmul_rn(q, n));
+                        z[e + 1] = __fadd_rn(__fmul_rn(q, c), __fmul_rn(p, n));
+                    }
+                }
+            }
+        } else if (rot == D) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float p = u[e], q = v[e];
+                u[e] = __fsub_rn(__fmul_rn(p, co[e]), __fmul_rn(q, si[e]));
+                v[e] = __fadd_rn(__fmul_rn(q, co[e]), __fmul_rn(p, si[e]));
+            }
+        } else if (rot > 0) {
+            // a pair (c, c + half) inside the first rot channels: its members may be different lanes',
+            // so the warp's rows pass through shared memory (partial rotation is the rare case)
+            float* mine = s_rows + group * D;
+            __syncwarp();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                mine[8 * l + e] = u[e];
+                mine[H + 8 * l + e] = v[e];
+            }
+            __syncwarp();
+            if (row) {
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    float(&z)[8] = part ? v : u;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int c = part * H + 8 * l + e;
+                        if (c < half) z[e] = __fsub_rn(__fmul_rn(z[e], cs[c]), __fmul_rn(mine[c + half], cs[half + c]));
+                        else if (c < rot) z[e] = __fadd_rn(__fmul_rn(z[e], cs[c - half]), __fmul_rn(mine[c - half], cs[c]));
+                    }
+                }
+            }
+        }
+        if (live && h < hq) {
+            const int64_t at = (t * hq + h) * D + 8 * l;
+            store8<DT, VEC>(a.q_out, at, u);
+            store8<DT, VEC>(a.q_out, at + H, v);
+        }
+        if (live && key && h < heads && a.k_out != nullptr) {
+            const int64_t at = (t * hkv + h - hq) * D + 8 * l;
+            store8<DT, VEC>(a.k_out, at, u);
+            store8<DT, VEC>(a.k_out, at + H, v);
+        }
+        if (!__any_sync(0xFFFFFFFFu, row && key)) continue;
+        bool bad;
+        const KvQuant z = kv_row_quantiser<L>(u, v, bad);
+        if (row && key && slot != AASD_NONE && AASD_IN_RANGE(slot / kPage < a.p.n_pages && h - hq < hkv, a.state)) {
+            if (bad) bits |= AASD_STATUS_BAD_ROW;
+            uint8_t* block = a.pages + ((int64_t)(slot / kPage) * hkv + h - hq) * kv_head_bytes(D);
+            const int at = slot % kPage;
+            *reinterpret_cast<unsigned long long*>(block + at * H + 8 * l) = kv_row_codes(u, v, z, bad);
+            if (l == 0) reinterpret_cast<unsigned int*>(block + kv_key_meta_offset(D))[at] = z.meta;
         }
     }
     if (bits) raise(a.state, bits);
@@ -521,55 +645,72 @@ struct KvReadArgs {
     DeviceState* state;
 };
 
-// Lanes as in the writing kernel: one row (slot, head, key or value) per D / 16 lanes.
+// A CTA takes kValueTokens slots of one head.  The values' bytes are fetched with a lane per slot, so
+// that neighbouring slots are one access, and pass through shared memory; then D / 16 lanes turn out a
+// row as in the writing kernel.
 template <int DT, int D, bool VEC>
-__global__ void __launch_bounds__(256) kv_read_kernel(const KvReadArgs a) {
-    constexpr int L = D / 16, H = D / 2;
+__global__ void __launch_bounds__(kWriteThreads) kv_read_kernel(const KvReadArgs a) {
+    constexpr int L = D / 16, H = D / 2, kRows = kWriteThreads / L, kPitch = H + 8;
+    __shared__ alignas(16) unsigned char s_code[kValueTokens * kPitch];
+    __shared__ int s_slot[kValueTokens];
     pdl_launch_dependents();
     pdl_wait();
-    const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
+    const int hkv = a.n_kv_heads;
+    const int64_t i0 = (int64_t)(blockIdx.x / hkv) * kValueTokens;
+    const int head = (int)(blockIdx.x % hkv);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int slot = AASD_NONE;
+    if (i0 + lane < a.n) {
+        slot = a.slots[i0 + lane];
+        if (slot < AASD_NONE || slot / kPage >= a.n_pages) {
+            if (warp == 0) raise(a.state, AASD_STATUS_ID_RANGE);
+            slot = AASD_NONE;
+        }
+    }
+    if (warp == 0) s_slot[lane] = slot;
+    if (a.v_out != nullptr) {
+        constexpr int kWordsPerWarp = H / 4 / (kWriteThreads / 32);
+        unsigned char b[kWordsPerWarp][4];
+        const uint8_t* col = a.pages + ((int64_t)((slot < 0 ? 0 : slot) / kPage) * hkv + head) * kv_head_bytes(D) + kv_value_offset(D) + (slot < 0 ? 0 : slot) % kPage;
+#pragma unroll
+        for (int w = 0; w < kWordsPerWarp; ++w)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) b[w][e] = slot != AASD_NONE ? col[((warp * kWordsPerWarp + w) * 4 + e) * kPage] : (unsigned char)0;
+#pragma unroll
+        for (int w = 0; w < kWordsPerWarp; ++w)
+            *reinterpret_cast<unsigned int*>(s_code + lane * kPitch + (warp * kWordsPerWarp + w) * 4) =
+                b[w][0] | (b[w][1] << 8) | (b[w][2] << 16) | ((unsigned int)b[w][3] << 24);
+    }
+    __syncthreads();
     const int l = threadIdx.x % L;
-    const int heads = 2 * a.n_kv_heads;
-    if (row >= a.n * heads) return;
-    const int64_t i = row / heads;
-    const int h = (int)(row - i * heads);
-    const bool value = h >= a.n_kv_heads;
-    const int head = value ? h - a.n_kv_heads : h;
-    void* out = value ? a.v_out : a.k_out;
-    if (out == nullptr) return;
-    int slot = a.slots[i];
-    if (slot < AASD_NONE || slot / kPage >= a.n_pages) {
-        raise(a.state, AASD_STATUS_ID_RANGE);
-        slot = AASD_NONE;
-    }
-    float x[8], y[8];
+    // rows: keys of all slots, then values
+    for (int k = threadIdx.x / L; k < 2 * kValueTokens; k += kRows) {
+        const int q = k % kValueTokens;
+        const bool value = k >= kValueTokens;
+        void* out = value ? a.v_out : a.k_out;
+        if (out == nullptr || i0 + q >= a.n) continue;
+        const int at = s_slot[q];
+        float x[8], y[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = y[e] = 0.f;
-    if (slot != AASD_NONE) {
-        const uint8_t* block = a.pages + ((int64_t)(slot / kPage) * a.n_kv_heads + head) * kv_head_bytes(D);
-        const int at = slot % kPage;
-        unsigned long long bytes = 0;
-        unsigned int meta;
-        if (!value) {
-            bytes = *reinterpret_cast<const unsigned long long*>(block + at * H + 8 * l);
-            meta = reinterpret_cast<const unsigned int*>(block + kv_key_meta_offset(D))[at];
-        } else {
-            const uint8_t* col = block + kv_value_offset(D) + at;
+        for (int e = 0; e < 8; ++e) x[e] = y[e] = 0.f;
+        if (at != AASD_NONE) {
+            const uint8_t* block = a.pages + ((int64_t)(at / kPage) * hkv + head) * kv_head_bytes(D);
+            const int off = at % kPage;
+            const unsigned long long bytes = value ? *reinterpret_cast<const unsigned long long*>(s_code + q * kPitch + 8 * l)
+                                                   : *reinterpret_cast<const unsigned long long*>(block + off * H + 8 * l);
+            const unsigned int meta = reinterpret_cast<const unsigned int*>(block + (value ? kv_value_meta_offset(D) : kv_key_meta_offset(D)))[off];
+            const float s = meta_scale(meta), m = meta_min(meta);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) bytes |= (unsigned long long)col[(8 * l + e) * kPage] << (8 * e);
-            meta = reinterpret_cast<const unsigned int*>(block + kv_value_meta_offset(D))[at];
+            for (int e = 0; e < 8; ++e) {
+                const unsigned int b = (unsigned int)(bytes >> (8 * e)) & 255u;
+                x[e] = __fadd_rn(__fmul_rn(s, (float)(b & 15u)), m);
+                y[e] = __fadd_rn(__fmul_rn(s, (float)(b >> 4)), m);
+            }
         }
-        const float s = meta_scale(meta), m = meta_min(meta);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const unsigned int b = (unsigned int)(bytes >> (8 * e)) & 255u;
-            x[e] = __fadd_rn(__fmul_rn(s, (float)(b & 15u)), m);
-            y[e] = __fadd_rn(__fmul_rn(s, (float)(b >> 4)), m);
-        }
+        const int64_t to = ((i0 + q) * hkv + head) * D + 8 * l;
+        store8<DT, VEC>(out, to, x);
+        store8<DT, VEC>(out, to + H, y);
     }
-    const int64_t to = (i * a.n_kv_heads + head) * D + 8 * l;
-    store8<DT, VEC>(out, to, x);
-    store8<DT, VEC>(out, to + H, y);
 }
 
 // ---- the accepted path ------------------------------------------------------------------------------
@@ -598,7 +739,7 @@ template <int D>
 __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const KvCommitArgs a) {
     constexpr int H = D / 2, W = H / 4;        // W: 32-bit words of a token's keys
     __shared__ int s_node[AASD_KV_MAX_NODES];   // parents, then sources
-    __shared__ int s_path[AASD_KV_MAX_NODES];
+    __shared__ int s_path[AASD_KV_MAX_NODES];   // leaf first
     __shared__ int s_len, s_bad;
     pdl_launch_dependents();
     pdl_wait();
@@ -664,19 +805,37 @@ __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const KvCommi
          it += (int64_t)gridDim.y * (kCommitThreads / 32)) {
         const int layer = (int)(it / a.p.n_kv_heads), head = (int)(it % a.p.n_kv_heads);
         uint8_t* pool = a.pages + (int64_t)layer * a.p.layer_stride;
-        for (int i = from; i < len; ++i) {
-            const int src = s_node[i], dst = slot_of(i);
-            if (src == dst) continue;
-            const uint8_t* sb = pool + ((int64_t)(src / kPage) * a.p.n_kv_heads + head) * hb;
-            uint8_t* db = pool + ((int64_t)(dst / kPage) * a.p.n_kv_heads + head) * hb;
-            const int so = src % kPage, to = dst % kPage;
-            for (int w = lane; w < W; w += 32)
-                reinterpret_cast<unsigned int*>(db + to * H)[w] = reinterpret_cast<const unsigned int*>(sb + so * H)[w];
-            for (int r = lane; r < H; r += 32)
-                db[kv_value_offset(D) + r * kPage + to] = sb[kv_value_offset(D) + r * kPage + so];
-            if (lane < 2) {
-                const int off = kv_key_meta_offset(D) + lane * kPage * 4;
-                reinterpret_cast<unsigned int*>(db + off)[to] = reinterpret_cast<const unsigned int*>(sb + off)[so];
+        constexpr int NB = 4;                                    // entries whose loads are under way together
+        constexpr int KW = (W + 31) / 32, VW = (H + 31) / 32;    // words of keys, bytes of values per lane
+        for (int i0 = from; i0 < len; i0 += NB) {
+            unsigned int kw[NB][KW], meta[NB];
+            uint8_t vb[NB][VW];
+            int dst[NB];
+#pragma unroll
+            for (int e = 0; e < NB; ++e) {
+                const int src = s_node[min(i0 + e, len - 1)];
+                dst[e] = slot_of(min(i0 + e, len - 1));
+                const uint8_t* sb = pool + ((int64_t)(src / kPage) * a.p.n_kv_heads + head) * hb;
+                const int so = src % kPage;
+#pragma unroll
+                for (int w = 0; w < KW; ++w)
+                    kw[e][w] = lane + 32 * w < W ? reinterpret_cast<const unsigned int*>(sb + so * H)[lane + 32 * w] : 0u;
+#pragma unroll
+                for (int w = 0; w < VW; ++w) vb[e][w] = sb[kv_value_offset(D) + (lane + 32 * w) * kPage + so];
+                meta[e] = reinterpret_cast<const unsigned int*>(sb + kv_key_meta_offset(D) + (lane & 1) * kPage * 4)[so];
+            }
+            __syncwarp();   // every lane has its loads before the first store
+#pragma unroll
+            for (int e = 0; e < NB; ++e) {
+                if (i0 + e >= len) break;
+                uint8_t* db = pool + ((int64_t)(dst[e] / kPage) * a.p.n_kv_heads + head) * hb;
+                const int to = dst[e] % kPage;
+#pragma unroll
+                for (int w = 0; w < KW; ++w)
+                    if (lane + 32 * w < W) reinterpret_cast<unsigned int*>(db + to * H)[lane + 32 * w] = kw[e][w];
+#pragma unroll
+                for (int w = 0; w < VW; ++w) db[kv_value_offset(D) + (lane + 32 * w) * kPage + to] = vb[e][w];
+                if (lane < 2) reinterpret_cast<unsigned int*>(db + kv_key_meta_offset(D) + lane * kPage * 4)[to] = meta[e];
             }
             __syncwarp();
         }
