@@ -251,7 +251,7 @@ def _kv_dim(pages: torch.Tensor) -> int:
 
 def _kv_i32(*tensors):
     for t in tensors:
-        assert t is None or (t.dtype == torch.int32 and t.is_cuda and t.is_contiguous()), "int32, on the device, contiguous"
+        assert t is None or (t.dtype is torch.int32 and t.is_cuda and t.is_contiguous()), "int32, on the device, contiguous"
 
 
 def verify_static(target_logits, draft_ids, cand_offsets=None, draft_flags=None, alpha=0.1,
@@ -316,6 +316,7 @@ class Context:
         self._ws = None
         self._ws_rows = self._ws_cands = -1
         self._kv_ws, self._kv_ws_dim = None, 0
+        self._kv_structs = {}     # parameter structs by their values (filling one costs as much as the call)
 
     def close(self):
         if self._h:
@@ -532,6 +533,16 @@ class Context:
         _check(self.lib.aasd_probe_read(self._h, _p(buffer), n - n % 16, _p(sink)), "aasd_probe_read")
 
     # ---- the paged 4-bit cache ------------------------------------------------------------
+    def _kv_struct(self, cls, *values):
+        key = (cls, values)
+        r = self._kv_structs.get(key)
+        if r is None:
+            if len(self._kv_structs) > 4096:
+                self._kv_structs.clear()
+            prm = cls(*values)
+            r = self._kv_structs[key] = (C.byref(prm), prm)
+        return r[0]
+
     def kv_plan(self, cached_len, n_new, block_table, seq_pages, free_pages, n_free, n_tokens,
                 rows_per_seq=0, node_depth=None, outputs=None):
         """aasd_kv_plan: brings ``block_table`` [B, max_pages], ``seq_pages``, ``free_pages`` and
@@ -539,16 +550,17 @@ class Context:
         sequence; returns kv_len, tok_offsets, slot_map and positions of the new tokens."""
         _kv_i32(cached_len, n_new, block_table, seq_pages, free_pages, n_free, node_depth)
         B, P = block_table.shape
-        dev = block_table.device
-        o = outputs or dict(kv_len=torch.empty(B, dtype=torch.int32, device=dev),
-                            tok_offsets=torch.empty(B + 1, dtype=torch.int32, device=dev),
-                            slot_map=torch.empty(n_tokens, dtype=torch.int32, device=dev),
-                            positions=torch.empty(n_tokens, dtype=torch.int32, device=dev))
-        prm = KvPlanParams(B, free_pages.numel(), P, int(rows_per_seq), int(n_tokens))
-        st = KvPlanState(_p(block_table), _p(seq_pages), _p(free_pages), _p(n_free))
-        out = KvPlanOut(_p(o["kv_len"]), _p(o["tok_offsets"]), _p(o["slot_map"]), _p(o["positions"]))
-        _check(self.lib.aasd_kv_plan(self._h, _p(cached_len), _p(n_new), _p(node_depth), C.byref(prm),
-                                     C.byref(st), C.byref(out)), "aasd_kv_plan")
+        o = outputs
+        if o is None:
+            new = block_table.new_empty
+            o = dict(kv_len=new(B), tok_offsets=new(B + 1), slot_map=new(n_tokens), positions=new(n_tokens))
+        prm = self._kv_struct(KvPlanParams, B, free_pages.numel(), P, int(rows_per_seq), int(n_tokens))
+        st = KvPlanState(block_table.data_ptr(), seq_pages.data_ptr(), free_pages.data_ptr(), n_free.data_ptr())
+        out = KvPlanOut(o["kv_len"].data_ptr(), o["tok_offsets"].data_ptr(), o["slot_map"].data_ptr(), o["positions"].data_ptr())
+        rc = self.lib.aasd_kv_plan(self._h, cached_len.data_ptr(), n_new.data_ptr(),
+                                   None if node_depth is None else node_depth.data_ptr(), prm, C.byref(st), C.byref(out))
+        if rc:
+            raise AasdError(rc, "aasd_kv_plan")
         return o
 
     def kv_write(self, pages, q, k, v, slot_map, positions, cos_sin=None, q_weight=None, k_weight=None,
@@ -560,21 +572,32 @@ class Context:
         _kv_i32(slot_map, positions)
         T, Hq, D = q.shape
         Hkv = k.shape[1]
-        assert q.stride(2) == 1 and (T == 0 or (q.stride(1) == D and k.stride(1) == D and v.stride(1) == D))
-        assert k.dtype == q.dtype and v.dtype == q.dtype and k.shape == v.shape and k.shape[2] == D and _kv_dim(pages) == D
-        assert pages.dtype == torch.uint8 and pages.is_contiguous() and pages.shape[1] == Hkv
+        qs, ks, vs = q.stride(), k.stride(), v.stride()
+        assert qs[2] == 1 and (T == 0 or (qs[1] == D and ks[1] == D and vs[1] == D and ks[2] == 1 and vs[2] == 1))
+        dt = q.dtype
+        assert k.dtype is dt and v.dtype is dt and k.shape == v.shape and k.shape[2] == D and _kv_dim(pages) == D
+        assert pages.dtype is torch.uint8 and pages.is_contiguous() and pages.shape[1] == Hkv
         assert slot_map.numel() == T and positions.numel() == T
         for w in (q_weight, k_weight):
-            assert w is None or (w.dtype == q.dtype and w.numel() == D and w.is_contiguous())
-        assert cos_sin is None or (cos_sin.dtype == torch.float32 and cos_sin.is_contiguous())
-        o = outputs or dict(q=torch.empty((T, Hq, D), dtype=q.dtype, device=q.device),
-                            k=torch.empty((T, Hkv, D), dtype=q.dtype, device=q.device) if keep_k else None)
-        prm = KvWriteParams(Hq, Hkv, D, pages.shape[0], _dtype_code(q), q.stride(0), k.stride(0), v.stride(0),
-                            0 if cos_sin is None else cos_sin.shape[1], 0 if cos_sin is None else cos_sin.shape[0],
-                            eps, KV_ROPE_INTERLEAVED if interleaved else 0)
-        _check(self.lib.aasd_kv_write(self._h, _p(q), _p(k), _p(v), _p(q_weight), _p(k_weight), _p(cos_sin),
-                                      _p(positions), _p(slot_map), T, C.byref(prm), _p(pages), _p(o["q"]),
-                                      _p(o.get("k"))), "aasd_kv_write")
+            assert w is None or (w.dtype is dt and w.numel() == D and w.is_contiguous())
+        o = outputs
+        if o is None:
+            o = dict(q=q.new_empty((T, Hq, D)), k=q.new_empty((T, Hkv, D)) if keep_k else None)
+        rot = limit = 0
+        if cos_sin is not None:
+            assert cos_sin.dtype is torch.float32 and cos_sin.is_contiguous()
+            limit, rot = cos_sin.shape
+        prm = self._kv_struct(KvWriteParams, Hq, Hkv, D, pages.shape[0], _dtype_code(q), qs[0], ks[0], vs[0], rot, limit,
+                              eps, KV_ROPE_INTERLEAVED if interleaved else 0)
+        ko = o.get("k")
+        rc = self.lib.aasd_kv_write(self._h, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                    None if q_weight is None else q_weight.data_ptr(),
+                                    None if k_weight is None else k_weight.data_ptr(),
+                                    None if cos_sin is None else cos_sin.data_ptr(), positions.data_ptr(),
+                                    slot_map.data_ptr(), T, prm, pages.data_ptr(), o["q"].data_ptr(),
+                                    None if ko is None else ko.data_ptr())
+        if rc:
+            raise AasdError(rc, "aasd_kv_write")
         return o
 
     def kv_workspace(self, head_dim: int) -> torch.Tensor:
@@ -600,18 +623,25 @@ class Context:
         _kv_i32(block_table, cached_len, kv_len, tok_offsets, node_parent)
         T, Hq, D = q.shape
         B, P = block_table.shape
-        assert q.stride(2) == 1 and (T == 0 or q.stride(1) == D) and _kv_dim(pages) == D
-        assert pages.dtype == torch.uint8 and pages.is_contiguous()
-        o = outputs or dict(out=torch.empty((T, Hq, D), dtype=q.dtype, device=q.device))
-        if want_lse and "lse" not in o:
-            o["lse"] = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
-        prm = KvAttendParams(B, Hq, pages.shape[1], D, pages.shape[0], P, _dtype_code(q), int(rows_per_seq), T,
-                             q.stride(0), scale)
-        out = KvAttendOut(_p(o["out"]), _p(o.get("lse")))
+        qs = q.stride()
+        assert qs[2] == 1 and (T == 0 or qs[1] == D) and _kv_dim(pages) == D
+        assert pages.dtype is torch.uint8 and pages.is_contiguous()
+        o = outputs
+        if o is None:
+            o = dict(out=q.new_empty((T, Hq, D)))
+        lse = o.get("lse")
+        if want_lse and lse is None:
+            lse = o["lse"] = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
+        prm = self._kv_struct(KvAttendParams, B, Hq, pages.shape[1], D, pages.shape[0], P, _dtype_code(q), int(rows_per_seq),
+                              T, qs[0], scale)
+        out = KvAttendOut(o["out"].data_ptr(), None if lse is None else lse.data_ptr())
         ws = self.kv_workspace(D)
-        _check(self.lib.aasd_kv_attend(self._h, _p(q), _p(pages), _p(block_table), _p(cached_len), _p(kv_len),
-                                       _p(tok_offsets), _p(node_parent), C.byref(prm), _p(ws), ws.numel(),
-                                       C.byref(out)), "aasd_kv_attend")
+        rc = self.lib.aasd_kv_attend(self._h, q.data_ptr(), pages.data_ptr(), block_table.data_ptr(), cached_len.data_ptr(),
+                                     kv_len.data_ptr(), None if tok_offsets is None else tok_offsets.data_ptr(),
+                                     None if node_parent is None else node_parent.data_ptr(), prm, ws.data_ptr(),
+                                     ws.numel(), C.byref(out))
+        if rc:
+            raise AasdError(rc, "aasd_kv_attend")
         return o
 
     def kv_commit(self, pages, block_table, cached_len, kv_len, best_node, node_parent, tok_offsets=None,
@@ -620,27 +650,33 @@ class Context:
         [layers, n_pages, Hkv, bytes]) and returns the new cached lengths.  ``node_parent`` is
         [B, rows_per_seq], or flat with ``tok_offsets``."""
         _kv_i32(block_table, cached_len, kv_len, best_node, node_parent, tok_offsets)
-        assert pages.dim() == 4 and pages.dtype == torch.uint8 and pages.is_contiguous()
+        assert pages.dim() == 4 and pages.dtype is torch.uint8 and pages.is_contiguous()
         B, P = block_table.shape
         L, N, H, _ = pages.shape
-        new_len = outputs if outputs is not None else torch.empty_like(cached_len)
-        prm = KvCommitParams(B, H, _kv_dim(pages), N, P, 0 if tok_offsets is not None else node_parent.shape[1], L,
-                             pages.stride(0))
-        _check(self.lib.aasd_kv_commit(self._h, _p(pages), _p(block_table), _p(cached_len), _p(kv_len),
-                                       _p(tok_offsets), _p(best_node), _p(node_parent), C.byref(prm), _p(new_len)),
-               "aasd_kv_commit")
+        new_len = outputs if outputs is not None else cached_len.new_empty(B)
+        prm = self._kv_struct(KvCommitParams, B, H, _kv_dim(pages), N, P,
+                              0 if tok_offsets is not None else node_parent.shape[1], L, pages.stride(0))
+        rc = self.lib.aasd_kv_commit(self._h, pages.data_ptr(), block_table.data_ptr(), cached_len.data_ptr(), kv_len.data_ptr(),
+                                     None if tok_offsets is None else tok_offsets.data_ptr(), best_node.data_ptr(),
+                                     node_parent.data_ptr(), prm, new_len.data_ptr())
+        if rc:
+            raise AasdError(rc, "aasd_kv_commit")
         return new_len
 
     def kv_read(self, pages, slots, head_dim, dtype=torch.bfloat16, outputs=None):
         """aasd_kv_read: the entries at ``slots`` as values, k and v [n, Hkv, D].  Several layers at
         once: pass ``pages.flatten(0, 1)`` and slots raised by layer * n_pages * KV_PAGE."""
         _kv_i32(slots)
-        assert pages.dim() == 3 and pages.dtype == torch.uint8 and pages.is_contiguous() and _kv_dim(pages) == head_dim
-        n, H = slots.numel(), pages.shape[1]
-        o = outputs or dict(k=torch.empty((n, H, head_dim), dtype=dtype, device=pages.device),
-                            v=torch.empty((n, H, head_dim), dtype=dtype, device=pages.device))
-        _check(self.lib.aasd_kv_read(self._h, _p(pages), _p(slots), n, pages.shape[0], H, int(head_dim),
-                                     _dtype_code(o["k"]), _p(o["k"]), _p(o["v"])), "aasd_kv_read")
+        assert pages.dim() == 3 and pages.dtype is torch.uint8 and pages.is_contiguous() and _kv_dim(pages) == head_dim
+        n, N, H = slots.numel(), pages.shape[0], pages.shape[1]
+        o = outputs
+        if o is None:
+            shape = (n, H, head_dim)
+            o = dict(k=torch.empty(shape, dtype=dtype, device=pages.device), v=torch.empty(shape, dtype=dtype, device=pages.device))
+        rc = self.lib.aasd_kv_read(self._h, pages.data_ptr(), slots.data_ptr(), n, N, H, head_dim, _dtype_code(o["k"]),
+                                   o["k"].data_ptr(), o["v"].data_ptr())
+        if rc:
+            raise AasdError(rc, "aasd_kv_read")
         return o
 
     def select(self, accept_len, next_token, draft_ids, emit_stride, cand_offsets=None,

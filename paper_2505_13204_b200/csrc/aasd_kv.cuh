@@ -44,9 +44,24 @@ __device__ __forceinline__ KvQuant kv_quantiser(float lo, float hi, bool bad) {
     z.meta = (__float_as_uint(m) & 0xFFFF0000u) | (__float_as_uint(s) >> 16);
     return z;
 }
-__device__ __forceinline__ unsigned int kv_code(float x, const KvQuant& z) {
-    const float c = rintf(__fmul_rn(__fsub_rn(x, z.m), z.inv));
-    return (unsigned int)fminf(fmaxf(c, 0.f), 15.f);   // (NaN cannot reach this: such rows are zeroed)
+// Codes of eight channels of each half of a row, a byte per pair.  Adding 1.5 * 2^23 to a value in 0..15
+// rounds it to the nearest whole number (ties to even) and leaves that in the low bits.  (NaN
+// cannot reach this: such rows are zeroed.)
+__device__ __forceinline__ unsigned long long kv_row_codes(const float2 (&x)[4], const float2 (&y)[4], const KvQuant& z, bool bad) {
+    const float2 m = make_float2(-z.m, -z.m), inv = make_float2(z.inv, z.inv), magic = make_float2(12582912.f, 12582912.f);
+    unsigned int word[2] = {0u, 0u};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float2 a = __fmul2_rn(__fadd2_rn(x[e], m), inv), b = __fmul2_rn(__fadd2_rn(y[e], m), inv);
+        a = make_float2(fminf(fmaxf(a.x, 0.f), 15.f), fminf(fmaxf(a.y, 0.f), 15.f));
+        b = make_float2(fminf(fmaxf(b.x, 0.f), 15.f), fminf(fmaxf(b.y, 0.f), 15.f));
+        a = __fadd2_rn(a, magic);
+        b = __fadd2_rn(b, magic);
+        const unsigned int c0 = (__float_as_uint(a.x) & 15u) | ((__float_as_uint(b.x) & 15u) << 4);
+        const unsigned int c1 = (__float_as_uint(a.y) & 15u) | ((__float_as_uint(b.y) & 15u) << 4);
+        word[e >> 1] |= (c0 | (c1 << 8)) << (16 * (e & 1));
+    }
+    return bad ? 0ull : (unsigned long long)word[0] | ((unsigned long long)word[1] << 32);
 }
 
 // Eight consecutive elements as fp32; `vec`: the address is 16-byte aligned.
@@ -65,6 +80,45 @@ __device__ __forceinline__ void load8(const void* base, int64_t i, float (&x)[8]
         Elt<AASD_BF16>::unpack(q, x);
     }
 }
+// The same eight elements as they come from memory, so that many can be under way in few registers.
+template <int DT, bool VEC>
+struct Raw8 {
+    uint4 a, b;   // (bf16: a alone)
+    __device__ __forceinline__ void clear() { a = b = make_uint4(0u, 0u, 0u, 0u); }
+    __device__ __forceinline__ void load(const void* base, int64_t i) {
+        if constexpr (!VEC) {
+            float x[8];
+            load8<DT, false>(base, i, x);
+            if constexpr (DT == AASD_F32) {
+                a = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+                b = make_uint4(__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7]));
+            } else {   // (bf16 values as fp32 hold their bits in the upper half)
+                a.x = (__float_as_uint(x[0]) >> 16) | __float_as_uint(x[1]);
+                a.y = (__float_as_uint(x[2]) >> 16) | __float_as_uint(x[3]);
+                a.z = (__float_as_uint(x[4]) >> 16) | __float_as_uint(x[5]);
+                a.w = (__float_as_uint(x[6]) >> 16) | __float_as_uint(x[7]);
+            }
+        } else if constexpr (DT == AASD_F32) {
+            const uint4* p = reinterpret_cast<const uint4*>(static_cast<const float*>(base) + i);
+            a = __ldg(p);
+            b = __ldg(p + 1);
+        } else {
+            a = __ldg(reinterpret_cast<const uint4*>(static_cast<const unsigned short*>(base) + i));
+        }
+    }
+    __device__ __forceinline__ void unpack(float2 (&x)[4]) const {
+        if constexpr (DT == AASD_F32) {
+            x[0] = make_float2(__uint_as_float(a.x), __uint_as_float(a.y));
+            x[1] = make_float2(__uint_as_float(a.z), __uint_as_float(a.w));
+            x[2] = make_float2(__uint_as_float(b.x), __uint_as_float(b.y));
+            x[3] = make_float2(__uint_as_float(b.z), __uint_as_float(b.w));
+        } else {
+            const unsigned int w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = make_float2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xFFFF0000u));
+        }
+    }
+};
 __device__ __forceinline__ unsigned int pack_bf16(float a, float b) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const unsigned int*>(&h);
@@ -91,6 +145,12 @@ __device__ __forceinline__ void store8(void* base, int64_t i, const float (&x)[8
             for (int e = 0; e < 8; ++e) p[e] = __float2bfloat16_rn(x[e]);
         }
     }
+}
+
+template <int DT, bool VEC>
+__device__ __forceinline__ void store8(void* base, int64_t i, const float2 (&x)[4]) {
+    const float y[8] = {x[0].x, x[0].y, x[1].x, x[1].y, x[2].x, x[2].y, x[3].x, x[3].y};
+    store8<DT, VEC>(base, i, y);
 }
 
 // ---- page tables, slots and positions -----------------------------------------------------------
@@ -404,32 +464,27 @@ __device__ __forceinline__ unsigned int kv_write_token(const KvWriteArgs& a, int
 }
 // Quantiser of a row spread over L lanes; every lane of the warp takes part.
 template <int L>
-__device__ __forceinline__ KvQuant kv_row_quantiser(const float (&x)[8], const float (&y)[8], bool& bad) {
-    float lo = x[0], hi = x[0], sick = 0.f;   // sick: NaN as soon as one value is NaN or infinite
+__device__ __forceinline__ KvQuant kv_row_quantiser(const float2 (&x)[4], const float2 (&y)[4], bool& bad) {
+    float lo = x[0].x, hi = x[0].x;
+    float2 sick = make_float2(0.f, 0.f);   // NaN as soon as one value is NaN or infinite
+    const float2 zero = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        lo = fminf(lo, fminf(x[e], y[e]));
-        hi = fmaxf(hi, fmaxf(x[e], y[e]));
-        sick += x[e] * 0.f + y[e] * 0.f;
+    for (int e = 0; e < 4; ++e) {
+        lo = fminf(lo, fminf(fminf(x[e].x, x[e].y), fminf(y[e].x, y[e].y)));
+        hi = fmaxf(hi, fmaxf(fmaxf(x[e].x, x[e].y), fmaxf(y[e].x, y[e].y)));
+        sick = __ffma2_rn(x[e], zero, sick);
+        sick = __ffma2_rn(y[e], zero, sick);
     }
+    float s = sick.x + sick.y;
 #pragma unroll
     for (int o = 1; o < L; o <<= 1) {
         lo = fminf(lo, __shfl_xor_sync(0xFFFFFFFFu, lo, o));
         hi = fmaxf(hi, __shfl_xor_sync(0xFFFFFFFFu, hi, o));
-        sick += __shfl_xor_sync(0xFFFFFFFFu, sick, o);
+        s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
     }
     const float m = bf16_round(lo);
-    bad = sick != 0.f || !(hi - m <= 3.3e38f) || !(fabsf(m) <= 3.4e38f);
+    bad = s != 0.f || !(hi - m <= 3.3e38f) || !(fabsf(m) <= 3.4e38f);
     return kv_quantiser(lo, hi, bad);
-}
-__device__ __forceinline__ unsigned long long kv_row_codes(const float (&x)[8], const float (&y)[8], const KvQuant& z, bool bad) {
-    unsigned long long bytes = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const unsigned int b = bad ? 0u : kv_code(x[e], z) | (kv_code(y[e], z) << 4);
-        bytes |= (unsigned long long)b << (8 * e);
-    }
-    return bytes;
 }
 
 template <int DT, int D, bool VEC, int HP>
@@ -454,14 +509,17 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteAr
             const bool live = t < a.n_tokens;
             int pos, slot = AASD_NONE;
             if (live) bits |= kv_write_token(a, t, true, pos, slot);
-            float x[8], y[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = y[e] = 0.f;
+            Raw8<DT, VEC> rx, ry;
+            rx.clear();
+            ry.clear();
             if (slot != AASD_NONE) {
                 const int64_t at = t * a.p.v_stride + (int64_t)head * D + 8 * l;
-                load8<DT, VEC>(a.v, at, x);
-                load8<DT, VEC>(a.v, at + H, y);
+                rx.load(a.v, at);
+                ry.load(a.v, at + H);
             }
+            float2 x[4], y[4];
+            rx.unpack(x);
+            ry.unpack(y);
             bool bad;
             const KvQuant z = kv_row_quantiser<L>(x, y, bad);
             if (slot != AASD_NONE && bad) bits |= AASD_STATUS_BAD_ROW;
@@ -503,17 +561,17 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteAr
     int pos = AASD_NONE, slot = AASD_NONE;
     if (live) bits |= kv_write_token(a, t, hkv > 0, pos, slot);
     const bool used = live && pos != AASD_NONE;
-    float x[HP][8], y[HP][8];   // channels 8l + e and D/2 + 8l + e
+    Raw8<DT, VEC> rx[HP], ry[HP];   // channels 8l .. and D/2 + 8l ..
 #pragma unroll
     for (int i = 0; i < HP; ++i) {
         const int h = h0 + i;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[i][e] = y[i][e] = 0.f;
+        rx[i].clear();
+        ry[i].clear();
         if (used && h < heads) {
             const void* src = h < hq ? a.q : a.k;
             const int64_t at = h < hq ? t * a.p.q_stride + (int64_t)h * D + 8 * l : t * a.p.k_stride + (int64_t)(h - hq) * D + 8 * l;
-            load8<DT, VEC>(src, at, x[i]);
-            load8<DT, VEC>(src, at + H, y[i]);
+            rx[i].load(src, at);
+            ry[i].load(src, at + H);
         }
     }
     // cosines and sines of the lane's pairs (the branches on the form of the rotation are the same for every lane)
@@ -541,50 +599,63 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteAr
             load8<AASD_F32, VEC>(cs, half + 8 * l, si);
         }
     }
+    float2 wx[4], wy[4];
+    const void* held = nullptr;    // the weight that wx, wy hold
 #pragma unroll
     for (int i = 0; i < HP; ++i) {
         const int h = h0 + i;
         const bool row = used && h < heads, key = h >= hq;
         const void* w = key ? a.k_weight : a.q_weight;
-        float(&u)[8] = x[i];
-        float(&v)[8] = y[i];
+        float2 u[4], v[4];
+        rx[i].unpack(u);
+        ry[i].unpack(v);
         // (the lanes of a row take the same way; shuffles stay among all lanes of the warp)
-        float s[8];
+        float s[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] = __fadd_rn(__fmul_rn(u[e], u[e]), __fmul_rn(v[e], v[e]));
-        float sum = __fadd_rn(__fadd_rn(__fadd_rn(s[0], s[1]), __fadd_rn(s[2], s[3])), __fadd_rn(__fadd_rn(s[4], s[5]), __fadd_rn(s[6], s[7])));
+        for (int e = 0; e < 4; ++e) {
+            const float2 q = __fadd2_rn(__fmul2_rn(u[e], u[e]), __fmul2_rn(v[e], v[e]));
+            s[e] = __fadd_rn(q.x, q.y);
+        }
+        float sum = __fadd_rn(__fadd_rn(s[0], s[1]), __fadd_rn(s[2], s[3]));
 #pragma unroll
         for (int o = 1; o < L; o <<= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xFFFFFFFFu, sum, o));
         if (row && w != nullptr) {
+            if (w != held) {
+                held = w;
+                Raw8<DT, VEC> g;
+                g.load(w, 8 * l);
+                g.unpack(wx);
+                g.load(w, H + 8 * l);
+                g.unpack(wy);
+            }
             const float r = __frcp_rn(__fsqrt_rn(__fadd_rn(__fmul_rn(sum, 1.0f / D), a.p.eps)));
-            float wx[8], wy[8];
-            load8<DT, VEC>(w, 8 * l, wx);
-            load8<DT, VEC>(w, H + 8 * l, wy);
+            const float2 rr = make_float2(r, r);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                u[e] = __fmul_rn(__fmul_rn(u[e], r), wx[e]);
-                v[e] = __fmul_rn(__fmul_rn(v[e], r), wy[e]);
+            for (int e = 0; e < 4; ++e) {
+                u[e] = __fmul2_rn(__fmul2_rn(u[e], rr), wx[e]);
+                v[e] = __fmul2_rn(__fmul2_rn(v[e], rr), wy[e]);
             }
         }
+        // (a - b is written a + (-b): the same rounding)
         if (rot > 0 && neighbours) {
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
-                float(&z)[8] = part ? v : u;
+                float2(&z)[4] = part ? v : u;
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    if (part * H + 8 * l + e < rot) {
-                        const float p = z[e], q = z[e + 1], c = co[4 * part + e / 2], n = si[4 * part + e / 2];
-                        z[e] = __fsub_rn(__fmul_rn(p, c), __fmul_rn(q, n));
-                        z[e + 1] = __fadd_rn(__fmul_rn(q, c), __fmul_rn(p, n));
+                for (int e = 0; e < 4; ++e) {
+                    if (part * H + 8 * l + 2 * e < rot) {
+                        const float c = co[4 * part + e], n = si[4 * part + e];
+                        z[e] = __fadd2_rn(__fmul2_rn(z[e], make_float2(c, c)), __fmul2_rn(make_float2(z[e].y, z[e].x), make_float2(-n, n)));
                     }
                 }
             }
         } else if (rot == D) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float p = u[e], q = v[e];
-                u[e] = __fsub_rn(__fmul_rn(p, co[e]), __fmul_rn(q, si[e]));
-                v[e] = __fadd_rn(__fmul_rn(q, co[e]), __fmul_rn(p, si[e]));
+            for (int e = 0; e < 4; ++e) {
+                const float2 c = make_float2(co[2 * e], co[2 * e + 1]), n = make_float2(si[2 * e], si[2 * e + 1]);
+                const float2 p = u[e], q = v[e];
+                u[e] = __fadd2_rn(__fmul2_rn(p, c), __fmul2_rn(q, make_float2(-n.x, -n.y)));
+                v[e] = __fadd2_rn(__fmul2_rn(q, c), __fmul2_rn(p, n));
             }
         } else if (rot > 0) {
             // a pair (c, c + half) inside the first rot channels: its members may be different lanes',
@@ -592,20 +663,21 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteAr
             float* mine = s_rows + group * D;
             __syncwarp();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                mine[8 * l + e] = u[e];
-                mine[H + 8 * l + e] = v[e];
+            for (int e = 0; e < 4; ++e) {
+                *reinterpret_cast<float2*>(mine + 8 * l + 2 * e) = u[e];
+                *reinterpret_cast<float2*>(mine + H + 8 * l + 2 * e) = v[e];
             }
             __syncwarp();
             if (row) {
 #pragma unroll
                 for (int part = 0; part < 2; ++part) {
-                    float(&z)[8] = part ? v : u;
+                    float2(&z)[4] = part ? v : u;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
+                        float& x = e & 1 ? z[e >> 1].y : z[e >> 1].x;
                         const int c = part * H + 8 * l + e;
-                        if (c < half) z[e] = __fsub_rn(__fmul_rn(z[e], cs[c]), __fmul_rn(mine[c + half], cs[half + c]));
-                        else if (c < rot) z[e] = __fadd_rn(__fmul_rn(z[e], cs[c - half]), __fmul_rn(mine[c - half], cs[c]));
+                        if (c < half) x = __fsub_rn(__fmul_rn(x, cs[c]), __fmul_rn(mine[c + half], cs[half + c]));
+                        else if (c < rot) x = __fadd_rn(__fmul_rn(x, cs[c - half]), __fmul_rn(mine[c - half], cs[c]));
                     }
                 }
             }
