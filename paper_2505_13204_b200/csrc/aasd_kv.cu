@@ -98,7 +98,8 @@ int aasd_kv_write(aasd_ctx* ctx, const void* q, const void* k, const void* v, co
     if (hkv > 0) vec = vec && (p->k_stride * es) % 16 == 0 && (p->v_stride * es) % 16 == 0;
     const int lanes = D / 16;
     const int64_t rows = n_tokens * (hq + hkv);
-    const bool sets = vec && rows * lanes >= kManyRowThreads;
+    const bool full = p->rotary_dim == D && !(p->flags & AASD_KV_ROPE_INTERLEAVED);
+    const bool sets = vec && full && rows * lanes >= kManyRowThreads;
     const int64_t groups = sets ? n_tokens * ((hq + hkv + 3) / 4) : rows;
     const int64_t value_blocks = (n_tokens + kValueTokens - 1) / kValueTokens * hkv;
     const int64_t blocks = value_blocks + (groups * lanes + kWriteThreads - 1) / kWriteThreads;
@@ -108,9 +109,10 @@ int aasd_kv_write(aasd_ctx* ctx, const void* q, const void* k, const void* v, co
     with_type(p->dtype, [&](auto dt) {
         with_dim(D, [&](auto d) {
             auto go = [&](auto kernel) { launch(kernel, (unsigned int)blocks, (unsigned int)kWriteThreads, 0, ctx->stream, a); };
-            if (vec && sets) go(kv_write_kernel<dt(), d(), true, 4>);
-            else if (vec) go(kv_write_kernel<dt(), d(), true, 1>);
-            else go(kv_write_kernel<dt(), d(), false, 1>);
+            if (sets) go(kv_write_kernel<dt(), d(), true, 4, true>);
+            else if (vec && full) go(kv_write_kernel<dt(), d(), true, 1, true>);
+            else if (vec) go(kv_write_kernel<dt(), d(), true, 1, false>);
+            else go(kv_write_kernel<dt(), d(), false, 1, false>);
         });
     });
     return after_launch(ctx, 1);

@@ -487,13 +487,14 @@ __device__ __forceinline__ KvQuant kv_row_quantiser(const float2 (&x)[4], const 
     return kv_quantiser(lo, hi, bad);
 }
 
-template <int DT, int D, bool VEC, int HP>
+// FULL: all D channels are rotated, in halves (the usual form); otherwise whatever the parameters say.
+template <int DT, int D, bool VEC, int HP, bool FULL>
 __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteArgs a) {
     constexpr int L = D / 16;              // lanes of a row
     constexpr int H = D / 2;
     // rows in passage: partial rotation (a float per channel), or the values' codes (rows padded to 8 bytes more)
     constexpr int kRows = kWriteThreads / L, kPitch = H + 8;
-    __shared__ alignas(16) unsigned char s_mem[kRows * D * 4 > kValueTokens * kPitch ? kRows * D * 4 : kValueTokens * kPitch];
+    __shared__ alignas(16) unsigned char s_mem[!FULL && kRows * D * 4 > kValueTokens * kPitch ? kRows * D * 4 : kValueTokens * kPitch];
     __shared__ int s_slot[kValueTokens];
     pdl_launch_dependents();
     pdl_wait();
@@ -507,16 +508,17 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteAr
         for (int k = group; k < kValueTokens; k += kRows) {
             const int64_t t = t0 + k;
             const bool live = t < a.n_tokens;
-            int pos, slot = AASD_NONE;
-            if (live) bits |= kv_write_token(a, t, true, pos, slot);
+            // (the row does not wait for its slot)
             Raw8<DT, VEC> rx, ry;
             rx.clear();
             ry.clear();
-            if (slot != AASD_NONE) {
+            if (live) {
                 const int64_t at = t * a.p.v_stride + (int64_t)head * D + 8 * l;
                 rx.load(a.v, at);
                 ry.load(a.v, at + H);
             }
+            int pos, slot = AASD_NONE;
+            if (live) bits |= kv_write_token(a, t, true, pos, slot);
             float2 x[4], y[4];
             rx.unpack(x);
             ry.unpack(y);
@@ -558,25 +560,33 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteAr
     const bool live = g < a.n_tokens * sets;
     const int64_t t = live ? g / sets : 0;
     const int h0 = live ? (int)(g - t * sets) * HP : 0;
-    int pos = AASD_NONE, slot = AASD_NONE;
-    if (live) bits |= kv_write_token(a, t, hkv > 0, pos, slot);
-    const bool used = live && pos != AASD_NONE;
+    // (the rows do not wait for their token's position)
     Raw8<DT, VEC> rx[HP], ry[HP];   // channels 8l .. and D/2 + 8l ..
 #pragma unroll
     for (int i = 0; i < HP; ++i) {
         const int h = h0 + i;
         rx[i].clear();
         ry[i].clear();
-        if (used && h < heads) {
+        if (live && h < heads) {
             const void* src = h < hq ? a.q : a.k;
             const int64_t at = h < hq ? t * a.p.q_stride + (int64_t)h * D + 8 * l : t * a.p.k_stride + (int64_t)(h - hq) * D + 8 * l;
             rx[i].load(src, at);
             ry[i].load(src, at + H);
         }
     }
+    int pos = AASD_NONE, slot = AASD_NONE;
+    if (live) bits |= kv_write_token(a, t, hkv > 0, pos, slot);
+    const bool used = live && pos != AASD_NONE;
+    if (!used) {
+#pragma unroll
+        for (int i = 0; i < HP; ++i) {
+            rx[i].clear();
+            ry[i].clear();
+        }
+    }
     // cosines and sines of the lane's pairs (the branches on the form of the rotation are the same for every lane)
-    const int rot = a.p.rotary_dim, half = rot / 2;
-    const bool neighbours = (a.p.flags & AASD_KV_ROPE_INTERLEAVED) != 0;
+    const int rot = FULL ? D : a.p.rotary_dim, half = rot / 2;
+    const bool neighbours = !FULL && (a.p.flags & AASD_KV_ROPE_INTERLEAVED) != 0;
     const float* cs = a.cos_sin + (int64_t)(used ? pos : 0) * rot;
     float co[8], si[8];   // neighbours: pairs of the low half, then of the high half; else of channels 8l + e
 #pragma unroll
@@ -599,6 +609,28 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteAr
             load8<AASD_F32, VEC>(cs, half + 8 * l, si);
         }
     }
+    // 1 / sqrt(mean square + eps): the sums of all HP rows, then lane i of a row's lanes has row i's factor
+    float factor = 0.f;
+    if (a.q_weight != nullptr || a.k_weight != nullptr) {
+        float own = 0.f;
+#pragma unroll
+        for (int i = 0; i < HP; ++i) {
+            float2 u[4], v[4];
+            rx[i].unpack(u);
+            ry[i].unpack(v);
+            float s[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float2 q = __fadd2_rn(__fmul2_rn(u[e], u[e]), __fmul2_rn(v[e], v[e]));
+                s[e] = __fadd_rn(q.x, q.y);
+            }
+            float sum = __fadd_rn(__fadd_rn(s[0], s[1]), __fadd_rn(s[2], s[3]));
+#pragma unroll
+            for (int o = 1; o < L; o <<= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xFFFFFFFFu, sum, o));
+            if (l % HP == i) own = sum;
+        }
+        factor = __frcp_rn(__fsqrt_rn(__fadd_rn(__fmul_rn(own, 1.0f / D), a.p.eps)));
+    }
     float2 wx[4], wy[4];
     const void* held = nullptr;    // the weight that wx, wy hold
 #pragma unroll
@@ -610,15 +642,7 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteAr
         rx[i].unpack(u);
         ry[i].unpack(v);
         // (the lanes of a row take the same way; shuffles stay among all lanes of the warp)
-        float s[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float2 q = __fadd2_rn(__fmul2_rn(u[e], u[e]), __fmul2_rn(v[e], v[e]));
-            s[e] = __fadd_rn(q.x, q.y);
-        }
-        float sum = __fadd_rn(__fadd_rn(s[0], s[1]), __fadd_rn(s[2], s[3]));
-#pragma unroll
-        for (int o = 1; o < L; o <<= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xFFFFFFFFu, sum, o));
+        const float r = __shfl_sync(0xFFFFFFFFu, factor, i, HP < L ? HP : L);
         if (row && w != nullptr) {
             if (w != held) {
                 held = w;
@@ -628,7 +652,6 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteAr
                 g.load(w, H + 8 * l);
                 g.unpack(wy);
             }
-            const float r = __frcp_rn(__fsqrt_rn(__fadd_rn(__fmul_rn(sum, 1.0f / D), a.p.eps)));
             const float2 rr = make_float2(r, r);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -637,7 +660,7 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteAr
             }
         }
         // (a - b is written a + (-b): the same rounding)
-        if (rot > 0 && neighbours) {
+        if (!FULL && rot > 0 && neighbours) {
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
                 float2(&z)[4] = part ? v : u;
@@ -649,7 +672,7 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteAr
                     }
                 }
             }
-        } else if (rot == D) {
+        } else if (FULL || rot == D) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float2 c = make_float2(co[2 * e], co[2 * e + 1]), n = make_float2(si[2 * e], si[2 * e + 1]);
@@ -657,7 +680,7 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteAr
                 u[e] = __fadd2_rn(__fmul2_rn(p, c), __fmul2_rn(q, make_float2(-n.x, -n.y)));
                 v[e] = __fadd2_rn(__fmul2_rn(q, c), __fmul2_rn(p, n));
             }
-        } else if (rot > 0) {
+        } else if (!FULL && rot > 0) {
             // a pair (c, c + half) inside the first rot channels: its members may be different lanes',
             // so the warp's rows pass through shared memory (partial rotation is the rare case)
             float* mine = s_rows + group * D;
