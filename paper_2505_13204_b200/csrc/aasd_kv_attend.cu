@@ -37,6 +37,8 @@ int launch_tile(const LaunchEnv& env, int sm_count, const KvAttendArgs& a) {
     }();
     if (!enough) return AASD_ERR_UNSUPPORTED;
     launch(kernel, (unsigned int)(sm_count < kKvMaxCtas ? sm_count : kKvMaxCtas), (unsigned int)kTileThreads, smem, env.stream, a);
+    launch_grid2(kv_tile_join_kernel<D, PAIR>, (unsigned int)(sm_count < kKvMaxCtas ? sm_count : kKvMaxCtas), (PAIR ? 2u : 1u) * kTileRows / 8, 256u,
+                 env.stream, a);
     return AASD_OK;
 }
 #endif
@@ -54,6 +56,7 @@ int launch_kv_attend_bf16(const LaunchEnv& env, int sm_count, const KvAttendArgs
     char* ws = static_cast<char*>(scratch);
     a.tickets = reinterpret_cast<unsigned int*>(ws);
     a.cta_parts = reinterpret_cast<float*>(ws + L.off_cta);
+    a.tile_open = reinterpret_cast<KvTileOpen*>(ws + L.off_open);
     a.warp_parts = reinterpret_cast<float*>(ws + L.off_warp);
     // rows per key/value head that a sequence brings (packed rows: on average)
     const int64_t per_seq = a.p.rows_per_seq > 0 ? a.p.rows_per_seq : (a.p.n_tokens + a.p.n_seqs - 1) / (a.p.n_seqs > 0 ? a.p.n_seqs : 1);
@@ -61,6 +64,7 @@ int launch_kv_attend_bf16(const LaunchEnv& env, int sm_count, const KvAttendArgs
     *launches = 1;
 #if AASD_DT == 1
     if (rows > kSplitRows && a.p.head_dim <= 128) {
+        *launches = 2;
         if (a.p.head_dim == 64) return rows > kTileRows ? launch_tile<64, true>(env, sm_count, a) : launch_tile<64, false>(env, sm_count, a);
         return rows > kTileRows ? launch_tile<128, true>(env, sm_count, a) : launch_tile<128, false>(env, sm_count, a);
     }

@@ -19,6 +19,22 @@
 
 namespace aasd {
 
+// A partial result: the part of a segment (one row tile of one head of one sequence) whose pages
+// one warp, or one CTA, has been through.
+struct KvPiece {
+    int seg;            // unit of the segment's first page, -1: no piece
+    int pages;          // of the segment
+    int h, row0, n;     // head, first row of the tile, rows in use
+    int first;          // token row of the sequence's first new token
+};
+
+// What the tile kernel leaves per CTA: the segment that it began and others go on with, and how many
+// CTAs hold parts of it (0: there is none).
+struct KvTileOpen {
+    KvPiece piece;
+    int parts;
+};
+
 struct KvAttendArgs {
     const void* q;
     const uint8_t* pages;
@@ -34,6 +50,7 @@ struct KvAttendArgs {
     DeviceState* state;
     unsigned int* tickets;        // scratch, zero between calls
     float* cta_parts;             // scratch: partial results of segments that several CTAs share
+    KvTileOpen* tile_open;        // scratch, one per CTA of the tile kernel
     float* warp_parts;            // scratch: a warp's first piece, when it goes on to another segment
 };
 
@@ -85,19 +102,19 @@ __device__ __forceinline__ long long kv_units(const KvAttendArgs& a, const KvSeq
 // A place in the list of all units: sequence by sequence, head by head, tile by tile, page by page.
 struct KvCursor {
     int b, h, tile, pg;
-    long long unit;           // of page pg
+    int unit;                 // of page pg
     KvSeq s;
     const int32_t* table;     // the sequence's row of the block table
     // To the first page at or behind unit u, which is unit rem of sequence b_.
-    __device__ __forceinline__ void seek(const KvAttendArgs& a, int b_, const KvSeq& s_, long long rem, long long u) {
+    __device__ __forceinline__ void seek(const KvAttendArgs& a, int b_, const KvSeq& s_, int rem, int u) {
         b = b_;
         s = s_;
         unit = u;
-        const int seg = (int)(rem / (s.pages + kSegCost));
+        const int seg = rem / (s.pages + kSegCost);
         unit -= rem;                                           // (of the sequence's first unit)
-        rem -= (long long)seg * (s.pages + kSegCost);
-        pg = rem < kSegCost ? 0 : (int)rem - kSegCost;
-        unit += (long long)seg * (s.pages + kSegCost) + kSegCost + pg;
+        rem -= seg * (s.pages + kSegCost);
+        pg = rem < kSegCost ? 0 : rem - kSegCost;
+        unit += seg * (s.pages + kSegCost) + kSegCost + pg;
         h = seg / s.tiles;
         tile = seg - h * s.tiles;
         table = a.block_table + (long long)b * a.p.max_pages;
@@ -109,6 +126,7 @@ struct KvCursor {
         tile = 0;
         if (++h < a.p.n_kv_heads) return;
         h = 0;
+#pragma unroll 1
         do {
             if (++b >= a.p.n_seqs) return;   // (past the last unit: never looked at)
             s = kv_load_seq(a, b, tile_rows);
@@ -119,19 +137,25 @@ struct KvCursor {
 
 // `total` units in `n` shares that differ by one unit at most, the larger ones first.
 struct KvShares {
-    long long each, more;     // units of a small share; shares with one more
+    int each, more;           // units of a small share; shares with one more
     KvShares() = default;
-    __device__ __forceinline__ KvShares(long long total, long long n) {
-        if (total < 0x7FFFFFFFLL) each = (long long)((unsigned int)total / (unsigned int)n);
-        else each = total / n;
+    __device__ __forceinline__ KvShares(int total, int n) {
+        each = (int)((unsigned int)total / (unsigned int)n);
         more = total - each * n;
     }
-    __device__ __forceinline__ long long first(long long share) const { return each * share + (share < more ? share : more); }
-    __device__ __forceinline__ long long owner(long long unit) const {
-        const long long big = (each + 1) * more;
-        return unit < big ? unit / (each + 1) : more + (unit - big) / each;
+    __device__ __forceinline__ int first(int share) const { return each * share + min(share, more); }
+    __device__ __forceinline__ int owner(int unit) const {
+        const int big = (each + 1) * more;
+        return unit < big ? (int)((unsigned int)unit / (unsigned int)(each + 1)) : more + (int)((unsigned int)(unit - big) / (unsigned int)each);
     }
 };
+
+// All units of a call: what the threads of a CTA have added up.  Units are counted in 31 bits (137 G keys).
+__device__ __forceinline__ int kv_total(const KvAttendArgs& a, long long total) {
+    if (total <= 0x7FFFFFFFLL) return (int)total;
+    raise(a.state, AASD_STATUS_BAD_OFFSETS);
+    return 0;
+}
 
 // One row tile of one head of one sequence, as a warp works on it.
 struct KvSegment {
@@ -139,7 +163,7 @@ struct KvSegment {
     int pages;
     int h, row0;              // head, first row of the tile
     int pg;                   // the warp's first page of it
-    long long unit;           // of page 0
+    int unit;                 // of page 0
 };
 
 // Bit j of the result: place 64 pg + j of a sequence (a cached token or a new one) is seen by its new
@@ -153,6 +177,7 @@ __device__ __forceinline__ u64 kv_seen(const KvAttendArgs& a, int cached, int fr
         return upto >= kPage ? ~0ull : upto <= 0 ? 0ull : (1ull << upto) - 1ull;
     }
     int x = i;
+#pragma unroll 1
     while (x >= 0) {
         const int j = before + x;
         if (j < 0) break;                                         // ancestors only get smaller
@@ -234,6 +259,7 @@ template <int DT>
 __device__ __forceinline__ void kv_clear_rows(const KvAttendArgs& a, int D, int warp, int warps) {
     const int lane = threadIdx.x & 31;
     const int Hq = a.p.n_q_heads;
+#pragma unroll 1
     for (int b = warp; b <= a.p.n_seqs; b += warps) {
         long long lo, hi;
         if (b < a.p.n_seqs) {
@@ -246,9 +272,65 @@ __device__ __forceinline__ void kv_clear_rows(const KvAttendArgs& a, int D, int 
             hi = a.p.n_tokens;
         }
         const long long e0 = lo * Hq * D, e1 = hi * Hq * D;
+#pragma unroll 1
         for (long long e = e0 + lane * 4; e < e1; e += 128) store4<DT>(a.o.out, e, make_float4(0.f, 0.f, 0.f, 0.f), a.out_vec);
         if (a.o.lse)
+#pragma unroll 1
             for (long long e = lo * Hq + lane; e < hi * Hq; e += 32) a.o.lse[e] = -CUDART_INF_F;
+    }
+}
+
+// ---- joining ---------------------------------------------------------------------------------------------
+
+// Row r of a segment from its parts, one warp.  Part k lies at base + 2 k stride, the first one stride further;
+// a part is rows of D sums, then the rows' maxima, then their denominators.  The weights are found lane
+// by lane, the channels summed as independent loads.
+template <int DT, int D>
+__device__ __forceinline__ void kv_join_row(const KvAttendArgs& a, const KvPiece& pc, int r, const float* base, int stride, int rows, int parts, int G,
+                                            int lane) {
+    float M = kKvNothing;
+#pragma unroll 1
+    for (int k = lane; k < parts; k += 32) M = fmaxf(M, __ldcg(base + (long long)(2 * k + (k == 0)) * stride + rows * D + r));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
+#pragma unroll 1
+    for (int cb = 0; cb < D; cb += 128) {
+        const int ch = cb + lane * 4;
+        const bool on = ch < D;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        float L = 0.f, f = 0.f;
+#pragma unroll 1
+        for (int k0 = 0; k0 < parts; k0 += 8) {
+            if ((k0 & 31) == 0) {
+                const int k = k0 + lane;
+                const float* from = base + (long long)(2 * k + (k == 0)) * stride + rows * D + r;
+                f = k < parts ? ex2_approx(__ldcg(from) - M) : 0.f;
+                if (k < parts) L = fmaf(__ldcg(from + rows), f, L);
+            }
+            float4 x[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const int k = k0 + q;
+                x[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (on && k < parts) x[q] = __ldcg(reinterpret_cast<const float4*>(base + (long long)(2 * k + (k == 0)) * stride + r * D + ch));
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const float fk = __shfl_sync(0xFFFFFFFFu, f, (k0 + q) & 31);
+                o.x = fmaf(x[q].x, fk, o.x);
+                o.y = fmaf(x[q].y, fk, o.y);
+                o.z = fmaf(x[q].z, fk, o.z);
+                o.w = fmaf(x[q].w, fk, o.w);
+            }
+        }
+#pragma unroll
+        for (int q = 16; q > 0; q >>= 1) L += __shfl_xor_sync(0xFFFFFFFFu, L, q);
+        if (!on) continue;
+        const float inv = L > 0.f ? 1.f / L : 0.f;
+        const int row = pc.row0 + r;
+        const long long head = ((long long)pc.first + row / G) * a.p.n_q_heads + pc.h * G + row % G;
+        store4<DT>(a.o.out, head * D + ch, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), a.out_vec);
+        if (a.o.lse != nullptr && ch == 0) a.o.lse[head] = L > 0.f ? (M + log2f(L)) * (float)kLn2 : -CUDART_INF_F;
     }
 }
 
@@ -266,22 +348,12 @@ struct KvSplitShape {
     static constexpr int kThreads = W * 32;
 };
 
-// A partial result: the part of a segment (one row tile of one head of one sequence) whose pages
-// one warp, or one CTA, has been through.  Rows are padded by four floats in shared memory so that
-// a warp's stores meet every bank once.
-struct KvPiece {
-    long long seg;      // unit of the segment's first page, -1: no piece
-    int pages;          // of the segment
-    int h, row0, n;     // head, first row of the tile, rows in use
-    int first;          // token row of the sequence's first new token
-};
-
 template <int DT, int D, int NT>
 struct KvSplitShared {
     using Sh = KvSplitShape<DT, D, NT>;
     static constexpr int R = 8 * NT;
     alignas(128) unsigned char ring[Sh::W][Sh::S][Sh::kBlock];
-    long long base[Sh::kThreads + 1];
+    int base[Sh::kThreads];
     long long scan[Sh::W];
     KvSegment seg[Sh::W][Sh::S + 1];   // of the blocks on their way, and the one being worked on
     KvPiece piece[2 * Sh::W];
@@ -297,7 +369,8 @@ template <int DT, int D, int NT>
 __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_attend_split_kernel(const KvAttendArgs a) {
     using Sh = KvSplitShape<DT, D, NT>;
     using Shared = KvSplitShared<DT, D, NT>;
-    constexpr int W = Sh::W, S = Sh::S, R = 8 * NT, H = D / 2, TS = D + 4;
+    constexpr int W = Sh::W, S = Sh::S, R = 8 * NT, H = D / 2;
+    constexpr int TS = D + 4;                       // floats between the rows of a warp's piece: its stores meet every bank once
     constexpr int NP = DT == AASD_F32 ? 2 : 1;      // fp16 numbers per query element and probability
     constexpr bool CEN = NP == 2;                   // codes are centred (see codes())
     constexpr int kC = CEN ? 0 : 24;                // the operands hold the codes times 2^-kC
@@ -315,6 +388,7 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, j = lane & 3;
     if (tid == 0) {
+#pragma unroll 1
         for (int i = 0; i < W * S; ++i) mbar_init(&sh.full[0][0] + i, 1);
         sh.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -325,22 +399,22 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
     // every thread adds up the units of its strip of sequences
     const int strip = (B + Sh::kThreads - 1) / Sh::kThreads;
     long long mine = 0;
+#pragma unroll 1
     for (int b = tid * strip; b < min(B, (tid + 1) * strip); ++b) {
         const KvSeq s = kv_load_seq(a, b, R);
         mine += kv_units(a, s);
         if (s.fresh > 0 && (long long)s.cached + s.fresh > (long long)a.p.max_pages * kPage) raise(a.state, AASD_STATUS_BAD_OFFSETS);
     }
-    long long total;
-    const long long before = block_scan<Sh::kThreads>(mine, sh.scan, total);
-    sh.base[tid] = before;
+    long long sum;
+    const long long before = block_scan<Sh::kThreads>(mine, sh.scan, sum);
+    sh.base[tid] = (int)before;
     __syncthreads();
+    const int total = kv_total(a, sum);
     // CTAs at work: as many as leave every warp a page
-    long long active = (total + W - 1) / W;
-    active = active > gridDim.x ? gridDim.x : active;
-    const long long c = blockIdx.x;
+    const int c = blockIdx.x, active = min((total + W - 1) / W, (int)gridDim.x);
     const bool works = c < active;
     const KvShares shares(total, works ? active * W : 1);
-    const long long u0 = works ? shares.first(c * W + warp) : 0, u1 = works ? shares.first(c * W + warp + 1) : 0;
+    const int u0 = works ? shares.first(c * W + warp) : 0, u1 = works ? shares.first(c * W + warp + 1) : 0;
     volatile int* abort_flag = &sh.abort_flag;
     u64* full = sh.full[warp];
 
@@ -348,18 +422,16 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
         KvCursor ahead;
         {
             int lo = 0, hi = (B + strip - 1) / strip;
+#pragma unroll 1
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
                 if (sh.base[mid] <= u0) lo = mid;
                 else hi = mid;
             }
-            long long rem = u0 - sh.base[lo];
-            int b = lo * strip;
+            int rem = u0 - sh.base[lo], b = lo * strip;
             KvSeq s = kv_load_seq(a, b, R);
-            while (rem >= kv_units(a, s)) {
-                rem -= kv_units(a, s);
-                s = kv_load_seq(a, ++b, R);
-            }
+#pragma unroll 1
+            for (int n; rem >= (n = (int)kv_units(a, s)); s = kv_load_seq(a, ++b, R)) rem -= n;
             ahead.seek(a, b, s, rem, u0);
         }
         const unsigned int page_stride = (unsigned int)a.p.n_kv_heads * Sh::kBlock;
@@ -414,6 +486,7 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
             }
         };
         if (ahead.unit < u1) prefetch_queries();   // (in front of the copies, which would hold them up)
+#pragma unroll 1
         for (int s = 0; s < S && ahead.unit < u1; ++s, ++issued) issue(s);
         __syncwarp();
 
@@ -423,9 +496,10 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
         float oacc[NT][2][MQ][4];             // [tile][half][channel tile][fragment]
         int ev = 0;                           // exponent field that the probabilities are scaled by
         bool fresh_segment = true;
-        int stage = 0, seg_out = -1, pg = 0, last_pg = 0, cached = 0, end = 0;
+        int stage = 0, seg_out = -1, pg = 0, last_pg = 0, open_to = 0, end = 0;
         unsigned int phase = 0;
 
+#pragma unroll 1
         for (int u = 0; u < issued; ++u) {
             if (fresh_segment) {
                 fresh_segment = false;
@@ -433,7 +507,8 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
                 const KvSegment at = sh.seg[warp][seg_out];
                 pg = at.pg;
                 last_pg = at.pages - 1;
-                cached = at.cached;
+                // places up to which every row of the tile sees everything
+                open_to = a.node_parent != nullptr ? at.cached : at.cached + at.row0 / G + 1;
                 end = at.cached + at.fresh;
                 ev = 64;
 #pragma unroll
@@ -550,7 +625,7 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
                 }
                 // scales, masks, running maximum
                 uint2 vm[4];
-                const bool masked = (pg + 1) * kPage > cached;
+                const bool masked = (pg + 1) * kPage > open_to;
                 const int live = end - pg * kPage;
                 float mx[NT][2];
 #pragma unroll
@@ -576,12 +651,14 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
                         }
                 }
                 if (masked) {
+                    // (lane r finds out what row r sees)
                     const KvSegment at = sh.seg[warp][seg_out];
+                    const u64 mine = kv_seen(a, at.cached, at.fresh, at.first, pg, (at.row0 + (lane & (R - 1))) / G);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int col = 0; col < 2; ++col) {
-                            const u64 seen = kv_seen(a, at.cached, at.fresh, at.first, pg, (at.row0 + 8 * nt + 2 * j + col) / G);
+                            const u64 seen = __shfl_sync(0xFFFFFFFFu, mine, 8 * nt + 2 * j + col);
 #pragma unroll
                             for (int mt = 0; mt < 4; ++mt)
 #pragma unroll
@@ -721,7 +798,7 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
                 const float unscale = pow2f((ev - 127) - kP), back = pow2f(kC);
                 const int n = min(R, at.fresh * G - at.row0);
                 const int slot = 2 * warp + (tail ? 1 : 0);
-                float* to = tail ? reinterpret_cast<float*>(sh.ring[warp][0]) : a.warp_parts + (c * W + warp) * (R * TS);
+                float* to = tail ? reinterpret_cast<float*>(sh.ring[warp][0]) : a.warp_parts + (long long)(c * W + warp) * (R * TS);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -774,11 +851,11 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
         // channels summed as independent loads.
         static_assert(2 * W <= 32, "a lane per piece");
         constexpr int kPart = R * D + 2 * R;
-        const long long U0 = shares.first(c * W), U1 = shares.first(c * W + W);
-        const long long seg = lane < 2 * W ? sh.piece[lane].seg : -1;
+        const int U0 = shares.first(c * W), U1 = shares.first(c * W + W);
+        const int seg = lane < 2 * W ? sh.piece[lane].seg : -1;
         const unsigned int valid = __ballot_sync(0xFFFFFFFFu, seg >= 0);
         const unsigned int below = valid & ((1u << lane) - 1u);
-        const long long previous = __shfl_sync(0xFFFFFFFFu, seg, below ? 31 - __clz(below) : 0);
+        const int previous = __shfl_sync(0xFFFFFFFFu, seg, below ? 31 - __clz(below) : 0);
         unsigned int starts = __ballot_sync(0xFFFFFFFFu, seg >= 0 && (below == 0 || previous != seg));
         auto finish_row = [&](const KvPiece& pc, int r, float M, float L, float4 o, int ch) {
             const float inv = L > 0.f ? 1.f / L : 0.f;
@@ -817,7 +894,7 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
                     const int k = __ffs(left) - 1;
                     left &= left - 1;
                     const float* from = (k & 1) ? reinterpret_cast<const float*>(sh.ring[k >> 1][0])
-                                                : a.warp_parts + (c * W + (k >> 1)) * (R * TS);
+                                                : a.warp_parts + (long long)(c * W + (k >> 1)) * (R * TS);
                     float4 x[RB];
 #pragma unroll
                     for (int i = 0; i < RB; ++i) {
@@ -859,7 +936,7 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
             const bool complete = pc.seg >= U0 && pc.seg + pc.pages <= U1;
             const int which = pc.seg < U0 ? 0 : 1;   // scratch slot of this CTA
             if (!complete) open[which] = p;
-            float* part = a.cta_parts + (c * 2 + which) * kPart;
+            float* part = a.cta_parts + (long long)(c * 2 + which) * kPart;
             const int batches = few ? pc.n : (pc.n + 3) / 4;
             int k = warp - done;
             k += k < 0 ? W : 0;
@@ -876,7 +953,7 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
                 int last = 0;
                 if (open[tid] >= 0) {
                     const KvPiece pc = sh.piece[open[tid]];
-                    const long long c0 = shares.owner(pc.seg) / W, c1 = shares.owner(pc.seg + pc.pages - 1) / W;
+                    const int c0 = shares.owner(pc.seg) / W, c1 = shares.owner(pc.seg + pc.pages - 1) / W;
                     last = take_ticket(a.tickets + c0) == (unsigned int)(c1 - c0);
                     if (last) a.tickets[c0] = 0;
                 }
@@ -887,61 +964,10 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
             for (int which = 0; which < 2; ++which) {
                 if (!sh.last[which]) continue;
                 const KvPiece pc = sh.piece[open[which]];
-                const long long c0 = shares.owner(pc.seg) / W;
-                const int parts = (int)(shares.owner(pc.seg + pc.pages - 1) / W - c0) + 1;
-                const float* base = a.cta_parts + c0 * 2 * kPart;   // part k: 2 k, the first one's 1
-                for (int r = warp; r < pc.n; r += W) {
-                    constexpr int NK = (kKvMaxCtas + 31) / 32;
-                    float M = kKvNothing, L = 0.f;
-                    float m[NK], l[NK];
-#pragma unroll
-                    for (int i = 0; i < NK; ++i) {
-                        const int k = 32 * i + lane;
-                        const float* from = base + (2 * k + (k == 0)) * kPart + R * D + r;
-                        m[i] = kKvNothing;
-                        l[i] = 0.f;
-                        if (k < parts) {
-                            m[i] = __ldcg(from);
-                            l[i] = __ldcg(from + R);
-                        }
-                        M = fmaxf(M, m[i]);
-                    }
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
-#pragma unroll
-                    for (int i = 0; i < NK; ++i) {
-                        m[i] = ex2_approx(m[i] - M);
-                        L = fmaf(l[i], m[i], L);
-                    }
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xFFFFFFFFu, L, o);
-                    for (int cb = 0; cb < D; cb += 128) {
-                        const int ch = cb + lane * 4;
-                        const bool on = ch < D;
-                        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                        for (int i = 0; i < NK; ++i) {
-                            for (int q0 = 0; q0 < min(32, parts - 32 * i); q0 += 8) {
-                                float4 x[8];
-#pragma unroll
-                                for (int q = 0; q < 8; ++q) {
-                                    const int k = 32 * i + q0 + q;
-                                    x[q] = make_float4(0.f, 0.f, 0.f, 0.f);
-                                    if (on && k < parts) x[q] = __ldcg(reinterpret_cast<const float4*>(base + (2 * k + (k == 0)) * kPart + r * D + ch));
-                                }
-#pragma unroll
-                                for (int q = 0; q < 8; ++q) {
-                                    const float fk = __shfl_sync(0xFFFFFFFFu, m[i], q0 + q);
-                                    o.x = fmaf(x[q].x, fk, o.x);
-                                    o.y = fmaf(x[q].y, fk, o.y);
-                                    o.z = fmaf(x[q].z, fk, o.z);
-                                    o.w = fmaf(x[q].w, fk, o.w);
-                                }
-                            }
-                        }
-                        if (on) finish_row(pc, r, M, L, o, ch);
-                    }
-                }
+                const int c0 = shares.owner(pc.seg) / W;
+                const int parts = (shares.owner(pc.seg + pc.pages - 1) / W - c0) + 1;
+                const float* base = a.cta_parts + (long long)c0 * 2 * kPart;   // part k: 2 k, the first one's 1
+                for (int r = warp; r < pc.n; r += W) kv_join_row<DT, D>(a, pc, r, base, kPart, R, parts, G, lane);
             }
         }
     }

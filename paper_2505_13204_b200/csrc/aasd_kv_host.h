@@ -14,7 +14,7 @@ namespace aasd {
 // Scratch of the attention kernels: tickets (zero between calls), then per CTA two partial
 // results, then per warp one.
 struct KvScratch {
-    size_t zero_bytes, off_cta, off_warp, bytes;
+    size_t zero_bytes, off_open, off_cta, off_warp, bytes;
 };
 constexpr KvScratch kv_attend_scratch(int head_dim) {
     KvScratch L{};
@@ -22,7 +22,8 @@ constexpr KvScratch kv_attend_scratch(int head_dim) {
     const size_t D = (size_t)head_dim, W = 12;
     const size_t part = 2 * kTileRows * ((D < 128 ? D : 128) + 2);   // the largest: two tiles of 128 rows (head_dim 256 has parts of 8 rows)
     L.zero_bytes = align_up(4 * kKvMaxCtas, 256);
-    L.off_cta = L.zero_bytes;
+    L.off_open = L.zero_bytes;
+    L.off_cta = align_up(L.off_open + kKvMaxCtas * sizeof(KvTileOpen), 256);
     L.off_warp = align_up(L.off_cta + kKvMaxCtas * 2 * part * 4, 256);
     L.bytes = align_up(L.off_warp + kKvMaxCtas * W * 16 * (D + 4) * 4, 256);
     return L;

@@ -2,12 +2,13 @@
 // prompt): tiles of 128 rows on the fifth-generation tensor cores.
 //
 // One persistent CTA per SM; its warps have roles:
+//   walker      goes through the CTA's share of the work and hands it out piece by piece;
 //   loader      brings pages (packed blocks) in by bulk copies;
 //   unpackers   (4 warps) turn a page's codes into fp16 operands in shared memory, K-major rows of 128
 //               bytes in the 128-byte swizzle;
 //   two issuers, one thread each: tcgen05.mma of S = Q K^T (both operands in shared memory) and
 //               O += P V (P in tensor memory) for one softmax group, a page (64 tokens) at a time;
-//   two softmax groups of 4 warps, a thread per row: S to registers, probabilities back as P.
+//   two softmax groups of 4 warps, 32 rows each: S to registers, probabilities back as P.
 // The two groups work on two row tiles of the same pages (PAIR), or, where a segment has no more
 // than 128 rows, on alternate pages of one tile, joined at the end.  A group has two S buffers, so
 // that the next page's products are there when it is done with one.
@@ -25,15 +26,16 @@
 
 namespace aasd {
 
-constexpr int kTileThreads = 512;      // 8 softmax warps, 4 unpackers; issuer, loader and two that fill their group of four
+constexpr int kTileThreads = 512;      // 8 softmax warps, 4 unpackers, two issuers, loader, walker
 // Registers per thread: a launch of 512 threads has 128 for each; the softmax groups, which hold a
 // row of S, take what the others give up (2 x 184 + 2 x 72 = 4 x 128).
 constexpr int kTileLaunchRegs = 128, kTileSoftmaxRegs = 184, kTileOtherRegs = 72;
 static_assert(2 * kTileSoftmaxRegs + 2 * kTileOtherRegs <= 4 * kTileLaunchRegs, "the shares add up to the launch's registers");
 constexpr int kTileRows = 128;
 constexpr int kTileRaw = 4, kTileKeys = 3, kTileValues = 4, kTileMeta = 6;   // ring depths, in pages
-// the probabilities' power of two and the running maximum's lag (see the split kernel)
-constexpr float kTileP = 7.f, kTileLazy = 8.f;
+constexpr int kTilePieces = 8;
+// the probabilities' power of two (see the split kernel): the maximum may lag by what is left of fp16's range
+constexpr float kTileP = 7.f;
 
 // ---- the list of work ---------------------------------------------------------------------------------
 
@@ -50,48 +52,18 @@ __device__ __forceinline__ long long kv_tile_head_units(const KvAttendArgs& a, c
     if (s.pages == 0) return 0;
     if (a.node_parent != nullptr) return (long long)s.tiles * (s.pages + kTileSegCost);
     long long n = 0;
+#pragma unroll 1
     for (int t = 0; t < s.tiles; ++t) n += kv_tile_pages(a, s.cached, s.fresh, s.pages, t, R, G) + kTileSegCost;
     return n;
 }
 
-// One CTA's way through its share; every role walks it for itself.  A piece is the run of pages of
-// one segment that falls into the share.
-struct KvTileWalk {
+// A piece: the run of pages of one segment that falls into a CTA's share.  One lane walks the share and
+// hands the pieces to the other roles through a ring.
+struct KvTilePiece {
     int b, h, tile;
-    int pg, pages;            // next page, and how many the segment has
-    int left;                 // units of the share from page pg on
-    int cached, fresh, first, seq_pages, tiles;   // see KvSeq
-    __device__ __forceinline__ bool live() const { return left > 0; }
-    __device__ __forceinline__ int piece_pages() const { return min(pages - pg, left); }
-    __device__ __forceinline__ int tile_pages(const KvAttendArgs& a, int R, int G) const {
-        return kv_tile_pages(a, cached, fresh, seq_pages, tile, R, G);
-    }
-    __device__ __forceinline__ void take(const KvSeq& s) {
-        cached = s.cached;
-        fresh = s.fresh;
-        first = s.first;
-        seq_pages = s.pages;
-        tiles = s.tiles;
-    }
-    __device__ __forceinline__ void next(const KvAttendArgs& a, int R, int G) {
-        left -= pages - pg + kTileSegCost;
-        if (left <= 0) return;
-        pg = 0;
-        if (++tile == tiles) {
-            tile = 0;
-            if (++h == a.p.n_kv_heads) {
-                h = 0;
-                do {
-                    if (++b >= a.p.n_seqs) {
-                        left = 0;
-                        return;
-                    }
-                    take(kv_load_seq(a, b, R));
-                } while (seq_pages == 0 || tiles == 0);
-            }
-        }
-        pages = tile_pages(a, R, G);
-    }
+    int pg, np, pages;        // first page, pages of the piece (0: the share is done), pages of the segment
+    int cached, fresh, first; // see KvSeq
+    int seg;                  // unit of the segment's first page
 };
 
 template <int D, bool PAIR>
@@ -105,19 +77,20 @@ struct KvTileShared {
     uint4 vmeta[4][kPage / 4];         // per unpacking warp, four tokens each: scales of 0 and 2, 1 and 3, minima likewise
     int ev[kTileMeta];                 // exponent field that a page's values are relative to; -1: page hidden
     int raw_missing[kTileRaw];
+    float row_r[PAIR ? 2 : 1][kTileRows], row_q[PAIR ? 2 : 1][kTileRows];         // factors of the rows' queries
     float exchange_m[kTileRows], exchange_l[kTileRows], exchange_up[kTileRows];   // between the groups, where they share a tile
-    long long base[kTileThreads];
+    int base[kTileThreads];
     long long scan[kTileThreads / 32];
-    KvTileWalk start;                  // the CTA's share of the work: where it begins, and the unit behind its last one
-    long long end;
+    KvTilePiece piece[kTilePieces];
     KvShares shares;
-    KvPiece open[2];                   // segments that other CTAs hold parts of: begun before this CTA, in it
+    KvPiece open;                      // the segment that begins in this CTA and ends in another
+    u64 piece_full[kTilePieces], piece_empty[kTilePieces];
     u64 raw_full[kTileRaw], raw_empty[kTileRaw];
     u64 k_full[kTileKeys], k_empty[kTileKeys], v_full[kTileValues], v_empty[kTileValues];
     u64 m_full[kTileMeta], m_empty[kTileMeta];
-    u64 q_full[2], s_full[2][2], p_full[2][2], o_done[2], x_full, x_empty, r_full, drain[2];
+    u64 q_full[2], s_full[2][2], p_full[2][2], o_done[2][2], x_full, x_empty, r_full, drain[2];
     unsigned int tmem;
-    int abort_flag, last[2];
+    int abort_flag;
 };
 
 // ---- tcgen05 ----------------------------------------------------------------------------------------
@@ -156,26 +129,21 @@ __host__ __device__ constexpr unsigned int tc_idesc(int n) { return (1u << 4) | 
 __device__ __forceinline__ u64 tc_desc(unsigned int addr) {
     return (u64)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
-// Columns of a warp's 32 lanes; the values have arrived when the statement is done.
-__device__ __forceinline__ void tc_load32(unsigned int addr, float (&x)[32]) {
+// 64 columns of 16 lanes (rows): thread (g = lane / 4, j = lane % 4) has columns 8 k + 2 j and the next of rows
+// g (x[4 k], x[4 k + 1]) and g + 8 (x[4 k + 2], x[4 k + 3]).  Loads have arrived when the statement is done.
+__device__ __forceinline__ void tc_load(unsigned int addr, float (&x)[32]) {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\t"
+        "tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\t"
         "tcgen05.wait::ld.sync.aligned;"
         : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]), "=f"(x[8]), "=f"(x[9]), "=f"(x[10]), "=f"(x[11]), "=f"(x[12]), "=f"(x[13]), "=f"(x[14]), "=f"(x[15]), "=f"(x[16]), "=f"(x[17]), "=f"(x[18]), "=f"(x[19]), "=f"(x[20]), "=f"(x[21]), "=f"(x[22]), "=f"(x[23]), "=f"(x[24]), "=f"(x[25]), "=f"(x[26]), "=f"(x[27]), "=f"(x[28]), "=f"(x[29]), "=f"(x[30]), "=f"(x[31])
         : "r"(addr) : "memory");
 }
-__device__ __forceinline__ void tc_load64(unsigned int addr, float (&x)[64]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]), "=f"(x[8]), "=f"(x[9]), "=f"(x[10]), "=f"(x[11]), "=f"(x[12]), "=f"(x[13]), "=f"(x[14]), "=f"(x[15]), "=f"(x[16]), "=f"(x[17]), "=f"(x[18]), "=f"(x[19]), "=f"(x[20]), "=f"(x[21]), "=f"(x[22]), "=f"(x[23]), "=f"(x[24]), "=f"(x[25]), "=f"(x[26]), "=f"(x[27]), "=f"(x[28]), "=f"(x[29]), "=f"(x[30]), "=f"(x[31]), "=f"(x[32]), "=f"(x[33]), "=f"(x[34]), "=f"(x[35]), "=f"(x[36]), "=f"(x[37]), "=f"(x[38]), "=f"(x[39]), "=f"(x[40]), "=f"(x[41]), "=f"(x[42]), "=f"(x[43]), "=f"(x[44]), "=f"(x[45]), "=f"(x[46]), "=f"(x[47]), "=f"(x[48]), "=f"(x[49]), "=f"(x[50]), "=f"(x[51]), "=f"(x[52]), "=f"(x[53]), "=f"(x[54]), "=f"(x[55]), "=f"(x[56]), "=f"(x[57]), "=f"(x[58]), "=f"(x[59]), "=f"(x[60]), "=f"(x[61]), "=f"(x[62]), "=f"(x[63])
-        : "r"(addr) : "memory");
+__device__ __forceinline__ void tc_store(unsigned int addr, const float (&x)[32]) {
+    asm volatile("tcgen05.st.sync.aligned.16x256b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(addr), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]), "f"(x[8]), "f"(x[9]), "f"(x[10]), "f"(x[11]), "f"(x[12]), "f"(x[13]), "f"(x[14]), "f"(x[15]), "f"(x[16]), "f"(x[17]), "f"(x[18]), "f"(x[19]), "f"(x[20]), "f"(x[21]), "f"(x[22]), "f"(x[23]), "f"(x[24]), "f"(x[25]), "f"(x[26]), "f"(x[27]), "f"(x[28]), "f"(x[29]), "f"(x[30]), "f"(x[31]) : "memory");
 }
-__device__ __forceinline__ void tc_store8(unsigned int addr, unsigned int x0, unsigned int x1, unsigned int x2, unsigned int x3, unsigned int x4,
-                                          unsigned int x5, unsigned int x6, unsigned int x7) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(addr), "r"(x0), "r"(x1), "r"(x2), "r"(x3), "r"(x4),
-                 "r"(x5), "r"(x6), "r"(x7)
-                 : "memory");
+// 32 columns of 16 lanes, a 32-bit cell each: column 4 k + j of rows g (x[2 k]) and g + 8 (x[2 k + 1]).
+__device__ __forceinline__ void tc_store_cells(unsigned int addr, const unsigned int (&x)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]), "r"(x[9]), "r"(x[10]), "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]) : "memory");
 }
 __device__ __forceinline__ void tc_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ __half2 as_half2(unsigned int x) { return *reinterpret_cast<const __half2*>(&x); }
@@ -187,12 +155,34 @@ __device__ __forceinline__ unsigned int expand(unsigned int w, __half2 scale, __
     const __half2 v = __hfma2(c, scale, minimum);
     return *reinterpret_cast<const unsigned int*>(&v);
 }
+// Column of S (row of the key operand) of a page's token: the two inner ones of every four change
+// places, so that neighbouring columns are the tokens whose codes leave a word of the values together.
+__device__ __forceinline__ int tile_place(int t) { return (t & ~3) | ((t & 1) << 1) | ((t >> 1) & 1); }
+__device__ __forceinline__ u64 tile_places(u64 tokens) {
+    return (tokens & 0x9999999999999999ull) | ((tokens & 0x2222222222222222ull) << 1) | ((tokens & 0x4444444444444444ull) >> 1);
+}
 template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }   // the eight softmax warps
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// O of a warp's 32 rows times a factor per row (fo[q]: row g + 8 q).
+template <int D>
+__device__ __forceinline__ void tile_scale_o(unsigned int col_o, const float (&fo)[4]) {
+#pragma unroll 1
+    for (int cb = 0; cb < D; cb += 64)
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+            const float f0 = half ? fo[2] : fo[0], f1 = half ? fo[3] : fo[1];
+            float o[32];
+            tc_load(col_o + cb + ((unsigned int)(16 * half) << 16), o);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] *= (k >> 1) & 1 ? f1 : f0;
+            tc_store(col_o + cb + ((unsigned int)(16 * half) << 16), o);
+        }
+    tc_wait_store();   // (a page may scale O twice)
+}
 
 // ---- the kernel ---------------------------------------------------------------------------------------
 
@@ -207,36 +197,46 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
     pdl_launch_dependents();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
+#pragma unroll 1
+        for (int i = 0; i < kTilePieces; ++i) {
+            mbar_init(&sh.piece_full[i], 1);
+            mbar_init(&sh.piece_empty[i], 8 + 4 + 2 + 1);
+        }
+#pragma unroll 1
         for (int i = 0; i < kTileRaw; ++i) {
             mbar_init(&sh.raw_full[i], 1);
             mbar_init(&sh.raw_empty[i], 4);
         }
+#pragma unroll 1
         for (int i = 0; i < kTileKeys; ++i) {
             mbar_init(&sh.k_full[i], 4);
             mbar_init(&sh.k_empty[i], PAIR ? 2 : 1);
         }
+#pragma unroll 1
         for (int i = 0; i < kTileValues; ++i) {
             mbar_init(&sh.v_full[i], 4);
             mbar_init(&sh.v_empty[i], PAIR ? 2 : 1);
         }
+#pragma unroll 1
         for (int i = 0; i < kTileMeta; ++i) {
             mbar_init(&sh.m_full[i], 4);
             mbar_init(&sh.m_empty[i], PAIR ? 8 : 4);
         }
+#pragma unroll 1
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.q_full[i], 4);
             for (int b = 0; b < 2; ++b) {
                 mbar_init(&sh.s_full[i][b], 1);
                 mbar_init(&sh.p_full[i][b], 4);
+                mbar_init(&sh.o_done[i][b], 1);
             }
-            mbar_init(&sh.o_done[i], 1);
             mbar_init(&sh.drain[i], 1);
-            sh.open[i].seg = -1;
         }
         mbar_init(&sh.x_full, 4);
         mbar_init(&sh.x_empty, 4);
         mbar_init(&sh.r_full, 4);
         sh.abort_flag = 0;
+        sh.open.seg = -1;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 12) tc_alloc(&sh.tmem, 512);
@@ -244,86 +244,126 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
     const int B = a.p.n_seqs, G = a.p.n_q_heads / a.p.n_kv_heads;
     const int strip = (B + kTileThreads - 1) / kTileThreads;
     long long mine = 0;
+#pragma unroll 1
     for (int b = tid * strip; b < min(B, (tid + 1) * strip); ++b) {
         const KvSeq s = kv_load_seq(a, b, R);
         mine += kv_tile_head_units(a, s, R, G) * a.p.n_kv_heads;
         if (s.fresh > 0 && (long long)s.cached + s.fresh > (long long)a.p.max_pages * kPage) raise(a.state, AASD_STATUS_BAD_OFFSETS);
     }
     tc_fence_before();
-    long long total;
-    sh.base[tid] = block_scan<kTileThreads>(mine, sh.scan, total);
+    long long sum;
+    sh.base[tid] = (int)block_scan<kTileThreads>(mine, sh.scan, sum);
     __syncthreads();
     tc_fence_after();
     const unsigned int tm = sh.tmem;
     volatile int* abort_flag = &sh.abort_flag;
-    const long long c = blockIdx.x;
-    const bool works = c < total;
-    if (tid == 0) {
-        const KvShares shares(total, works ? min((long long)gridDim.x, total) : 1);
-        KvTileWalk start{};
-        long long u1 = 0;
-        if (works) {
-            const long long u0 = shares.first(c);
-            u1 = shares.first(c + 1);
-            int lo = 0, hi = (B + strip - 1) / strip;
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (sh.base[mid] <= u0) lo = mid;
-                else hi = mid;
-            }
-            long long rem = u0 - sh.base[lo];
-            int b = lo * strip;
-            KvSeq s = kv_load_seq(a, b, R);
-            long long per_head = kv_tile_head_units(a, s, R, G);
-            while (rem >= per_head * a.p.n_kv_heads) {
-                rem -= per_head * a.p.n_kv_heads;
-                s = kv_load_seq(a, ++b, R);
-                per_head = kv_tile_head_units(a, s, R, G);
-            }
-            start.b = b;
-            start.take(s);
-            start.h = (int)(rem / per_head);
-            rem -= start.h * per_head;
-            start.pages = start.tile_pages(a, R, G);
-            if (a.node_parent != nullptr) {
-                start.tile = (int)(rem / (s.pages + kTileSegCost));
-                rem -= (long long)start.tile * (s.pages + kTileSegCost);
-            } else {
-                while (rem >= start.pages + kTileSegCost) {
-                    rem -= start.pages + kTileSegCost;
-                    ++start.tile;
-                    start.pages = start.tile_pages(a, R, G);
-                }
-            }
-            const int lead = rem < kTileSegCost ? kTileSegCost - (int)rem : 0;
-            start.pg = lead > 0 ? 0 : (int)rem - kTileSegCost;
-            start.left = (int)min(u1 - u0, (long long)0x7FFFFFFF) - lead;
-        }
-        sh.start = start;
-        sh.end = u1;
-        sh.shares = shares;
-    }
-    __syncthreads();
+    const int c = blockIdx.x, total = kv_total(a, sum);
+    // Waits are bounded; a role that gives up says so when it leaves, and the others find out in theirs.
     const auto wait_one = [&](u64* bar, unsigned int parity) {
-        if (mbar_wait(bar, parity, abort_flag, kWaitLimit)) return true;
-        give_up(abort_flag, a.state);
+#pragma unroll 1
+        for (unsigned int it = 0; it < kWaitLimit; ++it) {
+            if (mbar_try_wait(bar, parity)) return true;
+            if ((it & 255u) == 255u && *abort_flag) break;
+        }
         return false;
     };
     // (the lanes of a warp go on, or give up, together)
     const auto wait = [&](u64* bar, unsigned int parity) { return __all_sync(0xFFFFFFFFu, wait_one(bar, parity)) != 0; };
+    bool ok = true;
 
     if (warp >= 12) {
         fewer_registers<kTileOtherRegs>();
-        if (warp == 13) {
+        if (warp == 15) {
+            // ---- walker
+            if (lane == 0) {
+                const KvShares shares(total, min((int)gridDim.x, max(total, 1)));
+                sh.shares = shares;
+                KvTilePiece w{};
+                int left = 0;            // units of the share from page w.pg on
+                KvSeq q{};
+                if (c < total) {
+                    // the share's first unit: its sequence, head, tile and page
+                    const int u0 = shares.first(c);
+                    int lo = 0, hi = (B + strip - 1) / strip;
+#pragma unroll 1
+                    while (hi - lo > 1) {
+                        const int mid = (lo + hi) >> 1;
+                        if (sh.base[mid] <= u0) lo = mid;
+                        else hi = mid;
+                    }
+                    int rem = u0 - sh.base[lo], per_head;
+                    w.b = lo * strip - 1;
+#pragma unroll 1
+                    do {
+                        q = kv_load_seq(a, ++w.b, R);
+                        per_head = (int)kv_tile_head_units(a, q, R, G);
+                        rem -= per_head * a.p.n_kv_heads;
+                    } while (rem >= 0);
+                    rem += per_head * a.p.n_kv_heads;
+                    w.h = rem / per_head;
+                    rem -= w.h * per_head;
+                    w.tile = -1;
+#pragma unroll 1
+                    do {
+                        w.pages = kv_tile_pages(a, q.cached, q.fresh, q.pages, ++w.tile, R, G);
+                        rem -= w.pages + kTileSegCost;
+                    } while (rem >= 0);
+                    rem += w.pages;              // of the first page, counted from page 0
+                    w.pg = max(rem, 0);
+                    left = shares.first(c + 1) - u0 - (w.pg - rem);
+                    w.seg = u0 - rem;
+                }
+#pragma unroll 1
+                for (int k = 0; ok; ++k) {
+                    ok = wait_one(&sh.piece_empty[k % kTilePieces], ((k / kTilePieces) & 1) ^ 1);
+                    if (!ok) break;
+                    w.np = max(0, min(w.pages - w.pg, left));
+                    w.cached = q.cached;
+                    w.fresh = q.fresh;
+                    w.first = q.first;
+                    sh.piece[k % kTilePieces] = w;
+                    mbar_arrive(&sh.piece_full[k % kTilePieces]);
+                    if (w.np == 0) break;
+                    left -= w.pages - w.pg + kTileSegCost;
+                    w.seg += w.pages + kTileSegCost;
+                    w.pg = 0;
+                    if (++w.tile == q.tiles) {
+                        w.tile = 0;
+                        if (++w.h == a.p.n_kv_heads) {
+                            w.h = 0;
+#pragma unroll 1
+                            do {
+                                if (++w.b >= B) {
+                                    left = 0;
+                                    break;
+                                }
+                                q = kv_load_seq(a, w.b, R);
+                            } while (q.pages == 0 || q.tiles == 0);
+                        }
+                    }
+                    if (left > 0) w.pages = kv_tile_pages(a, q.cached, q.fresh, q.pages, w.tile, R, G);
+                }
+            }
+            __syncwarp();
+        } else if (warp == 13) {
             // ---- loader
             int n = 0;
-            bool ok = true;
-            for (KvTileWalk w = sh.start; ok && w.live(); w.next(a, R, G)) {
-                const int np = w.piece_pages();
-                const int32_t* table = a.block_table + (long long)w.b * a.p.max_pages;
+#pragma unroll 1
+            for (int k = 0;; ++k) {
+                ok = wait(&sh.piece_full[k % kTilePieces], (k / kTilePieces) & 1);
+                if (!ok) break;
+                const KvTilePiece& w = sh.piece[k % kTilePieces];
+                const int np = w.np, pg = w.pg;
+                if (np == 0) break;
+                const int32_t* table = a.block_table + (long long)w.b * a.p.max_pages + pg;
+                const uint8_t* head = a.pages + (long long)w.h * kv_head_bytes(D);
+                const u64 stride = (u64)a.p.n_kv_heads * kv_head_bytes(D);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.piece_empty[k % kTilePieces]);
                 int ids = 0;
+#pragma unroll 1
                 for (int i = 0; i < np; ++i, ++n) {
-                    if ((i & 31) == 0) ids = i + lane < np ? table[w.pg + i + lane] : -1;
+                    if ((i & 31) == 0) ids = i + lane < np ? table[i + lane] : -1;
                     const int page = __shfl_sync(0xFFFFFFFFu, ids, i & 31);
                     const int slot = n % kTileRaw;
                     ok = wait(&sh.raw_empty[slot], ((n / kTileRaw) & 1) ^ 1);
@@ -333,8 +373,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                         sh.raw_missing[slot] = !there;
                         if (there) {
                             mbar_arrive_expect_tx(&sh.raw_full[slot], kv_head_bytes(D));
-                            bulk_copy_g2s(sh.raw[slot], a.pages + ((long long)page * a.p.n_kv_heads + w.h) * kv_head_bytes(D), kv_head_bytes(D),
-                                          &sh.raw_full[slot]);
+                            bulk_copy_g2s(sh.raw[slot], head + (u64)(unsigned int)page * stride, kv_head_bytes(D), &sh.raw_full[slot]);
                         } else {
                             raise(a.state, AASD_STATUS_BAD_OFFSETS);
                             mbar_arrive(&sh.raw_full[slot]);
@@ -342,79 +381,65 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                     }
                     __syncwarp();
                 }
+                if (!ok) break;
             }
-            if (*abort_flag)   // nothing may be on its way into this CTA's shared memory when it leaves
-                for (int k = max(0, n - kTileRaw); k < n; ++k)
-                    for (unsigned int it = 0; it < kWaitLimit && !mbar_try_wait(&sh.raw_full[k % kTileRaw], (k / kTileRaw) & 1); ++it) {}
-        } else if (warp == 12 || warp == 14) {
+            // nothing may be on its way into this CTA's shared memory when it leaves
+#pragma unroll 1
+            for (int k = max(0, n - kTileRaw); k < n; ++k)
+#pragma unroll 1
+                for (unsigned int it = 0; it < kWaitLimit && !mbar_try_wait(&sh.raw_full[k % kTileRaw], (k / kTileRaw) & 1); ++it) {}
+        } else {
             // ---- issuers: warp 12 for group 0, warp 14 for group 1
             if (lane == 0) {
                 const int x = (warp - 12) >> 1;
-                // The group's pages: all of a piece, or every other page of the share.
-                struct Pages {
-                    KvTileWalk w;
-                    int np, i, n, j, piece;   // pages of the piece, page in it, page of the share, of the group, piece of the share
-                    bool first;               // of the group in this piece
-                };
-                auto skip = [&](Pages& p) {   // one page on, into the next piece if need be
-                    ++p.n;
-                    if (++p.i == p.np) {
-                        p.i = 0;
-                        ++p.piece;
-                        p.first = true;
-                        p.w.next(a, R, G);
-                        if (p.w.live()) p.np = p.w.piece_pages();
-                    }
-                };
-                auto begin = [&]() {
-                    Pages p{sh.start, sh.start.piece_pages(), 0, 0, 0, 0, true};
-                    if (!PAIR && x == 1 && p.w.live()) skip(p);
-                    return p;
-                };
-                auto step = [&](Pages& p) {
-                    p.first = false;
-                    ++p.j;
-                    skip(p);
-                    if (!PAIR && p.w.live()) skip(p);
-                };
-                bool ok = true;
-                int asked = 0;           // pieces whose queries have been waited for
-                auto multiply_keys = [&](Pages& p) {
-                    const int slot = p.n % kTileKeys, buf = p.j & 1;
-                    while (ok && asked <= p.piece) {
-                        ok = wait_one(&sh.q_full[x], asked & 1);
-                        ++asked;
-                    }
-                    ok = ok && wait_one(&sh.k_full[slot], (p.n / kTileKeys) & 1);
-                    if (!ok) return;
-                    tc_fence_after();
-                    const u64 q = tc_desc(smem_u32(sh.queries[PAIR ? x : 0])), k = tc_desc(smem_u32(sh.keys[slot]));
-#pragma unroll
-                    for (int ks = 0; ks < D / 16; ++ks)   // (descriptors count 16 bytes; a panel is 64 channels of all rows)
-                        tc_mma_ss(tm + kColS + x * kStep + buf * 64, q + (ks / 4) * (kTileRows * 8) + (ks % 4) * 2,
-                                  k + (ks / 4) * (kPage * 8) + (ks % 4) * 2, kIdescS, ks > 0);
-                    tc_commit(&sh.s_full[x][buf]);
-                    tc_commit(&sh.k_empty[slot]);
-                    step(p);
-                };
-                Pages keys = begin(), vals = begin();
-                while (ok && vals.w.live()) {
-                    // (not into the next piece: its queries come when this one's last page is in O)
-                    while (ok && keys.w.live() && keys.piece == vals.piece && keys.j < vals.j + 2) multiply_keys(keys);
-                    const int slot = vals.n % kTileValues, buf = vals.j & 1;
-                    ok = ok && wait_one(&sh.v_full[slot], (vals.n / kTileValues) & 1) && wait_one(&sh.p_full[x][buf], (vals.j >> 1) & 1);
+                // A piece's pages of the group: all, or every other page of the share.  The keys' products run up to two
+                // pages ahead, but not into the next piece: its queries come when this one's last page is in O.
+                int n0 = 0, taken = 0;   // pages of the share before the piece; of the group so far
+#pragma unroll 1
+                for (int k = 0;; ++k) {
+                    ok = wait_one(&sh.piece_full[k % kTilePieces], (k / kTilePieces) & 1);
                     if (!ok) break;
-                    tc_fence_after();
-                    const u64 v = tc_desc(smem_u32(sh.values[slot]));
+                    const int np = sh.piece[k % kTilePieces].np;
+                    if (np == 0) break;
+                    mbar_arrive(&sh.piece_empty[k % kTilePieces]);
+                    ok = wait_one(&sh.q_full[x], k & 1);
+                    if (!ok) break;
+                    const u64 q = tc_desc(smem_u32(sh.queries[PAIR ? x : 0]));
+                    const int first = PAIR ? 0 : (n0 ^ x) & 1, step = PAIR ? 1 : 2;
+                    int ahead = first, asked = taken;
+#pragma unroll 1
+                    for (int i = first; i < np; i += step, ++taken) {
+#pragma unroll 1
+                        for (; ahead < np && asked < taken + 2; ahead += step, ++asked) {
+                            const int n = n0 + ahead, slot = n % kTileKeys, buf = asked & 1;
+                            ok = wait_one(&sh.k_full[slot], (n / kTileKeys) & 1);
+                            if (!ok) break;
+                            tc_fence_after();
+                            const u64 keys = tc_desc(smem_u32(sh.keys[slot]));
 #pragma unroll
-                    for (int ks = 0; ks < kPage / 16; ++ks)
-                        tc_mma(tm + kColO + x * kStep, tm + kColS + x * kStep + buf * 64 + ks * 8, v + ks * 2, kIdescO, !vals.first || ks > 0);
-                    tc_commit(&sh.v_empty[slot]);
-                    tc_commit(&sh.o_done[x]);
-                    step(vals);
+                            for (int ks = 0; ks < D / 16; ++ks)   // (descriptors count 16 bytes; a panel is 64 channels of all rows)
+                                tc_mma_ss(tm + kColS + x * kStep + buf * 64, q + (ks / 4) * (kTileRows * 8) + (ks % 4) * 2,
+                                          keys + (ks / 4) * (kPage * 8) + (ks % 4) * 2, kIdescS, ks > 0);
+                            tc_commit(&sh.s_full[x][buf]);
+                            tc_commit(&sh.k_empty[slot]);
+                        }
+                        const int n = n0 + i, slot = n % kTileValues, buf = taken & 1;
+                        ok = ok && wait_one(&sh.v_full[slot], (n / kTileValues) & 1) && wait_one(&sh.p_full[x][buf], (taken >> 1) & 1);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const u64 v = tc_desc(smem_u32(sh.values[slot]));
+#pragma unroll
+                        for (int ks = 0; ks < kPage / 16; ++ks)
+                            tc_mma(tm + kColO + x * kStep, tm + kColS + x * kStep + buf * 64 + ks * 8, v + ks * 2, kIdescO, i > first || ks > 0);
+                        tc_commit(&sh.v_empty[slot]);
+                        tc_commit(&sh.o_done[x][buf]);
+                    }
+                    if (!ok) break;
+                    n0 += np;
                 }
                 // products in flight read this CTA's shared memory
                 tc_commit(&sh.drain[x]);
+#pragma unroll 1
                 for (unsigned int it = 0; it < kWaitLimit && !mbar_try_wait(&sh.drain[x], 0); ++it) {}
             }
             __syncwarp();
@@ -424,10 +449,17 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
         fewer_registers<kTileOtherRegs>();
         const int u = tid - 256, uw = warp - 8;
         int n = 0;
-        bool ok = true;
-        for (KvTileWalk w = sh.start; ok && w.live(); w.next(a, R, G)) {
-            const int np = w.piece_pages();
+#pragma unroll 1
+        for (int k = 0;; ++k) {
+            ok = wait(&sh.piece_full[k % kTilePieces], (k / kTilePieces) & 1);
+            if (!ok) break;
+            const KvTilePiece& piece = sh.piece[k % kTilePieces];
+            const int np = piece.np, end = piece.cached + piece.fresh - piece.pg * kPage;   // places from the first page's on
+            __syncwarp();
+            if (np == 0) break;
+            if (lane == 0) mbar_arrive(&sh.piece_empty[k % kTilePieces]);
             int ev = 64;
+#pragma unroll 1
             for (int i = 0; i < np; ++i, ++n) {
                 const int slot = n % kTileRaw, mslot = n % kTileMeta, kslot = n % kTileKeys, vslot = n % kTileValues;
                 ok = wait(&sh.raw_full[slot], (n / kTileRaw) & 1) && wait(&sh.m_empty[mslot], ((n / kTileMeta) & 1) ^ 1) &&
@@ -435,7 +467,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                 if (!ok) break;
                 const unsigned char* raw = sh.raw[slot];
                 const bool missing = sh.raw_missing[slot] != 0;
-                const int left = missing ? 0 : w.cached + w.fresh - (w.pg + i) * kPage;   // places in use
+                const int left = missing ? 0 : end - i * kPage;   // places in use
                 // largest value of the page (every warp for itself): codes run from the minimum to 15 scales above it
                 const uint2 vm = *reinterpret_cast<const uint2*>(raw + kv_value_meta_offset(D) + 8 * lane);
                 auto reach = [](unsigned int m) { return fmaxf(fabsf(meta_min(m)), fabsf(fmaf(15.f, meta_scale(m), meta_min(m)))); };
@@ -445,9 +477,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                 ev = max(ev, min(250, (int)(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(vt)) >> 23)));
                 if (u < kPage) {
                     const unsigned int km = u < left ? *reinterpret_cast<const unsigned int*>(raw + kv_key_meta_offset(D) + 4 * u) : 0u;
-                    float* kq = reinterpret_cast<float*>(&sh.kmeta[mslot][u >> 1]);
-                    kq[u & 1] = meta_scale(km);
-                    kq[2 + (u & 1)] = meta_min(km);
+                    const int at = tile_place(u);
+                    float* kq = reinterpret_cast<float*>(&sh.kmeta[mslot][at >> 1]);
+                    kq[at & 1] = meta_scale(km);
+                    kq[2 + (at & 1)] = meta_min(km);
                     if (u == 0) sh.ev[mslot] = missing ? -1 : ev;
                 }
                 {
@@ -463,13 +496,14 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                         const uint4 q = lds16(from + 4 * k);
                         wd[k] = q.x; wd[k + 1] = q.y; wd[k + 2] = q.z; wd[k + 3] = q.w;
                     }
-                    unsigned char* to = sh.keys[kslot] + t * 128;
+                    const int at = tile_place(t);
+                    unsigned char* to = sh.keys[kslot] + at * 128;
 #pragma unroll
                     for (int k = 0; k < NW; ++k) {
                         const int kk = NW == 8 ? k ^ (part * 4) : k;
                         const unsigned int x = NW == 8 ? (part ? wd[k ^ 4] : wd[k]) : wd[k], y = x >> 8;
                         const int piece = part * NW + kk;        // of the token's H / 4
-                        *reinterpret_cast<uint4*>(to + (piece >> 3) * (kPage * 128) + (((piece & 7) ^ (t & 7)) << 4)) =
+                        *reinterpret_cast<uint4*>(to + (piece >> 3) * (kPage * 128) + (((piece & 7) ^ (at & 7)) << 4)) =
                             make_uint4(x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u);
                     }
                 }
@@ -522,170 +556,222 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                     mbar_arrive(&sh.raw_empty[slot]);
                 }
             }
+            if (!ok) break;
         }
     } else {
-        // ---- softmax: thread = row
+        // ---- softmax: thread (g, j) of a warp has rows g, g + 8, g + 16, g + 24 of the warp's 32 and two columns of every eight
         more_registers<kTileSoftmaxRegs>();
-        const int x = warp >> 2, row_in = tid & 127;
-        const unsigned int lanes = (unsigned int)(warp & 3) << 21;         // the warp's lanes in an address: 32 (warp % 4) << 16
+        const int x = warp >> 2, g = lane >> 2, j = lane & 3, row_base = (warp & 3) * 32;   // (of the group's 128 rows)
+        const unsigned int lanes = (unsigned int)row_base << 16;
         const unsigned int col_s = tm + kColS + x * kStep + lanes, col_o = tm + kColO + x * kStep + lanes;
-        int n0 = 0, taken = 0, added = 0, pieces = 0;    // pages before the piece; pages taken; pages known to be in O; pieces done
-        bool ok = true;
-        for (KvTileWalk w = sh.start; ok && w.live(); w.next(a, R, G)) {
-            const int np = w.piece_pages();
-            const int row = w.tile * R + (PAIR ? x * kTileRows : 0) + row_in;
-            const bool valid = row < w.fresh * G;
-            const int tok = valid ? row / G : 0;
-            const long long head = ((long long)w.first + tok) * a.p.n_q_heads + w.h * G + (valid ? row - tok * G : 0);
-            float rfac = 1.f, qfac = 0.f;  // exponent (base 2) of a product = rfac * (scale * S + minimum * qfac)
+        int n0 = 0, taken = 0;    // pages of the share before the piece; of the group so far
+        // All pages taken so far are in O.  (Not waited for with every page: a barrier for every other page keeps the
+        // phases apart, since S of a page comes after O of the page two before it.)
+        const auto o_complete = [&]() {
+            const bool done = wait(&sh.o_done[x][(taken - 1) & 1], ((taken - 1) >> 1) & 1);
+            tc_fence_after();
+            return done;
+        };
+#pragma unroll 1
+        for (int piece = 0;; ++piece) {
+            ok = wait(&sh.piece_full[piece % kTilePieces], (piece / kTilePieces) & 1);
+            if (!ok) break;
+            const KvTilePiece w = sh.piece[piece % kTilePieces];
+            __syncwarp();
+            const int np = w.np;
+            if (np == 0) break;
+            if (lane == 0) mbar_arrive(&sh.piece_empty[piece % kTilePieces]);
+            const int row0 = w.tile * R + (PAIR ? x * kTileRows : 0) + row_base;   // of the warp's first row, among the head's
+            const int rows_here = w.fresh * G;                                    // rows of the head
+            const int own_row = max(min(row0 + lane, rows_here - 1), 0);   // the lane's row: what the warp wants to know of its 32 rows
+            const int token = own_row / G, member = own_row - token * G;
             if (PAIR || x == 0) {
-                // the row's queries as fp16 numbers, its largest element 2^14 .. 2^15, channels in the order of the keys' words
-                const long long q0 = ((long long)w.first + tok) * a.p.q_stride + (head - ((long long)w.first + tok) * a.p.n_q_heads) * D;
-                float top = 0.f, sum = 0.f;
-#pragma unroll 4
-                for (int k = 0; k < D; k += 8) {
-                    float y[8];
-                    if (a.q_vec) load8<AASD_BF16, true>(a.q, q0 + k, y);
-                    else load8<AASD_BF16, false>(a.q, q0 + k, y);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        top = fmaxf(top, fabsf(y[e]));
-                        sum += y[e];
-                    }
-                }
-                int e = (int)(__float_as_uint(top) >> 23) - 127;
-                e = e < -100 ? -100 : e > 100 ? 100 : e;
-                const float up = valid ? pow2f(14 - e) : 0.f;
-                rfac = fmaxf(a.scale_log2 * pow2f(e + 10), 1e-37f);   // (never 0: what is hidden is -inf times it)
-                qfac = valid ? sum * pow2f(-10 - e) : 0.f;
-                unsigned char* to = sh.queries[PAIR ? x : 0] + row_in * 128;
-#pragma unroll 4
-                for (int cb = 0; cb < H; cb += 8) {       // eight channels of each half are two 16-byte pieces
-                    float lo[8], hi[8];
+                // The rows' queries as fp16 numbers, a row's largest element 2^14 .. 2^15, channels in the order of the
+                // keys' words; D / 8 lanes fetch a row together.
+                constexpr int LR = D / 8, RI = 32 / LR;        // lanes per row, rows per step
+                const int part = lane % LR;                    // eight channels: of the low half, then of the high one
+                const long long at = ((long long)w.first + token) * a.p.q_stride + (long long)(w.h * G + member) * D;   // of the lane's row
+                unsigned char* to = sh.queries[PAIR ? x : 0];
+#pragma unroll 1
+                for (int rb = 0; rb < 32; rb += 8 * RI) {
+                    Raw8<AASD_BF16, true> raw[8];
+                    // (all on their way before the first is looked at; rows past the last one repeat it, and become zero)
                     if (a.q_vec) {
-                        load8<AASD_BF16, true>(a.q, q0 + cb, lo);
-                        load8<AASD_BF16, true>(a.q, q0 + H + cb, hi);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) raw[k].load(a.q, __shfl_sync(0xFFFFFFFFu, at, rb + k * RI + lane / LR) + part * 8);
                     } else {
-                        load8<AASD_BF16, false>(a.q, q0 + cb, lo);
-                        load8<AASD_BF16, false>(a.q, q0 + H + cb, hi);
-                    }
+#pragma unroll 1
+                        for (int k = 0; k < 8; ++k) {
+                            Raw8<AASD_BF16, false> slow;
+                            slow.load(a.q, __shfl_sync(0xFFFFFFFFu, at, rb + k * RI + lane / LR) + part * 8);
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        lo[q] = valid ? lo[q] * up : 0.f;
-                        hi[q] = valid ? hi[q] * (up * 0.0625f) : 0.f;
+                            for (int i = 0; i < 8; ++i)
+                                if (i == k) raw[i].a = slow.a;
+                        }
                     }
+                    float top[8], sum[8];
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const int piece = cb / 4 + q;
-                        *reinterpret_cast<uint4*>(to + (piece >> 3) * (kTileRows * 128) + (((piece & 7) ^ (row_in & 7)) << 4)) =
-                            make_uint4(pack_half(lo[4 * q], lo[4 * q + 2]), pack_half(lo[4 * q + 1], lo[4 * q + 3]), pack_half(hi[4 * q], hi[4 * q + 2]),
-                                       pack_half(hi[4 * q + 1], hi[4 * q + 3]));
+                    for (int k = 0; k < 8; ++k) {
+                        if (row0 + rb + k * RI + lane / LR >= rows_here) raw[k].clear();
+                        float2 y[4];
+                        raw[k].unpack(y);
+                        top[k] = fmaxf(fmaxf(fmaxf(fabsf(y[0].x), fabsf(y[0].y)), fmaxf(fabsf(y[1].x), fabsf(y[1].y))),
+                                       fmaxf(fmaxf(fabsf(y[2].x), fabsf(y[2].y)), fmaxf(fabsf(y[3].x), fabsf(y[3].y))));
+                        sum[k] = ((y[0].x + y[0].y) + (y[1].x + y[1].y)) + ((y[2].x + y[2].y) + (y[3].x + y[3].y));
+                    }
+#pragma unroll 1
+                    for (int o = 1; o < LR; o <<= 1)
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            top[k] = fmaxf(top[k], __shfl_xor_sync(0xFFFFFFFFu, top[k], o));
+                            sum[k] += __shfl_xor_sync(0xFFFFFFFFu, sum[k], o);
+                        }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int r = row_base + rb + k * RI + lane / LR;
+                        float2 y[4];
+                        raw[k].unpack(y);
+                        int e = (int)(__float_as_uint(top[k]) >> 23) - 127;
+                        e = e < -100 ? -100 : e > 100 ? 100 : e;
+                        const bool high = part >= LR / 2;
+                        const float up = pow2f((high ? 10 : 14) - e);
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            const int piece = 2 * (part % (LR / 2)) + q;
+                            *reinterpret_cast<uint2*>(to + r * 128 + (piece >> 3) * (kTileRows * 128) + (((piece & 7) ^ (r & 7)) << 4) + (high ? 8 : 0)) =
+                                make_uint2(pack_half(y[2 * q].x * up, y[2 * q + 1].x * up), pack_half(y[2 * q].y * up, y[2 * q + 1].y * up));
+                        }
+                        if (part == 0) {
+                            // exponent (base 2) of a product = row_r * (scale * S + minimum * row_q)
+                            sh.row_r[PAIR ? x : 0][r] = fmaxf(a.scale_log2 * pow2f(e + 10), 1e-37f);   // (never 0: what is hidden is -inf times it)
+                            sh.row_q[PAIR ? x : 0][r] = sum[k] * pow2f(-10 - e);
+                        }
                     }
                 }
                 fence_async_smem();
-                if (!PAIR) {
-                    sh.exchange_up[row_in] = rfac;
-                    sh.exchange_m[row_in] = qfac;
-                }
+                __syncwarp();
             }
             if (!PAIR) {
                 // one set of queries for both groups
                 if (x == 0) {
-                    __syncwarp();
                     if (lane == 0) mbar_arrive(&sh.r_full);
                 } else {
-                    ok = wait(&sh.r_full, pieces & 1);
+                    ok = wait(&sh.r_full, piece & 1);
                     if (!ok) break;
-                    rfac = sh.exchange_up[row_in];
-                    qfac = sh.exchange_m[row_in];
                 }
             }
-            __syncwarp();
             if (lane == 0) mbar_arrive(&sh.q_full[x]);
-            float mref = kKvNothing, l = 0.f;
+            float rf[4], qf[4], mref[4], l[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                rf[i] = sh.row_r[PAIR ? x : 0][row_base + g + 8 * i];
+                qf[i] = sh.row_q[PAIR ? x : 0][row_base + g + 8 * i];
+                mref[i] = kKvNothing;
+                l[i] = 0.f;
+            }
+            // places up to which every row of the warp sees everything
+            const int open_to = a.node_parent != nullptr ? w.cached : w.cached + row0 / G + 1;
             int ev = 64;
             bool first = true;
-            float s[64];
+#pragma unroll 1
             for (int i = PAIR ? 0 : (n0 ^ x) & 1; i < np; i += PAIR ? 1 : 2) {
                 const int n = n0 + i, mslot = n % kTileMeta, pg = w.pg + i, buf = taken & 1;
                 const unsigned int col = col_s + buf * 64;
                 ok = wait(&sh.m_full[mslot], (n / kTileMeta) & 1) && wait(&sh.s_full[x][buf], (taken >> 1) & 1);
                 if (!ok) break;
                 tc_fence_after();
-                tc_load64(col, s);
+                float s[2][32];   // rows g and g + 8; g + 16 and g + 24
+                tc_load(col, s[0]);
+                tc_load(col + (16u << 16), s[1]);
                 const int evn = sh.ev[mslot];
 #pragma unroll
-                for (int k = 0; k < 32; ++k) {
-                    const float4 m = sh.kmeta[mslot][k];
-                    const float2 y = __ffma2_rn(make_float2(m.z, m.w), make_float2(qfac, qfac),
-                                                __fmul2_rn(make_float2(s[2 * k], s[2 * k + 1]), make_float2(m.x, m.y)));
-                    s[2 * k] = y.x;
-                    s[2 * k + 1] = y.y;
-                }
-                if (evn < 0 || (pg + 1) * kPage > w.cached) {   // what the row does not see becomes -inf
-                    const u64 seen = evn < 0 || !valid ? 0ull : kv_seen(a, w.cached, w.fresh, w.first, pg, tok);
+                for (int k = 0; k < 8; ++k) {
+                    const float4 m = sh.kmeta[mslot][4 * k + j];
 #pragma unroll
-                    for (int k = 0; k < 64; ++k)
-                        if (!((seen >> k) & 1ull)) s[k] = -CUDART_INF_F;
+                    for (int q = 0; q < 4; ++q) {   // row g + 8 q
+                        float& s0 = s[q >> 1][4 * k + 2 * (q & 1)];
+                        float& s1 = s[q >> 1][4 * k + 2 * (q & 1) + 1];
+                        const float2 y = __ffma2_rn(make_float2(m.z, m.w), make_float2(qf[q], qf[q]), __fmul2_rn(make_float2(s0, s1), make_float2(m.x, m.y)));
+                        s0 = y.x;
+                        s1 = y.y;
+                    }
                 }
-                float m0 = s[0], m1 = s[1], m2 = s[2], m3 = s[3];
+                if (evn < 0 || (pg + 1) * kPage > open_to) {   // what a row does not see becomes -inf (lane r finds out for row r)
+                    const u64 mine = evn < 0 || row0 + lane >= rows_here ? 0ull : tile_places(kv_seen(a, w.cached, w.fresh, w.first, pg, token));
 #pragma unroll
-                for (int k = 4; k < 64; k += 4) {
-                    m0 = fmaxf(m0, s[k]);
-                    m1 = fmaxf(m1, s[k + 1]);
-                    m2 = fmaxf(m2, s[k + 2]);
-                    m3 = fmaxf(m3, s[k + 3]);
-                }
-                const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * rfac;
-                // (the page before is in O: the issuer's products of it ran during the steps above)
-                if (added < taken) {
-                    ok = wait(&sh.o_done[x], added & 1);
-                    ++added;
-                    if (!ok) break;
-                }
-                const int en = max(ev, evn);
-                if (__any_sync(0xFFFFFFFFu, top > mref + kTileLazy || en > ev)) {
-                    const float mn = fmaxf(mref, top);
-                    const float f = ex2_approx(mref - mn);
-                    mref = mn;
-                    l *= f;
-                    if (!first) {
-                        tc_fence_after();
-                        const float fo = en - ev > 126 ? 0.f : f * pow2f(ev - en);
+                    for (int q = 0; q < 4; ++q) {
+                        const u64 seen = __shfl_sync(0xFFFFFFFFu, mine, g + 8 * q) >> (2 * j);
 #pragma unroll
-                        for (int cb = 0; cb < D; cb += 32) {
-                            float o[32];
-                            tc_load32(col_o + cb, o);
-#pragma unroll
-                            for (int k = 0; k < 32; k += 8)
-                                tc_store8(col_o + cb + k, __float_as_uint(o[k] * fo), __float_as_uint(o[k + 1] * fo), __float_as_uint(o[k + 2] * fo),
-                                          __float_as_uint(o[k + 3] * fo), __float_as_uint(o[k + 4] * fo), __float_as_uint(o[k + 5] * fo),
-                                          __float_as_uint(o[k + 6] * fo), __float_as_uint(o[k + 7] * fo));
+                        for (int k = 0; k < 8; ++k) {
+                            const unsigned int two = (unsigned int)(seen >> (8 * k));
+                            if (!(two & 1u)) s[q >> 1][4 * k + 2 * (q & 1)] = -CUDART_INF_F;
+                            if (!(two & 2u)) s[q >> 1][4 * k + 2 * (q & 1) + 1] = -CUDART_INF_F;
                         }
                     }
-                    ev = en;
+                }
+                // Probabilities with the maximum as it stands; only where a thread's sum of them leaves fp16's range (by a
+                // new maximum at least 2^5 above it), and on the first page, is the maximum looked for and this done again.
+                float ls[4];
+                bool again = first;
+#pragma unroll 1
+                for (;;) {
+                    if (again) {
+                        float fo[4];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            float m = -CUDART_INF_F;
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) m = fmaxf(m, fmaxf(s[q >> 1][4 * k + 2 * (q & 1)], s[q >> 1][4 * k + 2 * (q & 1) + 1]));
+                            m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+                            m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+                            const float mn = fmaxf(mref[q], m * rf[q]);
+                            fo[q] = ex2_approx(mref[q] - mn);
+                            mref[q] = mn;
+                            l[q] *= fo[q];
+                        }
+                        if (!first) {
+                            ok = o_complete();
+                            if (!ok) break;
+                            tile_scale_o<D>(col_o, fo);
+                        }
+                    }
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        unsigned int pk[16];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int q = 2 * half + e;
+                            const float2 ff = make_float2(rf[q], rf[q]), mm = make_float2(kTileP - mref[q], kTileP - mref[q]);
+                            float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                float2 p = __ffma2_rn(make_float2(s[half][4 * k + 2 * e], s[half][4 * k + 2 * e + 1]), ff, mm);
+                                p = make_float2(ex2_approx(p.x), ex2_approx(p.y));
+                                sum = __fadd2_rn(sum, p);
+                                pk[2 * k + e] = pack_half(p.x, p.y);
+                            }
+                            ls[q] = sum.x + sum.y;
+                        }
+                        tc_store_cells(col + ((unsigned int)(16 * half) << 16), pk);
+                    }
+                    if (again || __all_sync(0xFFFFFFFFu, fmaxf(fmaxf(ls[0], ls[1]), fmaxf(ls[2], ls[3])) < 65504.f)) break;
+                    again = true;
+                }
+                if (!ok) break;
+                if (evn > ev) {
+                    // values of this page are relative to a larger exponent than O
+                    if (!first) {
+                        ok = o_complete();
+                        if (!ok) break;
+                        const float f = evn - ev > 126 ? 0.f : pow2f(ev - evn);
+                        const float fo[4] = {f, f, f, f};
+                        tile_scale_o<D>(col_o, fo);
+                    }
+                    ev = evn;
                 }
                 first = false;
-                // probabilities, to 32 columns in the order of the values' words
-                const float2 ff = make_float2(rfac, rfac), mm = make_float2(kTileP - mref, kTileP - mref);
-                float2 l0 = make_float2(0.f, 0.f), l1 = make_float2(0.f, 0.f);
 #pragma unroll
-                for (int kb = 0; kb < 4; ++kb) {             // sixteen tokens are eight columns
-                    unsigned int pk[8];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int t = 16 * kb + 4 * k;
-                        float2 p = __ffma2_rn(make_float2(s[t], s[t + 1]), ff, mm), q = __ffma2_rn(make_float2(s[t + 2], s[t + 3]), ff, mm);
-                        p = make_float2(ex2_approx(p.x), ex2_approx(p.y));
-                        q = make_float2(ex2_approx(q.x), ex2_approx(q.y));
-                        l0 = __fadd2_rn(l0, p);
-                        l1 = __fadd2_rn(l1, q);
-                        pk[2 * k] = pack_half(p.x, q.x);
-                        pk[2 * k + 1] = pack_half(p.y, q.y);
-                    }
-                    tc_store8(col + 8 * kb, pk[0], pk[1], pk[2], pk[3], pk[4], pk[5], pk[6], pk[7]);
-                }
-                l += (l0.x + l0.y) + (l1.x + l1.y);
+                for (int q = 0; q < 4; ++q) l[q] += ls[q];
                 ++taken;
                 tc_wait_store();
                 tc_fence_before();
@@ -699,172 +785,179 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
             // the result of the piece
             const bool any = !first;
             if (any) {
-                ok = wait(&sh.o_done[x], added & 1);
-                ++added;
+                ok = o_complete();
                 if (!ok) break;
-                tc_fence_after();
             }
-            float unscale = pow2f(ev - 127);
-            mref -= kTileP;                // (l and O carry the probabilities' power of two)
             const bool complete = w.pg == 0 && np == w.pages;
             const int which = w.pg > 0 ? 0 : 1;
-            const int rows = min(R, w.fresh * G - w.tile * R);
+            const int rows = min(R, rows_here - w.tile * R);
             constexpr int kPart = R * D + 2 * R;
-            const int r = (PAIR ? x * kTileRows : 0) + row_in;
-            float* part = a.cta_parts + (c * 2 + which) * kPart;
-            float other = 0.f;             // factor of the other group's O
+            float* part = a.cta_parts + (long long)(c * 2 + which) * kPart;
+            float own[4], other[4];        // factors of this group's O, and of the other's
+            const float unscale = any ? pow2f(ev - 127) : 0.f;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                l[q] += __shfl_xor_sync(0xFFFFFFFFu, l[q], 1);
+                l[q] += __shfl_xor_sync(0xFFFFFFFFu, l[q], 2);
+                mref[q] -= kTileP;         // (l and O carry the probabilities' power of two)
+                own[q] = unscale;
+                other[q] = 0.f;
+            }
             if (!PAIR) {
                 // group 0 reads both groups' O (the same lanes of tensor memory)
                 if (x == 1) {
-                    sh.exchange_m[row_in] = mref;
-                    sh.exchange_l[row_in] = l;
-                    sh.exchange_up[row_in] = any ? unscale : 0.f;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        if (j == 0) {
+                            const int r = row_base + g + 8 * q;
+                            sh.exchange_m[r] = mref[q];
+                            sh.exchange_l[r] = l[q];
+                            sh.exchange_up[r] = unscale;
+                        }
+                    }
                     __syncwarp();
                     tc_fence_before();
                     if (lane == 0) mbar_arrive(&sh.x_full);
-                    ok = wait(&sh.x_empty, pieces & 1);
+                    ok = wait(&sh.x_empty, piece & 1);
                     if (!ok) break;
                 } else {
-                    ok = wait(&sh.x_full, pieces & 1);
+                    ok = wait(&sh.x_full, piece & 1);
                     if (!ok) break;
                     tc_fence_after();
-                    const float om = sh.exchange_m[row_in], mn = fmaxf(mref, om), of = ex2_approx(om - mn), own = ex2_approx(mref - mn);
-                    l = l * own + sh.exchange_l[row_in] * of;
-                    unscale *= own;
-                    other = sh.exchange_up[row_in] * of;
-                    mref = mn;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int r = row_base + g + 8 * q;
+                        const float om = sh.exchange_m[r], mn = fmaxf(mref[q], om), of = ex2_approx(om - mn), f = ex2_approx(mref[q] - mn);
+                        l[q] = l[q] * f + sh.exchange_l[r] * of;
+                        own[q] *= f;
+                        other[q] = sh.exchange_up[r] * of;
+                        mref[q] = mn;
+                    }
                 }
             }
             if (PAIR || x == 0) {
-                const bool any1 = !PAIR && __any_sync(0xFFFFFFFFu, sh.exchange_up[row_in] != 0.f);   // (the same for every row)
-                const float inv = complete ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
+                const bool any1 = !PAIR && sh.exchange_up[row_base] != 0.f;   // (the same for every row)
+                // the results go through the places of the warp's own queries, which have been used
+                const auto stage = [&](int lr, int piece) {
+                    return sh.queries[PAIR ? x : 0] + (row_base + lr) * 128 + (piece >> 3) * (kTileRows * 128) + (((piece & 7) ^ (lr & 7)) << 4);
+                };
+                if (complete) {
 #pragma unroll
-                for (int cb = 0; cb < D; cb += 32) {
-                    float o[32];
-                    if (any) {
-                        tc_load32(col_o + cb, o);
-                    } else {
+                    for (int q = 0; q < 4; ++q) {
+                        const float inv = l[q] > 0.f ? 1.f / l[q] : 0.f;
+                        own[q] *= inv;
+                        other[q] *= inv;
+                    }
+                }
+#pragma unroll 1
+                for (int cb = 0; cb < D; cb += 64) {
+#pragma unroll 1
+                    for (int half = 0; half < 2; ++half) {      // rows g, g + 8; g + 16, g + 24
+                        const float f0 = half ? own[2] : own[0], f1 = half ? own[3] : own[1];
+                        float o[32];
 #pragma unroll
                         for (int k = 0; k < 32; ++k) o[k] = 0.f;
-                    }
+                        if (any) {
+                            tc_load(col_o + cb + ((unsigned int)(16 * half) << 16), o);
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) o[k] *= unscale;
-                    if (!PAIR && any1) {
-                        float y[32];
-                        tc_load32(col_o + kStep + cb, y);
+                            for (int k = 0; k < 32; ++k) o[k] *= (k >> 1) & 1 ? f1 : f0;
+                        }
+                        if (any1) {
+                            const float g0 = half ? other[2] : other[0], g1 = half ? other[3] : other[1];
+                            float y[32];
+                            tc_load(col_o + kStep + cb + ((unsigned int)(16 * half) << 16), y);
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] = fmaf(y[k], other, o[k]);
-                    }
-                    if (r < rows) {
-                        if (complete) {
+                            for (int k = 0; k < 32; ++k) o[k] = fmaf(y[k], (k >> 1) & 1 ? g1 : g0, o[k]);
+                        }
 #pragma unroll
-                            for (int k = 0; k < 32; k += 8) {
-                                float y[8];
+                        for (int k = 0; k < 8; ++k)
 #pragma unroll
-                                for (int q = 0; q < 8; ++q) y[q] = o[k + q] * inv;
-                                if (a.out_vec) store8<AASD_BF16, true>(a.o.out, head * D + cb + k, y);
-                                else store8<AASD_BF16, false>(a.o.out, head * D + cb + k, y);
+                            for (int e = 0; e < 2; ++e) {
+                                const int lr = g + 16 * half + 8 * e, ch = cb + 8 * k + 2 * j;
+                                const float2 v = make_float2(o[4 * k + 2 * e], o[4 * k + 2 * e + 1]);
+                                if (complete) {
+                                    *reinterpret_cast<unsigned int*>(stage(lr, ch >> 3) + 4 * j) = pack_bf16(v.x, v.y);
+                                } else if ((PAIR ? x * kTileRows : 0) + row_base + lr < rows) {
+                                    *reinterpret_cast<float2*>(part + ((PAIR ? x * kTileRows : 0) + row_base + lr) * D + ch) = v;
+                                }
                             }
-                        } else {
+                    }
+                }
+                if (complete) {
+                    __syncwarp();
+                    constexpr int LR = D / 8, RI = 32 / LR;     // lanes per row, rows per step
+                    const long long own_head = ((long long)w.first + token) * a.p.n_q_heads + w.h * G + member;
+#pragma unroll 4
+                    for (int rb = 0; rb < 32; rb += RI) {
+                        const int lr = rb + lane / LR;
+                        const long long head = __shfl_sync(0xFFFFFFFFu, own_head, lr);
+                        if (row0 + lr < rows_here) {
+                            const uint4 v = lds16(stage(lr, lane % LR));
+                            if (a.out_vec) {
+                                *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.o.out) + head * D + (lane % LR) * 8) = v;
+                            } else {
+                                unsigned short* to = static_cast<unsigned short*>(a.o.out) + head * D + (lane % LR) * 8;
+                                const unsigned int u4[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                            for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(part + r * D + cb + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+                                for (int e = 0; e < 8; ++e) to[e] = (unsigned short)(u4[e >> 1] >> (16 * (e & 1)));
+                            }
+                        }
+                    }
+                    __syncwarp();
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int r = (PAIR ? x * kTileRows : 0) + row_base + g + 8 * q, row = row0 + g + 8 * q;
+                    if (j == 0 && row < rows_here) {
+                        if (!complete) {
+                            part[R * D + r] = mref[q];
+                            part[R * D + R + r] = l[q];
+                        } else if (a.o.lse != nullptr) {
+                            a.o.lse[((long long)w.first + row / G) * a.p.n_q_heads + w.h * G + row % G] =
+                                l[q] > 0.f ? (mref[q] + log2f(l[q])) * (float)kLn2 : -CUDART_INF_F;
                         }
                     }
                 }
-                if (r < rows) {
-                    if (complete) {
-                        if (a.o.lse != nullptr) a.o.lse[head] = l > 0.f ? (mref + log2f(l)) * (float)kLn2 : -CUDART_INF_F;
-                    } else {
-                        part[R * D + r] = mref;
-                        part[R * D + R + r] = l;
-                    }
-                }
-                if (!complete && tid == 0) sh.open[which] = KvPiece{sh.end - w.left - w.pg, w.pages, w.h, w.tile * R, rows, w.first};
+                if (!complete && which == 1 && tid == 0) sh.open = KvPiece{w.seg, w.pages, w.h, w.tile * R, rows, w.first};
             }
             if (!PAIR && x == 0) {   // group 1 may go on
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.x_empty);
             }
-            ++pieces;
             tc_fence_before();
             n0 += np;
         }
-        softmax_sync();
-        if (works && !*abort_flag && (sh.open[0].seg >= 0 || sh.open[1].seg >= 0)) {
-            // the last CTA that delivers a part of a segment joins them all
-            if (tid < 2) {
-                int last = 0;
-                if (sh.open[tid].seg >= 0) {
-                    const KvPiece pc = sh.open[tid];
-                    const long long c0 = sh.shares.owner(pc.seg), c1 = sh.shares.owner(pc.seg + pc.pages - 1);
-                    last = take_ticket(a.tickets + c0) == (unsigned int)(c1 - c0);
-                    if (last) a.tickets[c0] = 0;
-                }
-                sh.last[tid] = last;
-            }
-            softmax_sync();
-            constexpr int kPart = R * D + 2 * R;
-            constexpr int RB = 8;             // rows that a warp has under way together
-#pragma unroll 1
-            for (int which = 0; which < 2; ++which) {
-                if (!sh.last[which]) continue;
-                const KvPiece pc = sh.open[which];
-                const long long c0 = sh.shares.owner(pc.seg);
-                const int parts = (int)(sh.shares.owner(pc.seg + pc.pages - 1) - c0) + 1;
-                const float* base = a.cta_parts + c0 * 2 * kPart;   // part k: 2 k, the first one's 1
-                for (int r0 = warp * RB; r0 < pc.n; r0 += 8 * RB) {
-                    float M[RB], L[RB];
-                    float4 o[RB];
-#pragma unroll
-                    for (int i = 0; i < RB; ++i) {
-                        M[i] = kKvNothing;
-                        L[i] = 0.f;
-                        o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    }
-                    const int ch = lane * 4;
-                    for (int k = 0; k < parts; ++k) {
-                        const float* from = base + (2 * k + (k == 0)) * kPart;
-                        float4 y[RB];
-                        float m[RB], ll[RB];
-#pragma unroll
-                        for (int i = 0; i < RB; ++i) {
-                            const int r = min(r0 + i, pc.n - 1);
-                            m[i] = __ldcg(from + R * D + r);
-                            ll[i] = __ldcg(from + R * D + R + r);
-                            y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                            if (ch < D) y[i] = __ldcg(reinterpret_cast<const float4*>(from + r * D + ch));
-                        }
-#pragma unroll
-                        for (int i = 0; i < RB; ++i) {
-                            const float mn = fmaxf(M[i], m[i]), f0 = ex2_approx(M[i] - mn), f1 = ex2_approx(m[i] - mn);
-                            M[i] = mn;
-                            L[i] = fmaf(L[i], f0, ll[i] * f1);
-                            o[i].x = fmaf(o[i].x, f0, y[i].x * f1);
-                            o[i].y = fmaf(o[i].y, f0, y[i].y * f1);
-                            o[i].z = fmaf(o[i].z, f0, y[i].z * f1);
-                            o[i].w = fmaf(o[i].w, f0, y[i].w * f1);
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < RB; ++i) {
-                        const int r = r0 + i;
-                        if (r >= pc.n || ch >= D) continue;
-                        const float inv = L[i] > 0.f ? 1.f / L[i] : 0.f;
-                        const int row = pc.row0 + r;
-                        const long long head = ((long long)pc.first + row / G) * a.p.n_q_heads + pc.h * G + row % G;
-                        store4<AASD_BF16>(a.o.out, head * D + ch, make_float4(o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv), a.out_vec);
-                        if (a.o.lse != nullptr && ch == 0) a.o.lse[head] = L[i] > 0.f ? (M[i] + log2f(L[i])) * (float)kLn2 : -CUDART_INF_F;
-                    }
-                }
-            }
+        // the segment that this CTA begins and others go on with: the joining kernel's work
+        if (tid == 0) {
+            KvTileOpen o{sh.open, 0};
+            if (sh.open.seg >= 0 && ok && !*abort_flag) o.parts = sh.shares.owner(sh.open.seg + sh.open.pages - 1) - c + 1;
+            a.tile_open[c] = o;
         }
         kv_clear_rows<AASD_BF16>(a, D, (int)(blockIdx.x * 8 + warp), (int)(gridDim.x * 8));
     }
+    if (!ok) give_up(abort_flag, a.state);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     if (warp == 12) tc_free(tm, 512);
+}
+
+// Joins the parts of the segments that several CTAs of the tile kernel went through: block (c, k) takes rows
+// 8 k .. of the segment that CTA c began, a warp per row.  (Left to the last CTA that delivers a part, one
+// sequence of 64k tokens with 64 new ones waited 100 us for 19 parts of 256 rows.)
+template <int D, bool PAIR>
+__global__ void __launch_bounds__(256) kv_tile_join_kernel(const KvAttendArgs a) {
+    constexpr int R = PAIR ? 2 * kTileRows : kTileRows, kPart = R * D + 2 * R;
+    pdl_launch_dependents();
+    pdl_wait();
+    const KvTileOpen open = a.tile_open[blockIdx.x];
+    const KvPiece& pc = open.piece;
+    const int r = (int)blockIdx.y * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (open.parts == 0 || r >= pc.n) return;
+    const int G = a.p.n_q_heads / a.p.n_kv_heads;
+    const float* base = a.cta_parts + (long long)blockIdx.x * 2 * kPart;   // part k: 2 k, the first one's 1
+    kv_join_row<AASD_BF16, D>(a, pc, r, base, kPart, R, open.parts, G, lane);
 }
 
 }  // namespace aasd
