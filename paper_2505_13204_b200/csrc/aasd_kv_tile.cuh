@@ -46,7 +46,7 @@ __device__ __forceinline__ int kv_tile_pages(const KvAttendArgs& a, int cached, 
     return min(pages, (int)(((unsigned int)cached + (unsigned int)(last / G) + kPage) / kPage));
 }
 // Loading the queries into tensor memory and the result out of it takes about as long as two pages.
-constexpr int kTileSegCost = 2;
+constexpr int kTileSegCost = 6;
 // Units of one head of a sequence.
 __device__ __forceinline__ long long kv_tile_head_units(const KvAttendArgs& a, const KvSeq& s, int R, int G) {
     if (s.pages == 0) return 0;
@@ -77,7 +77,7 @@ struct KvTileShared {
     uint4 vmeta[4][kPage / 4];         // per unpacking warp, four tokens each: scales of 0 and 2, 1 and 3, minima likewise
     int ev[kTileMeta];                 // exponent field that a page's values are relative to; -1: page hidden
     int raw_missing[kTileRaw];
-    float row_r[PAIR ? 2 : 1][kTileRows], row_q[PAIR ? 2 : 1][kTileRows];         // factors of the rows' queries
+    float row_q[PAIR ? 2 : 1][kTileRows];         // sums of the rows' queries
     float exchange_m[kTileRows], exchange_l[kTileRows], exchange_up[kTileRows];   // between the groups, where they share a tile
     int base[kTileThreads];
     long long scan[kTileThreads / 32];
@@ -123,8 +123,10 @@ __device__ __forceinline__ void tc_mma_ss(unsigned int d, u64 a, u64 b, unsigned
         "l"(a), "l"(b), "r"(idesc), "r"(add ? 1u : 0u)
         : "memory");
 }
-// fp32 result, fp16 operands, both K-major, M = 128
-__host__ __device__ constexpr unsigned int tc_idesc(int n) { return (1u << 4) | ((unsigned int)(n >> 3) << 17) | ((128u >> 4) << 24); }
+// fp32 result, fp16 or bf16 operands, both K-major, M = 128
+__host__ __device__ constexpr unsigned int tc_idesc(int n, bool bf16) {
+    return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | ((unsigned int)(n >> 3) << 17) | ((128u >> 4) << 24);
+}
 // Rows of 128 bytes in the 128-byte swizzle, groups of eight rows 1024 bytes apart.
 __device__ __forceinline__ u64 tc_desc(unsigned int addr) {
     return (u64)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
@@ -138,6 +140,15 @@ __device__ __forceinline__ void tc_load(unsigned int addr, float (&x)[32]) {
         : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]), "=f"(x[8]), "=f"(x[9]), "=f"(x[10]), "=f"(x[11]), "=f"(x[12]), "=f"(x[13]), "=f"(x[14]), "=f"(x[15]), "=f"(x[16]), "=f"(x[17]), "=f"(x[18]), "=f"(x[19]), "=f"(x[20]), "=f"(x[21]), "=f"(x[22]), "=f"(x[23]), "=f"(x[24]), "=f"(x[25]), "=f"(x[26]), "=f"(x[27]), "=f"(x[28]), "=f"(x[29]), "=f"(x[30]), "=f"(x[31])
         : "r"(addr) : "memory");
 }
+// ... of 32 lanes: rows g and g + 8, then g + 16 and g + 24
+__device__ __forceinline__ void tc_load(unsigned int addr, float (&x)[2][32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%64];\n\t"
+        "tcgen05.ld.sync.aligned.16x256b.x8.b32 {%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%65];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=f"(x[0][0]), "=f"(x[0][1]), "=f"(x[0][2]), "=f"(x[0][3]), "=f"(x[0][4]), "=f"(x[0][5]), "=f"(x[0][6]), "=f"(x[0][7]), "=f"(x[0][8]), "=f"(x[0][9]), "=f"(x[0][10]), "=f"(x[0][11]), "=f"(x[0][12]), "=f"(x[0][13]), "=f"(x[0][14]), "=f"(x[0][15]), "=f"(x[0][16]), "=f"(x[0][17]), "=f"(x[0][18]), "=f"(x[0][19]), "=f"(x[0][20]), "=f"(x[0][21]), "=f"(x[0][22]), "=f"(x[0][23]), "=f"(x[0][24]), "=f"(x[0][25]), "=f"(x[0][26]), "=f"(x[0][27]), "=f"(x[0][28]), "=f"(x[0][29]), "=f"(x[0][30]), "=f"(x[0][31]), "=f"(x[1][0]), "=f"(x[1][1]), "=f"(x[1][2]), "=f"(x[1][3]), "=f"(x[1][4]), "=f"(x[1][5]), "=f"(x[1][6]), "=f"(x[1][7]), "=f"(x[1][8]), "=f"(x[1][9]), "=f"(x[1][10]), "=f"(x[1][11]), "=f"(x[1][12]), "=f"(x[1][13]), "=f"(x[1][14]), "=f"(x[1][15]), "=f"(x[1][16]), "=f"(x[1][17]), "=f"(x[1][18]), "=f"(x[1][19]), "=f"(x[1][20]), "=f"(x[1][21]), "=f"(x[1][22]), "=f"(x[1][23]), "=f"(x[1][24]), "=f"(x[1][25]), "=f"(x[1][26]), "=f"(x[1][27]), "=f"(x[1][28]), "=f"(x[1][29]), "=f"(x[1][30]), "=f"(x[1][31])
+        : "r"(addr), "r"(addr + (16u << 16)) : "memory");
+}
 __device__ __forceinline__ void tc_store(unsigned int addr, const float (&x)[32]) {
     asm volatile("tcgen05.st.sync.aligned.16x256b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(addr), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]), "f"(x[8]), "f"(x[9]), "f"(x[10]), "f"(x[11]), "f"(x[12]), "f"(x[13]), "f"(x[14]), "f"(x[15]), "f"(x[16]), "f"(x[17]), "f"(x[18]), "f"(x[19]), "f"(x[20]), "f"(x[21]), "f"(x[22]), "f"(x[23]), "f"(x[24]), "f"(x[25]), "f"(x[26]), "f"(x[27]), "f"(x[28]), "f"(x[29]), "f"(x[30]), "f"(x[31]) : "memory");
 }
@@ -148,6 +159,13 @@ __device__ __forceinline__ void tc_store_cells(unsigned int addr, const unsigned
 __device__ __forceinline__ void tc_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ __half2 as_half2(unsigned int x) { return *reinterpret_cast<const __half2*>(&x); }
 // Values of two codes of a word (those in bits 0-3 and 16-19, or 4-7 and 20-23).
+// Two codes of a word as bf16 numbers: 128 + c, less 128 (both exact).
+template <bool HIGH>
+__device__ __forceinline__ unsigned int bf16_codes(unsigned int w) {
+    const unsigned int b = ((HIGH ? w >> 4 : w) & 0x000F000Fu) | 0x43004300u;
+    const __nv_bfloat162 c = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&b), __float2bfloat162_rn(128.f));
+    return *reinterpret_cast<const unsigned int*>(&c);
+}
 template <bool HIGH>
 __device__ __forceinline__ unsigned int expand(unsigned int w, __half2 scale, __half2 minimum) {
     const unsigned int b = (w & (HIGH ? 0x00F000F0u : 0x000F000Fu)) | 0x64006400u;     // 1024 + c, or 1024 + 16 c
@@ -191,7 +209,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
     using Shared = KvTileShared<D, PAIR>;
     constexpr int R = Shared::R, H = D / 2;
     constexpr unsigned int kColS = 0, kColO = 256, kStep = 128;    // first columns of group 0's S and O; group 1's are kStep behind
-    constexpr unsigned int kIdescS = tc_idesc(kPage), kIdescO = tc_idesc(D);
+    constexpr unsigned int kIdescS = tc_idesc(kPage, true), kIdescO = tc_idesc(D, false);
     extern __shared__ unsigned char smem_raw[];
     Shared& sh = *reinterpret_cast<Shared*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
     pdl_launch_dependents();
@@ -504,7 +522,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                         const unsigned int x = NW == 8 ? (part ? wd[k ^ 4] : wd[k]) : wd[k], y = x >> 8;
                         const int piece = part * NW + kk;        // of the token's H / 4
                         *reinterpret_cast<uint4*>(to + (piece >> 3) * (kPage * 128) + (((piece & 7) ^ (at & 7)) << 4)) =
-                            make_uint4(x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u);
+                            make_uint4(bf16_codes<false>(x), bf16_codes<false>(y), bf16_codes<true>(x), bf16_codes<true>(y));
                     }
                 }
                 // the values' table: lane q < 16 has tokens 4q .. 4q + 3, in the order in which their codes leave a word
@@ -564,6 +582,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
         const int x = warp >> 2, g = lane >> 2, j = lane & 3, row_base = (warp & 3) * 32;   // (of the group's 128 rows)
         const unsigned int lanes = (unsigned int)row_base << 16;
         const unsigned int col_s = tm + kColS + x * kStep + lanes, col_o = tm + kColO + x * kStep + lanes;
+        const float rf = fmaxf(a.scale_log2, 1e-37f);   // (never 0: what is hidden is -inf times it)
         int n0 = 0, taken = 0;    // pages of the share before the piece; of the group so far
         // All pages taken so far are in O.  (Not waited for with every page: a barrier for every other page keeps the
         // phases apart, since S of a page comes after O of the page two before it.)
@@ -586,8 +605,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
             const int own_row = max(min(row0 + lane, rows_here - 1), 0);   // the lane's row: what the warp wants to know of its 32 rows
             const int token = own_row / G, member = own_row - token * G;
             if (PAIR || x == 0) {
-                // The rows' queries as fp16 numbers, a row's largest element 2^14 .. 2^15, channels in the order of the
-                // keys' words; D / 8 lanes fetch a row together.
+                // The rows' queries, channels in the order of the keys' words, and their sums; D / 8 lanes fetch a row together.
                 constexpr int LR = D / 8, RI = 32 / LR;        // lanes per row, rows per step
                 const int part = lane % LR;                    // eight channels: of the low half, then of the high one
                 const long long at = ((long long)w.first + token) * a.p.q_stride + (long long)(w.h * G + member) * D;   // of the lane's row
@@ -609,44 +627,29 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                                 if (i == k) raw[i].a = slow.a;
                         }
                     }
-                    float top[8], sum[8];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        if (row0 + rb + k * RI + lane / LR >= rows_here) raw[k].clear();
-                        float2 y[4];
-                        raw[k].unpack(y);
-                        top[k] = fmaxf(fmaxf(fmaxf(fabsf(y[0].x), fabsf(y[0].y)), fmaxf(fabsf(y[1].x), fabsf(y[1].y))),
-                                       fmaxf(fmaxf(fabsf(y[2].x), fabsf(y[2].y)), fmaxf(fabsf(y[3].x), fabsf(y[3].y))));
-                        sum[k] = ((y[0].x + y[0].y) + (y[1].x + y[1].y)) + ((y[2].x + y[2].y) + (y[3].x + y[3].y));
-                    }
-#pragma unroll 1
-                    for (int o = 1; o < LR; o <<= 1)
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            top[k] = fmaxf(top[k], __shfl_xor_sync(0xFFFFFFFFu, top[k], o));
-                            sum[k] += __shfl_xor_sync(0xFFFFFFFFu, sum[k], o);
-                        }
+                    float sum[8];
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         const int r = row_base + rb + k * RI + lane / LR;
+                        if (row0 + rb + k * RI + lane / LR >= rows_here) raw[k].clear();
                         float2 y[4];
                         raw[k].unpack(y);
-                        int e = (int)(__float_as_uint(top[k]) >> 23) - 127;
-                        e = e < -100 ? -100 : e > 100 ? 100 : e;
-                        const bool high = part >= LR / 2;
-                        const float up = pow2f((high ? 10 : 14) - e);
+                        sum[k] = ((y[0].x + y[0].y) + (y[1].x + y[1].y)) + ((y[2].x + y[2].y) + (y[3].x + y[3].y));
 #pragma unroll
                         for (int q = 0; q < 2; ++q) {
                             const int piece = 2 * (part % (LR / 2)) + q;
-                            *reinterpret_cast<uint2*>(to + r * 128 + (piece >> 3) * (kTileRows * 128) + (((piece & 7) ^ (r & 7)) << 4) + (high ? 8 : 0)) =
-                                make_uint2(pack_half(y[2 * q].x * up, y[2 * q + 1].x * up), pack_half(y[2 * q].y * up, y[2 * q + 1].y * up));
-                        }
-                        if (part == 0) {
-                            // exponent (base 2) of a product = row_r * (scale * S + minimum * row_q)
-                            sh.row_r[PAIR ? x : 0][r] = fmaxf(a.scale_log2 * pow2f(e + 10), 1e-37f);   // (never 0: what is hidden is -inf times it)
-                            sh.row_q[PAIR ? x : 0][r] = sum[k] * pow2f(-10 - e);
+                            const unsigned int c01 = q ? raw[k].a.z : raw[k].a.x, c23 = q ? raw[k].a.w : raw[k].a.y;
+                            *reinterpret_cast<uint2*>(to + r * 128 + (piece >> 3) * (kTileRows * 128) + (((piece & 7) ^ (r & 7)) << 4) +
+                                                      (part >= LR / 2 ? 8 : 0)) = make_uint2(__byte_perm(c01, c23, 0x5410), __byte_perm(c01, c23, 0x7632));
                         }
                     }
+#pragma unroll
+                    for (int o = 1; o < LR; o <<= 1)
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) sum[k] += __shfl_xor_sync(0xFFFFFFFFu, sum[k], o);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (part == 0) sh.row_q[PAIR ? x : 0][row_base + rb + k * RI + lane / LR] = sum[k];
                 }
                 fence_async_smem();
                 __syncwarp();
@@ -661,14 +664,16 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                 }
             }
             if (lane == 0) mbar_arrive(&sh.q_full[x]);
-            float rf[4], qf[4], mref[4], l[4];
+            float qf[4], mref[4], l[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                rf[i] = sh.row_r[PAIR ? x : 0][row_base + g + 8 * i];
                 qf[i] = sh.row_q[PAIR ? x : 0][row_base + g + 8 * i];
                 mref[i] = kKvNothing;
                 l[i] = 0.f;
             }
+            // sixteen rows at a time are left out where the head has none of them (their probabilities are anything, and so
+            // is what becomes of them)
+            const int halves = min(2, (rows_here - row0 + 15) >> 4);
             // places up to which every row of the warp sees everything
             const int open_to = a.node_parent != nullptr ? w.cached : w.cached + row0 / G + 1;
             int ev = 64;
@@ -679,99 +684,110 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                 const unsigned int col = col_s + buf * 64;
                 ok = wait(&sh.m_full[mslot], (n / kTileMeta) & 1) && wait(&sh.s_full[x][buf], (taken >> 1) & 1);
                 if (!ok) break;
-                tc_fence_after();
-                float s[2][32];   // rows g and g + 8; g + 16 and g + 24
-                tc_load(col, s[0]);
-                tc_load(col + (16u << 16), s[1]);
-                const int evn = sh.ev[mslot];
+                if (halves > 0) {
+                    tc_fence_after();
+                    float s[2][32];   // rows g and g + 8; g + 16 and g + 24
+                    if (halves == 2) {
+                        tc_load(col, s);
+                    } else {
+                        tc_load(col, s[0]);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float4 m = sh.kmeta[mslot][4 * k + j];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {   // row g + 8 q
-                        float& s0 = s[q >> 1][4 * k + 2 * (q & 1)];
-                        float& s1 = s[q >> 1][4 * k + 2 * (q & 1) + 1];
-                        const float2 y = __ffma2_rn(make_float2(m.z, m.w), make_float2(qf[q], qf[q]), __fmul2_rn(make_float2(s0, s1), make_float2(m.x, m.y)));
-                        s0 = y.x;
-                        s1 = y.y;
+                        for (int k = 0; k < 32; ++k) s[1][k] = 0.f;
                     }
-                }
-                if (evn < 0 || (pg + 1) * kPage > open_to) {   // what a row does not see becomes -inf (lane r finds out for row r)
-                    const u64 mine = evn < 0 || row0 + lane >= rows_here ? 0ull : tile_places(kv_seen(a, w.cached, w.fresh, w.first, pg, token));
+                    const int evn = sh.ev[mslot];
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const u64 seen = __shfl_sync(0xFFFFFFFFu, mine, g + 8 * q) >> (2 * j);
+                    for (int k = 0; k < 8; ++k) {
+                        const float4 m = sh.kmeta[mslot][4 * k + j];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const unsigned int two = (unsigned int)(seen >> (8 * k));
-                            if (!(two & 1u)) s[q >> 1][4 * k + 2 * (q & 1)] = -CUDART_INF_F;
-                            if (!(two & 2u)) s[q >> 1][4 * k + 2 * (q & 1) + 1] = -CUDART_INF_F;
+                        for (int q = 0; q < 4; ++q) {   // row g + 8 q
+                            float& s0 = s[q >> 1][4 * k + 2 * (q & 1)];
+                            float& s1 = s[q >> 1][4 * k + 2 * (q & 1) + 1];
+                            const float2 y = __ffma2_rn(make_float2(m.z, m.w), make_float2(qf[q], qf[q]), __fmul2_rn(make_float2(s0, s1), make_float2(m.x, m.y)));
+                            s0 = y.x;
+                            s1 = y.y;
                         }
                     }
-                }
-                // Probabilities with the maximum as it stands; only where a thread's sum of them leaves fp16's range (by a
-                // new maximum at least 2^5 above it), and on the first page, is the maximum looked for and this done again.
-                float ls[4];
-                bool again = first;
-#pragma unroll 1
-                for (;;) {
-                    if (again) {
-                        float fo[4];
+                    if (evn < 0 || (pg + 1) * kPage > open_to) {   // what a row does not see becomes -inf (lane r finds out for row r)
+                        const u64 mine = evn < 0 || row0 + lane >= rows_here ? 0ull : tile_places(kv_seen(a, w.cached, w.fresh, w.first, pg, token));
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
-                            float m = -CUDART_INF_F;
+                            const u64 seen = __shfl_sync(0xFFFFFFFFu, mine, g + 8 * q) >> (2 * j);
 #pragma unroll
-                            for (int k = 0; k < 8; ++k) m = fmaxf(m, fmaxf(s[q >> 1][4 * k + 2 * (q & 1)], s[q >> 1][4 * k + 2 * (q & 1) + 1]));
-                            m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-                            m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-                            const float mn = fmaxf(mref[q], m * rf[q]);
-                            fo[q] = ex2_approx(mref[q] - mn);
-                            mref[q] = mn;
-                            l[q] *= fo[q];
+                            for (int k = 0; k < 8; ++k) {
+                                const unsigned int two = (unsigned int)(seen >> (8 * k));
+                                if (!(two & 1u)) s[q >> 1][4 * k + 2 * (q & 1)] = -CUDART_INF_F;
+                                if (!(two & 2u)) s[q >> 1][4 * k + 2 * (q & 1) + 1] = -CUDART_INF_F;
+                            }
                         }
+                    }
+                    // Probabilities with the maximum as it stands; only where a thread's sum of them leaves fp16's range (by a
+                    // new maximum at least 2^5 above it), and on the first page, is the maximum looked for and this done again.
+                    float ls[4];
+                    bool again = first;
+#pragma unroll 1
+                    for (;;) {
+                        if (again) {
+                            float fo[4];
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                float m = -CUDART_INF_F;
+#pragma unroll
+                                for (int k = 0; k < 8; ++k) m = fmaxf(m, fmaxf(s[q >> 1][4 * k + 2 * (q & 1)], s[q >> 1][4 * k + 2 * (q & 1) + 1]));
+                                m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+                                m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+                                const float mn = fmaxf(mref[q], m * rf);
+                                fo[q] = ex2_approx(mref[q] - mn);
+                                mref[q] = mn;
+                                l[q] *= fo[q];
+                            }
+                            if (!first) {
+                                ok = o_complete();
+                                if (!ok) break;
+                                tile_scale_o<D>(col_o, fo);
+                            }
+                        }
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            if (half >= halves) {
+                                ls[2] = ls[3] = 0.f;
+                                break;
+                            }
+                            unsigned int pk[16];
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const int q = 2 * half + e;
+                                const float2 ff = make_float2(rf, rf), mm = make_float2(kTileP - mref[q], kTileP - mref[q]);
+                                float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+                                for (int k = 0; k < 8; ++k) {
+                                    float2 p = __ffma2_rn(make_float2(s[half][4 * k + 2 * e], s[half][4 * k + 2 * e + 1]), ff, mm);
+                                    p = make_float2(ex2_approx(p.x), ex2_approx(p.y));
+                                    sum = __fadd2_rn(sum, p);
+                                    pk[2 * k + e] = pack_half(p.x, p.y);
+                                }
+                                ls[q] = sum.x + sum.y;
+                            }
+                            tc_store_cells(col + ((unsigned int)(16 * half) << 16), pk);
+                        }
+                        if (again || __all_sync(0xFFFFFFFFu, fmaxf(fmaxf(ls[0], ls[1]), fmaxf(ls[2], ls[3])) < 65504.f)) break;
+                        again = true;
+                    }
+                    if (!ok) break;
+                    if (evn > ev) {
+                        // values of this page are relative to a larger exponent than O
                         if (!first) {
                             ok = o_complete();
                             if (!ok) break;
+                            const float f = evn - ev > 126 ? 0.f : pow2f(ev - evn);
+                            const float fo[4] = {f, f, f, f};
                             tile_scale_o<D>(col_o, fo);
                         }
+                        ev = evn;
                     }
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        unsigned int pk[16];
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const int q = 2 * half + e;
-                            const float2 ff = make_float2(rf[q], rf[q]), mm = make_float2(kTileP - mref[q], kTileP - mref[q]);
-                            float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) {
-                                float2 p = __ffma2_rn(make_float2(s[half][4 * k + 2 * e], s[half][4 * k + 2 * e + 1]), ff, mm);
-                                p = make_float2(ex2_approx(p.x), ex2_approx(p.y));
-                                sum = __fadd2_rn(sum, p);
-                                pk[2 * k + e] = pack_half(p.x, p.y);
-                            }
-                            ls[q] = sum.x + sum.y;
-                        }
-                        tc_store_cells(col + ((unsigned int)(16 * half) << 16), pk);
-                    }
-                    if (again || __all_sync(0xFFFFFFFFu, fmaxf(fmaxf(ls[0], ls[1]), fmaxf(ls[2], ls[3])) < 65504.f)) break;
-                    again = true;
-                }
-                if (!ok) break;
-                if (evn > ev) {
-                    // values of this page are relative to a larger exponent than O
-                    if (!first) {
-                        ok = o_complete();
-                        if (!ok) break;
-                        const float f = evn - ev > 126 ? 0.f : pow2f(ev - evn);
-                        const float fo[4] = {f, f, f, f};
-                        tile_scale_o<D>(col_o, fo);
-                    }
-                    ev = evn;
+                    for (int q = 0; q < 4; ++q) l[q] += ls[q];
                 }
                 first = false;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) l[q] += ls[q];
                 ++taken;
                 tc_wait_store();
                 tc_fence_before();
