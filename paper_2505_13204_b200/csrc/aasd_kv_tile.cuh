@@ -86,8 +86,8 @@ struct KvTileShared {
     KvPiece open;                      // the segment that begins in this CTA and ends in another
     u64 piece_full[kTilePieces], piece_empty[kTilePieces];
     u64 raw_full[kTileRaw], raw_empty[kTileRaw];
-    u64 k_full[kTileKeys], k_empty[kTileKeys], v_full[kTileValues], v_empty[kTileValues];
-    u64 m_full[kTileMeta], m_empty[kTileMeta];
+    u64 full[kTileMeta];               // a page is unpacked: keys, values and their scales
+    u64 k_empty[kTileKeys], v_empty[kTileValues], m_empty[kTileMeta];
     u64 q_full[2], s_full[2][2], p_full[2][2], o_done[2][2], x_full, x_empty, r_full, drain[2];
     unsigned int tmem;
     int abort_flag;
@@ -227,17 +227,15 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
         }
 #pragma unroll 1
         for (int i = 0; i < kTileKeys; ++i) {
-            mbar_init(&sh.k_full[i], 4);
             mbar_init(&sh.k_empty[i], PAIR ? 2 : 1);
         }
 #pragma unroll 1
         for (int i = 0; i < kTileValues; ++i) {
-            mbar_init(&sh.v_full[i], 4);
             mbar_init(&sh.v_empty[i], PAIR ? 2 : 1);
         }
 #pragma unroll 1
         for (int i = 0; i < kTileMeta; ++i) {
-            mbar_init(&sh.m_full[i], 4);
+            mbar_init(&sh.full[i], 4);
             mbar_init(&sh.m_empty[i], PAIR ? 8 : 4);
         }
 #pragma unroll 1
@@ -286,7 +284,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
         return false;
     };
     // (the lanes of a warp go on, or give up, together)
-    const auto wait = [&](u64* bar, unsigned int parity) { return __all_sync(0xFFFFFFFFu, wait_one(bar, parity)) != 0; };
+    const auto together = [](bool on) { return __all_sync(0xFFFFFFFFu, on) != 0; };
+    const auto wait = [&](u64* bar, unsigned int parity) { return together(wait_one(bar, parity)); };
     bool ok = true;
 
     if (warp >= 12) {
@@ -430,7 +429,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
 #pragma unroll 1
                         for (; ahead < np && asked < taken + 2; ahead += step, ++asked) {
                             const int n = n0 + ahead, slot = n % kTileKeys, buf = asked & 1;
-                            ok = wait_one(&sh.k_full[slot], (n / kTileKeys) & 1);
+                            ok = wait_one(&sh.full[n % kTileMeta], (n / kTileMeta) & 1);
                             if (!ok) break;
                             tc_fence_after();
                             const u64 keys = tc_desc(smem_u32(sh.keys[slot]));
@@ -442,7 +441,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                             tc_commit(&sh.k_empty[slot]);
                         }
                         const int n = n0 + i, slot = n % kTileValues, buf = taken & 1;
-                        ok = ok && wait_one(&sh.v_full[slot], (n / kTileValues) & 1) && wait_one(&sh.p_full[x][buf], (taken >> 1) & 1);
+                        ok = ok && wait_one(&sh.p_full[x][buf], (taken >> 1) & 1);   // (the page's values came with its keys)
                         if (!ok) break;
                         tc_fence_after();
                         const u64 v = tc_desc(smem_u32(sh.values[slot]));
@@ -480,21 +479,47 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
 #pragma unroll 1
             for (int i = 0; i < np; ++i, ++n) {
                 const int slot = n % kTileRaw, mslot = n % kTileMeta, kslot = n % kTileKeys, vslot = n % kTileValues;
-                ok = wait(&sh.raw_full[slot], (n / kTileRaw) & 1) && wait(&sh.m_empty[mslot], ((n / kTileMeta) & 1) ^ 1) &&
-                     wait(&sh.k_empty[kslot], ((n / kTileKeys) & 1) ^ 1);
+                ok = together(wait_one(&sh.raw_full[slot], (n / kTileRaw) & 1) && wait_one(&sh.k_empty[kslot], ((n / kTileKeys) & 1) ^ 1) &&
+                              wait_one(&sh.v_empty[vslot], ((n / kTileValues) & 1) ^ 1) && wait_one(&sh.m_empty[mslot], ((n / kTileMeta) & 1) ^ 1));
                 if (!ok) break;
                 const unsigned char* raw = sh.raw[slot];
                 const bool missing = sh.raw_missing[slot] != 0;
                 const int left = missing ? 0 : end - i * kPage;   // places in use
-                // largest value of the page (every warp for itself): codes run from the minimum to 15 scales above it
+                // Everything is fetched first.  Keys: half a token's row per thread (word k of a token: channels 4k .. of each
+                // half).  Values: a channel's 64 codes, and those of the channel H above it, per TPR threads.
+                constexpr int NW = H / 8;                        // words of keys per thread
+                constexpr int TPR = 128 / H, NP = 8 / TPR;       // threads per row of values; 16-byte pieces per thread and half
+                const int t = u >> 1, khalf = u & 1, r = u / TPR, vpart = u % TPR;
+                unsigned int kw[NW], vw[2 * NP];
                 const uint2 vm = *reinterpret_cast<const uint2*>(raw + kv_value_meta_offset(D) + 8 * lane);
+                const uint4 four = lds16(raw + kv_value_meta_offset(D) + 16 * (lane & 15));
+                const unsigned int key_meta = *reinterpret_cast<const unsigned int*>(raw + kv_key_meta_offset(D) + 4 * (u & (kPage - 1)));
+#pragma unroll
+                for (int k = 0; k < NW; k += 4) {
+                    const uint4 q = lds16(raw + t * H + khalf * (H / 2) + 4 * k);
+                    kw[k] = q.x; kw[k + 1] = q.y; kw[k + 2] = q.z; kw[k + 3] = q.w;
+                }
+#pragma unroll
+                for (int k = 0; k < 2 * NP; k += 4) {
+                    const uint4 q = lds16(raw + kv_value_offset(D) + r * kPage + vpart * (kPage / TPR) + 4 * k);
+                    vw[k] = q.x; vw[k + 1] = q.y; vw[k + 2] = q.z; vw[k + 3] = q.w;
+                }
+                // largest value of the page (every warp for itself): codes run from the minimum to 15 scales above it
                 auto reach = [](unsigned int m) { return fmaxf(fabsf(meta_min(m)), fabsf(fmaf(15.f, meta_scale(m), meta_min(m)))); };
                 float vt = 2 * lane < left ? reach(vm.x) : 0.f;
                 if (2 * lane + 1 < left) vt = fmaxf(vt, reach(vm.y));
                 // (an exponent field, held to a range in which the factors below are normal numbers)
                 ev = max(ev, min(250, (int)(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(vt)) >> 23)));
+                // the values' table: lane q < 16 has tokens 4q .. 4q + 3, in the order in which their codes leave a word
+                if (lane < kPage / 4) {
+                    const float norm = pow2f(127 - ev);
+                    const unsigned int m0 = 4 * lane < left ? four.x : 0u, m1 = 4 * lane + 1 < left ? four.y : 0u,
+                                       m2 = 4 * lane + 2 < left ? four.z : 0u, m3 = 4 * lane + 3 < left ? four.w : 0u;
+                    sh.vmeta[uw][lane] = make_uint4(pack_half(meta_scale(m0) * norm, meta_scale(m2) * norm), pack_half(meta_scale(m1) * norm, meta_scale(m3) * norm),
+                                                    pack_half(meta_min(m0) * norm, meta_min(m2) * norm), pack_half(meta_min(m1) * norm, meta_min(m3) * norm));
+                }
                 if (u < kPage) {
-                    const unsigned int km = u < left ? *reinterpret_cast<const unsigned int*>(raw + kv_key_meta_offset(D) + 4 * u) : 0u;
+                    const unsigned int km = u < left ? key_meta : 0u;
                     const int at = tile_place(u);
                     float* kq = reinterpret_cast<float*>(&sh.kmeta[mslot][at >> 1]);
                     kq[at & 1] = meta_scale(km);
@@ -502,66 +527,30 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                     if (u == 0) sh.ev[mslot] = missing ? -1 : ev;
                 }
                 {
-                    // keys: half a token's row per thread.  Word k of a token (channels 4k .. of each half) becomes
-                    // 16-byte piece k of its row; the two threads of a token take their pieces in orders that keep
-                    // eight neighbouring threads on eight different pieces.
-                    constexpr int NW = H / 8;                       // words per thread: a token's H / 4, halved
-                    const int t = u >> 1, part = u & 1;
-                    const unsigned char* from = raw + t * H + part * (H / 2);
-                    unsigned int wd[NW];
-#pragma unroll
-                    for (int k = 0; k < NW; k += 4) {
-                        const uint4 q = lds16(from + 4 * k);
-                        wd[k] = q.x; wd[k + 1] = q.y; wd[k + 2] = q.z; wd[k + 3] = q.w;
-                    }
+                    // Keys: word k becomes 16-byte piece k of the token's row; the two threads of a token take their pieces
+                    // in orders that keep eight neighbouring threads on eight different pieces.
                     const int at = tile_place(t);
                     unsigned char* to = sh.keys[kslot] + at * 128;
 #pragma unroll
                     for (int k = 0; k < NW; ++k) {
-                        const int kk = NW == 8 ? k ^ (part * 4) : k;
-                        const unsigned int x = NW == 8 ? (part ? wd[k ^ 4] : wd[k]) : wd[k], y = x >> 8;
-                        const int piece = part * NW + kk;        // of the token's H / 4
+                        const int kk = NW == 8 ? k ^ (khalf * 4) : k;
+                        const unsigned int x = NW == 8 ? (khalf ? kw[k ^ 4] : kw[k]) : kw[k], y = x >> 8;
+                        const int piece = khalf * NW + kk;       // of the token's H / 4
                         *reinterpret_cast<uint4*>(to + (piece >> 3) * (kPage * 128) + (((piece & 7) ^ (at & 7)) << 4)) =
                             make_uint4(bf16_codes<false>(x), bf16_codes<false>(y), bf16_codes<true>(x), bf16_codes<true>(y));
                     }
                 }
-                // the values' table: lane q < 16 has tokens 4q .. 4q + 3, in the order in which their codes leave a word
-                const float norm = pow2f(127 - ev);
-                if (lane < kPage / 4) {
-                    const uint4 m = lds16(raw + kv_value_meta_offset(D) + 16 * lane);
-                    const unsigned int m0 = 4 * lane < left ? m.x : 0u, m1 = 4 * lane + 1 < left ? m.y : 0u, m2 = 4 * lane + 2 < left ? m.z : 0u,
-                                       m3 = 4 * lane + 3 < left ? m.w : 0u;
-                    sh.vmeta[uw][lane] = make_uint4(pack_half(meta_scale(m0) * norm, meta_scale(m2) * norm), pack_half(meta_scale(m1) * norm, meta_scale(m3) * norm),
-                                                    pack_half(meta_min(m0) * norm, meta_min(m2) * norm), pack_half(meta_min(m1) * norm, meta_min(m3) * norm));
-                }
-                fence_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(&sh.k_full[kslot]);
-                    mbar_arrive(&sh.m_full[mslot]);
-                }
-                // values: rows of channels; 8 tokens of a channel are a 16-byte piece
-                ok = wait(&sh.v_empty[vslot], ((n / kTileValues) & 1) ^ 1);
-                if (!ok) break;
-                constexpr int TPR = 128 / H;                 // threads per channel-pair row
-                constexpr int NP = 8 / TPR;                  // pieces per thread and half
-                const int r = u / TPR, part = u % TPR;
-                const unsigned char* from = raw + kv_value_offset(D) + r * kPage + part * (kPage / TPR);
-                unsigned int wd[2 * NP];
-#pragma unroll
-                for (int k = 0; k < 2 * NP; k += 4) {
-                    const uint4 q = lds16(from + 4 * k);
-                    wd[k] = q.x; wd[k + 1] = q.y; wd[k + 2] = q.z; wd[k + 3] = q.w;
-                }
+                __syncwarp();   // (the table)
+                // values: 8 tokens of a channel are a 16-byte piece
                 unsigned char* lo = sh.values[vslot] + r * 128;
                 unsigned char* hi = lo + H * 128;            // (H is a multiple of 8: the same swizzle)
 #pragma unroll
                 for (int k = 0; k < NP; ++k) {
-                    const unsigned int x0 = wd[2 * k], x1 = wd[2 * k + 1], y0 = x0 >> 8, y1 = x1 >> 8;
-                    const uint4 q0 = sh.vmeta[uw][2 * (part * NP + k)], q1 = sh.vmeta[uw][2 * (part * NP + k) + 1];
+                    const unsigned int x0 = vw[2 * k], x1 = vw[2 * k + 1], y0 = x0 >> 8, y1 = x1 >> 8;
+                    const uint4 q0 = sh.vmeta[uw][2 * (vpart * NP + k)], q1 = sh.vmeta[uw][2 * (vpart * NP + k) + 1];
                     const __half2 s0 = as_half2(q0.x), s1 = as_half2(q0.y), m0 = as_half2(q0.z), m1 = as_half2(q0.w);
                     const __half2 s2 = as_half2(q1.x), s3 = as_half2(q1.y), m2 = as_half2(q1.z), m3 = as_half2(q1.w);
-                    const int at = ((part * NP + k) ^ (r & 7)) << 4;
+                    const int at = ((vpart * NP + k) ^ (r & 7)) << 4;
                     *reinterpret_cast<uint4*>(lo + at) =
                         make_uint4(expand<false>(x0, s0, m0), expand<false>(y0, s1, m1), expand<false>(x1, s2, m2), expand<false>(y1, s3, m3));
                     *reinterpret_cast<uint4*>(hi + at) =
@@ -570,7 +559,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                    mbar_arrive(&sh.v_full[vslot]);
+                    mbar_arrive(&sh.full[mslot]);
                     mbar_arrive(&sh.raw_empty[slot]);
                 }
             }
@@ -682,7 +671,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
             for (int i = PAIR ? 0 : (n0 ^ x) & 1; i < np; i += PAIR ? 1 : 2) {
                 const int n = n0 + i, mslot = n % kTileMeta, pg = w.pg + i, buf = taken & 1;
                 const unsigned int col = col_s + buf * 64;
-                ok = wait(&sh.m_full[mslot], (n / kTileMeta) & 1) && wait(&sh.s_full[x][buf], (taken >> 1) & 1);
+                ok = together(wait_one(&sh.full[mslot], (n / kTileMeta) & 1) && wait_one(&sh.s_full[x][buf], (taken >> 1) & 1));
                 if (!ok) break;
                 if (halves > 0) {
                     tc_fence_after();
