@@ -26,14 +26,13 @@ void with_type(int dtype, F&& f) {
     else f(std::integral_constant<int, AASD_BF16>());
 }
 
-// Token rows up to which the planning CTA writes the token arrays itself (a second launch costs
-// about 2 us; one CTA places 256 tokens per 0.6 us).
+// Token rows up to which the planning CTA writes the token arrays itself, and from which a second launch
+// does: 256 tokens 3.3 us inline and 7.3 us in two launches, 1024 tokens 5.0 and 7.1, 2048 tokens 7.4 and 6.2, 4096 tokens
+// 11.8 and 6.1.
 constexpr int64_t kInlineTokens = 1024;
-// Threads from which the lanes of a query or key row go through four rows of a token: with fewer, one
-// row each (and four times the CTAs) fills the machine better.
-constexpr int64_t kManyRowThreads = 1 << 18;
-// Sequences up to which the planning CTA has 256 threads: its scans cost a barrier per warp.
-constexpr int kPlanManySeqs = 64;
+// Sequences up to which the planning CTA has 256 threads, one for each: its scans cost a barrier per warp (4 to
+// 256 sequences take 3.5 us with them and 8.2 us with 1024 threads; 300 sequences, a second round for the 256, 22.6 and 8.6).
+constexpr int kPlanManySeqs = 256;
 
 }  // namespace
 
@@ -99,20 +98,17 @@ int aasd_kv_write(aasd_ctx* ctx, const void* q, const void* k, const void* v, co
     const int lanes = D / 16;
     const int64_t rows = n_tokens * (hq + hkv);
     const bool full = p->rotary_dim == D && !(p->flags & AASD_KV_ROPE_INTERLEAVED);
-    const bool sets = vec && full && rows * lanes >= kManyRowThreads;
-    const int64_t groups = sets ? n_tokens * ((hq + hkv + 3) / 4) : rows;
     const int64_t value_blocks = (n_tokens + kValueTokens - 1) / kValueTokens * hkv;
-    const int64_t blocks = value_blocks + (groups * lanes + kWriteThreads - 1) / kWriteThreads;
+    const int64_t blocks = value_blocks + (rows * lanes + kWriteThreads - 1) / kWriteThreads;
     if (blocks > 0x7FFFFFFFLL) return AASD_ERR_BAD_SHAPE;
     a.value_blocks = (unsigned int)value_blocks;
     AASD_CUDA(cudaSetDevice(ctx->device));
     with_type(p->dtype, [&](auto dt) {
         with_dim(D, [&](auto d) {
             auto go = [&](auto kernel) { launch(kernel, (unsigned int)blocks, (unsigned int)kWriteThreads, 0, ctx->stream, a); };
-            if (sets) go(kv_write_kernel<dt(), d(), true, 4, true>);
-            else if (vec && full) go(kv_write_kernel<dt(), d(), true, 1, true>);
-            else if (vec) go(kv_write_kernel<dt(), d(), true, 1, false>);
-            else go(kv_write_kernel<dt(), d(), false, 1, false>);
+            if (vec && full) go(kv_write_kernel<dt(), d(), true, true>);
+            else if (vec) go(kv_write_kernel<dt(), d(), true, false>);
+            else go(kv_write_kernel<dt(), d(), false, false>);
         });
     });
     return after_launch(ctx, 1);

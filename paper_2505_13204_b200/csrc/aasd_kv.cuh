@@ -218,7 +218,7 @@ __device__ __forceinline__ void kv_place_token(const KvPlanArgs& a, int64_t t, i
 }
 
 #ifdef AASD_KV_TU
-constexpr int kPlanThreads = 256, kPlanThreadsMany = 1024;   // of batches up to 64 sequences, and larger ones
+constexpr int kPlanThreads = 256, kPlanThreadsMany = 1024;   // of batches up to 256 sequences, and larger ones
 
 // One CTA: the books of all sequences (NT at a time) by prefix sums, the pages moved
 // by all threads together (a thread finds its page's sequence by bisection of the sums), so one
@@ -434,9 +434,10 @@ struct KvWriteArgs {
 // A CTA either takes query and key rows or stores values; both kinds share the launch.
 //
 // Query and key rows: D / 16 lanes share a row, a lane holds eight channels of each half, so that both
-// members of a rotated pair, and both halves of a stored byte, are its own.  The lanes stay with
-// one token for up to HP of its heads, whose loads are under way together and which share the
-// cosines and weights.  The norm's sum follows the order of the definition: halves, then
+// members of a rotated pair, and both halves of a stored byte, are its own.  One row each: four rows of
+// a token per lane, with the cosines, weights and a reciprocal root shared, were slower at every size
+// (64 tokens 4.6 us instead of 2.7, 512 tokens 7.0 instead of 6.3, 4096 tokens 34.4 instead of 30.0; 32 query and 8 key
+// heads of 128 channels).  The norm's sum follows the order of the definition: halves, then
 // neighbours (three steps inside the lane, the others across lanes by butterfly; a sum does not
 // ask which operand is first), each operation rounded by itself.
 //
@@ -488,7 +489,7 @@ __device__ __forceinline__ KvQuant kv_row_quantiser(const float2 (&x)[4], const 
 }
 
 // FULL: all D channels are rotated, in halves (the usual form); otherwise whatever the parameters say.
-template <int DT, int D, bool VEC, int HP, bool FULL>
+template <int DT, int D, bool VEC, bool FULL>
 __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteArgs a) {
     constexpr int L = D / 16;              // lanes of a row
     constexpr int H = D / 2;
@@ -555,34 +556,26 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteAr
     // ---- queries and keys
     float* s_rows = reinterpret_cast<float*>(s_mem);
     const int heads = hq + hkv;
-    const int sets = (heads + HP - 1) / HP;                 // sets of HP rows of a token
     const int64_t g = ((int64_t)(blockIdx.x - a.value_blocks) * kWriteThreads + threadIdx.x) / L;
-    const bool live = g < a.n_tokens * sets;
-    const int64_t t = live ? g / sets : 0;
-    const int h0 = live ? (int)(g - t * sets) * HP : 0;
-    // (the rows do not wait for their token's position)
-    Raw8<DT, VEC> rx[HP], ry[HP];   // channels 8l .. and D/2 + 8l ..
-#pragma unroll
-    for (int i = 0; i < HP; ++i) {
-        const int h = h0 + i;
-        rx[i].clear();
-        ry[i].clear();
-        if (live && h < heads) {
-            const void* src = h < hq ? a.q : a.k;
-            const int64_t at = h < hq ? t * a.p.q_stride + (int64_t)h * D + 8 * l : t * a.p.k_stride + (int64_t)(h - hq) * D + 8 * l;
-            rx[i].load(src, at);
-            ry[i].load(src, at + H);
-        }
+    const bool live = g < a.n_tokens * heads;
+    const int64_t t = live ? g / heads : 0;
+    const int h = live ? (int)(g - t * heads) : 0;
+    // (the row does not wait for its token's position)
+    Raw8<DT, VEC> rx, ry;           // channels 8l .. and D/2 + 8l ..
+    rx.clear();
+    ry.clear();
+    if (live) {
+        const void* src = h < hq ? a.q : a.k;
+        const int64_t at = h < hq ? t * a.p.q_stride + (int64_t)h * D + 8 * l : t * a.p.k_stride + (int64_t)(h - hq) * D + 8 * l;
+        rx.load(src, at);
+        ry.load(src, at + H);
     }
     int pos = AASD_NONE, slot = AASD_NONE;
     if (live) bits |= kv_write_token(a, t, hkv > 0, pos, slot);
     const bool used = live && pos != AASD_NONE;
     if (!used) {
-#pragma unroll
-        for (int i = 0; i < HP; ++i) {
-            rx[i].clear();
-            ry[i].clear();
-        }
+        rx.clear();
+        ry.clear();
     }
     // cosines and sines of the lane's pairs (the branches on the form of the rotation are the same for every lane)
     const int rot = FULL ? D : a.p.rotary_dim, half = rot / 2;
@@ -609,49 +602,30 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteAr
             load8<AASD_F32, VEC>(cs, half + 8 * l, si);
         }
     }
-    // 1 / sqrt(mean square + eps): the sums of all HP rows, then lane i of a row's lanes has row i's factor
-    float factor = 0.f;
+    const bool key = h >= hq;
+    float2 u[4], v[4];
+    rx.unpack(u);
+    ry.unpack(v);
+    // (the lanes of a row take the same way; shuffles stay among all lanes of the warp)
     if (a.q_weight != nullptr || a.k_weight != nullptr) {
-        float own = 0.f;
+        float s[4];
 #pragma unroll
-        for (int i = 0; i < HP; ++i) {
-            float2 u[4], v[4];
-            rx[i].unpack(u);
-            ry[i].unpack(v);
-            float s[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float2 q = __fadd2_rn(__fmul2_rn(u[e], u[e]), __fmul2_rn(v[e], v[e]));
-                s[e] = __fadd_rn(q.x, q.y);
-            }
-            float sum = __fadd_rn(__fadd_rn(s[0], s[1]), __fadd_rn(s[2], s[3]));
-#pragma unroll
-            for (int o = 1; o < L; o <<= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xFFFFFFFFu, sum, o));
-            if (l % HP == i) own = sum;
+        for (int e = 0; e < 4; ++e) {
+            const float2 q = __fadd2_rn(__fmul2_rn(u[e], u[e]), __fmul2_rn(v[e], v[e]));
+            s[e] = __fadd_rn(q.x, q.y);
         }
-        factor = __frcp_rn(__fsqrt_rn(__fadd_rn(__fmul_rn(own, 1.0f / D), a.p.eps)));
-    }
-    float2 wx[4], wy[4];
-    const void* held = nullptr;    // the weight that wx, wy hold
+        float sum = __fadd_rn(__fadd_rn(s[0], s[1]), __fadd_rn(s[2], s[3]));
 #pragma unroll
-    for (int i = 0; i < HP; ++i) {
-        const int h = h0 + i;
-        const bool row = used && h < heads, key = h >= hq;
+        for (int o = 1; o < L; o <<= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xFFFFFFFFu, sum, o));
+        const float r = __frcp_rn(__fsqrt_rn(__fadd_rn(__fmul_rn(sum, 1.0f / D), a.p.eps)));
         const void* w = key ? a.k_weight : a.q_weight;
-        float2 u[4], v[4];
-        rx[i].unpack(u);
-        ry[i].unpack(v);
-        // (the lanes of a row take the same way; shuffles stay among all lanes of the warp)
-        const float r = __shfl_sync(0xFFFFFFFFu, factor, i, HP < L ? HP : L);
-        if (row && w != nullptr) {
-            if (w != held) {
-                held = w;
-                Raw8<DT, VEC> g;
-                g.load(w, 8 * l);
-                g.unpack(wx);
-                g.load(w, H + 8 * l);
-                g.unpack(wy);
-            }
+        if (used && w != nullptr) {
+            Raw8<DT, VEC> g;
+            float2 wx[4], wy[4];
+            g.load(w, 8 * l);
+            g.unpack(wx);
+            g.load(w, H + 8 * l);
+            g.unpack(wy);
             const float2 rr = make_float2(r, r);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -659,66 +633,67 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteAr
                 v[e] = __fmul2_rn(__fmul2_rn(v[e], rr), wy[e]);
             }
         }
-        // (a - b is written a + (-b): the same rounding)
-        if (!FULL && rot > 0 && neighbours) {
+    }
+    // (a - b is written a + (-b): the same rounding)
+    if (!FULL && rot > 0 && neighbours) {
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            float2(&z)[4] = part ? v : u;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (part * H + 8 * l + 2 * e < rot) {
+                    const float c = co[4 * part + e], n = si[4 * part + e];
+                    z[e] = __fadd2_rn(__fmul2_rn(z[e], make_float2(c, c)), __fmul2_rn(make_float2(z[e].y, z[e].x), make_float2(-n, n)));
+                }
+            }
+        }
+    } else if (FULL || rot == D) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 c = make_float2(co[2 * e], co[2 * e + 1]), n = make_float2(si[2 * e], si[2 * e + 1]);
+            const float2 p = u[e], q = v[e];
+            u[e] = __fadd2_rn(__fmul2_rn(p, c), __fmul2_rn(q, make_float2(-n.x, -n.y)));
+            v[e] = __fadd2_rn(__fmul2_rn(q, c), __fmul2_rn(p, n));
+        }
+    } else if (!FULL && rot > 0) {
+        // a pair (c, c + half) inside the first rot channels: its members may be different lanes',
+        // so the warp's rows pass through shared memory (partial rotation is the rare case)
+        float* mine = s_rows + group * D;
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            *reinterpret_cast<float2*>(mine + 8 * l + 2 * e) = u[e];
+            *reinterpret_cast<float2*>(mine + H + 8 * l + 2 * e) = v[e];
+        }
+        __syncwarp();
+        if (used) {
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
                 float2(&z)[4] = part ? v : u;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (part * H + 8 * l + 2 * e < rot) {
-                        const float c = co[4 * part + e], n = si[4 * part + e];
-                        z[e] = __fadd2_rn(__fmul2_rn(z[e], make_float2(c, c)), __fmul2_rn(make_float2(z[e].y, z[e].x), make_float2(-n, n)));
-                    }
-                }
-            }
-        } else if (FULL || rot == D) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float2 c = make_float2(co[2 * e], co[2 * e + 1]), n = make_float2(si[2 * e], si[2 * e + 1]);
-                const float2 p = u[e], q = v[e];
-                u[e] = __fadd2_rn(__fmul2_rn(p, c), __fmul2_rn(q, make_float2(-n.x, -n.y)));
-                v[e] = __fadd2_rn(__fmul2_rn(q, c), __fmul2_rn(p, n));
-            }
-        } else if (!FULL && rot > 0) {
-            // a pair (c, c + half) inside the first rot channels: its members may be different lanes',
-            // so the warp's rows pass through shared memory (partial rotation is the rare case)
-            float* mine = s_rows + group * D;
-            __syncwarp();
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                *reinterpret_cast<float2*>(mine + 8 * l + 2 * e) = u[e];
-                *reinterpret_cast<float2*>(mine + H + 8 * l + 2 * e) = v[e];
-            }
-            __syncwarp();
-            if (row) {
-#pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    float2(&z)[4] = part ? v : u;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        float& x = e & 1 ? z[e >> 1].y : z[e >> 1].x;
-                        const int c = part * H + 8 * l + e;
-                        if (c < half) x = __fsub_rn(__fmul_rn(x, cs[c]), __fmul_rn(mine[c + half], cs[half + c]));
-                        else if (c < rot) x = __fadd_rn(__fmul_rn(x, cs[c - half]), __fmul_rn(mine[c - half], cs[c]));
-                    }
+                for (int e = 0; e < 8; ++e) {
+                    float& x = e & 1 ? z[e >> 1].y : z[e >> 1].x;
+                    const int c = part * H + 8 * l + e;
+                    if (c < half) x = __fsub_rn(__fmul_rn(x, cs[c]), __fmul_rn(mine[c + half], cs[half + c]));
+                    else if (c < rot) x = __fadd_rn(__fmul_rn(x, cs[c - half]), __fmul_rn(mine[c - half], cs[c]));
                 }
             }
         }
-        if (live && h < hq) {
-            const int64_t at = (t * hq + h) * D + 8 * l;
-            store8<DT, VEC>(a.q_out, at, u);
-            store8<DT, VEC>(a.q_out, at + H, v);
-        }
-        if (live && key && h < heads && a.k_out != nullptr) {
-            const int64_t at = (t * hkv + h - hq) * D + 8 * l;
-            store8<DT, VEC>(a.k_out, at, u);
-            store8<DT, VEC>(a.k_out, at + H, v);
-        }
-        if (!__any_sync(0xFFFFFFFFu, row && key)) continue;
+    }
+    if (live && h < hq) {
+        const int64_t at = (t * hq + h) * D + 8 * l;
+        store8<DT, VEC>(a.q_out, at, u);
+        store8<DT, VEC>(a.q_out, at + H, v);
+    }
+    if (live && key && a.k_out != nullptr) {
+        const int64_t at = (t * hkv + h - hq) * D + 8 * l;
+        store8<DT, VEC>(a.k_out, at, u);
+        store8<DT, VEC>(a.k_out, at + H, v);
+    }
+    if (__any_sync(0xFFFFFFFFu, used && key)) {
         bool bad;
         const KvQuant z = kv_row_quantiser<L>(u, v, bad);
-        if (row && key && slot != AASD_NONE && AASD_IN_RANGE(slot / kPage < a.p.n_pages && h - hq < hkv, a.state)) {
+        if (used && key && slot != AASD_NONE && AASD_IN_RANGE(slot / kPage < a.p.n_pages && h - hq < hkv, a.state)) {
             if (bad) bits |= AASD_STATUS_BAD_ROW;
             uint8_t* block = a.pages + ((int64_t)(slot / kPage) * hkv + h - hq) * kv_head_bytes(D);
             const int at = slot % kPage;
