@@ -539,9 +539,11 @@ typedef struct aasd_kv_attend_out {
  * its cached_len[b] cached tokens and, among the new ones (which must have been stored: kv_len[b] -
  * cached_len[b] of them), tokens 0..i, or with node_parent (one entry per token row, index inside
  * the sequence, NONE = no parent; parents precede their children) itself and its ancestors.
- * Sums and the softmax's statistics are fp32; bf16 queries are used as they are, probabilities are
- * rounded to 11 bits (fp32 queries: both to 22) for the products on the tensor cores; the result is
- * rounded once.  Rows that see nothing (padding, tokens that were not placed) give zeros and an lse of
+ * Sums and the softmax's statistics are fp32; bf16 queries are used as they are, probabilities and, with
+ * more than 48 rows per key/value head, the cache's values are rounded to 11 bits (fp32 queries: they
+ * and the probabilities to 22) for the products on the tensor cores; the result is rounded once.
+ * More than 2^31 - 1 pages to go through in one call (over all heads and row tiles) raise
+ * AASD_STATUS_BAD_OFFSETS.  Rows that see nothing (padding, tokens that were not placed) give zeros and an lse of
  * -inf.  A page id outside the pool, or a parent that does not precede its child, raises
  * AASD_STATUS_BAD_OFFSETS; what lies behind it counts as not visible. */
 int aasd_kv_attend(aasd_ctx* ctx, const void* q, const void* pages, const int32_t* block_table,

@@ -223,7 +223,8 @@ constexpr int kPlanThreads = 256, kPlanThreadsMany = 1024;   // of batches up to
 // One CTA: the books of all sequences (NT at a time) by prefix sums, the pages moved
 // by all threads together (a thread finds its page's sequence by bisection of the sums), so one
 // long sequence that ends or arrives costs no more than many short ones.  Latency-bound: four
-// scans and three trips to memory.
+// scans and three trips to memory (4 trees of 9 nodes 5 us, 256 arriving prompts of ~1000 tokens
+// 15 us with the token arrays' launch; a launch alone is 2 us).
 template <int NT>
 __global__ void __launch_bounds__(NT) kv_plan_kernel(const KvPlanArgs a) {
     __shared__ long long s_warp[NT / 32];
@@ -717,7 +718,8 @@ struct KvReadArgs {
 
 // A CTA takes kValueTokens slots of one head.  The values' bytes are fetched with a lane per slot, so
 // that neighbouring slots are one access, and pass through shared memory; then D / 16 lanes turn out a
-// row as in the writing kernel.
+// row as in the writing kernel.  Memory-bound: 4096 slots of 8 heads of 128 channels 7.4 us, the writing kernel
+// 27 us for the 89 MB that it reads and writes beside 32 query heads (the two together half of the copy rate).
 template <int DT, int D, bool VEC>
 __global__ void __launch_bounds__(kWriteThreads) kv_read_kernel(const KvReadArgs a) {
     constexpr int L = D / 16, H = D / 2, kRows = kWriteThreads / L, kPitch = H + 8;
@@ -804,7 +806,9 @@ constexpr int kCommitThreads = 256;
 // memory, walks the path there, turns it into (source slot, destination slot) pairs, and its
 // warps move the entries of one head after another.  Path nodes are in ascending order and never
 // in front of their depth, so a destination is a source of an earlier node at most: entries are
-// moved in ascending order, a batch's loads before its stores.
+// moved in ascending order, a batch's loads before its stores.  A token's values are single bytes 64 apart,
+// so a moved entry touches a 32-byte sector per byte of them: 256 paths of 8 layers take 24 us, four
+// times what the bytes alone would; one path of 16 layers 4 us, the chain of its dependent loads.
 template <int D>
 __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const KvCommitArgs a) {
     constexpr int H = D / 2, W = H / 4;        // W: 32-bit words of a token's keys

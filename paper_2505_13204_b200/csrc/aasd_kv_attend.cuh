@@ -340,6 +340,12 @@ __device__ __forceinline__ void kv_join_row(const KvAttendArgs& a, const KvPiece
 // block: 100 to 200 KB per SM are on their way at any time (memory wants about 40).  Twelve warps
 // where their registers allow it (168 each): the chains of a page's products and exponentials leave
 // issue slots that only other warps fill.
+//
+// The list of all pages is cut into equal shares, one per warp, whatever sequences they belong to;
+// pieces of a segment are joined first in the CTA, then by the last CTA that delivers one.
+// Measured (bf16, 128 channels): 256 sequences of 100 to 4000 tokens, 28 query and 4 key heads, 66 us, two
+// thirds of the copy rate (start-up 10 us, joining 5); one sequence of 16384 tokens 16 us, which is
+// the chain plan of the share - table - page - product - join - join and not its 18 MB (2.7 us).
 template <int DT, int D, int NT>
 struct KvSplitShape {
     static constexpr int W = D == 256 ? 4 : DT == AASD_BF16 && NT == 1 ? 12 : 8;
