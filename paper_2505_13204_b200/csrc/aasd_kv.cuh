@@ -807,8 +807,8 @@ constexpr int kCommitThreads = 256;
 // warps move the entries of one head after another.  Path nodes are in ascending order and never
 // in front of their depth, so a destination is a source of an earlier node at most: entries are
 // moved in ascending order, a batch's loads before its stores.  A token's values are single bytes 64 apart,
-// so a moved entry touches a 32-byte sector per byte of them: 256 paths of 8 layers take 24 us, four
-// times what the bytes alone would; one path of 16 layers 4 us, the chain of its dependent loads.
+// so a moved entry touches a 32-byte sector per byte of them: 256 paths of 8 layers (4 heads of 128
+// channels) take 15.4 us, and one path of 16 layers 2.9 us, the chain of its dependent loads.
 template <int D>
 __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const KvCommitArgs a) {
     constexpr int H = D / 2, W = H / 4;        // W: 32-bit words of a token's keys
