@@ -254,29 +254,34 @@ __device__ __forceinline__ void store4(void* base, long long i, float4 x, bool v
 // ---- rows that see nothing ---------------------------------------------------------------------------
 
 // Zeros (and an lse of -inf) for the token rows that hold no placed token; the warps of the whole
-// grid share the sequences.  Rows outside every sequence's range count as rows past the last one.
+// grid share the sequences.  A sequence whose rows pass n_tokens (aasd_kv_plan leaves it out) has none
+// placed: those of its rows that exist are cleared.  Rows outside every sequence's range go with the
+// rows past the last one.
 template <int DT>
 __device__ __forceinline__ void kv_clear_rows(const KvAttendArgs& a, int D, int warp, int warps) {
     const int lane = threadIdx.x & 31;
     const int Hq = a.p.n_q_heads;
-#pragma unroll 1
-    for (int b = warp; b <= a.p.n_seqs; b += warps) {
-        long long lo, hi;
-        if (b < a.p.n_seqs) {
-            const KvSeq s = kv_load_seq(a, b, 8);
-            lo = (long long)s.first + s.fresh;
-            hi = (long long)s.first + s.rows;
-        } else {
-            lo = a.p.rows_per_seq > 0 ? a.p.n_tokens : a.p.n_seqs > 0 ? a.tok_offsets[a.p.n_seqs] : 0;
-            lo = lo < 0 ? 0 : lo;
-            hi = a.p.n_tokens;
-        }
+    const bool padded = a.p.rows_per_seq > 0;
+    const auto clear = [&](long long lo, long long hi) {
+        lo = lo < 0 ? 0 : lo;
+        hi = hi < a.p.n_tokens ? hi : a.p.n_tokens;
         const long long e0 = lo * Hq * D, e1 = hi * Hq * D;
 #pragma unroll 1
         for (long long e = e0 + lane * 4; e < e1; e += 128) store4<DT>(a.o.out, e, make_float4(0.f, 0.f, 0.f, 0.f), a.out_vec);
         if (a.o.lse)
 #pragma unroll 1
             for (long long e = lo * Hq + lane; e < hi * Hq; e += 32) a.o.lse[e] = -CUDART_INF_F;
+    };
+#pragma unroll 1
+    for (int b = warp; b <= a.p.n_seqs; b += warps) {
+        if (b < a.p.n_seqs) {
+            // (not KvSeq's first and rows, which are none where they do not all exist)
+            const long long first = padded ? (long long)b * a.p.rows_per_seq : a.tok_offsets[b];
+            clear(first + kv_load_seq(a, b, 8).fresh, padded ? first + a.p.rows_per_seq : a.tok_offsets[b + 1]);
+        } else if (!padded) {
+            if (a.p.n_seqs > 0) clear(0, a.tok_offsets[0]);
+            clear(a.p.n_seqs > 0 ? a.tok_offsets[a.p.n_seqs] : 0, a.p.n_tokens);
+        }
     }
 }
 

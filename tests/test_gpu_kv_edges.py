@@ -1,0 +1,86 @@
+"""Edges of the paged 4-bit cache's calls: rows that no sequence owns, aliased and misshapen
+arguments, captured graphs, and the branches of the attention kernels that ordinary inputs do not
+take."""
+import numpy as np
+import pytest
+import torch
+
+import kv_ref as ref
+from paper_2505_13204_b200 import binding
+from test_gpu_kv import DT, PAGE, Pool, _tree, f64, i32
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = binding.Context()
+    yield c
+    c.close()
+
+
+def nan_outputs(T, Hq, D, dtype, shift=0):
+    """Outputs that hold NaN before the call; out starts `shift` elements past a 16-byte boundary."""
+    out = torch.full((T * Hq * D + shift,), float("nan"), dtype=DT[dtype], device="cuda")[shift:].view(T, Hq, D)
+    return dict(out=out, lse=torch.full((T, Hq), float("nan"), device="cuda"))
+
+
+def queries(rng, T, Hq, D, dtype, size=1.0):
+    return torch.as_tensor((rng.standard_normal((T, Hq, D)) * size).astype(np.float32)).to(DT[dtype]).cuda()
+
+
+def check_rows(pool, q, o, rows, scale=None):
+    """rows: {token row: (sequence, visible places)}; every other row is zeros with an lse of -inf.
+    The bounds are those of test_gpu_kv._check_attend, which derives them."""
+    s = 1.0 / np.sqrt(pool.D) if scale is None else scale
+    got, lse, qn, f32 = f64(o["out"]), f64(o["lse"]), f64(q), q.dtype == torch.float32
+    for t in range(q.shape[0]):
+        b, vis = rows.get(t, (0, []))
+        if not vis:
+            assert (got[t] == 0).all() and np.isneginf(lse[t]).all(), t
+            continue
+        want, wl, size = ref.attend(qn[t], pool.k[b], pool.v[b], vis, s)
+        spread = np.ptp(pool.v[b][vis], axis=(0, 2)).repeat(q.shape[1] // pool.Hkv) + 2.0 ** -60
+        wrong = size * 2.0 ** -20 + 2.0 ** -20 + np.abs(wl) * 2.0 ** -22
+        lim = spread * (2 * wrong + (2.0 ** -21 if f32 else 2.0 ** -11) + 2.0 ** -20) + 2.0 ** -21 * np.abs(pool.v[b][vis]).max()
+        lim = lim[:, None] + np.abs(want) * (2.0 ** -24 if f32 else 2.0 ** -8)
+        err = np.abs(got[t] - want)
+        assert (err <= lim).all(), (t, float((err / lim).max()))
+        assert (np.abs(lse[t] - wl) <= wrong + 2.0 ** -21 * np.abs(wl)).all(), t
+
+
+# query heads per key head: the split kernel, one tile, the pair of tiles (bf16, at 4 token rows per sequence on average)
+GROUPS = [(3, "f32"), (3, "bf16"), (16, "bf16"), (40, "bf16")]
+
+
+# ---- rows that no sequence owns --------------------------------------------------------------------
+
+@pytest.mark.parametrize("G,dtype", GROUPS)
+@pytest.mark.parametrize("new", [(5, 6, 0), (5, 7, 2), (0, 11, 3)])
+def test_tokens_of_a_sequence_that_passes_the_end_give_zeros(ctx, G, dtype, new):
+    """kv_plan leaves the whole sequence out; its rows that do exist see nothing."""
+    rng = np.random.default_rng(G)
+    T = 10
+    table, held = i32(np.full((3, 3), -1)), i32([0, 0, 0])
+    plan = ctx.kv_plan(i32([0, 0, 0]), i32(new), table, held, i32([0, 1, 2, 3]), i32([4]), T)
+    assert ctx.poll_status() == binding.STATUS_KV_FULL
+    assert plan["tok_offsets"].tolist() == [0, new[0], new[0] + new[1], sum(new)] and plan["kv_len"].tolist() == [new[0], 0, 0]
+    pool = Pool(rng, [new[0], 0, 0], 1, 64)
+    q = queries(rng, T, G, 64, dtype)
+    o = ctx.kv_attend(q, pool.pages, i32(pool.table), i32([0, 0, 0]), plan["kv_len"], plan["tok_offsets"], want_lse=True,
+                      outputs=nan_outputs(T, G, 64, dtype))
+    assert ctx.poll_status() == 0
+    check_rows(pool, q, o, {i: (0, list(range(i + 1))) for i in range(new[0])})
+
+
+@pytest.mark.parametrize("G,dtype", GROUPS)
+def test_rows_in_front_of_the_first_sequence_and_behind_the_last_give_zeros(ctx, G, dtype):
+    rng = np.random.default_rng(G + 1)
+    pool = Pool(rng, [70, 5], 1, 64)
+    q = queries(rng, 11, G, 64, dtype)
+    o = ctx.kv_attend(q, pool.pages, i32(pool.table), i32([67, 2]), i32(pool.kv_len), i32([2, 5, 8]), want_lse=True,
+                      outputs=nan_outputs(11, G, 64, dtype))
+    assert ctx.poll_status() == 0
+    rows = {2 + i: (0, list(range(68 + i))) for i in range(3)}
+    rows.update({5 + i: (1, list(range(3 + i))) for i in range(3)})
+    check_rows(pool, q, o, rows)
