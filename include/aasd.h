@@ -543,8 +543,8 @@ typedef struct aasd_kv_attend_out {
  * more than 48 rows per key/value head, the cache's values are rounded to 11 bits (fp32 queries: they
  * and the probabilities to 22) for the products on the tensor cores; the result is rounded once.
  * More than 2^31 - 1 pages to go through in one call (over all heads and row tiles) raise
- * AASD_STATUS_BAD_OFFSETS.  Rows that see nothing (padding, tokens that were not placed, rows that no
- * sequence owns) give zeros and an lse of -inf.  A page id outside the pool, or a parent that does not precede its child, raises
+ * AASD_STATUS_BAD_OFFSETS; no row sees anything then.  Rows that see nothing (padding, tokens that were
+ * not placed, rows that no sequence owns) give zeros and an lse of -inf.  A page id outside the pool, or a parent that does not precede its child, raises
  * AASD_STATUS_BAD_OFFSETS; what lies behind it counts as not visible. */
 int aasd_kv_attend(aasd_ctx* ctx, const void* q, const void* pages, const int32_t* block_table,
                    const int32_t* cached_len, const int32_t* kv_len, const int32_t* tok_offsets,

@@ -256,9 +256,10 @@ __device__ __forceinline__ void store4(void* base, long long i, float4 x, bool v
 // Zeros (and an lse of -inf) for the token rows that hold no placed token; the warps of the whole
 // grid share the sequences.  A sequence whose rows pass n_tokens (aasd_kv_plan leaves it out) has none
 // placed: those of its rows that exist are cleared.  Rows outside every sequence's range go with the
-// rows past the last one.
+// rows past the last one.  total: all units of the call; where there are none (or more than can be
+// counted) no row is worked on.
 template <int DT>
-__device__ __forceinline__ void kv_clear_rows(const KvAttendArgs& a, int D, int warp, int warps) {
+__device__ __forceinline__ void kv_clear_rows(const KvAttendArgs& a, int D, int total, int warp, int warps) {
     const int lane = threadIdx.x & 31;
     const int Hq = a.p.n_q_heads;
     const bool padded = a.p.rows_per_seq > 0;
@@ -277,7 +278,7 @@ __device__ __forceinline__ void kv_clear_rows(const KvAttendArgs& a, int D, int 
         if (b < a.p.n_seqs) {
             // (not KvSeq's first and rows, which are none where they do not all exist)
             const long long first = padded ? (long long)b * a.p.rows_per_seq : a.tok_offsets[b];
-            clear(first + kv_load_seq(a, b, 8).fresh, padded ? first + a.p.rows_per_seq : a.tok_offsets[b + 1]);
+            clear(first + (total > 0 ? kv_load_seq(a, b, 8).fresh : 0), padded ? first + a.p.rows_per_seq : a.tok_offsets[b + 1]);
         } else if (!padded) {
             if (a.p.n_seqs > 0) clear(0, a.tok_offsets[0]);
             clear(a.p.n_seqs > 0 ? a.tok_offsets[a.p.n_seqs] : 0, a.p.n_tokens);
@@ -982,7 +983,7 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
             }
         }
     }
-    kv_clear_rows<DT>(a, D, (int)(blockIdx.x * W + warp), (int)(gridDim.x * W));
+    kv_clear_rows<DT>(a, D, total, (int)(blockIdx.x * W + warp), (int)(gridDim.x * W));
 }
 
 }  // namespace aasd

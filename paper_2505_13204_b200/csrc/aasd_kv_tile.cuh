@@ -947,7 +947,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
             if (sh.open.seg >= 0 && ok && !*abort_flag) o.parts = sh.shares.owner(sh.open.seg + sh.open.pages - 1) - c + 1;
             a.tile_open[c] = o;
         }
-        kv_clear_rows<AASD_BF16>(a, D, (int)(blockIdx.x * 8 + warp), (int)(gridDim.x * 8));
+        kv_clear_rows<AASD_BF16>(a, D, total, (int)(blockIdx.x * 8 + warp), (int)(gridDim.x * 8));
     }
     if (!ok) give_up(abort_flag, a.state);
     tc_fence_before();

@@ -84,3 +84,16 @@ def test_rows_in_front_of_the_first_sequence_and_behind_the_last_give_zeros(ctx,
     rows = {2 + i: (0, list(range(68 + i))) for i in range(3)}
     rows.update({5 + i: (1, list(range(3 + i))) for i in range(3)})
     check_rows(pool, q, o, rows)
+
+
+@pytest.mark.parametrize("dtype,width,H", [("f32", 1 << 20, 8), ("bf16", 1 << 24, 16)])
+def test_more_pages_than_a_call_can_count_give_zeros(ctx, dtype, width, H):
+    """(The table names no page, so there would be nothing to see either.)"""
+    T = 4096
+    kv = width * PAGE
+    pages = binding.kv_pages(1, H, 64)
+    q = torch.ones((T, H, 64), dtype=DT[dtype], device="cuda")
+    table = torch.full((1, width), -1, dtype=torch.int32, device="cuda")
+    o = ctx.kv_attend(q, pages, table, i32([kv - T]), i32([kv]), rows_per_seq=T, want_lse=True, outputs=nan_outputs(T, H, 64, dtype))
+    assert ctx.poll_status() == binding.STATUS_BAD_OFFSETS
+    assert bool((o["out"] == 0).all()) and bool((o["lse"] == float("-inf")).all())
