@@ -516,7 +516,8 @@ int aasd_kv_write(aasd_ctx* ctx, const void* q, const void* k, const void* v,
 int aasd_kv_workspace_bytes(int32_t head_dim, size_t* bytes);
 /* Registers a 256-byte aligned device buffer of at least that size and clears what must start at
  * zero (asynchronous).  Like the other workspace, it must not be shared by overlapping calls;
- * aasd_workspace_release forgets it. */
+ * aasd_workspace_release forgets it.  After a call that raised AASD_STATUS_TIMEOUT it must be registered
+ * again: tickets may be left that are not zero. */
 int aasd_kv_workspace_init(aasd_ctx* ctx, void* workspace, size_t bytes, int32_t head_dim);
 
 typedef struct aasd_kv_attend_params {

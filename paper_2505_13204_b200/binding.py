@@ -357,8 +357,11 @@ class Context:
                "aasd_debug_withhold_tile")
 
     def reinit_workspace(self):
-        """Registers the context's own workspace again (clears it): required after a launch
+        """Registers the context's own workspaces again (clears them): required after a launch
         that ended with STATUS_TIMEOUT."""
+        if self._kv_ws is not None:
+            _check(self.lib.aasd_kv_workspace_init(self._h, _vp(self._kv_ws.data_ptr()), self._kv_ws.numel(),
+                                                   self._kv_ws_dim), "aasd_kv_workspace_init")
         if self._ws is not None:
             _check(self.lib.aasd_workspace_init(self._h, _vp(self._ws.data_ptr()), self._ws.numel(),
                                                 self._ws_rows, self._ws_cands), "aasd_workspace_init")

@@ -97,3 +97,23 @@ def test_more_pages_than_a_call_can_count_give_zeros(ctx, dtype, width, H):
     o = ctx.kv_attend(q, pages, table, i32([kv - T]), i32([kv]), rows_per_seq=T, want_lse=True, outputs=nan_outputs(T, H, 64, dtype))
     assert ctx.poll_status() == binding.STATUS_BAD_OFFSETS
     assert bool((o["out"] == 0).all()) and bool((o["lse"] == float("-inf")).all())
+
+
+# ---- captured graphs and scratch -----------------------------------------------------------------------
+
+def attend_case(rng, D=64, dtype="bf16"):
+    """One long sequence: many CTAs meet in the scratch."""
+    pool = Pool(rng, [4000], 1, D)
+    q = queries(rng, 1, 4, D, dtype)
+    return pool, q, (pool.pages, i32(pool.table), i32([3999]), i32([4000]))
+
+
+def test_scratch_is_cleared_by_registering_it_again(ctx):
+    """What a call that timed out leaves behind: tickets that are not zero."""
+    pool, q, args = attend_case(np.random.default_rng(30))
+    want = ctx.kv_attend(q, *args, rows_per_seq=1)["out"].clone()
+    torch.cuda.synchronize()
+    ctx.kv_workspace(64).fill_(0x5A)
+    ctx.reinit_workspace()
+    o = ctx.kv_attend(q, *args, rows_per_seq=1, want_lse=True, outputs=nan_outputs(1, 4, 64, "bf16"))
+    assert torch.equal(o["out"], want) and ctx.poll_status() == 0
