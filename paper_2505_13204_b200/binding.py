@@ -315,7 +315,7 @@ class Context:
         self._h = h
         self._ws = None
         self._ws_rows = self._ws_cands = -1
-        self._kv_ws, self._kv_ws_dim = None, 0
+        self._kv_ws = {}          # scratch of kv_attend by head dimension
         self._kv_structs = {}     # parameter structs by their values (filling one costs as much as the call)
 
     def close(self):
@@ -359,9 +359,9 @@ class Context:
     def reinit_workspace(self):
         """Registers the context's own workspaces again (clears them): required after a launch
         that ended with STATUS_TIMEOUT."""
-        if self._kv_ws is not None:
-            _check(self.lib.aasd_kv_workspace_init(self._h, _vp(self._kv_ws.data_ptr()), self._kv_ws.numel(),
-                                                   self._kv_ws_dim), "aasd_kv_workspace_init")
+        for dim in sorted(self._kv_ws):       # (a scratch that serves smaller dimensions too is registered for its own last)
+            ws = self._kv_ws[dim]
+            _check(self.lib.aasd_kv_workspace_init(self._h, _vp(ws.data_ptr()), ws.numel(), dim), "aasd_kv_workspace_init")
         if self._ws is not None:
             _check(self.lib.aasd_workspace_init(self._h, _vp(self._ws.data_ptr()), self._ws.numel(),
                                                 self._ws_rows, self._ws_cands), "aasd_workspace_init")
@@ -604,19 +604,25 @@ class Context:
         return o
 
     def kv_workspace(self, head_dim: int) -> torch.Tensor:
-        """The context's own scratch for ``kv_attend``."""
-        if self._kv_ws is None or head_dim > self._kv_ws_dim:
+        """The context's own scratch for ``kv_attend``, kept as long as the context: captured graphs
+        hold its address.  A call that is captured before there is one gets a scratch of its own, which
+        belongs to the graph like the clearing in front of the call."""
+        ws = self._kv_ws.get(head_dim)
+        if ws is None:
+            larger = [d for d in self._kv_ws if d > head_dim]
+            if larger:
+                ws = self._kv_ws[head_dim] = self._kv_ws[max(larger)]
+                return ws
             n = C.c_size_t()
             _check(self.lib.aasd_kv_workspace_bytes(int(head_dim), C.byref(n)), "aasd_kv_workspace_bytes")
-            if self._kv_ws is not None:
-                self.stream.synchronize()
-                self.lib.aasd_workspace_release(self._h, _vp(self._kv_ws.data_ptr()))
             with torch.cuda.stream(self.stream):
                 ws = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+                captured = torch.cuda.is_current_stream_capturing()
             _check(self.lib.aasd_kv_workspace_init(self._h, _vp(ws.data_ptr()), n.value, int(head_dim)),
                    "aasd_kv_workspace_init")
-            self._kv_ws, self._kv_ws_dim = ws, head_dim
-        return self._kv_ws
+            if not captured:
+                self._kv_ws[head_dim] = ws
+        return ws
 
     def kv_attend(self, q, pages, block_table, cached_len, kv_len, tok_offsets=None, rows_per_seq=0,
                   node_parent=None, scale=0.0, want_lse=False, outputs=None):
@@ -643,6 +649,8 @@ class Context:
                                      kv_len.data_ptr(), None if tok_offsets is None else tok_offsets.data_ptr(),
                                      None if node_parent is None else node_parent.data_ptr(), prm, ws.data_ptr(),
                                      ws.numel(), C.byref(out))
+        if D not in self._kv_ws:      # (captured: see kv_workspace)
+            self.lib.aasd_workspace_release(self._h, _vp(ws.data_ptr()))
         if rc:
             raise AasdError(rc, "aasd_kv_attend")
         return o

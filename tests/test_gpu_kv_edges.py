@@ -117,3 +117,54 @@ def test_scratch_is_cleared_by_registering_it_again(ctx):
     ctx.reinit_workspace()
     o = ctx.kv_attend(q, *args, rows_per_seq=1, want_lse=True, outputs=nan_outputs(1, 4, 64, "bf16"))
     assert torch.equal(o["out"], want) and ctx.poll_status() == 0
+
+
+def test_a_captured_call_keeps_its_scratch():
+    """A graph holds the scratch's address: calls with a larger head dimension do not move it."""
+    c = binding.Context()
+    try:
+        pool, q, args = attend_case(np.random.default_rng(31))
+        o = nan_outputs(1, 4, 64, "bf16")
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            c.set_stream(side)
+            want = c.kv_attend(q, *args, rows_per_seq=1)["out"].clone()
+            size = c.kv_workspace(64).numel()
+            side.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                c.kv_attend(q, *args, rows_per_seq=1, outputs=dict(out=o["out"]))
+            wide, wq, wargs = attend_case(np.random.default_rng(32), 256)
+            c.kv_attend(wq, *wargs, rows_per_seq=1)
+            others = [torch.full((size,), 0x5A, dtype=torch.uint8, device="cuda") for _ in range(4)]
+            for _ in range(2):
+                g.replay()
+            side.synchronize()
+        assert torch.equal(o["out"], want) and c.poll_status() == 0
+        assert all(bool((x == 0x5A).all()) for x in others)
+    finally:
+        c.close()
+
+
+def test_scratch_of_a_call_that_is_captured_first_is_not_taken_for_cleared():
+    """Its clearing is part of the graph and has not run when the next call is made."""
+    c = binding.Context()
+    try:
+        pool, q, args = attend_case(np.random.default_rng(33))
+        first, second = nan_outputs(1, 4, 64, "bf16"), nan_outputs(1, 4, 64, "bf16")
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            c.set_stream(side)
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                c.kv_attend(q, *args, rows_per_seq=1, outputs=dict(out=first["out"]))
+            assert c._kv_ws == {}
+            c.kv_attend(q, *args, rows_per_seq=1, outputs=dict(out=second["out"]))
+            for _ in range(2):
+                g.replay()
+            side.synchronize()
+        assert torch.equal(first["out"], second["out"]) and bool(torch.isfinite(first["out"]).all()) and c.poll_status() == 0
+    finally:
+        c.close()
