@@ -254,6 +254,15 @@ def _kv_i32(*tensors):
         assert t is None or (t.dtype is torch.int32 and t.is_cuda and t.is_contiguous()), "int32, on the device, contiguous"
 
 
+def _kv_token_stride(x: torch.Tensor) -> int:
+    """Elements between the tokens of x [T, H, D], whose heads are contiguous.  (The stride of a dimension of
+    one entry says nothing: views of single tokens or heads have any.)"""
+    T, H, D = x.shape
+    st, sh, sd = x.stride()
+    assert T == 0 or (sd == 1 and (sh == D or H <= 1)), "the heads of a token are contiguous"
+    return st if T > 1 else H * D
+
+
 def verify_static(target_logits, draft_ids, cand_offsets=None, draft_flags=None, alpha=0.1,
                   beta=0.1, mode=VERIFY_CONDITIONAL, seed=0, step=0, inv_temperature=1.0,
                   rows_per_cand=0, outputs=None, status_bits=None, stream=None, top_k=5):
@@ -575,8 +584,7 @@ class Context:
         _kv_i32(slot_map, positions)
         T, Hq, D = q.shape
         Hkv = k.shape[1]
-        qs, ks, vs = q.stride(), k.stride(), v.stride()
-        assert qs[2] == 1 and (T == 0 or (qs[1] == D and ks[1] == D and vs[1] == D and ks[2] == 1 and vs[2] == 1))
+        qs, ks, vs = _kv_token_stride(q), _kv_token_stride(k), _kv_token_stride(v)
         dt = q.dtype
         assert k.dtype is dt and v.dtype is dt and k.shape == v.shape and k.shape[2] == D and _kv_dim(pages) == D
         assert pages.dtype is torch.uint8 and pages.is_contiguous() and pages.shape[1] == Hkv
@@ -590,7 +598,7 @@ class Context:
         if cos_sin is not None:
             assert cos_sin.dtype is torch.float32 and cos_sin.is_contiguous()
             limit, rot = cos_sin.shape
-        prm = self._kv_struct(KvWriteParams, Hq, Hkv, D, pages.shape[0], _dtype_code(q), qs[0], ks[0], vs[0], rot, limit,
+        prm = self._kv_struct(KvWriteParams, Hq, Hkv, D, pages.shape[0], _dtype_code(q), qs, ks, vs, rot, limit,
                               eps, KV_ROPE_INTERLEAVED if interleaved else 0)
         ko = o.get("k")
         rc = self.lib.aasd_kv_write(self._h, q.data_ptr(), k.data_ptr(), v.data_ptr(),
@@ -632,8 +640,8 @@ class Context:
         _kv_i32(block_table, cached_len, kv_len, tok_offsets, node_parent)
         T, Hq, D = q.shape
         B, P = block_table.shape
-        qs = q.stride()
-        assert qs[2] == 1 and (T == 0 or qs[1] == D) and _kv_dim(pages) == D
+        qs = _kv_token_stride(q)
+        assert _kv_dim(pages) == D
         assert pages.dtype is torch.uint8 and pages.is_contiguous()
         o = outputs
         if o is None:
@@ -642,7 +650,7 @@ class Context:
         if want_lse and lse is None:
             lse = o["lse"] = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
         prm = self._kv_struct(KvAttendParams, B, Hq, pages.shape[1], D, pages.shape[0], P, _dtype_code(q), int(rows_per_seq),
-                              T, qs[0], scale)
+                              T, qs, scale)
         out = KvAttendOut(o["out"].data_ptr(), None if lse is None else lse.data_ptr())
         ws = self.kv_workspace(D)
         rc = self.lib.aasd_kv_attend(self._h, q.data_ptr(), pages.data_ptr(), block_table.data_ptr(), cached_len.data_ptr(),

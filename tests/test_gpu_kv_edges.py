@@ -99,6 +99,31 @@ def test_more_pages_than_a_call_can_count_give_zeros(ctx, dtype, width, H):
     assert bool((o["out"] == 0).all()) and bool((o["lse"] == float("-inf")).all())
 
 
+# ---- arguments -----------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_strides_of_single_tokens_and_heads_do_not_matter(ctx, dtype):
+    """One token, or one head, is contiguous whatever the stride of that dimension says."""
+    rng = np.random.default_rng(21)
+    D, Hq, Hkv = 64, 4, 1
+    q = queries(rng, Hq, 1, D, dtype).transpose(0, 1)                  # one token: strides (D, D, 1)
+    k, v = (queries(rng, 1, 5, D, dtype)[:, 2:3].transpose(0, 1) for _ in range(2))     # one head: strides (D, 5 D, 1)
+    assert q.stride(0) < Hq * D and k.stride(1) != D
+    pages, same = (torch.zeros((1, Hkv, ref.head_bytes(D)), dtype=torch.uint8, device="cuda") for _ in range(2))
+    a = ctx.kv_write(pages, q, k, v, i32([7]), i32([0]), keep_k=True)
+    b = ctx.kv_write(same, q.contiguous().clone(memory_format=torch.contiguous_format).reshape(1, Hq, D), k.reshape(1, 1, D).clone(),
+                     v.reshape(1, 1, D).clone(), i32([7]), i32([0]), keep_k=True)
+    assert torch.equal(a["q"], b["q"]) and torch.equal(a["k"], b["k"]) and torch.equal(pages, same)
+    pool = Pool(rng, [9], 1, D)
+    o = ctx.kv_attend(q, pool.pages, i32(pool.table), i32([8]), i32([9]), rows_per_seq=1, want_lse=True)
+    check_rows(pool, q, o, {0: (0, list(range(9)))})
+    one = queries(rng, 1, 3, D, dtype).transpose(0, 1)                 # three tokens of one head: strides (D, 3 D, 1)
+    assert one.shape == (3, 1, D) and one.stride(1) == 3 * D
+    o = ctx.kv_attend(one, pool.pages, i32(pool.table), i32([6]), i32([9]), rows_per_seq=3, want_lse=True)
+    check_rows(pool, one, o, {i: (0, list(range(7 + i))) for i in range(3)})
+    assert ctx.poll_status() == 0
+
+
 # ---- captured graphs and scratch -----------------------------------------------------------------------
 
 def attend_case(rng, D=64, dtype="bf16"):
