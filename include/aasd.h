@@ -566,7 +566,8 @@ typedef struct aasd_kv_commit_params {
  * the cached_len of the next step.  A best_node of NONE, or one whose token was not placed, leaves
  * new_len[b] = cached_len[b]; so does a path whose parents do not precede their children or whose
  * pages are not in the pool (AASD_STATUS_BAD_OFFSETS).  At most AASD_KV_MAX_NODES new tokens per
- * sequence (more raise that status too).  new_len must not be cached_len. */
+ * sequence (more raise that status too).  new_len must not lie over any of the inputs
+ * (AASD_ERR_INVALID_ARG): they are read while it is written. */
 #define AASD_KV_MAX_NODES 4096
 int aasd_kv_commit(aasd_ctx* ctx, void* pages, const int32_t* block_table, const int32_t* cached_len,
                    const int32_t* kv_len, const int32_t* tok_offsets, const int32_t* best_node,

@@ -13,6 +13,12 @@ bool dtype_ok(int d) { return d == AASD_F32 || d == AASD_BF16; }
 size_t elt_size(int dtype) { return dtype == AASD_F32 ? 4 : 2; }
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
+// Whether two arrays have a byte in common.
+bool overlap(const void* x, int64_t x_bytes, const void* y, int64_t y_bytes) {
+    const uintptr_t a = (uintptr_t)x, b = (uintptr_t)y;
+    return x != nullptr && y != nullptr && a < b + (uintptr_t)y_bytes && b < a + (uintptr_t)x_bytes;
+}
+
 // Calls f with the head dimension as a constant.
 template <class F>
 void with_dim(int head_dim, F&& f) {
@@ -150,10 +156,17 @@ int aasd_kv_commit(aasd_ctx* ctx, void* pages, const int32_t* block_table, const
         p->rows_per_seq < 0 || p->n_layers < 0 || p->layer_stride < 0 || (p->layer_stride % 16) != 0)
         return AASD_ERR_BAD_SHAPE;
     if (p->n_seqs == 0) return AASD_OK;
-    if (!block_table || !cached_len || !kv_len || !best_node || !node_parent || !new_len || new_len == cached_len)
-        return AASD_ERR_INVALID_ARG;
+    if (!block_table || !cached_len || !kv_len || !best_node || !node_parent || !new_len) return AASD_ERR_INVALID_ARG;
     if (p->rows_per_seq == 0 && !tok_offsets) return AASD_ERR_INVALID_ARG;
     if (p->n_layers > 0 && (!pages || !aligned16(pages))) return AASD_ERR_INVALID_ARG;
+    // Every CTA of a sequence reads its inputs for itself, in no order with the one that writes the new length.
+    const int64_t n4 = 4 * (int64_t)p->n_seqs;
+    const int64_t pool = (int64_t)p->n_pages * p->n_kv_heads * kv_head_bytes(p->head_dim);
+    if (overlap(new_len, n4, cached_len, n4) || overlap(new_len, n4, kv_len, n4) || overlap(new_len, n4, best_node, n4) ||
+        overlap(new_len, n4, tok_offsets, n4 + 4) || overlap(new_len, n4, block_table, n4 * p->max_pages) ||
+        overlap(new_len, n4, node_parent, p->rows_per_seq > 0 ? n4 * p->rows_per_seq : 4) ||
+        (p->n_layers > 0 && overlap(new_len, n4, pages, (p->n_layers - 1) * p->layer_stride + pool)))
+        return AASD_ERR_INVALID_ARG;
     KvCommitArgs a{static_cast<uint8_t*>(pages), block_table, cached_len, kv_len, tok_offsets, best_node, node_parent, *p, new_len,
                    ctx->state};
     const int64_t items = (int64_t)p->n_layers * p->n_kv_heads;

@@ -101,6 +101,32 @@ def test_more_pages_than_a_call_can_count_give_zeros(ctx, dtype, width, H):
 
 # ---- arguments -----------------------------------------------------------------------------------------
 
+def refused(ctx, f, *a, **kw):
+    before = ctx.launch_count()
+    with pytest.raises(binding.AasdError) as e:
+        f(*a, **kw)
+    assert ctx.launch_count() == before
+    return e.value.code
+
+
+def test_commit_refuses_results_over_its_inputs(ctx):
+    """Every CTA reads the lengths and the chosen node on its own, in no order with the new length."""
+    pages = binding.kv_pages(2, 1, 64, layers=1)
+    table, cached, kv, best, parent = i32([[0, -1]]), i32([3]), i32([5]), i32([1]), i32([[-1, 0]])
+    offs = i32([0, 2])
+    args = (pages, table, cached, kv, best)
+    for out in (cached, kv, best):
+        assert refused(ctx, ctx.kv_commit, *args, parent, outputs=out) == 1
+    flat = i32([-1])
+    assert refused(ctx, ctx.kv_commit, pages, table, i32([3]), i32([4]), i32([0]), flat, i32([0, 1]), outputs=flat) == 1
+    prm = binding.KvCommitParams(1, 1, 64, 2, 2, 0, 1, 0)
+    lib, h = ctx.lib, ctx._h
+    call = [pages.data_ptr(), table.data_ptr(), cached.data_ptr(), kv.data_ptr(), offs.data_ptr(), best.data_ptr(), parent.data_ptr(), prm]
+    for out in (table, offs, pages):
+        assert lib.aasd_kv_commit(h, *call, out.data_ptr()) == 1
+    assert ctx.poll_status() == 0
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_strides_of_single_tokens_and_heads_do_not_matter(ctx, dtype):
     """One token, or one head, is contiguous whatever the stride of that dimension says."""
