@@ -474,7 +474,8 @@ typedef struct aasd_kv_plan_out {     /* all required (tok_offsets: NULL allowed
  * writes it, one entry per token row) is given.  A sequence that has ended passes 0 and 0 and gives
  * all its pages back.  Inconsistent books (a held count outside the table, fewer held pages than
  * cached tokens, page ids outside the pool, a stack that would overflow) raise
- * AASD_STATUS_BAD_OFFSETS; nothing outside the arrays is touched. */
+ * AASD_STATUS_BAD_OFFSETS; nothing outside the arrays is touched.  No output may lie over cached_len
+ * (AASD_ERR_INVALID_ARG): a token's slot needs the old length beside the new one. */
 int aasd_kv_plan(aasd_ctx* ctx, const int32_t* cached_len, const int32_t* n_new,
                  const int32_t* node_depth, const aasd_kv_plan_params* params,
                  const aasd_kv_plan_state* state, const aasd_kv_plan_out* out);

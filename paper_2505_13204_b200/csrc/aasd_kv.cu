@@ -63,6 +63,11 @@ int aasd_kv_plan(aasd_ctx* ctx, const int32_t* cached_len, const int32_t* n_new,
         return AASD_ERR_INVALID_ARG;
     if (p->n_tokens > 0 && (!o->slot_map || !o->positions)) return AASD_ERR_INVALID_ARG;
     if (p->rows_per_seq == 0 && !o->tok_offsets) return AASD_ERR_INVALID_ARG;
+    // a token's slot and position are found from the old length and the new one
+    const int64_t n4 = 4 * (int64_t)p->n_seqs;
+    if (overlap(cached_len, n4, o->kv_len, n4) || overlap(cached_len, n4, o->tok_offsets, n4 + 4) ||
+        overlap(cached_len, n4, o->slot_map, 4 * p->n_tokens) || overlap(cached_len, n4, o->positions, 4 * p->n_tokens))
+        return AASD_ERR_INVALID_ARG;
     KvPlanArgs a{cached_len, n_new, node_depth, *p, *s, *o, ctx->state, 0};
     const bool many = p->n_seqs > kPlanManySeqs;
     a.tokens_inline = p->n_tokens <= kInlineTokens && p->n_seqs <= (many ? kPlanThreadsMany : kPlanThreads);

@@ -127,6 +127,15 @@ def test_commit_refuses_results_over_its_inputs(ctx):
     assert ctx.poll_status() == 0
 
 
+def test_plan_refuses_the_new_length_over_the_old_one(ctx):
+    """The slots are found from both."""
+    cached, books = i32([10]), (i32([[0, -1]]), i32([1]), i32([1, -1]), i32([1]))
+    new = torch.empty(1, dtype=torch.int32, device="cuda")
+    o = dict(kv_len=cached, tok_offsets=i32([0, 0]), slot_map=new, positions=new.clone())
+    assert refused(ctx, ctx.kv_plan, cached, i32([1]), *books, 1, rows_per_seq=1, outputs=o) == 1
+    assert ctx.poll_status() == 0
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_strides_of_single_tokens_and_heads_do_not_matter(ctx, dtype):
     """One token, or one head, is contiguous whatever the stride of that dimension says."""
