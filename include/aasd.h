@@ -444,7 +444,7 @@ int aasd_verify_tree(aasd_ctx* ctx, const void* target_logits, const int32_t* no
 typedef struct aasd_kv_plan_params {
     int32_t n_seqs;
     int32_t n_pages;        /* pages of the pool */
-    int32_t max_pages;      /* width of a block-table row */
+    int32_t max_pages;      /* width of a block-table row, at most (2^31 - 1) / 64: places are 32-bit */
     int32_t rows_per_seq;   /* > 0: padded token rows; 0: packed */
     int64_t n_tokens;       /* length of slot_map / positions (n_seqs * rows_per_seq when padded) */
 } aasd_kv_plan_params;

@@ -57,7 +57,7 @@ int aasd_kv_plan(aasd_ctx* ctx, const int32_t* cached_len, const int32_t* n_new,
     if (ctx == nullptr || p == nullptr || s == nullptr || o == nullptr) return AASD_ERR_INVALID_ARG;
     if (p->n_seqs < 0 || p->n_pages < 0 || p->max_pages < 1 || p->rows_per_seq < 0 || p->n_tokens < 0) return AASD_ERR_BAD_SHAPE;
     if (p->rows_per_seq > 0 && (int64_t)p->n_seqs * p->rows_per_seq != p->n_tokens) return AASD_ERR_BAD_SHAPE;
-    if (p->n_tokens > 0x7FFFFFFFLL || p->n_pages > 0x7FFFFFFF / kPage) return AASD_ERR_BAD_SHAPE;
+    if (p->n_tokens > 0x7FFFFFFFLL || p->n_pages > 0x7FFFFFFF / kPage || p->max_pages > 0x7FFFFFFF / kPage) return AASD_ERR_BAD_SHAPE;
     if (p->n_seqs == 0 && p->n_tokens == 0) return AASD_OK;
     if (!s->n_free || !s->free_pages || (p->n_seqs > 0 && (!cached_len || !n_new || !s->block_table || !s->seq_pages || !o->kv_len)))
         return AASD_ERR_INVALID_ARG;
@@ -158,7 +158,7 @@ int aasd_kv_commit(aasd_ctx* ctx, void* pages, const int32_t* block_table, const
     if (ctx == nullptr || p == nullptr) return AASD_ERR_INVALID_ARG;
     if (!head_dim_ok(p->head_dim)) return AASD_ERR_UNSUPPORTED;
     if (p->n_seqs < 0 || p->n_kv_heads < 1 || p->n_pages < 0 || p->n_pages > 0x7FFFFFFF / kPage || p->max_pages < 1 ||
-        p->rows_per_seq < 0 || p->n_layers < 0 || p->layer_stride < 0 || (p->layer_stride % 16) != 0)
+        p->max_pages > 0x7FFFFFFF / kPage || p->rows_per_seq < 0 || p->n_layers < 0 || p->layer_stride < 0 || (p->layer_stride % 16) != 0)
         return AASD_ERR_BAD_SHAPE;
     if (p->n_seqs == 0) return AASD_OK;
     if (!block_table || !cached_len || !kv_len || !best_node || !node_parent || !new_len) return AASD_ERR_INVALID_ARG;

@@ -136,6 +136,18 @@ def test_plan_refuses_the_new_length_over_the_old_one(ctx):
     assert ctx.poll_status() == 0
 
 
+def test_tables_wider_than_a_sequence_can_be_are_refused(ctx):
+    """Places of a sequence are 32-bit numbers: ceil(2^31 / 64) - 1 pages at most."""
+    one = i32([0, 0]).data_ptr()
+    lib, h = ctx.lib, ctx._h
+    prm = binding.KvPlanParams(1, 1, 1 << 25, 1, 1)
+    before = ctx.launch_count()
+    assert lib.aasd_kv_plan(h, one, one, None, prm, binding.KvPlanState(one, one, one, one), binding.KvPlanOut(one + 4, one, one, one)) == 2
+    prm = binding.KvCommitParams(1, 1, 64, 1, 1 << 25, 1, 0, 0)
+    assert lib.aasd_kv_commit(h, None, one, one, one, None, one, one, prm, one + 4) == 2
+    assert ctx.launch_count() == before
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_strides_of_single_tokens_and_heads_do_not_matter(ctx, dtype):
     """One token, or one head, is contiguous whatever the stride of that dimension says."""
