@@ -246,12 +246,28 @@ def kv_pages(n_pages: int, n_kv_heads: int, head_dim: int, layers: int | None = 
 
 def _kv_dim(pages: torch.Tensor) -> int:
     """Head dimension of a page pool."""
-    return (pages.shape[-1] - 512) // KV_PAGE
+    n = pages.shape[-1] - 512
+    _kv_need(n > 0 and n % KV_PAGE == 0, "blocks of a page")
+    return n // KV_PAGE
 
 
-def _kv_i32(*tensors):
+# The library cannot see how long its arrays are: what it reads and writes by the counts of the
+# others is checked here.  (Longer ones are fine.)
+def _kv_need(ok, what: str):
+    if not ok:
+        raise AasdError(2, "aasd_kv: " + what)
+
+
+def _kv_i32(device: int, *tensors):
     for t in tensors:
-        assert t is None or (t.dtype is torch.int32 and t.is_cuda and t.is_contiguous()), "int32, on the device, contiguous"
+        assert t is None or (t.dtype is torch.int32 and t.get_device() == device and t.is_contiguous()), "int32, on the device, contiguous"
+
+
+def _kv_like(x: torch.Tensor, n: int, *tensors):
+    """Outputs of at least n entries, of x's type and on its device."""
+    for t in tensors:
+        assert t is None or (t.dtype is x.dtype and t.get_device() == x.get_device() and t.is_contiguous()), "of the inputs' type, on their device, contiguous"
+        _kv_need(t is None or t.numel() >= n, "outputs")
 
 
 def _kv_token_stride(x: torch.Tensor) -> int:
@@ -560,12 +576,18 @@ class Context:
         """aasd_kv_plan: brings ``block_table`` [B, max_pages], ``seq_pages``, ``free_pages`` and
         ``n_free`` (all int32, changed in place) in line with ``cached_len + n_new`` tokens per
         sequence; returns kv_len, tok_offsets, slot_map and positions of the new tokens."""
-        _kv_i32(cached_len, n_new, block_table, seq_pages, free_pages, n_free, node_depth)
+        _kv_i32(self.device_index, cached_len, n_new, block_table, seq_pages, free_pages, n_free, node_depth)
         B, P = block_table.shape
+        _kv_need(cached_len.numel() >= B and n_new.numel() >= B and seq_pages.numel() >= B and n_free.numel() > 0 and
+                 (node_depth is None or node_depth.numel() >= n_tokens), "lengths of kv_plan's arrays")
         o = outputs
         if o is None:
             new = block_table.new_empty
             o = dict(kv_len=new(B), tok_offsets=new(B + 1), slot_map=new(n_tokens), positions=new(n_tokens))
+        else:
+            _kv_i32(self.device_index, o["kv_len"], o["tok_offsets"], o["slot_map"], o["positions"])
+            _kv_need(o["kv_len"].numel() >= B and o["tok_offsets"].numel() > B and o["slot_map"].numel() >= n_tokens and
+                     o["positions"].numel() >= n_tokens, "kv_plan's outputs")
         prm = self._kv_struct(KvPlanParams, B, free_pages.numel(), P, int(rows_per_seq), int(n_tokens))
         st = KvPlanState(block_table.data_ptr(), seq_pages.data_ptr(), free_pages.data_ptr(), n_free.data_ptr())
         out = KvPlanOut(o["kv_len"].data_ptr(), o["tok_offsets"].data_ptr(), o["slot_map"].data_ptr(), o["positions"].data_ptr())
@@ -581,22 +603,26 @@ class Context:
         fused projection are fine: only the heads of a token have to be contiguous), stores k and
         ``v`` at ``slot_map``.  ``cos_sin``: fp32 [positions, rotary_dim] or None.  Returns a dict
         with q and, with ``keep_k``, the rotated k."""
-        _kv_i32(slot_map, positions)
+        _kv_i32(self.device_index, slot_map, positions)
         T, Hq, D = q.shape
         Hkv = k.shape[1]
         qs, ks, vs = _kv_token_stride(q), _kv_token_stride(k), _kv_token_stride(v)
-        dt = q.dtype
+        dt, dev = q.dtype, self.device_index
         assert k.dtype is dt and v.dtype is dt and k.shape == v.shape and k.shape[2] == D and _kv_dim(pages) == D
-        assert pages.dtype is torch.uint8 and pages.is_contiguous() and pages.shape[1] == Hkv
-        assert slot_map.numel() == T and positions.numel() == T
+        assert pages.dtype is torch.uint8 and pages.is_contiguous() and pages.dim() == 3 and pages.shape[1] == Hkv
+        assert q.get_device() == dev and k.get_device() == dev and v.get_device() == dev and pages.get_device() == dev
+        _kv_need(k.shape[0] == T and slot_map.numel() == T and positions.numel() == T, "lengths of kv_write's arrays")
         for w in (q_weight, k_weight):
-            assert w is None or (w.dtype is dt and w.numel() == D and w.is_contiguous())
+            assert w is None or (w.dtype is dt and w.get_device() == dev and w.numel() == D and w.is_contiguous())
         o = outputs
         if o is None:
             o = dict(q=q.new_empty((T, Hq, D)), k=q.new_empty((T, Hkv, D)) if keep_k else None)
+        else:
+            _kv_like(q, T * Hq * D, o["q"])
+            _kv_like(q, T * Hkv * D, o.get("k"))
         rot = limit = 0
         if cos_sin is not None:
-            assert cos_sin.dtype is torch.float32 and cos_sin.is_contiguous()
+            assert cos_sin.dtype is torch.float32 and cos_sin.get_device() == dev and cos_sin.is_contiguous() and cos_sin.dim() == 2
             limit, rot = cos_sin.shape
         prm = self._kv_struct(KvWriteParams, Hq, Hkv, D, pages.shape[0], _dtype_code(q), qs, ks, vs, rot, limit,
                               eps, KV_ROPE_INTERLEAVED if interleaved else 0)
@@ -637,18 +663,26 @@ class Context:
         """aasd_kv_attend: attention of the new tokens ``q`` [T, Hq, D] over the cache.  Token rows
         are packed (``tok_offsets``) or padded (``rows_per_seq``); ``node_parent`` makes them draft
         trees.  Returns a dict with out [T, Hq, D] and, with ``want_lse``, lse [T, Hq]."""
-        _kv_i32(block_table, cached_len, kv_len, tok_offsets, node_parent)
+        _kv_i32(self.device_index, block_table, cached_len, kv_len, tok_offsets, node_parent)
         T, Hq, D = q.shape
         B, P = block_table.shape
         qs = _kv_token_stride(q)
         assert _kv_dim(pages) == D
-        assert pages.dtype is torch.uint8 and pages.is_contiguous()
+        assert pages.dtype is torch.uint8 and pages.is_contiguous() and pages.dim() == 3
+        assert q.get_device() == self.device_index and pages.get_device() == self.device_index
+        _kv_need(cached_len.numel() >= B and kv_len.numel() >= B and (tok_offsets is None or tok_offsets.numel() > B) and
+                 (node_parent is None or node_parent.numel() >= T), "lengths of kv_attend's arrays")
         o = outputs
         if o is None:
             o = dict(out=q.new_empty((T, Hq, D)))
+        else:
+            _kv_like(q, T * Hq * D, o["out"])
         lse = o.get("lse")
         if want_lse and lse is None:
             lse = o["lse"] = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
+        elif lse is not None:
+            assert lse.dtype is torch.float32 and lse.get_device() == self.device_index and lse.is_contiguous()
+            _kv_need(lse.numel() >= T * Hq, "outputs")
         prm = self._kv_struct(KvAttendParams, B, Hq, pages.shape[1], D, pages.shape[0], P, _dtype_code(q), int(rows_per_seq),
                               T, qs, scale)
         out = KvAttendOut(o["out"].data_ptr(), None if lse is None else lse.data_ptr())
@@ -668,10 +702,13 @@ class Context:
         """aasd_kv_commit: moves the accepted paths' entries in the pools of all layers (``pages``
         [layers, n_pages, Hkv, bytes]) and returns the new cached lengths.  ``node_parent`` is
         [B, rows_per_seq], or flat with ``tok_offsets``."""
-        _kv_i32(block_table, cached_len, kv_len, best_node, node_parent, tok_offsets)
-        assert pages.dim() == 4 and pages.dtype is torch.uint8 and pages.is_contiguous()
+        _kv_i32(self.device_index, block_table, cached_len, kv_len, best_node, node_parent, tok_offsets, outputs)
+        assert pages.dim() == 4 and pages.dtype is torch.uint8 and pages.is_contiguous() and pages.get_device() == self.device_index
         B, P = block_table.shape
         L, N, H, _ = pages.shape
+        _kv_need(cached_len.numel() >= B and kv_len.numel() >= B and best_node.numel() >= B and (outputs is None or outputs.numel() >= B) and
+                 (node_parent.dim() == 2 and node_parent.shape[0] >= B if tok_offsets is None else tok_offsets.numel() > B),
+                 "lengths of kv_commit's arrays")
         new_len = outputs if outputs is not None else cached_len.new_empty(B)
         prm = self._kv_struct(KvCommitParams, B, H, _kv_dim(pages), N, P,
                               0 if tok_offsets is not None else node_parent.shape[1], L, pages.stride(0))
@@ -685,13 +722,17 @@ class Context:
     def kv_read(self, pages, slots, head_dim, dtype=torch.bfloat16, outputs=None):
         """aasd_kv_read: the entries at ``slots`` as values, k and v [n, Hkv, D].  Several layers at
         once: pass ``pages.flatten(0, 1)`` and slots raised by layer * n_pages * KV_PAGE."""
-        _kv_i32(slots)
+        _kv_i32(self.device_index, slots)
         assert pages.dim() == 3 and pages.dtype is torch.uint8 and pages.is_contiguous() and _kv_dim(pages) == head_dim
+        assert pages.get_device() == self.device_index
         n, N, H = slots.numel(), pages.shape[0], pages.shape[1]
         o = outputs
         if o is None:
             shape = (n, H, head_dim)
             o = dict(k=torch.empty(shape, dtype=dtype, device=pages.device), v=torch.empty(shape, dtype=dtype, device=pages.device))
+        else:
+            assert o["k"].get_device() == self.device_index
+            _kv_like(o["k"], n * H * head_dim, o["k"], o["v"])
         rc = self.lib.aasd_kv_read(self._h, pages.data_ptr(), slots.data_ptr(), n, N, H, head_dim, _dtype_code(o["k"]),
                                    o["k"].data_ptr(), o["v"].data_ptr())
         if rc:

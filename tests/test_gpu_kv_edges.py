@@ -148,6 +148,85 @@ def test_tables_wider_than_a_sequence_can_be_are_refused(ctx):
     assert ctx.launch_count() == before
 
 
+def test_lengths_that_do_not_go_together_are_refused(ctx):
+    """Every array is read or written by the counts of the others."""
+    B, T = 3, 6
+    table, held, free, n = i32(np.full((B, 2), -1)), i32([0] * B), i32([0, 1, 2, 3]), i32([4])
+    z3, z2, z5, z7 = i32([0] * 3), i32([0] * 2), i32([0] * 5), i32([0] * 7)
+
+    def plan(**kw):
+        a = dict(cached_len=z3, n_new=i32([0] * 3), block_table=table, seq_pages=held, free_pages=free, n_free=n, n_tokens=T, rows_per_seq=2)
+        a.update(kw)
+        return lambda: ctx.kv_plan(**a)
+
+    new = dict(kv_len=i32([0] * 3), tok_offsets=i32([0] * 4), slot_map=i32([0] * T), positions=i32([0] * T))
+    bad = [plan(cached_len=z2), plan(n_new=z2), plan(seq_pages=z2), plan(n_free=i32([])), plan(node_depth=z5)]
+    bad += [plan(outputs=dict(new, kv_len=z2)), plan(outputs=dict(new, tok_offsets=z3)), plan(outputs=dict(new, slot_map=z5)),
+            plan(outputs=dict(new, positions=z5))]
+
+    pages = binding.kv_pages(4, 1, 64)
+    q = torch.zeros((T, 2, 64), device="cuda")
+    k = torch.zeros((T, 1, 64), device="cuda")
+    z6 = i32([0] * 6)
+
+    def attend(**kw):
+        a = dict(q=q, pages=pages, block_table=table, cached_len=z3, kv_len=z3, rows_per_seq=2)
+        a.update(kw)
+        return lambda: ctx.kv_attend(**a)
+
+    bad += [attend(cached_len=z2), attend(kv_len=z2), attend(node_parent=z5), attend(tok_offsets=z3, rows_per_seq=0),
+            attend(outputs=dict(out=q[:5])), attend(outputs=dict(out=q.to(torch.bfloat16))), attend(outputs=dict(out=torch.zeros((T, 4, 64), device="cuda")[:, :2])),
+            attend(outputs=dict(out=torch.empty_like(q), lse=torch.zeros((T, 1), device="cuda"))),
+            attend(outputs=dict(out=torch.empty_like(q), lse=torch.zeros((T, 2), device="cuda", dtype=torch.float64)))]
+    # blocks that are not a whole number of channels
+    odd = torch.zeros((4, 1, ref.head_bytes(64) + 32), dtype=torch.uint8, device="cuda")
+    bad += [attend(pages=odd), lambda: ctx.kv_read(odd, z6, 64), lambda: ctx.kv_commit(odd[None], table, z3, z3, z3, i32(np.zeros((3, 2)))),
+            lambda: ctx.kv_write(odd, q, k, k, z6, z6)]
+
+    def write(**kw):
+        a = dict(pages=pages, q=q, k=k, v=k, slot_map=z6, positions=z6)
+        a.update(kw)
+        return lambda: ctx.kv_write(**a)
+
+    bad += [write(slot_map=z5), write(positions=z7), write(k=k[:5], v=k[:5]), write(v=k[:5]), write(q_weight=torch.ones(63, device="cuda")),
+            write(cos_sin=torch.ones((0, 64), device="cuda")[:, :, None]),
+            write(outputs=dict(q=q[:5])), write(outputs=dict(q=torch.empty_like(q), k=k[:5])), write(outputs=dict(q=torch.empty_like(q, dtype=torch.bfloat16)))]
+
+    layers = pages[None]
+    tree = i32(np.zeros((3, 2)))
+
+    def commit(**kw):
+        a = dict(pages=layers, block_table=table, cached_len=i32([0] * 3), kv_len=z3, best_node=z3, node_parent=tree)
+        a.update(kw)
+        return lambda: ctx.kv_commit(**a)
+
+    bad += [commit(cached_len=z2), commit(kv_len=z2), commit(best_node=z2), commit(node_parent=tree[:2]), commit(node_parent=tree.view(-1)), commit(tok_offsets=z3, node_parent=z6),
+            commit(outputs=z2)]
+
+    def read(**kw):
+        a = dict(pages=pages, slots=z6, head_dim=64, dtype=torch.float32)
+        a.update(kw)
+        return lambda: ctx.kv_read(**a)
+
+    bad += [read(outputs=dict(k=k[:5], v=k)), read(outputs=dict(k=k, v=k[:5])), read(outputs=dict(k=k, v=k.to(torch.bfloat16))), read(head_dim=128)]
+    # int32, on the device, one after another
+    bad += [plan(cached_len=z3.long()), attend(kv_len=z3.cpu()), commit(best_node=i32([0] * 6)[::2]), read(slots=z6.long()),
+            plan(outputs=dict(new, positions=torch.zeros(T, device="cuda")))]
+    before = ctx.launch_count()
+    for i, f in enumerate(bad):
+        with pytest.raises((binding.AasdError, AssertionError)):
+            f()
+            raise RuntimeError("call %d was not refused" % i)
+    assert ctx.launch_count() == before and ctx.poll_status() == 0
+    # what goes together still goes
+    plan(outputs=new)()
+    attend(outputs=dict(out=torch.empty_like(q), lse=torch.zeros((T, 2), device="cuda")), kv_len=z7, node_parent=z7)()
+    write(outputs=dict(q=torch.empty_like(q)), slot_map=i32([-1] * 6))()
+    commit(best_node=i32([-1] * 3))()
+    read()()
+    assert ctx.poll_status() == 0
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_strides_of_single_tokens_and_heads_do_not_matter(ctx, dtype):
     """One token, or one head, is contiguous whatever the stride of that dimension says."""
