@@ -100,7 +100,7 @@ int aasd_kv_write(aasd_ctx* ctx, const void* q, const void* k, const void* v, co
     for (const void* x : {q, k, v, q_weight, k_weight, (const void*)q_out, (const void*)k_out})
         if (((uintptr_t)x % es) != 0) return AASD_ERR_INVALID_ARG;
     KvWriteArgs a{q, k, v, q_weight, k_weight, cos_sin, positions, slot_map, n_tokens, *p, static_cast<uint8_t*>(pages), q_out, k_out,
-                  ctx->state, 0u};
+                  ctx->state, 0u, make_float2(-0.f, -0.f)};
     // 16-byte accesses where every row of every operand starts on a 16-byte boundary
     bool vec = p->rotary_dim == 0 || aligned16(cos_sin);
     for (const void* x : {q, k, v, q_weight, k_weight, (const void*)q_out, (const void*)k_out}) vec = vec && aligned16(x);

@@ -429,7 +429,14 @@ struct KvWriteArgs {
     void *q_out, *k_out;
     DeviceState* state;
     unsigned int value_blocks;   // CTAs that store values; the others take queries and keys
+    float2 minus_zero;           // see mul2_rounded
 };
+
+// A product rounded by itself.  The assembler makes one fused multiply-add, which rounds once, of a
+// packed product and the packed sum behind it, whatever their rounding modes say (scalar ones are left
+// alone).  a * b + (-0) is the rounded product, as fast, and stays as it is as long as -0 is a number
+// that the compiler does not know: a launch argument.
+__device__ __forceinline__ float2 mul2_rounded(float2 a, float2 b, float2 minus_zero) { return __ffma2_rn(a, b, minus_zero); }
 
 #ifdef AASD_KV_TU
 // A CTA either takes query and key rows or stores values; both kinds share the launch.
@@ -607,12 +614,13 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteAr
     float2 u[4], v[4];
     rx.unpack(u);
     ry.unpack(v);
+    const float2 mz = a.minus_zero;
     // (the lanes of a row take the same way; shuffles stay among all lanes of the warp)
     if (a.q_weight != nullptr || a.k_weight != nullptr) {
         float s[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float2 q = __fadd2_rn(__fmul2_rn(u[e], u[e]), __fmul2_rn(v[e], v[e]));
+            const float2 q = __fadd2_rn(mul2_rounded(u[e], u[e], mz), mul2_rounded(v[e], v[e], mz));
             s[e] = __fadd_rn(q.x, q.y);
         }
         float sum = __fadd_rn(__fadd_rn(s[0], s[1]), __fadd_rn(s[2], s[3]));
@@ -644,7 +652,7 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteAr
             for (int e = 0; e < 4; ++e) {
                 if (part * H + 8 * l + 2 * e < rot) {
                     const float c = co[4 * part + e], n = si[4 * part + e];
-                    z[e] = __fadd2_rn(__fmul2_rn(z[e], make_float2(c, c)), __fmul2_rn(make_float2(z[e].y, z[e].x), make_float2(-n, n)));
+                    z[e] = __fadd2_rn(mul2_rounded(z[e], make_float2(c, c), mz), mul2_rounded(make_float2(z[e].y, z[e].x), make_float2(-n, n), mz));
                 }
             }
         }
@@ -653,8 +661,8 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteAr
         for (int e = 0; e < 4; ++e) {
             const float2 c = make_float2(co[2 * e], co[2 * e + 1]), n = make_float2(si[2 * e], si[2 * e + 1]);
             const float2 p = u[e], q = v[e];
-            u[e] = __fadd2_rn(__fmul2_rn(p, c), __fmul2_rn(q, make_float2(-n.x, -n.y)));
-            v[e] = __fadd2_rn(__fmul2_rn(q, c), __fmul2_rn(p, n));
+            u[e] = __fadd2_rn(mul2_rounded(p, c, mz), mul2_rounded(q, make_float2(-n.x, -n.y), mz));
+            v[e] = __fadd2_rn(mul2_rounded(q, c, mz), mul2_rounded(p, n, mz));
         }
     } else if (!FULL && rot > 0) {
         // a pair (c, c + half) inside the first rot channels: its members may be different lanes',

@@ -250,6 +250,50 @@ def test_strides_of_single_tokens_and_heads_do_not_matter(ctx, dtype):
     assert ctx.poll_status() == 0
 
 
+# ---- roundings --------------------------------------------------------------------------------------------
+
+def rounded32(x, w, cs, rot, inter, eps):
+    """Norm and rotation in numpy's fp32, whose every operation is rounded by itself: [T, H, D]."""
+    f = np.float32
+    D = x.shape[-1]
+    if w is not None:
+        s = x * x
+        s = s[..., :D // 2] + s[..., D // 2:]
+        while s.shape[-1] > 1:
+            s = s[..., 0::2] + s[..., 1::2]
+        x = (x * (f(1) / np.sqrt(s * f(1.0 / D) + f(eps)))) * w
+    half = rot // 2
+    y = x.copy()
+    a, b = (slice(0, rot, 2), slice(1, rot, 2)) if inter else (slice(0, half), slice(half, rot))
+    c, n = cs[:, None, :half], cs[:, None, half:rot]
+    y[..., a], y[..., b] = x[..., a] * c - x[..., b] * n, x[..., b] * c + x[..., a] * n
+    return y
+
+
+@pytest.mark.parametrize("D,rot,inter", [(64, 64, False), (128, 128, False), (256, 256, False), (128, 128, True), (128, 48, False), (64, 32, True)])
+@pytest.mark.parametrize("norm", [False, True])
+def test_write_rounds_every_operation_by_itself(ctx, D, rot, inter, norm):
+    """Whatever the form of the rotation: the outputs, and with them the keys' bytes, are numpy's to the bit."""
+    rng = np.random.default_rng(D + rot + norm)
+    T, Hq, Hkv = 70, 3, 2
+    x = rng.standard_normal((T, Hq + 2 * Hkv, D)).astype(np.float32)
+    w = [(1 + 0.2 * rng.standard_normal(D)).astype(np.float32) for _ in range(2)] if norm else [None, None]
+    cs = rng.standard_normal((T, rot)).astype(np.float32)
+    dev = torch.as_tensor(x).cuda()
+    pages = torch.zeros((2, Hkv, ref.head_bytes(D)), dtype=torch.uint8, device="cuda")
+    wd = [None if y is None else torch.as_tensor(y).cuda() for y in w]
+    o = ctx.kv_write(pages, dev[:, :Hq], dev[:, Hq:Hq + Hkv], dev[:, Hq + Hkv:], i32(np.arange(T)), i32(np.arange(T)), torch.as_tensor(cs).cuda(),
+                     *wd, interleaved=inter, keep_k=True)
+    assert ctx.poll_status() == 0
+    k = rounded32(x[:, Hq:Hq + Hkv], w[1], cs, rot, inter, 1e-6)
+    assert np.array_equal(o["q"].cpu().numpy(), rounded32(x[:, :Hq], w[0], cs, rot, inter, 1e-6))
+    assert np.array_equal(o["k"].cpu().numpy(), k)
+    raw = np.zeros(pages.shape, np.uint8)
+    for t in range(T):
+        ref.store(raw, t, ref.Entry(k[t], x[t, Hq + Hkv:]), D)
+    assert np.array_equal(pages.cpu().numpy(), raw)
+
+
 # ---- captured graphs and scratch -----------------------------------------------------------------------
 
 def attend_case(rng, D=64, dtype="bf16"):
