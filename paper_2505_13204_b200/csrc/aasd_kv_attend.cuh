@@ -263,7 +263,22 @@ __device__ __forceinline__ void kv_clear_rows(const KvAttendArgs& a, int D, int 
     const int lane = threadIdx.x & 31;
     const int Hq = a.p.n_q_heads;
     const bool padded = a.p.rows_per_seq > 0;
-    const auto clear = [&](long long lo, long long hi) {
+    const int items = padded || a.p.n_seqs == 0 ? a.p.n_seqs + 1 : a.p.n_seqs + 2;   // sequences, rows behind them, rows in front
+#pragma unroll 1
+    for (int b = warp; b < items; b += warps) {
+        long long lo, hi;
+        if (b < a.p.n_seqs) {
+            // (not KvSeq's first and rows, which are none where they do not all exist)
+            lo = padded ? (long long)b * a.p.rows_per_seq : a.tok_offsets[b];
+            hi = padded ? lo + a.p.rows_per_seq : a.tok_offsets[b + 1];
+            lo += total > 0 ? kv_load_seq(a, b, 8).fresh : 0;
+        } else if (b == a.p.n_seqs) {
+            lo = padded ? a.p.n_tokens : a.p.n_seqs > 0 ? a.tok_offsets[a.p.n_seqs] : 0;
+            hi = a.p.n_tokens;
+        } else {
+            lo = 0;
+            hi = a.tok_offsets[0];
+        }
         lo = lo < 0 ? 0 : lo;
         hi = hi < a.p.n_tokens ? hi : a.p.n_tokens;
         const long long e0 = lo * Hq * D, e1 = hi * Hq * D;
@@ -272,17 +287,6 @@ __device__ __forceinline__ void kv_clear_rows(const KvAttendArgs& a, int D, int 
         if (a.o.lse)
 #pragma unroll 1
             for (long long e = lo * Hq + lane; e < hi * Hq; e += 32) a.o.lse[e] = -CUDART_INF_F;
-    };
-#pragma unroll 1
-    for (int b = warp; b <= a.p.n_seqs; b += warps) {
-        if (b < a.p.n_seqs) {
-            // (not KvSeq's first and rows, which are none where they do not all exist)
-            const long long first = padded ? (long long)b * a.p.rows_per_seq : a.tok_offsets[b];
-            clear(first + (total > 0 ? kv_load_seq(a, b, 8).fresh : 0), padded ? first + a.p.rows_per_seq : a.tok_offsets[b + 1]);
-        } else if (!padded) {
-            if (a.p.n_seqs > 0) clear(0, a.tok_offsets[0]);
-            clear(a.p.n_seqs > 0 ? a.tok_offsets[a.p.n_seqs] : 0, a.p.n_tokens);
-        }
     }
 }
 
