@@ -55,8 +55,8 @@ struct KvAttendArgs {
 };
 
 constexpr int kKvMaxCtas = 160;        // CTAs of a launch (one per SM)
-constexpr float kKvNothing = -1.0e30f; // running maximum of a row that has seen nothing
-constexpr float kKvHidden = -2.0e30f;  // exponent of a key that the row does not see
+constexpr float kKvNothing = -3.0e38f; // running maximum of a row that has seen nothing (below any sum of products)
+constexpr float kKvHidden = -3.3e38f;  // exponent of a key that the row does not see
 
 // ---- what there is to do ---------------------------------------------------------------------------
 

@@ -294,6 +294,27 @@ def test_write_rounds_every_operation_by_itself(ctx, D, rot, inter, norm):
     assert np.array_equal(pages.cpu().numpy(), raw)
 
 
+@pytest.mark.parametrize("new,dtype", [(3, "f32"), (3, "bf16")])
+def test_attend_with_products_far_below_zero(ctx, new, dtype):
+    """Sums near -10^33, that is, far below anything but -inf: the largest of them still wins."""
+    rng = np.random.default_rng(new)
+    pool = Pool(rng, [150], 1, 64, garbage=False)
+    raw = pool.pages.cpu().numpy()
+    for c in range(150):
+        e = ref.Entry(np.abs(rng.standard_normal((1, 64))).astype(np.float32) * 1e16, rng.standard_normal((1, 64)).astype(np.float32))
+        ref.store(raw, int(pool.table[0, c // PAGE]) * PAGE + c % PAGE, e, 64)
+        pool.k[0][c], pool.v[0][c] = e.values("k"), e.values("v")
+    pool.pages = torch.as_tensor(raw).cuda()
+    q = -queries(rng, new, 4, 64, dtype, 1e16).abs()
+    o = ctx.kv_attend(q, pool.pages, i32(pool.table), i32([150 - new]), i32([150]), rows_per_seq=new, want_lse=True)
+    assert ctx.poll_status() == 0
+    qn, got, lse = f64(q), f64(o["out"]), f64(o["lse"])
+    for i in range(new):
+        _, wl, size = ref.attend(qn[i], pool.k[0], pool.v[0], list(range(151 - new + i)), 0.125)
+        assert (wl < -1e31).all() and (np.abs(lse[i] - wl) <= size * 2.0 ** -20 + 2.0 ** -21 * np.abs(wl)).all()
+        assert (np.abs(got[i]).max(-1) > 0).all() and np.abs(got[i]).max() <= np.abs(pool.v[0]).max() * (1 + 2.0 ** -7)
+
+
 # ---- captured graphs and scratch -----------------------------------------------------------------------
 
 def attend_case(rng, D=64, dtype="bf16"):
