@@ -43,6 +43,10 @@ constexpr int kTileRaw = 4, kTileKeys = 3, kTileValues = 4, kTileMeta = 6;   // 
 constexpr int kTilePieces = 8;
 // the probabilities' power of two (see the split kernel): the maximum may lag by what is left of fp16's range
 constexpr float kTileP = 7.f;
+// Exponents from which products are scaled in an operation of their own.  Below, the scaling is fused with the
+// subtraction of the rounded maximum: what its rounding left out, at most 2^-5 here, is a factor that the row's
+// probabilities and their sum share.  At 2^28 that factor would leave fp16's range.
+constexpr float kTileLarge = 1048576.f;
 
 // ---- the list of work ---------------------------------------------------------------------------------
 
@@ -674,7 +678,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
             // places up to which every row of the warp sees everything
             const int open_to = a.node_parent != nullptr ? w.cached : w.cached + row0 / G + 1;
             int ev = 64;
-            bool first = true;
+            bool first = true, large = false;
 #pragma unroll 1
             for (int i = PAIR ? 0 : (n0 ^ x) & 1; i < np; i += PAIR ? 1 : 2) {
                 const int n = n0 + i, mslot = n % kTileMeta, pg = w.pg + i, buf = taken & 1;
@@ -718,21 +722,36 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                         }
                     }
                     // Probabilities with the maximum as it stands; only where a thread's sum of them leaves fp16's range (by a
-                    // new maximum at least 2^5 above it), and on the first page, is the maximum looked for and this done again.
+                    // new maximum at least 2^5 above it), on the first page, and with large products, is the maximum looked for
+                    // and this done again.
                     float ls[4];
-                    bool again = first;
+                    bool again = first || large;
+                    float rr = rf;             // what S is still to be multiplied by
 #pragma unroll 1
                     for (;;) {
                         if (again) {
-                            float fo[4];
+                            float fo[4], m[4], top = 0.f;
 #pragma unroll
                             for (int q = 0; q < 4; ++q) {
-                                float m = -CUDART_INF_F;
+                                m[q] = -CUDART_INF_F;
 #pragma unroll
-                                for (int k = 0; k < 8; ++k) m = fmaxf(m, fmaxf(s[q >> 1][4 * k + 2 * (q & 1)], s[q >> 1][4 * k + 2 * (q & 1) + 1]));
-                                m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-                                m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-                                const float mn = fmaxf(mref[q], m * rf);
+                                for (int k = 0; k < 8; ++k) m[q] = fmaxf(m[q], fmaxf(s[q >> 1][4 * k + 2 * (q & 1)], s[q >> 1][4 * k + 2 * (q & 1) + 1]));
+                                m[q] = fmaxf(m[q], __shfl_xor_sync(0xFFFFFFFFu, m[q], 1));
+                                m[q] = fmaxf(m[q], __shfl_xor_sync(0xFFFFFFFFu, m[q], 2));
+                                m[q] *= rf;
+                                if (m[q] > -CUDART_INF_F) top = fmaxf(top, fabsf(m[q]));
+                            }
+                            large = large || __any_sync(0xFFFFFFFFu, top >= kTileLarge);
+                            if (large) {
+                                rr = 1.f;
+#pragma unroll
+                                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                                    for (int k = 0; k < 32; ++k) s[half][k] *= rf;
+                            }
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                const float mn = fmaxf(mref[q], m[q]);
                                 fo[q] = ex2_approx(mref[q] - mn);
                                 mref[q] = mn;
                                 l[q] *= fo[q];
@@ -753,7 +772,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
                                 const int q = 2 * half + e;
-                                const float2 ff = make_float2(rf, rf), mm = make_float2(kTileP - mref[q], kTileP - mref[q]);
+                                const float2 ff = make_float2(rr, rr), mm = make_float2(kTileP - mref[q], kTileP - mref[q]);
                                 float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
                                 for (int k = 0; k < 8; ++k) {

@@ -294,7 +294,7 @@ def test_write_rounds_every_operation_by_itself(ctx, D, rot, inter, norm):
     assert np.array_equal(pages.cpu().numpy(), raw)
 
 
-@pytest.mark.parametrize("new,dtype", [(3, "f32"), (3, "bf16")])
+@pytest.mark.parametrize("new,dtype", [(3, "f32"), (3, "bf16"), (20, "bf16"), (40, "bf16")])
 def test_attend_with_products_far_below_zero(ctx, new, dtype):
     """Sums near -10^33, that is, far below anything but -inf: the largest of them still wins."""
     rng = np.random.default_rng(new)
@@ -384,3 +384,39 @@ def test_scratch_of_a_call_that_is_captured_first_is_not_taken_for_cleared():
         assert torch.equal(first["out"], second["out"]) and bool(torch.isfinite(first["out"]).all()) and c.poll_status() == 0
     finally:
         c.close()
+
+
+# ---- branches of the many-row kernel ------------------------------------------------------------------
+
+# tokens, query heads of one key head: one tile of 128 rows (two groups on alternate pages), a pair of tiles
+TILES = [(16, 4), (35, 4)]
+
+
+def replace(pool, which, entry):
+    """Other entries at places {(sequence, place)}."""
+    raw = pool.pages.cpu().numpy()
+    for b, c in which:
+        e = entry(b, c)
+        ref.store(raw, int(pool.table[b, c // PAGE]) * PAGE + c % PAGE, e, pool.D)
+        pool.k[b][c], pool.v[b][c] = e.values("k"), e.values("v")
+    pool.pages = torch.as_tensor(raw).cuda()
+
+
+@pytest.mark.parametrize("new,G", TILES)
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("size", [1e4, 1e7, 1e15])
+def test_tiles_whose_products_are_larger_than_fp32_counts(ctx, new, G, sign, size):
+    """At 2^24 and more the products' own roundings decide the weights: the results stay means of the values,
+    and the lse the largest product."""
+    rng = np.random.default_rng(56)
+    pool = Pool(rng, [390], 1, 64)
+    replace(pool, [(0, c) for c in range(390)], lambda b, c: ref.Entry(np.abs(rng.standard_normal((1, 64))).astype(np.float32) * size,
+                                                                        rng.standard_normal((1, 64)).astype(np.float32)))
+    q = queries(rng, new, G, 64, "bf16", size).abs() * sign
+    o = ctx.kv_attend(q, pool.pages, i32(pool.table), i32([390 - new]), i32([390]), rows_per_seq=new, want_lse=True)
+    assert ctx.poll_status() == 0
+    got, lse, qn, top = f64(o["out"]), f64(o["lse"]), f64(q), np.abs(pool.v[0]).max()
+    for i in range(new):
+        _, wl, most = ref.attend(qn[i], pool.k[0], pool.v[0], list(range(391 - new + i)), 0.125)
+        assert (np.abs(lse[i] - wl) <= most * 2.0 ** -20 + 2.0 ** -21 * np.abs(wl)).all()
+        assert (np.abs(got[i]).max(-1) > 0).all() and np.abs(got[i]).max() <= top * (1 + 2.0 ** -7)
