@@ -386,6 +386,58 @@ def test_scratch_of_a_call_that_is_captured_first_is_not_taken_for_cleared():
         c.close()
 
 
+def test_a_steps_calls_replayed_from_a_graph(ctx):
+    """Plan, write, attend and commit as one graph: two replays over changed inputs give what the calls give."""
+    rng = np.random.default_rng(34)
+    B, cap, Hq, Hkv, D = 3, 9, 8, 2, 64
+    P, pool = 6, 20
+    parent = i32(np.stack([_tree(rng, cap) for _ in range(B)]))
+    depth = i32([[len(ref.path_of(i, parent.cpu().numpy()[b])) - 1 for i in range(cap)] for b in range(B)])
+    cs = torch.as_tensor(rng.standard_normal((400, D)).astype(np.float32)).cuda()
+
+    def state(seed):
+        r = np.random.default_rng(seed)
+        x = torch.as_tensor(r.standard_normal((B * cap, Hq + 2 * Hkv, D)).astype(np.float32)).to(torch.bfloat16).cuda()
+        return dict(x=x, best=i32(r.integers(0, cap, B)))
+
+    def books():
+        return dict(pages=torch.zeros((1, pool, Hkv, ref.head_bytes(D)), dtype=torch.uint8, device="cuda"), table=i32(np.full((B, P), -1)),
+                    held=i32([0] * B), free=i32(np.arange(pool)), n_free=i32([pool]), length=i32([0] * B), new=i32([cap] * B))
+
+    def step(s, k):
+        plan = ctx.kv_plan(k["length"], k["new"], k["table"], k["held"], k["free"], k["n_free"], B * cap, cap, depth.view(-1))
+        x = s["x"]
+        q = ctx.kv_write(k["pages"][0], x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], plan["slot_map"], plan["positions"], cs)["q"]
+        out = ctx.kv_attend(q, k["pages"][0], k["table"], k["length"], plan["kv_len"], rows_per_seq=cap, node_parent=parent.view(-1))["out"]
+        k["length"].copy_(ctx.kv_commit(k["pages"], k["table"], k["length"], plan["kv_len"], s["best"], parent))
+        return out
+
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    try:
+        with torch.cuda.stream(side):
+            ctx.set_stream(side)
+            a, want = books(), []
+            inputs = [state(40 + i) for i in range(3)]
+            for s in inputs:
+                want.append(step(s, a).clone())
+            b, held = books(), {k: v.clone() for k, v in inputs[0].items()}
+            side.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                out = step(held, b)
+            for s, w in zip(inputs, want):
+                for k in held:
+                    held[k].copy_(s[k])
+                g.replay()
+                side.synchronize()
+                assert torch.equal(out, w)
+            assert all(torch.equal(a[k], b[k]) for k in a)
+    finally:
+        ctx.set_stream(torch.cuda.current_stream())
+    assert ctx.poll_status() == 0
+
+
 # ---- branches of the many-row kernel ------------------------------------------------------------------
 
 # tokens, query heads of one key head: one tile of 128 rows (two groups on alternate pages), a pair of tiles
@@ -400,6 +452,50 @@ def replace(pool, which, entry):
         ref.store(raw, int(pool.table[b, c // PAGE]) * PAGE + c % PAGE, e, pool.D)
         pool.k[b][c], pool.v[b][c] = e.values("k"), e.values("v")
     pool.pages = torch.as_tensor(raw).cuda()
+
+
+def causal(kv, new):
+    return {b * new + i: (b, list(range(n - new + i + 1))) for b, n in enumerate(kv) for i in range(new)}
+
+
+@pytest.mark.parametrize("new,G", TILES)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kscale,vscale,qscale", [(4.0, 1e-4, 3.0), (0.01, 3e4, 1.0), (1.0, 1.0, 1e3), (1e-3, 1.0, 1e-3)])
+def test_tiles_with_large_products_and_values_of_any_size(ctx, new, G, D, kscale, vscale, qscale):
+    rng = np.random.default_rng(50)
+    kv = [300, 70]
+    pool = Pool(rng, kv, 2, D, kscale, vscale)
+    q = queries(rng, 2 * new, 2 * G, D, "bf16", qscale)
+    o = ctx.kv_attend(q, pool.pages, i32(pool.table), i32([n - new for n in kv]), i32(kv), rows_per_seq=new, want_lse=True,
+                      outputs=nan_outputs(2 * new, 2 * G, D, "bf16"))
+    assert ctx.poll_status() == 0
+    check_rows(pool, q, o, causal(kv, new))
+
+
+@pytest.mark.parametrize("new,G", TILES)
+@pytest.mark.parametrize("page", [0, 1, 3])
+def test_tiles_whose_values_grow_by_2_to_the_20_on_one_page(ctx, new, G, page):
+    rng = np.random.default_rng(51)
+    pool = Pool(rng, [390], 1, 128)
+    replace(pool, [(0, page * PAGE + 17)], lambda b, c: ref.Entry(rng.standard_normal((1, 128)), rng.standard_normal((1, 128)).astype(np.float32) * 2.0 ** 20))
+    q = queries(rng, new, G, 128, "bf16")
+    o = ctx.kv_attend(q, pool.pages, i32(pool.table), i32([390 - new]), i32([390]), rows_per_seq=new, want_lse=True)
+    assert ctx.poll_status() == 0
+    check_rows(pool, q, o, causal([390], new))
+
+
+@pytest.mark.parametrize("new,G", TILES)
+def test_tiles_whose_products_rise_from_page_to_page(ctx, new, G):
+    """Every later page's products are far above all that came before: O is rescaled each time."""
+    rng = np.random.default_rng(52)
+    pool = Pool(rng, [390], 1, 64)
+    grow = [1, 30, 200, 1000, 3000, 10000, 30000]
+    replace(pool, [(0, c) for c in range(390)], lambda b, c: ref.Entry(np.abs(rng.standard_normal((1, 64))).astype(np.float32) * grow[c // PAGE],
+                                                                        rng.standard_normal((1, 64)).astype(np.float32)))
+    q = queries(rng, new, G, 64, "bf16").abs()
+    o = ctx.kv_attend(q, pool.pages, i32(pool.table), i32([390 - new]), i32([390]), rows_per_seq=new, want_lse=True)
+    assert ctx.poll_status() == 0
+    check_rows(pool, q, o, causal([390], new))
 
 
 @pytest.mark.parametrize("new,G", TILES)
@@ -420,3 +516,66 @@ def test_tiles_whose_products_are_larger_than_fp32_counts(ctx, new, G, sign, siz
         _, wl, most = ref.attend(qn[i], pool.k[0], pool.v[0], list(range(391 - new + i)), 0.125)
         assert (np.abs(lse[i] - wl) <= most * 2.0 ** -20 + 2.0 ** -21 * np.abs(wl)).all()
         assert (np.abs(got[i]).max(-1) > 0).all() and np.abs(got[i]).max() <= top * (1 + 2.0 ** -7)
+
+
+@pytest.mark.parametrize("new,G", TILES)
+def test_tiles_with_a_scale_and_unaligned_queries_and_results(ctx, new, G):
+    rng = np.random.default_rng(53)
+    kv = [130, 41]
+    pool = Pool(rng, kv, 2, 64)
+    buf = queries(rng, 2 * new, 1, 2 * G * 64 + 3, "bf16")[:, 0]
+    q = buf[:, 1:1 + 2 * G * 64].unflatten(1, (2 * G, 64))
+    o = ctx.kv_attend(q, pool.pages, i32(pool.table), i32([n - new for n in kv]), i32(kv), rows_per_seq=new, scale=0.37, want_lse=True,
+                      outputs=nan_outputs(2 * new, 2 * G, 64, "bf16", shift=1))
+    assert ctx.poll_status() == 0
+    check_rows(pool, q, o, causal(kv, new), scale=0.37)
+
+
+@pytest.mark.parametrize("new,G", TILES + [(3, 4)])
+@pytest.mark.parametrize("gone", [(0,), (1,), (2, 3), (0, 1, 2, 3, 4, 5, 6)])
+def test_pages_that_the_table_does_not_name_are_not_seen(ctx, new, G, gone):
+    rng = np.random.default_rng(54)
+    pool = Pool(rng, [390], 1, 64)
+    table = pool.table.copy()
+    for p in gone:
+        table[0, p] = -1 if p % 2 else pool.pages.shape[0] + 3
+    q = queries(rng, new, G, 64, "bf16")
+    o = ctx.kv_attend(q, pool.pages, i32(table), i32([390 - new]), i32([390]), rows_per_seq=new, want_lse=True,
+                      outputs=nan_outputs(new, G, 64, "bf16"))
+    assert ctx.poll_status() == binding.STATUS_BAD_OFFSETS
+    check_rows(pool, q, o, {t: (b, [c for c in vis if c // PAGE not in gone]) for t, (b, vis) in causal([390], new).items()})
+
+
+@pytest.mark.parametrize("new,G", TILES + [(3, 4)])
+def test_parents_that_do_not_precede_their_children_end_the_path(ctx, new, G):
+    rng = np.random.default_rng(55)
+    pool = Pool(rng, [200], 1, 64)
+    parent = _tree(rng, new)
+    parent[1], parent[new - 1] = 1, new + 5
+    q = queries(rng, new, G, 64, "bf16")
+    o = ctx.kv_attend(q, pool.pages, i32(pool.table), i32([200 - new]), i32([200]), rows_per_seq=new, node_parent=i32(parent), want_lse=True)
+    assert ctx.poll_status() == binding.STATUS_BAD_OFFSETS
+    rows = {}
+    for i in range(new):
+        path, x = [], i
+        while x >= 0:
+            path.append(x)
+            x = int(parent[x]) if parent[x] < x else -1
+        rows[i] = (0, list(range(200 - new)) + [200 - new + x for x in sorted(path)])
+    check_rows(pool, q, o, rows)
+
+
+@pytest.mark.parametrize("new", [(1,) * 12 + (200,), (200,) + (1,) * 70, (1, 90, 1, 0, 33, 1, 2)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_chunks_and_single_tokens_in_one_packed_call(ctx, new, D):
+    """Whichever kernel the mean length chooses, with room left behind the last sequence."""
+    rng = np.random.default_rng(sum(new))
+    cached = rng.integers(0, 200, len(new))
+    kv = cached + np.array(new)
+    pool = Pool(rng, kv, 1, D)
+    offs = np.concatenate([[0], np.cumsum(new)])
+    T = int(offs[-1]) + 9
+    q = queries(rng, T, 4, D, "bf16")
+    o = ctx.kv_attend(q, pool.pages, i32(pool.table), i32(cached), i32(kv), i32(offs), want_lse=True, outputs=nan_outputs(T, 4, D, "bf16"))
+    assert ctx.poll_status() == 0
+    check_rows(pool, q, o, {int(offs[b]) + i: (b, list(range(int(cached[b]) + i + 1))) for b in range(len(new)) for i in range(new[b])})
