@@ -208,6 +208,7 @@ __device__ __forceinline__ void kv_place_token(const KvPlanArgs& a, int64_t t, i
     const int cached = a.cached_len[b];
     const int64_t at = (int64_t)cached + i;
     if (i < 0 || at >= a.o.kv_len[b]) return;
+    if (!AASD_IN_RANGE(b < a.p.n_seqs && at >= 0 && at / kPage < a.p.max_pages && t < a.p.n_tokens, a.state)) return;
     const int page = a.s.block_table[(int64_t)b * a.p.max_pages + at / kPage];
     if (page < 0 || page >= a.p.n_pages) {
         raise(a.state, AASD_STATUS_BAD_OFFSETS);
@@ -271,6 +272,7 @@ __global__ void __launch_bounds__(NT) kv_plan_kernel(const KvPlanArgs a) {
         __syncthreads();
         for (int r = tid; r < (int)total; r += NT) {
             const int k = last_not_above(s_first, NT, r);
+            if (!AASD_IN_RANGE(base + k < B && s_at[k] >= 0 && s_at[k] + (r - s_first[k]) < P, a.state)) continue;
             int32_t* entry = a.s.block_table + (int64_t)(base + k) * P + s_at[k] + (r - s_first[k]);
             const int page = *entry;
             *entry = AASD_NONE;
@@ -315,13 +317,15 @@ __global__ void __launch_bounds__(NT) kv_plan_kernel(const KvPlanArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int r = r0 + e * NT;
-                page[e] = r < (int)got ? a.s.free_pages[n_free - 1 - (asked + r)] : 0;
+                const bool there = r < (int)got && AASD_IN_RANGE(n_free - 1 - (asked + r) >= 0 && n_free <= a.p.n_pages, a.state);
+                page[e] = there ? a.s.free_pages[n_free - 1 - (asked + r)] : 0;
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int r = r0 + e * NT;
                 if (r >= (int)got) break;
                 const int k = last_not_above(s_first, NT, r);
+                if (!AASD_IN_RANGE(n_free - 1 - (asked + r) >= 0 && base + k < B && s_at[k] >= 0 && s_at[k] + (r - s_first[k]) < P, a.state)) continue;
                 a.s.free_pages[n_free - 1 - (asked + r)] = AASD_NONE;
                 if (page[e] < 0 || page[e] >= a.p.n_pages) bits |= AASD_STATUS_BAD_OFFSETS;
                 a.s.block_table[(int64_t)(base + k) * P + s_at[k] + (r - s_first[k])] = page[e];
@@ -773,7 +777,7 @@ __global__ void __launch_bounds__(kWriteThreads) kv_read_kernel(const KvReadArgs
         float x[8], y[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = y[e] = 0.f;
-        if (at != AASD_NONE) {
+        if (at != AASD_NONE && AASD_IN_RANGE(at >= 0 && at / kPage < a.n_pages && head < hkv, a.state)) {
             const uint8_t* block = a.pages + ((int64_t)(at / kPage) * hkv + head) * kv_head_bytes(D);
             const int off = at % kPage;
             const unsigned long long bytes = value ? *reinterpret_cast<const unsigned long long*>(s_code + q * kPitch + 8 * l)
@@ -839,6 +843,7 @@ __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const KvCommi
         }
         return;
     }
+    if (!AASD_IN_RANGE(best < AASD_KV_MAX_NODES && first >= 0, a.state)) return;
     for (int i = tid; i <= best; i += kCommitThreads) s_node[i] = a.node_parent[first + i];
     if (tid == 0) s_bad = 0;
     __syncthreads();
@@ -893,6 +898,13 @@ __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const KvCommi
             unsigned int kw[NB][KW], meta[NB];
             uint8_t vb[NB][VW];
             int dst[NB];
+            bool inside = true;   // (checked builds: every slot of the batch, by every lane alike)
+#pragma unroll
+            for (int e = 0; e < NB; ++e) {
+                const int at = min(i0 + e, len - 1);
+                inside = inside && AASD_IN_RANGE(s_node[at] >= 0 && s_node[at] / kPage < a.p.n_pages && slot_of(at) >= 0 && layer < a.p.n_layers, a.state);
+            }
+            if (!inside) break;
 #pragma unroll
             for (int e = 0; e < NB; ++e) {
                 const int src = s_node[min(i0 + e, len - 1)];

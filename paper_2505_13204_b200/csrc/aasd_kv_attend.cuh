@@ -339,6 +339,7 @@ __device__ __forceinline__ void kv_join_row(const KvAttendArgs& a, const KvPiece
         const float inv = L > 0.f ? 1.f / L : 0.f;
         const int row = pc.row0 + r;
         const long long head = ((long long)pc.first + row / G) * a.p.n_q_heads + pc.h * G + row % G;
+        if (!AASD_IN_RANGE(parts <= kKvMaxCtas && head < a.p.n_tokens * a.p.n_q_heads, a.state)) continue;
         store4<DT>(a.o.out, head * D + ch, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), a.out_vec);
         if (a.o.lse != nullptr && ch == 0) a.o.lse[head] = L > 0.f ? (M + log2f(L)) * (float)kLn2 : -CUDART_INF_F;
     }
@@ -477,7 +478,8 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
                 ids = ids_at + lane < ahead.s.pages ? ahead.table[ids_at + lane] : -1;
             }
             const int page = __shfl_sync(0xFFFFFFFFu, ids, ahead.pg - ids_at);
-            const bool ok = page >= 0 && page < a.p.n_pages;
+            const bool ok = page >= 0 && page < a.p.n_pages &&
+                            AASD_IN_RANGE(ahead.b < B && ahead.h < a.p.n_kv_heads && ahead.pg < ahead.s.pages && ahead.pg < a.p.max_pages, a.state);
             missing = (missing & ~(1u << stage)) | (ok ? 0u : 1u << stage);
             if (lane == 0) {
                 if (ok) {
@@ -531,7 +533,7 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
                 for (int nt = 0; nt < NT; ++nt) {
                     // lane (g, j): row 8 nt + g, channels (H / 4) j .. of each half
                     const int row = at.row0 + 8 * nt + g;
-                    const bool valid = row < at.fresh * G;
+                    const bool valid = row < at.fresh * G && AASD_IN_RANGE(row >= 0 && at.first + row / G < a.p.n_tokens && at.h < a.p.n_kv_heads, a.state);
                     const long long tok = at.first + (valid ? row / G : 0);
                     const long long q0 = tok * a.p.q_stride + (long long)(at.h * G + (valid ? row % G : 0)) * D + (H / 4) * j;
                     float top = 0.f, sum = 0.f;
@@ -837,7 +839,7 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
                                 a.o.lse[head] = ls > 0.f ? (mref[nt][col] + log2f(ls)) * (float)kLn2 : -CUDART_INF_F;
                             }
                         }
-                        if (r < n) {
+                        if (r < n && AASD_IN_RANGE(c < kKvMaxCtas && head < a.p.n_tokens * a.p.n_q_heads, a.state)) {
 #pragma unroll
                             for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -877,6 +879,7 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
             const float inv = L > 0.f ? 1.f / L : 0.f;
             const int row = pc.row0 + r;
             const long long head = ((long long)pc.first + row / G) * a.p.n_q_heads + pc.h * G + row % G;
+            if (!AASD_IN_RANGE(head < a.p.n_tokens * a.p.n_q_heads, a.state)) return;
             store4<DT>(a.o.out, head * D + ch, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), a.out_vec);
             if (a.o.lse != nullptr && ch == 0) a.o.lse[head] = L > 0.f ? (M + log2f(L)) * (float)kLn2 : -CUDART_INF_F;
         };

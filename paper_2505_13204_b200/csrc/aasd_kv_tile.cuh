@@ -384,6 +384,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                 const KvTilePiece& w = sh.piece[k % kTilePieces];
                 const int np = w.np, pg = w.pg;
                 if (np == 0) break;
+                const bool inside = AASD_IN_RANGE(w.b < B && w.h < a.p.n_kv_heads && pg + np <= a.p.max_pages, a.state);
                 const int32_t* table = a.block_table + (long long)w.b * a.p.max_pages + pg;
                 const uint8_t* head = a.pages + (long long)w.h * kv_head_bytes(D);
                 const u64 stride = (u64)a.p.n_kv_heads * kv_head_bytes(D);
@@ -392,7 +393,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                 int ids = 0;
 #pragma unroll 1
                 for (int i = 0; i < np; ++i, ++n) {
-                    if ((i & 31) == 0) ids = i + lane < np ? table[i + lane] : -1;
+                    if ((i & 31) == 0) ids = i + lane < np && inside ? table[i + lane] : -1;
                     const int page = __shfl_sync(0xFFFFFFFFu, ids, i & 31);
                     const int slot = n % kTileRaw;
                     ok = wait(&sh.raw_empty[slot], ((n / kTileRaw) & 1) ^ 1);
@@ -602,7 +603,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
             if (np == 0) break;
             if (lane == 0) mbar_arrive(&sh.piece_empty[piece % kTilePieces]);
             const int row0 = w.tile * R + (PAIR ? x * kTileRows : 0) + row_base;   // of the warp's first row, among the head's
-            const int rows_here = w.fresh * G;                                    // rows of the head
+            const int rows_here = AASD_IN_RANGE(w.first + w.fresh <= a.p.n_tokens && w.h < a.p.n_kv_heads, a.state) ? w.fresh * G : 0;   // rows of the head
             const int own_row = max(min(row0 + lane, rows_here - 1), 0);   // the lane's row: what the warp wants to know of its 32 rows
             const int token = own_row / G, member = own_row - token * G;
             if (PAIR || x == 0) {
@@ -822,7 +823,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
             }
             const bool complete = w.pg == 0 && np == w.pages;
             const int which = w.pg > 0 ? 0 : 1;
-            const int rows = min(R, rows_here - w.tile * R);
+            const int rows = AASD_IN_RANGE(c < kKvMaxCtas, a.state) ? min(R, rows_here - w.tile * R) : 0;
             constexpr int kPart = R * D + 2 * R;
             float* part = a.cta_parts + (long long)(c * 2 + which) * kPart;
             float own[4], other[4];        // factors of this group's O, and of the other's
