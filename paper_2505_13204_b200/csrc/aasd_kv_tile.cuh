@@ -961,6 +961,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
             tc_fence_before();
             n0 += np;
         }
+        if (!ok) tc_wait_store();   // (a group that gave up may have stores on their way to the memory that is freed below)
         // the segment that this CTA begins and others go on with: the joining kernel's work
         if (tid == 0) {
             KvTileOpen o{sh.open, 0};
