@@ -595,7 +595,8 @@ int aasd_probe_read(aasd_ctx* ctx, const void* buffer, size_t bytes, uint32_t* s
  * then ends like any other, with invalid results for the rows concerned and a workspace that
  * has to be registered again.  This call lets a test see that happen without any fault: it
  * arms, for the NEXT launch of the streaming kernel made through this context (by
- * aasd_verify, aasd_align_sample, aasd_step or aasd_verify_tree) and for that launch only,
+ * aasd_verify, aasd_align_sample, aasd_step or aasd_verify_tree), or of an attention kernel (by
+ * aasd_kv_attend: see below), and for that launch only,
  *   - a wait limit of `wait_limit` polls (>= 1024) instead of the default 2^24, and
  *   - the CTA that handles work item `item` (a logits row when the call has at least twice
  *     as many rows as the device has SMs, else a piece of a row) never issuing the copy of
@@ -603,7 +604,9 @@ int aasd_probe_read(aasd_ctx* ctx, const void* buffer, size_t bytes, uint32_t* s
  * The consumers of that CTA run out of polls, the CTA leaves, the other CTAs finish their
  * rows, and aasd_poll_status shows AASD_STATUS_TIMEOUT.  Afterwards: aasd_workspace_init on
  * the workspace, and the context works as before.  Nothing is armed when `item` lies beyond
- * the launch's items (the limit still applies).  Not for production use. */
+ * the launch's items (the limit still applies).  In aasd_kv_attend page number `item` of those
+ * that the first CTA asks for at its start never arrives; `tile` is not looked at, and
+ * aasd_kv_workspace_init is what clears up afterwards.  Not for production use. */
 int aasd_debug_withhold_tile(aasd_ctx* ctx, int64_t item, int32_t tile, uint32_t wait_limit);
 
 /* ---- verification for callers that cannot allocate ------------------------------- */

@@ -376,8 +376,9 @@ class Context:
         return int(self.lib.aasd_launch_count(self._h))
 
     def debug_withhold_tile(self, item: int, tile: int, wait_limit: int):
-        """aasd_debug_withhold_tile: the next streaming launch never copies one tile and gives
-        up its waits after ``wait_limit`` polls (a testing aid, see include/aasd.h)."""
+        """aasd_debug_withhold_tile: the next streaming launch never copies one tile (one page never arrives
+        in the next ``kv_attend``) and gives up its waits after ``wait_limit`` polls (a testing aid, see
+        include/aasd.h)."""
         _check(self.lib.aasd_debug_withhold_tile(self._h, int(item), int(tile), int(wait_limit)),
                "aasd_debug_withhold_tile")
 

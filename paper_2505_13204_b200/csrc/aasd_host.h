@@ -185,7 +185,7 @@ struct aasd_ctx {
     aasd::Tuning tuning;
     std::map<void*, aasd::WorkspaceLayout> workspaces;
     std::map<void*, int> kv_workspaces;   // head_dim that the scratch of aasd_kv_attend was registered for
-    // testing aid, armed by aasd_debug_withhold_tile and used up by the next streaming launch
+    // testing aid, armed by aasd_debug_withhold_tile and used up by the next streaming or attention launch
     long long withhold_item = -1;
     int withhold_tile = 0;
     unsigned int test_wait_limit = 0;

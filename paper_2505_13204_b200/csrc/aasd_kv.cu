@@ -242,6 +242,13 @@ int aasd_kv_attend(aasd_ctx* ctx, const void* q, const void* pages, const int32_
     a.out_vec = aligned16(o->out);
     a.scale_log2 = (p->scale > 0.f ? p->scale : 1.0f / sqrtf((float)p->head_dim)) * kLog2e;
     a.state = ctx->state;
+    a.wait_limit = kWaitLimit;
+    a.withhold_page = -1;
+    if (ctx->withhold_item >= 0) {
+        a.wait_limit = ctx->test_wait_limit;
+        a.withhold_page = ctx->withhold_item < 0x7FFFFFFF ? (int)ctx->withhold_item : 0x7FFFFFFF;
+        ctx->withhold_item = -1;
+    }
     AASD_CUDA(cudaSetDevice(ctx->device));
     const LaunchEnv env{ctx->stream, ctx->device};
     int launches = 0;

@@ -52,7 +52,19 @@ struct KvAttendArgs {
     float* cta_parts;             // scratch: partial results of segments that several CTAs share
     KvTileOpen* tile_open;        // scratch, one per CTA of the tile kernel
     float* warp_parts;            // scratch: a warp's first piece, when it goes on to another segment
+    unsigned int wait_limit;      // polls after which a wait inside the kernels gives up (kWaitLimit)
+    int withhold_page;            // testing aid (aasd_debug_withhold_tile): the first CTA's page of this number never arrives; -1: none
 };
+
+// Bounded wait (see mbar_wait).  The call's limit is looked at every 256 polls, off the path of waits that end.
+__device__ __forceinline__ bool kv_wait(const KvAttendArgs& a, u64* bar, unsigned int parity, volatile int* abort_flag) {
+#pragma unroll 1
+    for (unsigned int it = 0; it < kWaitLimit; ++it) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((it & 255u) == 255u && (*abort_flag || it > a.wait_limit)) break;
+    }
+    return false;
+}
 
 constexpr int kKvMaxCtas = 160;        // CTAs of a launch (one per SM)
 constexpr float kKvNothing = -3.0e38f; // running maximum of a row that has seen nothing (below any sum of products)
@@ -406,7 +418,7 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
     const int g = lane >> 2, j = lane & 3;
     if (tid == 0) {
 #pragma unroll 1
-        for (int i = 0; i < W * S; ++i) mbar_init(&sh.full[0][0] + i, 1);
+        for (int i = 0; i < W * S; ++i) mbar_init(&sh.full[0][0] + i, blockIdx.x == 0 && i == a.withhold_page ? 2 : 1);   // (the second arrival never comes)
         sh.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -590,7 +602,7 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
                 }
             }
             // (the lanes of a warp go on, or give up, together)
-            if (!__all_sync(0xFFFFFFFFu, mbar_wait(&full[stage], phase, abort_flag, kWaitLimit))) {
+            if (!__all_sync(0xFFFFFFFFu, kv_wait(a, &full[stage], phase, abort_flag))) {
                 give_up(abort_flag, a.state);
                 break;
             }
@@ -859,7 +871,7 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
         }
         if (*abort_flag) {   // nothing may be on its way into this CTA's shared memory when it leaves
             for (int s = 0; s < S; ++s)
-                for (unsigned int it = 0; it < kWaitLimit && s < issued && !mbar_try_wait(&full[s], ((unsigned int)((issued - 1 - s) / S)) & 1u); ++it) {}
+                for (unsigned int it = 0; it < a.wait_limit && s < issued && !mbar_try_wait(&full[s], ((unsigned int)((issued - 1 - s) / S)) & 1u); ++it) {}
         }
     }
     __syncthreads();

@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
         }
 #pragma unroll 1
         for (int i = 0; i < kTileRaw; ++i) {
-            mbar_init(&sh.raw_full[i], 1);
+            mbar_init(&sh.raw_full[i], blockIdx.x == 0 && i == a.withhold_page ? 2 : 1);   // (testing aid: the second arrival never comes)
             mbar_init(&sh.raw_empty[i], 4);
         }
 #pragma unroll 1
@@ -287,14 +287,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
     volatile int* abort_flag = &sh.abort_flag;
     const int c = blockIdx.x, total = kv_total(a, sum);
     // Waits are bounded; a role that gives up says so when it leaves, and the others find out in theirs.
-    const auto wait_one = [&](u64* bar, unsigned int parity) {
-#pragma unroll 1
-        for (unsigned int it = 0; it < kWaitLimit; ++it) {
-            if (mbar_try_wait(bar, parity)) return true;
-            if ((it & 255u) == 255u && *abort_flag) break;
-        }
-        return false;
-    };
+    const auto wait_one = [&](u64* bar, unsigned int parity) { return kv_wait(a, bar, parity, abort_flag); };
     // (the lanes of a warp go on, or give up, together)
     const auto together = [](bool on) { return __all_sync(0xFFFFFFFFu, on) != 0; };
     const auto wait = [&](u64* bar, unsigned int parity) { return together(wait_one(bar, parity)); };
@@ -417,7 +410,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
 #pragma unroll 1
             for (int k = max(0, n - kTileRaw); k < n; ++k)
 #pragma unroll 1
-                for (unsigned int it = 0; it < kWaitLimit && !mbar_try_wait(&sh.raw_full[k % kTileRaw], (k / kTileRaw) & 1); ++it) {}
+                for (unsigned int it = 0; it < a.wait_limit && !mbar_try_wait(&sh.raw_full[k % kTileRaw], (k / kTileRaw) & 1); ++it) {}
         } else {
             // ---- issuers: warp 12 for group 0, warp 14 for group 1
             if (lane == 0) {
@@ -470,7 +463,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                 // products in flight read this CTA's shared memory
                 tc_commit(&sh.drain[x]);
 #pragma unroll 1
-                for (unsigned int it = 0; it < kWaitLimit && !mbar_try_wait(&sh.drain[x], 0); ++it) {}
+                for (unsigned int it = 0; it < a.wait_limit && !mbar_try_wait(&sh.drain[x], 0); ++it) {}
             }
             __syncwarp();
         }

@@ -335,6 +335,37 @@ def test_scratch_is_cleared_by_registering_it_again(ctx):
     assert torch.equal(o["out"], want) and ctx.poll_status() == 0
 
 
+@pytest.fixture(scope="module")
+def long_pools():
+    rng = np.random.default_rng(35)
+    return {D: Pool(rng, [4000], 1, D) for D in (64, 128, 256)}
+
+
+@pytest.mark.parametrize("new,D,dtype", [(1, 64, "bf16"), (1, 128, "f32"), (1, 256, "bf16"), (16, 128, "bf16"), (35, 64, "bf16")])
+@pytest.mark.parametrize("page", [0, 1, 3])
+def test_a_wait_that_runs_out_ends_the_call_and_the_context_recovers(long_pools, new, D, dtype, page):
+    """One of the first CTA's pages never arrives: its waits run out, the call ends by itself and the status
+    word says so.  Nothing faults; with the scratch registered again the same call gives what it gave."""
+    c = binding.Context()
+    try:
+        B, n, pool = 200, 4000, long_pools[D]      # several pages for every warp, and sequences that CTAs share
+        q = queries(np.random.default_rng(page), B * new, 4, D, dtype)
+        args = (q, pool.pages, i32(np.tile(pool.table, (B, 1))), i32([n - new] * B), i32([n] * B))
+        want = c.kv_attend(*args, rows_per_seq=new)["out"].clone()
+        assert c.poll_status() == 0
+        c.debug_withhold_tile(page, 0, 1 << 14)
+        c.kv_attend(*args, rows_per_seq=new)
+        torch.cuda.synchronize()                   # the call ended by itself
+        assert c.poll_status() == binding.STATUS_TIMEOUT
+        c.reinit_workspace()
+        assert torch.equal(c.kv_attend(*args, rows_per_seq=new)["out"], want) and c.poll_status() == 0
+        # used up by one call; there is no page of that number
+        c.debug_withhold_tile(10 ** 12, 0, 1 << 22)
+        assert torch.equal(c.kv_attend(*args, rows_per_seq=new)["out"], want) and c.poll_status() == 0
+    finally:
+        c.close()
+
+
 def test_a_captured_call_keeps_its_scratch():
     """A graph holds the scratch's address: calls with a larger head dimension do not move it."""
     c = binding.Context()
