@@ -244,13 +244,6 @@ def kv_pages(n_pages: int, n_kv_heads: int, head_dim: int, layers: int | None = 
     return torch.empty(shape if layers is None else (layers,) + shape, dtype=torch.uint8, device=device)
 
 
-def _kv_dim(pages: torch.Tensor) -> int:
-    """Head dimension of a page pool."""
-    n = pages.shape[-1] - 512
-    _kv_need(n > 0 and n % KV_PAGE == 0, "blocks of a page")
-    return n // KV_PAGE
-
-
 # The library cannot see how long its arrays are: what it reads and writes by the counts of the
 # others is checked here.  (Longer ones are fine.)
 def _kv_need(ok, what: str):
@@ -268,6 +261,19 @@ def _kv_like(x: torch.Tensor, n: int, *tensors):
     for t in tensors:
         assert t is None or (t.dtype is x.dtype and t.get_device() == x.get_device() and t.is_contiguous()), "of the inputs' type, on their device, contiguous"
         _kv_need(t is None or t.numel() >= n, "outputs")
+
+
+def _kv_pool(pages: torch.Tensor, dims: int, device: int):
+    """Pages, key heads and head dimension of a page pool."""
+    shape = pages.shape
+    assert len(shape) == dims and pages.dtype is torch.uint8 and pages.get_device() == device and pages.is_contiguous()
+    n = shape[-1] - 512
+    _kv_need(n > 0 and n % KV_PAGE == 0, "blocks of a page")
+    return shape[-3], shape[-2], n // KV_PAGE
+
+
+def _kv_dtype(x: torch.Tensor, dt) -> int:
+    return BF16 if dt is torch.bfloat16 else F32 if dt is torch.float32 else _dtype_code(x)
 
 
 def _kv_token_stride(x: torch.Tensor) -> int:
@@ -606,13 +612,16 @@ class Context:
         with q and, with ``keep_k``, the rotated k."""
         _kv_i32(self.device_index, slot_map, positions)
         T, Hq, D = q.shape
-        Hkv = k.shape[1]
-        qs, ks, vs = _kv_token_stride(q), _kv_token_stride(k), _kv_token_stride(v)
+        kv = k.shape
+        Tk, Hkv, Dk = kv
+        (qs, qh, qd), (ks, kh, kd), (vs, vh, vd) = q.stride(), k.stride(), v.stride()
+        if not (T > 1 and qh == D and kh == D and vh == D and qd == 1 and kd == 1 and vd == 1):
+            qs, ks, vs = _kv_token_stride(q), _kv_token_stride(k), _kv_token_stride(v)
         dt, dev = q.dtype, self.device_index
-        assert k.dtype is dt and v.dtype is dt and k.shape == v.shape and k.shape[2] == D and _kv_dim(pages) == D
-        assert pages.dtype is torch.uint8 and pages.is_contiguous() and pages.dim() == 3 and pages.shape[1] == Hkv
-        assert q.get_device() == dev and k.get_device() == dev and v.get_device() == dev and pages.get_device() == dev
-        _kv_need(k.shape[0] == T and slot_map.numel() == T and positions.numel() == T, "lengths of kv_write's arrays")
+        N, Hp, Dp = _kv_pool(pages, 3, dev)
+        assert k.dtype is dt and v.dtype is dt and v.shape == kv and Dk == D and Dp == D and Hp == Hkv
+        assert q.get_device() == dev and k.get_device() == dev and v.get_device() == dev
+        _kv_need(Tk == T and slot_map.numel() == T and positions.numel() == T, "lengths of kv_write's arrays")
         for w in (q_weight, k_weight):
             assert w is None or (w.dtype is dt and w.get_device() == dev and w.numel() == D and w.is_contiguous())
         o = outputs
@@ -625,7 +634,7 @@ class Context:
         if cos_sin is not None:
             assert cos_sin.dtype is torch.float32 and cos_sin.get_device() == dev and cos_sin.is_contiguous() and cos_sin.dim() == 2
             limit, rot = cos_sin.shape
-        prm = self._kv_struct(KvWriteParams, Hq, Hkv, D, pages.shape[0], _dtype_code(q), qs, ks, vs, rot, limit,
+        prm = self._kv_struct(KvWriteParams, Hq, Hkv, D, N, _kv_dtype(q, dt), qs, ks, vs, rot, limit,
                               eps, KV_ROPE_INTERLEAVED if interleaved else 0)
         ko = o.get("k")
         rc = self.lib.aasd_kv_write(self._h, q.data_ptr(), k.data_ptr(), v.data_ptr(),
@@ -667,10 +676,11 @@ class Context:
         _kv_i32(self.device_index, block_table, cached_len, kv_len, tok_offsets, node_parent)
         T, Hq, D = q.shape
         B, P = block_table.shape
-        qs = _kv_token_stride(q)
-        assert _kv_dim(pages) == D
-        assert pages.dtype is torch.uint8 and pages.is_contiguous() and pages.dim() == 3
-        assert q.get_device() == self.device_index and pages.get_device() == self.device_index
+        qs, qh, qd = q.stride()
+        if not (T > 1 and qh == D and qd == 1):
+            qs = _kv_token_stride(q)
+        N, Hkv, Dp = _kv_pool(pages, 3, self.device_index)
+        assert Dp == D and q.get_device() == self.device_index
         _kv_need(cached_len.numel() >= B and kv_len.numel() >= B and (tok_offsets is None or tok_offsets.numel() > B) and
                  (node_parent is None or node_parent.numel() >= T), "lengths of kv_attend's arrays")
         o = outputs
@@ -684,7 +694,7 @@ class Context:
         elif lse is not None:
             assert lse.dtype is torch.float32 and lse.get_device() == self.device_index and lse.is_contiguous()
             _kv_need(lse.numel() >= T * Hq, "outputs")
-        prm = self._kv_struct(KvAttendParams, B, Hq, pages.shape[1], D, pages.shape[0], P, _dtype_code(q), int(rows_per_seq),
+        prm = self._kv_struct(KvAttendParams, B, Hq, Hkv, D, N, P, _kv_dtype(q, q.dtype), int(rows_per_seq),
                               T, qs, scale)
         out = KvAttendOut(o["out"].data_ptr(), None if lse is None else lse.data_ptr())
         ws = self.kv_workspace(D)
@@ -704,15 +714,16 @@ class Context:
         [layers, n_pages, Hkv, bytes]) and returns the new cached lengths.  ``node_parent`` is
         [B, rows_per_seq], or flat with ``tok_offsets``."""
         _kv_i32(self.device_index, block_table, cached_len, kv_len, best_node, node_parent, tok_offsets, outputs)
-        assert pages.dim() == 4 and pages.dtype is torch.uint8 and pages.is_contiguous() and pages.get_device() == self.device_index
+        N, H, D = _kv_pool(pages, 4, self.device_index)
         B, P = block_table.shape
-        L, N, H, _ = pages.shape
+        nodes, rows = node_parent.shape, 0
+        if tok_offsets is None:
+            _kv_need(len(nodes) == 2 and nodes[0] >= B, "lengths of kv_commit's arrays")
+            rows = nodes[1]
         _kv_need(cached_len.numel() >= B and kv_len.numel() >= B and best_node.numel() >= B and (outputs is None or outputs.numel() >= B) and
-                 (node_parent.dim() == 2 and node_parent.shape[0] >= B if tok_offsets is None else tok_offsets.numel() > B),
-                 "lengths of kv_commit's arrays")
+                 (tok_offsets is None or tok_offsets.numel() > B), "lengths of kv_commit's arrays")
         new_len = outputs if outputs is not None else cached_len.new_empty(B)
-        prm = self._kv_struct(KvCommitParams, B, H, _kv_dim(pages), N, P,
-                              0 if tok_offsets is not None else node_parent.shape[1], L, pages.stride(0))
+        prm = self._kv_struct(KvCommitParams, B, H, D, N, P, rows, pages.shape[0], pages.stride(0))
         rc = self.lib.aasd_kv_commit(self._h, pages.data_ptr(), block_table.data_ptr(), cached_len.data_ptr(), kv_len.data_ptr(),
                                      None if tok_offsets is None else tok_offsets.data_ptr(), best_node.data_ptr(),
                                      node_parent.data_ptr(), prm, new_len.data_ptr())
@@ -724,9 +735,9 @@ class Context:
         """aasd_kv_read: the entries at ``slots`` as values, k and v [n, Hkv, D].  Several layers at
         once: pass ``pages.flatten(0, 1)`` and slots raised by layer * n_pages * KV_PAGE."""
         _kv_i32(self.device_index, slots)
-        assert pages.dim() == 3 and pages.dtype is torch.uint8 and pages.is_contiguous() and _kv_dim(pages) == head_dim
-        assert pages.get_device() == self.device_index
-        n, N, H = slots.numel(), pages.shape[0], pages.shape[1]
+        N, H, D = _kv_pool(pages, 3, self.device_index)
+        assert D == head_dim
+        n = slots.numel()
         o = outputs
         if o is None:
             shape = (n, H, head_dim)
