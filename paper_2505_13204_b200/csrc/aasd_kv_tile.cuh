@@ -102,7 +102,7 @@ struct KvTileShared {
     u64 k_empty[kTileKeys], v_empty[kTileValues], m_empty[kTileMeta];
     u64 q_full[2], s_full[2][2], p_full[2][2], o_done[2][2], x_full, x_empty, r_full, drain[2];
     unsigned int tmem;
-    int abort_flag;
+    int abort_flag, padding;
 };
 
 // ---- tcgen05 ----------------------------------------------------------------------------------------
@@ -272,15 +272,20 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
     const int B = a.p.n_seqs, G = a.p.n_q_heads / a.p.n_kv_heads;
     const int strip = (B + kTileThreads - 1) / kTileThreads;
     long long mine = 0;
+    bool padding = B == 0;
 #pragma unroll 1
     for (int b = tid * strip; b < min(B, (tid + 1) * strip); ++b) {
         const KvSeq s = kv_load_seq(a, b, R);
         mine += kv_tile_head_units(a, s, R, G) * a.p.n_kv_heads;
+        padding = padding || kv_has_padding(a, s, b);
         if (s.fresh > 0 && (long long)s.cached + s.fresh > (long long)a.p.max_pages * kPage) raise(a.state, AASD_STATUS_BAD_OFFSETS);
     }
     tc_fence_before();
     long long sum;
     sh.base[tid] = (int)block_scan<kTileThreads>(mine, sh.scan, sum);
+    if (tid == 0) sh.padding = 0;
+    __syncthreads();
+    if (padding) sh.padding = 1;
     __syncthreads();
     tc_fence_after();
     const unsigned int tm = sh.tmem;
@@ -955,13 +960,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
             n0 += np;
         }
         if (!ok) tc_wait_store();   // (a group that gave up may have stores on their way to the memory that is freed below)
-        // the segment that this CTA begins and others go on with: the joining kernel's work
+        // the segment that this CTA begins and others go on with, and rows to clear: the joining kernel's work
         if (tid == 0) {
-            KvTileOpen o{sh.open, 0};
+            KvTileOpen o{sh.open, 0, total == 0 ? 2 : sh.padding ? 1 : 0};
             if (sh.open.seg >= 0 && ok && !*abort_flag) o.parts = sh.shares.owner(sh.open.seg + sh.open.pages - 1) - c + 1;
             a.tile_open[c] = o;
         }
-        kv_clear_rows<AASD_BF16>(a, D, total, (int)(blockIdx.x * 8 + warp), (int)(gridDim.x * 8));
     }
     if (!ok) give_up(abort_flag, a.state);
     tc_fence_before();
@@ -972,7 +976,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
 
 // Joins the parts of the segments that several CTAs of the tile kernel went through: block (c, k) takes rows
 // 8 k .. of the segment that CTA c began, a warp per row.  (Left to the last CTA that delivers a part, one
-// sequence of 64k tokens with 64 new ones waited 100 us for 19 parts of 256 rows.)
+// sequence of 64k tokens with 64 new ones waited 100 us for 19 parts of 256 rows.)  Its warps clear the rows
+// that no tile has.
 template <int D, bool PAIR>
 __global__ void __launch_bounds__(256) kv_tile_join_kernel(const KvAttendArgs a) {
     constexpr int R = PAIR ? 2 * kTileRows : kTileRows, kPart = R * D + 2 * R;
@@ -981,6 +986,8 @@ __global__ void __launch_bounds__(256) kv_tile_join_kernel(const KvAttendArgs a)
     const KvTileOpen open = a.tile_open[blockIdx.x];
     const KvPiece& pc = open.piece;
     const int r = (int)blockIdx.y * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (open.padding != 0)
+        kv_clear_rows<AASD_BF16>(a, D, 2 - open.padding, r * (int)gridDim.x + (int)blockIdx.x, (int)(gridDim.x * gridDim.y) * 8);
     if (open.parts == 0 || r >= pc.n) return;
     const int G = a.p.n_q_heads / a.p.n_kv_heads;
     const float* base = a.cta_parts + (long long)blockIdx.x * 2 * kPart;   // part k: 2 k, the first one's 1

@@ -86,6 +86,30 @@ def test_rows_in_front_of_the_first_sequence_and_behind_the_last_give_zeros(ctx,
     check_rows(pool, q, o, rows)
 
 
+@pytest.mark.parametrize("G,dtype", [(3, "f32"), (4, "bf16"), (40, "bf16")])
+@pytest.mark.parametrize("B,rows", [(1, 5000), (5, 900), (300, 17), (4000, 3), (7, 0)])
+def test_padding_of_any_length_gives_zeros(ctx, G, dtype, B, rows):
+    """Few sequences with much padding, more sequences than warps, and (rows 0) packed ones with room behind them."""
+    rng = np.random.default_rng(B)
+    table, kv = np.zeros((B, 2), np.int32), rng.integers(0, 3, B)
+    kv[0], table[:, 1] = 2, 1
+    pool = Pool(rng, [100], 1, 64)
+    pool.k, pool.v = [pool.k[0]] * B, [pool.v[0]] * B
+    table[:] = pool.table[0, :2]                            # (every sequence the same tokens)
+    offs = np.arange(B + 1) * rows if rows else np.concatenate([[0], np.cumsum(kv)])
+    T = B * rows if rows else int(offs[-1]) + 3001
+    q = queries(rng, T, G, 64, dtype)
+    o = ctx.kv_attend(q, pool.pages, i32(table), i32([50] * B), i32(50 + kv), None if rows else i32(offs), rows_per_seq=rows, want_lse=True,
+                      outputs=nan_outputs(T, G, 64, dtype))
+    assert ctx.poll_status() == 0
+    used = torch.zeros(T, dtype=torch.bool, device="cuda")
+    live = {int(offs[b]) + i: (b, list(range(51 + i))) for b in range(B) for i in range(kv[b])}
+    used[list(live)] = True
+    assert bool((o["out"][~used] == 0).all()) and bool((o["lse"][~used] == float("-inf")).all())
+    some = sorted(live)[:3] + sorted(live)[-3:]
+    check_rows(pool, q[some], dict(out=o["out"][some], lse=o["lse"][some]), {n: live[t] for n, t in enumerate(some)})
+
+
 @pytest.mark.parametrize("dtype,width,H", [("f32", 1 << 20, 8), ("bf16", 1 << 24, 16)])
 def test_more_pages_than_a_call_can_count_give_zeros(ctx, dtype, width, H):
     """(The table names no page, so there would be nothing to see either.)"""
