@@ -541,13 +541,18 @@ typedef struct aasd_kv_attend_out {
  * its cached_len[b] cached tokens and, among the new ones (which must have been stored: kv_len[b] -
  * cached_len[b] of them), tokens 0..i, or with node_parent (one entry per token row, index inside
  * the sequence, NONE = no parent; parents precede their children) itself and its ancestors.
- * Sums and the softmax's statistics are fp32; bf16 queries are used as they are, probabilities and, with
- * more than 48 rows per key/value head, the cache's values are rounded to 11 bits (fp32 queries: they
- * and the probabilities to 22) for the products on the tensor cores; the result is rounded once.
- * More than 2^31 - 1 pages to go through in one call (over all heads and row tiles) raise
- * AASD_STATUS_BAD_OFFSETS; no row sees anything then.  Rows that see nothing (padding, tokens that were
- * not placed, rows that no sequence owns) give zeros and an lse of -inf.  A page id outside the pool, or a parent that does not precede its child, raises
- * AASD_STATUS_BAD_OFFSETS; what lies behind it counts as not visible. */
+ * Sums and the softmax's statistics are fp32; the result is rounded once.  For the products on the
+ * tensor cores bf16 queries are used as they are (with few rows, those below 2^-27 of their row's largest
+ * element lose bits), and probabilities are rounded to 11 bits; fp32 queries and their probabilities
+ * to 22.  With bf16 queries, head_dim 64 or 128 and more than 48 rows per key/value head (query heads of
+ * a group times token rows; rows_per_seq of them, or n_tokens / n_seqs when packed, whether placed or
+ * not: one choice for the whole call) the cache's values are rounded too, to 11 bits, and to about
+ * 2^-20 of the largest value in the pages that a CTA has been through.
+ * Rows that see nothing (padding, tokens that were not placed, rows that no sequence owns) give zeros
+ * and an lse of -inf.  More than 2^31 - 1 pages to go through in one call (over all heads and row
+ * tiles) raise AASD_STATUS_BAD_OFFSETS; no row sees anything then.  A page id outside the pool, or a
+ * parent that does not precede its child, raises AASD_STATUS_BAD_OFFSETS; what lies behind it counts
+ * as not visible. */
 int aasd_kv_attend(aasd_ctx* ctx, const void* q, const void* pages, const int32_t* block_table,
                    const int32_t* cached_len, const int32_t* kv_len, const int32_t* tok_offsets,
                    const int32_t* node_parent, const aasd_kv_attend_params* params, void* workspace,

@@ -224,8 +224,9 @@ constexpr int kPlanThreads = 256, kPlanThreadsMany = 1024;   // of batches up to
 // One CTA: the books of all sequences (NT at a time) by prefix sums, the pages moved
 // by all threads together (a thread finds its page's sequence by bisection of the sums), so one
 // long sequence that ends or arrives costs no more than many short ones.  Latency-bound: four
-// scans and three trips to memory (4 trees of 9 nodes 5 us, 256 arriving prompts of ~1000 tokens
-// 15 us with the token arrays' launch; a launch alone is 2 us).
+// scans and three trips to memory (4 trees of 9 nodes 3.4 us, 256 sequences of one token 3.7; 256 arriving
+// prompts of 1000 tokens 14 us with the token arrays' launch, which waits while this CTA hands
+// out 4096 pages; a launch alone is 2 us).
 template <int NT>
 __global__ void __launch_bounds__(NT) kv_plan_kernel(const KvPlanArgs a) {
     __shared__ long long s_warp[NT / 32];
@@ -449,13 +450,14 @@ __device__ __forceinline__ float2 mul2_rounded(float2 a, float2 b, float2 minus_
 // members of a rotated pair, and both halves of a stored byte, are its own.  One row each: four rows of
 // a token per lane, with the cosines, weights and a reciprocal root shared, were slower at every size
 // (64 tokens 4.6 us instead of 2.7, 512 tokens 7.0 instead of 6.3, 4096 tokens 34.4 instead of 30.0; 32 query and 8 key
-// heads of 128 channels).  The norm's sum follows the order of the definition: halves, then
+// heads of 128 channels, which take 2.5, 5.8 and 27.4 us as the kernel stands).  4096 tokens: 89 MB at half the
+// copy rate; seven of ten issue slots are used, so that it is the instructions that bound it.  The norm's sum follows the order of the definition: halves, then
 // neighbours (three steps inside the lane, the others across lanes by butterfly; a sum does not
 // ask which operand is first), each operation rounded by itself.
 //
 // Values: a CTA takes kValueTokens tokens of one head.  Their codes meet in shared memory, and lane t
 // of a warp stores the bytes of token t: neighbouring tokens, which lie in neighbouring bytes, in one
-// go (byte by byte from the rows' own lanes, 4096 tokens took 62 us in all instead of 25).
+// go (byte by byte from the rows' own lanes, 4096 tokens took 62 us in all).
 constexpr int kValueTokens = 32;
 constexpr int kWriteThreads = 256;
 
@@ -730,8 +732,8 @@ struct KvReadArgs {
 
 // A CTA takes kValueTokens slots of one head.  The values' bytes are fetched with a lane per slot, so
 // that neighbouring slots are one access, and pass through shared memory; then D / 16 lanes turn out a
-// row as in the writing kernel.  Memory-bound: 4096 slots of 8 heads of 128 channels 7.4 us, the writing kernel
-// 27 us for the 89 MB that it reads and writes beside 32 query heads (the two together half of the copy rate).
+// row as in the writing kernel.  4096 slots of 8 heads of 128 channels take 7.8 us; their 21 MB would take
+// 3.2, and six of ten issue slots are used.
 template <int DT, int D, bool VEC>
 __global__ void __launch_bounds__(kWriteThreads) kv_read_kernel(const KvReadArgs a) {
     constexpr int L = D / 16, H = D / 2, kRows = kWriteThreads / L, kPitch = H + 8;

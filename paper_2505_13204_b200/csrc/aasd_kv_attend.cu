@@ -13,8 +13,9 @@ namespace {
 // Rows per key/value head up to which the split kernel takes bf16 queries: it goes over the pages once
 // for every 16 rows, but shares them among all warps of the device and fetches nothing a page does not
 // hold.  Measured with trees over 32 query and 8 key heads of 128 channels, split kernel against tiles:
-//   64 sequences of 4000 tokens: 32 rows 161 and 262 us; of 2000 tokens: 96 rows 243 and 176 us;
-//   8 of 4000: 32 rows 39 and 45 us, 96 rows 74 and 49 us;  one of 16000: 16 rows 26.5 and 27.0 us, 32 rows 29.8 and 27.7 us.
+//   64 sequences of 4000 tokens: 32 rows 164 and 276 us, 48 rows 235 and 283 us, 64 rows 304 and 276 us; of 2000 tokens:
+//   96 rows 245 and 184 us;  8 of 4000: 32 rows 38 and 47 us, 48 rows 49 and 48 us, 96 rows 74 and 50 us;  one of 16000: 16
+//   rows 26.6 and 28.3 us, 32 rows 30.0 and 29.0 us.
 constexpr int64_t kSplitRows = 48;
 
 template <int DT, int D, int NT>
@@ -69,7 +70,7 @@ int launch_kv_attend_bf16(const LaunchEnv& env, int sm_count, const KvAttendArgs
 #if AASD_DT == 1
     if (rows > kSplitRows && a.p.head_dim <= 128) {
         // Two row tiles of the same pages, or two groups on alternate pages of one: with 8 sequences of 4000 tokens the pair
-        // takes 57.8 us for 128 rows and 61.6 us for 132, the single tile 50.9 and 79.7 us (64 of 2000: 219 and 209 us, and 177 and 317 us).
+        // takes 55.0 us for 128 rows and 58.8 us for 132, the single tile 51.8 and 82.0 us (64 of 2000: 196 and 195 us, and 184 and 328).
         *launches = 2;
         if (a.p.head_dim == 64) return rows > kTileRows ? launch_tile<64, true>(env, sm_count, a) : launch_tile<64, false>(env, sm_count, a);
         return rows > kTileRows ? launch_tile<128, true>(env, sm_count, a) : launch_tile<128, false>(env, sm_count, a);

@@ -21,12 +21,13 @@
 //
 // Tensor memory (512 columns): two S buffers of each group, whose first halves P takes over, and O.
 //
-// Measured (32 query and 8 key heads of 128 channels): 2 chunks of 2048 tokens 228 us, 600 TFLOP/s; 32 trees of
-// 33 nodes over 4000 tokens 180 us; 64 new tokens over 131072 182 us, 754 TFLOP/s.  A pair of tiles takes 2500
-// cycles per page, of which the tensor cores work 1300 and the exponentials 1000.  It is the softmax warps'
-// chain (load S, scale, exponentials, store P: 2400 cycles) that paces it: with the exponentials left
-// out it took 5 % less, with cheaper unpacking of values no less.  A piece costs 15000 cycles beside
-// its pages (queries in, result out), about six pages.
+// Measured (32 query and 8 key heads of 128 channels): 2 chunks of 2048 tokens over ~1000 cached ones 222 us, 617
+// TFLOP/s; 32 trees of 33 nodes over ~3800 174 us; 64 new tokens over 131072 176 us, 782 TFLOP/s.  A pair of
+// tiles takes some 2400 cycles per page, of which the tensor cores work 1300 and the exponentials 1000, and no unit is
+// busy for more than 40 % of the time (issue slots 47 %): the roles wait for one another.  Which of them sets
+// the pace is not known: with the exponentials left out it took 5 % less, with cheaper unpacking of values
+// no less, and the single tile, where a softmax group has the time of two pages for each, is a sixth faster
+// per page.  A piece costs 15000 cycles beside its pages (queries in, result out), about six pages.
 #pragma once
 
 #include "aasd_kv_attend.cuh"
@@ -57,7 +58,7 @@ __device__ __forceinline__ int kv_tile_pages(const KvAttendArgs& a, int cached, 
     return min(pages, (int)(((unsigned int)cached + (unsigned int)(last / G) + kPage) / kPage));
 }
 // Loading the queries and handing the result on takes about as long as six pages (2 chunks of 2048 tokens: 264 us
-// with 2, 247 with 4, 233 with 6, 238 with 9).
+// with 2, 247 with 4, 233 with 6, 238 with 9, when it was chosen).
 constexpr int kTileSegCost = 6;
 // Units of one head of a sequence.
 __device__ __forceinline__ long long kv_tile_head_units(const KvAttendArgs& a, const KvSeq& s, int R, int G) {
