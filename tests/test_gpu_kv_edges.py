@@ -99,12 +99,13 @@ def test_padding_of_any_length_gives_zeros(ctx, G, dtype, B, rows):
     offs = np.arange(B + 1) * rows if rows else np.concatenate([[0], np.cumsum(kv)])
     T = B * rows if rows else int(offs[-1]) + 3001
     q = queries(rng, T, G, 64, dtype)
-    o = ctx.kv_attend(q, pool.pages, i32(table), i32([50] * B), i32(50 + kv), None if rows else i32(offs), rows_per_seq=rows, want_lse=True,
-                      outputs=nan_outputs(T, G, 64, dtype))
-    assert ctx.poll_status() == 0
     used = torch.zeros(T, dtype=torch.bool, device="cuda")
     live = {int(offs[b]) + i: (b, list(range(51 + i))) for b in range(B) for i in range(kv[b])}
     used[list(live)] = True
+    q[~used] = float("nan")                                 # (whatever the queries of such rows hold)
+    o = ctx.kv_attend(q, pool.pages, i32(table), i32([50] * B), i32(50 + kv), None if rows else i32(offs), rows_per_seq=rows, want_lse=True,
+                      outputs=nan_outputs(T, G, 64, dtype))
+    assert ctx.poll_status() == 0
     assert bool((o["out"][~used] == 0).all()) and bool((o["lse"][~used] == float("-inf")).all())
     some = sorted(live)[:3] + sorted(live)[-3:]
     check_rows(pool, q[some], dict(out=o["out"][some], lse=o["lse"][some]), {n: live[t] for n, t in enumerate(some)})
@@ -634,3 +635,34 @@ def test_chunks_and_single_tokens_in_one_packed_call(ctx, new, D):
     o = ctx.kv_attend(q, pool.pages, i32(pool.table), i32(cached), i32(kv), i32(offs), want_lse=True, outputs=nan_outputs(T, 4, D, "bf16"))
     assert ctx.poll_status() == 0
     check_rows(pool, q, o, {int(offs[b]) + i: (b, list(range(int(cached[b]) + i + 1))) for b in range(len(new)) for i in range(new[b])})
+
+
+def test_pools_of_more_than_4_gb(ctx):
+    """Every call on pages whose bytes lie past 32-bit offsets, in a second layer: what a small pool gives, to the bit."""
+    g = torch.Generator(device="cuda").manual_seed(60)
+    Hq, Hkv, D, B, cap = 32, 8, 128, 2, 24
+    n, P = 66000, 4                                         # 4.6 GB a layer
+    big, small = binding.kv_pages(n, Hkv, D, layers=2), binding.kv_pages(B * P, Hkv, D, layers=2)
+    assert big[0].numel() > 1 << 32
+    big[:, -B * P:].fill_(85)
+    small.fill_(85)
+    cached, kv = i32([130, 70]), i32([130 + cap, 70 + cap])
+    parent = i32(np.stack([_tree(np.random.default_rng(b), cap) for b in range(B)]))
+    got = []
+    for pages, at in ((small, 0), (big, n - B * P)):
+        g.manual_seed(61)
+        table = (torch.arange(B * P, dtype=torch.int32, device="cuda") + at).view(B, P).contiguous()
+        place = torch.cat([table[b, torch.arange(int(kv[b]), device="cuda") // PAGE] * PAGE + torch.arange(int(kv[b]), device="cuda") % PAGE for b in range(B)])
+        slots = place.to(torch.int32).contiguous()
+        out = []
+        for layer in range(2):
+            x = torch.randn((slots.numel(), Hq + 2 * Hkv, D), generator=g, device="cuda").bfloat16()
+            ctx.kv_write(pages[layer], x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], slots, torch.zeros_like(slots))
+            for new, dtype in ((cap, torch.bfloat16), (1, torch.bfloat16), (1, torch.float32)):
+                q = torch.randn((B * new, Hq, D), generator=g, device="cuda").to(dtype)
+                out.append(ctx.kv_attend(q, pages[layer], table, kv - new, kv, rows_per_seq=new, node_parent=parent if new == cap else None)["out"])
+        new_len = ctx.kv_commit(pages, table, cached, kv, i32([cap - 1, cap - 2]), parent)
+        e = ctx.kv_read(pages[1], slots, D)
+        got.append(out + [new_len, e["k"], e["v"], pages[:, at:at + B * P].clone()])
+    assert ctx.poll_status() == 0
+    assert all(torch.equal(a, b) for a, b in zip(*got))
