@@ -564,15 +564,15 @@ def _context():
 def run_own(s):
     c, ctx = s["case"], _context()
     if c["op"] == "write":
-        o = ctx.kv8_write(s["pages"], s["q"], s["k"], s["v"], s["table"], s["cached"], s["kv"], s["pos"], None if c["rows"] else s["offs"], c["rows"],
+        o = ctx.kvb_write(s["pages"], s["q"], s["k"], s["v"], s["table"], s["cached"], s["kv"], s["pos"], None if c["rows"] else s["offs"], c["rows"],
                           s["cs"], q_weight=s["w"][0], k_weight=s["w"][1], interleaved=bool(c["inter"]))
-        kv = ctx.kv8_read(s["pages"], s["slots"], c["dim"], DTYPES[c["dtype"]])
+        kv = ctx.kvb_read(s["pages"], s["slots"], c["dim"], DTYPES[c["dtype"]])
         return dict(q=o["q"], k=kv["k"], v=kv["v"])
     if c["op"] == "attend":
-        return ctx.kv8_attend(s["q"], s["pages"], s["table"], s["cached"], s["kv"], rows_per_seq=c["new"], node_parent=s["par"])
+        return ctx.kvb_attend(s["q"], s["pages"], s["table"], s["cached"], s["kv"], rows_per_seq=c["new"], node_parent=s["par"])
     if c["op"] == "commit":
-        new_len = ctx.kv8_commit(s["pages"], s["table"], s["cached"], s["kv"], s["best"], s["par"])
-        kv = ctx.kv8_read(s["pages"].flatten(0, 1), s["slots"], c["dim"], torch.bfloat16)
+        new_len = ctx.kvb_commit(s["pages"], s["table"], s["cached"], s["kv"], s["best"], s["par"])
+        kv = ctx.kvb_read(s["pages"].flatten(0, 1), s["slots"], c["dim"], torch.bfloat16)
         return dict(new_len=new_len, k=kv["k"], v=kv["v"])
     width, pool = s["width"], s["pool"]
     if c["op"] == "fork":
