@@ -502,6 +502,115 @@ __device__ __forceinline__ KvQuant kv_row_quantiser(const float2 (&x)[4], const 
     return kv_quantiser(lo, hi, bad);
 }
 
+// Norm and rotation of a row spread over D / 16 lanes: rx and ry are the lane's channels 8l .. and D/2 + 8l .. as they
+// came, u and v what they become.  used: the row has a position (others stay zeros).  w: the norm's weight, or NULL.
+// mine: D floats for the row, touched with partial rotation only.  Every lane of the warp takes part.
+template <int DT, int D, bool VEC, bool FULL>
+__device__ __forceinline__ void kv_norm_rotate(const KvWriteArgs& a, const Raw8<DT, VEC>& rx, const Raw8<DT, VEC>& ry, int l, bool used, int pos, const void* w,
+                                               float* mine, float2 (&u)[4], float2 (&v)[4]) {
+    constexpr int L = D / 16, H = D / 2;
+    // cosines and sines of the lane's pairs (the branches on the form of the rotation are the same for every lane)
+    const int rot = FULL ? D : a.p.rotary_dim, half = rot / 2;
+    const bool neighbours = !FULL && (a.p.flags & AASD_KV_ROPE_INTERLEAVED) != 0;
+    const float* cs = a.cos_sin + (int64_t)(used ? pos : 0) * rot;
+    float co[8], si[8];   // neighbours: pairs of the low half, then of the high half; else of channels 8l + e
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        co[e] = 1.f;
+        si[e] = 0.f;
+    }
+    if (rot > 0 && used) {
+        if (neighbours) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int c = (e < 4 ? 8 * l : H + 8 * l) + 2 * (e & 3);
+                if (c < rot) {
+                    co[e] = __ldg(cs + c / 2);
+                    si[e] = __ldg(cs + half + c / 2);
+                }
+            }
+        } else if (rot == D) {
+            load8<AASD_F32, VEC>(cs, 8 * l, co);
+            load8<AASD_F32, VEC>(cs, half + 8 * l, si);
+        }
+    }
+    rx.unpack(u);
+    ry.unpack(v);
+    const float2 mz = a.minus_zero;
+    // (the lanes of a row take the same way; shuffles stay among all lanes of the warp)
+    if (a.q_weight != nullptr || a.k_weight != nullptr) {
+        float s[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 q = __fadd2_rn(mul2_rounded(u[e], u[e], mz), mul2_rounded(v[e], v[e], mz));
+            s[e] = __fadd_rn(q.x, q.y);
+        }
+        float sum = __fadd_rn(__fadd_rn(s[0], s[1]), __fadd_rn(s[2], s[3]));
+#pragma unroll
+        for (int o = 1; o < L; o <<= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xFFFFFFFFu, sum, o));
+        const float r = __frcp_rn(__fsqrt_rn(__fadd_rn(__fmul_rn(sum, 1.0f / D), a.p.eps)));
+        if (used && w != nullptr) {
+            Raw8<DT, VEC> g;
+            float2 wx[4], wy[4];
+            g.load(w, 8 * l);
+            g.unpack(wx);
+            g.load(w, H + 8 * l);
+            g.unpack(wy);
+            const float2 rr = make_float2(r, r);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                u[e] = __fmul2_rn(__fmul2_rn(u[e], rr), wx[e]);
+                v[e] = __fmul2_rn(__fmul2_rn(v[e], rr), wy[e]);
+            }
+        }
+    }
+    // (a - b is written a + (-b): the same rounding)
+    if (!FULL && rot > 0 && neighbours) {
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            float2(&z)[4] = part ? v : u;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (part * H + 8 * l + 2 * e < rot) {
+                    const float c = co[4 * part + e], n = si[4 * part + e];
+                    z[e] = __fadd2_rn(mul2_rounded(z[e], make_float2(c, c), mz), mul2_rounded(make_float2(z[e].y, z[e].x), make_float2(-n, n), mz));
+                }
+            }
+        }
+    } else if (FULL || rot == D) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 c = make_float2(co[2 * e], co[2 * e + 1]), n = make_float2(si[2 * e], si[2 * e + 1]);
+            const float2 p = u[e], q = v[e];
+            u[e] = __fadd2_rn(mul2_rounded(p, c, mz), mul2_rounded(q, make_float2(-n.x, -n.y), mz));
+            v[e] = __fadd2_rn(mul2_rounded(q, c, mz), mul2_rounded(p, n, mz));
+        }
+    } else if (!FULL && rot > 0) {
+        // a pair (c, c + half) inside the first rot channels: its members may be different lanes',
+        // so the warp's rows pass through shared memory (partial rotation is the rare case)
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            *reinterpret_cast<float2*>(mine + 8 * l + 2 * e) = u[e];
+            *reinterpret_cast<float2*>(mine + H + 8 * l + 2 * e) = v[e];
+        }
+        __syncwarp();
+        if (used) {
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                float2(&z)[4] = part ? v : u;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float& x = e & 1 ? z[e >> 1].y : z[e >> 1].x;
+                    const int c = part * H + 8 * l + e;
+                    if (c < half) x = __fsub_rn(__fmul_rn(x, cs[c]), __fmul_rn(mine[c + half], cs[half + c]));
+                    else if (c < rot) x = __fadd_rn(__fmul_rn(x, cs[c - half]), __fmul_rn(mine[c - half], cs[c]));
+                }
+            }
+        }
+    }
+}
+
 // FULL: all D channels are rotated, in halves (the usual form); otherwise whatever the parameters say.
 template <int DT, int D, bool VEC, bool FULL>
 __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteArgs a) {
@@ -591,110 +700,9 @@ __global__ void __launch_bounds__(kWriteThreads) kv_write_kernel(const KvWriteAr
         rx.clear();
         ry.clear();
     }
-    // cosines and sines of the lane's pairs (the branches on the form of the rotation are the same for every lane)
-    const int rot = FULL ? D : a.p.rotary_dim, half = rot / 2;
-    const bool neighbours = !FULL && (a.p.flags & AASD_KV_ROPE_INTERLEAVED) != 0;
-    const float* cs = a.cos_sin + (int64_t)(used ? pos : 0) * rot;
-    float co[8], si[8];   // neighbours: pairs of the low half, then of the high half; else of channels 8l + e
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        co[e] = 1.f;
-        si[e] = 0.f;
-    }
-    if (rot > 0 && used) {
-        if (neighbours) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int c = (e < 4 ? 8 * l : H + 8 * l) + 2 * (e & 3);
-                if (c < rot) {
-                    co[e] = __ldg(cs + c / 2);
-                    si[e] = __ldg(cs + half + c / 2);
-                }
-            }
-        } else if (rot == D) {
-            load8<AASD_F32, VEC>(cs, 8 * l, co);
-            load8<AASD_F32, VEC>(cs, half + 8 * l, si);
-        }
-    }
     const bool key = h >= hq;
     float2 u[4], v[4];
-    rx.unpack(u);
-    ry.unpack(v);
-    const float2 mz = a.minus_zero;
-    // (the lanes of a row take the same way; shuffles stay among all lanes of the warp)
-    if (a.q_weight != nullptr || a.k_weight != nullptr) {
-        float s[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float2 q = __fadd2_rn(mul2_rounded(u[e], u[e], mz), mul2_rounded(v[e], v[e], mz));
-            s[e] = __fadd_rn(q.x, q.y);
-        }
-        float sum = __fadd_rn(__fadd_rn(s[0], s[1]), __fadd_rn(s[2], s[3]));
-#pragma unroll
-        for (int o = 1; o < L; o <<= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xFFFFFFFFu, sum, o));
-        const float r = __frcp_rn(__fsqrt_rn(__fadd_rn(__fmul_rn(sum, 1.0f / D), a.p.eps)));
-        const void* w = key ? a.k_weight : a.q_weight;
-        if (used && w != nullptr) {
-            Raw8<DT, VEC> g;
-            float2 wx[4], wy[4];
-            g.load(w, 8 * l);
-            g.unpack(wx);
-            g.load(w, H + 8 * l);
-            g.unpack(wy);
-            const float2 rr = make_float2(r, r);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                u[e] = __fmul2_rn(__fmul2_rn(u[e], rr), wx[e]);
-                v[e] = __fmul2_rn(__fmul2_rn(v[e], rr), wy[e]);
-            }
-        }
-    }
-    // (a - b is written a + (-b): the same rounding)
-    if (!FULL && rot > 0 && neighbours) {
-#pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            float2(&z)[4] = part ? v : u;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (part * H + 8 * l + 2 * e < rot) {
-                    const float c = co[4 * part + e], n = si[4 * part + e];
-                    z[e] = __fadd2_rn(mul2_rounded(z[e], make_float2(c, c), mz), mul2_rounded(make_float2(z[e].y, z[e].x), make_float2(-n, n), mz));
-                }
-            }
-        }
-    } else if (FULL || rot == D) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float2 c = make_float2(co[2 * e], co[2 * e + 1]), n = make_float2(si[2 * e], si[2 * e + 1]);
-            const float2 p = u[e], q = v[e];
-            u[e] = __fadd2_rn(mul2_rounded(p, c, mz), mul2_rounded(q, make_float2(-n.x, -n.y), mz));
-            v[e] = __fadd2_rn(mul2_rounded(q, c, mz), mul2_rounded(p, n, mz));
-        }
-    } else if (!FULL && rot > 0) {
-        // a pair (c, c + half) inside the first rot channels: its members may be different lanes',
-        // so the warp's rows pass through shared memory (partial rotation is the rare case)
-        float* mine = s_rows + group * D;
-        __syncwarp();
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            *reinterpret_cast<float2*>(mine + 8 * l + 2 * e) = u[e];
-            *reinterpret_cast<float2*>(mine + H + 8 * l + 2 * e) = v[e];
-        }
-        __syncwarp();
-        if (used) {
-#pragma unroll
-            for (int part = 0; part < 2; ++part) {
-                float2(&z)[4] = part ? v : u;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float& x = e & 1 ? z[e >> 1].y : z[e >> 1].x;
-                    const int c = part * H + 8 * l + e;
-                    if (c < half) x = __fsub_rn(__fmul_rn(x, cs[c]), __fmul_rn(mine[c + half], cs[half + c]));
-                    else if (c < rot) x = __fadd_rn(__fmul_rn(x, cs[c - half]), __fmul_rn(mine[c - half], cs[c]));
-                }
-            }
-        }
-    }
+    kv_norm_rotate<DT, D, VEC, FULL>(a, rx, ry, l, used, pos, key ? a.k_weight : a.q_weight, s_rows + group * D, u, v);
     if (live && h < hq) {
         const int64_t at = (t * hq + h) * D + 8 * l;
         store8<DT, VEC>(a.q_out, at, u);
@@ -816,23 +824,21 @@ struct KvCommitArgs {
 
 constexpr int kCommitThreads = 256;
 
-// grid: (sequence, group of heads of all layers).  Every CTA reads its tree's parents into shared
-// memory, walks the path there, turns it into (source slot, destination slot) pairs, and its
-// warps move the entries of one head after another.  Path nodes are in ascending order and never
-// in front of their depth, so a destination is a source of an earlier node at most: entries are
-// moved in ascending order, a batch's loads before its stores.  A token's values are single bytes 64 apart,
-// so a moved entry touches a 32-byte sector per byte of them: 256 paths of 8 layers (4 heads of 128
-// channels) take 15.4 us, and one path of 16 layers 2.9 us, the chain of its dependent loads.
-template <int D>
-__global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const KvCommitArgs a) {
-    constexpr int H = D / 2, W = H / 4;        // W: 32-bit words of a token's keys
-    __shared__ int s_node[AASD_KV_MAX_NODES];   // parents, then sources
-    __shared__ int s_path[AASD_KV_MAX_NODES];   // leaf first
-    __shared__ int s_len, s_bad;
-    pdl_launch_dependents();
-    pdl_wait();
-    const int b = blockIdx.x, tid = threadIdx.x;
-    const int cached = a.cached_len[b];
+// Slot of place `place` behind the cached tokens of sequence b, -1 where there is none.
+__device__ __forceinline__ int kv_commit_slot(const KvCommitArgs& a, int b, int cached, int place) {
+    const int64_t at = (int64_t)cached + place;
+    if (at / kPage >= a.p.max_pages) return -1;
+    const int page = a.block_table[(int64_t)b * a.p.max_pages + at / kPage];
+    return page < 0 || page >= a.p.n_pages ? -1 : page * kPage + (int)(at % kPage);
+}
+// The accepted path of sequence b, found by the whole CTA: `len` nodes, of which the first `from` are where they belong
+// already (len = 0: nothing to do).  Node of depth i: s_path[len - 1 - i], its slot: s_node[i] (AASD_KV_MAX_NODES
+// entries each).  The CTAs with blockIdx.y = 0 write the new length.
+struct KvPath {
+    int len, from;
+};
+__device__ __forceinline__ KvPath kv_accepted_path(const KvCommitArgs& a, int b, int cached, int* s_node, int* s_path, int& s_len, int& s_bad) {
+    const int tid = threadIdx.x;
     const int64_t first = a.p.rows_per_seq > 0 ? (int64_t)b * a.p.rows_per_seq : a.tok_offsets[b];
     const int n = a.kv_len[b] - cached;        // new tokens in the cache
     const int best = a.best_node[b];
@@ -843,9 +849,9 @@ __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const KvCommi
             if (n > AASD_KV_MAX_NODES || cached < 0 || (a.p.rows_per_seq > 0 && n > a.p.rows_per_seq))
                 raise(a.state, AASD_STATUS_BAD_OFFSETS);
         }
-        return;
+        return KvPath{0, 0};
     }
-    if (!AASD_IN_RANGE(best < AASD_KV_MAX_NODES && first >= 0, a.state)) return;
+    if (!AASD_IN_RANGE(best < AASD_KV_MAX_NODES && first >= 0, a.state)) return KvPath{0, 0};
     for (int i = tid; i <= best; i += kCommitThreads) s_node[i] = a.node_parent[first + i];
     if (tid == 0) s_bad = 0;
     __syncthreads();
@@ -865,16 +871,10 @@ __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const KvCommi
     __syncthreads();
     const int len = s_len;
     // the path is leaf first: entry i (depth i) is s_path[len - 1 - i]
-    auto slot_of = [&](int place) {
-        const int64_t at = (int64_t)cached + place;
-        if (at / kPage >= a.p.max_pages) return -1;
-        const int page = a.block_table[(int64_t)b * a.p.max_pages + at / kPage];
-        return page < 0 || page >= a.p.n_pages ? -1 : page * kPage + (int)(at % kPage);
-    };
     if (!s_bad)
         for (int i = tid; i < len; i += kCommitThreads) {
-            const int src = slot_of(s_path[len - 1 - i]);
-            if (src < 0 || slot_of(i) < 0) s_bad = 1;
+            const int src = kv_commit_slot(a, b, cached, s_path[len - 1 - i]);
+            if (src < 0 || kv_commit_slot(a, b, cached, i) < 0) s_bad = 1;
             s_node[i] = src;     // (the parents have been read)
         }
     __syncthreads();
@@ -883,10 +883,33 @@ __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const KvCommi
         a.new_len[b] = bad ? cached : cached + len;
         if (bad) raise(a.state, AASD_STATUS_BAD_OFFSETS);
     }
-    if (bad) return;
+    if (bad) return KvPath{0, 0};
     int from = 0;                               // nodes that are where they belong already
     while (from < len && s_path[len - 1 - from] == from) ++from;
-    if (from == len) return;
+    return KvPath{len, from};
+}
+
+// grid: (sequence, group of heads of all layers).  Every CTA reads its tree's parents into shared
+// memory, walks the path there, turns it into (source slot, destination slot) pairs, and its
+// warps move the entries of one head after another.  Path nodes are in ascending order and never
+// in front of their depth, so a destination is a source of an earlier node at most: entries are
+// moved in ascending order, a batch's loads before its stores.  A token's values are single bytes 64 apart,
+// so a moved entry touches a 32-byte sector per byte of them: 256 paths of 8 layers (4 heads of 128
+// channels) take 15.4 us, and one path of 16 layers 2.9 us, the chain of its dependent loads.
+template <int D>
+__global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(const KvCommitArgs a) {
+    constexpr int H = D / 2, W = H / 4;        // W: 32-bit words of a token's keys
+    __shared__ int s_node[AASD_KV_MAX_NODES];   // parents, then sources
+    __shared__ int s_path[AASD_KV_MAX_NODES];   // leaf first
+    __shared__ int s_len, s_bad;
+    pdl_launch_dependents();
+    pdl_wait();
+    const int b = blockIdx.x, tid = threadIdx.x;
+    const int cached = a.cached_len[b];
+    const KvPath path = kv_accepted_path(a, b, cached, s_node, s_path, s_len, s_bad);
+    const int len = path.len, from = path.from;
+    if (from >= len) return;
+    const auto slot_of = [&](int place) { return kv_commit_slot(a, b, cached, place); };
     const int lane = tid & 31;
     const int64_t items = (int64_t)a.p.n_layers * a.p.n_kv_heads;
     const int64_t hb = kv_head_bytes(D);
