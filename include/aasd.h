@@ -585,6 +585,126 @@ int aasd_kv_commit(aasd_ctx* ctx, void* pages, const int32_t* block_table, const
 int aasd_kv_read(aasd_ctx* ctx, const void* pages, const int32_t* slots, int64_t n, int32_t n_pages,
                  int32_t n_kv_heads, int32_t head_dim, int32_t dtype, void* k_out, void* v_out);
 
+/* ---- the same cache held in 8 bits ---------------------------------------------------------- */
+
+/* (No counterpart in the paper.)  Pages of 64 tokens as above, planned by the same aasd_kv_plan, with an e4m3 code
+ * per channel and one scale for the keys and one for the values of a page's head: 2 D bytes per token and head,
+ * half of bf16.  One head's block of a page, aasd_kvb_head_bytes(head_dim) = 128 * head_dim + 16 bytes:
+ *   keys    [64][D]    e4m3 codes; rows of 128 bytes (64 with D = 64; D = 256: channels 0..127 of all tokens, then the
+ *                      others), in which 16-byte chunk c of token t lies at chunk c ^ (t % 8) (D = 64: c ^ (t / 2 % 4))
+ *   values  [64][D]    likewise
+ *   f32     scale of the keys, scale of the values; 8 bytes of nothing
+ * A code stands for scale * code.  A scale is a power of two, 2^-64 to 2^120: the least one with max|x| <= 448 * scale over
+ * the rows that are stored together.  Where the page holds older tokens the scale is never lowered; when it grows
+ * they are rounded to the new one, which changes no value of at least 2^-6 new scales.
+ * The pool starts on a 16-byte boundary; head_dim is 64, 128 or 256.  What lies in a page past a sequence's end is
+ * never looked at, whatever it holds, and neither is the scale of a page without a cached token when it is stored to. */
+int aasd_kvb_head_bytes(int32_t head_dim, size_t* bytes);
+
+typedef struct aasd_kvb_write_params {
+    aasd_kv_write_params rows;   /* as in aasd_kv_write */
+    int32_t n_seqs;
+    int32_t max_pages;
+    int32_t rows_per_seq;        /* > 0: padded token rows; 0: packed (tok_offsets) */
+} aasd_kvb_write_params;
+
+/* Norm, rotation and q_out / k_out as in aasd_kv_write.  Tokens 0 .. kv_len[b] - cached_len[b] - 1 of sequence b (as
+ * aasd_kv_plan has placed them; at most the sequence's rows) are stored at places cached_len[b] + i of its pages, the codes
+ * rounded to nearest from fp32; all operations round by themselves, so that the cache's bytes are a function of the
+ * inputs and of what the pages held.  A row with a NaN or infinity is stored as zeros and raises
+ * AASD_STATUS_BAD_ROW; so is (without that status) a row that has a place but no position.  Positions as in aasd_kv_write.  A
+ * page outside the pool or the table raises AASD_STATUS_BAD_OFFSETS; its rows are not stored (k_out keeps what it held).  k_out
+ * rows of tokens without a place are left as they are.  Two sequences must not share a page that is stored to. */
+int aasd_kvb_write(aasd_ctx* ctx, const void* q, const void* k, const void* v, const void* q_weight,
+                   const void* k_weight, const float* cos_sin, const int32_t* positions,
+                   const int32_t* block_table, const int32_t* cached_len, const int32_t* kv_len,
+                   const int32_t* tok_offsets, int64_t n_tokens, const aasd_kvb_write_params* params, void* pages,
+                   void* q_out, void* k_out);
+
+/* aasd_kv_attend over an 8-bit pool: the same arguments, masks, errors and scratch (aasd_kv_workspace_init).  Sums and the
+ * softmax's statistics are fp32; the result is rounded once. */
+int aasd_kvb_attend(aasd_ctx* ctx, const void* q, const void* pages, const int32_t* block_table,
+                    const int32_t* cached_len, const int32_t* kv_len, const int32_t* tok_offsets,
+                    const int32_t* node_parent, const aasd_kv_attend_params* params, void* workspace,
+                    size_t workspace_bytes, const aasd_kv_attend_out* out);
+
+/* aasd_kv_commit on 8-bit pools.  A page that entries move to takes the largest scale among its own and those of the pages
+ * they come from, in each layer, head and half; its live entries are rounded to it. */
+int aasd_kvb_commit(aasd_ctx* ctx, void* pages, const int32_t* block_table, const int32_t* cached_len,
+                    const int32_t* kv_len, const int32_t* tok_offsets, const int32_t* best_node,
+                    const int32_t* node_parent, const aasd_kv_commit_params* params, int32_t* new_len);
+
+/* aasd_kv_read on an 8-bit pool: values scale * code, exact before the rounding to dtype (and exact in bf16 from 2^-126 on). */
+int aasd_kvb_read(aasd_ctx* ctx, const void* pages, const int32_t* slots, int64_t n, int32_t n_pages,
+                  int32_t n_kv_heads, int32_t head_dim, int32_t dtype, void* k_out, void* v_out);
+
+/* ---- pages with several holders: forking, freeing, copying, compacting ------------------------ */
+
+/* (No counterpart in the paper.)  Sequences that begin alike (several samples of one prompt, a prompt kept for
+ * others) can hold the same pages: page_shares[p] counts page p's holders beyond the first (0 for a page with one holder, and for
+ * a free one).  Pages are moved as bytes, so the calls serve 4-bit and 8-bit pools.
+ * A shared page must not be written: that cannot happen as long as a sequence is not cut to fewer cached tokens than others
+ * took from it.  aasd_kv_plan knows nothing of holders.  Where pages may be shared, call aasd_kv_free with the
+ * same cached_len and n_new in front of it: it leaves nothing that plan would give back. */
+typedef struct aasd_kv_books {   /* as in aasd_kv_plan_state; all read and written */
+    int32_t* block_table;   /* [n_seqs x max_pages] */
+    int32_t* seq_pages;     /* [n_seqs] */
+    int32_t* free_pages;    /* [n_pages] */
+    int32_t* n_free;        /* [1] */
+    int32_t* page_shares;   /* [n_pages] */
+} aasd_kv_books;
+
+typedef struct aasd_kv_books_params {
+    int32_t n_seqs;
+    int32_t n_pages;
+    int32_t max_pages;
+} aasd_kv_books_params;
+
+/* The layers' pools: page p of layer l is the page_bytes (a multiple of 16) from pages + l * layer_stride + p * page_bytes on.
+ * n_layers = 0: books alone are dealt with. */
+typedef struct aasd_kv_pool {
+    void* pages;            /* 16-byte aligned */
+    int32_t n_layers;
+    int64_t page_bytes;     /* n_kv_heads times the bytes of a head's block */
+    int64_t layer_stride;   /* bytes, a multiple of 16 */
+} aasd_kv_pool;
+
+/* Drops every page that sequence b holds past its first ceil((keep_len[b] + n_new[b]) / 64) ones (n_new NULL: zeros; a keep_len of
+ * NONE leaves the sequence alone).  Pages that lose their last holder go on the stack in the order of their numbers.
+ * Inconsistent books raise AASD_STATUS_BAD_OFFSETS; nothing outside the arrays is touched. */
+int aasd_kv_free(aasd_ctx* ctx, const int32_t* keep_len, const int32_t* n_new, const aasd_kv_books_params* params,
+                 const aasd_kv_books* books);
+
+typedef struct aasd_kv_fork_out {   /* all required, [n_forks] each */
+    int32_t* new_len;       /* cached tokens that the new sequence has; NONE: the fork was not made */
+    int32_t* copy_src;      /* page that was begun, NONE where the length ends with a page */
+    int32_t* copy_dst;      /* its copy */
+} aasd_kv_fork_out;
+
+/* For every fork i: sequence dst_seq[i], which holds no pages, becomes the first fork_len[i] cached tokens (NULL: all) of
+ * sequence src_seq[i].  Whole pages are shared; a last page that is begun is copied, in every layer, to one off the stack.
+ * cached_len[dst], its row of the table, its page count and page_shares are set.  Pages come off the top fork by fork; a fork that the
+ * stack cannot give a page any more is not made (AASD_STATUS_KV_FULL); those after it that need none are.  A fork whose
+ * destination holds pages or is an earlier fork's, whose source is such a destination of the same call, or whose length the
+ * source does not have, is not made either (AASD_STATUS_BAD_OFFSETS). */
+int aasd_kv_fork(aasd_ctx* ctx, const int32_t* src_seq, const int32_t* dst_seq, const int32_t* fork_len,
+                 int32_t n_forks, const aasd_kv_books_params* params, const aasd_kv_books* books,
+                 int32_t* cached_len, const aasd_kv_pool* pool, const aasd_kv_fork_out* out);
+
+/* Copies page src[i] to page dst[i], i < n, in every layer.  NONE in either leaves a pair out; a page outside the pool
+ * raises AASD_STATUS_ID_RANGE and does the same.  No destination may be named twice or be a source as well. */
+int aasd_kv_copy(aasd_ctx* ctx, const aasd_kv_pool* pool, int32_t n_pages, const int32_t* src, const int32_t* dst,
+                 int32_t n);
+
+/* Moves the pages in use to the front: with u of them, the k-th one at or behind place u goes to the k-th free place before it, in
+ * every layer; the tables and page_shares follow.  Afterwards the first u pages of the pool are the ones in use (the
+ * pool may be cut or grown behind them) and the stack holds the others, page u on top.  page_map [n_pages]: the new
+ * number of each page that was in use, NONE for the others, for whatever else names pages; moves [n_pages]: scratch (the
+ * moves as pairs); n_moved [1].  A stack with repetitions or pages outside the pool raises AASD_STATUS_BAD_OFFSETS and nothing
+ * moves; an entry of the table that is not in use raises it and stays. */
+int aasd_kv_compact(aasd_ctx* ctx, const aasd_kv_books_params* params, const aasd_kv_books* books,
+                    const aasd_kv_pool* pool, int32_t* page_map, int32_t* moves, int32_t* n_moved);
+
 /* ---- measurement aid ------------------------------------------------------------------ */
 
 /* Reads `bytes` bytes at `buffer` (16-byte aligned, bytes a multiple of 16) once with plain

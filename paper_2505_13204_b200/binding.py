@@ -37,6 +37,8 @@ EXPORTS = [
     "aasd_tree_build", "aasd_verify_tree", "aasd_probe_read", "aasd_debug_withhold_tile",
     "aasd_kv_plan", "aasd_kv_head_bytes", "aasd_kv_write", "aasd_kv_read", "aasd_kv_commit",
     "aasd_kv_workspace_bytes", "aasd_kv_workspace_init", "aasd_kv_attend",
+    "aasd_kvb_head_bytes", "aasd_kvb_write", "aasd_kvb_read", "aasd_kvb_commit", "aasd_kvb_attend",
+    "aasd_kv_free", "aasd_kv_fork", "aasd_kv_copy", "aasd_kv_compact",
 ]
 STATIC_MAX_ROWS = STATIC_MAX_CANDS = 8192
 
@@ -132,6 +134,26 @@ class KvCommitParams(C.Structure):
                 ("n_layers", C.c_int32), ("layer_stride", C.c_int64)]
 
 
+class KvbWriteParams(C.Structure):
+    _fields_ = [("rows", KvWriteParams), ("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("rows_per_seq", C.c_int32)]
+
+
+class KvBooks(C.Structure):
+    _fields_ = [(n, _vp) for n in ("block_table", "seq_pages", "free_pages", "n_free", "page_shares")]
+
+
+class KvBooksParams(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32)]
+
+
+class KvPool(C.Structure):
+    _fields_ = [("pages", _vp), ("n_layers", C.c_int32), ("page_bytes", C.c_int64), ("layer_stride", C.c_int64)]
+
+
+class KvForkOut(C.Structure):
+    _fields_ = [(n, _vp) for n in ("new_len", "copy_src", "copy_dst")]
+
+
 class Counters(C.Structure):
     _fields_ = [(n, C.c_uint64) for n in ("rows", "bad_rows", "redo_rows", "near_threshold",
                                           "accepted", "sampler_recheck", "sampler_exact",
@@ -192,6 +214,16 @@ def load_library(path: str | None = None):
     lib.aasd_kv_workspace_bytes.argtypes = [C.c_int32, C.POINTER(C.c_size_t)]
     lib.aasd_kv_workspace_init.argtypes = [_vp, _vp, C.c_size_t, C.c_int32]
     lib.aasd_kv_attend.argtypes = [_vp] * 8 + [C.POINTER(KvAttendParams), _vp, C.c_size_t, C.POINTER(KvAttendOut)]
+    lib.aasd_kvb_head_bytes.argtypes = lib.aasd_kv_head_bytes.argtypes
+    lib.aasd_kvb_write.argtypes = [_vp] * 12 + [C.c_int64, C.POINTER(KvbWriteParams), _vp, _vp, _vp]
+    lib.aasd_kvb_read.argtypes = lib.aasd_kv_read.argtypes
+    lib.aasd_kvb_commit.argtypes = lib.aasd_kv_commit.argtypes
+    lib.aasd_kvb_attend.argtypes = lib.aasd_kv_attend.argtypes
+    books = [C.POINTER(KvBooksParams), C.POINTER(KvBooks)]
+    lib.aasd_kv_free.argtypes = [_vp, _vp, _vp] + books
+    lib.aasd_kv_fork.argtypes = [_vp, _vp, _vp, _vp, C.c_int32] + books + [_vp, C.POINTER(KvPool), C.POINTER(KvForkOut)]
+    lib.aasd_kv_copy.argtypes = [_vp, C.POINTER(KvPool), C.c_int32, _vp, _vp, C.c_int32]
+    lib.aasd_kv_compact.argtypes = [_vp] + books + [C.POINTER(KvPool), _vp, _vp, _vp]
     if path == _build.LIB:
         _lib = lib
     return lib
@@ -244,6 +276,19 @@ def kv_pages(n_pages: int, n_kv_heads: int, head_dim: int, layers: int | None = 
     return torch.empty(shape if layers is None else (layers,) + shape, dtype=torch.uint8, device=device)
 
 
+def kvb_head_bytes(head_dim: int) -> int:
+    """Bytes of one key/value head's block of an 8-bit cache page (aasd_kvb_head_bytes)."""
+    n = C.c_size_t()
+    _check(load_library().aasd_kvb_head_bytes(int(head_dim), C.byref(n)), "aasd_kvb_head_bytes")
+    return n.value
+
+
+def kvb_pages(n_pages: int, n_kv_heads: int, head_dim: int, layers: int | None = None, device="cuda") -> torch.Tensor:
+    """``kv_pages`` for the 8-bit cache."""
+    shape = (n_pages, n_kv_heads, kvb_head_bytes(head_dim))
+    return torch.empty(shape if layers is None else (layers,) + shape, dtype=torch.uint8, device=device)
+
+
 # The library cannot see how long its arrays are: what it reads and writes by the counts of the
 # others is checked here.  (Longer ones are fine.)
 def _kv_need(ok, what: str):
@@ -270,6 +315,15 @@ def _kv_pool(pages: torch.Tensor, dims: int, device: int):
     n = shape[-1] - 512
     _kv_need(n > 0 and n % KV_PAGE == 0, "blocks of a page")
     return shape[-3], shape[-2], n // KV_PAGE
+
+
+def _kvb_pool(pages: torch.Tensor, dims: int, device: int):
+    """The same of an 8-bit page pool."""
+    shape = pages.shape
+    assert len(shape) == dims and pages.dtype is torch.uint8 and pages.get_device() == device and pages.is_contiguous()
+    n = shape[-1] - 16
+    _kv_need(n > 0 and n % (2 * KV_PAGE) == 0, "blocks of a page")
+    return shape[-3], shape[-2], n // (2 * KV_PAGE)
 
 
 def _kv_dtype(x: torch.Tensor, dt) -> int:
@@ -326,6 +380,90 @@ def verify_static(target_logits, draft_ids, cand_offsets=None, draft_flags=None,
                                   Cn, R, C.byref(prm), C.byref(out), _p(status_bits)),
            "aasd_verify_static")
     return o
+
+
+# Calls that both caches have: ``name`` of the library, ``pool`` looks a page pool over.
+def _kv_attend_call(name, pool):
+    def attend(self, q, pages, block_table, cached_len, kv_len, tok_offsets=None, rows_per_seq=0,
+               node_parent=None, scale=0.0, want_lse=False, outputs=None):
+        _kv_i32(self.device_index, block_table, cached_len, kv_len, tok_offsets, node_parent)
+        T, Hq, D = q.shape
+        B, P = block_table.shape
+        qs, qh, qd = q.stride()
+        if not (T > 1 and qh == D and qd == 1):
+            qs = _kv_token_stride(q)
+        N, Hkv, Dp = pool(pages, 3, self.device_index)
+        assert Dp == D and q.get_device() == self.device_index
+        _kv_need(cached_len.numel() >= B and kv_len.numel() >= B and (tok_offsets is None or tok_offsets.numel() > B) and
+                 (node_parent is None or node_parent.numel() >= T), "lengths of %s's arrays" % name)
+        o = outputs
+        if o is None:
+            o = dict(out=q.new_empty((T, Hq, D)))
+        else:
+            _kv_like(q, T * Hq * D, o["out"])
+        lse = o.get("lse")
+        if want_lse and lse is None:
+            lse = o["lse"] = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
+        elif lse is not None:
+            assert lse.dtype is torch.float32 and lse.get_device() == self.device_index and lse.is_contiguous()
+            _kv_need(lse.numel() >= T * Hq, "outputs")
+        prm = self._kv_struct(KvAttendParams, B, Hq, Hkv, D, N, P, _kv_dtype(q, q.dtype), int(rows_per_seq),
+                              T, qs, scale)
+        out = KvAttendOut(o["out"].data_ptr(), None if lse is None else lse.data_ptr())
+        ws = self.kv_workspace(D)
+        rc = getattr(self.lib, name)(self._h, q.data_ptr(), pages.data_ptr(), block_table.data_ptr(), cached_len.data_ptr(),
+                                     kv_len.data_ptr(), None if tok_offsets is None else tok_offsets.data_ptr(),
+                                     None if node_parent is None else node_parent.data_ptr(), prm, ws.data_ptr(),
+                                     ws.numel(), C.byref(out))
+        if D not in self._kv_ws:      # (captured: see kv_workspace)
+            self.lib.aasd_workspace_release(self._h, _vp(ws.data_ptr()))
+        if rc:
+            raise AasdError(rc, name)
+        return o
+    return attend
+
+
+def _kv_commit_call(name, pool):
+    def commit(self, pages, block_table, cached_len, kv_len, best_node, node_parent, tok_offsets=None, outputs=None):
+        _kv_i32(self.device_index, block_table, cached_len, kv_len, best_node, node_parent, tok_offsets, outputs)
+        N, H, D = pool(pages, 4, self.device_index)
+        B, P = block_table.shape
+        nodes, rows = node_parent.shape, 0
+        if tok_offsets is None:
+            _kv_need(len(nodes) == 2 and nodes[0] >= B, "lengths of %s's arrays" % name)
+            rows = nodes[1]
+        _kv_need(cached_len.numel() >= B and kv_len.numel() >= B and best_node.numel() >= B and (outputs is None or outputs.numel() >= B) and
+                 (tok_offsets is None or tok_offsets.numel() > B), "lengths of %s's arrays" % name)
+        new_len = outputs if outputs is not None else cached_len.new_empty(B)
+        prm = self._kv_struct(KvCommitParams, B, H, D, N, P, rows, pages.shape[0], pages.stride(0))
+        rc = getattr(self.lib, name)(self._h, pages.data_ptr(), block_table.data_ptr(), cached_len.data_ptr(), kv_len.data_ptr(),
+                                     None if tok_offsets is None else tok_offsets.data_ptr(), best_node.data_ptr(),
+                                     node_parent.data_ptr(), prm, new_len.data_ptr())
+        if rc:
+            raise AasdError(rc, name)
+        return new_len
+    return commit
+
+
+def _kv_read_call(name, pool):
+    def read(self, pages, slots, head_dim, dtype=torch.bfloat16, outputs=None):
+        _kv_i32(self.device_index, slots)
+        N, H, D = pool(pages, 3, self.device_index)
+        assert D == head_dim
+        n = slots.numel()
+        o = outputs
+        if o is None:
+            shape = (n, H, head_dim)
+            o = dict(k=torch.empty(shape, dtype=dtype, device=pages.device), v=torch.empty(shape, dtype=dtype, device=pages.device))
+        else:
+            assert o["k"].get_device() == self.device_index
+            _kv_like(o["k"], n * H * head_dim, o["k"], o["v"])
+        rc = getattr(self.lib, name)(self._h, pages.data_ptr(), slots.data_ptr(), n, N, H, head_dim, _dtype_code(o["k"]),
+                                   o["k"].data_ptr(), o["v"].data_ptr())
+        if rc:
+            raise AasdError(rc, name)
+        return o
+    return read
 
 
 class Context:
@@ -579,10 +717,13 @@ class Context:
         return r[0]
 
     def kv_plan(self, cached_len, n_new, block_table, seq_pages, free_pages, n_free, n_tokens,
-                rows_per_seq=0, node_depth=None, outputs=None):
+                rows_per_seq=0, node_depth=None, outputs=None, page_shares=None):
         """aasd_kv_plan: brings ``block_table`` [B, max_pages], ``seq_pages``, ``free_pages`` and
         ``n_free`` (all int32, changed in place) in line with ``cached_len + n_new`` tokens per
-        sequence; returns kv_len, tok_offsets, slot_map and positions of the new tokens."""
+        sequence; returns kv_len, tok_offsets, slot_map and positions of the new tokens.  ``page_shares``: pages may
+        have several holders (``kv_fork``); ``kv_free`` then gives pages back in front of the call."""
+        if page_shares is not None:
+            self.kv_free(cached_len, block_table, seq_pages, free_pages, n_free, page_shares, n_new)
         _kv_i32(self.device_index, cached_len, n_new, block_table, seq_pages, free_pages, n_free, node_depth)
         B, P = block_table.shape
         _kv_need(cached_len.numel() >= B and n_new.numel() >= B and seq_pages.numel() >= B and n_free.numel() > 0 and
@@ -668,87 +809,138 @@ class Context:
                 self._kv_ws[head_dim] = ws
         return ws
 
-    def kv_attend(self, q, pages, block_table, cached_len, kv_len, tok_offsets=None, rows_per_seq=0,
-                  node_parent=None, scale=0.0, want_lse=False, outputs=None):
-        """aasd_kv_attend: attention of the new tokens ``q`` [T, Hq, D] over the cache.  Token rows
+    kv_attend = _kv_attend_call("aasd_kv_attend", _kv_pool)
+    kv_attend.__doc__ = """aasd_kv_attend: attention of the new tokens ``q`` [T, Hq, D] over the cache.  Token rows
         are packed (``tok_offsets``) or padded (``rows_per_seq``); ``node_parent`` makes them draft
         trees.  Returns a dict with out [T, Hq, D] and, with ``want_lse``, lse [T, Hq]."""
-        _kv_i32(self.device_index, block_table, cached_len, kv_len, tok_offsets, node_parent)
-        T, Hq, D = q.shape
-        B, P = block_table.shape
-        qs, qh, qd = q.stride()
-        if not (T > 1 and qh == D and qd == 1):
-            qs = _kv_token_stride(q)
-        N, Hkv, Dp = _kv_pool(pages, 3, self.device_index)
-        assert Dp == D and q.get_device() == self.device_index
-        _kv_need(cached_len.numel() >= B and kv_len.numel() >= B and (tok_offsets is None or tok_offsets.numel() > B) and
-                 (node_parent is None or node_parent.numel() >= T), "lengths of kv_attend's arrays")
-        o = outputs
-        if o is None:
-            o = dict(out=q.new_empty((T, Hq, D)))
-        else:
-            _kv_like(q, T * Hq * D, o["out"])
-        lse = o.get("lse")
-        if want_lse and lse is None:
-            lse = o["lse"] = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
-        elif lse is not None:
-            assert lse.dtype is torch.float32 and lse.get_device() == self.device_index and lse.is_contiguous()
-            _kv_need(lse.numel() >= T * Hq, "outputs")
-        prm = self._kv_struct(KvAttendParams, B, Hq, Hkv, D, N, P, _kv_dtype(q, q.dtype), int(rows_per_seq),
-                              T, qs, scale)
-        out = KvAttendOut(o["out"].data_ptr(), None if lse is None else lse.data_ptr())
-        ws = self.kv_workspace(D)
-        rc = self.lib.aasd_kv_attend(self._h, q.data_ptr(), pages.data_ptr(), block_table.data_ptr(), cached_len.data_ptr(),
-                                     kv_len.data_ptr(), None if tok_offsets is None else tok_offsets.data_ptr(),
-                                     None if node_parent is None else node_parent.data_ptr(), prm, ws.data_ptr(),
-                                     ws.numel(), C.byref(out))
-        if D not in self._kv_ws:      # (captured: see kv_workspace)
-            self.lib.aasd_workspace_release(self._h, _vp(ws.data_ptr()))
-        if rc:
-            raise AasdError(rc, "aasd_kv_attend")
-        return o
-
-    def kv_commit(self, pages, block_table, cached_len, kv_len, best_node, node_parent, tok_offsets=None,
-                  outputs=None):
-        """aasd_kv_commit: moves the accepted paths' entries in the pools of all layers (``pages``
+    kv_commit = _kv_commit_call("aasd_kv_commit", _kv_pool)
+    kv_commit.__doc__ = """aasd_kv_commit: moves the accepted paths' entries in the pools of all layers (``pages``
         [layers, n_pages, Hkv, bytes]) and returns the new cached lengths.  ``node_parent`` is
         [B, rows_per_seq], or flat with ``tok_offsets``."""
-        _kv_i32(self.device_index, block_table, cached_len, kv_len, best_node, node_parent, tok_offsets, outputs)
-        N, H, D = _kv_pool(pages, 4, self.device_index)
-        B, P = block_table.shape
-        nodes, rows = node_parent.shape, 0
-        if tok_offsets is None:
-            _kv_need(len(nodes) == 2 and nodes[0] >= B, "lengths of kv_commit's arrays")
-            rows = nodes[1]
-        _kv_need(cached_len.numel() >= B and kv_len.numel() >= B and best_node.numel() >= B and (outputs is None or outputs.numel() >= B) and
-                 (tok_offsets is None or tok_offsets.numel() > B), "lengths of kv_commit's arrays")
-        new_len = outputs if outputs is not None else cached_len.new_empty(B)
-        prm = self._kv_struct(KvCommitParams, B, H, D, N, P, rows, pages.shape[0], pages.stride(0))
-        rc = self.lib.aasd_kv_commit(self._h, pages.data_ptr(), block_table.data_ptr(), cached_len.data_ptr(), kv_len.data_ptr(),
-                                     None if tok_offsets is None else tok_offsets.data_ptr(), best_node.data_ptr(),
-                                     node_parent.data_ptr(), prm, new_len.data_ptr())
-        if rc:
-            raise AasdError(rc, "aasd_kv_commit")
-        return new_len
-
-    def kv_read(self, pages, slots, head_dim, dtype=torch.bfloat16, outputs=None):
-        """aasd_kv_read: the entries at ``slots`` as values, k and v [n, Hkv, D].  Several layers at
+    kv_read = _kv_read_call("aasd_kv_read", _kv_pool)
+    kv_read.__doc__ = """aasd_kv_read: the entries at ``slots`` as values, k and v [n, Hkv, D].  Several layers at
         once: pass ``pages.flatten(0, 1)`` and slots raised by layer * n_pages * KV_PAGE."""
-        _kv_i32(self.device_index, slots)
-        N, H, D = _kv_pool(pages, 3, self.device_index)
-        assert D == head_dim
-        n = slots.numel()
+
+    # ---- the paged 8-bit cache (kv_plan and kv_workspace serve it too) -----------------------
+    def kvb_write(self, pages, q, k, v, block_table, cached_len, kv_len, positions, tok_offsets=None, rows_per_seq=0,
+                  cos_sin=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, keep_k=False, outputs=None):
+        """aasd_kvb_write: norms and rotates ``q`` [T, Hq, D] and ``k`` [T, Hkv, D] as ``kv_write`` does and stores the tokens
+        that ``kv_plan`` has placed (``kv_len`` and ``positions`` are its outputs) at the end of their sequences' pages.  Token
+        rows are packed (``tok_offsets``) or padded (``rows_per_seq``).  Returns a dict with q and, with
+        ``keep_k``, the rotated k."""
+        dev = self.device_index
+        _kv_i32(dev, block_table, cached_len, kv_len, positions, tok_offsets)
+        T, Hq, D = q.shape
+        kv = k.shape
+        Tk, Hkv, Dk = kv
+        qs, ks, vs = _kv_token_stride(q), _kv_token_stride(k), _kv_token_stride(v)
+        dt = q.dtype
+        B, P = block_table.shape
+        N, Hp, Dp = _kvb_pool(pages, 3, dev)
+        assert k.dtype is dt and v.dtype is dt and v.shape == kv and Dk == D and Dp == D and Hp == Hkv
+        assert q.get_device() == dev and k.get_device() == dev and v.get_device() == dev
+        _kv_need(Tk == T and positions.numel() == T and cached_len.numel() >= B and kv_len.numel() >= B and
+                 (tok_offsets is None or tok_offsets.numel() > B), "lengths of kvb_write's arrays")
+        for w in (q_weight, k_weight):
+            assert w is None or (w.dtype is dt and w.get_device() == dev and w.numel() == D and w.is_contiguous())
         o = outputs
         if o is None:
-            shape = (n, H, head_dim)
-            o = dict(k=torch.empty(shape, dtype=dtype, device=pages.device), v=torch.empty(shape, dtype=dtype, device=pages.device))
+            o = dict(q=q.new_empty((T, Hq, D)), k=q.new_empty((T, Hkv, D)) if keep_k else None)
         else:
-            assert o["k"].get_device() == self.device_index
-            _kv_like(o["k"], n * H * head_dim, o["k"], o["v"])
-        rc = self.lib.aasd_kv_read(self._h, pages.data_ptr(), slots.data_ptr(), n, N, H, head_dim, _dtype_code(o["k"]),
-                                   o["k"].data_ptr(), o["v"].data_ptr())
+            _kv_like(q, T * Hq * D, o["q"])
+            _kv_like(q, T * Hkv * D, o.get("k"))
+        rot = limit = 0
+        if cos_sin is not None:
+            assert cos_sin.dtype is torch.float32 and cos_sin.get_device() == dev and cos_sin.is_contiguous() and cos_sin.dim() == 2
+            limit, rot = cos_sin.shape
+        key = (KvbWriteParams, Hq, Hkv, D, N, dt, qs, ks, vs, rot, limit, eps, interleaved, B, P, rows_per_seq)
+        prm = self._kv_structs.get(key)
+        if prm is None:
+            if len(self._kv_structs) > 4096:
+                self._kv_structs.clear()
+            rows = KvWriteParams(Hq, Hkv, D, N, _kv_dtype(q, dt), qs, ks, vs, rot, limit, eps, KV_ROPE_INTERLEAVED if interleaved else 0)
+            one = KvbWriteParams(rows, B, P, int(rows_per_seq))
+            prm = self._kv_structs[key] = (C.byref(one), one)
+        ko = o.get("k")
+        rc = self.lib.aasd_kvb_write(self._h, q.data_ptr(), k.data_ptr(), v.data_ptr(), _p(q_weight), _p(k_weight), _p(cos_sin),
+                                     positions.data_ptr(), block_table.data_ptr(), cached_len.data_ptr(), kv_len.data_ptr(), _p(tok_offsets),
+                                     T, prm[0], pages.data_ptr(), o["q"].data_ptr(), _p(ko))
         if rc:
-            raise AasdError(rc, "aasd_kv_read")
+            raise AasdError(rc, "aasd_kvb_write")
+        return o
+
+    kvb_attend = _kv_attend_call("aasd_kvb_attend", _kvb_pool)
+    kvb_attend.__doc__ = """aasd_kvb_attend: ``kv_attend`` over an 8-bit pool."""
+    kvb_commit = _kv_commit_call("aasd_kvb_commit", _kvb_pool)
+    kvb_commit.__doc__ = """aasd_kvb_commit: ``kv_commit`` on 8-bit pools."""
+    kvb_read = _kv_read_call("aasd_kvb_read", _kvb_pool)
+    kvb_read.__doc__ = """aasd_kvb_read: ``kv_read`` on an 8-bit pool."""
+
+    # ---- pages with several holders, in pools of either format -------------------------------
+    def _kv_books(self, block_table, seq_pages, free_pages, n_free, page_shares):
+        _kv_i32(self.device_index, block_table, seq_pages, free_pages, n_free, page_shares)
+        B, P = block_table.shape
+        N = free_pages.numel()
+        _kv_need(seq_pages.numel() >= B and n_free.numel() > 0 and page_shares.numel() >= N, "lengths of the books")
+        return B, P, N, self._kv_struct(KvBooksParams, B, N, P), KvBooks(
+            block_table.data_ptr(), seq_pages.data_ptr(), free_pages.data_ptr(), n_free.data_ptr(), page_shares.data_ptr())
+
+    def _kv_layers(self, pages, n_pages):
+        """The pools of all layers, [layers, n_pages, Hkv, bytes] of either format."""
+        assert pages.dim() == 4 and pages.dtype is torch.uint8 and pages.get_device() == self.device_index and pages.is_contiguous()
+        L, N, H, size = pages.shape
+        _kv_need(N == n_pages and H * size % 16 == 0, "pages of the pools")
+        return KvPool(pages.data_ptr(), L, H * size, N * H * size)
+
+    def kv_free(self, keep_len, block_table, seq_pages, free_pages, n_free, page_shares, n_new=None):
+        """aasd_kv_free: sequences keep the pages of their first ``keep_len`` (+ ``n_new``) tokens; pages without another holder go
+        back on the stack.  The books (int32) are changed in place; ``page_shares`` counts holders beyond the first."""
+        B, P, N, prm, books = self._kv_books(block_table, seq_pages, free_pages, n_free, page_shares)
+        _kv_i32(self.device_index, keep_len, n_new)
+        _kv_need(keep_len.numel() >= B and (n_new is None or n_new.numel() >= B), "lengths of kv_free's arrays")
+        _check(self.lib.aasd_kv_free(self._h, keep_len.data_ptr(), _p(n_new), prm, C.byref(books)), "aasd_kv_free")
+
+    def kv_fork(self, pages, src_seq, dst_seq, block_table, seq_pages, cached_len, free_pages, n_free, page_shares, fork_len=None, outputs=None):
+        """aasd_kv_fork: every sequence ``dst_seq[i]``, which holds no pages, becomes the first ``fork_len[i]`` cached tokens (None: all)
+        of ``src_seq[i]``.  ``pages``: the pools of all layers.  The books and ``cached_len`` are changed in place.  Returns new_len (NONE: not made)
+        and the pages copied, copy_src and copy_dst."""
+        B, P, N, prm, books = self._kv_books(block_table, seq_pages, free_pages, n_free, page_shares)
+        n = src_seq.numel()
+        o = outputs
+        if o is None:
+            new = src_seq.new_empty
+            o = dict(new_len=new(n), copy_src=new(n), copy_dst=new(n))
+        _kv_i32(self.device_index, src_seq, dst_seq, cached_len, fork_len, o["new_len"], o["copy_src"], o["copy_dst"])
+        _kv_need(dst_seq.numel() == n and cached_len.numel() >= B and (fork_len is None or fork_len.numel() >= n) and
+                 all(o[x].numel() >= n for x in ("new_len", "copy_src", "copy_dst")), "lengths of kv_fork's arrays")
+        pool = self._kv_layers(pages, N)
+        out = KvForkOut(o["new_len"].data_ptr(), o["copy_src"].data_ptr(), o["copy_dst"].data_ptr())
+        _check(self.lib.aasd_kv_fork(self._h, src_seq.data_ptr(), dst_seq.data_ptr(), _p(fork_len), n, prm, C.byref(books),
+                                     cached_len.data_ptr(), C.byref(pool), C.byref(out)), "aasd_kv_fork")
+        return o
+
+    def kv_copy(self, pages, src, dst):
+        """aasd_kv_copy: page ``src[i]`` to page ``dst[i]`` in the pools of all layers; NONE leaves a pair out."""
+        _kv_i32(self.device_index, src, dst)
+        _kv_need(src.numel() == dst.numel(), "lengths of kv_copy's arrays")
+        pool = self._kv_layers(pages, pages.shape[1])
+        _check(self.lib.aasd_kv_copy(self._h, C.byref(pool), pages.shape[1], src.data_ptr(), dst.data_ptr(), src.numel()), "aasd_kv_copy")
+
+    def kv_compact(self, pages, block_table, seq_pages, free_pages, n_free, page_shares, outputs=None):
+        """aasd_kv_compact: the pages in use move to the front of the pools of all layers; the books follow.  Returns page_map, the
+        new number of each page (NONE: it was free), and n_moved."""
+        B, P, N, prm, books = self._kv_books(block_table, seq_pages, free_pages, n_free, page_shares)
+        o = outputs
+        if o is None:
+            o = dict(page_map=free_pages.new_empty(N), n_moved=free_pages.new_empty(1))
+        else:
+            _kv_i32(self.device_index, o["page_map"], o["n_moved"])
+            _kv_need(o["page_map"].numel() >= N and o["n_moved"].numel() > 0, "outputs")
+        with torch.cuda.stream(self.stream):
+            moves = free_pages.new_empty(N)
+        pool = self._kv_layers(pages, N)
+        _check(self.lib.aasd_kv_compact(self._h, prm, C.byref(books), C.byref(pool), o["page_map"].data_ptr(), moves.data_ptr(),
+                                        o["n_moved"].data_ptr()), "aasd_kv_compact")
         return o
 
     def select(self, accept_len, next_token, draft_ids, emit_stride, cand_offsets=None,

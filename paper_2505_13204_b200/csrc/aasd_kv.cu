@@ -8,30 +8,6 @@ using namespace aasd;
 
 namespace {
 
-bool head_dim_ok(int d) { return d == 64 || d == 128 || d == 256; }
-bool dtype_ok(int d) { return d == AASD_F32 || d == AASD_BF16; }
-size_t elt_size(int dtype) { return dtype == AASD_F32 ? 4 : 2; }
-bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-
-// Whether two arrays have a byte in common.
-bool overlap(const void* x, int64_t x_bytes, const void* y, int64_t y_bytes) {
-    const uintptr_t a = (uintptr_t)x, b = (uintptr_t)y;
-    return x != nullptr && y != nullptr && a < b + (uintptr_t)y_bytes && b < a + (uintptr_t)x_bytes;
-}
-
-// Calls f with the head dimension as a constant.
-template <class F>
-void with_dim(int head_dim, F&& f) {
-    if (head_dim == 64) f(std::integral_constant<int, 64>());
-    else if (head_dim == 128) f(std::integral_constant<int, 128>());
-    else f(std::integral_constant<int, 256>());
-}
-template <class F>
-void with_type(int dtype, F&& f) {
-    if (dtype == AASD_F32) f(std::integral_constant<int, AASD_F32>());
-    else f(std::integral_constant<int, AASD_BF16>());
-}
-
 // Token rows up to which the planning CTA writes the token arrays itself, and from which a second launch
 // does: 256 tokens 3.3 us inline and 7.3 us in two launches, 1024 tokens 5.0 and 7.1, 2048 tokens 7.4 and 6.2, 4096 tokens
 // 11.8 and 6.1.
@@ -42,11 +18,110 @@ constexpr int kPlanManySeqs = 256;
 
 }  // namespace
 
+namespace aasd {
+
+int kv_check_write(const aasd_kv_write_params& p, int64_t n_tokens) {
+    if (!kv_dtype_ok(p.dtype)) return AASD_ERR_BAD_DTYPE;
+    if (!kv_head_dim_ok(p.head_dim)) return AASD_ERR_UNSUPPORTED;
+    const int hq = p.n_q_heads, hkv = p.n_kv_heads, D = p.head_dim;
+    if (n_tokens < 0 || hq < 0 || hkv < 0 || p.n_pages < 0 || p.n_pages > 0x7FFFFFFF / kPage) return AASD_ERR_BAD_SHAPE;
+    if (p.rotary_dim < 0 || p.rotary_dim > D || (p.rotary_dim & 1) || p.max_positions < 0) return AASD_ERR_BAD_SHAPE;
+    if ((hq > 0 && p.q_stride < (int64_t)hq * D) || (hkv > 0 && (p.k_stride < (int64_t)hkv * D || p.v_stride < (int64_t)hkv * D)))
+        return AASD_ERR_BAD_SHAPE;
+    if (!(p.eps >= 0.f) || (p.flags & ~AASD_KV_ROPE_INTERLEAVED)) return AASD_ERR_INVALID_ARG;
+    return AASD_OK;
+}
+
+int kv_check_read(aasd_ctx* ctx, const void* pages, const int32_t* slots, int64_t n, int32_t n_pages, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                  const void* k_out, const void* v_out) {
+    if (ctx == nullptr) return AASD_ERR_INVALID_ARG;
+    if (!kv_dtype_ok(dtype)) return AASD_ERR_BAD_DTYPE;
+    if (!kv_head_dim_ok(head_dim)) return AASD_ERR_UNSUPPORTED;
+    if (n < 0 || n_kv_heads < 1 || n_pages < 0 || n_pages > 0x7FFFFFFF / kPage) return AASD_ERR_BAD_SHAPE;
+    if (n == 0 || (!k_out && !v_out)) return AASD_OK;
+    if (!pages || !aligned16(pages) || !slots) return AASD_ERR_INVALID_ARG;
+    const size_t es = kv_elt_size(dtype);
+    if (((uintptr_t)k_out % es) != 0 || ((uintptr_t)v_out % es) != 0) return AASD_ERR_INVALID_ARG;
+    return AASD_OK;
+}
+
+int kv_prepare_commit(aasd_ctx* ctx, void* pages, const int32_t* block_table, const int32_t* cached_len, const int32_t* kv_len, const int32_t* tok_offsets,
+                      const int32_t* best_node, const int32_t* node_parent, const aasd_kv_commit_params* p, int32_t* new_len, int64_t head_bytes,
+                      KvCommitArgs& a) {
+    if (ctx == nullptr || p == nullptr) return AASD_ERR_INVALID_ARG;
+    if (!kv_head_dim_ok(p->head_dim)) return AASD_ERR_UNSUPPORTED;
+    if (p->n_seqs < 0 || p->n_kv_heads < 1 || p->n_pages < 0 || p->n_pages > 0x7FFFFFFF / kPage || p->max_pages < 1 ||
+        p->max_pages > 0x7FFFFFFF / kPage || p->rows_per_seq < 0 || p->n_layers < 0 || p->layer_stride < 0 || (p->layer_stride % 16) != 0)
+        return AASD_ERR_BAD_SHAPE;
+    if (p->n_seqs == 0) return AASD_OK;
+    if (!block_table || !cached_len || !kv_len || !best_node || !node_parent || !new_len) return AASD_ERR_INVALID_ARG;
+    if (p->rows_per_seq == 0 && !tok_offsets) return AASD_ERR_INVALID_ARG;
+    if (p->n_layers > 0 && (!pages || !aligned16(pages))) return AASD_ERR_INVALID_ARG;
+    // Every CTA of a sequence reads its inputs for itself, in no order with the one that writes the new length.
+    const int64_t n4 = 4 * (int64_t)p->n_seqs;
+    const int64_t pool = (int64_t)p->n_pages * p->n_kv_heads * head_bytes;
+    if (overlap(new_len, n4, cached_len, n4) || overlap(new_len, n4, kv_len, n4) || overlap(new_len, n4, best_node, n4) ||
+        overlap(new_len, n4, tok_offsets, n4 + 4) || overlap(new_len, n4, block_table, n4 * p->max_pages) ||
+        overlap(new_len, n4, node_parent, p->rows_per_seq > 0 ? n4 * p->rows_per_seq : 4) ||
+        (p->n_layers > 0 && overlap(new_len, n4, pages, (p->n_layers - 1) * p->layer_stride + pool)))
+        return AASD_ERR_INVALID_ARG;
+    a = KvCommitArgs{static_cast<uint8_t*>(pages), block_table, cached_len, kv_len, tok_offsets, best_node, node_parent, *p, new_len,
+                   ctx->state};
+    return AASD_OK;
+}
+
+int kv_prepare_attend(aasd_ctx* ctx, const void* q, const void* pages, const int32_t* block_table, const int32_t* cached_len, const int32_t* kv_len,
+                      const int32_t* tok_offsets, const int32_t* node_parent, const aasd_kv_attend_params* p, void* workspace, size_t workspace_bytes,
+                      const aasd_kv_attend_out* o, KvAttendArgs& a) {
+    if (ctx == nullptr || p == nullptr || o == nullptr) return AASD_ERR_INVALID_ARG;
+    if (!kv_dtype_ok(p->dtype)) return AASD_ERR_BAD_DTYPE;
+    if (!kv_head_dim_ok(p->head_dim)) return AASD_ERR_UNSUPPORTED;
+    if (p->n_seqs < 0 || p->n_tokens < 0 || p->n_kv_heads < 1 || p->n_q_heads < 1 || p->n_q_heads > 65536 || p->n_q_heads % p->n_kv_heads != 0 ||
+        p->n_pages < 0 || p->n_pages > 0x7FFFFFFF / kPage || p->max_pages < 1 || p->max_pages > 0x7FFFFFFF / kPage || p->rows_per_seq < 0 ||
+        p->q_stride < (int64_t)p->n_q_heads * p->head_dim)
+        return AASD_ERR_BAD_SHAPE;
+    if (p->rows_per_seq > 0 && (int64_t)p->n_seqs * p->rows_per_seq != p->n_tokens) return AASD_ERR_BAD_SHAPE;
+    if (!(p->scale >= 0.f) || !(p->scale <= 3.0e38f)) return AASD_ERR_INVALID_ARG;
+    if (p->n_tokens == 0) return AASD_OK;
+    if (p->n_tokens > 0x7FFFFFFFLL / p->n_q_heads) return AASD_ERR_BAD_SHAPE;
+    if (!q || !o->out) return AASD_ERR_INVALID_ARG;
+    if (p->n_seqs > 0 && (!block_table || !cached_len || !kv_len || !pages || !aligned16(pages))) return AASD_ERR_INVALID_ARG;
+    if (p->rows_per_seq == 0 && p->n_seqs > 0 && !tok_offsets) return AASD_ERR_INVALID_ARG;
+    const size_t es = kv_elt_size(p->dtype);
+    if (((uintptr_t)q % es) != 0 || ((uintptr_t)o->out % es) != 0) return AASD_ERR_INVALID_ARG;
+    const auto it = ctx->kv_workspaces.find(workspace);
+    if (workspace == nullptr || it == ctx->kv_workspaces.end()) return AASD_ERR_INVALID_ARG;
+    if (it->second < p->head_dim || workspace_bytes < kv_attend_scratch(p->head_dim).bytes) return AASD_ERR_WORKSPACE_TOO_SMALL;
+    a.q = q;
+    a.pages = static_cast<const uint8_t*>(pages);
+    a.block_table = block_table;
+    a.cached_len = cached_len;
+    a.kv_len = kv_len;
+    a.tok_offsets = tok_offsets;
+    a.node_parent = node_parent;
+    a.p = *p;
+    a.o = *o;
+    a.q_vec = aligned16(q) && (p->q_stride * es) % 16 == 0;
+    a.out_vec = aligned16(o->out);
+    a.scale_log2 = (p->scale > 0.f ? p->scale : 1.0f / sqrtf((float)p->head_dim)) * kLog2e;
+    a.state = ctx->state;
+    a.wait_limit = kWaitLimit;
+    a.withhold_page = -1;
+    if (ctx->withhold_item >= 0) {
+        a.wait_limit = ctx->test_wait_limit;
+        a.withhold_page = ctx->withhold_item < 0x7FFFFFFF ? (int)ctx->withhold_item : 0x7FFFFFFF;
+        ctx->withhold_item = -1;
+    }
+    return AASD_OK;
+}
+
+}  // namespace aasd
+
 extern "C" {
 
 int aasd_kv_head_bytes(int32_t head_dim, size_t* bytes) {
     if (bytes == nullptr) return AASD_ERR_INVALID_ARG;
-    if (!head_dim_ok(head_dim)) return AASD_ERR_UNSUPPORTED;
+    if (!kv_head_dim_ok(head_dim)) return AASD_ERR_UNSUPPORTED;
     *bytes = (size_t)kv_head_bytes(head_dim);
     return AASD_OK;
 }
@@ -84,19 +159,13 @@ int aasd_kv_write(aasd_ctx* ctx, const void* q, const void* k, const void* v, co
                   const aasd_kv_write_params* p, void* pages, void* q_out, void* k_out) {
     TraceRange trace("aasd_kv_write");
     if (ctx == nullptr || p == nullptr) return AASD_ERR_INVALID_ARG;
-    if (!dtype_ok(p->dtype)) return AASD_ERR_BAD_DTYPE;
-    if (!head_dim_ok(p->head_dim)) return AASD_ERR_UNSUPPORTED;
+    if (const int rc = kv_check_write(*p, n_tokens)) return rc;
     const int hq = p->n_q_heads, hkv = p->n_kv_heads, D = p->head_dim;
-    if (n_tokens < 0 || hq < 0 || hkv < 0 || p->n_pages < 0 || p->n_pages > 0x7FFFFFFF / kPage) return AASD_ERR_BAD_SHAPE;
-    if (p->rotary_dim < 0 || p->rotary_dim > D || (p->rotary_dim & 1) || p->max_positions < 0) return AASD_ERR_BAD_SHAPE;
-    if ((hq > 0 && p->q_stride < (int64_t)hq * D) || (hkv > 0 && (p->k_stride < (int64_t)hkv * D || p->v_stride < (int64_t)hkv * D)))
-        return AASD_ERR_BAD_SHAPE;
-    if (!(p->eps >= 0.f) || (p->flags & ~AASD_KV_ROPE_INTERLEAVED)) return AASD_ERR_INVALID_ARG;
     if (n_tokens == 0 || hq + hkv == 0) return AASD_OK;
     if (!positions || (p->rotary_dim > 0 && !cos_sin)) return AASD_ERR_INVALID_ARG;
     if (hq > 0 && (!q || !q_out)) return AASD_ERR_INVALID_ARG;
     if (hkv > 0 && (!k || !v || !slot_map || !pages || !aligned16(pages))) return AASD_ERR_INVALID_ARG;
-    const size_t es = elt_size(p->dtype);
+    const size_t es = kv_elt_size(p->dtype);
     for (const void* x : {q, k, v, q_weight, k_weight, (const void*)q_out, (const void*)k_out})
         if (((uintptr_t)x % es) != 0) return AASD_ERR_INVALID_ARG;
     KvWriteArgs a{q, k, v, q_weight, k_weight, cos_sin, positions, slot_map, n_tokens, *p, static_cast<uint8_t*>(pages), q_out, k_out,
@@ -128,14 +197,8 @@ int aasd_kv_write(aasd_ctx* ctx, const void* q, const void* k, const void* v, co
 int aasd_kv_read(aasd_ctx* ctx, const void* pages, const int32_t* slots, int64_t n, int32_t n_pages, int32_t n_kv_heads,
                  int32_t head_dim, int32_t dtype, void* k_out, void* v_out) {
     TraceRange trace("aasd_kv_read");
-    if (ctx == nullptr) return AASD_ERR_INVALID_ARG;
-    if (!dtype_ok(dtype)) return AASD_ERR_BAD_DTYPE;
-    if (!head_dim_ok(head_dim)) return AASD_ERR_UNSUPPORTED;
-    if (n < 0 || n_kv_heads < 1 || n_pages < 0 || n_pages > 0x7FFFFFFF / kPage) return AASD_ERR_BAD_SHAPE;
-    if (n == 0 || (!k_out && !v_out)) return AASD_OK;
-    if (!pages || !aligned16(pages) || !slots) return AASD_ERR_INVALID_ARG;
-    const size_t es = elt_size(dtype);
-    if (((uintptr_t)k_out % es) != 0 || ((uintptr_t)v_out % es) != 0) return AASD_ERR_INVALID_ARG;
+    const int rc = kv_check_read(ctx, pages, slots, n, n_pages, n_kv_heads, head_dim, dtype, k_out, v_out);
+    if (rc != AASD_OK || n == 0 || (!k_out && !v_out)) return rc;
     KvReadArgs a{static_cast<const uint8_t*>(pages), slots, n, n_pages, n_kv_heads, k_out, v_out, ctx->state};
     const int64_t blocks = (n + kValueTokens - 1) / kValueTokens * n_kv_heads;
     if (blocks > 0x7FFFFFFFLL) return AASD_ERR_BAD_SHAPE;
@@ -155,25 +218,11 @@ int aasd_kv_commit(aasd_ctx* ctx, void* pages, const int32_t* block_table, const
                    const int32_t* tok_offsets, const int32_t* best_node, const int32_t* node_parent,
                    const aasd_kv_commit_params* p, int32_t* new_len) {
     TraceRange trace("aasd_kv_commit");
-    if (ctx == nullptr || p == nullptr) return AASD_ERR_INVALID_ARG;
-    if (!head_dim_ok(p->head_dim)) return AASD_ERR_UNSUPPORTED;
-    if (p->n_seqs < 0 || p->n_kv_heads < 1 || p->n_pages < 0 || p->n_pages > 0x7FFFFFFF / kPage || p->max_pages < 1 ||
-        p->max_pages > 0x7FFFFFFF / kPage || p->rows_per_seq < 0 || p->n_layers < 0 || p->layer_stride < 0 || (p->layer_stride % 16) != 0)
-        return AASD_ERR_BAD_SHAPE;
-    if (p->n_seqs == 0) return AASD_OK;
-    if (!block_table || !cached_len || !kv_len || !best_node || !node_parent || !new_len) return AASD_ERR_INVALID_ARG;
-    if (p->rows_per_seq == 0 && !tok_offsets) return AASD_ERR_INVALID_ARG;
-    if (p->n_layers > 0 && (!pages || !aligned16(pages))) return AASD_ERR_INVALID_ARG;
-    // Every CTA of a sequence reads its inputs for itself, in no order with the one that writes the new length.
-    const int64_t n4 = 4 * (int64_t)p->n_seqs;
-    const int64_t pool = (int64_t)p->n_pages * p->n_kv_heads * kv_head_bytes(p->head_dim);
-    if (overlap(new_len, n4, cached_len, n4) || overlap(new_len, n4, kv_len, n4) || overlap(new_len, n4, best_node, n4) ||
-        overlap(new_len, n4, tok_offsets, n4 + 4) || overlap(new_len, n4, block_table, n4 * p->max_pages) ||
-        overlap(new_len, n4, node_parent, p->rows_per_seq > 0 ? n4 * p->rows_per_seq : 4) ||
-        (p->n_layers > 0 && overlap(new_len, n4, pages, (p->n_layers - 1) * p->layer_stride + pool)))
-        return AASD_ERR_INVALID_ARG;
-    KvCommitArgs a{static_cast<uint8_t*>(pages), block_table, cached_len, kv_len, tok_offsets, best_node, node_parent, *p, new_len,
-                   ctx->state};
+    if (p == nullptr || !kv_head_dim_ok(p->head_dim)) return p == nullptr ? AASD_ERR_INVALID_ARG : AASD_ERR_UNSUPPORTED;
+    KvCommitArgs a{};
+    const int rc = kv_prepare_commit(ctx, pages, block_table, cached_len, kv_len, tok_offsets, best_node, node_parent, p, new_len,
+                                     kv_head_bytes(p->head_dim), a);
+    if (rc != AASD_OK || p->n_seqs == 0) return rc;
     const int64_t items = (int64_t)p->n_layers * p->n_kv_heads;
     int64_t groups = (items + kCommitThreads / 32 - 1) / (kCommitThreads / 32);
     groups = groups < 1 ? 1 : groups > 64 ? 64 : groups;
@@ -186,14 +235,14 @@ int aasd_kv_commit(aasd_ctx* ctx, void* pages, const int32_t* block_table, const
 
 int aasd_kv_workspace_bytes(int32_t head_dim, size_t* bytes) {
     if (bytes == nullptr) return AASD_ERR_INVALID_ARG;
-    if (!head_dim_ok(head_dim)) return AASD_ERR_UNSUPPORTED;
+    if (!kv_head_dim_ok(head_dim)) return AASD_ERR_UNSUPPORTED;
     *bytes = kv_attend_scratch(head_dim).bytes;
     return AASD_OK;
 }
 
 int aasd_kv_workspace_init(aasd_ctx* ctx, void* workspace, size_t bytes, int32_t head_dim) {
     if (ctx == nullptr || workspace == nullptr || (uintptr_t)workspace % 256 != 0) return AASD_ERR_INVALID_ARG;
-    if (!head_dim_ok(head_dim)) return AASD_ERR_UNSUPPORTED;
+    if (!kv_head_dim_ok(head_dim)) return AASD_ERR_UNSUPPORTED;
     const KvScratch L = kv_attend_scratch(head_dim);
     if (bytes < L.bytes) return AASD_ERR_WORKSPACE_TOO_SMALL;
     AASD_CUDA(cudaMemsetAsync(workspace, 0, L.zero_bytes, ctx->stream));
@@ -209,50 +258,13 @@ int aasd_kv_attend(aasd_ctx* ctx, const void* q, const void* pages, const int32_
                    const int32_t* kv_len, const int32_t* tok_offsets, const int32_t* node_parent, const aasd_kv_attend_params* p,
                    void* workspace, size_t workspace_bytes, const aasd_kv_attend_out* o) {
     TraceRange trace("aasd_kv_attend");
-    if (ctx == nullptr || p == nullptr || o == nullptr) return AASD_ERR_INVALID_ARG;
-    if (!dtype_ok(p->dtype)) return AASD_ERR_BAD_DTYPE;
-    if (!head_dim_ok(p->head_dim)) return AASD_ERR_UNSUPPORTED;
-    if (p->n_seqs < 0 || p->n_tokens < 0 || p->n_kv_heads < 1 || p->n_q_heads < 1 || p->n_q_heads > 65536 || p->n_q_heads % p->n_kv_heads != 0 ||
-        p->n_pages < 0 || p->n_pages > 0x7FFFFFFF / kPage || p->max_pages < 1 || p->max_pages > 0x7FFFFFFF / kPage || p->rows_per_seq < 0 ||
-        p->q_stride < (int64_t)p->n_q_heads * p->head_dim)
-        return AASD_ERR_BAD_SHAPE;
-    if (p->rows_per_seq > 0 && (int64_t)p->n_seqs * p->rows_per_seq != p->n_tokens) return AASD_ERR_BAD_SHAPE;
-    if (!(p->scale >= 0.f) || !(p->scale <= 3.0e38f)) return AASD_ERR_INVALID_ARG;
-    if (p->n_tokens == 0) return AASD_OK;
-    if (p->n_tokens > 0x7FFFFFFFLL / p->n_q_heads) return AASD_ERR_BAD_SHAPE;
-    if (!q || !o->out) return AASD_ERR_INVALID_ARG;
-    if (p->n_seqs > 0 && (!block_table || !cached_len || !kv_len || !pages || !aligned16(pages))) return AASD_ERR_INVALID_ARG;
-    if (p->rows_per_seq == 0 && p->n_seqs > 0 && !tok_offsets) return AASD_ERR_INVALID_ARG;
-    const size_t es = elt_size(p->dtype);
-    if (((uintptr_t)q % es) != 0 || ((uintptr_t)o->out % es) != 0) return AASD_ERR_INVALID_ARG;
-    const auto it = ctx->kv_workspaces.find(workspace);
-    if (workspace == nullptr || it == ctx->kv_workspaces.end()) return AASD_ERR_INVALID_ARG;
-    if (it->second < p->head_dim || workspace_bytes < kv_attend_scratch(p->head_dim).bytes) return AASD_ERR_WORKSPACE_TOO_SMALL;
     KvAttendArgs a{};
-    a.q = q;
-    a.pages = static_cast<const uint8_t*>(pages);
-    a.block_table = block_table;
-    a.cached_len = cached_len;
-    a.kv_len = kv_len;
-    a.tok_offsets = tok_offsets;
-    a.node_parent = node_parent;
-    a.p = *p;
-    a.o = *o;
-    a.q_vec = aligned16(q) && (p->q_stride * es) % 16 == 0;
-    a.out_vec = aligned16(o->out);
-    a.scale_log2 = (p->scale > 0.f ? p->scale : 1.0f / sqrtf((float)p->head_dim)) * kLog2e;
-    a.state = ctx->state;
-    a.wait_limit = kWaitLimit;
-    a.withhold_page = -1;
-    if (ctx->withhold_item >= 0) {
-        a.wait_limit = ctx->test_wait_limit;
-        a.withhold_page = ctx->withhold_item < 0x7FFFFFFF ? (int)ctx->withhold_item : 0x7FFFFFFF;
-        ctx->withhold_item = -1;
-    }
+    int rc = kv_prepare_attend(ctx, q, pages, block_table, cached_len, kv_len, tok_offsets, node_parent, p, workspace, workspace_bytes, o, a);
+    if (rc != AASD_OK || p->n_tokens == 0) return rc;
     AASD_CUDA(cudaSetDevice(ctx->device));
     const LaunchEnv env{ctx->stream, ctx->device};
     int launches = 0;
-    const int rc = p->dtype == AASD_F32 ? launch_kv_attend_f32(env, ctx->sm_count, a, workspace, &launches)
+    rc = p->dtype == AASD_F32 ? launch_kv_attend_f32(env, ctx->sm_count, a, workspace, &launches)
                                         : launch_kv_attend_bf16(env, ctx->sm_count, a, workspace, &launches);
     if (rc != AASD_OK) return rc;
     return after_launch(ctx, launches);

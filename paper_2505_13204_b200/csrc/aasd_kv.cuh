@@ -443,7 +443,7 @@ struct KvWriteArgs {
 // that the compiler does not know: a launch argument.
 __device__ __forceinline__ float2 mul2_rounded(float2 a, float2 b, float2 minus_zero) { return __ffma2_rn(a, b, minus_zero); }
 
-#ifdef AASD_KV_TU
+#if defined(AASD_KV_TU) || defined(AASD_KVB_TU)
 // A CTA either takes query and key rows or stores values; both kinds share the launch.
 //
 // Query and key rows: D / 16 lanes share a row, a lane holds eight channels of each half, so that both
