@@ -81,7 +81,8 @@ struct KvSeq {
     int tiles;                // row tiles of a key/value head
 };
 
-// tile_rows: rows of a tile
+// tile_rows: rows of a tile.  PAGE: tokens of what is counted as a page (a kernel may take pages in parts).
+template <int PAGE = kPage>
 __device__ __forceinline__ KvSeq kv_load_seq(const KvAttendArgs& a, int b, int tile_rows) {
     KvSeq s;
     s.cached = a.cached_len[b];
@@ -98,8 +99,8 @@ __device__ __forceinline__ KvSeq kv_load_seq(const KvAttendArgs& a, int b, int t
     s.first = inside ? (int)first : 0;
     s.rows = inside ? (int)rows : 0;
     s.fresh = s.cached < 0 || fresh < 0 ? 0 : (int)(fresh < s.rows ? fresh : s.rows);
-    const long long pages = ((long long)s.cached + s.fresh + kPage - 1) / kPage;
-    s.pages = s.fresh == 0 ? 0 : (int)(pages < a.p.max_pages ? pages : a.p.max_pages);
+    const long long pages = ((long long)s.cached + s.fresh + PAGE - 1) / PAGE, most = (long long)a.p.max_pages * (kPage / PAGE);
+    s.pages = s.fresh == 0 ? 0 : (int)(pages < most ? pages : most);
     const long long n = (long long)s.fresh * (a.p.n_q_heads / a.p.n_kv_heads);
     s.tiles = (int)((n + tile_rows - 1) / tile_rows);
     return s;
@@ -113,6 +114,7 @@ __device__ __forceinline__ long long kv_units(const KvAttendArgs& a, const KvSeq
 }
 
 // A place in the list of all units: sequence by sequence, head by head, tile by tile, page by page.
+template <int PAGE = kPage>
 struct KvCursor {
     int b, h, tile, pg;
     int unit;                 // of page pg
@@ -142,7 +144,7 @@ struct KvCursor {
 #pragma unroll 1
         do {
             if (++b >= a.p.n_seqs) return;   // (past the last unit: never looked at)
-            s = kv_load_seq(a, b, tile_rows);
+            s = kv_load_seq<PAGE>(a, b, tile_rows);
         } while (s.pages == 0 || s.tiles == 0);
         table = a.block_table + (long long)b * a.p.max_pages;
     }
@@ -404,6 +406,139 @@ struct KvSplitShared {
     int abort_flag, last[2], padding;
 };
 
+// Joining the pieces of a CTA's W warps: a piece lies in its warp's first ring block (the last one of the share), or in the warp's
+// scratch; rows are TS floats apart.
+template <int DT, int D, int W, int R, int TS, class Shared>
+__device__ __forceinline__ void kv_split_join(const KvAttendArgs& a, Shared& sh, const KvShares& shares) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c = blockIdx.x;
+    const int G = a.p.n_q_heads / a.p.n_kv_heads;
+    // Every warp finds the groups of pieces that belong together (lane k looks
+    // at piece k) and the warps share the groups' rows; a row's weights are found lane by lane, its
+    // channels summed as independent loads.
+    static_assert(2 * W <= 32, "a lane per piece");
+    constexpr int kPart = R * D + 2 * R;
+    const int U0 = shares.first(c * W), U1 = shares.first(c * W + W);
+    const int seg = lane < 2 * W ? sh.piece[lane].seg : -1;
+    const unsigned int valid = __ballot_sync(0xFFFFFFFFu, seg >= 0);
+    const unsigned int below = valid & ((1u << lane) - 1u);
+    const int previous = __shfl_sync(0xFFFFFFFFu, seg, below ? 31 - __clz(below) : 0);
+    unsigned int starts = __ballot_sync(0xFFFFFFFFu, seg >= 0 && (below == 0 || previous != seg));
+    auto finish_row = [&](const KvPiece& pc, int r, float M, float L, float4 o, int ch) {
+        const float inv = L > 0.f ? 1.f / L : 0.f;
+        const int row = pc.row0 + r;
+        const long long head = ((long long)pc.first + row / G) * a.p.n_q_heads + pc.h * G + row % G;
+        if (!AASD_IN_RANGE(head < a.p.n_tokens * a.p.n_q_heads, a.state)) return;
+        store4<DT>(a.o.out, head * D + ch, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), a.out_vec);
+        if (a.o.lse != nullptr && ch == 0) a.o.lse[head] = L > 0.f ? (M + log2f(L)) * (float)kLn2 : -CUDART_INF_F;
+    };
+    int open[2] = {-1, -1};        // first pieces of the groups that other CTAs hold parts of: begun before this CTA, in it
+    // rows r0 .. r0 + RB of the group of pieces `group`
+    auto join_rows = [&](auto rb, const KvPiece& pc, unsigned int group, bool complete, float* part, int r0) {
+        constexpr int RB = decltype(rb)::value;
+        const bool in = (group >> lane) & 1u;
+        const int own = lane < 2 * W ? lane : 0;
+        float M[RB], L[RB], f[RB];
+#pragma unroll
+        for (int i = 0; i < RB; ++i) {
+            const int r = min(r0 + i, pc.n - 1);
+            const float m = in ? sh.m[own][r] : kKvNothing;
+            M[i] = m;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) M[i] = fmaxf(M[i], __shfl_xor_sync(0xFFFFFFFFu, M[i], o));
+            f[i] = in ? ex2_approx(m - M[i]) : 0.f;
+            L[i] = in ? sh.l[own][r] * f[i] : 0.f;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) L[i] += __shfl_xor_sync(0xFFFFFFFFu, L[i], o);
+        }
+        for (int cb = 0; cb < D; cb += 128) {
+            const int ch = cb + lane * 4;
+            const bool on = ch < D;
+            float4 o[RB];
+#pragma unroll
+            for (int i = 0; i < RB; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            unsigned int left = group;
+            while (left) {
+                const int k = __ffs(left) - 1;
+                left &= left - 1;
+                const float* from = (k & 1) ? reinterpret_cast<const float*>(sh.ring[k >> 1][0])
+                                            : a.warp_parts + (long long)(c * W + (k >> 1)) * (R * TS);
+                float4 x[RB];
+#pragma unroll
+                for (int i = 0; i < RB; ++i) {
+                    x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (on) x[i] = *reinterpret_cast<const float4*>(from + min(r0 + i, pc.n - 1) * TS + ch);
+                }
+#pragma unroll
+                for (int i = 0; i < RB; ++i) {
+                    const float fk = __shfl_sync(0xFFFFFFFFu, f[i], k);
+                    o[i].x = fmaf(x[i].x, fk, o[i].x);
+                    o[i].y = fmaf(x[i].y, fk, o[i].y);
+                    o[i].z = fmaf(x[i].z, fk, o[i].z);
+                    o[i].w = fmaf(x[i].w, fk, o[i].w);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < RB; ++i) {
+                const int r = r0 + i;
+                if (!on || r >= pc.n) continue;
+                if (complete) {
+                    finish_row(pc, r, M[i], L[i], o[i], ch);
+                } else {
+                    *reinterpret_cast<float4*>(part + r * D + ch) = o[i];
+                    if (ch == 0) {
+                        part[R * D + r] = M[i];
+                        part[R * D + R + r] = L[i];
+                    }
+                }
+            }
+        }
+    };
+    const bool few = __popc(starts) * 2 < W;   // few groups: a row per warp, else four rows at a time
+    int done = 0;                              // row batches dealt with so far, modulo W
+    while (starts) {
+        const int p = __ffs(starts) - 1;
+        starts &= starts - 1;
+        const unsigned int group = valid & ~((1u << p) - 1u) & (starts ? (1u << (__ffs(starts) - 1)) - 1u : 0xFFFFFFFFu);
+        const KvPiece pc = sh.piece[p];
+        const bool complete = pc.seg >= U0 && pc.seg + pc.pages <= U1;
+        const int which = pc.seg < U0 ? 0 : 1;   // scratch slot of this CTA
+        if (!complete) open[which] = p;
+        float* part = a.cta_parts + (long long)(c * 2 + which) * kPart;
+        const int batches = few ? pc.n : (pc.n + 3) / 4;
+        int k = warp - done;
+        k += k < 0 ? W : 0;
+        done = (done + batches) % W;
+        for (; k < batches; k += W) {
+            if (few) join_rows(std::integral_constant<int, 1>(), pc, group, complete, part, k);
+            else join_rows(std::integral_constant<int, 4>(), pc, group, complete, part, 4 * k);
+        }
+    }
+    // the last CTA that delivers a part of a segment joins them all
+    if (open[0] >= 0 || open[1] >= 0) {
+        __syncthreads();
+        if (tid < 2) {
+            int last = 0;
+            if (open[tid] >= 0) {
+                const KvPiece pc = sh.piece[open[tid]];
+                const int c0 = shares.owner(pc.seg) / W, c1 = shares.owner(pc.seg + pc.pages - 1) / W;
+                last = take_ticket(a.tickets + c0) == (unsigned int)(c1 - c0);
+                if (last) a.tickets[c0] = 0;
+            }
+            sh.last[tid] = last;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            if (!sh.last[which]) continue;
+            const KvPiece pc = sh.piece[open[which]];
+            const int c0 = shares.owner(pc.seg) / W;
+            const int parts = (shares.owner(pc.seg + pc.pages - 1) / W - c0) + 1;
+            const float* base = a.cta_parts + (long long)c0 * 2 * kPart;   // part k: 2 k, the first one's 1
+            for (int r = warp; r < pc.n; r += W) kv_join_row<DT, D>(a, pc, r, base, kPart, R, parts, G, lane);
+        }
+    }
+}
+
 // DT: type of the queries.  bf16 values fit an fp16 number scaled by the row's own power of two;
 // fp32 queries and their probabilities travel as two fp16 numbers each (22 bits).
 // NT: row tiles of eight that share the codes of a page.
@@ -463,7 +598,7 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
     u64* full = sh.full[warp];
 
     if (u0 < u1) {
-        KvCursor ahead;
+        KvCursor<> ahead;
         {
             int lo = 0, hi = (B + strip - 1) / strip;
 #pragma unroll 1
@@ -890,133 +1025,7 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
         }
     }
     __syncthreads();
-    if (works && !*abort_flag) {
-        // Joining the pieces.  Every warp finds the groups of pieces that belong together (lane k looks
-        // at piece k) and the warps share the groups' rows; a row's weights are found lane by lane, its
-        // channels summed as independent loads.
-        static_assert(2 * W <= 32, "a lane per piece");
-        constexpr int kPart = R * D + 2 * R;
-        const int U0 = shares.first(c * W), U1 = shares.first(c * W + W);
-        const int seg = lane < 2 * W ? sh.piece[lane].seg : -1;
-        const unsigned int valid = __ballot_sync(0xFFFFFFFFu, seg >= 0);
-        const unsigned int below = valid & ((1u << lane) - 1u);
-        const int previous = __shfl_sync(0xFFFFFFFFu, seg, below ? 31 - __clz(below) : 0);
-        unsigned int starts = __ballot_sync(0xFFFFFFFFu, seg >= 0 && (below == 0 || previous != seg));
-        auto finish_row = [&](const KvPiece& pc, int r, float M, float L, float4 o, int ch) {
-            const float inv = L > 0.f ? 1.f / L : 0.f;
-            const int row = pc.row0 + r;
-            const long long head = ((long long)pc.first + row / G) * a.p.n_q_heads + pc.h * G + row % G;
-            if (!AASD_IN_RANGE(head < a.p.n_tokens * a.p.n_q_heads, a.state)) return;
-            store4<DT>(a.o.out, head * D + ch, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), a.out_vec);
-            if (a.o.lse != nullptr && ch == 0) a.o.lse[head] = L > 0.f ? (M + log2f(L)) * (float)kLn2 : -CUDART_INF_F;
-        };
-        int open[2] = {-1, -1};        // first pieces of the groups that other CTAs hold parts of: begun before this CTA, in it
-        // rows r0 .. r0 + RB of the group of pieces `group`
-        auto join_rows = [&](auto rb, const KvPiece& pc, unsigned int group, bool complete, float* part, int r0) {
-            constexpr int RB = decltype(rb)::value;
-            const bool in = (group >> lane) & 1u;
-            const int own = lane < 2 * W ? lane : 0;
-            float M[RB], L[RB], f[RB];
-#pragma unroll
-            for (int i = 0; i < RB; ++i) {
-                const int r = min(r0 + i, pc.n - 1);
-                const float m = in ? sh.m[own][r] : kKvNothing;
-                M[i] = m;
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) M[i] = fmaxf(M[i], __shfl_xor_sync(0xFFFFFFFFu, M[i], o));
-                f[i] = in ? ex2_approx(m - M[i]) : 0.f;
-                L[i] = in ? sh.l[own][r] * f[i] : 0.f;
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) L[i] += __shfl_xor_sync(0xFFFFFFFFu, L[i], o);
-            }
-            for (int cb = 0; cb < D; cb += 128) {
-                const int ch = cb + lane * 4;
-                const bool on = ch < D;
-                float4 o[RB];
-#pragma unroll
-                for (int i = 0; i < RB; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                unsigned int left = group;
-                while (left) {
-                    const int k = __ffs(left) - 1;
-                    left &= left - 1;
-                    const float* from = (k & 1) ? reinterpret_cast<const float*>(sh.ring[k >> 1][0])
-                                                : a.warp_parts + (long long)(c * W + (k >> 1)) * (R * TS);
-                    float4 x[RB];
-#pragma unroll
-                    for (int i = 0; i < RB; ++i) {
-                        x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                        if (on) x[i] = *reinterpret_cast<const float4*>(from + min(r0 + i, pc.n - 1) * TS + ch);
-                    }
-#pragma unroll
-                    for (int i = 0; i < RB; ++i) {
-                        const float fk = __shfl_sync(0xFFFFFFFFu, f[i], k);
-                        o[i].x = fmaf(x[i].x, fk, o[i].x);
-                        o[i].y = fmaf(x[i].y, fk, o[i].y);
-                        o[i].z = fmaf(x[i].z, fk, o[i].z);
-                        o[i].w = fmaf(x[i].w, fk, o[i].w);
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < RB; ++i) {
-                    const int r = r0 + i;
-                    if (!on || r >= pc.n) continue;
-                    if (complete) {
-                        finish_row(pc, r, M[i], L[i], o[i], ch);
-                    } else {
-                        *reinterpret_cast<float4*>(part + r * D + ch) = o[i];
-                        if (ch == 0) {
-                            part[R * D + r] = M[i];
-                            part[R * D + R + r] = L[i];
-                        }
-                    }
-                }
-            }
-        };
-        const bool few = __popc(starts) * 2 < W;   // few groups: a row per warp, else four rows at a time
-        int done = 0;                              // row batches dealt with so far, modulo W
-        while (starts) {
-            const int p = __ffs(starts) - 1;
-            starts &= starts - 1;
-            const unsigned int group = valid & ~((1u << p) - 1u) & (starts ? (1u << (__ffs(starts) - 1)) - 1u : 0xFFFFFFFFu);
-            const KvPiece pc = sh.piece[p];
-            const bool complete = pc.seg >= U0 && pc.seg + pc.pages <= U1;
-            const int which = pc.seg < U0 ? 0 : 1;   // scratch slot of this CTA
-            if (!complete) open[which] = p;
-            float* part = a.cta_parts + (long long)(c * 2 + which) * kPart;
-            const int batches = few ? pc.n : (pc.n + 3) / 4;
-            int k = warp - done;
-            k += k < 0 ? W : 0;
-            done = (done + batches) % W;
-            for (; k < batches; k += W) {
-                if (few) join_rows(std::integral_constant<int, 1>(), pc, group, complete, part, k);
-                else join_rows(std::integral_constant<int, 4>(), pc, group, complete, part, 4 * k);
-            }
-        }
-        // the last CTA that delivers a part of a segment joins them all
-        if (open[0] >= 0 || open[1] >= 0) {
-            __syncthreads();
-            if (tid < 2) {
-                int last = 0;
-                if (open[tid] >= 0) {
-                    const KvPiece pc = sh.piece[open[tid]];
-                    const int c0 = shares.owner(pc.seg) / W, c1 = shares.owner(pc.seg + pc.pages - 1) / W;
-                    last = take_ticket(a.tickets + c0) == (unsigned int)(c1 - c0);
-                    if (last) a.tickets[c0] = 0;
-                }
-                sh.last[tid] = last;
-            }
-            __syncthreads();
-#pragma unroll
-            for (int which = 0; which < 2; ++which) {
-                if (!sh.last[which]) continue;
-                const KvPiece pc = sh.piece[open[which]];
-                const int c0 = shares.owner(pc.seg) / W;
-                const int parts = (shares.owner(pc.seg + pc.pages - 1) / W - c0) + 1;
-                const float* base = a.cta_parts + (long long)c0 * 2 * kPart;   // part k: 2 k, the first one's 1
-                for (int r = warp; r < pc.n; r += W) kv_join_row<DT, D>(a, pc, r, base, kPart, R, parts, G, lane);
-            }
-        }
-    }
+    if (works && !*abort_flag) kv_split_join<DT, D, Sh::W, R, TS>(a, sh, shares);
     if (sh.padding || total == 0) kv_clear_rows<DT>(a, D, total, (int)(blockIdx.x * W + warp), (int)(gridDim.x * W));
 }
 
