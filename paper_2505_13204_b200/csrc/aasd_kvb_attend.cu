@@ -11,6 +11,8 @@ namespace aasd {
 
 namespace {
 
+constexpr int64_t kSplitRows = 48;
+
 template <int DT, int D, int NT>
 int launch_split(const LaunchEnv& env, int sm_count, const KvAttendArgs& a) {
     constexpr auto kernel = kvb_attend_split_kernel<DT, D, NT>;
@@ -20,6 +22,26 @@ int launch_split(const LaunchEnv& env, int sm_count, const KvAttendArgs& a) {
     launch(kernel, (unsigned int)(sm_count < kKvMaxCtas ? sm_count : kKvMaxCtas), (unsigned int)KvbSplitShape<DT, D, NT>::kThreads, smem, env.stream, a);
     return AASD_OK;
 }
+
+#if AASD_DT == 1
+template <int D, bool PAIR>
+int launch_tile(const LaunchEnv& env, int sm_count, const KvAttendArgs& a) {
+    constexpr auto kernel = kv_attend_tile_kernel<8, D, PAIR>;
+    constexpr size_t smem = sizeof(KvbTileShared<D, PAIR>) + 1024;   // (its first member wants a 1024-byte boundary)
+    static_assert(smem <= 227 * 1024, "fits an SM");
+    if (enable_smem<kernel, smem>(env.device) != AASD_OK) return AASD_ERR_CUDA;
+    // the softmax warps wait for registers that the launch must have brought along
+    static const bool enough = [] {
+        cudaFuncAttributes f;
+        return cudaFuncGetAttributes(&f, kernel) == cudaSuccess && f.numRegs >= kTileLaunchRegs;
+    }();
+    if (!enough) return AASD_ERR_UNSUPPORTED;
+    launch(kernel, (unsigned int)(sm_count < kKvMaxCtas ? sm_count : kKvMaxCtas), (unsigned int)kTileThreads, smem, env.stream, a);
+    launch_grid2(kv_tile_join_kernel<D, PAIR>, (unsigned int)(sm_count < kKvMaxCtas ? sm_count : kKvMaxCtas), (PAIR ? 2u : 1u) * kTileRows / 8, 256u,
+                 env.stream, a);
+    return AASD_OK;
+}
+#endif
 
 }  // namespace
 
@@ -40,6 +62,13 @@ int launch_kvb_attend_bf16(const LaunchEnv& env, int sm_count, const KvAttendArg
     const int64_t per_seq = a.p.rows_per_seq > 0 ? a.p.rows_per_seq : (a.p.n_tokens + a.p.n_seqs - 1) / (a.p.n_seqs > 0 ? a.p.n_seqs : 1);
     const int64_t rows = per_seq * (a.p.n_q_heads / a.p.n_kv_heads);
     *launches = 1;
+#if AASD_DT == 1
+    if (rows > kSplitRows && a.p.head_dim <= 128) {
+        *launches = 2;
+        if (a.p.head_dim == 64) return rows > kTileRows ? launch_tile<64, true>(env, sm_count, a) : launch_tile<64, false>(env, sm_count, a);
+        return rows > kTileRows ? launch_tile<128, true>(env, sm_count, a) : launch_tile<128, false>(env, sm_count, a);
+    }
+#endif
     if (a.p.head_dim == 64)
         return rows > 8 ? launch_split<DT, 64, 2>(env, sm_count, a) : launch_split<DT, 64, 1>(env, sm_count, a);
     if (a.p.head_dim == 128)

@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(KvbSplitShape<DT, D, NT>::kThreads, 1) kvb_att
                     top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
                     // the row's largest element becomes 2^14 .. 2^15
                     int e = (int)(__float_as_uint(top) >> 23) - 127;
-                    e = e < -100 ? -100 : e > 100 ? 100 : e;
+                    e = max(e, -112);
                     const float up = kvb_pow2(14 - e);
 #pragma unroll
                     for (int k = 0; k < C; ++k)
