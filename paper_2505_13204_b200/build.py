@@ -26,7 +26,7 @@ UNITS = [("aasd.cu", "host", [])] + [
     for dt in (1, 0)] + [("aasd_kv.cu", "kv", []), ("aasd_kvb.cu", "kvb", []), ("aasd_kv_share.cu", "kv_share", [])]
 DEPENDS = ["aasd.cu", "aasd_verify.cu", "aasd_align.cu", "aasd_align_gumbel.cu", "aasd_tree.cu", "aasd_host.h",
            "aasd_kv.cu", "aasd_kv_attend.cu", "aasd_kv_host.h", "aasd_kv.cuh", "aasd_kv_attend.cuh", "aasd_kv_tile.cuh",
-           "aasd_kvb.cu", "aasd_kvb_attend.cu", "aasd_kvb.cuh", "aasd_kvb_attend.cuh", "aasd_kv_share.cu", "aasd_kv_share.cuh",
+           "aasd_kvb.cu", "aasd_kvb_attend.cu", "aasd_kvb.cuh", "aasd_kvb_attend.cuh", "aasd_kvb_tile.cuh", "aasd_kv_share.cu", "aasd_kv_share.cuh",
            "aasd_device.cuh", "aasd_rows.cuh", "aasd_sampler.cuh", "aasd_stream.cuh", "aasd_tokens.cuh",
            "aasd_tree.cuh", os.path.join("..", "..", "include", "aasd.h")]
 # -fno-gnu-unique / -Bsymbolic: two builds of the library (the normal and the checked one) can

@@ -31,7 +31,7 @@ int launch_split(const LaunchEnv& env, int sm_count, const KvAttendArgs& a) {
 #if AASD_DT == 1
 template <int D, bool PAIR>
 int launch_tile(const LaunchEnv& env, int sm_count, const KvAttendArgs& a) {
-    constexpr auto kernel = kv_attend_tile_kernel<4, D, PAIR>;
+    constexpr auto kernel = kv_attend_tile_kernel<D, PAIR>;
     constexpr size_t smem = sizeof(KvTileShared<D, PAIR>) + 1024;   // (its first member wants a 1024-byte boundary)
     static_assert(smem <= 227 * 1024, "fits an SM");
     if (enable_smem<kernel, smem>(env.device) != AASD_OK) return AASD_ERR_CUDA;

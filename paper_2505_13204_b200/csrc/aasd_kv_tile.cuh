@@ -31,7 +31,6 @@
 #pragma once
 
 #include "aasd_kv_attend.cuh"
-#include "aasd_kvb_attend.cuh"
 
 namespace aasd {
 
@@ -107,38 +106,6 @@ struct KvTileShared {
     int abort_flag, padding;
 };
 
-// The same of the 8-bit cache: pages are operands as they come, so there are no keys apart; queries are two e4m3 numbers
-// each (D = 128: a panel of 128 bytes per row for each, D = 64: the halves of one).
-constexpr int kByteRaw = 5, kByteValues = 4;
-template <int D, bool PAIR>
-struct KvbTileShared {
-    static constexpr int R = PAIR ? 2 * kTileRows : kTileRows;
-    static constexpr int kRaw = (kvb_head_bytes(D) + 1023) / 1024 * 1024;
-    alignas(1024) unsigned char queries[PAIR ? 2 : 1][kTileRows * D * 2];
-    alignas(1024) unsigned char raw[kByteRaw][kRaw];
-    alignas(1024) unsigned char values[kByteValues][kPage * D * 2];
-    float kscale[kTileMeta];           // a page's scale of the keys
-    int ev[kTileMeta];                 // exponent field that a page's values are relative to; -1: page hidden
-    int raw_missing[kByteRaw];
-    float row_q[PAIR ? 2 : 1][kTileRows];         // what the rows' queries were divided by, times the scale of the products
-    float exchange_m[kTileRows], exchange_l[kTileRows], exchange_up[kTileRows];   // between the groups, where they share a tile
-    int base[kTileThreads];
-    long long scan[kTileThreads / 32];
-    KvTilePiece piece[kTilePieces];
-    KvShares shares;
-    KvPiece open;                      // the segment that begins in this CTA and ends in another
-    u64 piece_full[kTilePieces], piece_empty[kTilePieces];
-    u64 raw_full[kByteRaw], raw_empty[kByteRaw];
-    u64 full[kTileMeta];               // a page's values are unpacked
-    u64 v_empty[kByteValues], m_empty[kTileMeta];
-    u64 q_full[2], s_full[2][2], p_full[2][2], o_done[2][2], x_full, x_empty, r_full, drain[2];
-    unsigned int tmem;
-    int abort_flag, padding;
-};
-
-template <int BITS, int D, bool PAIR>
-using KvTileSharedOf = std::conditional_t<BITS == 8, KvbTileShared<D, PAIR>, KvTileShared<D, PAIR>>;
-
 // ---- tcgen05 ----------------------------------------------------------------------------------------
 
 __device__ __forceinline__ void tc_alloc(unsigned int* where, unsigned int columns) {
@@ -169,27 +136,9 @@ __device__ __forceinline__ void tc_mma_ss(unsigned int d, u64 a, u64 b, unsigned
         "l"(a), "l"(b), "r"(idesc), "r"(add ? 1u : 0u)
         : "memory");
 }
-// ... of e4m3 numbers
-__device__ __forceinline__ void tc_mma_bytes(unsigned int d, u64 a, u64 b, unsigned int idesc, bool add) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(add ? 1u : 0u)
-        : "memory");
-}
-// fp32 result, fp16 or bf16 (or, in the byte form, e4m3: all type fields 0) operands, both K-major, M = 128
+// fp32 result, fp16 or bf16 operands, both K-major, M = 128
 __host__ __device__ constexpr unsigned int tc_idesc(int n, bool bf16) {
     return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | ((unsigned int)(n >> 3) << 17) | ((128u >> 4) << 24);
-}
-constexpr unsigned int kTcTransposedB = 1u << 16;   // the second operand's rows run along K
-// Rows of 64 bytes in the 64-byte swizzle, groups of eight rows 512 bytes apart.
-__device__ __forceinline__ u64 tc_desc_64(unsigned int addr) {
-    return (u64)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | (32ull << 32) | (1ull << 46) | (4ull << 61);
-}
-// An operand whose rows (128 bytes, 64 fp16 numbers, in the 128-byte swizzle) run along K: groups of eight rows 1024 bytes
-// apart, panels of 64 numbers kPage rows apart.
-__device__ __forceinline__ u64 tc_desc_rows(unsigned int addr) {
-    return (u64)((addr & 0x3FFFFu) >> 4) | ((u64)(kPage * 128 / 16) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
 // Rows of 128 bytes in the 128-byte swizzle, groups of eight rows 1024 bytes apart.
 __device__ __forceinline__ u64 tc_desc(unsigned int addr) {
@@ -266,16 +215,89 @@ __device__ __forceinline__ void tile_scale_o(unsigned int col_o, const float (&f
     tc_wait_store();   // (a page may scale O twice)
 }
 
+// The walker's one thread: goes through the CTA's share of the work and hands it out piece by piece.  False: a wait has given up.
+template <class Shared, class Wait>
+__device__ __forceinline__ bool kv_tile_walk(const KvAttendArgs& a, Shared& sh, int total, int strip, int R, int G, const Wait& wait_one) {
+    const int B = a.p.n_seqs, c = blockIdx.x;
+    bool ok = true;
+    const KvShares shares(total, min((int)gridDim.x, max(total, 1)));
+    sh.shares = shares;
+    KvTilePiece w{};
+    int left = 0;            // units of the share from page w.pg on
+    KvSeq q{};
+    if (c < total) {
+        // the share's first unit: its sequence, head, tile and page
+        const int u0 = shares.first(c);
+        int lo = 0, hi = (B + strip - 1) / strip;
+#pragma unroll 1
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (sh.base[mid] <= u0) lo = mid;
+            else hi = mid;
+        }
+        int rem = u0 - sh.base[lo], per_head;
+        w.b = lo * strip - 1;
+#pragma unroll 1
+        do {
+            q = kv_load_seq(a, ++w.b, R);
+            per_head = (int)kv_tile_head_units(a, q, R, G);
+            rem -= per_head * a.p.n_kv_heads;
+        } while (rem >= 0);
+        rem += per_head * a.p.n_kv_heads;
+        w.h = rem / per_head;
+        rem -= w.h * per_head;
+        w.tile = -1;
+#pragma unroll 1
+        do {
+            w.pages = kv_tile_pages(a, q.cached, q.fresh, q.pages, ++w.tile, R, G);
+            rem -= w.pages + kTileSegCost;
+        } while (rem >= 0);
+        rem += w.pages;              // of the first page, counted from page 0
+        w.pg = max(rem, 0);
+        left = shares.first(c + 1) - u0 - (w.pg - rem);
+        w.seg = u0 - rem;
+    }
+#pragma unroll 1
+    for (int k = 0; ok; ++k) {
+        ok = wait_one(&sh.piece_empty[k % kTilePieces], ((k / kTilePieces) & 1) ^ 1);
+        if (!ok) break;
+        w.np = max(0, min(w.pages - w.pg, left));
+        w.cached = q.cached;
+        w.fresh = q.fresh;
+        w.first = q.first;
+        sh.piece[k % kTilePieces] = w;
+        mbar_arrive(&sh.piece_full[k % kTilePieces]);
+        if (w.np == 0) break;
+        left -= w.pages - w.pg + kTileSegCost;
+        w.seg += w.pages + kTileSegCost;
+        w.pg = 0;
+        if (++w.tile == q.tiles) {
+            w.tile = 0;
+            if (++w.h == a.p.n_kv_heads) {
+                w.h = 0;
+#pragma unroll 1
+                do {
+                    if (++w.b >= B) {
+                        left = 0;
+                        break;
+                    }
+                    q = kv_load_seq(a, w.b, R);
+                } while (q.pages == 0 || q.tiles == 0);
+            }
+        }
+        if (left > 0) w.pages = kv_tile_pages(a, q.cached, q.fresh, q.pages, w.tile, R, G);
+    }
+    return ok;
+}
+
 // ---- the kernel ---------------------------------------------------------------------------------------
 
-template <int BITS, int D, bool PAIR>
+template <int D, bool PAIR>
 __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const KvAttendArgs a) {
-    using Shared = KvTileSharedOf<BITS, D, PAIR>;
+    using Shared = KvTileShared<D, PAIR>;
     constexpr int R = Shared::R, H = D / 2;
-    constexpr int NR = BITS == 8 ? kByteRaw : kTileRaw, NV = BITS == 8 ? kByteValues : kTileValues;   // ring depths
-    constexpr int kHead = BITS == 8 ? kvb_head_bytes(D) : kv_head_bytes(D);
     constexpr unsigned int kColS = 0, kColO = 256, kStep = 128;    // first columns of group 0's S and O; group 1's are kStep behind
-    constexpr unsigned int kIdescS = tc_idesc(kPage, BITS == 4), kIdescO = tc_idesc(D, false) | (BITS == 8 ? kTcTransposedB : 0u);
+    constexpr unsigned int kIdescS = tc_idesc(kPage, true), kIdescO = tc_idesc(D, false);
     extern __shared__ unsigned char smem_raw[];
     Shared& sh = *reinterpret_cast<Shared*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
     pdl_launch_dependents();
@@ -287,18 +309,16 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
             mbar_init(&sh.piece_empty[i], 8 + 4 + 2 + 1);
         }
 #pragma unroll 1
-        for (int i = 0; i < NR; ++i) {
+        for (int i = 0; i < kTileRaw; ++i) {
             mbar_init(&sh.raw_full[i], blockIdx.x == 0 && i == a.withhold_page ? 2 : 1);   // (testing aid: the second arrival never comes)
-            mbar_init(&sh.raw_empty[i], BITS == 8 ? 4 + (PAIR ? 2 : 1) : 4);               // (8 bits: the products with the keys read it too)
-        }
-        if constexpr (BITS == 4) {
-#pragma unroll 1
-            for (int i = 0; i < kTileKeys; ++i) {
-                mbar_init(&sh.k_empty[i], PAIR ? 2 : 1);
-            }
+            mbar_init(&sh.raw_empty[i], 4);
         }
 #pragma unroll 1
-        for (int i = 0; i < NV; ++i) {
+        for (int i = 0; i < kTileKeys; ++i) {
+            mbar_init(&sh.k_empty[i], PAIR ? 2 : 1);
+        }
+#pragma unroll 1
+        for (int i = 0; i < kTileValues; ++i) {
             mbar_init(&sh.v_empty[i], PAIR ? 2 : 1);
         }
 #pragma unroll 1
@@ -359,73 +379,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
         if (warp == 15) {
             // ---- walker
             if (lane == 0) {
-                const KvShares shares(total, min((int)gridDim.x, max(total, 1)));
-                sh.shares = shares;
-                KvTilePiece w{};
-                int left = 0;            // units of the share from page w.pg on
-                KvSeq q{};
-                if (c < total) {
-                    // the share's first unit: its sequence, head, tile and page
-                    const int u0 = shares.first(c);
-                    int lo = 0, hi = (B + strip - 1) / strip;
-#pragma unroll 1
-                    while (hi - lo > 1) {
-                        const int mid = (lo + hi) >> 1;
-                        if (sh.base[mid] <= u0) lo = mid;
-                        else hi = mid;
-                    }
-                    int rem = u0 - sh.base[lo], per_head;
-                    w.b = lo * strip - 1;
-#pragma unroll 1
-                    do {
-                        q = kv_load_seq(a, ++w.b, R);
-                        per_head = (int)kv_tile_head_units(a, q, R, G);
-                        rem -= per_head * a.p.n_kv_heads;
-                    } while (rem >= 0);
-                    rem += per_head * a.p.n_kv_heads;
-                    w.h = rem / per_head;
-                    rem -= w.h * per_head;
-                    w.tile = -1;
-#pragma unroll 1
-                    do {
-                        w.pages = kv_tile_pages(a, q.cached, q.fresh, q.pages, ++w.tile, R, G);
-                        rem -= w.pages + kTileSegCost;
-                    } while (rem >= 0);
-                    rem += w.pages;              // of the first page, counted from page 0
-                    w.pg = max(rem, 0);
-                    left = shares.first(c + 1) - u0 - (w.pg - rem);
-                    w.seg = u0 - rem;
-                }
-#pragma unroll 1
-                for (int k = 0; ok; ++k) {
-                    ok = wait_one(&sh.piece_empty[k % kTilePieces], ((k / kTilePieces) & 1) ^ 1);
-                    if (!ok) break;
-                    w.np = max(0, min(w.pages - w.pg, left));
-                    w.cached = q.cached;
-                    w.fresh = q.fresh;
-                    w.first = q.first;
-                    sh.piece[k % kTilePieces] = w;
-                    mbar_arrive(&sh.piece_full[k % kTilePieces]);
-                    if (w.np == 0) break;
-                    left -= w.pages - w.pg + kTileSegCost;
-                    w.seg += w.pages + kTileSegCost;
-                    w.pg = 0;
-                    if (++w.tile == q.tiles) {
-                        w.tile = 0;
-                        if (++w.h == a.p.n_kv_heads) {
-                            w.h = 0;
-#pragma unroll 1
-                            do {
-                                if (++w.b >= B) {
-                                    left = 0;
-                                    break;
-                                }
-                                q = kv_load_seq(a, w.b, R);
-                            } while (q.pages == 0 || q.tiles == 0);
-                        }
-                    }
-                    if (left > 0) w.pages = kv_tile_pages(a, q.cached, q.fresh, q.pages, w.tile, R, G);
-                }
+                ok = kv_tile_walk(a, sh, total, strip, R, G, wait_one);
             }
             __syncwarp();
         } else if (warp == 13) {
@@ -440,8 +394,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                 if (np == 0) break;
                 const bool inside = AASD_IN_RANGE(w.b < B && w.h < a.p.n_kv_heads && pg + np <= a.p.max_pages, a.state);
                 const int32_t* table = a.block_table + (long long)w.b * a.p.max_pages + pg;
-                const uint8_t* head = a.pages + (long long)w.h * kHead;
-                const u64 stride = (u64)a.p.n_kv_heads * kHead;
+                const uint8_t* head = a.pages + (long long)w.h * kv_head_bytes(D);
+                const u64 stride = (u64)a.p.n_kv_heads * kv_head_bytes(D);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.piece_empty[k % kTilePieces]);
                 int ids = 0;
@@ -449,15 +403,15 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                 for (int i = 0; i < np; ++i, ++n) {
                     if ((i & 31) == 0) ids = i + lane < np && inside ? table[i + lane] : -1;
                     const int page = __shfl_sync(0xFFFFFFFFu, ids, i & 31);
-                    const int slot = n % NR;
-                    ok = wait(&sh.raw_empty[slot], ((n / NR) & 1) ^ 1);
+                    const int slot = n % kTileRaw;
+                    ok = wait(&sh.raw_empty[slot], ((n / kTileRaw) & 1) ^ 1);
                     if (!ok) break;
                     if (lane == 0) {
                         const bool there = page >= 0 && page < a.p.n_pages;
                         sh.raw_missing[slot] = !there;
                         if (there) {
-                            mbar_arrive_expect_tx(&sh.raw_full[slot], kHead);
-                            bulk_copy_g2s(sh.raw[slot], head + (u64)(unsigned int)page * stride, kHead, &sh.raw_full[slot]);
+                            mbar_arrive_expect_tx(&sh.raw_full[slot], kv_head_bytes(D));
+                            bulk_copy_g2s(sh.raw[slot], head + (u64)(unsigned int)page * stride, kv_head_bytes(D), &sh.raw_full[slot]);
                         } else {
                             raise(a.state, AASD_STATUS_BAD_OFFSETS);
                             mbar_arrive(&sh.raw_full[slot]);
@@ -469,9 +423,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
             }
             // nothing may be on its way into this CTA's shared memory when it leaves
 #pragma unroll 1
-            for (int k = max(0, n - NR); k < n; ++k)
+            for (int k = max(0, n - kTileRaw); k < n; ++k)
 #pragma unroll 1
-                for (unsigned int it = 0; it < a.wait_limit && !mbar_try_wait(&sh.raw_full[k % NR], (k / NR) & 1); ++it) {}
+                for (unsigned int it = 0; it < a.wait_limit && !mbar_try_wait(&sh.raw_full[k % kTileRaw], (k / kTileRaw) & 1); ++it) {}
         } else {
             // ---- issuers: warp 12 for group 0, warp 14 for group 1
             if (lane == 0) {
@@ -495,43 +449,26 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                     for (int i = first; i < np; i += step, ++taken) {
 #pragma unroll 1
                         for (; ahead < np && asked < taken + 2; ahead += step, ++asked) {
-                            const int n = n0 + ahead, buf = asked & 1;
-                            if constexpr (BITS == 8) {
-                                const int slot = n % NR;
-                                ok = wait_one(&sh.raw_full[slot], (n / NR) & 1);
-                                if (!ok) break;
-                                tc_fence_after();
-                                const unsigned int at = smem_u32(sh.raw[slot]);
-                                const u64 keys = D == 64 ? tc_desc_64(at) : tc_desc(at);
+                            const int n = n0 + ahead, slot = n % kTileKeys, buf = asked & 1;
+                            ok = wait_one(&sh.full[n % kTileMeta], (n / kTileMeta) & 1);
+                            if (!ok) break;
+                            tc_fence_after();
+                            const u64 keys = tc_desc(smem_u32(sh.keys[slot]));
 #pragma unroll
-                                for (int ks = 0; ks < 2 * (D / 32); ++ks) {   // (the queries' first numbers, then their second ones)
-                                    const int second = ks / (D / 32), k = ks % (D / 32);
-                                    tc_mma_bytes(tm + kColS + x * kStep + buf * 64, q + second * (D == 64 ? 4 : kTileRows * 8) + k * 2, keys + k * 2, kIdescS, ks > 0);
-                                }
-                                tc_commit(&sh.s_full[x][buf]);
-                                tc_commit(&sh.raw_empty[slot]);
-                            } else {
-                                const int slot = n % kTileKeys;
-                                ok = wait_one(&sh.full[n % kTileMeta], (n / kTileMeta) & 1);
-                                if (!ok) break;
-                                tc_fence_after();
-                                const u64 keys = tc_desc(smem_u32(sh.keys[slot]));
-#pragma unroll
-                                for (int ks = 0; ks < D / 16; ++ks)   // (descriptors count 16 bytes; a panel is 64 channels of all rows)
-                                    tc_mma_ss(tm + kColS + x * kStep + buf * 64, q + (ks / 4) * (kTileRows * 8) + (ks % 4) * 2,
-                                              keys + (ks / 4) * (kPage * 8) + (ks % 4) * 2, kIdescS, ks > 0);
-                                tc_commit(&sh.s_full[x][buf]);
-                                tc_commit(&sh.k_empty[slot]);
-                            }
+                            for (int ks = 0; ks < D / 16; ++ks)   // (descriptors count 16 bytes; a panel is 64 channels of all rows)
+                                tc_mma_ss(tm + kColS + x * kStep + buf * 64, q + (ks / 4) * (kTileRows * 8) + (ks % 4) * 2,
+                                          keys + (ks / 4) * (kPage * 8) + (ks % 4) * 2, kIdescS, ks > 0);
+                            tc_commit(&sh.s_full[x][buf]);
+                            tc_commit(&sh.k_empty[slot]);
                         }
-                        const int n = n0 + i, slot = n % NV, buf = taken & 1;
-                        ok = ok && wait_one(&sh.p_full[x][buf], (taken >> 1) & 1);   // (the probabilities came after the page's values)
+                        const int n = n0 + i, slot = n % kTileValues, buf = taken & 1;
+                        ok = ok && wait_one(&sh.p_full[x][buf], (taken >> 1) & 1);   // (the page's values came with its keys)
                         if (!ok) break;
                         tc_fence_after();
-                        const u64 v = BITS == 8 ? tc_desc_rows(smem_u32(sh.values[slot])) : tc_desc(smem_u32(sh.values[slot]));
+                        const u64 v = tc_desc(smem_u32(sh.values[slot]));
 #pragma unroll
                         for (int ks = 0; ks < kPage / 16; ++ks)
-                            tc_mma(tm + kColO + x * kStep, tm + kColS + x * kStep + buf * 64 + ks * 8, v + ks * (BITS == 8 ? 128 : 2), kIdescO, i > first || ks > 0);
+                            tc_mma(tm + kColO + x * kStep, tm + kColS + x * kStep + buf * 64 + ks * 8, v + ks * 2, kIdescO, i > first || ks > 0);
                         tc_commit(&sh.v_empty[slot]);
                         tc_commit(&sh.o_done[x][buf]);
                     }
@@ -562,146 +499,89 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
             int ev = 64;
 #pragma unroll 1
             for (int i = 0; i < np; ++i, ++n) {
-                if constexpr (BITS == 8) {
-                    // Values to fp16, relative to the largest scale of the pages so far: a lane takes 16 channels of a token at a time, and
-                    // eight neighbouring lanes write to eight different chunks.
-                    constexpr int C = D / 16, TS = 128 / C;      // chunks of a token; tokens at a time
-                    const int slot = n % NR, mslot = n % kTileMeta, vslot = n % NV;
-                    ok = together(wait_one(&sh.raw_full[slot], (n / NR) & 1) && wait_one(&sh.v_empty[vslot], ((n / NV) & 1) ^ 1) &&
-                                  wait_one(&sh.m_empty[mslot], ((n / kTileMeta) & 1) ^ 1));
-                    if (!ok) break;
-                    const unsigned char* raw = sh.raw[slot];
-                    const bool missing = sh.raw_missing[slot] != 0;
-                    const int left = missing ? 0 : end - i * kPage;   // places in use
-                    const uint2 scale = *reinterpret_cast<const uint2*>(raw + kvb_scale_offset(D));
-                    const int chunk = u % C, ep = missing ? 0 : kvb_exponent(scale.y) + 127;
-                    uint4 w[kPage / TS];
+                const int slot = n % kTileRaw, mslot = n % kTileMeta, kslot = n % kTileKeys, vslot = n % kTileValues;
+                ok = together(wait_one(&sh.raw_full[slot], (n / kTileRaw) & 1) && wait_one(&sh.k_empty[kslot], ((n / kTileKeys) & 1) ^ 1) &&
+                              wait_one(&sh.v_empty[vslot], ((n / kTileValues) & 1) ^ 1) && wait_one(&sh.m_empty[mslot], ((n / kTileMeta) & 1) ^ 1));
+                if (!ok) break;
+                const unsigned char* raw = sh.raw[slot];
+                const bool missing = sh.raw_missing[slot] != 0;
+                const int left = missing ? 0 : end - i * kPage;   // places in use
+                // Everything is fetched first.  Keys: half a token's row per thread (word k of a token: channels 4k .. of each
+                // half).  Values: a channel's 64 codes, and those of the channel H above it, per TPR threads.
+                constexpr int NW = H / 8;                        // words of keys per thread
+                constexpr int TPR = 128 / H, NP = 8 / TPR;       // threads per row of values; 16-byte pieces per thread and half
+                const int t = u >> 1, khalf = u & 1, r = u / TPR, vpart = u % TPR;
+                unsigned int kw[NW], vw[2 * NP];
+                const uint2 vm = *reinterpret_cast<const uint2*>(raw + kv_value_meta_offset(D) + 8 * lane);
+                const uint4 four = lds16(raw + kv_value_meta_offset(D) + 16 * (lane & 15));
+                const unsigned int key_meta = *reinterpret_cast<const unsigned int*>(raw + kv_key_meta_offset(D) + 4 * (u & (kPage - 1)));
 #pragma unroll
-                    for (int k = 0; k < kPage / TS; ++k) w[k] = lds16(raw + kvb_value_offset(D) + kvb_chunk_offset(D, k * TS + u / C, chunk));
-                    ev = max(ev, ep);
-                    if (u == 0) {
-                        sh.kscale[mslot] = missing ? 1.f : kvb_pow2(kvb_exponent(scale.x));
-                        sh.ev[mslot] = missing ? -1 : ev;
-                    }
-                    const __half2 by = __float2half2_rn(ev - ep > 40 ? 0.f : kvb_pow2(ep - ev));
-                    unsigned char* to = sh.values[vslot] + (chunk >> 2) * (kPage * 128);
+                for (int k = 0; k < NW; k += 4) {
+                    const uint4 q = lds16(raw + t * H + khalf * (H / 2) + 4 * k);
+                    kw[k] = q.x; kw[k + 1] = q.y; kw[k + 2] = q.z; kw[k + 3] = q.w;
+                }
 #pragma unroll
-                    for (int k = 0; k < kPage / TS; ++k) {
-                        const int t = k * TS + u / C;
-                        const unsigned int word[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
-                        unsigned int h[8];
+                for (int k = 0; k < 2 * NP; k += 4) {
+                    const uint4 q = lds16(raw + kv_value_offset(D) + r * kPage + vpart * (kPage / TPR) + 4 * k);
+                    vw[k] = q.x; vw[k + 1] = q.y; vw[k + 2] = q.z; vw[k + 3] = q.w;
+                }
+                // largest value of the page (every warp for itself): codes run from the minimum to 15 scales above it
+                auto reach = [](unsigned int m) { return fmaxf(fabsf(meta_min(m)), fabsf(fmaf(15.f, meta_scale(m), meta_min(m)))); };
+                float vt = 2 * lane < left ? reach(vm.x) : 0.f;
+                if (2 * lane + 1 < left) vt = fmaxf(vt, reach(vm.y));
+                // (an exponent field, held to a range in which the factors below are normal numbers)
+                ev = max(ev, min(250, (int)(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(vt)) >> 23)));
+                // the values' table: lane q < 16 has tokens 4q .. 4q + 3, in the order in which their codes leave a word
+                if (lane < kPage / 4) {
+                    const float norm = pow2f(127 - ev);
+                    const unsigned int m0 = 4 * lane < left ? four.x : 0u, m1 = 4 * lane + 1 < left ? four.y : 0u,
+                                       m2 = 4 * lane + 2 < left ? four.z : 0u, m3 = 4 * lane + 3 < left ? four.w : 0u;
+                    sh.vmeta[uw][lane] = make_uint4(pack_half(meta_scale(m0) * norm, meta_scale(m2) * norm), pack_half(meta_scale(m1) * norm, meta_scale(m3) * norm),
+                                                    pack_half(meta_min(m0) * norm, meta_min(m2) * norm), pack_half(meta_min(m1) * norm, meta_min(m3) * norm));
+                }
+                if (u < kPage) {
+                    const unsigned int km = u < left ? key_meta : 0u;
+                    const int at = tile_place(u);
+                    float* kq = reinterpret_cast<float*>(&sh.kmeta[mslot][at >> 1]);
+                    kq[at & 1] = meta_scale(km);
+                    kq[2 + (at & 1)] = meta_min(km);
+                    if (u == 0) sh.ev[mslot] = missing ? -1 : ev;
+                }
+                {
+                    // Keys: word k becomes 16-byte piece k of the token's row; the two threads of a token take their pieces
+                    // in orders that keep eight neighbouring threads on eight different pieces.
+                    const int at = tile_place(t);
+                    unsigned char* to = sh.keys[kslot] + at * 128;
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            h[2 * q] = t < left ? kvb_halves<false>(word[q]) : 0u;
-                            h[2 * q + 1] = t < left ? kvb_halves<true>(word[q]) : 0u;
-                        }
-                        if (ep < ev) {
+                    for (int k = 0; k < NW; ++k) {
+                        const int kk = NW == 8 ? k ^ (khalf * 4) : k;
+                        const unsigned int x = NW == 8 ? (khalf ? kw[k ^ 4] : kw[k]) : kw[k], y = x >> 8;
+                        const int piece = khalf * NW + kk;       // of the token's H / 4
+                        *reinterpret_cast<uint4*>(to + (piece >> 3) * (kPage * 128) + (((piece & 7) ^ (at & 7)) << 4)) =
+                            make_uint4(bf16_codes<false>(x), bf16_codes<false>(y), bf16_codes<true>(x), bf16_codes<true>(y));
+                    }
+                }
+                __syncwarp();   // (the table)
+                // values: 8 tokens of a channel are a 16-byte piece
+                unsigned char* lo = sh.values[vslot] + r * 128;
+                unsigned char* hi = lo + H * 128;            // (H is a multiple of 8: the same swizzle)
 #pragma unroll
-                            for (int q = 0; q < 8; ++q) {
-                                const __half2 y = __hmul2(as_half2(h[q]), by);
-                                h[q] = *reinterpret_cast<const unsigned int*>(&y);
-                            }
-                        }
-                        const int second = chunk >> 2;   // (D = 128: the panels' lanes store their halves in turn)
-#pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            const bool high = (q ^ second) != 0;
-                            *reinterpret_cast<uint4*>(to + t * 128 + (((2 * (chunk & 3) + (high ? 1 : 0)) ^ (t & 7)) << 4)) =
-                                high ? make_uint4(h[4], h[5], h[6], h[7]) : make_uint4(h[0], h[1], h[2], h[3]);
-                        }
-                    }
-                    fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(&sh.full[mslot]);
-                        mbar_arrive(&sh.raw_empty[slot]);
-                    }
-                } else {
-                    const int slot = n % kTileRaw, mslot = n % kTileMeta, kslot = n % kTileKeys, vslot = n % kTileValues;
-                    ok = together(wait_one(&sh.raw_full[slot], (n / kTileRaw) & 1) && wait_one(&sh.k_empty[kslot], ((n / kTileKeys) & 1) ^ 1) &&
-                                  wait_one(&sh.v_empty[vslot], ((n / kTileValues) & 1) ^ 1) && wait_one(&sh.m_empty[mslot], ((n / kTileMeta) & 1) ^ 1));
-                    if (!ok) break;
-                    const unsigned char* raw = sh.raw[slot];
-                    const bool missing = sh.raw_missing[slot] != 0;
-                    const int left = missing ? 0 : end - i * kPage;   // places in use
-                    // Everything is fetched first.  Keys: half a token's row per thread (word k of a token: channels 4k .. of each
-                    // half).  Values: a channel's 64 codes, and those of the channel H above it, per TPR threads.
-                    constexpr int NW = H / 8;                        // words of keys per thread
-                    constexpr int TPR = 128 / H, NP = 8 / TPR;       // threads per row of values; 16-byte pieces per thread and half
-                    const int t = u >> 1, khalf = u & 1, r = u / TPR, vpart = u % TPR;
-                    unsigned int kw[NW], vw[2 * NP];
-                    const uint2 vm = *reinterpret_cast<const uint2*>(raw + kv_value_meta_offset(D) + 8 * lane);
-                    const uint4 four = lds16(raw + kv_value_meta_offset(D) + 16 * (lane & 15));
-                    const unsigned int key_meta = *reinterpret_cast<const unsigned int*>(raw + kv_key_meta_offset(D) + 4 * (u & (kPage - 1)));
-#pragma unroll
-                    for (int k = 0; k < NW; k += 4) {
-                        const uint4 q = lds16(raw + t * H + khalf * (H / 2) + 4 * k);
-                        kw[k] = q.x; kw[k + 1] = q.y; kw[k + 2] = q.z; kw[k + 3] = q.w;
-                    }
-#pragma unroll
-                    for (int k = 0; k < 2 * NP; k += 4) {
-                        const uint4 q = lds16(raw + kv_value_offset(D) + r * kPage + vpart * (kPage / TPR) + 4 * k);
-                        vw[k] = q.x; vw[k + 1] = q.y; vw[k + 2] = q.z; vw[k + 3] = q.w;
-                    }
-                    // largest value of the page (every warp for itself): codes run from the minimum to 15 scales above it
-                    auto reach = [](unsigned int m) { return fmaxf(fabsf(meta_min(m)), fabsf(fmaf(15.f, meta_scale(m), meta_min(m)))); };
-                    float vt = 2 * lane < left ? reach(vm.x) : 0.f;
-                    if (2 * lane + 1 < left) vt = fmaxf(vt, reach(vm.y));
-                    // (an exponent field, held to a range in which the factors below are normal numbers)
-                    ev = max(ev, min(250, (int)(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(vt)) >> 23)));
-                    // the values' table: lane q < 16 has tokens 4q .. 4q + 3, in the order in which their codes leave a word
-                    if (lane < kPage / 4) {
-                        const float norm = pow2f(127 - ev);
-                        const unsigned int m0 = 4 * lane < left ? four.x : 0u, m1 = 4 * lane + 1 < left ? four.y : 0u,
-                                           m2 = 4 * lane + 2 < left ? four.z : 0u, m3 = 4 * lane + 3 < left ? four.w : 0u;
-                        sh.vmeta[uw][lane] = make_uint4(pack_half(meta_scale(m0) * norm, meta_scale(m2) * norm), pack_half(meta_scale(m1) * norm, meta_scale(m3) * norm),
-                                                        pack_half(meta_min(m0) * norm, meta_min(m2) * norm), pack_half(meta_min(m1) * norm, meta_min(m3) * norm));
-                    }
-                    if (u < kPage) {
-                        const unsigned int km = u < left ? key_meta : 0u;
-                        const int at = tile_place(u);
-                        float* kq = reinterpret_cast<float*>(&sh.kmeta[mslot][at >> 1]);
-                        kq[at & 1] = meta_scale(km);
-                        kq[2 + (at & 1)] = meta_min(km);
-                        if (u == 0) sh.ev[mslot] = missing ? -1 : ev;
-                    }
-                    {
-                        // Keys: word k becomes 16-byte piece k of the token's row; the two threads of a token take their pieces
-                        // in orders that keep eight neighbouring threads on eight different pieces.
-                        const int at = tile_place(t);
-                        unsigned char* to = sh.keys[kslot] + at * 128;
-#pragma unroll
-                        for (int k = 0; k < NW; ++k) {
-                            const int kk = NW == 8 ? k ^ (khalf * 4) : k;
-                            const unsigned int x = NW == 8 ? (khalf ? kw[k ^ 4] : kw[k]) : kw[k], y = x >> 8;
-                            const int piece = khalf * NW + kk;       // of the token's H / 4
-                            *reinterpret_cast<uint4*>(to + (piece >> 3) * (kPage * 128) + (((piece & 7) ^ (at & 7)) << 4)) =
-                                make_uint4(bf16_codes<false>(x), bf16_codes<false>(y), bf16_codes<true>(x), bf16_codes<true>(y));
-                        }
-                    }
-                    __syncwarp();   // (the table)
-                    // values: 8 tokens of a channel are a 16-byte piece
-                    unsigned char* lo = sh.values[vslot] + r * 128;
-                    unsigned char* hi = lo + H * 128;            // (H is a multiple of 8: the same swizzle)
-#pragma unroll
-                    for (int k = 0; k < NP; ++k) {
-                        const unsigned int x0 = vw[2 * k], x1 = vw[2 * k + 1], y0 = x0 >> 8, y1 = x1 >> 8;
-                        const uint4 q0 = sh.vmeta[uw][2 * (vpart * NP + k)], q1 = sh.vmeta[uw][2 * (vpart * NP + k) + 1];
-                        const __half2 s0 = as_half2(q0.x), s1 = as_half2(q0.y), m0 = as_half2(q0.z), m1 = as_half2(q0.w);
-                        const __half2 s2 = as_half2(q1.x), s3 = as_half2(q1.y), m2 = as_half2(q1.z), m3 = as_half2(q1.w);
-                        const int at = ((vpart * NP + k) ^ (r & 7)) << 4;
-                        *reinterpret_cast<uint4*>(lo + at) =
-                            make_uint4(expand<false>(x0, s0, m0), expand<false>(y0, s1, m1), expand<false>(x1, s2, m2), expand<false>(y1, s3, m3));
-                        *reinterpret_cast<uint4*>(hi + at) =
-                            make_uint4(expand<true>(x0, s0, m0), expand<true>(y0, s1, m1), expand<true>(x1, s2, m2), expand<true>(y1, s3, m3));
-                    }
-                    fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(&sh.full[mslot]);
-                        mbar_arrive(&sh.raw_empty[slot]);
-                    }
-            
+                for (int k = 0; k < NP; ++k) {
+                    const unsigned int x0 = vw[2 * k], x1 = vw[2 * k + 1], y0 = x0 >> 8, y1 = x1 >> 8;
+                    const uint4 q0 = sh.vmeta[uw][2 * (vpart * NP + k)], q1 = sh.vmeta[uw][2 * (vpart * NP + k) + 1];
+                    const __half2 s0 = as_half2(q0.x), s1 = as_half2(q0.y), m0 = as_half2(q0.z), m1 = as_half2(q0.w);
+                    const __half2 s2 = as_half2(q1.x), s3 = as_half2(q1.y), m2 = as_half2(q1.z), m3 = as_half2(q1.w);
+                    const int at = ((vpart * NP + k) ^ (r & 7)) << 4;
+                    *reinterpret_cast<uint4*>(lo + at) =
+                        make_uint4(expand<false>(x0, s0, m0), expand<false>(y0, s1, m1), expand<false>(x1, s2, m2), expand<false>(y1, s3, m3));
+                    *reinterpret_cast<uint4*>(hi + at) =
+                        make_uint4(expand<true>(x0, s0, m0), expand<true>(y0, s1, m1), expand<true>(x1, s2, m2), expand<true>(y1, s3, m3));
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&sh.full[mslot]);
+                    mbar_arrive(&sh.raw_empty[slot]);
                 }
             }
             if (!ok) break;
@@ -757,73 +637,29 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                                 if (i == k) raw[i].a = slow.a;
                         }
                     }
-                    if constexpr (BITS == 8) {
-                        // Each as two e4m3 numbers, the row's largest element between 2^7 and 2^8: eight bits from 2^-2 on, smaller ones are
-                        // off by 2^-10 at most.  A row that is not finite becomes NaN.
-                        float top[8];
+                    float sum[8];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            if (row0 + rb + k * RI + lane / LR >= rows_here) raw[k].clear();
-                            float2 y[4];
-                            raw[k].unpack(y);
-                            top[k] = 0.f;
+                    for (int k = 0; k < 8; ++k) {
+                        const int r = row_base + rb + k * RI + lane / LR;
+                        if (row0 + rb + k * RI + lane / LR >= rows_here) raw[k].clear();
+                        float2 y[4];
+                        raw[k].unpack(y);
+                        sum[k] = ((y[0].x + y[0].y) + (y[1].x + y[1].y)) + ((y[2].x + y[2].y) + (y[3].x + y[3].y));
 #pragma unroll
-                            for (int q = 0; q < 4; ++q)   // (as bits: NaN is above everything)
-                                top[k] = __uint_as_float(max(__float_as_uint(top[k]), max(__float_as_uint(fabsf(y[q].x)), __float_as_uint(fabsf(y[q].y)))));
+                        for (int q = 0; q < 2; ++q) {
+                            const int piece = 2 * (part % (LR / 2)) + q;
+                            const unsigned int c01 = q ? raw[k].a.z : raw[k].a.x, c23 = q ? raw[k].a.w : raw[k].a.y;
+                            *reinterpret_cast<uint2*>(to + r * 128 + (piece >> 3) * (kTileRows * 128) + (((piece & 7) ^ (r & 7)) << 4) +
+                                                      (part >= LR / 2 ? 8 : 0)) = make_uint2(__byte_perm(c01, c23, 0x5410), __byte_perm(c01, c23, 0x7632));
                         }
-#pragma unroll
-                        for (int o = 1; o < LR; o <<= 1)
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) top[k] = __uint_as_float(max(__float_as_uint(top[k]), __shfl_xor_sync(0xFFFFFFFFu, __float_as_uint(top[k]), o)));
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const int r = row_base + rb + k * RI + lane / LR;
-                            const unsigned int bits = __float_as_uint(top[k]);
-                            const int e = max(-119, min(127, (int)(bits >> 23) - 127));
-                            const float up = kvb_pow2(7 - e);
-                            float2 y[4];
-                            raw[k].unpack(y);
-                            unsigned int hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) {
-                                const float2 z = make_float2(y[q].x * up, y[q].y * up);
-                                const unsigned int h = kvb_codes(z);
-                                const float2 v = kvb_values(h);
-                                hi[q >> 1] |= h << (16 * (q & 1));
-                                lo[q >> 1] |= kvb_codes(make_float2(z.x - v.x, z.y - v.y)) << (16 * (q & 1));
-                            }
-                            if (bits >= 0x7F800000u) hi[0] = hi[1] = 0x7F7F7F7Fu;
-                            const int chunk = part >> 1;     // of 16 channels
-                            unsigned char* at8 = to + r * 128 + 8 * (part & 1);
-                            *reinterpret_cast<uint2*>(at8 + ((chunk ^ (r & 7)) << 4)) = make_uint2(hi[0], hi[1]);
-                            *reinterpret_cast<uint2*>(at8 + (D == 64 ? ((chunk + 4) ^ (r & 7)) << 4 : kTileRows * 128 + ((chunk ^ (r & 7)) << 4))) = make_uint2(lo[0], lo[1]);
-                            if (part == 0) sh.row_q[PAIR ? x : 0][r] = a.scale_log2 * kvb_pow2(e - 7);
-                        }
-                    } else {
-                        float sum[8];
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const int r = row_base + rb + k * RI + lane / LR;
-                            if (row0 + rb + k * RI + lane / LR >= rows_here) raw[k].clear();
-                            float2 y[4];
-                            raw[k].unpack(y);
-                            sum[k] = ((y[0].x + y[0].y) + (y[1].x + y[1].y)) + ((y[2].x + y[2].y) + (y[3].x + y[3].y));
-#pragma unroll
-                            for (int q = 0; q < 2; ++q) {
-                                const int piece = 2 * (part % (LR / 2)) + q;
-                                const unsigned int c01 = q ? raw[k].a.z : raw[k].a.x, c23 = q ? raw[k].a.w : raw[k].a.y;
-                                *reinterpret_cast<uint2*>(to + r * 128 + (piece >> 3) * (kTileRows * 128) + (((piece & 7) ^ (r & 7)) << 4) +
-                                                          (part >= LR / 2 ? 8 : 0)) = make_uint2(__byte_perm(c01, c23, 0x5410), __byte_perm(c01, c23, 0x7632));
-                            }
-                        }
-#pragma unroll
-                        for (int o = 1; o < LR; o <<= 1)
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) sum[k] += __shfl_xor_sync(0xFFFFFFFFu, sum[k], o);
-#pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            if (part == 0) sh.row_q[PAIR ? x : 0][row_base + rb + k * RI + lane / LR] = sum[k];
                     }
+#pragma unroll
+                    for (int o = 1; o < LR; o <<= 1)
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) sum[k] += __shfl_xor_sync(0xFFFFFFFFu, sum[k], o);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (part == 0) sh.row_q[PAIR ? x : 0][row_base + rb + k * RI + lane / LR] = sum[k];
                 }
                 fence_async_smem();
                 __syncwarp();
@@ -869,30 +705,20 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                         for (int k = 0; k < 32; ++k) s[1][k] = 0.f;
                     }
                     const int evn = sh.ev[mslot];
-                    float ff[BITS == 8 ? 4 : 1];   // what S is to be multiplied by, row by row with 8 bits (never 0: what is hidden is -inf times it)
-                    const auto factor = [&](int q) { return ff[BITS == 8 ? q : 0]; };
-                    if constexpr (BITS == 8) {
-                        const float ks = sh.kscale[mslot];
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) ff[q] = fmaxf(qf[q] * ks, 1e-37f);
-                    } else {
-                        ff[0] = rf;
+                    for (int k = 0; k < 8; ++k) {
+                        const float4 m = sh.kmeta[mslot][4 * k + j];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const float4 m = sh.kmeta[mslot][4 * k + j];
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) {   // row g + 8 q
-                                float& s0 = s[q >> 1][4 * k + 2 * (q & 1)];
-                                float& s1 = s[q >> 1][4 * k + 2 * (q & 1) + 1];
-                                const float2 y = __ffma2_rn(make_float2(m.z, m.w), make_float2(qf[q], qf[q]), __fmul2_rn(make_float2(s0, s1), make_float2(m.x, m.y)));
-                                s0 = y.x;
-                                s1 = y.y;
-                            }
+                        for (int q = 0; q < 4; ++q) {   // row g + 8 q
+                            float& s0 = s[q >> 1][4 * k + 2 * (q & 1)];
+                            float& s1 = s[q >> 1][4 * k + 2 * (q & 1) + 1];
+                            const float2 y = __ffma2_rn(make_float2(m.z, m.w), make_float2(qf[q], qf[q]), __fmul2_rn(make_float2(s0, s1), make_float2(m.x, m.y)));
+                            s0 = y.x;
+                            s1 = y.y;
                         }
                     }
                     if (evn < 0 || (pg + 1) * kPage > open_to) {   // what a row does not see becomes -inf (lane r finds out for row r)
-                        const u64 see = evn < 0 || row0 + lane >= rows_here ? 0ull : kv_seen(a, w.cached, w.fresh, w.first, pg, token);
-                        const u64 mine = BITS == 8 ? see : tile_places(see);
+                        const u64 mine = evn < 0 || row0 + lane >= rows_here ? 0ull : tile_places(kv_seen(a, w.cached, w.fresh, w.first, pg, token));
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
                             const u64 seen = __shfl_sync(0xFFFFFFFFu, mine, g + 8 * q) >> (2 * j);
@@ -909,6 +735,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                     // and this done again.
                     float ls[4];
                     bool again = first || large;
+                    float rr = rf;             // what S is still to be multiplied by
 #pragma unroll 1
                     for (;;) {
                         if (again) {
@@ -920,17 +747,16 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                                 for (int k = 0; k < 8; ++k) m[q] = fmaxf(m[q], fmaxf(s[q >> 1][4 * k + 2 * (q & 1)], s[q >> 1][4 * k + 2 * (q & 1) + 1]));
                                 m[q] = fmaxf(m[q], __shfl_xor_sync(0xFFFFFFFFu, m[q], 1));
                                 m[q] = fmaxf(m[q], __shfl_xor_sync(0xFFFFFFFFu, m[q], 2));
-                                m[q] *= factor(q);
+                                m[q] *= rf;
                                 if (m[q] > -CUDART_INF_F) top = fmaxf(top, fabsf(m[q]));
                             }
                             large = large || __any_sync(0xFFFFFFFFu, top >= kTileLarge);
                             if (large) {
+                                rr = 1.f;
 #pragma unroll
                                 for (int half = 0; half < 2; ++half)
 #pragma unroll
-                                    for (int k = 0; k < 32; ++k) s[half][k] *= factor(2 * half + ((k >> 1) & 1));
-#pragma unroll
-                                for (float& f : ff) f = 1.f;
+                                    for (int k = 0; k < 32; ++k) s[half][k] *= rf;
                             }
 #pragma unroll
                             for (int q = 0; q < 4; ++q) {
@@ -955,11 +781,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
                                 const int q = 2 * half + e;
-                                const float2 fq = make_float2(factor(q), factor(q)), mm = make_float2(kTileP - mref[q], kTileP - mref[q]);
+                                const float2 ff = make_float2(rr, rr), mm = make_float2(kTileP - mref[q], kTileP - mref[q]);
                                 float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
                                 for (int k = 0; k < 8; ++k) {
-                                    float2 p = __ffma2_rn(make_float2(s[half][4 * k + 2 * e], s[half][4 * k + 2 * e + 1]), fq, mm);
+                                    float2 p = __ffma2_rn(make_float2(s[half][4 * k + 2 * e], s[half][4 * k + 2 * e + 1]), ff, mm);
                                     p = make_float2(ex2_approx(p.x), ex2_approx(p.y));
                                     sum = __fadd2_rn(sum, p);
                                     pk[2 * k + e] = pack_half(p.x, p.y);

@@ -2,6 +2,7 @@
 // -DAASD_DT=0 for fp32 and once with -DAASD_DT=1 for bf16).
 #include "aasd_kvb_attend.cuh"
 #include "aasd_kv_host.h"
+#include "aasd_kvb_tile.cuh"
 
 #ifndef AASD_DT
 #error "compile with -DAASD_DT=0 (fp32) or -DAASD_DT=1 (bf16)"
@@ -26,17 +27,17 @@ int launch_split(const LaunchEnv& env, int sm_count, const KvAttendArgs& a) {
 #if AASD_DT == 1
 template <int D, bool PAIR>
 int launch_tile(const LaunchEnv& env, int sm_count, const KvAttendArgs& a) {
-    constexpr auto kernel = kv_attend_tile_kernel<8, D, PAIR>;
+    constexpr auto kernel = kvb_attend_tile_kernel<D, PAIR>;
     constexpr size_t smem = sizeof(KvbTileShared<D, PAIR>) + 1024;   // (its first member wants a 1024-byte boundary)
     static_assert(smem <= 227 * 1024, "fits an SM");
     if (enable_smem<kernel, smem>(env.device) != AASD_OK) return AASD_ERR_CUDA;
     // the softmax warps wait for registers that the launch must have brought along
     static const bool enough = [] {
         cudaFuncAttributes f;
-        return cudaFuncGetAttributes(&f, kernel) == cudaSuccess && f.numRegs >= kTileLaunchRegs;
+        return cudaFuncGetAttributes(&f, kernel) == cudaSuccess && f.numRegs >= kByteLaunchRegs;
     }();
     if (!enough) return AASD_ERR_UNSUPPORTED;
-    launch(kernel, (unsigned int)(sm_count < kKvMaxCtas ? sm_count : kKvMaxCtas), (unsigned int)kTileThreads, smem, env.stream, a);
+    launch(kernel, (unsigned int)(sm_count < kKvMaxCtas ? sm_count : kKvMaxCtas), (unsigned int)kByteTileThreads, smem, env.stream, a);
     launch_grid2(kv_tile_join_kernel<D, PAIR>, (unsigned int)(sm_count < kKvMaxCtas ? sm_count : kKvMaxCtas), (PAIR ? 2u : 1u) * kTileRows / 8, 256u,
                  env.stream, a);
     return AASD_OK;
