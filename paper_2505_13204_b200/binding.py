@@ -454,7 +454,7 @@ def _kv_read_call(name, pool):
         o = outputs
         if o is None:
             shape = (n, H, head_dim)
-            o = dict(k=torch.empty(shape, dtype=dtype, device=pages.device), v=torch.empty(shape, dtype=dtype, device=pages.device))
+            o = dict(k=pages.new_empty(shape, dtype=dtype), v=pages.new_empty(shape, dtype=dtype))
         else:
             assert o["k"].get_device() == self.device_index
             _kv_like(o["k"], n * H * head_dim, o["k"], o["v"])
@@ -833,7 +833,9 @@ class Context:
         T, Hq, D = q.shape
         kv = k.shape
         Tk, Hkv, Dk = kv
-        qs, ks, vs = _kv_token_stride(q), _kv_token_stride(k), _kv_token_stride(v)
+        (qs, qh, qd), (ks, kh, kd), (vs, vh, vd) = q.stride(), k.stride(), v.stride()
+        if not (T > 1 and qh == D and kh == D and vh == D and qd == 1 and kd == 1 and vd == 1):
+            qs, ks, vs = _kv_token_stride(q), _kv_token_stride(k), _kv_token_stride(v)
         dt = q.dtype
         B, P = block_table.shape
         N, Hp, Dp = _kvb_pool(pages, 3, dev)
@@ -862,9 +864,12 @@ class Context:
             one = KvbWriteParams(rows, B, P, int(rows_per_seq))
             prm = self._kv_structs[key] = (C.byref(one), one)
         ko = o.get("k")
-        rc = self.lib.aasd_kvb_write(self._h, q.data_ptr(), k.data_ptr(), v.data_ptr(), _p(q_weight), _p(k_weight), _p(cos_sin),
-                                     positions.data_ptr(), block_table.data_ptr(), cached_len.data_ptr(), kv_len.data_ptr(), _p(tok_offsets),
-                                     T, prm[0], pages.data_ptr(), o["q"].data_ptr(), _p(ko))
+        rc = self.lib.aasd_kvb_write(self._h, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                     None if q_weight is None else q_weight.data_ptr(),
+                                     None if k_weight is None else k_weight.data_ptr(),
+                                     None if cos_sin is None else cos_sin.data_ptr(), positions.data_ptr(), block_table.data_ptr(),
+                                     cached_len.data_ptr(), kv_len.data_ptr(), None if tok_offsets is None else tok_offsets.data_ptr(),
+                                     T, prm[0], pages.data_ptr(), o["q"].data_ptr(), None if ko is None else ko.data_ptr())
         if rc:
             raise AasdError(rc, "aasd_kvb_write")
         return o
@@ -898,7 +903,9 @@ class Context:
         B, P, N, prm, books = self._kv_books(block_table, seq_pages, free_pages, n_free, page_shares)
         _kv_i32(self.device_index, keep_len, n_new)
         _kv_need(keep_len.numel() >= B and (n_new is None or n_new.numel() >= B), "lengths of kv_free's arrays")
-        _check(self.lib.aasd_kv_free(self._h, keep_len.data_ptr(), _p(n_new), prm, C.byref(books)), "aasd_kv_free")
+        rc = self.lib.aasd_kv_free(self._h, keep_len.data_ptr(), None if n_new is None else n_new.data_ptr(), prm, C.byref(books))
+        if rc:
+            raise AasdError(rc, "aasd_kv_free")
 
     def kv_fork(self, pages, src_seq, dst_seq, block_table, seq_pages, cached_len, free_pages, n_free, page_shares, fork_len=None, outputs=None):
         """aasd_kv_fork: every sequence ``dst_seq[i]``, which holds no pages, becomes the first ``fork_len[i]`` cached tokens (None: all)
@@ -908,15 +915,20 @@ class Context:
         n = src_seq.numel()
         o = outputs
         if o is None:
-            new = src_seq.new_empty
-            o = dict(new_len=new(n), copy_src=new(n), copy_dst=new(n))
-        _kv_i32(self.device_index, src_seq, dst_seq, cached_len, fork_len, o["new_len"], o["copy_src"], o["copy_dst"])
-        _kv_need(dst_seq.numel() == n and cached_len.numel() >= B and (fork_len is None or fork_len.numel() >= n) and
-                 all(o[x].numel() >= n for x in ("new_len", "copy_src", "copy_dst")), "lengths of kv_fork's arrays")
+            new_len, copy_src, copy_dst = src_seq.new_empty((3, n)).unbind()
+            o = dict(new_len=new_len, copy_src=copy_src, copy_dst=copy_dst)
+        else:
+            new_len, copy_src, copy_dst = o["new_len"], o["copy_src"], o["copy_dst"]
+            _kv_i32(self.device_index, new_len, copy_src, copy_dst)
+            _kv_need(new_len.numel() >= n and copy_src.numel() >= n and copy_dst.numel() >= n, "outputs")
+        _kv_i32(self.device_index, src_seq, dst_seq, cached_len, fork_len)
+        _kv_need(dst_seq.numel() == n and cached_len.numel() >= B and (fork_len is None or fork_len.numel() >= n), "lengths of kv_fork's arrays")
         pool = self._kv_layers(pages, N)
-        out = KvForkOut(o["new_len"].data_ptr(), o["copy_src"].data_ptr(), o["copy_dst"].data_ptr())
-        _check(self.lib.aasd_kv_fork(self._h, src_seq.data_ptr(), dst_seq.data_ptr(), _p(fork_len), n, prm, C.byref(books),
-                                     cached_len.data_ptr(), C.byref(pool), C.byref(out)), "aasd_kv_fork")
+        out = KvForkOut(new_len.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr())
+        rc = self.lib.aasd_kv_fork(self._h, src_seq.data_ptr(), dst_seq.data_ptr(), None if fork_len is None else fork_len.data_ptr(), n, prm,
+                                   C.byref(books), cached_len.data_ptr(), C.byref(pool), C.byref(out))
+        if rc:
+            raise AasdError(rc, "aasd_kv_fork")
         return o
 
     def kv_copy(self, pages, src, dst):
@@ -932,15 +944,16 @@ class Context:
         B, P, N, prm, books = self._kv_books(block_table, seq_pages, free_pages, n_free, page_shares)
         o = outputs
         if o is None:
-            o = dict(page_map=free_pages.new_empty(N), n_moved=free_pages.new_empty(1))
+            page_map, n_moved, moves = free_pages.new_empty(2 * N + 1).split((N, 1, N))
+            o = dict(page_map=page_map, n_moved=n_moved)
         else:
-            _kv_i32(self.device_index, o["page_map"], o["n_moved"])
-            _kv_need(o["page_map"].numel() >= N and o["n_moved"].numel() > 0, "outputs")
-        with torch.cuda.stream(self.stream):
-            moves = free_pages.new_empty(N)
+            page_map, n_moved, moves = o["page_map"], o["n_moved"], free_pages.new_empty(N)
+            _kv_i32(self.device_index, page_map, n_moved)
+            _kv_need(page_map.numel() >= N and n_moved.numel() > 0, "outputs")
         pool = self._kv_layers(pages, N)
-        _check(self.lib.aasd_kv_compact(self._h, prm, C.byref(books), C.byref(pool), o["page_map"].data_ptr(), moves.data_ptr(),
-                                        o["n_moved"].data_ptr()), "aasd_kv_compact")
+        rc = self.lib.aasd_kv_compact(self._h, prm, C.byref(books), C.byref(pool), page_map.data_ptr(), moves.data_ptr(), n_moved.data_ptr())
+        if rc:
+            raise AasdError(rc, "aasd_kv_compact")
         return o
 
     def select(self, accept_len, next_token, draft_ids, emit_stride, cand_offsets=None,

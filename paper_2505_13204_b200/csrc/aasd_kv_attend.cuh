@@ -457,24 +457,34 @@ __device__ __forceinline__ void kv_split_join(const KvAttendArgs& a, Shared& sh,
 #pragma unroll
             for (int i = 0; i < RB; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
             unsigned int left = group;
+#pragma unroll 1
             while (left) {
-                const int k = __ffs(left) - 1;
-                left &= left - 1;
-                const float* from = (k & 1) ? reinterpret_cast<const float*>(sh.ring[k >> 1][0])
-                                            : a.warp_parts + (long long)(c * W + (k >> 1)) * (R * TS);
-                float4 x[RB];
+                constexpr int NB = RB == 1 ? 4 : 1;   // pieces whose loads are under way together
+                int k[NB];
+                float4 x[NB][RB];
 #pragma unroll
-                for (int i = 0; i < RB; ++i) {
-                    x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (on) x[i] = *reinterpret_cast<const float4*>(from + min(r0 + i, pc.n - 1) * TS + ch);
+                for (int b = 0; b < NB; ++b) {
+                    k[b] = left ? __ffs(left) - 1 : -1;
+                    left &= left - 1;
+                    const float* from = (k[b] & 1) ? reinterpret_cast<const float*>(sh.ring[k[b] >> 1][0])
+                                                   : a.warp_parts + (long long)(c * W + (k[b] >> 1)) * (R * TS);
+#pragma unroll
+                    for (int i = 0; i < RB; ++i) {
+                        x[b][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        if (on && k[b] >= 0) x[b][i] = *reinterpret_cast<const float4*>(from + min(r0 + i, pc.n - 1) * TS + ch);
+                    }
                 }
 #pragma unroll
-                for (int i = 0; i < RB; ++i) {
-                    const float fk = __shfl_sync(0xFFFFFFFFu, f[i], k);
-                    o[i].x = fmaf(x[i].x, fk, o[i].x);
-                    o[i].y = fmaf(x[i].y, fk, o[i].y);
-                    o[i].z = fmaf(x[i].z, fk, o[i].z);
-                    o[i].w = fmaf(x[i].w, fk, o[i].w);
+                for (int b = 0; b < NB; ++b) {
+                    if (NB > 1 && k[b] < 0) break;
+#pragma unroll
+                    for (int i = 0; i < RB; ++i) {
+                        const float fk = __shfl_sync(0xFFFFFFFFu, f[i], k[b]);
+                        o[i].x = fmaf(x[b][i].x, fk, o[i].x);
+                        o[i].y = fmaf(x[b][i].y, fk, o[i].y);
+                        o[i].z = fmaf(x[b][i].z, fk, o[i].z);
+                        o[i].w = fmaf(x[b][i].w, fk, o[i].w);
+                    }
                 }
             }
 #pragma unroll
@@ -493,7 +503,8 @@ __device__ __forceinline__ void kv_split_join(const KvAttendArgs& a, Shared& sh,
             }
         }
     };
-    const bool few = __popc(starts) * 2 < W;   // few groups: a row per warp, else four rows at a time
+    // few rows: one per warp, else four at a time
+    const bool few = __reduce_add_sync(0xFFFFFFFFu, (starts >> lane) & 1u ? (unsigned int)sh.piece[lane].n : 0u) <= (unsigned int)W;
     int done = 0;                              // row batches dealt with so far, modulo W
     while (starts) {
         const int p = __ffs(starts) - 1;

@@ -7,6 +7,9 @@ using namespace aasd;
 
 namespace {
 
+// Sequences up to which the collecting CTA goes through the tables itself.
+constexpr int kDropInline = 64;
+
 int check_books(const aasd_kv_books_params* p, const aasd_kv_books* k) {
     if (p == nullptr || k == nullptr) return AASD_ERR_INVALID_ARG;
     if (p->n_seqs < 0 || p->n_pages < 0 || p->n_pages > 0x7FFFFFFF / kPage || p->max_pages < 1 || p->max_pages > 0x7FFFFFFF / kPage) return AASD_ERR_BAD_SHAPE;
@@ -44,8 +47,12 @@ int aasd_kv_free(aasd_ctx* ctx, const int32_t* keep_len, const int32_t* n_new, c
     if (!keep_len) return AASD_ERR_INVALID_ARG;
     KvFreeArgs a{keep_len, n_new, *k, *p, ctx->state};
     AASD_CUDA(cudaSetDevice(ctx->device));
+    if (p->n_seqs <= kDropInline) {
+        launch(kv_collect_kernel<true>, 1u, (unsigned int)kShareThreads, 0, ctx->stream, a);
+        return after_launch(ctx, 1);
+    }
     launch(kv_drop_kernel, (unsigned int)((p->n_seqs + 7) / 8), 256u, 0, ctx->stream, a);
-    launch(kv_collect_kernel, 1u, (unsigned int)kShareThreads, 0, ctx->stream, a);
+    launch(kv_collect_kernel<false>, 1u, (unsigned int)kShareThreads, 0, ctx->stream, a);
     return after_launch(ctx, 2);
 }
 

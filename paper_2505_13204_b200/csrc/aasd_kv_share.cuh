@@ -26,15 +26,11 @@ struct KvFreeArgs {
     DeviceState* state;
 };
 
-// A warp per sequence: the table's entries past what is kept go, and each takes a holder off its page.
-__global__ void __launch_bounds__(256) kv_drop_kernel(const KvFreeArgs a) {
-    pdl_launch_dependents();
-    pdl_wait();
-    const int b = (int)((blockIdx.x * 256u + threadIdx.x) >> 5), lane = threadIdx.x & 31;
-    if (b >= a.p.n_seqs) return;
-    const int keep = a.keep_len[b], held = a.k.seq_pages[b];
+// A warp takes a sequence: the table's entries past what is kept go, and each takes a holder off its page.
+__device__ __forceinline__ void kv_drop(const KvFreeArgs& a, int b) {
+    const int lane = threadIdx.x & 31;
+    const int keep = a.keep_len[b], held = a.k.seq_pages[b], fresh = a.n_new ? a.n_new[b] : 0;
     if (keep == AASD_NONE) return;
-    const int fresh = a.n_new ? a.n_new[b] : 0;
     if (keep < 0 || fresh < 0 || held < 0 || held > a.p.max_pages) {
         if (lane == 0) raise(a.state, AASD_STATUS_BAD_OFFSETS);
         return;
@@ -50,12 +46,24 @@ __global__ void __launch_bounds__(256) kv_drop_kernel(const KvFreeArgs a) {
     }
     if (lane == 0) a.k.seq_pages[b] = (int)need;
 }
+__global__ void __launch_bounds__(256) kv_drop_kernel(const KvFreeArgs a) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int b = (int)((blockIdx.x * 256u + threadIdx.x) >> 5);
+    if (b < a.p.n_seqs) kv_drop(a, b);
+}
 
 // One CTA: pages without a holder go on the stack, in order of their numbers (whatever order the atomics came in).
+// DROP: a small batch's tables are gone through first, without a launch of their own.
+template <bool DROP>
 __global__ void __launch_bounds__(kShareThreads) kv_collect_kernel(const KvFreeArgs a) {
     __shared__ long long s_warp[kShareThreads / 32];
     pdl_launch_dependents();
     pdl_wait();
+    if (DROP) {
+        for (int b = (int)threadIdx.x >> 5; b < a.p.n_seqs; b += kShareThreads / 32) kv_drop(a, b);
+        __syncthreads();
+    }
     unsigned int bits = 0;
     const int N = a.p.n_pages;
     long long n = kv_free_count(a.k.n_free, N, bits);
@@ -64,7 +72,7 @@ __global__ void __launch_bounds__(kShareThreads) kv_collect_kernel(const KvFreeA
         int v[kShareEach], mine = 0;
 #pragma unroll
         for (int e = 0; e < kShareEach; ++e) {
-            v[e] = first + e < N ? a.k.page_shares[first + e] : 0;
+            v[e] = first + e < N ? __ldcg(a.k.page_shares + first + e) : 0;   // (the atomics' own level)
             mine += v[e] < 0;
             if (v[e] < -1) bits |= AASD_STATUS_BAD_OFFSETS;      // listed more often than it had holders
         }

@@ -87,8 +87,9 @@ struct KvbUnit {
 // W warps store the rows of one page, head and half (a unit): they are normed and rotated (keys), the largest magnitude
 // gives the page's scale, and the codes follow.  Rows of a page that fit the unit's registers are held between the two,
 // others are made again.  Queries are rows of their own (D / 16 lanes each), as in the 4-bit store.
+constexpr int kWriteCtas = 3;
 template <int DT, int D, bool VEC, bool FULL, int W>
-__global__ void __launch_bounds__(kByteThreads) kvb_write_kernel(const KvbWriteArgs a) {
+__global__ void __launch_bounds__(kByteThreads, D == 256 ? 1 : kWriteCtas) kvb_write_kernel(const KvbWriteArgs a) {
     constexpr int L = D / 16, H = D / 2;
     constexpr int T = 32 * W, U = kByteThreads / T;      // threads of a unit, units of a CTA
     constexpr int kRows = T / L;                         // rows of a pass

@@ -40,6 +40,7 @@ struct KvbSplitShared {
     static constexpr int R = 8 * NT;
     alignas(128) unsigned char ring[Sh::W][Sh::S][Sh::kBlock];
     int base[Sh::kThreads];
+    KvSeq seq[Sh::kThreads];           // batches up to the number of threads: what the scan has loaded
     long long scan[Sh::W];
     KvSegment seg[Sh::W][Sh::S + 1];   // of the blocks on their way, and the one being worked on
     KvPiece piece[2 * Sh::W];
@@ -94,6 +95,7 @@ __global__ void __launch_bounds__(KvbSplitShape<DT, D, NT>::kThreads, 1) kvb_att
 #pragma unroll 1
     for (int b = tid * strip; b < min(B, (tid + 1) * strip); ++b) {
         const KvSeq s = kv_load_seq<TB>(a, b, R);
+        if (strip == 1) sh.seq[b] = s;
         mine += kv_units(a, s);
         padding = padding || kv_has_padding(a, s, b);
         if (s.fresh > 0 && (long long)s.cached + s.fresh > (long long)a.p.max_pages * kPage) raise(a.state, AASD_STATUS_BAD_OFFSETS);
@@ -122,9 +124,10 @@ __global__ void __launch_bounds__(KvbSplitShape<DT, D, NT>::kThreads, 1) kvb_att
                 else hi = mid;
             }
             int rem = u0 - sh.base[lo], b = lo * strip;
-            KvSeq s = kv_load_seq<TB>(a, b, R);
+            const auto load = [&](int k) { return strip == 1 ? sh.seq[k] : kv_load_seq<TB>(a, k, R); };
+            KvSeq s = load(b);
 #pragma unroll 1
-            for (int n; rem >= (n = (int)kv_units(a, s)); s = kv_load_seq<TB>(a, ++b, R)) rem -= n;
+            for (int n; rem >= (n = (int)kv_units(a, s)); s = load(++b)) rem -= n;
             ahead.seek(a, b, s, rem, u0);
         }
         unsigned int missing = 0;   // bit s: stage s holds no block (the table names no page)

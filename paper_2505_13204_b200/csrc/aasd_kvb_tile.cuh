@@ -52,7 +52,7 @@ struct KvbTileShared {
     KvPiece open;                      // the segment that begins in this CTA and ends in another
     u64 piece_full[kTilePieces], piece_empty[kTilePieces];
     u64 raw_full[kByteRaw], raw_empty[kByteRaw];
-    u64 scale_full[kByteScales], scale_empty[kByteScales];
+    u64 scale_empty[kByteScales];
     u64 v_full[kByteValues], v_empty[kByteValues];
     u64 q_full[2], s_full[2][2], p_full[2][2], o_done[2][2], x_full, x_empty, r_full, drain[2];
     unsigned int tmem;
@@ -75,13 +75,34 @@ struct KvRing {
     }
 };
 
-// D (fp32, tensor memory) (+)= A B, e4m3 both, in shared memory
-__device__ __forceinline__ void tc_mma_bytes(unsigned int d, u64 a, u64 b, unsigned int idesc, bool add) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(add ? 1u : 0u)
-        : "memory");
+// The issuers run as whole warps, whose values the compiler can see to be the same in every lane and keep in uniform registers,
+// where the tensor-core instructions want them; a lane is elected for each.  Eight products take 118 cycles to
+// issue so, and 410 from one thread inside a branch, which set the pace of the whole kernel (2 x 2048 chunk 225 us with it).
+__device__ __forceinline__ bool elect_one() {
+    unsigned int on;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(on));
+    return on != 0;
+}
+// D (fp32, tensor memory) (+)= A B, e4m3 both, in shared memory.  Operands: low and high words of their descriptors.
+__device__ __forceinline__ void tc_mma_bytes(unsigned int d, unsigned int a, unsigned int a_high, unsigned int b, unsigned int b_high, unsigned int idesc, bool add) {
+    if (elect_one())
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tsetp.ne.u32 p, %6, 0;\n\tmov.b64 x, {%1, %2};\n\tmov.b64 y, {%3, %4};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], x, y, %5, p;\n\t}" ::"r"(d),
+            "r"(a), "r"(a_high), "r"(b), "r"(b_high), "r"(idesc), "r"(add ? 1u : 0u)
+            : "memory");
+}
+// ... A B, fp16 both, A in tensor memory
+__device__ __forceinline__ void tc_mma_halves(unsigned int d, unsigned int a, unsigned int b, unsigned int b_high, unsigned int idesc, bool add) {
+    if (elect_one())
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.b64 y, {%2, %3};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %4, p;\n\t}" ::"r"(d),
+            "r"(a), "r"(b), "r"(b_high), "r"(idesc), "r"(add ? 1u : 0u)
+            : "memory");
+}
+__device__ __forceinline__ void tc_commit_one(unsigned int bar) {
+    if (elect_one()) asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 // (e4m3 is type 0 of its kind, as fp16 is of the other: tc_idesc(n, false) describes both.)
 constexpr unsigned int kTcRowsB = 1u << 16;   // the second operand's rows run along K
@@ -143,7 +164,6 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
         }
 #pragma unroll 1
         for (int i = 0; i < kByteScales; ++i) {
-            mbar_init(&sh.scale_full[i], 1);
             mbar_init(&sh.scale_empty[i], PAIR ? kByteSoftmax : kByteSoftmax / 2);
         }
 #pragma unroll 1
@@ -155,7 +175,7 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.q_full[i], kByteSoftmax / 2);
             for (int b = 0; b < 2; ++b) {
-                mbar_init(&sh.s_full[i][b], 1);
+                mbar_init(&sh.s_full[i][b], 2);    // the products' end, and the issuer's word
                 mbar_init(&sh.p_full[i][b], kByteSoftmax / 2);
                 mbar_init(&sh.o_done[i][b], 1);
             }
@@ -235,14 +255,12 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
                         sh.raw_missing[raw.slot] = sh.missing[sc.slot] = !there;
                         if (there) {
                             const uint8_t* from = head + (u64)(unsigned int)page * stride;
-                            mbar_arrive_expect_tx(&sh.raw_full[raw.slot], 2 * kPage * D);
+                            mbar_arrive_expect_tx(&sh.raw_full[raw.slot], 2 * kPage * D + 16);
                             bulk_copy_g2s(sh.raw[raw.slot], from, 2 * kPage * D, &sh.raw_full[raw.slot]);
-                            mbar_arrive_expect_tx(&sh.scale_full[sc.slot], 16);
-                            bulk_copy_g2s(&sh.scale[sc.slot], from + kvb_scale_offset(D), 16, &sh.scale_full[sc.slot]);
+                            bulk_copy_g2s(&sh.scale[sc.slot], from + kvb_scale_offset(D), 16, &sh.raw_full[raw.slot]);
                         } else {
                             raise(a.state, AASD_STATUS_BAD_OFFSETS);
                             mbar_arrive(&sh.raw_full[raw.slot]);
-                            mbar_arrive(&sh.scale_full[sc.slot]);
                         }
                     }
                     __syncwarp();
@@ -254,74 +272,74 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
             for (int k = max(0, n - kByteRaw); k < n; ++k)
 #pragma unroll 1
                 for (unsigned int it = 0; it < a.wait_limit && !mbar_try_wait(&sh.raw_full[k % kByteRaw], (k / kByteRaw) & 1); ++it) {}
-#pragma unroll 1
-            for (int k = max(0, n - kByteScales); k < n; ++k)
-#pragma unroll 1
-                for (unsigned int it = 0; it < a.wait_limit && !mbar_try_wait(&sh.scale_full[k % kByteScales], (k / kByteScales) & 1); ++it) {}
         } else {
             // ---- issuers, one for each group
-            if (lane == 0) {
-                const int x = (warp - kByteSoftmax - 4) >> 1;
-                // A piece's pages of the group: all, or every other page of the share.  The keys' products run up to two
-                // pages ahead, but not into the next piece: its queries come when this one's last page is in O.
-                KvRing<kByteRaw> raw;
-                KvRing<kByteValues> val;
-                if (!PAIR && x == 1) {
-                    raw.next();
-                    val.next();
-                }
-                int n0 = 0, taken = 0;   // pages of the share before the piece; of the group so far
+            const int x = __shfl_sync(0xFFFFFFFFu, (warp - kByteSoftmax - 4) >> 1, 0);
+            const unsigned int tmem = __shfl_sync(0xFFFFFFFFu, tm, 0) + x * kStep;
+            const auto low = [](u64 desc) { return (unsigned int)desc; };
+            const auto high = [](u64 desc) { return (unsigned int)(desc >> 32); };
+            const unsigned int q0 = low(tc_desc(smem_u32(sh.queries[0]))) + (PAIR ? x * (kTileRows * D * 2 / 16) : 0), q_high = high(tc_desc(0));
+            const unsigned int k0 = low(D == 64 ? tc_desc_64(smem_u32(sh.raw[0])) : tc_desc(smem_u32(sh.raw[0]))), k_high = high(D == 64 ? tc_desc_64(0) : tc_desc(0));
+            const unsigned int v0 = low(tc_desc_rows(smem_u32(sh.values[0]))), v_high = high(tc_desc_rows(0));
+            // A piece's pages of the group: all, or every other page of the share.  The keys' products run up to two
+            // pages ahead, but not into the next piece: its queries come when this one's last page is in O.
+            KvRing<kByteRaw> raw;
+            KvRing<kByteValues> val;
+            if (!PAIR && x == 1) {
+                raw.next();
+                val.next();
+            }
+            int n0 = 0, taken = 0;   // pages of the share before the piece; of the group so far
 #pragma unroll 1
-                for (int k = 0;; ++k) {
-                    ok = wait_one(&sh.piece_full[k % kTilePieces], (k / kTilePieces) & 1);
-                    if (!ok) break;
-                    const int np = sh.piece[k % kTilePieces].np;
-                    if (np == 0) break;
-                    mbar_arrive(&sh.piece_empty[k % kTilePieces]);
-                    ok = wait_one(&sh.q_full[x], k & 1);
-                    if (!ok) break;
-                    const u64 q = tc_desc(smem_u32(sh.queries[PAIR ? x : 0]));
-                    const int first = PAIR ? 0 : (n0 ^ x) & 1;
-                    int ahead = first, asked = taken;
+            for (int k = 0;; ++k) {
+                ok = wait(&sh.piece_full[k % kTilePieces], (k / kTilePieces) & 1);
+                if (!ok) break;
+                const int np = __shfl_sync(0xFFFFFFFFu, sh.piece[k % kTilePieces].np, 0);
+                if (np == 0) break;
+                if (elect_one()) mbar_arrive(&sh.piece_empty[k % kTilePieces]);
+                ok = wait(&sh.q_full[x], k & 1);
+                if (!ok) break;
+                const int first = PAIR ? 0 : (n0 ^ x) & 1;
+                int ahead = first, asked = taken;
 #pragma unroll 1
-                    for (int i = first; i < np; i += STEP, ++taken) {
+                for (int i = first; i < np; i += STEP, ++taken) {
 #pragma unroll 1
-                        for (; ahead < np && asked < taken + 2; ahead += STEP, ++asked) {
-                            const int buf = asked & 1;
-                            ok = wait_one(&sh.raw_full[raw.slot], raw.round);
-                            if (!ok) break;
-                            tc_fence_after();
-                            const unsigned int at = smem_u32(sh.raw[raw.slot]);
-                            const u64 keys = D == 64 ? tc_desc_64(at) : tc_desc(at);
-#pragma unroll
-                            for (int ks = 0; ks < 2 * (D / 32); ++ks) {   // (the queries' first numbers, then their second ones; descriptors count 16 bytes)
-                                const int second = ks / (D / 32), j = ks % (D / 32);
-                                tc_mma_bytes(tm + kColS + x * kStep + buf * 64, q + second * (D == 64 ? 4 : kTileRows * 8) + j * 2, keys + j * 2, kIdescS, ks > 0);
-                            }
-                            tc_commit(&sh.s_full[x][buf]);
-                            tc_commit(&sh.raw_empty[raw.slot]);
-                            raw.next(STEP);
-                        }
-                        const int buf = taken & 1;
-                        ok = ok && wait_one(&sh.v_full[val.slot], val.round) && wait_one(&sh.p_full[x][buf], (taken >> 1) & 1);
+                    for (; ahead < np && asked < taken + 2; ahead += STEP, ++asked) {
+                        const unsigned int buf = asked & 1;
+                        ok = wait(&sh.raw_full[raw.slot], raw.round);
                         if (!ok) break;
                         tc_fence_after();
-                        const u64 v = tc_desc_rows(smem_u32(sh.values[val.slot]));
+                        const unsigned int keys = k0 + raw.slot * (2 * kPage * D / 16), to = tmem + kColS + buf * 64;
 #pragma unroll
-                        for (int ks = 0; ks < kPage / 16; ++ks)   // (16 rows are 2048 bytes)
-                            tc_mma(tm + kColO + x * kStep, tm + kColS + x * kStep + buf * 64 + ks * 8, v + ks * 128, kIdescO, i > first || ks > 0);
-                        tc_commit(&sh.v_empty[val.slot]);
-                        tc_commit(&sh.o_done[x][buf]);
-                        val.next(STEP);
+                        for (int ks = 0; ks < 2 * (D / 32); ++ks) {   // (the queries' first numbers, then their second ones; descriptors count 16 bytes)
+                            const int second = ks / (D / 32), j = ks % (D / 32);
+                            tc_mma_bytes(to, q0 + second * (D == 64 ? 4 : kTileRows * 8) + j * 2, q_high, keys + j * 2, k_high, kIdescS, ks > 0);
+                        }
+                        tc_commit_one(smem_u32(&sh.s_full[x][buf]));
+                        tc_commit_one(smem_u32(&sh.raw_empty[raw.slot]));
+                        // (the softmax warps look at no other barrier: what came with the page's codes is theirs too)
+                        if (elect_one()) mbar_arrive(&sh.s_full[x][buf]);
+                        raw.next(STEP);
                     }
+                    const unsigned int buf = taken & 1;
+                    ok = ok && together(wait_one(&sh.v_full[val.slot], val.round) && wait_one(&sh.p_full[x][buf], (taken >> 1) & 1));
                     if (!ok) break;
-                    n0 += np;
+                    tc_fence_after();
+                    const unsigned int v = v0 + val.slot * (kPage * D * 2 / 16);
+#pragma unroll
+                    for (int ks = 0; ks < kPage / 16; ++ks)   // (16 rows are 2048 bytes)
+                        tc_mma_halves(tmem + kColO, tmem + kColS + buf * 64 + ks * 8, v + ks * 128, v_high, kIdescO, i > first || ks > 0);
+                    tc_commit_one(smem_u32(&sh.v_empty[val.slot]));
+                    tc_commit_one(smem_u32(&sh.o_done[x][buf]));
+                    val.next(STEP);
                 }
-                // products in flight read this CTA's shared memory
-                tc_commit(&sh.drain[x]);
-#pragma unroll 1
-                for (unsigned int it = 0; it < a.wait_limit && !mbar_try_wait(&sh.drain[x], 0); ++it) {}
+                if (!ok) break;
+                n0 += np;
             }
+            // products in flight read this CTA's shared memory
+            tc_commit_one(smem_u32(&sh.drain[x]));
+#pragma unroll 1
+            for (unsigned int it = 0; it < a.wait_limit && !mbar_try_wait(&sh.drain[x], 0); ++it) {}
             __syncwarp();
         }
     } else if (warp >= kByteSoftmax) {
@@ -500,19 +518,12 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
             for (int i = PAIR ? 0 : (n0 ^ x) & 1; i < np; i += STEP) {
                 const int pg = w.pg + i, buf = taken & 1;
                 const unsigned int col = col_s + buf * 64;
-                ok = wait(&sh.scale_full[sc.slot], sc.round);
-                if (!ok) break;
-                const uint2 scale = *reinterpret_cast<const uint2*>(&sh.scale[sc.slot]);
-                const bool missing = sh.missing[sc.slot] != 0;
-                const int ep = missing ? 0 : kvb_exponent(scale.y) + 127;
-                const float ks = missing ? 1.f : kvb_pow2(kvb_exponent(scale.x));
-                float ff[Q];              // what S is to be multiplied by (never 0: what is hidden is -inf times it)
-#pragma unroll
-                for (int q = 0; q < Q; ++q) ff[q] = fmaxf(qf[q] * ks, 1e-37f);
-                ok = wait(&sh.s_full[x][buf], (taken >> 1) & 1);
+                ok = wait(&sh.s_full[x][buf], (taken >> 1) & 1);   // (the page's scales came with its codes)
                 if (!ok) break;
                 if (halves > 0) {
                     tc_fence_after();
+                    const uint2 scale = *reinterpret_cast<const uint2*>(&sh.scale[sc.slot]);
+                    const bool missing = sh.missing[sc.slot] != 0;
                     float s[H][32];       // rows g (s[0][4 k], s[0][4 k + 1]) and g + 8; g + 16 and g + 24
                     if (halves == H) {
                         tc_load(col, s);
@@ -521,6 +532,11 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
 #pragma unroll
                         for (int k = 0; k < 32; ++k) s[H - 1][k] = 0.f;
                     }
+                    const int ep = missing ? 0 : kvb_exponent(scale.y) + 127;
+                    const float ks = missing ? 1.f : kvb_pow2(kvb_exponent(scale.x));
+                    float ff[Q];          // what S is to be multiplied by (never 0: what is hidden is -inf times it)
+#pragma unroll
+                    for (int q = 0; q < Q; ++q) ff[q] = fmaxf(qf[q] * ks, 1e-37f);
                     if (missing || (pg + 1) * kPage > open_to) {   // what a row does not see becomes -inf (lane r finds out for row r)
                         const u64 mine = missing || row0 + (lane & (16 * H - 1)) >= rows_here ? 0ull : kv_seen(a, w.cached, w.fresh, w.first, pg, own_row() / G);
 #pragma unroll
