@@ -25,8 +25,11 @@ __host__ __device__ constexpr int kvb_chunk_offset(int D, int t, int chunk) {
 }
 
 __device__ __forceinline__ float kvb_pow2(int e) { return __uint_as_float((unsigned int)(e + 127) << 23); }   // -126 <= e <= 127
-// Exponent of a stored scale.  (What a page holds that was never written is held to the range.)
-__device__ __forceinline__ int kvb_exponent(unsigned int scale) { return max(kByteLeast, min(kByteMost, (int)((scale >> 23) & 255u) - 127)); }
+// A stored scale, and its exponent.  (What a page holds that was never written is held to the range.)
+__device__ __forceinline__ unsigned int kvb_scale_bits(unsigned int scale) {
+    return min(max(scale & 0x7F800000u, (unsigned int)(kByteLeast + 127) << 23), (unsigned int)(kByteMost + 127) << 23);
+}
+__device__ __forceinline__ int kvb_exponent(unsigned int scale) { return (int)(kvb_scale_bits(scale) >> 23) - 127; }
 // Least exponent e >= -64 with top <= 448 * 2^e = 1.75 * 2^(e + 8); top: bits of a finite magnitude.
 __device__ __forceinline__ int kvb_fit(unsigned int top) { return max(kByteLeast, (int)(top >> 23) - 127 - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0)); }
 

@@ -214,9 +214,9 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
     const int c = blockIdx.x, total = kv_total(a, sum);
     // Waits are bounded; a role that gives up says so when it leaves, and the others find out in theirs.
     const auto wait_one = [&](u64* bar, unsigned int parity) { return kv_wait(a, bar, parity, abort_flag); };
-    // (the lanes of a warp go on, or give up, together)
+    // (The lanes of a warp go on, or give up, together.  What is there already costs one look.)
     const auto together = [](bool on) { return __all_sync(0xFFFFFFFFu, on) != 0; };
-    const auto wait = [&](u64* bar, unsigned int parity) { return together(wait_one(bar, parity)); };
+    const auto wait = [&](u64* bar, unsigned int parity) { return together(mbar_try_wait(bar, parity)) || together(wait_one(bar, parity)); };
     bool ok = true;
 
     if (warp >= kByteSoftmax + 4) {
@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
                 for (int i = 0; i < np; ++i, ++n, raw.next(), sc.next()) {
                     if ((i & 31) == 0) ids = i + lane < np && inside ? table[i + lane] : -1;
                     const int page = __shfl_sync(0xFFFFFFFFu, ids, i & 31);
-                    ok = together(wait_one(&sh.raw_empty[raw.slot], raw.round ^ 1u) && wait_one(&sh.scale_empty[sc.slot], sc.round ^ 1u));
+                    ok = wait(&sh.raw_empty[raw.slot], raw.round ^ 1u) && wait(&sh.scale_empty[sc.slot], sc.round ^ 1u);
                     if (!ok) break;
                     if (lane == 0) {
                         const bool there = page >= 0 && page < a.p.n_pages;
@@ -322,7 +322,7 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
                         raw.next(STEP);
                     }
                     const unsigned int buf = taken & 1;
-                    ok = ok && together(wait_one(&sh.v_full[val.slot], val.round) && wait_one(&sh.p_full[x][buf], (taken >> 1) & 1));
+                    ok = ok && wait(&sh.v_full[val.slot], val.round) && wait(&sh.p_full[x][buf], (taken >> 1) & 1);
                     if (!ok) break;
                     tc_fence_after();
                     const unsigned int v = v0 + val.slot * (kPage * D * 2 / 16);
@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
             if (lane == 0) mbar_arrive(&sh.piece_empty[k % kTilePieces]);
 #pragma unroll 1
             for (int i = 0; i < np; ++i, raw.next(), val.next()) {
-                ok = together(wait_one(&sh.raw_full[raw.slot], raw.round) && wait_one(&sh.v_empty[val.slot], val.round ^ 1u));
+                ok = wait(&sh.raw_full[raw.slot], raw.round) && wait(&sh.v_empty[val.slot], val.round ^ 1u);
                 if (!ok) break;
                 const unsigned char* src = sh.raw[raw.slot] + from;
                 unsigned char* to = sh.values[val.slot];
@@ -402,8 +402,7 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
         const int x = warp / (kByteSoftmax / 2), g = lane >> 2, j = lane & 3, row_base = (warp & 3) * 32 + (H == 1 ? ((warp >> 2) & 1) * 16 : 0);   // (of the group's 128 rows)
         const unsigned int lanes = (unsigned int)row_base << 16;
         const unsigned int col_s = tm + kColS + x * kStep + lanes, col_o = tm + kColO + x * kStep + lanes;
-        KvRing<kByteScales> sc;
-        if (!PAIR && x == 1) sc.next();
+        static_assert((kByteScales & (kByteScales - 1)) == 0, "a slot is a page's number, cut off");
         int n0 = 0, taken = 0;    // pages of the share before the piece; of the group so far
         // All pages taken so far are in O.  (Not waited for with every page: a barrier for every other page keeps the
         // phases apart, since S of a page comes after O of the page two before it.)
@@ -514,16 +513,17 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
             const int open_to = a.node_parent != nullptr ? w.cached : w.cached + row0 / G + 1;
             int ev = 64;              // exponent field that O is relative to
             bool first = true, large = false;
+            const int first_pg = w.pg;
 #pragma unroll 1
             for (int i = PAIR ? 0 : (n0 ^ x) & 1; i < np; i += STEP) {
-                const int pg = w.pg + i, buf = taken & 1;
+                const int pg = first_pg + i, buf = taken & 1, slot = (n0 + i) & (kByteScales - 1);
                 const unsigned int col = col_s + buf * 64;
                 ok = wait(&sh.s_full[x][buf], (taken >> 1) & 1);   // (the page's scales came with its codes)
                 if (!ok) break;
                 if (halves > 0) {
                     tc_fence_after();
-                    const uint2 scale = *reinterpret_cast<const uint2*>(&sh.scale[sc.slot]);
-                    const bool missing = sh.missing[sc.slot] != 0;
+                    const uint2 scale = *reinterpret_cast<const uint2*>(&sh.scale[slot]);
+                    const bool missing = sh.missing[slot] != 0;
                     float s[H][32];       // rows g (s[0][4 k], s[0][4 k + 1]) and g + 8; g + 16 and g + 24
                     if (halves == H) {
                         tc_load(col, s);
@@ -532,8 +532,8 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
 #pragma unroll
                         for (int k = 0; k < 32; ++k) s[H - 1][k] = 0.f;
                     }
-                    const int ep = missing ? 0 : kvb_exponent(scale.y) + 127;
-                    const float ks = missing ? 1.f : kvb_pow2(kvb_exponent(scale.x));
+                    const int ep = missing ? 0 : (int)(kvb_scale_bits(scale.y) >> 23);
+                    const float ks = __uint_as_float(kvb_scale_bits(scale.x));   // (anything where the page is missing)
                     float ff[Q];          // what S is to be multiplied by (never 0: what is hidden is -inf times it)
 #pragma unroll
                     for (int q = 0; q < Q; ++q) ff[q] = fmaxf(qf[q] * ks, 1e-37f);
@@ -643,9 +643,8 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
                 __syncwarp();
                 if (lane == 0) {
                     mbar_arrive(&sh.p_full[x][buf]);
-                    mbar_arrive(&sh.scale_empty[sc.slot]);
+                    mbar_arrive(&sh.scale_empty[slot]);
                 }
-                sc.next(STEP);
             }
             if (!ok) break;
             // the result of the piece
