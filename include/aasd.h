@@ -622,7 +622,12 @@ int aasd_kvb_write(aasd_ctx* ctx, const void* q, const void* k, const void* v, c
                    void* q_out, void* k_out);
 
 /* aasd_kv_attend over an 8-bit pool: the same arguments, masks, errors and scratch (aasd_kv_workspace_init).  Sums and the
- * softmax's statistics are fp32; the result is rounded once. */
+ * softmax's statistics are fp32; the result is rounded once.  Keys and values are used as they are (with many rows, values
+ * below 2^-23 of the largest scale of the pages that a CTA has been through lose bits).  bf16 queries lose bits below 2^-27 of their row's
+ * largest element with few rows, and below 2^-9 of it with many (2^-17 of the largest element is left out at most); probabilities are
+ * rounded to 11 bits; fp32 queries and their probabilities to 22.  Many rows are, with bf16 queries and head_dim 64 or 128, more than 32 or
+ * 16 rows per key/value head (query heads of a group times token rows; rows_per_seq of them, or n_tokens / n_seqs
+ * when packed: one choice for the whole call). */
 int aasd_kvb_attend(aasd_ctx* ctx, const void* q, const void* pages, const int32_t* block_table,
                     const int32_t* cached_len, const int32_t* kv_len, const int32_t* tok_offsets,
                     const int32_t* node_parent, const aasd_kv_attend_params* params, void* workspace,
@@ -686,7 +691,8 @@ typedef struct aasd_kv_fork_out {   /* all required, [n_forks] each */
  * cached_len[dst], its row of the table, its page count and page_shares are set.  Pages come off the top fork by fork; a fork that the
  * stack cannot give a page any more is not made (AASD_STATUS_KV_FULL); those after it that need none are.  A fork whose
  * destination holds pages or is an earlier fork's, whose source is such a destination of the same call, or whose length the
- * source does not have, is not made either (AASD_STATUS_BAD_OFFSETS). */
+ * source does not have, is not made either (AASD_STATUS_BAD_OFFSETS).  The outputs must lie over none of the other
+ * arrays (AASD_ERR_INVALID_ARG). */
 int aasd_kv_fork(aasd_ctx* ctx, const int32_t* src_seq, const int32_t* dst_seq, const int32_t* fork_len,
                  int32_t n_forks, const aasd_kv_books_params* params, const aasd_kv_books* books,
                  int32_t* cached_len, const aasd_kv_pool* pool, const aasd_kv_fork_out* out);
@@ -701,7 +707,8 @@ int aasd_kv_copy(aasd_ctx* ctx, const aasd_kv_pool* pool, int32_t n_pages, const
  * pool may be cut or grown behind them) and the stack holds the others, page u on top.  page_map [n_pages]: the new
  * number of each page that was in use, NONE for the others, for whatever else names pages; moves [n_pages]: scratch (the
  * moves as pairs); n_moved [1].  A stack with repetitions or pages outside the pool raises AASD_STATUS_BAD_OFFSETS and nothing
- * moves; an entry of the table that is not in use raises it and stays. */
+ * moves; an entry of the table that is not in use raises it and stays.  page_map, moves and n_moved must not lie over one
+ * another or over the books (AASD_ERR_INVALID_ARG). */
 int aasd_kv_compact(aasd_ctx* ctx, const aasd_kv_books_params* params, const aasd_kv_books* books,
                     const aasd_kv_pool* pool, int32_t* page_map, int32_t* moves, int32_t* n_moved);
 

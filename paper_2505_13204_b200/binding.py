@@ -827,7 +827,7 @@ class Context:
         """aasd_kvb_write: norms and rotates ``q`` [T, Hq, D] and ``k`` [T, Hkv, D] as ``kv_write`` does and stores the tokens
         that ``kv_plan`` has placed (``kv_len`` and ``positions`` are its outputs) at the end of their sequences' pages.  Token
         rows are packed (``tok_offsets``) or padded (``rows_per_seq``).  Returns a dict with q and, with
-        ``keep_k``, the rotated k."""
+        ``keep_k``, the rotated k (zeros for tokens without a place)."""
         dev = self.device_index
         _kv_i32(dev, block_table, cached_len, kv_len, positions, tok_offsets)
         T, Hq, D = q.shape
@@ -847,7 +847,7 @@ class Context:
             assert w is None or (w.dtype is dt and w.get_device() == dev and w.numel() == D and w.is_contiguous())
         o = outputs
         if o is None:
-            o = dict(q=q.new_empty((T, Hq, D)), k=q.new_empty((T, Hkv, D)) if keep_k else None)
+            o = dict(q=q.new_empty((T, Hq, D)), k=q.new_zeros((T, Hkv, D)) if keep_k else None)
         else:
             _kv_like(q, T * Hq * D, o["q"])
             _kv_like(q, T * Hkv * D, o.get("k"))

@@ -7,8 +7,17 @@ using namespace aasd;
 
 namespace {
 
-// Sequences up to which the collecting CTA goes through the tables itself.
+// Sequences up to which the collecting CTA goes through the tables itself, a warp for each.
 constexpr int kDropInline = 64;
+// Pages up to which the kernels with one CTA have few threads.
+constexpr int kFewPages = 4 * kShareThreads * kShareEach;
+
+// Calls f with the number of threads as a constant.
+template <class F>
+void one_cta(bool few, F&& f) {
+    if (few) f(std::integral_constant<int, kShareThreads>());
+    else f(std::integral_constant<int, kShareThreadsMany>());
+}
 
 int check_books(const aasd_kv_books_params* p, const aasd_kv_books* k) {
     if (p == nullptr || k == nullptr) return AASD_ERR_INVALID_ARG;
@@ -47,13 +56,13 @@ int aasd_kv_free(aasd_ctx* ctx, const int32_t* keep_len, const int32_t* n_new, c
     if (!keep_len) return AASD_ERR_INVALID_ARG;
     KvFreeArgs a{keep_len, n_new, *k, *p, ctx->state};
     AASD_CUDA(cudaSetDevice(ctx->device));
-    if (p->n_seqs <= kDropInline) {
-        launch(kv_collect_kernel<true>, 1u, (unsigned int)kShareThreads, 0, ctx->stream, a);
-        return after_launch(ctx, 1);
-    }
-    launch(kv_drop_kernel, (unsigned int)((p->n_seqs + 7) / 8), 256u, 0, ctx->stream, a);
-    launch(kv_collect_kernel<false>, 1u, (unsigned int)kShareThreads, 0, ctx->stream, a);
-    return after_launch(ctx, 2);
+    const bool drop = p->n_seqs <= kDropInline;
+    if (!drop) launch(kv_drop_kernel, (unsigned int)((p->n_seqs + 7) / 8), 256u, 0, ctx->stream, a);
+    one_cta(p->n_pages <= kFewPages, [&](auto nt) {
+        if (drop) launch(kv_collect_kernel<nt(), true>, 1u, (unsigned int)nt(), 0, ctx->stream, a);
+        else launch(kv_collect_kernel<nt(), false>, 1u, (unsigned int)nt(), 0, ctx->stream, a);
+    });
+    return after_launch(ctx, drop ? 1 : 2);
 }
 
 int aasd_kv_copy(aasd_ctx* ctx, const aasd_kv_pool* pool, int32_t n_pages, const int32_t* src, const int32_t* dst, int32_t n) {
@@ -77,10 +86,17 @@ int aasd_kv_fork(aasd_ctx* ctx, const int32_t* src_seq, const int32_t* dst_seq, 
     if (n_forks < 0) return AASD_ERR_BAD_SHAPE;
     if (n_forks == 0) return AASD_OK;
     if (!src_seq || !dst_seq || !o->new_len || !o->copy_src || !o->copy_dst || (p->n_seqs > 0 && !cached_len)) return AASD_ERR_INVALID_ARG;
+    // what the forks are made from is read again when their outputs have been written
+    const int64_t n4 = 4 * (int64_t)n_forks, b4 = 4 * (int64_t)p->n_seqs;
+    for (const int32_t* x : {o->new_len, o->copy_src, o->copy_dst})
+        if (overlap(x, n4, src_seq, n4) || overlap(x, n4, dst_seq, n4) || overlap(x, n4, fork_len, n4) || overlap(x, n4, cached_len, b4) ||
+            overlap(x, n4, k->seq_pages, b4) || overlap(x, n4, k->block_table, b4 * p->max_pages))
+            return AASD_ERR_INVALID_ARG;
+    if (overlap(o->new_len, n4, o->copy_src, n4) || overlap(o->new_len, n4, o->copy_dst, n4) || overlap(o->copy_src, n4, o->copy_dst, n4)) return AASD_ERR_INVALID_ARG;
     KvForkArgs a{src_seq, dst_seq, fork_len, n_forks, *k, *p, cached_len, o->new_len, o->copy_src, o->copy_dst,
                  copy_args(ctx, *pool, p->n_pages, o->copy_src, o->copy_dst, 1, n_forks, nullptr), ctx->state};
     AASD_CUDA(cudaSetDevice(ctx->device));
-    launch(kv_fork_kernel, 1u, (unsigned int)kShareThreads, 0, ctx->stream, a);
+    one_cta(n_forks <= kShareThreads, [&](auto nt) { launch(kv_fork_kernel<nt()>, 1u, (unsigned int)nt(), 0, ctx->stream, a); });
     unsigned int grid = copy_grid(ctx, *pool, n_forks);
     const unsigned int tables = (unsigned int)((n_forks + 7) / 8);
     if (grid < tables) grid = tables < 1024 ? tables : 1024;
@@ -95,9 +111,14 @@ int aasd_kv_compact(aasd_ctx* ctx, const aasd_kv_books_params* p, const aasd_kv_
     if (const int rc = check_books(p, k)) return rc;
     if (const int rc = check_pool(pool)) return rc;
     if (!n_moved || (p->n_pages > 0 && (!page_map || !moves))) return AASD_ERR_INVALID_ARG;
+    const int64_t n4 = 4 * (int64_t)p->n_pages;
+    if (overlap(page_map, n4, moves, n4) || overlap(n_moved, 4, page_map, n4) || overlap(n_moved, 4, moves, n4)) return AASD_ERR_INVALID_ARG;
+    for (const int32_t* x : {page_map, moves})
+        if (overlap(x, n4, k->free_pages, n4) || overlap(x, n4, k->page_shares, n4) || overlap(x, n4, k->block_table, 4 * (int64_t)p->n_seqs * p->max_pages))
+            return AASD_ERR_INVALID_ARG;
     KvCompactArgs a{*k, *p, page_map, moves, n_moved, copy_args(ctx, *pool, p->n_pages, moves, moves + 1, 2, p->n_pages / 2, n_moved), ctx->state};
     AASD_CUDA(cudaSetDevice(ctx->device));
-    launch(kv_compact_kernel, 1u, (unsigned int)kShareThreads, 0, ctx->stream, a);
+    one_cta(p->n_pages <= kFewPages, [&](auto nt) { launch(kv_compact_kernel<nt()>, 1u, (unsigned int)nt(), 0, ctx->stream, a); });
     launch(kv_compact_copy_kernel, copy_grid(ctx, *pool, p->n_pages), (unsigned int)kCopyThreads, 0, ctx->stream, a);
     return after_launch(ctx, 2);
 }

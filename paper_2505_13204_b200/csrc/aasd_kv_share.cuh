@@ -6,7 +6,7 @@
 
 namespace aasd {
 
-constexpr int kShareThreads = 1024;
+constexpr int kShareThreads = 256, kShareThreadsMany = 1024;   // of the kernels with one CTA: a scan costs a barrier for every warp
 constexpr int kShareEach = 8;              // pages that a thread looks at per round of a scan over the pool
 
 // The count on the stack, held to what the pool has.
@@ -55,19 +55,19 @@ __global__ void __launch_bounds__(256) kv_drop_kernel(const KvFreeArgs a) {
 
 // One CTA: pages without a holder go on the stack, in order of their numbers (whatever order the atomics came in).
 // DROP: a small batch's tables are gone through first, without a launch of their own.
-template <bool DROP>
-__global__ void __launch_bounds__(kShareThreads) kv_collect_kernel(const KvFreeArgs a) {
-    __shared__ long long s_warp[kShareThreads / 32];
+template <int NT, bool DROP>
+__global__ void __launch_bounds__(NT) kv_collect_kernel(const KvFreeArgs a) {
+    __shared__ long long s_warp[NT / 32];
     pdl_launch_dependents();
     pdl_wait();
     if (DROP) {
-        for (int b = (int)threadIdx.x >> 5; b < a.p.n_seqs; b += kShareThreads / 32) kv_drop(a, b);
+        for (int b = (int)threadIdx.x >> 5; b < a.p.n_seqs; b += NT / 32) kv_drop(a, b);
         __syncthreads();
     }
     unsigned int bits = 0;
     const int N = a.p.n_pages;
     long long n = kv_free_count(a.k.n_free, N, bits);
-    for (int base = 0; base < N; base += kShareThreads * kShareEach) {
+    for (int base = 0; base < N; base += NT * kShareEach) {
         const int first = base + (int)threadIdx.x * kShareEach;
         int v[kShareEach], mine = 0;
 #pragma unroll
@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(kShareThreads) kv_collect_kernel(const KvFreeA
             if (v[e] < -1) bits |= AASD_STATUS_BAD_OFFSETS;      // listed more often than it had holders
         }
         long long total;
-        long long at = n + block_scan<kShareThreads>(mine, s_warp, total);
+        long long at = n + block_scan<NT>(mine, s_warp, total);
 #pragma unroll
         for (int e = 0; e < kShareEach; ++e) {
             if (v[e] >= 0) continue;
@@ -160,20 +160,21 @@ struct KvForkArgs {
 // One CTA: who forks, what each gets, and the pages for the parts that are begun.
 // A sequence that is to be made is claimed by the first fork that names it: its held count (0) becomes that fork's number less
 // n_forks.  Counts are set when every fork has been looked at, so that no fork sees what another one of the call made.
-__global__ void __launch_bounds__(kShareThreads) kv_fork_kernel(const KvForkArgs a) {
-    __shared__ long long s_warp[kShareThreads / 32];
+template <int NT>
+__global__ void __launch_bounds__(NT) kv_fork_kernel(const KvForkArgs a) {
+    __shared__ long long s_warp[NT / 32];
     pdl_launch_dependents();
     pdl_wait();
     const int B = a.p.n_seqs, N = a.p.n_pages, F = a.n_forks;
     unsigned int bits = 0;
     const long long n_free = kv_free_count(a.k.n_free, N, bits);
-    for (int i = threadIdx.x; i < F; i += kShareThreads) {
+    for (int i = threadIdx.x; i < F; i += NT) {
         const int d = a.dst_seq[i];
         if (d >= 0 && d < B && a.k.seq_pages[d] <= 0) atomicMin(a.k.seq_pages + d, i - F);
     }
     __syncthreads();
     long long asked = 0, taken = 0;
-    for (int base = 0; base < F; base += kShareThreads) {
+    for (int base = 0; base < F; base += NT) {
         const int i = base + (int)threadIdx.x;
         int len = AASD_NONE, page = AASD_NONE;
         bool claimed = false;
@@ -190,9 +191,9 @@ __global__ void __launch_bounds__(kShareThreads) kv_fork_kernel(const KvForkArgs
         }
         const int want = len != AASD_NONE && len % kPage ? 1 : 0;
         long long total, got;
-        const long long rank = asked + block_scan<kShareThreads>(want, s_warp, total);
+        const long long rank = asked + block_scan<NT>(want, s_warp, total);
         const bool served = len != AASD_NONE && (!want || rank < n_free);
-        block_scan<kShareThreads>(want && served, s_warp, got);
+        block_scan<NT>(want && served, s_warp, got);
         int to = AASD_NONE;
         if (want && served) {
             to = a.k.free_pages[n_free - 1 - rank];
@@ -210,7 +211,7 @@ __global__ void __launch_bounds__(kShareThreads) kv_fork_kernel(const KvForkArgs
         taken += got;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < F; i += kShareThreads) {
+    for (int i = threadIdx.x; i < F; i += NT) {
         const int len = a.new_len[i];
         if (len == AASD_NONE) continue;
         const int d = a.dst_seq[i];
@@ -255,23 +256,24 @@ struct KvCompactArgs {
 };
 
 // One CTA: the k-th page in use behind the last place moves to the k-th free one before it.
-__global__ void __launch_bounds__(kShareThreads) kv_compact_kernel(const KvCompactArgs a) {
-    __shared__ long long s_warp[kShareThreads / 32];
+template <int NT>
+__global__ void __launch_bounds__(NT) kv_compact_kernel(const KvCompactArgs a) {
+    __shared__ long long s_warp[NT / 32];
     pdl_launch_dependents();
     pdl_wait();
     const int N = a.p.n_pages, tid = threadIdx.x;
     unsigned int bits = 0;
     const int n_free = kv_free_count(a.k.n_free, N, bits), used = N - n_free;
-    for (int i = tid; i < N; i += kShareThreads) a.page_map[i] = i;
+    for (int i = tid; i < N; i += NT) a.page_map[i] = i;
     __syncthreads();
-    for (int i = tid; i < n_free; i += kShareThreads) {
+    for (int i = tid; i < n_free; i += NT) {
         const int page = a.k.free_pages[i];
         if (page < 0 || page >= N) bits |= AASD_STATUS_BAD_OFFSETS;
         else if (atomicExch(a.page_map + page, AASD_NONE) == AASD_NONE) bits |= AASD_STATUS_BAD_OFFSETS;   // twice on the stack
     }
     const bool bad = __syncthreads_or(bits != 0) != 0;
     long long far = 0, holes = 0;
-    for (int base = 0; !bad && base < N; base += kShareThreads * kShareEach) {
+    for (int base = 0; !bad && base < N; base += NT * kShareEach) {
         const int first = base + tid * kShareEach;
         int v[kShareEach], out = 0, in = 0;
 #pragma unroll
@@ -282,7 +284,7 @@ __global__ void __launch_bounds__(kShareThreads) kv_compact_kernel(const KvCompa
             in += v[e] == AASD_NONE && first + e < used;
         }
         long long total;
-        const long long both = block_scan<kShareThreads>((long long)out << 32 | in, s_warp, total);
+        const long long both = block_scan<NT>((long long)out << 32 | in, s_warp, total);
         long long o = far + (both >> 32), h = holes + (both & 0xFFFFFFFFLL);
 #pragma unroll
         for (int e = 0; e < kShareEach; ++e) {
@@ -295,16 +297,16 @@ __global__ void __launch_bounds__(kShareThreads) kv_compact_kernel(const KvCompa
     }
     __syncthreads();
     // (a stack without repetitions has as many pages in front of the last place as pages in use lie behind it)
-    for (int i = tid; i < (int)far; i += kShareThreads) {
+    for (int i = tid; i < (int)far; i += NT) {
         const int from = a.moves[2 * i], to = a.moves[2 * i + 1];
         a.page_map[from] = to;
         a.k.page_shares[to] = a.k.page_shares[from];
         a.k.page_shares[from] = 0;
     }
-    for (int i = tid; i < n_free; i += kShareThreads)
+    for (int i = tid; i < n_free; i += NT)
         if (!bad) a.k.free_pages[i] = N - 1 - i;
     if (bad)
-        for (int i = tid; i < N; i += kShareThreads) a.page_map[i] = i;
+        for (int i = tid; i < N; i += NT) a.page_map[i] = i;
     if (tid == 0) *a.n_moved = (int)far;
     if (bits) raise(a.state, bits);
 }

@@ -12,7 +12,13 @@ namespace aasd {
 
 namespace {
 
-constexpr int64_t kSplitRows = 48;
+// Rows per key/value head up to which the split kernel takes bf16 queries: it goes over the pages once for every 16 rows, but
+// shares them among all warps of the device.  Measured with trees over 32 query and 8 key heads of 128 channels, split kernel
+// against tiles, graph replays: 64 sequences of 4000 tokens: 16 rows 130 and 178 us, 24 rows 217 and 197 us, 48 rows 313 and 199
+// us; 8 of 4000: 16 rows 39 and 43 us, 24 rows 47 and 45 us; one of 16000: 16 rows 35 and 33 us, 24 rows 37 and 35 us.  With 64
+// channels, where a page is half as long to fetch: 64 of 4000: 24 rows 119 and 154 us, 32 rows 123 and 156 us; 8 of 4000: 33 and 37, 35
+// and 37 us; one of 16000: 27 and 29, 29 and 29 us.
+constexpr int64_t split_rows(int head_dim) { return head_dim == 64 ? 32 : 16; }
 
 template <int DT, int D, int NT>
 int launch_split(const LaunchEnv& env, int sm_count, const KvAttendArgs& a) {
@@ -64,7 +70,8 @@ int launch_kvb_attend_bf16(const LaunchEnv& env, int sm_count, const KvAttendArg
     const int64_t rows = per_seq * (a.p.n_q_heads / a.p.n_kv_heads);
     *launches = 1;
 #if AASD_DT == 1
-    if (rows > kSplitRows && a.p.head_dim <= 128) {
+    if (rows > split_rows(a.p.head_dim) && a.p.head_dim <= 128) {
+        // (Two row tiles of the same pages, or two groups on alternate pages of one.)
         *launches = 2;
         if (a.p.head_dim == 64) return rows > kTileRows ? launch_tile<64, true>(env, sm_count, a) : launch_tile<64, false>(env, sm_count, a);
         return rows > kTileRows ? launch_tile<128, true>(env, sm_count, a) : launch_tile<128, false>(env, sm_count, a);

@@ -135,6 +135,11 @@ def test_fork_refuses_what_cannot_be(ctx):
         ctx.kv_fork(d.pages, i32([0]).long(), i32([2]), table, held, cached, free, top, shares)
     with pytest.raises(binding.AasdError):
         ctx.kv_fork(d.pages[:, :1].contiguous(), i32([0]), i32([2]), table, held, cached, free, top, shares)
+    src, dst = i32([0]), i32([5])
+    with pytest.raises(binding.AasdError):               # outputs over what the fork is made from
+        ctx.kv_fork(d.pages, src, dst, table, held, cached, free, top, shares, outputs=dict(new_len=dst, copy_src=i32([0]), copy_dst=i32([0])))
+    with pytest.raises(binding.AasdError):
+        ctx.kv_compact(d.pages, table, held, free, top, shares, outputs=dict(page_map=shares, n_moved=i32([0])))
     with pytest.raises(binding.AasdError):
         ctx.kv_free(i32([0]), table, held, free, top, shares)
     with pytest.raises(binding.AasdError):
