@@ -622,8 +622,8 @@ int aasd_kvb_write(aasd_ctx* ctx, const void* q, const void* k, const void* v, c
                    void* q_out, void* k_out);
 
 /* aasd_kv_attend over an 8-bit pool: the same arguments, masks, errors and scratch (aasd_kv_workspace_init).  Sums and the
- * softmax's statistics are fp32; the result is rounded once.  Keys and values are used as they are (with many rows, values
- * below 2^-23 of the largest scale of the pages that a CTA has been through lose bits).  bf16 queries lose bits below 2^-27 of their row's
+ * softmax's statistics are fp32; the result is rounded once.  Keys and values are used as they are (probabilities of
+ * pages whose values' scale is below 2^-21 of the largest that a CTA has come by lose bits).  bf16 queries lose bits below 2^-27 of their row's
  * largest element with few rows, and below 2^-9 of it with many (2^-17 of the largest element is left out at most); probabilities are
  * rounded to 11 bits; fp32 queries and their probabilities to 22.  Many rows are, with bf16 queries and head_dim 64 or 128, more than 32 or
  * 16 rows per key/value head (query heads of a group times token rows; rows_per_seq of them, or n_tokens / n_seqs

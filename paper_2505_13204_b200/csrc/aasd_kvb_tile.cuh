@@ -5,9 +5,9 @@
 // Its warps have roles:
 //   walker, loader   as there; the loader brings a page's codes in as they lie, and its scales apart;
 //   unpackers        (4 warps) turn the values' codes into fp16 numbers, token by token: an operand whose rows run along K;
-//   two issuers      one thread each: tcgen05.mma of S = Q K^T (e4m3, the keys as they came, both operands in shared memory)
+//   two issuers      a warp each: tcgen05.mma of S = Q K^T (e4m3, the keys as they came, both operands in shared memory)
 //                    and O += P V (fp16, P in tensor memory) for one softmax group, a page at a time;
-//   softmax          two groups of 4 warps, 32 rows each: S to registers, probabilities back as P.
+//   softmax          two groups of 8 warps, 16 rows each: S to registers, probabilities back as P.
 // The two groups work on two row tiles of the same pages (PAIR), or, where a segment has no more than 128 rows, on
 // alternate pages of one tile, joined at the end.  A group has two S buffers, so that the next page's products are there
 // when it is done with one.
@@ -17,6 +17,13 @@
 // of the pages so far, which O is relative to.
 //
 // Tensor memory (512 columns): two S buffers of each group, whose first halves P takes over, and O.
+//
+// A page and group of 128 rows cost 384 cycles of S products (64 columns from shared memory, twice) and 256 of PV, 1259 for both
+// groups with the shared memory that they contend for; two issuers, unpackers and loader alone go at 1390 a page.  With
+// the softmax warps it is about 2300, and they are what bounds it: 512 cycles of exponentials, 330 until S is in registers, the
+// rest scaling, sums, packing and storing of P.  Measured: 2 x 2048 tokens of a prompt (32 over 8 heads of 128, bf16) 210 to 218
+// us, 632 to 657 TFLOP/s; 32 draft trees of 33 over about 3800 tokens 164 us; 64 tokens over 65536 104 us.  Eight warps of 32 rows
+// took 236 us for the first (fewer waits, but half as many warps to hide them), exponentials in turns of the two groups 233.
 #pragma once
 
 #include "aasd_kv_tile.cuh"
@@ -24,11 +31,10 @@
 
 namespace aasd {
 
-constexpr int kByteHalves = 1;                                   // sixteen rows of a softmax warp
-constexpr int kByteSoftmax = 16 / kByteHalves;                   // softmax warps
+constexpr int kByteSoftmax = 16;                                 // softmax warps
 constexpr int kByteTileThreads = 32 * (kByteSoftmax + 8);        // and 4 unpackers, two issuers, loader, walker
 // Registers per thread: the softmax warps take what the others give up of the launch's.
-constexpr int kByteLaunchRegs = kByteHalves == 1 ? 80 : 128, kByteSoftmaxRegs = kByteHalves == 1 ? 96 : 184, kByteOtherRegs = kByteHalves == 1 ? 48 : 72;
+constexpr int kByteLaunchRegs = 80, kByteSoftmaxRegs = 96, kByteOtherRegs = 48;
 static_assert(kByteSoftmax * kByteSoftmaxRegs + 8 * kByteOtherRegs <= (kByteSoftmax + 8) * kByteLaunchRegs, "the shares add up to the launch's registers");
 constexpr int kByteRaw = 5, kByteValues = 4, kByteScales = 8;   // ring depths, in pages
 // Where a page's scale of the values is this much below the largest (in powers of two), the row's maximum is looked for: fp16's
@@ -77,7 +83,7 @@ struct KvRing {
 
 // The issuers run as whole warps, whose values the compiler can see to be the same in every lane and keep in uniform registers,
 // where the tensor-core instructions want them; a lane is elected for each.  Eight products take 118 cycles to
-// issue so, and 410 from one thread inside a branch, which set the pace of the whole kernel (2 x 2048 chunk 225 us with it).
+// issue so, and 410 from one thread inside a branch: the roles other than softmax then go at 2125 cycles a page, not 1390.
 __device__ __forceinline__ bool elect_one() {
     unsigned int on;
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(on));
@@ -124,20 +130,17 @@ __device__ __forceinline__ void tc_load(unsigned int addr, float (&x)[16]) {
 __device__ __forceinline__ void tc_store(unsigned int addr, const float (&x)[16]) {
     asm volatile("tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]), "f"(x[8]), "f"(x[9]), "f"(x[10]), "f"(x[11]), "f"(x[12]), "f"(x[13]), "f"(x[14]), "f"(x[15]) : "memory");
 }
-__device__ __forceinline__ void tc_load(unsigned int addr, float (&x)[1][32]) { tc_load(addr, x[0]); }
-// O of a warp's rows times a factor per row.
-template <int D, int Q>
-__device__ __forceinline__ void kvb_scale_o(unsigned int col_o, const float (&fo)[Q]) {
+// O of a warp's rows times a factor for each of a thread's two.
+template <int D>
+__device__ __forceinline__ void kvb_scale_o(unsigned int col_o, const float (&fo)[2]) {
 #pragma unroll 1
-    for (int cb = 0; cb < D; cb += 32)
+    for (int cb = 0; cb < D; cb += 32) {
+        float o[16];
+        tc_load(col_o + cb, o);
 #pragma unroll
-        for (int half = 0; half < Q / 2; ++half) {
-            float o[16];
-            tc_load(col_o + cb + ((unsigned int)(16 * half) << 16), o);
-#pragma unroll
-            for (int k = 0; k < 16; ++k) o[k] *= fo[2 * half + ((k >> 1) & 1)];
-            tc_store(col_o + cb + ((unsigned int)(16 * half) << 16), o);
-        }
+        for (int k = 0; k < 16; ++k) o[k] *= fo[(k >> 1) & 1];
+        tc_store(col_o + cb, o);
+    }
     tc_wait_store();   // (a page may scale O twice)
 }
 
@@ -396,10 +399,11 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
             if (!ok) break;
         }
     } else {
-        // ---- softmax: thread (g, j) of a warp has rows g, g + 8, g + 16, g + 24 of the warp's 32 and two columns of every eight
+        // ---- softmax: thread (g, j) of a warp has rows g and g + 8 of the warp's 16 and two columns of every eight
         more_registers<kByteSoftmaxRegs>();
-        constexpr int H = kByteHalves, Q = 2 * H;    // rows of a thread
-        const int x = warp / (kByteSoftmax / 2), g = lane >> 2, j = lane & 3, row_base = (warp & 3) * 32 + (H == 1 ? ((warp >> 2) & 1) * 16 : 0);   // (of the group's 128 rows)
+        constexpr int Q = 2;                         // rows of a thread
+        // (of the group's 128 rows; a warp reaches the 32 lanes of tensor memory that its number gives it)
+        const int x = warp / (kByteSoftmax / 2), g = lane >> 2, j = lane & 3, row_base = (warp & 3) * 32 + ((warp >> 2) & 1) * 16;
         const unsigned int lanes = (unsigned int)row_base << 16;
         const unsigned int col_s = tm + kColS + x * kStep + lanes, col_o = tm + kColO + x * kStep + lanes;
         static_assert((kByteScales & (kByteScales - 1)) == 0, "a slot is a page's number, cut off");
@@ -420,9 +424,9 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
             if (np == 0) break;
             const int row0 = w.tile * R + (PAIR ? x * kTileRows : 0) + row_base;   // of the warp's first row, among the head's
             const int rows_here = AASD_IN_RANGE(w.first + w.fresh <= a.p.n_tokens && w.h < a.p.n_kv_heads, a.state) ? w.fresh * G : 0;   // rows of the head
-            // the lane's row: what the warp wants to know of its 32 rows
-            const auto own_row = [&]() { return max(min(row0 + (lane & (16 * H - 1)), rows_here - 1), 0); };
-            constexpr int LR = D / 8, RI = 32 / LR, NL = 4 * H;    // lanes per row, rows per step, steps at a time
+            // the lane's row: what the warp wants to know of its 16 rows
+            const auto own_row = [&]() { return max(min(row0 + (lane & 15), rows_here - 1), 0); };
+            constexpr int LR = D / 8, RI = 32 / LR, NL = 4;    // lanes per row, rows per step, steps at a time
             if (PAIR || x == 0) {
                 // The rows' queries, each as two e4m3 numbers, the row's largest element between 2^7 and 2^8: eight bits from 2^-2 on,
                 // smaller ones are off by 2^-10 at most.  A row that is not finite becomes NaN.
@@ -431,7 +435,7 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
                 const long long at = ((long long)w.first + token) * a.p.q_stride + (long long)(w.h * G + member) * D;   // of the lane's row
                 unsigned char* to = sh.queries[PAIR ? x : 0];
 #pragma unroll 1
-                for (int rb = 0; rb < 16 * H; rb += NL * RI) {
+                for (int rb = 0; rb < 16; rb += NL * RI) {
                     Raw8<AASD_BF16, true> raw[NL];
                     // (all on their way before the first is looked at; rows past the last one repeat it, and become zero)
                     if (a.q_vec) {
@@ -506,9 +510,9 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
                 mref[q] = kKvNothing;
                 l[q] = 0.f;
             }
-            // sixteen rows at a time are left out where the head has none of them (their probabilities are anything, and so
-            // is what becomes of them)
-            const int halves = min(H, (rows_here - row0 + 15) >> 4);
+            // a warp whose rows the head does not have leaves them out (their probabilities are anything, and so is what becomes
+            // of them)
+            const bool busy = row0 < rows_here;
             // places up to which every row of the warp sees everything
             const int open_to = a.node_parent != nullptr ? w.cached : w.cached + row0 / G + 1;
             int ev = 64;              // exponent field that O is relative to
@@ -520,33 +524,27 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
                 const unsigned int col = col_s + buf * 64;
                 ok = wait(&sh.s_full[x][buf], (taken >> 1) & 1);   // (the page's scales came with its codes)
                 if (!ok) break;
-                if (halves > 0) {
+                if (busy) {
                     tc_fence_after();
                     const uint2 scale = *reinterpret_cast<const uint2*>(&sh.scale[slot]);
                     const bool missing = sh.missing[slot] != 0;
-                    float s[H][32];       // rows g (s[0][4 k], s[0][4 k + 1]) and g + 8; g + 16 and g + 24
-                    if (halves == H) {
-                        tc_load(col, s);
-                    } else {
-                        tc_load(col, s[0]);
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) s[H - 1][k] = 0.f;
-                    }
+                    float s[32];          // rows g (s[4 k], s[4 k + 1]) and g + 8
+                    tc_load(col, s);
                     const int ep = missing ? 0 : (int)(kvb_scale_bits(scale.y) >> 23);
                     const float ks = __uint_as_float(kvb_scale_bits(scale.x));   // (anything where the page is missing)
                     float ff[Q];          // what S is to be multiplied by (never 0: what is hidden is -inf times it)
 #pragma unroll
                     for (int q = 0; q < Q; ++q) ff[q] = fmaxf(qf[q] * ks, 1e-37f);
                     if (missing || (pg + 1) * kPage > open_to) {   // what a row does not see becomes -inf (lane r finds out for row r)
-                        const u64 mine = missing || row0 + (lane & (16 * H - 1)) >= rows_here ? 0ull : kv_seen(a, w.cached, w.fresh, w.first, pg, own_row() / G);
+                        const u64 mine = missing || row0 + (lane & 15) >= rows_here ? 0ull : kv_seen(a, w.cached, w.fresh, w.first, pg, own_row() / G);
 #pragma unroll
                         for (int q = 0; q < Q; ++q) {
                             const u64 seen = __shfl_sync(0xFFFFFFFFu, mine, g + 8 * q) >> (2 * j);
 #pragma unroll
                             for (int k = 0; k < 8; ++k) {
                                 const unsigned int two = (unsigned int)(seen >> (8 * k));
-                                if (!(two & 1u)) s[q >> 1][4 * k + 2 * (q & 1)] = -CUDART_INF_F;
-                                if (!(two & 2u)) s[q >> 1][4 * k + 2 * (q & 1) + 1] = -CUDART_INF_F;
+                                if (!(two & 1u)) s[4 * k + 2 * q] = -CUDART_INF_F;
+                                if (!(two & 2u)) s[4 * k + 2 * q + 1] = -CUDART_INF_F;
                             }
                         }
                     }
@@ -559,7 +557,7 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
                             float fo[Q];
 #pragma unroll
                             for (float& y : fo) y = f;
-                            kvb_scale_o<D, Q>(col_o, fo);
+                            kvb_scale_o<D>(col_o, fo);
                         }
                         ev = ep;
                     }
@@ -578,7 +576,7 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
                             for (int q = 0; q < Q; ++q) {
                                 m[q] = -CUDART_INF_F;
 #pragma unroll
-                                for (int k = 0; k < 8; ++k) m[q] = fmaxf(m[q], fmaxf(s[q >> 1][4 * k + 2 * (q & 1)], s[q >> 1][4 * k + 2 * (q & 1) + 1]));
+                                for (int k = 0; k < 8; ++k) m[q] = fmaxf(m[q], fmaxf(s[4 * k + 2 * q], s[4 * k + 2 * q + 1]));
                                 m[q] = fmaxf(m[q], __shfl_xor_sync(0xFFFFFFFFu, m[q], 1));
                                 m[q] = fmaxf(m[q], __shfl_xor_sync(0xFFFFFFFFu, m[q], 2));
                                 m[q] *= ff[q];
@@ -587,9 +585,7 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
                             large = large || __any_sync(0xFFFFFFFFu, top >= kTileLarge);
                             if (large) {
 #pragma unroll
-                                for (int half = 0; half < H; ++half)
-#pragma unroll
-                                    for (int k = 0; k < 32; ++k) s[half][k] *= ff[2 * half + ((k >> 1) & 1)];
+                                for (int k = 0; k < 32; ++k) s[k] *= ff[(k >> 1) & 1];
                                 for (float& y : ff) y = 1.f;
                             }
 #pragma unroll
@@ -602,33 +598,25 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
                             if (!first) {
                                 ok = o_complete();
                                 if (!ok) break;
-                                kvb_scale_o<D, Q>(col_o, fo);
+                                kvb_scale_o<D>(col_o, fo);
                             }
                         }
+                        unsigned int pk[16];
 #pragma unroll
-                        for (int half = 0; half < H; ++half) {
-                            if (half >= halves) {
-                                ls[Q - 2] = ls[Q - 1] = 0.f;
-                                break;
+                        for (int q = 0; q < Q; ++q) {
+                            const float2 fq = make_float2(ff[q], ff[q]), mm = make_float2(shift - mref[q], shift - mref[q]);
+                            float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                float2 p = __ffma2_rn(make_float2(s[4 * k + 2 * q], s[4 * k + 2 * q + 1]), fq, mm);
+                                p = make_float2(ex2_approx(p.x), ex2_approx(p.y));
+                                sum = __fadd2_rn(sum, p);
+                                pk[2 * k + q] = pack_half(p.x, p.y);
                             }
-                            unsigned int pk[16];
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const int q = 2 * half + e;
-                                const float2 fq = make_float2(ff[q], ff[q]), mm = make_float2(shift - mref[q], shift - mref[q]);
-                                float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-                                for (int k = 0; k < 8; ++k) {
-                                    float2 p = __ffma2_rn(make_float2(s[half][4 * k + 2 * e], s[half][4 * k + 2 * e + 1]), fq, mm);
-                                    p = make_float2(ex2_approx(p.x), ex2_approx(p.y));
-                                    sum = __fadd2_rn(sum, p);
-                                    pk[2 * k + e] = pack_half(p.x, p.y);
-                                }
-                                ls[q] = sum.x + sum.y;
-                            }
-                            tc_store_cells(col + ((unsigned int)(16 * half) << 16), pk);
+                            ls[q] = sum.x + sum.y;
                         }
-                        if (again || __all_sync(0xFFFFFFFFu, fmaxf(fmaxf(ls[0], ls[1]), fmaxf(ls[Q - 2], ls[Q - 1])) < 65504.f)) break;
+                        tc_store_cells(col, pk);
+                        if (again || __all_sync(0xFFFFFFFFu, fmaxf(ls[0], ls[1]) < 65504.f)) break;
                         again = true;
                     }
                     if (!ok) break;
@@ -716,44 +704,39 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
                 }
 #pragma unroll 1
                 for (int cb = 0; cb < D; cb += 64) {
-#pragma unroll 1
-                    for (int half = 0; half < H; ++half) {      // rows g, g + 8; g + 16, g + 24
-                        const float f0 = half ? own[Q - 2] : own[0], f1 = half ? own[Q - 1] : own[1];
-                        float o[32];
+                    float o[32];                                // rows g, g + 8
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] = 0.f;
-                        if (any) {
-                            tc_load(col_o + cb + ((unsigned int)(16 * half) << 16), o);
+                    for (int k = 0; k < 32; ++k) o[k] = 0.f;
+                    if (any) {
+                        tc_load(col_o + cb, o);
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) o[k] *= (k >> 1) & 1 ? f1 : f0;
-                        }
-                        if (any1) {
-                            const float g0 = half ? other[Q - 2] : other[0], g1 = half ? other[Q - 1] : other[1];
-                            float y[32];
-                            tc_load(col_o + kStep + cb + ((unsigned int)(16 * half) << 16), y);
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) o[k] = fmaf(y[k], (k >> 1) & 1 ? g1 : g0, o[k]);
-                        }
-#pragma unroll
-                        for (int k = 0; k < 8; ++k)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const int lr = g + 16 * half + 8 * e, ch = cb + 8 * k + 2 * j;
-                                const float2 v = make_float2(o[4 * k + 2 * e], o[4 * k + 2 * e + 1]);
-                                if (complete) {
-                                    *reinterpret_cast<unsigned int*>(stage(lr, ch >> 3) + 4 * j) = pack_bf16(v.x, v.y);
-                                } else if ((PAIR ? x * kTileRows : 0) + row_base + lr < rows) {
-                                    *reinterpret_cast<float2*>(part + ((PAIR ? x * kTileRows : 0) + row_base + lr) * D + ch) = v;
-                                }
-                            }
+                        for (int k = 0; k < 32; ++k) o[k] *= own[(k >> 1) & 1];
                     }
+                    if (any1) {
+                        float y[32];
+                        tc_load(col_o + kStep + cb, y);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) o[k] = fmaf(y[k], other[(k >> 1) & 1], o[k]);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int lr = g + 8 * e, ch = cb + 8 * k + 2 * j;
+                            const float2 v = make_float2(o[4 * k + 2 * e], o[4 * k + 2 * e + 1]);
+                            if (complete) {
+                                *reinterpret_cast<unsigned int*>(stage(lr, ch >> 3) + 4 * j) = pack_bf16(v.x, v.y);
+                            } else if ((PAIR ? x * kTileRows : 0) + row_base + lr < rows) {
+                                *reinterpret_cast<float2*>(part + ((PAIR ? x * kTileRows : 0) + row_base + lr) * D + ch) = v;
+                            }
+                        }
                 }
                 if (complete) {
                     __syncwarp();
                     const int token = own_row() / G, member = own_row() - token * G;
                     const long long own_head = ((long long)w.first + token) * a.p.n_q_heads + w.h * G + member;
 #pragma unroll 4
-                    for (int rb = 0; rb < 16 * H; rb += RI) {
+                    for (int rb = 0; rb < 16; rb += RI) {
                         const int lr = rb + lane / LR;
                         const long long head = __shfl_sync(0xFFFFFFFFu, own_head, lr);
                         if (row0 + lr < rows_here) {
