@@ -42,8 +42,8 @@ int launch_tile(const LaunchEnv& env, int sm_count, const KvAttendArgs& a) {
     }();
     if (!enough) return AASD_ERR_UNSUPPORTED;
     launch(kernel, (unsigned int)(sm_count < kKvMaxCtas ? sm_count : kKvMaxCtas), (unsigned int)kTileThreads, smem, env.stream, a);
-    launch_grid2(kv_tile_join_kernel<D, PAIR>, (unsigned int)(sm_count < kKvMaxCtas ? sm_count : kKvMaxCtas), (PAIR ? 2u : 1u) * kTileRows / 8, 256u,
-                 env.stream, a);
+    launch_grid2(kv_tile_join_kernel<D, PAIR>, (unsigned int)(sm_count < kKvMaxCtas ? sm_count : kKvMaxCtas), (unsigned int)kTileJoinCtas,
+                 (unsigned int)kTileJoinThreads, env.stream, a);
     return AASD_OK;
 }
 #endif

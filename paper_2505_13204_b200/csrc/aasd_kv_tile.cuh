@@ -984,24 +984,104 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
     if (warp == 12) tc_free(tm, 512);
 }
 
-// Joins the parts of the segments that several CTAs of the tile kernel went through: block (c, k) takes rows
-// 8 k .. of the segment that CTA c began, a warp per row.  (Left to the last CTA that delivers a part, one
-// sequence of 64k tokens with 64 new ones waited 100 us for 19 parts of 256 rows.)  Its warps clear the rows
-// that no tile has.
+constexpr int kTileJoinThreads = 256, kTileJoinCtas = 2;   // a CTA's threads; CTAs per SM (with 4, and 64 registers, loads spill: 2 us more)
+constexpr int kTileJoinRows = 4;
+
+// Rows r0 .. r0 + 3 of a segment of at most eight parts, one warp: as kv_join_row, eight lanes finding a row's weights, with the
+// first two parts' sums under way meanwhile.
+template <int D>
+__device__ __forceinline__ void kv_join_rows(const KvAttendArgs& a, const KvPiece& pc, int r0, const float* base, int stride, int rows, int parts, int G, int lane) {
+    constexpr int NR = kTileJoinRows;
+    const auto part = [&](int k) { return base + (long long)(2 * k + (k == 0)) * stride; };
+    const int own = min(r0 + (lane >> 3), pc.n - 1), k = lane & 7;
+    const bool mine = k < parts;
+    const float m = mine ? __ldcg(part(k) + rows * D + own) : kKvNothing, l = mine ? __ldcg(part(k) + rows * D + rows + own) : 0.f;
+    const bool on = lane * 4 < D;
+    float4 x[NR][2];
+    const auto load = [&](int k0) {
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                x[i][q] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (on && k0 + q < parts && r0 + i < pc.n) x[i][q] = __ldcg(reinterpret_cast<const float4*>(part(k0 + q) + (r0 + i) * D + lane * 4));
+            }
+    };
+    load(0);
+    float M = fmaxf(kKvNothing, m);
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
+    const float f = mine ? ex2_approx(m - M) : 0.f;
+    float L = mine ? fmaf(l, f, 0.f) : 0.f;
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) L += __shfl_xor_sync(0xFFFFFFFFu, L, o);
+    float4 o[NR];
+#pragma unroll
+    for (int i = 0; i < NR; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+    for (int k0 = 0;;) {
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const float fk = __shfl_sync(0xFFFFFFFFu, f, 8 * i + ((k0 + q) & 7));
+                o[i].x = fmaf(x[i][q].x, fk, o[i].x);
+                o[i].y = fmaf(x[i][q].y, fk, o[i].y);
+                o[i].z = fmaf(x[i][q].z, fk, o[i].z);
+                o[i].w = fmaf(x[i][q].w, fk, o[i].w);
+            }
+        k0 += 2;
+        if (k0 >= parts) break;
+        load(k0);
+    }
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+        const float Li = __shfl_sync(0xFFFFFFFFu, L, 8 * i), Mi = __shfl_sync(0xFFFFFFFFu, M, 8 * i);
+        if (!on || r0 + i >= pc.n) continue;
+        const float inv = Li > 0.f ? 1.f / Li : 0.f;
+        const int row = pc.row0 + r0 + i;
+        const long long head = ((long long)pc.first + row / G) * a.p.n_q_heads + pc.h * G + row % G;
+        if (!AASD_IN_RANGE(head < a.p.n_tokens * a.p.n_q_heads, a.state)) continue;
+        store4<AASD_BF16>(a.o.out, head * D + lane * 4, make_float4(o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv), a.out_vec);
+        if (a.o.lse != nullptr && lane == 0) a.o.lse[head] = Li > 0.f ? (Mi + log2f(Li)) * (float)kLn2 : -CUDART_INF_F;
+    }
+}
+
+// Joins the parts of the segments that several CTAs of the tile kernel went through.  Every warp of the launch takes its turn
+// at the list of their rows: four at a time, or one where there are more than eight parts.  It adds 6 to 14 us to a call's kernel
+// (39 MB of parts where every CTA of a device has cut segments at both ends).  A block for every eight rows that a CTA's segment
+// could have, most of which left at once, added 12 to 18; left to the last CTA that delivers a part, one
+// sequence of 64k tokens with 64 new ones waited 100 us for 19 parts of 256 rows.  The warps also clear the rows that no
+// tile has.  grid: (CTAs of the tile kernel, kTileJoinCtas).
 template <int D, bool PAIR>
-__global__ void __launch_bounds__(256) kv_tile_join_kernel(const KvAttendArgs a) {
+__global__ void __launch_bounds__(kTileJoinThreads, kTileJoinCtas) kv_tile_join_kernel(const KvAttendArgs a) {
     constexpr int R = PAIR ? 2 * kTileRows : kTileRows, kPart = R * D + 2 * R;
+    static_assert(D <= 128 && kKvMaxCtas <= kTileJoinThreads, "a row in one pass, a thread for each CTA's segment");
+    __shared__ int s_first[kTileJoinThreads];
+    __shared__ long long s_warp[kTileJoinThreads / 32];
     pdl_launch_dependents();
     pdl_wait();
-    const KvTileOpen open = a.tile_open[blockIdx.x];
-    const KvPiece& pc = open.piece;
-    const int r = (int)blockIdx.y * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (open.padding != 0)
-        kv_clear_rows<AASD_BF16>(a, D, 2 - open.padding, r * (int)gridDim.x + (int)blockIdx.x, (int)(gridDim.x * gridDim.y) * 8);
-    if (open.parts == 0 || r >= pc.n) return;
+    const int tid = threadIdx.x, lane = tid & 31, ctas = (int)gridDim.x;
+    const int warp = (int)(blockIdx.y * gridDim.x + blockIdx.x) * (kTileJoinThreads / 32) + (tid >> 5), warps = (int)(gridDim.x * gridDim.y) * (kTileJoinThreads / 32);
+    int items = 0;
+    if (tid < ctas) {
+        const int parts = a.tile_open[tid].parts, n = a.tile_open[tid].piece.n;
+        if (parts > 0) items = parts > 8 ? n : (n + kTileJoinRows - 1) / kTileJoinRows;
+    }
+    const int padding = a.tile_open[0].padding;
+    long long total;
+    s_first[tid] = (int)block_scan<kTileJoinThreads>(items, s_warp, total);
+    __syncthreads();
+    if (padding != 0) kv_clear_rows<AASD_BF16>(a, D, 2 - padding, warp, warps);
     const int G = a.p.n_q_heads / a.p.n_kv_heads;
-    const float* base = a.cta_parts + (long long)blockIdx.x * 2 * kPart;   // part k: 2 k, the first one's 1
-    kv_join_row<AASD_BF16, D>(a, pc, r, base, kPart, R, open.parts, G, lane);
+#pragma unroll 1
+    for (int i = warp; i < (int)total; i += warps) {
+        const int c = last_not_above(s_first, ctas, i), at = i - s_first[c];
+        const KvTileOpen open = a.tile_open[c];
+        const float* base = a.cta_parts + (long long)c * 2 * kPart;   // part k: 2 k, the first one's 1
+        if (open.parts > 8) kv_join_row<AASD_BF16, D>(a, open.piece, at, base, kPart, R, open.parts, G, lane);
+        else kv_join_rows<D>(a, open.piece, at * kTileJoinRows, base, kPart, R, open.parts, G, lane);
+    }
 }
 
 }  // namespace aasd
