@@ -7,10 +7,12 @@ using namespace aasd;
 
 namespace {
 
-// Sequences up to which the collecting CTA goes through the tables itself, a warp for each.
-constexpr int kDropInline = 64;
-// Pages up to which the kernels with one CTA have few threads.
-constexpr int kFewPages = 4 * kShareThreads * kShareEach;
+// Sequences up to which the collecting CTA goes through the tables itself, a warp for two of them: a launch less for the host.
+// Freeing and compacting, on the device: 16 sequences 14 us either way, 48 20 us against 16 with a launch for the tables.
+constexpr int kDropInline = 16;
+// Pages up to which the kernels with one CTA have few threads, one round of a scan: a round costs a barrier of all warps.  Freeing
+// and compacting with few threads and with many: 100 pages 14 and 18 us, 1300 20 and 22, 2300 27 and 24, 8000 51 and 37.
+constexpr int kFewPages = kShareThreads * kShareEach;
 
 // Calls f with the number of threads as a constant.
 template <class F>

@@ -57,6 +57,11 @@ int aasd_kvb_write(aasd_ctx* ctx, const void* q, const void* k, const void* v, c
     if (units > 0x7FFFFFFFLL || query_blocks > 0x3FFFFFFFLL) return AASD_ERR_BAD_SHAPE;
     if (units + query_blocks == 0) return AASD_OK;
     a.units = (unsigned int)units;
+    // A warp for each page, head and half, or a CTA.  A CTA holds a page's rows in registers, but most of its warps idle with few rows;
+    // a warp goes through its rows twice, four of 128 channels at a time.  A CTA where all of them run at once, or with more
+    // than 32 rows per sequence.  Measured with 32 query and 8 key heads of 128 channels, warps against CTAs, in us (read-back included,
+    // 5 to 12): 64 sequences of 1 row 16 and 25, 8 rows 18 and 27, 16 rows 25 and 31, 33 rows 39 and 39, 64 rows 57 and 55;
+    // 4 sequences of 1 row 12 and 12, 8 rows 14 and 12, 33 rows 27 and 14, 128 rows 41 and 16.
     AASD_CUDA(cudaSetDevice(ctx->device));
     with_type(p->dtype, [&](auto dt) {
         with_dim(D, [&](auto d) {
@@ -65,7 +70,7 @@ int aasd_kvb_write(aasd_ctx* ctx, const void* q, const void* k, const void* v, c
                 a.store_blocks = (unsigned int)((units + per - 1) / per);
                 launch(kernel, a.store_blocks + (unsigned int)query_blocks, (unsigned int)kByteThreads, 0, ctx->stream, a);
             };
-            const bool few = n_tokens <= 8 * (int64_t)B;
+            const bool few = units > (int64_t)kWriteCtas * ctx->sm_count && n_tokens <= 32 * (int64_t)B;
             if (vec && full) few ? go(kvb_write_kernel<dt(), d(), true, true, 1>, 1) : go(kvb_write_kernel<dt(), d(), true, true, 8>, 8);
             else if (vec) few ? go(kvb_write_kernel<dt(), d(), true, false, 1>, 1) : go(kvb_write_kernel<dt(), d(), true, false, 8>, 8);
             else few ? go(kvb_write_kernel<dt(), d(), false, false, 1>, 1) : go(kvb_write_kernel<dt(), d(), false, false, 8>, 8);
