@@ -94,7 +94,8 @@ def books(rng, B, longest, spare, live):
     return ref.Books(table, need, order[at:], [0] * N, cached, longest // PAGE + 3)
 
 
-@pytest.mark.parametrize("B,live,longest,spare", [(2, 1, 10, 1), (8, 3, 300, 20), (40, 10, 1000, 100), (1500, 300, 200, 1300), (6, 2, 64, 0), (30, 9, 700, 7)])
+@pytest.mark.parametrize("B,live,longest,spare", [(2, 1, 10, 1), (8, 3, 300, 20), (40, 10, 1000, 100), (1500, 300, 200, 1300), (6, 2, 64, 0), (30, 9, 700, 7),
+                                                  (12, 4, 300, 2600), (64, 20, 500, 9000)])   # pools of more than one round of a scan
 def test_fork_free_compact(ctx, B, live, longest, spare):
     rng = np.random.default_rng(B + longest)
     d = Device(books(rng, B, longest, spare, live), rng=rng)

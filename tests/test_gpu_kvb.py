@@ -73,7 +73,12 @@ WRITES = [  # sequences, new tokens (most), longest context, query heads, key he
     (4, 9, 130, 8, 2, 128, "f32", 128, False, True, True), (2, 150, 70, 4, 2, 64, "bf16", 32, True, False, False),
     (3, 70, 64, 6, 3, 128, "f32", 64, False, True, False), (2, 130, 1, 2, 1, 256, "bf16", 256, False, True, False),
     (5, 5, 63, 7, 1, 256, "f32", 128, True, True, True), (1, 300, 300, 5, 5, 64, "f32", 0, False, True, False),
-    (40, 3, 500, 4, 2, 128, "bf16", 128, True, True, True), (300, 2, 40, 2, 1, 64, "bf16", 64, False, True, False)]
+    (40, 3, 500, 4, 2, 128, "bf16", 128, True, True, True), (300, 2, 40, 2, 1, 64, "bf16", 64, False, True, False),
+    # more pages than CTAs at a time, few rows each (a warp per page), in one pass and in several; and many rows each
+    (160, 5, 300, 4, 2, 128, "bf16", 128, False, True, True), (160, 9, 130, 2, 1, 64, "f32", 64, False, True, False),
+    (160, 3, 70, 2, 1, 256, "bf16", 256, False, True, True), (160, 30, 100, 3, 1, 64, "bf16", 32, True, True, False),
+    (160, 40, 60, 2, 1, 256, "f32", 128, False, False, False), (160, 30, 100, 2, 1, 128, "f32", 0, False, True, False),
+    (120, 90, 64, 2, 1, 64, "bf16", 64, False, True, False)]
 
 
 @pytest.mark.parametrize("B,new,longest,Hq,Hkv,D,dtype,rot,inter,norm,padded", WRITES)
@@ -119,6 +124,30 @@ def test_write(ctx, B, new, longest, Hq, Hkv, D, dtype, rot, inter, norm, padded
             want = kv_ref.norm_rotate(x, None if ww is None else f64(ww), cos[pos[t]] if rot else None, rot, inter, eps)
             # fp32: the norm's factor 8 roundings, the products and the sum of a pair 4 more, relative to the pair's size
             assert (np.abs(got - want) <= 2.0 ** -24 * np.abs(want) + 12 * 2.0 ** -24 * np.abs(want).max(-1, keepdims=True)).all()
+
+
+@pytest.mark.parametrize("B,new", [(3, 70), (160, 12)])
+@pytest.mark.parametrize("D,dtype", [(64, "bf16"), (128, "f32"), (256, "bf16")])
+def test_write_of_unaligned_rows(ctx, B, new, D, dtype):
+    rng = np.random.default_rng(B + D)
+    cached, T = rng.integers(0, 100, B), B * new
+    rows, table, pool = tables(rng, cached + new)
+    raw = garbage(rng, pool, 1, D)
+    x = torch.as_tensor(rng.standard_normal((T, 3 * D)).astype(np.float32)).to(DT[dtype]).cuda()
+    flat = torch.zeros(T * (3 * D + 1) + 1, dtype=DT[dtype], device="cuda")
+    odd = flat[1:].view(T, 3 * D + 1)[:, :3 * D]          # every row starts somewhere else
+    odd.copy_(x)
+    ang = np.arange(200)[:, None] * 10000.0 ** (-np.arange(D // 2) / (D // 2))
+    cs = torch.as_tensor(np.concatenate([np.cos(ang), np.sin(ang)], 1).astype(np.float32)).cuda()
+    pos = i32((cached[:, None] + np.arange(new)).ravel())
+    got = []
+    for y in (x, odd):
+        pages = torch.as_tensor(raw).cuda()
+        q, k, v = (y[:, i * D:(i + 1) * D].unflatten(1, (1, D)) for i in range(3))
+        o = ctx.kvb_write(pages, q, k, v, i32(table), i32(cached), i32(cached + new), pos, None, new, cs, keep_k=True)
+        assert ctx.poll_status() == 0
+        got.append((pages, o["q"], o["k"]))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
 
 
 def test_write_of_rows_that_are_not_finite_or_have_no_position(ctx):
