@@ -26,8 +26,8 @@ __device__ __forceinline__ unsigned int kvb_halves(unsigned int w) {
 // SM are on their way.  (mma.sync: sixteen rows would leave a tcgen05 tile mostly empty.)
 //
 // Bound by memory with a batch, by the chain share - table - block - products - joins with one sequence.  Measured (bf16, 128
-// channels, one token each): 256 sequences of 100 to 4000 tokens, 28 query and 4 key heads, 106 us, 541 MB at 5.1 TB/s, 78 % of the copy
-// rate (start and joins 15 us); one sequence of 16384 tokens, 32 and 8 heads, 18 us, where its 34 MB alone take 5.
+// channels, one token each): 256 sequences of 100 to 4000 tokens, 28 query and 4 key heads, 101 us, 541 MB at 5.3 TB/s, 82 % of the copy
+// rate; one sequence of 16384 tokens, 32 and 8 heads, 18 us, where its 34 MB alone take 5.
 template <int DT, int D, int NT>
 struct KvbSplitShape {
     static constexpr int TB = D == 64 ? 64 : D == 128 ? 32 : 16;       // tokens of a block
