@@ -625,8 +625,8 @@ int aasd_kvb_write(aasd_ctx* ctx, const void* q, const void* k, const void* v, c
  * softmax's statistics are fp32; the result is rounded once.  Keys and values are used as they are (probabilities of
  * pages whose values' scale is below 2^-21 of the largest that a CTA has come by lose bits).  bf16 queries lose bits below 2^-27 of their row's
  * largest element with few rows, and below 2^-9 of it with many (2^-17 of the largest element is left out at most); probabilities are
- * rounded to 11 bits; fp32 queries and their probabilities to 22.  Many rows are, with bf16 queries and head_dim 64 or 128, more than 32 or
- * 16 rows per key/value head (query heads of a group times token rows; rows_per_seq of them, or n_tokens / n_seqs
+ * rounded to 11 bits; fp32 queries and their probabilities to 22.  Many rows are, with bf16 queries and head_dim 64, 128 or 256, more than
+ * 32, 16 or 8 rows per key/value head (query heads of a group times token rows; rows_per_seq of them, or n_tokens / n_seqs
  * when packed: one choice for the whole call). */
 int aasd_kvb_attend(aasd_ctx* ctx, const void* q, const void* pages, const int32_t* block_table,
                     const int32_t* cached_len, const int32_t* kv_len, const int32_t* tok_offsets,

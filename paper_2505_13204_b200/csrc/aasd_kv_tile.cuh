@@ -998,16 +998,16 @@ __device__ __forceinline__ void kv_join_rows(const KvAttendArgs& a, const KvPiec
     const float m = mine ? __ldcg(part(k) + rows * D + own) : kKvNothing, l = mine ? __ldcg(part(k) + rows * D + rows + own) : 0.f;
     const bool on = lane * 4 < D;
     float4 x[NR][2];
-    const auto load = [&](int k0) {
+    const auto load = [&](int k0, int ch) {
 #pragma unroll
         for (int i = 0; i < NR; ++i)
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
                 x[i][q] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (on && k0 + q < parts && r0 + i < pc.n) x[i][q] = __ldcg(reinterpret_cast<const float4*>(part(k0 + q) + (r0 + i) * D + lane * 4));
+                if (on && k0 + q < parts && r0 + i < pc.n) x[i][q] = __ldcg(reinterpret_cast<const float4*>(part(k0 + q) + (r0 + i) * D + ch));
             }
     };
-    load(0);
+    load(0, lane * 4);
     float M = fmaxf(kKvNothing, m);
 #pragma unroll
     for (int o = 4; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
@@ -1015,35 +1015,42 @@ __device__ __forceinline__ void kv_join_rows(const KvAttendArgs& a, const KvPiec
     float L = mine ? fmaf(l, f, 0.f) : 0.f;
 #pragma unroll
     for (int o = 4; o > 0; o >>= 1) L += __shfl_xor_sync(0xFFFFFFFFu, L, o);
-    float4 o[NR];
-#pragma unroll
-    for (int i = 0; i < NR; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
-    for (int k0 = 0;;) {
+    for (int ch = lane * 4;;) {
+        float4 o[NR];
 #pragma unroll
-        for (int i = 0; i < NR; ++i)
+        for (int i = 0; i < NR; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (int k0 = 0;;) {
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const float fk = __shfl_sync(0xFFFFFFFFu, f, 8 * i + ((k0 + q) & 7));
-                o[i].x = fmaf(x[i][q].x, fk, o[i].x);
-                o[i].y = fmaf(x[i][q].y, fk, o[i].y);
-                o[i].z = fmaf(x[i][q].z, fk, o[i].z);
-                o[i].w = fmaf(x[i][q].w, fk, o[i].w);
-            }
-        k0 += 2;
-        if (k0 >= parts) break;
-        load(k0);
-    }
+            for (int i = 0; i < NR; ++i)
 #pragma unroll
-    for (int i = 0; i < NR; ++i) {
-        const float Li = __shfl_sync(0xFFFFFFFFu, L, 8 * i), Mi = __shfl_sync(0xFFFFFFFFu, M, 8 * i);
-        if (!on || r0 + i >= pc.n) continue;
-        const float inv = Li > 0.f ? 1.f / Li : 0.f;
-        const int row = pc.row0 + r0 + i;
-        const long long head = ((long long)pc.first + row / G) * a.p.n_q_heads + pc.h * G + row % G;
-        if (!AASD_IN_RANGE(head < a.p.n_tokens * a.p.n_q_heads, a.state)) continue;
-        store4<AASD_BF16>(a.o.out, head * D + lane * 4, make_float4(o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv), a.out_vec);
-        if (a.o.lse != nullptr && lane == 0) a.o.lse[head] = Li > 0.f ? (Mi + log2f(Li)) * (float)kLn2 : -CUDART_INF_F;
+                for (int q = 0; q < 2; ++q) {
+                    const float fk = __shfl_sync(0xFFFFFFFFu, f, 8 * i + ((k0 + q) & 7));
+                    o[i].x = fmaf(x[i][q].x, fk, o[i].x);
+                    o[i].y = fmaf(x[i][q].y, fk, o[i].y);
+                    o[i].z = fmaf(x[i][q].z, fk, o[i].z);
+                    o[i].w = fmaf(x[i][q].w, fk, o[i].w);
+                }
+            k0 += 2;
+            if (k0 >= parts) break;
+            load(k0, ch);
+        }
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const float Li = __shfl_sync(0xFFFFFFFFu, L, 8 * i), Mi = __shfl_sync(0xFFFFFFFFu, M, 8 * i);
+            if (!on || r0 + i >= pc.n) continue;
+            const float inv = Li > 0.f ? 1.f / Li : 0.f;
+            const int row = pc.row0 + r0 + i;
+            const long long head = ((long long)pc.first + row / G) * a.p.n_q_heads + pc.h * G + row % G;
+            if (!AASD_IN_RANGE(head < a.p.n_tokens * a.p.n_q_heads, a.state)) continue;
+            store4<AASD_BF16>(a.o.out, head * D + ch, make_float4(o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv), a.out_vec);
+            if (a.o.lse != nullptr && ch == 0) a.o.lse[head] = Li > 0.f ? (Mi + log2f(Li)) * (float)kLn2 : -CUDART_INF_F;
+        }
+        if (D <= 128) break;
+        ch += 128;
+        if (ch >= D) break;
+        load(0, ch);
     }
 }
 
@@ -1056,7 +1063,7 @@ __device__ __forceinline__ void kv_join_rows(const KvAttendArgs& a, const KvPiec
 template <int D, bool PAIR>
 __global__ void __launch_bounds__(kTileJoinThreads, kTileJoinCtas) kv_tile_join_kernel(const KvAttendArgs a) {
     constexpr int R = PAIR ? 2 * kTileRows : kTileRows, kPart = R * D + 2 * R;
-    static_assert(D <= 128 && kKvMaxCtas <= kTileJoinThreads, "a row in one pass, a thread for each CTA's segment");
+    static_assert(kKvMaxCtas <= kTileJoinThreads, "a thread for each CTA's segment");
     __shared__ int s_first[kTileJoinThreads];
     __shared__ long long s_warp[kTileJoinThreads / 32];
     pdl_launch_dependents();

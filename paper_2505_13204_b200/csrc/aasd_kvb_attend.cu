@@ -17,8 +17,10 @@ namespace {
 // against tiles, graph replays: 64 sequences of 4000 tokens: 16 rows 130 and 178 us, 24 rows 217 and 197 us, 48 rows 313 and 199
 // us; 8 of 4000: 16 rows 39 and 43 us, 24 rows 47 and 45 us; one of 16000: 16 rows 35 and 33 us, 24 rows 37 and 35 us.  With 64
 // channels, where a page is half as long to fetch: 64 of 4000: 24 rows 119 and 154 us, 32 rows 123 and 156 us; 8 of 4000: 33 and 37, 35
-// and 37 us; one of 16000: 27 and 29, 29 and 29 us.
-constexpr int64_t split_rows(int head_dim) { return head_dim == 64 ? 32 : 16; }
+// and 37 us; one of 16000: 27 and 29, 29 and 29 us.  With 256 channels (16 and 4 heads), where the split kernel has eight rows at a time: 64 of
+// 4000: 8 rows 127 and 156 us, 12 rows 207 and 160 us; 8 of 4000: 35 and 45, 43 and 45 us; one of 16000: 41 and 41, 37 and 41 us (48 rows: 517 and
+// 170, 86 and 49, 55 and 43 us).
+constexpr int64_t split_rows(int head_dim) { return head_dim == 64 ? 32 : head_dim == 128 ? 16 : 8; }
 
 template <int DT, int D, int NT>
 int launch_split(const LaunchEnv& env, int sm_count, const KvAttendArgs& a) {
@@ -40,10 +42,10 @@ int launch_tile(const LaunchEnv& env, int sm_count, const KvAttendArgs& a) {
     // the softmax warps wait for registers that the launch must have brought along
     static const bool enough = [] {
         cudaFuncAttributes f;
-        return cudaFuncGetAttributes(&f, kernel) == cudaSuccess && f.numRegs >= kByteLaunchRegs;
+        return cudaFuncGetAttributes(&f, kernel) == cudaSuccess && f.numRegs >= KvbTileShape<D>::kLaunchRegs;
     }();
     if (!enough) return AASD_ERR_UNSUPPORTED;
-    launch(kernel, (unsigned int)(sm_count < kKvMaxCtas ? sm_count : kKvMaxCtas), (unsigned int)kByteTileThreads, smem, env.stream, a);
+    launch(kernel, (unsigned int)(sm_count < kKvMaxCtas ? sm_count : kKvMaxCtas), (unsigned int)KvbTileShape<D>::kThreads, smem, env.stream, a);
     launch_grid2(kv_tile_join_kernel<D, PAIR>, (unsigned int)(sm_count < kKvMaxCtas ? sm_count : kKvMaxCtas), (unsigned int)kTileJoinCtas,
                  (unsigned int)kTileJoinThreads, env.stream, a);
     return AASD_OK;
@@ -70,9 +72,10 @@ int launch_kvb_attend_bf16(const LaunchEnv& env, int sm_count, const KvAttendArg
     const int64_t rows = per_seq * (a.p.n_q_heads / a.p.n_kv_heads);
     *launches = 1;
 #if AASD_DT == 1
-    if (rows > split_rows(a.p.head_dim) && a.p.head_dim <= 128) {
+    if (rows > split_rows(a.p.head_dim)) {
         // (Two row tiles of the same pages, or two groups on alternate pages of one.)
         *launches = 2;
+        if (a.p.head_dim == 256) return launch_tile<256, false>(env, sm_count, a);
         if (a.p.head_dim == 64) return rows > kTileRows ? launch_tile<64, true>(env, sm_count, a) : launch_tile<64, false>(env, sm_count, a);
         return rows > kTileRows ? launch_tile<128, true>(env, sm_count, a) : launch_tile<128, false>(env, sm_count, a);
     }

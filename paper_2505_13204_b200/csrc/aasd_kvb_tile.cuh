@@ -9,7 +9,7 @@
 //                    and O += P V (fp16, P in tensor memory) for one softmax group, a page at a time;
 //   softmax          two groups of 8 warps, 16 rows each: S to registers, probabilities back as P.
 // The two groups work on two row tiles of the same pages (PAIR), or, where a segment has no more than 128 rows, on
-// alternate pages of one tile, joined at the end.  A group has two S buffers, so that the next page's products are there
+// alternate pages of one tile, joined at the end.  With 256 channels there is one group.  A group has two S buffers, so that the next page's products are there
 // when it is done with one.
 //
 // A bf16 query is two e4m3 numbers (eight bits), multiplied one after the other.  A page's scale of the keys is a factor of S that
@@ -24,6 +24,7 @@
 // rest scaling, sums, packing and storing of P.  Measured: 2 x 2048 tokens of a prompt (32 over 8 heads of 128, bf16) 193 to 219
 // us from GPU to GPU, 627 to 712 TFLOP/s; 32 draft trees of 33 over about 3800 tokens 158 to 162 us; 64 tokens over 65536 98 to 102 us.  Eight warps of 32 rows
 // took 236 us for the first (fewer waits, but half as many warps to hide them), exponentials in turns of the two groups 233.
+// With 256 channels (16 over 4 heads): the same prompt behind 1000 tokens 199 us, 684 TFLOP/s, 32 trees 166 us.
 #pragma once
 
 #include "aasd_kv_tile.cuh"
@@ -31,35 +32,44 @@
 
 namespace aasd {
 
-constexpr int kByteSoftmax = 16;                                 // softmax warps
-constexpr int kByteTileThreads = 32 * (kByteSoftmax + 8);        // and 4 unpackers, two issuers, loader, walker
-// Registers per thread: the softmax warps take what the others give up of the launch's.
-constexpr int kByteLaunchRegs = 80, kByteSoftmaxRegs = 96, kByteOtherRegs = 48;
-static_assert(kByteSoftmax * kByteSoftmaxRegs + 8 * kByteOtherRegs <= (kByteSoftmax + 8) * kByteLaunchRegs, "the shares add up to the launch's registers");
-constexpr int kByteRaw = 5, kByteValues = 4, kByteScales = 8;   // ring depths, in pages
+// What depends on the channels.  256 of them leave room for one group: O takes half of tensor memory, a page 32 KB and its values
+// in fp16 as much.
+template <int D>
+struct KvbTileShape {
+    static constexpr int kGroups = D == 256 ? 1 : 2;
+    static constexpr int kSoftmax = 8 * kGroups;                           // softmax warps
+    static constexpr int kThreads = 32 * (kSoftmax + 8);                   // and 4 unpackers, two issuers (one without work in a single group), loader, walker
+    static constexpr int kRaw = D == 256 ? 2 : 5, kValues = D == 256 ? 2 : 4;   // ring depths, in pages
+    // Registers per thread: the softmax warps take what the others give up of the launch's (fewer threads have enough).
+    static constexpr int kLaunchRegs = D == 256 ? 128 : 80, kSoftmaxRegs = D == 256 ? 128 : 96, kOtherRegs = D == 256 ? 128 : 48;
+    static_assert(kSoftmax * kSoftmaxRegs + 8 * kOtherRegs <= (kSoftmax + 8) * kLaunchRegs, "the shares add up to the launch's registers");
+};
+constexpr int kByteScales = 8;                                             // ring depth of the scales, in pages
 // Where a page's scale of the values is this much below the largest (in powers of two), the row's maximum is looked for: fp16's
 // range says nothing about probabilities that were scaled down so far.
 constexpr int kByteFar = 30;
 
 template <int D, bool PAIR>
 struct KvbTileShared {
+    using Shape = KvbTileShape<D>;
+    static constexpr int kRaw = Shape::kRaw, kValues = Shape::kValues, kThreads = Shape::kThreads;
     static constexpr int R = PAIR ? 2 * kTileRows : kTileRows;
-    alignas(1024) unsigned char queries[PAIR ? 2 : 1][kTileRows * D * 2];   // D = 128: a panel of 128 bytes per row for each of a query's numbers, D = 64: the halves of one
-    alignas(1024) unsigned char raw[kByteRaw][2 * kPage * D];
-    alignas(1024) unsigned char values[kByteValues][kPage * D * 2];
+    alignas(1024) unsigned char queries[PAIR ? 2 : 1][kTileRows * D * 2];   // panels of 128 bytes per row, a query's first numbers, then its second ones (D = 64: the halves of one)
+    alignas(1024) unsigned char raw[kRaw][2 * kPage * D];
+    alignas(1024) unsigned char values[kValues][kPage * D * 2];
     alignas(16) uint4 scale[kByteScales];         // as they lie in the page
-    int missing[kByteScales], raw_missing[kByteRaw];
+    int missing[kByteScales], raw_missing[kRaw];
     float row_q[PAIR ? 2 : 1][kTileRows];         // what the rows' queries were divided by, times the scale of the products
     float exchange_m[kTileRows], exchange_l[kTileRows], exchange_up[kTileRows];   // between the groups, where they share a tile
-    int base[kByteTileThreads];
-    long long scan[kByteTileThreads / 32];
+    int base[kThreads];
+    long long scan[kThreads / 32];
     KvTilePiece piece[kTilePieces];
     KvShares shares;
     KvPiece open;                      // the segment that begins in this CTA and ends in another
     u64 piece_full[kTilePieces], piece_empty[kTilePieces];
-    u64 raw_full[kByteRaw], raw_empty[kByteRaw];
+    u64 raw_full[kRaw], raw_empty[kRaw];
     u64 scale_empty[kByteScales];
-    u64 v_full[kByteValues], v_empty[kByteValues];
+    u64 v_full[kValues], v_empty[kValues];
     u64 q_full[2], s_full[2][2], p_full[2][2], o_done[2][2], x_full, x_empty, r_full, drain[2];
     unsigned int tmem;
     int abort_flag, padding;
@@ -145,9 +155,13 @@ __device__ __forceinline__ void kvb_scale_o(unsigned int col_o, const float (&fo
 }
 
 template <int D, bool PAIR>
-__global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(const KvAttendArgs a) {
+__global__ void __launch_bounds__(KvbTileShape<D>::kThreads, 1) kvb_attend_tile_kernel(const KvAttendArgs a) {
+    using Shape = KvbTileShape<D>;
     using Shared = KvbTileShared<D, PAIR>;
-    constexpr int R = Shared::R, STEP = PAIR ? 1 : 2;              // pages from one of a group to its next
+    static_assert(!PAIR || Shape::kGroups == 2, "a tile for each group");
+    constexpr int kByteSoftmax = Shape::kSoftmax, kByteTileThreads = Shape::kThreads, kByteRaw = Shape::kRaw, kByteValues = Shape::kValues;
+    constexpr bool ALT = !PAIR && Shape::kGroups == 2;             // the groups take alternate pages
+    constexpr int R = Shared::R, STEP = ALT ? 2 : 1;               // pages from one of a group to its next
     constexpr unsigned int kColS = 0, kColO = 256, kStep = 128;    // first columns of group 0's S and O; group 1's are kStep behind
     constexpr unsigned int kIdescS = tc_idesc(kPage, false), kIdescO = tc_idesc(D, false) | kTcRowsB;
     extern __shared__ unsigned char smem_raw[];
@@ -158,7 +172,7 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
 #pragma unroll 1
         for (int i = 0; i < kTilePieces; ++i) {
             mbar_init(&sh.piece_full[i], 1);
-            mbar_init(&sh.piece_empty[i], kByteSoftmax + 4 + 2 + 1);
+            mbar_init(&sh.piece_empty[i], kByteSoftmax + 4 + Shape::kGroups + 1);
         }
 #pragma unroll 1
         for (int i = 0; i < kByteRaw; ++i) {
@@ -167,7 +181,7 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
         }
 #pragma unroll 1
         for (int i = 0; i < kByteScales; ++i) {
-            mbar_init(&sh.scale_empty[i], PAIR ? kByteSoftmax : kByteSoftmax / 2);
+            mbar_init(&sh.scale_empty[i], PAIR ? 16 : 8);
         }
 #pragma unroll 1
         for (int i = 0; i < kByteValues; ++i) {
@@ -176,17 +190,17 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
         }
 #pragma unroll 1
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&sh.q_full[i], kByteSoftmax / 2);
+            mbar_init(&sh.q_full[i], 8);
             for (int b = 0; b < 2; ++b) {
                 mbar_init(&sh.s_full[i][b], 2);    // the products' end, and the issuer's word
-                mbar_init(&sh.p_full[i][b], kByteSoftmax / 2);
+                mbar_init(&sh.p_full[i][b], 8);
                 mbar_init(&sh.o_done[i][b], 1);
             }
             mbar_init(&sh.drain[i], 1);
         }
-        mbar_init(&sh.x_full, kByteSoftmax / 2);
-        mbar_init(&sh.x_empty, kByteSoftmax / 2);
-        mbar_init(&sh.r_full, kByteSoftmax / 2);
+        mbar_init(&sh.x_full, 8);
+        mbar_init(&sh.x_empty, 8);
+        mbar_init(&sh.r_full, 8);
         sh.abort_flag = 0;
         sh.open.seg = -1;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -223,7 +237,7 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
     bool ok = true;
 
     if (warp >= kByteSoftmax + 4) {
-        fewer_registers<kByteOtherRegs>();
+        if (Shape::kOtherRegs < Shape::kLaunchRegs) fewer_registers<Shape::kOtherRegs>();
         if (warp == kByteSoftmax + 7) {
             // ---- walker
             if (lane == 0) ok = kv_tile_walk(a, sh, total, strip, R, G, wait_one);
@@ -275,7 +289,7 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
             for (int k = max(0, n - kByteRaw); k < n; ++k)
 #pragma unroll 1
                 for (unsigned int it = 0; it < a.wait_limit && !mbar_try_wait(&sh.raw_full[k % kByteRaw], (k / kByteRaw) & 1); ++it) {}
-        } else {
+        } else if (Shape::kGroups == 2 || warp == kByteSoftmax + 4) {
             // ---- issuers, one for each group
             const int x = __shfl_sync(0xFFFFFFFFu, (warp - kByteSoftmax - 4) >> 1, 0);
             const unsigned int tmem = __shfl_sync(0xFFFFFFFFu, tm, 0) + x * kStep;
@@ -288,7 +302,7 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
             // pages ahead, but not into the next piece: its queries come when this one's last page is in O.
             KvRing<kByteRaw> raw;
             KvRing<kByteValues> val;
-            if (!PAIR && x == 1) {
+            if (ALT && x == 1) {
                 raw.next();
                 val.next();
             }
@@ -302,7 +316,7 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
                 if (elect_one()) mbar_arrive(&sh.piece_empty[k % kTilePieces]);
                 ok = wait(&sh.q_full[x], k & 1);
                 if (!ok) break;
-                const int first = PAIR ? 0 : (n0 ^ x) & 1;
+                const int first = ALT ? (n0 ^ x) & 1 : 0;
                 int ahead = first, asked = taken;
 #pragma unroll 1
                 for (int i = first; i < np; i += STEP, ++taken) {
@@ -315,8 +329,9 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
                         const unsigned int keys = k0 + raw.slot * (2 * kPage * D / 16), to = tmem + kColS + buf * 64;
 #pragma unroll
                         for (int ks = 0; ks < 2 * (D / 32); ++ks) {   // (the queries' first numbers, then their second ones; descriptors count 16 bytes)
-                            const int second = ks / (D / 32), j = ks % (D / 32);
-                            tc_mma_bytes(to, q0 + second * (D == 64 ? 4 : kTileRows * 8) + j * 2, q_high, keys + j * 2, k_high, kIdescS, ks > 0);
+                            const int second = ks / (D / 32), j = ks % (D / 32), panel = j / 4;
+                            tc_mma_bytes(to, q0 + (D == 64 ? second * 4 : (second * (D / 128) + panel) * (kTileRows * 8)) + (j % 4) * 2, q_high,
+                                         keys + panel * (kPage * 8) + (j % 4) * 2, k_high, kIdescS, ks > 0);
                         }
                         tc_commit_one(smem_u32(&sh.s_full[x][buf]));
                         tc_commit_one(smem_u32(&sh.raw_empty[raw.slot]));
@@ -347,15 +362,15 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
         }
     } else if (warp >= kByteSoftmax) {
         // ---- unpackers: a lane takes 16 channels of a token at a time, and eight neighbouring lanes write to eight different chunks
-        fewer_registers<kByteOtherRegs>();
+        if (Shape::kOtherRegs < Shape::kLaunchRegs) fewer_registers<Shape::kOtherRegs>();
         constexpr int C = D / 16, TS = 128 / C;      // chunks of a token; tokens at a time
         const int u = tid - 32 * kByteSoftmax, chunk = u % C, t0 = u / C;
         // (t % 8 is the same for all of a lane's tokens: one address, 128 TS bytes apart)
         static_assert(TS % 8 == 0, "the swizzle repeats");
         const int from = kvb_value_offset(D) + kvb_chunk_offset(D, t0, chunk);
-        const int second = chunk >> 2;               // (D = 128: the panels' lanes store their halves in turn)
-        const int to0 = second * (kPage * 128) + t0 * 128 + (((2 * (chunk & 3) + second) ^ (t0 & 7)) << 4);
-        const int to1 = second * (kPage * 128) + t0 * 128 + (((2 * (chunk & 3) + 1 - second) ^ (t0 & 7)) << 4);
+        const int panel = chunk >> 2, second = panel & 1;   // (neighbouring panels' lanes store their halves in turn)
+        const int to0 = panel * (kPage * 128) + t0 * 128 + (((2 * (chunk & 3) + second) ^ (t0 & 7)) << 4);
+        const int to1 = panel * (kPage * 128) + t0 * 128 + (((2 * (chunk & 3) + 1 - second) ^ (t0 & 7)) << 4);
         KvRing<kByteRaw> raw;
         KvRing<kByteValues> val;
 #pragma unroll 1
@@ -400,10 +415,10 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
         }
     } else {
         // ---- softmax: thread (g, j) of a warp has rows g and g + 8 of the warp's 16 and two columns of every eight
-        more_registers<kByteSoftmaxRegs>();
+        if (Shape::kSoftmaxRegs > Shape::kLaunchRegs) more_registers<Shape::kSoftmaxRegs>();
         constexpr int Q = 2;                         // rows of a thread
         // (of the group's 128 rows; a warp reaches the 32 lanes of tensor memory that its number gives it)
-        const int x = warp / (kByteSoftmax / 2), g = lane >> 2, j = lane & 3, row_base = (warp & 3) * 32 + ((warp >> 2) & 1) * 16;
+        const int x = warp / (8), g = lane >> 2, j = lane & 3, row_base = (warp & 3) * 32 + ((warp >> 2) & 1) * 16;
         const unsigned int lanes = (unsigned int)row_base << 16;
         const unsigned int col_s = tm + kColS + x * kStep + lanes, col_o = tm + kColO + x * kStep + lanes;
         static_assert((kByteScales & (kByteScales - 1)) == 0, "a slot is a page's number, cut off");
@@ -484,16 +499,17 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
                         }
                         if (top[k] >= 0x7F800000u) hi[0] = hi[1] = 0x7F7F7F7Fu;
                         const int chunk = part >> 1;     // of 16 channels
-                        unsigned char* row = to + r * 128 + 8 * (part & 1);
-                        *reinterpret_cast<uint2*>(row + ((chunk ^ (r & 7)) << 4)) = make_uint2(hi[0], hi[1]);
-                        *reinterpret_cast<uint2*>(row + (D == 64 ? ((chunk + 4) ^ (r & 7)) << 4 : kTileRows * 128 + ((chunk ^ (r & 7)) << 4))) = make_uint2(lo[0], lo[1]);
+                        unsigned char* row = to + r * 128 + 8 * (part & 1) + (chunk >> 3) * (kTileRows * 128);
+                        const int at16 = ((chunk & 7) ^ (r & 7)) << 4;
+                        *reinterpret_cast<uint2*>(row + at16) = make_uint2(hi[0], hi[1]);
+                        *reinterpret_cast<uint2*>(row + (D == 64 ? ((chunk + 4) ^ (r & 7)) << 4 : D / 128 * (kTileRows * 128) + at16)) = make_uint2(lo[0], lo[1]);
                         if (part == 0) sh.row_q[PAIR ? x : 0][r] = a.scale_log2 * kvb_pow2(e - 7);
                     }
                 }
                 fence_async_smem();
                 __syncwarp();
             }
-            if (!PAIR) {
+            if (ALT) {
                 // one set of queries for both groups
                 if (x == 0) {
                     if (lane == 0) mbar_arrive(&sh.r_full);
@@ -519,7 +535,7 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
             bool first = true, large = false;
             const int first_pg = w.pg;
 #pragma unroll 1
-            for (int i = PAIR ? 0 : (n0 ^ x) & 1; i < np; i += STEP) {
+            for (int i = ALT ? (n0 ^ x) & 1 : 0; i < np; i += STEP) {
                 const int pg = first_pg + i, buf = taken & 1, slot = (n0 + i) & (kByteScales - 1);
                 const unsigned int col = col_s + buf * 64;
                 ok = wait(&sh.s_full[x][buf], (taken >> 1) & 1);   // (the page's scales came with its codes)
@@ -656,7 +672,7 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
                 own[q] = unscale;
                 other[q] = 0.f;
             }
-            if (!PAIR) {
+            if (ALT) {
                 // group 0 reads both groups' O (the same lanes of tensor memory)
                 if (x == 1) {
 #pragma unroll
@@ -689,7 +705,7 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
                 }
             }
             if (PAIR || x == 0) {
-                const bool any1 = !PAIR && sh.exchange_up[row_base] != 0.f;   // (the same for every row)
+                const bool any1 = ALT && sh.exchange_up[row_base] != 0.f;   // (the same for every row)
                 // the results go through the places of the warp's own queries, which have been used
                 const auto stage = [&](int lr, int chunk) {
                     return sh.queries[PAIR ? x : 0] + (row_base + lr) * 128 + (chunk >> 3) * (kTileRows * 128) + (((chunk & 7) ^ (lr & 7)) << 4);
@@ -768,7 +784,7 @@ __global__ void __launch_bounds__(kByteTileThreads, 1) kvb_attend_tile_kernel(co
                 }
                 if (!complete && which == 1 && tid == 0) sh.open = KvPiece{w.seg, w.pages, w.h, w.tile * R, rows, w.first};
             }
-            if (!PAIR && x == 0) {   // group 1 may go on
+            if (ALT && x == 0) {   // group 1 may go on
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.x_empty);

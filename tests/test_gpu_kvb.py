@@ -286,7 +286,7 @@ ATTENDS = [  # sequences, new tokens (most), longest context, query heads, key h
     (2, 1, 130, 28, 4, 128, "f32"), (1, 1, 1500, 16, 2, 128, "bf16"), (5, 9, 150, 8, 2, 128, "bf16"), (3, 17, 140, 7, 1, 64, "bf16"),
     (2, 33, 64, 8, 2, 128, "bf16"), (2, 33, 65, 4, 4, 256, "bf16"), (2, 20, 63, 6, 2, 256, "f32"), (1, 70, 100, 8, 1, 128, "bf16"),
     (2, 150, 30, 4, 2, 64, "bf16"), (1, 200, 1, 2, 1, 128, "f32"), (1, 300, 500, 2, 1, 128, "bf16"), (9, 2, 128, 40, 8, 64, "bf16"),
-    (2, 90, 127, 3, 1, 256, "bf16")]
+    (2, 90, 127, 3, 1, 256, "bf16"), (1, 70, 100, 8, 1, 256, "bf16"), (5, 9, 300, 6, 2, 256, "bf16"), (1, 300, 500, 2, 1, 256, "bf16")]
 
 
 @pytest.mark.parametrize("B,new,longest,Hq,Hkv,D,dtype", ATTENDS)
@@ -317,7 +317,9 @@ LONG = [  # sequences, new tokens, contexts from .. to, query heads, key heads, 
     (64, 2, 0, 2000, 32, 4, 128, "bf16", True), (48, 33, 700, 2200, 16, 8, 128, "bf16", True), (60, 33, 0, 1800, 32, 8, 128, "bf16", True),
     (70, 17, 1, 2500, 10, 5, 64, "bf16", True), (3, 1500, 0, 700, 16, 4, 128, "bf16", False), (2, 1100, 300, 900, 16, 8, 64, "bf16", False),
     (9, 65, 1000, 1400, 8, 8, 128, "bf16", False), (40, 5, 600, 1900, 8, 2, 128, "f32", True), (20, 1, 10, 2000, 32, 8, 64, "f32", False),
-    (2, 400, 100, 600, 4, 2, 256, "bf16", False), (1, 64, 20000, 20000, 8, 2, 128, "bf16", False)]
+    (2, 400, 100, 600, 4, 2, 256, "bf16", False), (1, 64, 20000, 20000, 8, 2, 128, "bf16", False),
+    (1, 40, 20000, 20000, 4, 2, 256, "bf16", False), (48, 33, 700, 2200, 8, 4, 256, "bf16", True), (3, 1500, 0, 700, 4, 1, 256, "bf16", False),
+    (60, 3, 0, 1800, 16, 4, 256, "bf16", True)]
 
 
 @pytest.mark.parametrize("B,new,lo,hi,Hq,Hkv,D,dtype,trees", LONG)
@@ -377,43 +379,43 @@ def test_attend_long(ctx, B, new, lo, hi, Hq, Hkv, D, dtype, trees):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("G", [3, 60])                   # few rows, and many
-def test_attend_with_large_products_and_values_of_any_size(ctx, dtype, G):
+@pytest.mark.parametrize("G,D", [(3, 128), (60, 128), (60, 256)])                   # few rows, and many
+def test_attend_with_large_products_and_values_of_any_size(ctx, dtype, G, D):
     """Sharp softmaxes, scales of the pages far from 1 and from each other."""
     rng = np.random.default_rng(3)
     for kscale, vscale, qscale in ((4.0, 1e-4, 3.0), (0.01, 3e4, 1.0), (1.0, 1.0, 1e3), (1e-3, 1.0, 1e-3), (1.0, 1e30, 1.0), (1e-15, 1e-25, 1e15), (300.0, 1.0, 300.0)):
-        pool = Pool(rng, [300, 70], 2, 128, kscale, vscale)
-        q = torch.as_tensor(rng.standard_normal((2, 2 * G, 128)).astype(np.float32) * qscale).to(DT[dtype]).cuda()
+        pool = Pool(rng, [300, 70], 2, D, kscale, vscale)
+        q = torch.as_tensor(rng.standard_normal((2, 2 * G, D)).astype(np.float32) * qscale).to(DT[dtype]).cuda()
         check_attend(ctx, pool, q, [299, 69], [0, 1, 2], 1, None)
 
 
-@pytest.mark.parametrize("G", [3, 60])
-def test_attend_where_a_pages_values_dwarf_the_others(ctx, G):
+@pytest.mark.parametrize("G,D", [(3, 64), (60, 64), (60, 256)])
+def test_attend_where_a_pages_values_dwarf_the_others(ctx, G, D):
     rng = np.random.default_rng(4)
     for sizes in ((1.0, 1e5, 1e-5), (1e-6, 1.0, 1e6), (1e4, 1.0, 1e-8)):
-        pool = Pool(rng, [0], 1, 64)
+        pool = Pool(rng, [0], 1, D)
         pool.rows, pool.table, n = tables(rng, [190])
-        raw = np.full((n, 1, ref.head_bytes(64)), 0x7F, np.uint8)
-        k = rng.standard_normal((190, 1, 64)).astype(np.float32)
-        v = rng.standard_normal((190, 1, 64)).astype(np.float32)
+        raw = np.full((n, 1, ref.head_bytes(D)), 0x7F, np.uint8)
+        k = rng.standard_normal((190, 1, D)).astype(np.float32)
+        v = rng.standard_normal((190, 1, D)).astype(np.float32)
         for pg, s in enumerate(sizes):
             v[pg * PAGE:(pg + 1) * PAGE] *= s
-        ref.write(raw, pool.rows, [0], [190], [0], k, v, 64)
-        e = [ref.load(raw, pool.rows[0][c // PAGE] * PAGE + c % PAGE, 64) for c in range(190)]
+        ref.write(raw, pool.rows, [0], [190], [0], k, v, D)
+        e = [ref.load(raw, pool.rows[0][c // PAGE] * PAGE + c % PAGE, D) for c in range(190)]
         pool.k, pool.v, pool.kv_len = [np.asarray([x[0] for x in e])], [np.asarray([x[1] for x in e])], [190]
         pool.pages = torch.as_tensor(raw).cuda()
         for dtype in ("bf16", "f32"):
-            q = torch.as_tensor(rng.standard_normal((1, G, 64)).astype(np.float32)).to(DT[dtype]).cuda()
+            q = torch.as_tensor(rng.standard_normal((1, G, D)).astype(np.float32)).to(DT[dtype]).cuda()
             check_attend(ctx, pool, q, [189], [0, 1], 1, None)
 
 
-@pytest.mark.parametrize("G", [2, 64])
-def test_attend_scale_and_unaligned_queries(ctx, G):
+@pytest.mark.parametrize("G,D", [(2, 64), (64, 64), (64, 256)])
+def test_attend_scale_and_unaligned_queries(ctx, G, D):
     rng = np.random.default_rng(8)
-    pool = Pool(rng, [90, 10], 2, 64)
+    pool = Pool(rng, [90, 10], 2, D)
     for dtype in ("bf16", "f32"):
-        buf = torch.as_tensor(rng.standard_normal((2, 2 * G * 64 + 3)).astype(np.float32)).to(DT[dtype]).cuda()
-        q = buf[:, 1:1 + 2 * G * 64].unflatten(1, (2 * G, 64))
+        buf = torch.as_tensor(rng.standard_normal((2, 2 * G * D + 3)).astype(np.float32)).to(DT[dtype]).cuda()
+        q = buf[:, 1:1 + 2 * G * D].unflatten(1, (2 * G, D))
         check_attend(ctx, pool, q, [89, 9], [0, 1, 2], 1, None, scale=0.37)
 
 
@@ -470,14 +472,14 @@ def test_attend_reports_bad_tables_and_parents(ctx, rows):
     assert ctx.poll_status() == binding.STATUS_BAD_OFFSETS and torch.isfinite(o["out"]).all()
 
 
-@pytest.mark.parametrize("rows", [1, 30])
-def test_rows_that_no_sequence_owns_give_zeros(ctx, rows):
+@pytest.mark.parametrize("rows,D", [(1, 128), (30, 128), (30, 256)])
+def test_rows_that_no_sequence_owns_give_zeros(ctx, rows, D):
     rng = np.random.default_rng(11)
-    pool = Pool(rng, [64 + rows, rows], 2, 128)
+    pool = Pool(rng, [64 + rows, rows], 2, D)
     T = 2 * rows + 7
-    q = torch.as_tensor(rng.standard_normal((T, 8, 128)).astype(np.float32)).to(torch.bfloat16).cuda()
+    q = torch.as_tensor(rng.standard_normal((T, 8, D)).astype(np.float32)).to(torch.bfloat16).cuda()
     q[-2:] = float("nan")
-    out = dict(out=torch.full((T, 8, 128), 3.0, dtype=torch.bfloat16, device="cuda"), lse=torch.full((T, 8), 3.0, device="cuda"))
+    out = dict(out=torch.full((T, 8, D), 3.0, dtype=torch.bfloat16, device="cuda"), lse=torch.full((T, 8), 3.0, device="cuda"))
     offs = [3, 3 + rows, 3 + 2 * rows]
     ctx.kvb_attend(q, pool.pages, i32(pool.table), i32([64, 0]), i32(pool.kv_len), tok_offsets=i32(offs), outputs=out)
     assert ctx.poll_status() == 0

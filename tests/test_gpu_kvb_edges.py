@@ -13,10 +13,11 @@ i32 = kvb.i32
 @pytest.fixture(scope="module")
 def long_pools():
     rng = np.random.default_rng(20)
-    return {D: kvb.Pool(rng, [2000], 2, D) for D in (64, 128)}
+    return {D: kvb.Pool(rng, [2000], 2, D) for D in (64, 128, 256)}
 
 
-@pytest.mark.parametrize("new,D,dtype,page", [(1, 128, "bf16", 1), (1, 64, "f32", 0), (40, 128, "bf16", 2), (200, 128, "bf16", 0), (40, 64, "bf16", 4), (200, 64, "bf16", 1)])
+@pytest.mark.parametrize("new,D,dtype,page", [(1, 128, "bf16", 1), (1, 64, "f32", 0), (40, 128, "bf16", 2), (200, 128, "bf16", 0), (40, 64, "bf16", 4), (200, 64, "bf16", 1),
+                                             (40, 256, "bf16", 1)])
 def test_a_wait_that_runs_out_ends_the_call_and_the_context_recovers(long_pools, new, D, dtype, page):
     """One of the first CTA's pages never arrives: its waits run out, the call ends by itself and the status word says so.  Nothing
     faults; with the scratch registered again the same call gives what it gave."""
