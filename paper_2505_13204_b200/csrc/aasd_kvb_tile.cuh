@@ -24,7 +24,9 @@
 // rest scaling, sums, packing and storing of P.  Measured: 2 x 2048 tokens of a prompt (32 over 8 heads of 128, bf16) 193 to 219
 // us from GPU to GPU, 627 to 712 TFLOP/s; 32 draft trees of 33 over about 3800 tokens 158 to 162 us; 64 tokens over 65536 98 to 102 us.  Eight warps of 32 rows
 // took 236 us for the first (fewer waits, but half as many warps to hide them), exponentials in turns of the two groups 233.
-// With 256 channels (16 over 4 heads): the same prompt behind 1000 tokens 199 us, 684 TFLOP/s, 32 trees 166 us.
+// With 256 channels (16 over 4 heads): the same prompt behind 1000 tokens 199 us, 684 TFLOP/s, 32 trees 166 us.  There a page takes
+// about 2000 cycles of which shared memory is busy with operands, copies and unpacking for 1660 (without the softmax warps' work 5 % less;
+// with eight unpackers no less).
 #pragma once
 
 #include "aasd_kv_tile.cuh"
