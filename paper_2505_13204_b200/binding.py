@@ -915,7 +915,7 @@ class Context:
         n = src_seq.numel()
         o = outputs
         if o is None:
-            new_len, copy_src, copy_dst = src_seq.new_empty((3, n)).unbind()
+            new_len, copy_src, copy_dst = torch.empty_like(src_seq), torch.empty_like(src_seq), torch.empty_like(src_seq)
             o = dict(new_len=new_len, copy_src=copy_src, copy_dst=copy_dst)
         else:
             new_len, copy_src, copy_dst = o["new_len"], o["copy_src"], o["copy_dst"]
@@ -944,10 +944,10 @@ class Context:
         B, P, N, prm, books = self._kv_books(block_table, seq_pages, free_pages, n_free, page_shares)
         o = outputs
         if o is None:
-            page_map, n_moved, moves = free_pages.new_empty(2 * N + 1).split((N, 1, N))
+            page_map, n_moved, moves = torch.empty_like(free_pages), free_pages.new_empty(1), torch.empty_like(free_pages)
             o = dict(page_map=page_map, n_moved=n_moved)
         else:
-            page_map, n_moved, moves = o["page_map"], o["n_moved"], free_pages.new_empty(N)
+            page_map, n_moved, moves = o["page_map"], o["n_moved"], torch.empty_like(free_pages)
             _kv_i32(self.device_index, page_map, n_moved)
             _kv_need(page_map.numel() >= N and n_moved.numel() > 0, "outputs")
         pool = self._kv_layers(pages, N)

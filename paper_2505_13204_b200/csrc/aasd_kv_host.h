@@ -20,7 +20,7 @@ constexpr KvScratch kv_attend_scratch(int head_dim) {
     KvScratch L{};
     // a scratch for one head dimension serves the smaller ones too
     const size_t D = (size_t)head_dim, W = 12;
-    const size_t part = 2 * kTileRows * ((D < 128 ? D : 128) + 2);   // the largest: two tiles of 128 rows (head_dim 256 has parts of 8 rows)
+    const size_t part = 2 * kTileRows * ((D < 128 ? D : 128) + 2);   // the largest: two tiles of 128 rows (one with head_dim 256)
     L.zero_bytes = align_up(4 * kKvMaxCtas, 256);
     L.off_open = L.zero_bytes;
     L.off_cta = align_up(L.off_open + kKvMaxCtas * sizeof(KvTileOpen), 256);

@@ -38,6 +38,8 @@ int launch_tile(const LaunchEnv& env, int sm_count, const KvAttendArgs& a) {
     constexpr auto kernel = kvb_attend_tile_kernel<D, PAIR>;
     constexpr size_t smem = sizeof(KvbTileShared<D, PAIR>) + 1024;   // (its first member wants a 1024-byte boundary)
     static_assert(smem <= 227 * 1024, "fits an SM");
+    constexpr KvScratch L = kv_attend_scratch(D);
+    static_assert((size_t)kKvMaxCtas * 2 * KvbTileShared<D, PAIR>::R * (D + 2) * 4 <= L.off_warp - L.off_cta, "the parts fit the scratch");
     if (enable_smem<kernel, smem>(env.device) != AASD_OK) return AASD_ERR_CUDA;
     // the softmax warps wait for registers that the launch must have brought along
     static const bool enough = [] {

@@ -110,6 +110,15 @@ __device__ __forceinline__ void tc_mma_bytes(unsigned int d, unsigned int a, uns
             "r"(a), "r"(a_high), "r"(b), "r"(b_high), "r"(idesc), "r"(add ? 1u : 0u)
             : "memory");
 }
+// ... with A in tensor memory, four numbers in a cell
+__device__ __forceinline__ void tc_mma_bytes(unsigned int d, unsigned int a, unsigned int b, unsigned int b_high, unsigned int idesc, bool add) {
+    if (elect_one())
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.b64 y, {%2, %3};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], y, %4, p;\n\t}" ::"r"(d),
+            "r"(a), "r"(b), "r"(b_high), "r"(idesc), "r"(add ? 1u : 0u)
+            : "memory");
+}
 // ... A B, fp16 both, A in tensor memory
 __device__ __forceinline__ void tc_mma_halves(unsigned int d, unsigned int a, unsigned int b, unsigned int b_high, unsigned int idesc, bool add) {
     if (elect_one())
@@ -164,7 +173,7 @@ __global__ void __launch_bounds__(KvbTileShape<D>::kThreads, 1) kvb_attend_tile_
     constexpr int kByteSoftmax = Shape::kSoftmax, kByteTileThreads = Shape::kThreads, kByteRaw = Shape::kRaw, kByteValues = Shape::kValues;
     constexpr bool ALT = !PAIR && Shape::kGroups == 2;             // the groups take alternate pages
     constexpr int R = Shared::R, STEP = ALT ? 2 : 1;               // pages from one of a group to its next
-    constexpr unsigned int kColS = 0, kColO = 256, kStep = 128;    // first columns of group 0's S and O; group 1's are kStep behind
+    constexpr unsigned int kColS = 0, kColQ = 128, kColO = 256, kStep = 128;    // first columns of group 0's S and O; group 1's are kStep behind
     constexpr unsigned int kIdescS = tc_idesc(kPage, false), kIdescO = tc_idesc(D, false) | kTcRowsB;
     extern __shared__ unsigned char smem_raw[];
     Shared& sh = *reinterpret_cast<Shared*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
@@ -332,8 +341,11 @@ __global__ void __launch_bounds__(KvbTileShape<D>::kThreads, 1) kvb_attend_tile_
 #pragma unroll
                         for (int ks = 0; ks < 2 * (D / 32); ++ks) {   // (the queries' first numbers, then their second ones; descriptors count 16 bytes)
                             const int second = ks / (D / 32), j = ks % (D / 32), panel = j / 4;
-                            tc_mma_bytes(to, q0 + (D == 64 ? second * 4 : (second * (D / 128) + panel) * (kTileRows * 8)) + (j % 4) * 2, q_high,
-                                         keys + panel * (kPage * 8) + (j % 4) * 2, k_high, kIdescS, ks > 0);
+                            if (D == 256)
+                                tc_mma_bytes(to, tmem + kColQ + ks * 8, keys + panel * (kPage * 8) + (j % 4) * 2, k_high, kIdescS, ks > 0);
+                            else
+                                tc_mma_bytes(to, q0 + (D == 64 ? second * 4 : (second * (D / 128) + panel) * (kTileRows * 8)) + (j % 4) * 2, q_high,
+                                             keys + panel * (kPage * 8) + (j % 4) * 2, k_high, kIdescS, ks > 0);
                         }
                         tc_commit_one(smem_u32(&sh.s_full[x][buf]));
                         tc_commit_one(smem_u32(&sh.raw_empty[raw.slot]));
@@ -508,7 +520,28 @@ __global__ void __launch_bounds__(KvbTileShape<D>::kThreads, 1) kvb_attend_tile_
                         if (part == 0) sh.row_q[PAIR ? x : 0][r] = a.scale_log2 * kvb_pow2(e - 7);
                     }
                 }
-                fence_async_smem();
+                if (D == 256) {
+                    // .. and on to tensor memory: thread (g, j) has eight channels of every 32
+                    __syncwarp();
+#pragma unroll 1
+                    for (int cb = 0; cb < 2 * D / 4; cb += 32) {   // 32 cells of four channels
+                        float x[16];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const int r = row_base + g + 8 * e, byte = 4 * cb + 32 * k + 8 * j;
+                                const float2 v = *reinterpret_cast<const float2*>(to + (byte >> 7) * (kTileRows * 128) + r * 128 + ((((byte >> 4) & 7) ^ (r & 7)) << 4) + (byte & 8));
+                                x[4 * k + 2 * e] = v.x;
+                                x[4 * k + 2 * e + 1] = v.y;
+                            }
+                        tc_store(tm + lanes + kColQ + cb, x);
+                    }
+                    tc_wait_store();
+                    tc_fence_before();
+                } else {
+                    fence_async_smem();
+                }
                 __syncwarp();
             }
             if (ALT) {
