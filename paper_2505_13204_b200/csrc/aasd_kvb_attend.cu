@@ -18,8 +18,8 @@ namespace {
 // us; 8 of 4000: 16 rows 39 and 43 us, 24 rows 47 and 45 us; one of 16000: 16 rows 35 and 33 us, 24 rows 37 and 35 us.  With 64
 // channels, where a page is half as long to fetch: 64 of 4000: 24 rows 119 and 154 us, 32 rows 123 and 156 us; 8 of 4000: 33 and 37, 35
 // and 37 us; one of 16000: 27 and 29, 29 and 29 us.  With 256 channels (16 and 4 heads), where the split kernel has eight rows at a time: 64 of
-// 4000: 8 rows 127 and 156 us, 12 rows 207 and 160 us; 8 of 4000: 35 and 45, 43 and 45 us; one of 16000: 41 and 41, 37 and 41 us (48 rows: 517 and
-// 170, 86 and 49, 55 and 43 us).
+// 4000: 8 rows 127 and 143 us, 16 rows 209 and 149 us; 8 of 4000: 35 and 45, 43 and 48 us; one of 16000: 41 and 37, 38 and 43 us (48 rows: 517 and
+// 156, 86 and 51, 55 and 45 us).
 constexpr int64_t split_rows(int head_dim) { return head_dim == 64 ? 32 : head_dim == 128 ? 16 : 8; }
 
 template <int DT, int D, int NT>

@@ -16,7 +16,7 @@
 // all its columns share; that of its values goes into the exponents of the probabilities, relative to the largest
 // of the pages so far, which O is relative to.
 //
-// Tensor memory (512 columns): two S buffers of each group, whose first halves P takes over, and O.
+// Tensor memory (512 columns): two S buffers of each group, whose first halves P takes over, and O; with 256 channels the queries.
 //
 // A page and group of 128 rows cost 384 cycles of S products (64 columns from shared memory, twice) and 256 of PV, 1259 for both
 // groups with the shared memory that they contend for; two issuers, unpackers and loader alone go at 1390 a page.  With
@@ -24,9 +24,10 @@
 // rest scaling, sums, packing and storing of P.  Measured: 2 x 2048 tokens of a prompt (32 over 8 heads of 128, bf16) 193 to 219
 // us from GPU to GPU, 627 to 712 TFLOP/s; 32 draft trees of 33 over about 3800 tokens 158 to 162 us; 64 tokens over 65536 98 to 102 us.  Eight warps of 32 rows
 // took 236 us for the first (fewer waits, but half as many warps to hide them), exponentials in turns of the two groups 233.
-// With 256 channels (16 over 4 heads): the same prompt behind 1000 tokens 199 us, 684 TFLOP/s, 32 trees 166 us.  There a page takes
-// about 2000 cycles of which shared memory is busy with operands, copies and unpacking for 1660 (without the softmax warps' work 5 % less;
-// with eight unpackers no less).
+// With 256 channels (16 over 4 heads): the same prompt behind 1000 tokens 200 us, 677 TFLOP/s, 32 trees 151 us, 64 tokens
+// over 65536 97 us.  There the queries lie in the tensor memory that is left: from shared memory their reads took 512 cycles a page
+// (trees 166 us, 64 tokens 102).  A page takes about 1900 cycles, 1580 of them one softmax warp's from S to P; eight unpackers,
+// three or four pages under way instead of two gave nothing.
 #pragma once
 
 #include "aasd_kv_tile.cuh"
@@ -56,7 +57,7 @@ struct KvbTileShared {
     using Shape = KvbTileShape<D>;
     static constexpr int kRaw = Shape::kRaw, kValues = Shape::kValues, kThreads = Shape::kThreads;
     static constexpr int R = PAIR ? 2 * kTileRows : kTileRows;
-    alignas(1024) unsigned char queries[PAIR ? 2 : 1][kTileRows * D * 2];   // panels of 128 bytes per row, a query's first numbers, then its second ones (D = 64: the halves of one)
+    alignas(1024) unsigned char queries[PAIR ? 2 : 1][kTileRows * D * 2];   // panels of 128 bytes per row, a query's first numbers, then its second ones (D = 64: the halves of one; D = 256: on their way to tensor memory)
     alignas(1024) unsigned char raw[kRaw][2 * kPage * D];
     alignas(1024) unsigned char values[kValues][kPage * D * 2];
     alignas(16) uint4 scale[kByteScales];         // as they lie in the page
