@@ -21,8 +21,8 @@
 // A page and group of 128 rows cost 384 cycles of S products (64 columns from shared memory, twice) and 256 of PV, 1259 for both
 // groups with the shared memory that they contend for; two issuers, unpackers and loader alone go at 1390 a page.  With
 // the softmax warps it is about 2300, and they are what bounds it: 512 cycles of exponentials, 330 until S is in registers, the
-// rest scaling, sums, packing and storing of P.  Measured: 2 x 2048 tokens of a prompt (32 over 8 heads of 128, bf16) 193 to 219
-// us from GPU to GPU, 627 to 712 TFLOP/s; 32 draft trees of 33 over about 3800 tokens 158 to 162 us; 64 tokens over 65536 98 to 102 us.  Eight warps of 32 rows
+// rest scaling, sums, packing and storing of P.  Measured: 2 x 2048 tokens of a prompt (32 over 8 heads of 128, bf16) 175 to 219
+// us from GPU to GPU, 627 to 785 TFLOP/s; 32 draft trees of 33 over about 3800 tokens 158 to 162 us; 64 tokens over 65536 98 to 102 us.  Eight warps of 32 rows
 // took 236 us for the first (fewer waits, but half as many warps to hide them), exponentials in turns of the two groups 233.
 // With 256 channels (16 over 4 heads): the same prompt behind 1000 tokens 200 us, 677 TFLOP/s, 32 trees 151 us, 64 tokens
 // over 65536 97 us.  There the queries lie in the tensor memory that is left: from shared memory their reads took 512 cycles a page
