@@ -614,7 +614,9 @@ typedef struct aasd_kvb_write_params {
  * inputs and of what the pages held.  A row with a NaN or infinity is stored as zeros and raises
  * AASD_STATUS_BAD_ROW; so is (without that status) a row that has a place but no position.  Positions as in aasd_kv_write.  A
  * page outside the pool or the table raises AASD_STATUS_BAD_OFFSETS; its rows are not stored (k_out keeps what it held).  k_out
- * rows of tokens without a place are left as they are.  Two sequences must not share a page that is stored to. */
+ * rows of tokens without a place are left as they are.  q_out and k_out may lie where q and k lie (the same rows: dense ones, or a
+ * single token); lying otherwise over q, k, v or one another is AASD_ERR_INVALID_ARG.  Two sequences must not share a page that
+ * is stored to. */
 int aasd_kvb_write(aasd_ctx* ctx, const void* q, const void* k, const void* v, const void* q_weight,
                    const void* k_weight, const float* cos_sin, const int32_t* positions,
                    const int32_t* block_table, const int32_t* cached_len, const int32_t* kv_len,

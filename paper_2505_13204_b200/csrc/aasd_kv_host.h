@@ -52,7 +52,7 @@ inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 // Whether two arrays have a byte in common.
 inline bool overlap(const void* x, int64_t x_bytes, const void* y, int64_t y_bytes) {
     const uintptr_t a = (uintptr_t)x, b = (uintptr_t)y;
-    return x != nullptr && y != nullptr && a < b + (uintptr_t)y_bytes && b < a + (uintptr_t)x_bytes;
+    return x != nullptr && y != nullptr && x_bytes > 0 && y_bytes > 0 && a < b + (uintptr_t)y_bytes && b < a + (uintptr_t)x_bytes;
 }
 
 // Calls f with the head dimension, or the type, as a constant.

@@ -35,6 +35,22 @@ int aasd_kvb_write(aasd_ctx* ctx, const void* q, const void* k, const void* v, c
     const size_t es = kv_elt_size(p->dtype);
     for (const void* x : {q, k, v, q_weight, k_weight, (const void*)q_out, (const void*)k_out})
         if (((uintptr_t)x % es) != 0) return AASD_ERR_INVALID_ARG;
+    // Rows are read by the lanes that write them, other rows in no order with them: an output lies where its own rows lie, or apart.
+    struct Rows {
+        const void* at;
+        int64_t stride, bytes;   // elements between rows; bytes from the first element to behind the last
+    };
+    const auto rows = [&](const void* x, int64_t stride, int heads) {
+        const int64_t n = (int64_t)heads * D;
+        return Rows{x, stride, n == 0 ? 0 : ((n_tokens - 1) * stride + n) * (int64_t)es};
+    };
+    const auto apart = [](const Rows& x, const Rows& y) { return !overlap(x.at, x.bytes, y.at, y.bytes); };
+    const auto in_place = [&](const Rows& out, const Rows& in) { return out.at == in.at && (n_tokens == 1 || in.stride == out.stride); };
+    const Rows qi = rows(q, p->q_stride, hq), ki = rows(k, p->k_stride, hkv), vi = rows(v, p->v_stride, hkv);
+    const Rows qo = rows(q_out, (int64_t)hq * D, hq), ko = rows(k_out, (int64_t)hkv * D, hkv);
+    if (!(apart(qo, qi) || in_place(qo, qi)) || !(apart(ko, ki) || in_place(ko, ki)) || !apart(qo, ki) || !apart(qo, vi) || !apart(ko, qi) || !apart(ko, vi) ||
+        !apart(qo, ko))
+        return AASD_ERR_INVALID_ARG;
     KvbWriteArgs a{};
     a.w = KvWriteArgs{q, k, v, q_weight, k_weight, cos_sin, positions, nullptr, n_tokens, *p, static_cast<uint8_t*>(pages), q_out, k_out,
                       ctx->state, 0u, make_float2(-0.f, -0.f)};

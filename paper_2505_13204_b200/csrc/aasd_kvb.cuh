@@ -194,8 +194,9 @@ __global__ void __launch_bounds__(kByteThreads, D == 256 ? 1 : kWriteCtas) kvb_w
     unsigned int* scale = reinterpret_cast<unsigned int*>(block + kvb_scale_offset(D)) + (value ? 1 : 0);
     const unsigned int was = q.page >= 0 && q.older > 0 ? *scale : 0u;
     // Row r of the unit, as it is to be stored.  Every lane of the warp comes here; rows with a NaN or infinity, and rows without a
-    // position, become zeros.
-    auto row = [&](int r, bool first, float2(&u)[4], float2(&v)[4]) {
+    // position, become zeros.  first: what there is to say of the row is said; last: it is not read again, and k_out, which may be
+    // the row's own place, gets it.
+    auto row = [&](int r, bool first, bool last, float2(&u)[4], float2(&v)[4]) {
         const bool on = r < n;
         const int64_t t = q.row0 + q.i0 + (on ? r : 0);
         Raw8<DT, VEC> rx, ry;
@@ -218,7 +219,7 @@ __global__ void __launch_bounds__(kByteThreads, D == 256 ? 1 : kWriteCtas) kvb_w
             ry.unpack(v);
         } else {
             kv_norm_rotate<DT, D, VEC, FULL>(a.w, rx, ry, l, used, pos, a.w.k_weight, mine, u, v);
-            if (first && on && a.w.k_out != nullptr) {
+            if (last && on && a.w.k_out != nullptr) {
                 const int64_t at = (t * hkv + head) * D + 8 * l;
                 store8<DT, VEC>(a.w.k_out, at, u);
                 store8<DT, VEC>(a.w.k_out, at + H, v);
@@ -249,10 +250,10 @@ __global__ void __launch_bounds__(kByteThreads, D == 256 ? 1 : kWriteCtas) kvb_w
     if constexpr (kHold > 1) {
 #pragma unroll
         for (int p = 0; p < kHold; ++p)
-            if (p < rounds) top = max(top, row(p * kRows + r0, true, u[p], v[p]));
+            if (p < rounds) top = max(top, row(p * kRows + r0, true, true, u[p], v[p]));
     } else {
 #pragma unroll 1
-        for (int p = 0; p < rounds; ++p) top = max(top, row(p * kRows + r0, true, u[0], v[0]));
+        for (int p = 0; p < rounds; ++p) top = max(top, row(p * kRows + r0, true, p == rounds - 1, u[0], v[0]));
     }
 #pragma unroll
     for (int o = L; o < 32; o <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
@@ -281,7 +282,7 @@ __global__ void __launch_bounds__(kByteThreads, D == 256 ? 1 : kWriteCtas) kvb_w
             if (rounds > 0) put((rounds - 1) * kRows + r0, u[0], v[0]);
 #pragma unroll 1
             for (int p = 0; p < rounds - 1; ++p) {
-                row(p * kRows + r0, false, u[0], v[0]);
+                row(p * kRows + r0, false, true, u[0], v[0]);
                 put(p * kRows + r0, u[0], v[0]);
             }
         }
