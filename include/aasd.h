@@ -625,7 +625,8 @@ int aasd_kvb_write(aasd_ctx* ctx, const void* q, const void* k, const void* v, c
 
 /* aasd_kv_attend over an 8-bit pool: the same arguments, masks, errors and scratch (aasd_kv_workspace_init).  Sums and the
  * softmax's statistics are fp32; the result is rounded once.  Keys and values are used as they are (probabilities of
- * pages whose values' scale is below 2^-21 of the largest that a CTA has come by lose bits).  bf16 queries lose bits below 2^-27 of their row's
+ * pages whose values' scale is below 2^-21 of the largest that a CTA has come by, in pages that the row does not see included, lose
+ * bits, and below about 2^-32 of it such values count as zeros; the page's weight in the sum, and in the lse, is kept).  bf16 queries lose bits below 2^-27 of their row's
  * largest element with few rows, and below 2^-9 of it with many (2^-17 of the largest element is left out at most); probabilities are
  * rounded to 11 bits; fp32 queries and their probabilities to 22.  Many rows are, with bf16 queries and head_dim 64, 128 or 256, more than
  * 32, 16 or 8 rows per key/value head (query heads of a group times token rows; rows_per_seq of them, or n_tokens / n_seqs

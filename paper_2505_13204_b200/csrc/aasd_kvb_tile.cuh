@@ -51,6 +51,9 @@ constexpr int kByteScales = 8;                                             // ri
 // Where a page's scale of the values is this much below the largest (in powers of two), the row's maximum is looked for: fp16's
 // range says nothing about probabilities that were scaled down so far.
 constexpr int kByteFar = 30;
+// The most that probabilities are scaled down by.  With the maximum known they are 2^(kTileP - 40) at most, which fp16 rounds to zero
+// as it does everything smaller, so that O loses nothing more; their sum, which is scaled back, keeps weights down to 2^-93.
+constexpr int kByteDown = 40;
 
 template <int D, bool PAIR>
 struct KvbTileShared {
@@ -613,7 +616,7 @@ __global__ void __launch_bounds__(KvbTileShape<D>::kThreads, 1) kvb_attend_tile_
                         }
                         ev = ep;
                     }
-                    const int down = missing ? 0 : ev - ep;
+                    const int down = missing ? 0 : min(ev - ep, kByteDown);
                     const float shift = kTileP - (float)down;
                     // Probabilities with the maximum as it stands; only where a thread's sum of them leaves fp16's range (by a
                     // new maximum at least 2^5 above it), on the first page, and with large products, is the maximum looked for
@@ -672,7 +675,7 @@ __global__ void __launch_bounds__(KvbTileShape<D>::kThreads, 1) kvb_attend_tile_
                         again = true;
                     }
                     if (!ok) break;
-                    const float back = kvb_pow2(min(down, 126));   // (the probabilities were scaled down by so much)
+                    const float back = kvb_pow2(down);   // (the probabilities were scaled down by so much)
 #pragma unroll
                     for (int q = 0; q < Q; ++q) l[q] = fmaf(ls[q], back, l[q]);
                 }
