@@ -549,10 +549,10 @@ typedef struct aasd_kv_attend_out {
  * not: one choice for the whole call) the cache's values are rounded too, to 11 bits, and to about
  * 2^-20 of the largest value in the pages that a CTA has been through.
  * Rows that see nothing (padding, tokens that were not placed, rows that no sequence owns) give zeros
- * and an lse of -inf.  More than 2^31 - 1 pages to go through in one call (over all heads and row
- * tiles) raise AASD_STATUS_BAD_OFFSETS; no row sees anything then.  A page id outside the pool, or a
- * parent that does not precede its child, raises AASD_STATUS_BAD_OFFSETS; what lies behind it counts
- * as not visible. */
+ * and an lse of -inf; others whose query holds a NaN give NaN in both.  More than 2^31 - 1 pages to go
+ * through in one call (over all heads and row tiles) raise AASD_STATUS_BAD_OFFSETS; no row sees anything
+ * then.  A page id outside the pool, or a parent that does not precede its child, raises
+ * AASD_STATUS_BAD_OFFSETS; what lies behind it counts as not visible. */
 int aasd_kv_attend(aasd_ctx* ctx, const void* q, const void* pages, const int32_t* block_table,
                    const int32_t* cached_len, const int32_t* kv_len, const int32_t* tok_offsets,
                    const int32_t* node_parent, const aasd_kv_attend_params* params, void* workspace,
@@ -626,9 +626,10 @@ int aasd_kvb_write(aasd_ctx* ctx, const void* q, const void* k, const void* v, c
 /* aasd_kv_attend over an 8-bit pool: the same arguments, masks, errors and scratch (aasd_kv_workspace_init).  Sums and the
  * softmax's statistics are fp32; the result is rounded once.  Keys and values are used as they are (probabilities of
  * pages whose values' scale is below 2^-21 of the largest that a CTA has come by, in pages that the row does not see included, lose
- * bits, and below about 2^-32 of it such values count as zeros; the page's weight in the sum, and in the lse, is kept).  bf16 queries lose bits below 2^-27 of their row's
- * largest element with few rows, and below 2^-9 of it with many (2^-17 of the largest element is left out at most); probabilities are
- * rounded to 11 bits; fp32 queries and their probabilities to 22.  Many rows are, with bf16 queries and head_dim 64, 128 or 256, more than
+ * bits, and below about 2^-32 of it such values count as zeros; the page's weight in the sum, and in the lse, is kept).  A row that
+ * sees something and whose query holds a NaN or an infinity gives NaN in out and lse.  bf16 queries lose bits below 2^-27 of their
+ * row's largest element with few rows, and below 2^-9 of it with many (2^-17 of the largest element is left out at most);
+ * probabilities are rounded to 11 bits; fp32 queries and their probabilities to 22.  Many rows are, with bf16 queries and head_dim 64, 128 or 256, more than
  * 32, 16 or 8 rows per key/value head (query heads of a group times token rows; rows_per_seq of them, or n_tokens / n_seqs
  * when packed: one choice for the whole call). */
 int aasd_kvb_attend(aasd_ctx* ctx, const void* q, const void* pages, const int32_t* block_table,

@@ -317,6 +317,13 @@ __device__ __forceinline__ void kv_clear_rows(const KvAttendArgs& a, int D, int 
     }
 }
 
+// ---- a row's result ----------------------------------------------------------------------------------
+
+// From the row's denominator l and, in base 2, what it is relative to: a factor of the sums, and the lse.  A row that sees nothing (l = 0)
+// gives zeros and -inf; a denominator that is NaN (a query that is not finite) goes on into both.
+__device__ __forceinline__ float kv_inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
+__device__ __forceinline__ float kv_lse(float m, float l) { return l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * (float)kLn2; }
+
 // ---- joining ---------------------------------------------------------------------------------------------
 
 // Row r of a segment from its parts, one warp.  Part k lies at base + 2 k stride, the first one stride further;
@@ -363,12 +370,12 @@ __device__ __forceinline__ void kv_join_row(const KvAttendArgs& a, const KvPiece
 #pragma unroll
         for (int q = 16; q > 0; q >>= 1) L += __shfl_xor_sync(0xFFFFFFFFu, L, q);
         if (!on) continue;
-        const float inv = L > 0.f ? 1.f / L : 0.f;
+        const float inv = kv_inverse(L);
         const int row = pc.row0 + r;
         const long long head = ((long long)pc.first + row / G) * a.p.n_q_heads + pc.h * G + row % G;
         if (!AASD_IN_RANGE(parts <= kKvMaxCtas && head < a.p.n_tokens * a.p.n_q_heads, a.state)) continue;
         store4<DT>(a.o.out, head * D + ch, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), a.out_vec);
-        if (a.o.lse != nullptr && ch == 0) a.o.lse[head] = L > 0.f ? (M + log2f(L)) * (float)kLn2 : -CUDART_INF_F;
+        if (a.o.lse != nullptr && ch == 0) a.o.lse[head] = kv_lse(M, L);
     }
 }
 
@@ -424,12 +431,12 @@ __device__ __forceinline__ void kv_split_join(const KvAttendArgs& a, Shared& sh,
     const int previous = __shfl_sync(0xFFFFFFFFu, seg, below ? 31 - __clz(below) : 0);
     unsigned int starts = __ballot_sync(0xFFFFFFFFu, seg >= 0 && (below == 0 || previous != seg));
     auto finish_row = [&](const KvPiece& pc, int r, float M, float L, float4 o, int ch) {
-        const float inv = L > 0.f ? 1.f / L : 0.f;
+        const float inv = kv_inverse(L);
         const int row = pc.row0 + r;
         const long long head = ((long long)pc.first + row / G) * a.p.n_q_heads + pc.h * G + row % G;
         if (!AASD_IN_RANGE(head < a.p.n_tokens * a.p.n_q_heads, a.state)) return;
         store4<DT>(a.o.out, head * D + ch, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), a.out_vec);
-        if (a.o.lse != nullptr && ch == 0) a.o.lse[head] = L > 0.f ? (M + log2f(L)) * (float)kLn2 : -CUDART_INF_F;
+        if (a.o.lse != nullptr && ch == 0) a.o.lse[head] = kv_lse(M, L);
     };
     int open[2] = {-1, -1};        // first pieces of the groups that other CTAs hold parts of: begun before this CTA, in it
     // rows r0 .. r0 + RB of the group of pieces `group`
@@ -1002,14 +1009,14 @@ __global__ void __launch_bounds__(KvSplitShape<DT, D, NT>::kThreads, 1) kv_atten
                         }
                         const int r = 8 * nt + 2 * j + col;
                         const int row = at.row0 + r;
-                        const float inv = complete ? (ls > 0.f ? 1.f / ls : 0.f) : 1.f;
+                        const float inv = complete ? kv_inverse(ls) : 1.f;
                         const long long head = ((long long)at.first + row / G) * a.p.n_q_heads + at.h * G + row % G;
                         if (g == 0) {
                             if (!complete) {
                                 sh.m[slot][r] = mref[nt][col];
                                 sh.l[slot][r] = ls;
                             } else if (a.o.lse != nullptr && r < n) {
-                                a.o.lse[head] = ls > 0.f ? (mref[nt][col] + log2f(ls)) * (float)kLn2 : -CUDART_INF_F;
+                                a.o.lse[head] = kv_lse(mref[nt][col], ls);
                             }
                         }
                         if (r < n && AASD_IN_RANGE(c < kKvMaxCtas && head < a.p.n_tokens * a.p.n_q_heads, a.state)) {

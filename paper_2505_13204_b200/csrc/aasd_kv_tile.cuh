@@ -885,7 +885,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                 if (complete) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const float inv = l[q] > 0.f ? 1.f / l[q] : 0.f;
+                        const float inv = kv_inverse(l[q]);
                         own[q] *= inv;
                         other[q] *= inv;
                     }
@@ -954,8 +954,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) kv_attend_tile_kernel(const K
                             part[R * D + r] = mref[q];
                             part[R * D + R + r] = l[q];
                         } else if (a.o.lse != nullptr) {
-                            a.o.lse[((long long)w.first + row / G) * a.p.n_q_heads + w.h * G + row % G] =
-                                l[q] > 0.f ? (mref[q] + log2f(l[q])) * (float)kLn2 : -CUDART_INF_F;
+                            a.o.lse[((long long)w.first + row / G) * a.p.n_q_heads + w.h * G + row % G] = kv_lse(mref[q], l[q]);
                         }
                     }
                 }
@@ -1040,12 +1039,12 @@ __device__ __forceinline__ void kv_join_rows(const KvAttendArgs& a, const KvPiec
         for (int i = 0; i < NR; ++i) {
             const float Li = __shfl_sync(0xFFFFFFFFu, L, 8 * i), Mi = __shfl_sync(0xFFFFFFFFu, M, 8 * i);
             if (!on || r0 + i >= pc.n) continue;
-            const float inv = Li > 0.f ? 1.f / Li : 0.f;
+            const float inv = kv_inverse(Li);
             const int row = pc.row0 + r0 + i;
             const long long head = ((long long)pc.first + row / G) * a.p.n_q_heads + pc.h * G + row % G;
             if (!AASD_IN_RANGE(head < a.p.n_tokens * a.p.n_q_heads, a.state)) continue;
             store4<AASD_BF16>(a.o.out, head * D + ch, make_float4(o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv), a.out_vec);
-            if (a.o.lse != nullptr && ch == 0) a.o.lse[head] = Li > 0.f ? (Mi + log2f(Li)) * (float)kLn2 : -CUDART_INF_F;
+            if (a.o.lse != nullptr && ch == 0) a.o.lse[head] = kv_lse(Mi, Li);
         }
         if (D <= 128) break;
         ch += 128;

@@ -267,7 +267,8 @@ __global__ void __launch_bounds__(KvbSplitShape<DT, D, NT>::kThreads, 1) kvb_att
                                 qf[0][nt][4 * k + w][r] = hi;
                                 if (NP == 2) qf[NP - 1][nt][4 * k + w][r] = pack_rest(p, q, hi);
                             }
-                    const float rf = a.scale_log2 * kvb_pow2(e - 14);
+                    // (a row with an infinity becomes NaN, as one with a NaN is)
+                    const float rf = top < CUDART_INF_F ? a.scale_log2 * kvb_pow2(e - 14) : CUDART_NAN_F;
 #pragma unroll
                     for (int col = 0; col < 2; ++col) {
                         rfac[nt][col] = __shfl_sync(0xFFFFFFFFu, rf, (2 * j + col) * 4);
@@ -490,14 +491,14 @@ __global__ void __launch_bounds__(KvbSplitShape<DT, D, NT>::kThreads, 1) kvb_att
                         for (int o = 4; o < 32; o <<= 1) ls += __shfl_xor_sync(0xFFFFFFFFu, ls, o);
                         const int r = 8 * nt + 2 * j + col;
                         const int row = at.row0 + r;
-                        const float f = back * (complete ? (ls > 0.f ? 1.f / ls : 0.f) : 1.f);
+                        const float f = back * (complete ? kv_inverse(ls) : 1.f);
                         const long long head = ((long long)at.first + row / G) * a.p.n_q_heads + at.h * G + row % G;
                         if (g == 0) {
                             if (!complete) {
                                 sh.m[slot][r] = mref[nt][col];
                                 sh.l[slot][r] = ls;
                             } else if (a.o.lse != nullptr && r < n) {
-                                a.o.lse[head] = ls > 0.f ? (mref[nt][col] + log2f(ls)) * (float)kLn2 : -CUDART_INF_F;
+                                a.o.lse[head] = kv_lse(mref[nt][col], ls);
                             }
                         }
                         if (r < n && AASD_IN_RANGE(c < kKvMaxCtas && head < a.p.n_tokens * a.p.n_q_heads, a.state)) {

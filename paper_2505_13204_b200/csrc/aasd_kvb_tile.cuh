@@ -752,7 +752,7 @@ __global__ void __launch_bounds__(KvbTileShape<D>::kThreads, 1) kvb_attend_tile_
                 if (complete) {
 #pragma unroll
                     for (int q = 0; q < Q; ++q) {
-                        const float inv = l[q] > 0.f ? 1.f / l[q] : l[q];   // (NaN stays)
+                        const float inv = kv_inverse(l[q]);
                         own[q] *= inv;
                         other[q] *= inv;
                     }
@@ -816,8 +816,7 @@ __global__ void __launch_bounds__(KvbTileShape<D>::kThreads, 1) kvb_attend_tile_
                             part[R * D + r] = mref[q];
                             part[R * D + R + r] = l[q];
                         } else if (a.o.lse != nullptr) {
-                            a.o.lse[((long long)w.first + row / G) * a.p.n_q_heads + w.h * G + row % G] =
-                                l[q] == 0.f ? -CUDART_INF_F : (mref[q] + log2f(l[q])) * (float)kLn2;
+                            a.o.lse[((long long)w.first + row / G) * a.p.n_q_heads + w.h * G + row % G] = kv_lse(mref[q], l[q]);
                         }
                     }
                 }
