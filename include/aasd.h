@@ -712,7 +712,7 @@ int aasd_kv_copy(aasd_ctx* ctx, const aasd_kv_pool* pool, int32_t n_pages, const
  * number of each page that was in use, NONE for the others, for whatever else names pages; moves [n_pages]: scratch (the
  * moves as pairs); n_moved [1].  A stack with repetitions or pages outside the pool raises AASD_STATUS_BAD_OFFSETS and nothing
  * moves; an entry of the table that is not in use raises it and stays.  page_map, moves and n_moved must not lie over one
- * another or over the books (AASD_ERR_INVALID_ARG). */
+ * another, the books or the pools (AASD_ERR_INVALID_ARG). */
 int aasd_kv_compact(aasd_ctx* ctx, const aasd_kv_books_params* params, const aasd_kv_books* books,
                     const aasd_kv_pool* pool, int32_t* page_map, int32_t* moves, int32_t* n_moved);
 

@@ -36,6 +36,16 @@ int check_pool(const aasd_kv_pool* p) {
     return AASD_OK;
 }
 
+// Whether an array lies over one of the books, or over the layers' pools.
+bool over_books(const void* x, int64_t bytes, const aasd_kv_books_params& p, const aasd_kv_books& k) {
+    const int64_t b4 = 4 * (int64_t)p.n_seqs, n4 = 4 * (int64_t)p.n_pages;
+    return overlap(x, bytes, k.block_table, b4 * p.max_pages) || overlap(x, bytes, k.seq_pages, b4) || overlap(x, bytes, k.free_pages, n4) ||
+           overlap(x, bytes, k.n_free, 4) || overlap(x, bytes, k.page_shares, n4);
+}
+bool over_pool(const void* x, int64_t bytes, const aasd_kv_pool& p, int32_t n_pages) {
+    return p.n_layers > 0 && overlap(x, bytes, p.pages, (p.n_layers - 1) * p.layer_stride + n_pages * p.page_bytes);
+}
+
 KvCopyArgs copy_args(const aasd_ctx* ctx, const aasd_kv_pool& p, int32_t n_pages, const int32_t* src, const int32_t* dst, int step, int32_t n, const int32_t* count) {
     return KvCopyArgs{static_cast<uint8_t*>(p.pages), p.layer_stride, p.page_bytes, p.page_bytes > 0 ? p.n_layers : 0, n_pages, src, dst, step, n, count, ctx->state};
 }
@@ -92,7 +102,7 @@ int aasd_kv_fork(aasd_ctx* ctx, const int32_t* src_seq, const int32_t* dst_seq, 
     const int64_t n4 = 4 * (int64_t)n_forks, b4 = 4 * (int64_t)p->n_seqs;
     for (const int32_t* x : {o->new_len, o->copy_src, o->copy_dst})
         if (overlap(x, n4, src_seq, n4) || overlap(x, n4, dst_seq, n4) || overlap(x, n4, fork_len, n4) || overlap(x, n4, cached_len, b4) ||
-            overlap(x, n4, k->seq_pages, b4) || overlap(x, n4, k->block_table, b4 * p->max_pages))
+            over_books(x, n4, *p, *k) || over_pool(x, n4, *pool, p->n_pages))
             return AASD_ERR_INVALID_ARG;
     if (overlap(o->new_len, n4, o->copy_src, n4) || overlap(o->new_len, n4, o->copy_dst, n4) || overlap(o->copy_src, n4, o->copy_dst, n4)) return AASD_ERR_INVALID_ARG;
     KvForkArgs a{src_seq, dst_seq, fork_len, n_forks, *k, *p, cached_len, o->new_len, o->copy_src, o->copy_dst,
@@ -115,9 +125,10 @@ int aasd_kv_compact(aasd_ctx* ctx, const aasd_kv_books_params* p, const aasd_kv_
     if (!n_moved || (p->n_pages > 0 && (!page_map || !moves))) return AASD_ERR_INVALID_ARG;
     const int64_t n4 = 4 * (int64_t)p->n_pages;
     if (overlap(page_map, n4, moves, n4) || overlap(n_moved, 4, page_map, n4) || overlap(n_moved, 4, moves, n4)) return AASD_ERR_INVALID_ARG;
-    for (const int32_t* x : {page_map, moves})
-        if (overlap(x, n4, k->free_pages, n4) || overlap(x, n4, k->page_shares, n4) || overlap(x, n4, k->block_table, 4 * (int64_t)p->n_seqs * p->max_pages))
-            return AASD_ERR_INVALID_ARG;
+    for (const int32_t* x : {page_map, moves, n_moved}) {
+        const int64_t bytes = x == n_moved ? 4 : n4;
+        if (over_books(x, bytes, *p, *k) || over_pool(x, bytes, *pool, p->n_pages)) return AASD_ERR_INVALID_ARG;
+    }
     KvCompactArgs a{*k, *p, page_map, moves, n_moved, copy_args(ctx, *pool, p->n_pages, moves, moves + 1, 2, p->n_pages / 2, n_moved), ctx->state};
     AASD_CUDA(cudaSetDevice(ctx->device));
     one_cta(p->n_pages <= kFewPages, [&](auto nt) { launch(kv_compact_kernel<nt()>, 1u, (unsigned int)nt(), 0, ctx->stream, a); });

@@ -1,0 +1,100 @@
+"""What the page calls refuse and report."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2505_13204_b200 import binding
+
+pytestmark = pytest.mark.gpu
+BOOKS = ("block_table", "seq_pages", "free_pages", "n_free", "page_shares")
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = binding.Context()
+    yield c
+    c.close()
+
+
+def i32(a):
+    return torch.as_tensor(np.ascontiguousarray(a, dtype=np.int32)).cuda()
+
+
+def small_books():
+    """Two sequences with tokens, two without, six pages free; every array is longer than any output."""
+    table = np.full((4, 4), -1)
+    table[0, :3], table[1, :1] = (0, 1, 2), (7,)
+    return dict(block_table=i32(table), seq_pages=i32([3, 1, 0, 0]), free_pages=i32([3, 4, 5, 6, 8, 9, -1, -1, -1, -1]), n_free=i32([6]), page_shares=i32([0] * 10))
+
+
+def pages():
+    return torch.zeros((2, 10, 1, 48), dtype=torch.uint8, device="cuda")
+
+
+@pytest.mark.parametrize("which", BOOKS + ("cached_len", "src_seq", "dst_seq", "fork_len", "pages", "new_len"))
+@pytest.mark.parametrize("out", ["new_len", "copy_src", "copy_dst"])
+def test_fork_refuses_outputs_over_its_arrays(ctx, which, out):
+    b = small_books()
+    given = dict(b, cached_len=i32([150, 20, 0, 0]), src_seq=i32([0]), dst_seq=i32([2]), fork_len=i32([70]), pages=pages(), new_len=i32([9]))
+    outputs = {k: i32([9]) for k in ("new_len", "copy_src", "copy_dst")}
+    if which == "new_len":
+        if out == "new_len":
+            return
+        outputs["new_len"] = given["new_len"]
+    over = given[which].view(-1)
+    outputs[out] = over.view(torch.int32)[-1:] if which == "pages" else over[-1:]
+    kept = {k: v.clone() for k, v in given.items()}
+    with pytest.raises(binding.AasdError):
+        ctx.kv_fork(given["pages"], given["src_seq"], given["dst_seq"], b["block_table"], b["seq_pages"], given["cached_len"], b["free_pages"], b["n_free"], b["page_shares"],
+                    given["fork_len"], outputs=outputs)
+    assert all(torch.equal(given[k], kept[k]) for k in kept) and ctx.poll_status() == 0
+
+
+@pytest.mark.parametrize("which", BOOKS + ("pages", "page_map"))
+@pytest.mark.parametrize("out", ["page_map", "n_moved"])
+def test_compact_refuses_outputs_over_its_arrays(ctx, which, out):
+    b = small_books()
+    given = dict(b, pages=pages(), page_map=i32([9] * 10))
+    outputs = dict(page_map=given["page_map"], n_moved=i32([9]))
+    if which == out:
+        return
+    over = given[which].view(torch.int32).view(-1) if which == "pages" else given[which].view(-1)
+    if out == "n_moved":
+        outputs["n_moved"] = over[-1:]
+    else:                                     # page_map ends where the array begins: both are parts of one
+        joint = torch.zeros(9 + over.numel(), dtype=torch.int32, device="cuda")
+        joint[9:] = over
+        part = joint[9:]
+        if which == "pages":
+            if part.data_ptr() % 16:          # (pools start on 16-byte boundaries)
+                joint = torch.zeros(12 + over.numel(), dtype=torch.int32, device="cuda")
+                part = joint[12:]
+            given["pages"] = part.view(torch.uint8).view(2, 10, 1, 48)
+        else:
+            given[which] = b[which] = part.view(given[which].shape)
+        at = part.storage_offset() - 9
+        outputs["page_map"] = joint[at:at + 10]
+    kept = {k: v.clone() for k, v in given.items()}
+    with pytest.raises(binding.AasdError):
+        ctx.kv_compact(given["pages"], b["block_table"], b["seq_pages"], b["free_pages"], b["n_free"], b["page_shares"], outputs=outputs)
+    assert all(torch.equal(given[k], kept[k]) for k in kept) and ctx.poll_status() == 0
+
+
+def test_neighbouring_arrays_and_empty_ones_are_no_overlap(ctx):
+    """Outputs that begin where the books end, in one allocation, and calls without sequences."""
+    b = small_books()
+    sizes = [b[k].numel() for k in BOOKS]
+    joint = torch.empty(sum(sizes) + 4 + 3, dtype=torch.int32, device="cuda")
+    at, part = 0, {}
+    for k, n in zip(BOOKS, sizes):
+        part[k] = joint[at:at + n].view(b[k].shape)
+        part[k].copy_(b[k])
+        at += n
+    cached = joint[at:at + 4]
+    cached.copy_(i32([150, 20, 0, 0]))
+    outputs = {k: joint[at + 4 + i:at + 5 + i] for i, k in enumerate(("new_len", "copy_src", "copy_dst"))}
+    ctx.kv_fork(pages(), i32([0]), i32([3]), part["block_table"], part["seq_pages"], cached, part["free_pages"], part["n_free"], part["page_shares"], i32([64]), outputs=outputs)
+    assert ctx.poll_status() == 0 and outputs["new_len"].item() == 64 and part["seq_pages"].tolist() == [3, 1, 0, 1] and part["page_shares"].tolist() == [1] + [0] * 9
+    none = joint[2:2]                         # an empty array inside another one
+    ctx.kv_compact(pages(), part["block_table"][:0], none, part["free_pages"], part["n_free"], part["page_shares"])
+    assert ctx.poll_status() == 0
