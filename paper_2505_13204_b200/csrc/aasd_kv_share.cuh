@@ -315,15 +315,14 @@ __global__ void __launch_bounds__(NT) kv_compact_kernel(const KvCompactArgs a) {
 __global__ void __launch_bounds__(kCopyThreads) kv_compact_copy_kernel(const KvCompactArgs a) {
     pdl_launch_dependents();
     pdl_wait();
-    if (*a.n_moved > 0) {
-        const int64_t entries = (int64_t)a.p.n_seqs * a.p.max_pages;
-        for (int64_t i = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; i < entries; i += (int64_t)gridDim.x * kCopyThreads) {
-            const int page = a.k.block_table[i];
-            if (page == AASD_NONE) continue;
-            const int to = page >= 0 && page < a.p.n_pages ? a.page_map[page] : AASD_NONE;
-            if (to == AASD_NONE) raise(a.state, AASD_STATUS_BAD_OFFSETS);     // not in use, or not in the pool
-            else if (to != page) a.k.block_table[i] = to;
-        }
+    // (whether anything moves or not: a table that names a free page is found here)
+    const int64_t entries = (int64_t)a.p.n_seqs * a.p.max_pages;
+    for (int64_t i = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; i < entries; i += (int64_t)gridDim.x * kCopyThreads) {
+        const int page = a.k.block_table[i];
+        if (page == AASD_NONE) continue;
+        const int to = page >= 0 && page < a.p.n_pages ? a.page_map[page] : AASD_NONE;
+        if (to == AASD_NONE) raise(a.state, AASD_STATUS_BAD_OFFSETS);     // not in use, or not in the pool
+        else if (to != page) a.k.block_table[i] = to;
     }
     kv_copy_pages(a.c, blockIdx.x, gridDim.x);
 }

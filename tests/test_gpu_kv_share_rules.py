@@ -98,3 +98,15 @@ def test_neighbouring_arrays_and_empty_ones_are_no_overlap(ctx):
     none = joint[2:2]                         # an empty array inside another one
     ctx.kv_compact(pages(), part["block_table"][:0], none, part["free_pages"], part["n_free"], part["page_shares"])
     assert ctx.poll_status() == 0
+
+
+def test_compact_looks_at_tables_when_nothing_moves(ctx):
+    """Table entries that name a free page, or none of the pool, are reported and stay, whether pages move or not."""
+    for entry in (5, 77, -9):
+        for moves in (False, True):
+            free = [2, 3, 4, 5] if not moves else [0, 3, 4, 5]
+            used = [0, 1] if not moves else [1, 2]
+            table = i32([used + [entry], [-1, -1, -1]])
+            o = ctx.kv_compact(torch.zeros((1, 6, 1, 16), dtype=torch.uint8, device="cuda"), table, i32([3, 0]), i32(free + [-1, -1]), i32([4]), i32([0] * 6))
+            assert o["n_moved"].tolist() == [int(moves)] and ctx.poll_status() == binding.STATUS_BAD_OFFSETS
+            assert table.tolist() == [[1, 0, entry] if moves else [0, 1, entry], [-1, -1, -1]]
