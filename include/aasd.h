@@ -652,9 +652,10 @@ int aasd_kvb_read(aasd_ctx* ctx, const void* pages, const int32_t* slots, int64_
 /* (No counterpart in the paper.)  Sequences that begin alike (several samples of one prompt, a prompt kept for
  * others) can hold the same pages: page_shares[p] counts page p's holders beyond the first (0 for a page with one holder, and for
  * a free one).  Pages are moved as bytes, so the calls serve 4-bit and 8-bit pools.
- * A shared page must not be written: that cannot happen as long as a sequence is not cut to fewer cached tokens than others
- * took from it.  aasd_kv_plan knows nothing of holders.  Where pages may be shared, call aasd_kv_free with the
- * same cached_len and n_new in front of it: it leaves nothing that plan would give back. */
+ * A shared page must not be written: that cannot happen as long as no sequence is cut to fewer cached tokens than it took from
+ * another one, or others took from it.  aasd_kv_plan knows nothing of holders.  Where pages may be shared, call aasd_kv_free with
+ * the same cached_len and n_new in front of it: it leaves nothing that plan would give back, and reports a step that would write
+ * to a shared page.  (A fork with a fork_len goes on from any place of what another sequence holds.) */
 typedef struct aasd_kv_books {   /* as in aasd_kv_plan_state; all read and written */
     int32_t* block_table;   /* [n_seqs x max_pages] */
     int32_t* seq_pages;     /* [n_seqs] */
@@ -680,7 +681,8 @@ typedef struct aasd_kv_pool {
 
 /* Drops every page that sequence b holds past its first ceil((keep_len[b] + n_new[b]) / 64) ones (n_new NULL: zeros; a keep_len of
  * NONE leaves the sequence alone).  Pages that lose their last holder go on the stack in the order of their numbers.
- * Inconsistent books raise AASD_STATUS_BAD_OFFSETS; nothing outside the arrays is touched. */
+ * Inconsistent books raise AASD_STATUS_BAD_OFFSETS; nothing outside the arrays is touched.  So does a sequence with n_new > 0 that
+ * still holds, from the page of place keep_len[b] on, one that has other holders: its tokens would be stored over theirs. */
 int aasd_kv_free(aasd_ctx* ctx, const int32_t* keep_len, const int32_t* n_new, const aasd_kv_books_params* params,
                  const aasd_kv_books* books);
 

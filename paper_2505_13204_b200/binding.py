@@ -899,7 +899,8 @@ class Context:
 
     def kv_free(self, keep_len, block_table, seq_pages, free_pages, n_free, page_shares, n_new=None):
         """aasd_kv_free: sequences keep the pages of their first ``keep_len`` (+ ``n_new``) tokens; pages without another holder go
-        back on the stack.  The books (int32) are changed in place; ``page_shares`` counts holders beyond the first."""
+        back on the stack.  The books (int32) are changed in place; ``page_shares`` counts holders beyond the first.  New tokens that
+        would be stored to a page with other holders raise STATUS_BAD_OFFSETS."""
         B, P, N, prm, books = self._kv_books(block_table, seq_pages, free_pages, n_free, page_shares)
         _kv_i32(self.device_index, keep_len, n_new)
         _kv_need(keep_len.numel() >= B and (n_new is None or n_new.numel() >= B), "lengths of kv_free's arrays")

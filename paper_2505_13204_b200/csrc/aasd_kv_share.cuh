@@ -53,6 +53,33 @@ __global__ void __launch_bounds__(256) kv_drop_kernel(const KvFreeArgs a) {
     if (b < a.p.n_seqs) kv_drop(a, b);
 }
 
+// Whether the new tokens of a warp's 32 sequences (from b0 on) are going to be stored to a page that others hold too: a sequence was cut
+// inside what it shares.  Holders are those left when every sequence has dropped its pages.  A lane looks at its sequence's
+// first page, as a rule the only one that is there; the warp at what follows.
+__device__ __forceinline__ bool kv_writes_shared(const KvFreeArgs& a, int b0) {
+    const int lane = threadIdx.x & 31, b = b0 + lane;
+    int j = 0, end = 0;
+    if (b < a.p.n_seqs) {
+        const int keep = a.keep_len[b], fresh = a.n_new[b], held = a.k.seq_pages[b];
+        if (keep >= 0 && fresh > 0 && held >= 0 && held <= a.p.max_pages) {
+            j = keep / kPage;
+            end = (int)min((long long)held, ((long long)keep + fresh + kPage - 1) / kPage);
+        }
+    }
+    const auto shared = [&](int seq, int at) {
+        const int page = a.k.block_table[(int64_t)seq * a.p.max_pages + at];
+        return page >= 0 && page < a.p.n_pages && __ldcg(a.k.page_shares + page) > 0;   // (the atomics' own level)
+    };
+    bool found = j < end && shared(b, j);
+    unsigned int more = __ballot_sync(0xFFFFFFFFu, j + 1 < end);
+    while (more) {
+        const int k = __ffs(more) - 1, from = __shfl_sync(0xFFFFFFFFu, j, k) + 1, to = __shfl_sync(0xFFFFFFFFu, end, k);
+        more &= more - 1;
+        for (int i = from + lane; i < to; i += 32) found = found || shared(b0 + k, i);
+    }
+    return found;
+}
+
 // One CTA: pages without a holder go on the stack, in order of their numbers (whatever order the atomics came in).
 // DROP: a small batch's tables are gone through first, without a launch of their own.
 template <int NT, bool DROP>
@@ -65,6 +92,9 @@ __global__ void __launch_bounds__(NT) kv_collect_kernel(const KvFreeArgs a) {
         __syncthreads();
     }
     unsigned int bits = 0;
+    if (a.n_new != nullptr)
+        for (int b0 = (int)threadIdx.x & ~31; b0 < a.p.n_seqs; b0 += NT)
+            if (kv_writes_shared(a, b0)) bits |= AASD_STATUS_BAD_OFFSETS;
     const int N = a.p.n_pages;
     long long n = kv_free_count(a.k.n_free, N, bits);
     for (int base = 0; base < N; base += NT * kShareEach) {

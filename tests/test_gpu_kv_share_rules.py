@@ -110,3 +110,45 @@ def test_compact_looks_at_tables_when_nothing_moves(ctx):
             o = ctx.kv_compact(torch.zeros((1, 6, 1, 16), dtype=torch.uint8, device="cuda"), table, i32([3, 0]), i32(free + [-1, -1]), i32([4]), i32([0] * 6))
             assert o["n_moved"].tolist() == [int(moves)] and ctx.poll_status() == binding.STATUS_BAD_OFFSETS
             assert table.tolist() == [[1, 0, entry] if moves else [0, 1, entry], [-1, -1, -1]]
+
+
+@pytest.mark.parametrize("B", [4, 40, 1500])      # the tables looked through by the collecting CTA, or by a launch of their own; few threads
+def test_a_shared_page_that_is_about_to_be_written_is_reported(ctx, B):
+    """Sequences cut inside what others hold too: a step that stores to such a page is reported in front of it, by kv_free and by kv_plan with
+    page_shares; steps that store to pages of their own are not."""
+    N, P = 12, 5
+
+    def start():
+        cached = i32([0] * B)
+        books = [i32(np.full((B, P), -1)), i32([0] * B), i32(np.arange(N)[::-1]), i32([N]), i32([0] * N)]
+        p = ctx.kv_plan(cached, i32([150] + [0] * (B - 1)), *books[:4], 150)
+        cached = p["kv_len"].clone()
+        ctx.kv_fork(torch.zeros((1, N, 1, 16), dtype=torch.uint8, device="cuda"), i32([0]), i32([B - 1]), *books[:2], cached, *books[2:])
+        assert ctx.poll_status() == 0
+        return books
+
+    def at(first, last):
+        return i32([first] + [0] * (B - 2) + [last])
+
+    def keep(first, last):
+        return i32([first] + [binding.NONE] * (B - 2) + [last])
+
+    bad = binding.STATUS_BAD_OFFSETS
+    # (kept, new) of the sequence and of its sample; the status.  Pages 0 and 1 are shared, the third is each one's own.
+    cases = [((150, 150), (3, 3), 0), ((100, 150), (3, 1), bad), ((150, 100), (3, 1), bad), ((150, 127), (0, 1), bad), ((128, 150), (5, 0), 0), ((128, 128), (1, 70), 0),
+             ((100, 150), (0, 1), 0),                     # nothing is stored
+             ((100, 0), (3, 0), 0), ((0, 64), (0, 9), 0), # the other one ends in the same call
+             ((64, 150), (64, 0), bad), ((64, 150), (1, 0), bad)]   # (page 1 is kept for the new tokens)
+    for kept, new, status in cases:
+        books = start()
+        ctx.kv_free(keep(*kept), *books, at(*new))
+        assert ctx.poll_status() == status, (kept, new)
+        books = start()
+        p = ctx.kv_plan(at(*kept), at(*new), *books[:4], sum(new), page_shares=books[4])
+        assert ctx.poll_status() == status, (kept, new)
+        assert p["kv_len"].tolist() == at(kept[0] + new[0], kept[1] + new[1]).tolist()
+    # a sequence that is left alone is not looked at, and neither is one without new tokens in a call without them
+    books = start()
+    ctx.kv_free(keep(binding.NONE, 150), *books, at(3, 3))
+    ctx.kv_free(keep(100, 150), *books)
+    assert ctx.poll_status() == 0
