@@ -6,6 +6,7 @@ missing or the device is not sm_100, the calls raise.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -41,6 +42,7 @@ EXPORTS = [
     "aasd_kv_free", "aasd_kv_fork", "aasd_kv_copy", "aasd_kv_compact",
 ]
 STATIC_MAX_ROWS = STATIC_MAX_CANDS = 8192
+_NO_STREAM = contextlib.nullcontext()
 
 _vp = C.c_void_p
 
@@ -503,6 +505,10 @@ class Context:
         self.stream = stream
         _check(self.lib.aasd_set_stream(self._h, _vp(stream.cuda_stream)), "aasd_set_stream")
 
+    def _allocating(self):
+        """For what a call's kernels read again and the caller may drop at once: memory that only the context's stream gets again."""
+        return _NO_STREAM if torch.cuda.current_stream(self.device_index) == self.stream else torch.cuda.stream(self.stream)
+
     def poll_status(self) -> int:
         v = C.c_uint32()
         _check(self.lib.aasd_poll_status(self._h, C.byref(v)), "aasd_poll_status")
@@ -916,7 +922,8 @@ class Context:
         n = src_seq.numel()
         o = outputs
         if o is None:
-            new_len, copy_src, copy_dst = torch.empty_like(src_seq), torch.empty_like(src_seq), torch.empty_like(src_seq)
+            with self._allocating():
+                new_len, copy_src, copy_dst = torch.empty_like(src_seq), torch.empty_like(src_seq), torch.empty_like(src_seq)
             o = dict(new_len=new_len, copy_src=copy_src, copy_dst=copy_dst)
         else:
             new_len, copy_src, copy_dst = o["new_len"], o["copy_src"], o["copy_dst"]
@@ -945,10 +952,13 @@ class Context:
         B, P, N, prm, books = self._kv_books(block_table, seq_pages, free_pages, n_free, page_shares)
         o = outputs
         if o is None:
-            page_map, n_moved, moves = torch.empty_like(free_pages), free_pages.new_empty(1), torch.empty_like(free_pages)
+            with self._allocating():
+                page_map, n_moved, moves = torch.empty_like(free_pages), free_pages.new_empty(1), torch.empty_like(free_pages)
             o = dict(page_map=page_map, n_moved=n_moved)
         else:
-            page_map, n_moved, moves = o["page_map"], o["n_moved"], torch.empty_like(free_pages)
+            with self._allocating():
+                moves = torch.empty_like(free_pages)
+            page_map, n_moved = o["page_map"], o["n_moved"]
             _kv_i32(self.device_index, page_map, n_moved)
             _kv_need(page_map.numel() >= N and n_moved.numel() > 0, "outputs")
         pool = self._kv_layers(pages, N)

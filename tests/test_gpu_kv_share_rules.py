@@ -152,3 +152,45 @@ def test_a_shared_page_that_is_about_to_be_written_is_reported(ctx, B):
     ctx.kv_free(keep(binding.NONE, 150), *books, at(3, 3))
     ctx.kv_free(keep(100, 150), *books)
     assert ctx.poll_status() == 0
+
+
+@pytest.mark.parametrize("call", ["compact", "fork"])
+def test_what_a_call_gives_back_is_not_handed_to_another_stream(call):
+    """The context works on another stream than torch's current one, and what the call returns is dropped: what its kernels read again is not
+    handed to the current stream, which is not behind them."""
+    rng = np.random.default_rng(0)
+    N = 4000
+    c = binding.Context()
+    side = torch.cuda.Stream()
+    try:
+        order = rng.permutation(N)
+        used, rest = order[:N // 2], order[N // 2:]
+        raw = rng.integers(0, 256, (1, N, 1, 64)).astype(np.uint8)
+        pool = torch.as_tensor(raw).cuda()
+        n = 1 if call == "compact" else N // 2             # sequences of one page; or one sequence that holds all of them
+        table = np.full((2 * n, N // 2 // n), -1)
+        table[:n] = used.reshape(n, -1)
+        books = [i32(table), i32([N // 2 // n] * n + [0] * n), i32(np.concatenate([rest, np.full(N // 2, -1)])), i32([N - N // 2]), i32([0] * N)]
+        cached, src, dst = i32([63] * n + [0] * n), i32(np.arange(n)), i32(n + np.arange(n))
+        torch.cuda.synchronize()
+        c.set_stream(side)
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+        if call == "compact":
+            c.kv_compact(pool, *books)
+        else:
+            c.kv_fork(pool, src, dst, *books[:2], cached, *books[2:])
+        found = [torch.full((len(src) if call == "fork" else N,), 3, dtype=torch.int32, device="cuda") for _ in range(8)]
+        torch.cuda.synchronize()
+        assert c.poll_status() == 0 and all((x == 3).all() for x in found)
+        got = pool.cpu().numpy()[0]
+        if call == "compact":
+            far = np.sort(used[used >= N // 2])
+            to = np.arange(N)
+            to[far] = np.setdiff1d(np.arange(N // 2), used)
+            assert np.array_equal(books[0].cpu().numpy()[0], to[used]) and np.array_equal(got[to[used]], raw[0, used])
+        else:
+            assert books[0].cpu().numpy()[n:, 0].tolist() == rest[::-1].tolist() and cached.tolist() == [63] * (2 * n)
+            assert np.array_equal(got[rest[::-1]], raw[0, used])
+    finally:
+        c.close()
