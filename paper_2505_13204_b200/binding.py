@@ -506,7 +506,8 @@ class Context:
         _check(self.lib.aasd_set_stream(self._h, _vp(stream.cuda_stream)), "aasd_set_stream")
 
     def _allocating(self):
-        """For what a call's kernels read again and the caller may drop at once: memory that only the context's stream gets again."""
+        """For what a call's kernels read again and the caller may drop at once, and for what is cleared in front of them: memory of the
+        context's stream."""
         return _NO_STREAM if torch.cuda.current_stream(self.device_index) == self.stream else torch.cuda.stream(self.stream)
 
     def poll_status(self) -> int:
@@ -853,7 +854,10 @@ class Context:
             assert w is None or (w.dtype is dt and w.get_device() == dev and w.numel() == D and w.is_contiguous())
         o = outputs
         if o is None:
-            o = dict(q=q.new_empty((T, Hq, D)), k=q.new_zeros((T, Hkv, D)) if keep_k else None)
+            o = dict(q=q.new_empty((T, Hq, D)), k=None)
+            if keep_k:
+                with self._allocating():     # (the zeros are in front of the keys)
+                    o["k"] = q.new_zeros((T, Hkv, D))
         else:
             _kv_like(q, T * Hq * D, o["q"])
             _kv_like(q, T * Hkv * D, o.get("k"))

@@ -1,4 +1,4 @@
-"""The 8-bit store with its outputs over its inputs: the rows of q and k in place, and what is refused."""
+"""The 8-bit store and its outputs: the rows of q and k in place, what is refused, and the keys on another stream."""
 import numpy as np
 import pytest
 import torch
@@ -77,3 +77,24 @@ def test_outputs_over_anything_else_are_refused(ctx):
     ctx.kvb_write(pages, wide[:1, :2], wide[:1, 2:4], wide[:1, 4:], t, z, i32([1]), pos[:1].contiguous(), rows_per_seq=1, outputs=dict(q=wide[:1, :2], k=wide[:1, 2:4]))
     ctx.kvb_write(pages, k[:, :0], k, v, t, z, n, pos, rows_per_seq=T, outputs=dict(q=k[3:, :0], k=k))
     assert ctx.poll_status() == 0
+
+
+def test_zeros_of_rows_without_a_place_do_not_come_after_the_keys():
+    """The context works on another stream than torch's current one, whose own work ends after the call's: keep_k's rows are the keys."""
+    rng = np.random.default_rng(3)
+    D, T = 64, 8
+    c = binding.Context()
+    try:
+        x = torch.as_tensor(rng.standard_normal((T + 2, 3, D)).astype(np.float32)).cuda()
+        args = (x[:, :1], x[:, 1:2], x[:, 2:], i32([[0]]), i32([0]), i32([T]), i32(np.arange(T + 2)), i32([0, T + 2]))
+        pages = binding.kvb_pages(1, 1, D)
+        want = c.kvb_write(pages, *args, keep_k=True)["k"].clone()
+        assert (want[:T] != 0).any(-1).all() and (want[T:] == 0).all()
+        torch.cuda.synchronize()
+        c.set_stream(torch.cuda.Stream())
+        torch.cuda._sleep(20_000_000)
+        got = c.kvb_write(pages, *args, keep_k=True)["k"]
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and c.poll_status() == 0
+    finally:
+        c.close()
