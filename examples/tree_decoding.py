@@ -5,7 +5,9 @@ stored and its alignment table sampled; then, step by step, candidates are draft
 into a tree (Eq. 2), the tree's nodes run through the model in one pass (``kv_plan`` once,
 ``kv_write`` and ``kv_attend`` per layer), the tree is verified and the accepted path's entries
 are moved into place (``kv_commit``).  The weights are random: what the tokens say means nothing,
-but strict verification emits exactly the tokens of decoding one by one, which is what is compared.
+but strict verification over the 4-bit cache emits exactly the tokens of decoding one by one, which is what
+is compared.  In 8 bits it emits those that the model finds over the cache as it is then: a page's entries share a
+scale, and rejected nodes can raise it and round small values of what is accepted, so that a close call may fall otherwise.
 Several samples of a prompt hold its pages together (``kv_fork``); when some have ended, the pages that are left
 move to the front of the pools (``kv_free``, ``kv_compact``).
 

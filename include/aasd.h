@@ -596,7 +596,9 @@ int aasd_kv_read(aasd_ctx* ctx, const void* pages, const int32_t* slots, int64_t
  *   f32     scale of the keys, scale of the values; 8 bytes of nothing
  * A code stands for scale * code.  A scale is a power of two, 2^-64 to 2^120: the least one with max|x| <= 448 * scale over
  * the rows that are stored together.  Where the page holds older tokens the scale is never lowered; when it grows
- * they are rounded to the new one, which changes no value of at least 2^-6 new scales.
+ * they are rounded to the new one, which changes no value of at least 2^-6 new scales.  So an entry depends on what was stored beside
+ * it: rejected draft nodes too can round small values (below 2^-6 of the scale that they call for), and tokens decoded over this
+ * cache in trees need not be those of decoding one by one, as they are in 4 bits, where every entry has a scale of its own.
  * The pool starts on a 16-byte boundary; head_dim is 64, 128 or 256.  What lies in a page past a sequence's end is
  * never looked at, whatever it holds, and neither is the scale of a page without a cached token when it is stored to. */
 int aasd_kvb_head_bytes(int32_t head_dim, size_t* bytes);
