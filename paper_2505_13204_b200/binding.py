@@ -508,7 +508,8 @@ class Context:
     def _allocating(self):
         """For what a call's kernels read again and the caller may drop at once, and for what is cleared in front of them: memory of the
         context's stream."""
-        return _NO_STREAM if torch.cuda.current_stream(self.device_index) == self.stream else torch.cuda.stream(self.stream)
+        # (the current stream's handle; torch.cuda.current_stream makes an object of it, which takes 2.5 us)
+        return _NO_STREAM if torch._C._cuda_getCurrentRawStream(self.device_index) == self.stream.cuda_stream else torch.cuda.stream(self.stream)
 
     def poll_status(self) -> int:
         v = C.c_uint32()
