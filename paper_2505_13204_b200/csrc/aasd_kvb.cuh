@@ -92,7 +92,9 @@ struct KvbUnit {
 // others are made again.  Queries are rows of their own (D / 16 lanes each), as in the 4-bit store.
 //
 // The scale makes a page, head and half the unit: what it shares has to be known before its first code is stored.  Bound by
-// instructions with prompts (54 % of the issue slots, each row read once and held), by one pass of latency with a step's tokens.
+// latency: with prompts a unit's trips to memory stand in a row (lengths, table, rows, positions, cosines; each row read once and
+// held), and the registers of the held rows leave 21 of an SM's 64 warps to fill the time.  They wait for memory a third of it, for
+// the operation before a fifth, and issue in 55 % of the slots; DRAM is at 21 %.  With a step's tokens it is one pass of the chain.
 // Measured (32 query and 8 key heads of 128 channels, bf16): four prompts of 4150 tokens in all 30 us, 93 MB at 3.1 TB/s
 // (two CTAs per SM, whose registers are not held to 80, 39 us); 4 trees of 5 tokens 6 us.
 constexpr int kWriteCtas = 3;              // CTAs per SM that registers are kept free for
@@ -302,8 +304,10 @@ __global__ void __launch_bounds__(kByteThreads, D == 256 ? 1 : kWriteCtas) kvb_w
 
 // ---- entries as values -----------------------------------------------------------------------------
 
-// A lane per 16 bytes of a row (16 channels): keys and values of (slot, head), in the order of the outputs.  Bound by memory: 4150 slots of
-// 8 heads of 128 channels 8 us, 26 MB; a few slots are one trip to memory behind another (slot, codes), 4 us.
+// A lane per 16 bytes of a row (16 channels): keys and values of (slot, head), in the order of the outputs.  4150 slots of 8 heads
+// of 128 channels 8 us, 26 MB at half the copy rate; a few slots 4 us.  Both are one trip to memory behind another (slot, codes and
+// scale, stores): with many slots the warps wait for memory half of their time and for their stores to leave a seventh, in CTAs
+// that go through the chain once; DRAM is at 12 %, L1 at 68.
 template <int DT, int D, bool VEC>
 __global__ void __launch_bounds__(kByteThreads) kvb_read_kernel(const KvReadArgs a) {
     constexpr int C = D / 16;              // 16-byte chunks of a row

@@ -27,7 +27,9 @@ __device__ __forceinline__ unsigned int kvb_halves(unsigned int w) {
 //
 // Bound by memory with a batch, by the chain share - table - block - products - joins with one sequence.  Measured (bf16, 128
 // channels, one token each): 256 sequences of 100 to 4000 tokens, 28 query and 4 key heads, 101 us, 541 MB at 5.3 TB/s, 82 % of the copy
-// rate; one sequence of 16384 tokens, 32 and 8 heads, 18 us, where its 34 MB alone take 5.
+// rate; one sequence of 16384 tokens, 32 and 8 heads, 18 us, where its 34 MB alone take 5.  fp32 queries come here with any number of
+// rows and go over the pages once for every 16 of them (8 with 256 channels), two products each: 32 trees of 33 over 3800 tokens
+// 645 us, 2 x 2048 tokens of a prompt 1820, ten and nine times what the tiles take with bf16.
 template <int DT, int D, int NT>
 struct KvbSplitShape {
     static constexpr int TB = D == 64 ? 64 : D == 128 ? 32 : 16;       // tokens of a block

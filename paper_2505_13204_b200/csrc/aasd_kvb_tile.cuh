@@ -43,7 +43,9 @@ struct KvbTileShape {
     static constexpr int kSoftmax = 8 * kGroups;                           // softmax warps
     static constexpr int kThreads = 32 * (kSoftmax + 8);                   // and 4 unpackers, two issuers (one without work in a single group), loader, walker
     static constexpr int kRaw = D == 256 ? 2 : 5, kValues = D == 256 ? 2 : 4;   // ring depths, in pages
-    // Registers per thread: the softmax warps take what the others give up of the launch's (fewer threads have enough).
+    // Registers per thread: the softmax warps take what the others give up of the launch's (fewer threads have enough).  The compiler
+    // knows the launch's only, and spills: 68 bytes stored and 168 loaded (128 channels, one tile), 20 and 68 (two tiles), 56 and 132, 32 and 104
+    // (64 channels), 12 and 20 (256).
     static constexpr int kLaunchRegs = D == 256 ? 128 : 80, kSoftmaxRegs = D == 256 ? 128 : 96, kOtherRegs = D == 256 ? 128 : 48;
     static_assert(kSoftmax * kSoftmaxRegs + 8 * kOtherRegs <= (kSoftmax + 8) * kLaunchRegs, "the shares add up to the launch's registers");
 };
