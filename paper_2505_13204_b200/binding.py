@@ -835,7 +835,7 @@ class Context:
         """aasd_kvb_write: norms and rotates ``q`` [T, Hq, D] and ``k`` [T, Hkv, D] as ``kv_write`` does and stores the tokens
         that ``kv_plan`` has placed (``kv_len`` and ``positions`` are its outputs) at the end of their sequences' pages.  Token
         rows are packed (``tok_offsets``) or padded (``rows_per_seq``).  Returns a dict with q and, with
-        ``keep_k``, the rotated k (zeros for tokens without a place)."""
+        ``keep_k``, the rotated k (zeros for tokens without a place).  ``outputs`` may be q and k themselves (dense rows)."""
         dev = self.device_index
         _kv_i32(dev, block_table, cached_len, kv_len, positions, tok_offsets)
         T, Hq, D = q.shape
